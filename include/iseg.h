@@ -77,7 +77,7 @@ enum iseg_dev_status {
     ISEG_DEV_DESC = 8          /* a device descriptor field out of range (entry skipped) */
 };
 
-enum iseg_dtype { ISEG_I8 = 0, ISEG_I16 = 1, ISEG_I32 = 2, ISEG_I64 = 3 };
+enum iseg_dtype { ISEG_I8 = 0, ISEG_I16 = 1, ISEG_I32 = 2, ISEG_I64 = 3, ISEG_F32 = 4, ISEG_F16 = 5, ISEG_BF16 = 6 };
 
 enum iseg_qmode { ISEG_Q_UQ = 0, ISEG_Q_SQ = 1 };
 
@@ -565,6 +565,131 @@ size_t iseg_mse_onehot_ws(int64_t n);
 int iseg_mse_onehot(const int8_t* y, const int32_t* y_exp, const uint8_t* labels, int64_t N, int64_t H,
                     int64_t W, int64_t K, int32_t bits, double* loss, int8_t* err, int32_t* err_exp,
                     void* ws, size_t ws_bytes, int32_t* dev_status, hipStream_t stream);
+
+/* ------------------------------------------------------------------------ */
+/* Operators of language models around the integer products                  */
+/* ------------------------------------------------------------------------ */
+/* Matrices here are row-major with a row stride ("ld", in elements, at least
+ * the row's length); rows may start at any address that their element type
+ * allows.  Float tensors are ISEG_F32, ISEG_F16 or ISEG_BF16; statistics, sums
+ * and scales are float32 or wider whatever the tensors' type, and a result is
+ * rounded to its type once.  Bytes between a row's end and the next row are
+ * neither read into a result nor written.  An empty matrix (M = 0) is valid
+ * and its pointers may be NULL. */
+
+/* iseg_layernorm_fwd -- layer normalization of every row of x [M, C]:
+ *   mean = sum x / C, var = sum (x - mean)^2 / C, rstd = 1 / sqrt(var + eps),
+ *   y = (x - mean) rstd gamma + beta.
+ * x and y have x_dtype, gamma and beta [C] p_dtype (NULL: 1 and 0); mean and
+ * rstd [M] float32 (may be NULL) are what the backward needs.  eps > 0 and
+ * finite.  A row with a non-finite value, or whose sum or sum of squares
+ * leaves float32's range, sets ISEG_DEV_NONFINITE (that row's y unspecified).
+ *
+ * iseg_layernorm_bwd -- with g = dy gamma and xhat = (x - mean) rstd:
+ *   dx = rstd (g - sum(g) / C - xhat sum(g xhat) / C),
+ *   dgamma = sum over rows of dy xhat, dbeta = sum over rows of dy.
+ * dy (rows y_ld apart) and dx have x_dtype; dgamma and dbeta [C] p_dtype, each
+ * may be NULL.  Sums have one fixed order: the same call gives the same bits.
+ * With M = 0, dgamma and dbeta are zeros. */
+typedef struct iseg_layernorm_geom {
+    int64_t M, C;
+    int64_t x_ld, y_ld, dx_ld;   /* y_ld: rows of y, or of dy in the backward; dx_ld: backward only */
+    int32_t x_dtype, p_dtype;
+    float eps;                   /* forward only */
+    int32_t reserved;            /* 0 */
+} iseg_layernorm_geom;
+int iseg_layernorm_fwd(const void* x, const void* gamma, const void* beta, const iseg_layernorm_geom* g,
+                       void* y, float* mean, float* rstd, int32_t* dev_status, hipStream_t stream);
+size_t iseg_layernorm_bwd_ws(const iseg_layernorm_geom* g);
+int iseg_layernorm_bwd(const void* dy, const void* x, const void* gamma, const float* mean, const float* rstd,
+                       const iseg_layernorm_geom* g, void* dx, void* dgamma, void* dbeta,
+                       void* ws, size_t ws_bytes, hipStream_t stream);
+
+/* Scale of a row or column whose largest magnitude is t, for codes of at most
+ * L = 2^(bits-1) - 1: ISEG_SCALE_MAX, t / L (Eq. 3's Scale as printed: the
+ * largest element takes the code L); ISEG_SCALE_POW2, the step of Eq. 4 under
+ * the power-of-two Scale of this library, 2^(b+1-bits) with 2^b the smallest
+ * power of two above t.  Rounded to float32, at least 2^-126; 1 if t = 0. */
+enum iseg_scale_mode { ISEG_SCALE_MAX = 0, ISEG_SCALE_POW2 = 1 };
+
+/* iseg_quantize_rows -- a scale for each row (token) of x [M, C]: with
+ * v = x[m, c] mul[c] (mul NULL: 1), scale[m] as above and codes[m, c] =
+ * clamp(floor(v / scale[m] + 1/2), +-L), both decided on the exact product.
+ * x of x_dtype, mul [C] float32, codes int8 (rows codes_ld apart), scale [M]
+ * float32.  bits in [2, 8].  C = 0 gives scales of 1.  A row with a
+ * non-finite v, or whose scale is no finite float32, gets codes 0 and a NaN
+ * scale and sets ISEG_DEV_NONFINITE.
+ *
+ * iseg_quantize_cols -- a scale for each column (channel) of x [M, C], the
+ * codes stored transposed: v = x[m, c] mul[m] (mul [M]), codes[c, m] with rows
+ * codes_ld >= M apart, scale [C].  sums (may be NULL): [C] float32, the plain
+ * column sums of x (without mul), in one fixed order.
+ *
+ * Both are the quantizer of an operand of iseg_matmul_i8: rows for y = x w^T
+ * and for the input's gradient, columns for the weight's gradient. */
+int iseg_quantize_rows(const void* x, int32_t x_dtype, int64_t M, int64_t C, int64_t x_ld, const float* mul,
+                       int32_t bits, int32_t scale_mode, int8_t* codes, int64_t codes_ld, float* scale,
+                       int32_t* dev_status, hipStream_t stream);
+size_t iseg_quantize_cols_ws(int64_t M, int64_t C);
+int iseg_quantize_cols(const void* x, int32_t x_dtype, int64_t M, int64_t C, int64_t x_ld, const float* mul,
+                       int32_t bits, int32_t scale_mode, int8_t* codes, int64_t codes_ld, float* scale,
+                       float* sums, void* ws, size_t ws_bytes, int32_t* dev_status, hipStream_t stream);
+
+/* iseg_transpose_i8 -- out[c, m] = in[m, c] of int8 codes [M, C]: the second
+ * operand of the gradients' products.  in_ld >= C, out_ld >= M. */
+int iseg_transpose_i8(const int8_t* in, int64_t M, int64_t C, int64_t in_ld, int8_t* out, int64_t out_ld,
+                      hipStream_t stream);
+
+/* iseg_matmul_i8 -- out[m, n] = a_scale[m] b_scale[n] sum_k a[m, k] b[n, k] +
+ * bias[n].  a [M, K] and b [N, K] int8 codes, both with the reduction along
+ * the row (b as a 1x1 conv's weights); a_scale [M], b_scale [N], bias [N]
+ * float32, each may be NULL (1, 1, 0).  The sums are exact int32 (K <= 131071,
+ * ISEG_ERR_UNSUPPORTED beyond), rounded to float32, multiplied by a_scale, by
+ * b_scale, added to bias, and rounded to out_dtype (a float type).  K = 0
+ * gives the bias. */
+typedef struct iseg_matmul_geom {
+    int64_t M, N, K;
+    int64_t lda, ldb, ldc;
+    int32_t out_dtype, reserved;
+} iseg_matmul_geom;
+size_t iseg_matmul_i8_ws(const iseg_matmul_geom* g);
+int iseg_matmul_i8(const int8_t* a, const float* a_scale, const int8_t* b, const float* b_scale, const float* bias,
+                   const iseg_matmul_geom* g, void* out, void* ws, size_t ws_bytes, hipStream_t stream);
+
+/* iseg_logprob_fwd -- for every row x of logits [M, V]:
+ *   lse = log sum_v e^x_v; logprob = x_t - lse of the given token t;
+ *   entropy = -sum_v p_v log p_v, p_v = e^(x_v - lse);
+ *   the top_k largest logits, in falling order, equal ones by rising index:
+ *   top_ids, and their log probabilities top_logprob.
+ * tokens [M] of token_dtype (ISEG_I32 or ISEG_I64); a negative token means
+ * none is given: its logprob is 0 and has no gradient.  A token >= V sets
+ * ISEG_DEV_RANGE, its logprob is NaN.  logprob, lse [M] float32; entropy [M]
+ * (may be NULL); top_ids [M, top_k] int32 and top_logprob [M, top_k] float32
+ * (NULL if top_k = 0; top_k <= 64 and <= V).  A logit of -infinity is a banned
+ * token: probability 0, no part of the entropy; a row of nothing else has lse
+ * and every logprob -infinity, entropy 0.  A NaN or +infinity sets
+ * ISEG_DEV_NONFINITE, that row's results are NaN, its ids unspecified within
+ * [0, V).  V in [1, 2^31).
+ *
+ * iseg_logprob_bwd -- gradient of sum_m g_logprob[m] logprob[m] +
+ * g_entropy[m] entropy[m], given the forward's lse and entropy:
+ *   dlogits_v = g_logprob ([v = t] - p_v) - g_entropy p_v (log p_v + entropy).
+ * g_logprob, g_entropy [M] float32, one of them may be NULL (0); entropy may
+ * be NULL with g_entropy.  dlogits has the logits' type, rows out_ld apart.
+ * A row of banned tokens only has gradient 0; a token >= V sets
+ * ISEG_DEV_RANGE and counts as none.  The alternatives carry no gradient. */
+typedef struct iseg_logprob_geom {
+    int64_t M, V;
+    int64_t ld, out_ld;          /* out_ld: backward only */
+    int32_t dtype, token_dtype, top_k, reserved;
+} iseg_logprob_geom;
+size_t iseg_logprob_fwd_ws(const iseg_logprob_geom* g);
+int iseg_logprob_fwd(const void* logits, const void* tokens, const iseg_logprob_geom* g, float* logprob, float* lse,
+                     float* entropy, int32_t* top_ids, float* top_logprob, void* ws, size_t ws_bytes,
+                     int32_t* dev_status, hipStream_t stream);
+int iseg_logprob_bwd(const void* logits, const void* tokens, const float* lse, const float* entropy,
+                     const float* g_logprob, const float* g_entropy, const iseg_logprob_geom* g, void* dlogits,
+                     int32_t* dev_status, hipStream_t stream);
 
 /* ------------------------------------------------------------------------ */
 /* Host-side utilities                                                       */

@@ -270,7 +270,7 @@ static inline size_t align256(size_t v) { return (v + 255) & ~(size_t)255; }
 
 static inline int launch_ok() { return hipGetLastError() == hipSuccess ? ISEG_OK : ISEG_ERR_DEVICE; }
 
-static inline int64_t ceil_div64(int64_t a, int64_t b) { return (a + b - 1) / b; }
+ISEG_HD int64_t ceil_div64(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 // grid size for a grid-stride loop over n items with `per_block` items per block
 static inline unsigned grid_for(int64_t n, int64_t per_block, unsigned cap = 4096)

@@ -1,0 +1,113 @@
+// rowops.h -- device helpers of the row operators (layer norm, row and column
+// quantizers, log probabilities): typed 16-byte vectors of rows that may start
+// at any element, and float reductions over waves and blocks in a fixed order.
+#pragma once
+
+#include "iseg_common.h"
+
+typedef _Float16 f16_t;
+typedef __bf16 bf16_t;
+
+// N elements of a row, loaded and stored as one 16-byte access whatever the
+// row's alignment (gfx950 takes global accesses at any byte address).
+template <typename T>
+struct RowVec {
+    static constexpr int N = 16 / (int)sizeof(T);
+    T v[N];
+};
+
+template <typename T>
+__device__ __forceinline__ RowVec<T> row_load(const T* p)
+{
+    RowVec<T> r;
+    __builtin_memcpy(&r, p, 16);
+    return r;
+}
+
+// the first n (< N) elements; the others are `fill`
+template <typename T>
+__device__ __forceinline__ RowVec<T> row_load_part(const T* p, int n, T fill)
+{
+    RowVec<T> r;
+#pragma unroll
+    for (int i = 0; i < RowVec<T>::N; i++) r.v[i] = fill;
+#pragma unroll
+    for (int i = 0; i < RowVec<T>::N; i++)
+        if (i < n) r.v[i] = p[i];
+    return r;
+}
+
+template <typename T>
+__device__ __forceinline__ void row_store(T* p, const RowVec<T>& r)
+{
+    __builtin_memcpy(p, &r, 16);
+}
+
+template <typename T>
+__device__ __forceinline__ void row_store_part(T* p, const RowVec<T>& r, int n)
+{
+#pragma unroll
+    for (int i = 0; i < RowVec<T>::N; i++)
+        if (i < n) p[i] = r.v[i];
+}
+
+// One step of a wave reduction: the value of another lane by DPP, `old` where
+// the pattern reads past its row (row_shr 1, 2, 4, 8, then the broadcasts of
+// lanes 15 and 31 gather a wave's result in lane 63).
+template <int CTRL>
+__device__ __forceinline__ float dpp_f32(float old, float v)
+{
+    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(__builtin_bit_cast(int, old),
+                                                                 __builtin_bit_cast(int, v), CTRL, 0xf, 0xf, false));
+}
+
+__device__ __forceinline__ float lane63_f32(float v)
+{
+    return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), 63));
+}
+
+// sum over the 64 lanes, the same in every lane
+__device__ __forceinline__ float wave_sum_f32(float v)
+{
+    v += dpp_f32<0x111>(0.f, v);
+    v += dpp_f32<0x112>(0.f, v);
+    v += dpp_f32<0x114>(0.f, v);
+    v += dpp_f32<0x118>(0.f, v);
+    v += dpp_f32<0x142>(0.f, v);
+    v += dpp_f32<0x143>(0.f, v);
+    return lane63_f32(v);
+}
+
+__device__ __forceinline__ float wave_max_f32(float v)
+{
+    v = fmaxf(v, dpp_f32<0x111>(v, v));
+    v = fmaxf(v, dpp_f32<0x112>(v, v));
+    v = fmaxf(v, dpp_f32<0x114>(v, v));
+    v = fmaxf(v, dpp_f32<0x118>(v, v));
+    v = fmaxf(v, dpp_f32<0x142>(v, v));
+    v = fmaxf(v, dpp_f32<0x143>(v, v));
+    return lane63_f32(v);
+}
+
+// sums of two values over the NW waves of a block, the same in every thread.
+// red: 2 NW floats of LDS that no earlier call of this block may still read
+// (callers alternate between two, or have a barrier between).
+template <int NW>
+__device__ __forceinline__ void block_sum2_f32(float& a, float& b, float* red)
+{
+    a = wave_sum_f32(a);
+    b = wave_sum_f32(b);
+    if (NW == 1) return;
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    if (lane == 0) { red[2 * w] = a; red[2 * w + 1] = b; }
+    __syncthreads();
+    a = 0.f;
+    b = 0.f;
+#pragma unroll
+    for (int i = 0; i < NW; i++) { a += red[2 * i]; b += red[2 * i + 1]; }
+}
+
+static inline bool is_float_dtype(int32_t t) { return t == ISEG_F32 || t == ISEG_F16 || t == ISEG_BF16; }
+
+// launches walk their rows in a loop, so the grid may be cut at any count
+constexpr int64_t kRowGridMax = 1 << 20;

@@ -84,6 +84,14 @@ const Entry kEntries[] = {
     ISEG_TAPE_ENTRY(iseg_spatial_sum)
     ISEG_TAPE_ENTRY(iseg_softmax_ce)
     ISEG_TAPE_ENTRY(iseg_mse_onehot)
+    ISEG_TAPE_ENTRY(iseg_layernorm_fwd)
+    ISEG_TAPE_ENTRY(iseg_layernorm_bwd)
+    ISEG_TAPE_ENTRY(iseg_quantize_rows)
+    ISEG_TAPE_ENTRY(iseg_quantize_cols)
+    ISEG_TAPE_ENTRY(iseg_transpose_i8)
+    ISEG_TAPE_ENTRY(iseg_matmul_i8)
+    ISEG_TAPE_ENTRY(iseg_logprob_fwd)
+    ISEG_TAPE_ENTRY(iseg_logprob_bwd)
     ISEG_TAPE_ENTRY(iseg_profile_arm)
     ISEG_TAPE_ENTRY(iseg_status_clear)
     ISEG_TAPE_ENTRY(iseg_check_codes)

@@ -10,6 +10,8 @@ A quantized tensor is a pair (codes, exp): integer codes and a 1-element int32
 device tensor holding the power-of-two exponent (value = code * 2^exp).
 """
 import ctypes as C
+import functools
+import math
 import os
 
 import torch
@@ -19,7 +21,8 @@ LIB_PATH = os.path.join(_HERE, "lib", "libiseg.so")
 
 ISEG_OK, ISEG_ERR_ARG, ISEG_ERR_SHAPE, ISEG_ERR_UNSUPPORTED, ISEG_ERR_WORKSPACE, ISEG_ERR_DEVICE = range(6)
 ISEG_DEV_RANGE, ISEG_DEV_NONFINITE, ISEG_DEV_DESC = 1, 4, 8
-ISEG_I8, ISEG_I16, ISEG_I32, ISEG_I64 = range(4)
+ISEG_I8, ISEG_I16, ISEG_I32, ISEG_I64, ISEG_F32, ISEG_F16, ISEG_BF16 = range(7)
+ISEG_SCALE_MAX, ISEG_SCALE_POW2 = 0, 1
 ISEG_Q_UQ, ISEG_Q_SQ = 0, 1
 ISEG_OUT_Q8, ISEG_OUT_RAW = 0, 1
 ISEG_G_KEEP, ISEG_G_DROP, ISEG_G_RAW = 0, 1, 2
@@ -64,6 +67,21 @@ class BnCfg(C.Structure):
 
 BN_DEFAULT = dict(k_mu=16, k_sigma=16, k_xhat=16, k_gamma=8, k_beta=8, k_A=8, k_E1=8, k_E2=16,
                   eps_code=0, relu=1)
+
+class LayernormGeom(C.Structure):
+    _fields_ = [(n, C.c_int64) for n in ("M", "C", "x_ld", "y_ld", "dx_ld")] + \
+               [("x_dtype", C.c_int32), ("p_dtype", C.c_int32), ("eps", C.c_float), ("reserved", C.c_int32)]
+
+
+class MatmulGeom(C.Structure):
+    _fields_ = [(n, C.c_int64) for n in ("M", "N", "K", "lda", "ldb", "ldc")] + \
+               [("out_dtype", C.c_int32), ("reserved", C.c_int32)]
+
+
+class LogprobGeom(C.Structure):
+    _fields_ = [(n, C.c_int64) for n in ("M", "V", "ld", "out_ld")] + \
+               [(n, C.c_int32) for n in ("dtype", "token_dtype", "top_k", "reserved")]
+
 
 _lib = None
 _P, _I64, _I32, _U64, _U32, _SZ = C.c_void_p, C.c_int64, C.c_int32, C.c_uint64, C.c_uint32, C.c_size_t
@@ -127,6 +145,19 @@ _SIGS = {
     "iseg_mse_onehot_ws": ([_I64], _SZ),
     "iseg_mse_onehot": ([_P, _P, _P, _I64, _I64, _I64, _I64, _I32, _P, _P, _P, _P, _SZ, _P, _P], C.c_int),
     "iseg_update_multi": ([_P, _I32, _I32, _U64, _U32, _I32, _I32, _I32, _P, _P], C.c_int),
+    "iseg_layernorm_fwd": ([_P, _P, _P, _P, _P, _P, _P, _P, _P], C.c_int),
+    "iseg_layernorm_bwd_ws": ([_P], _SZ),
+    "iseg_layernorm_bwd": ([_P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _SZ, _P], C.c_int),
+    "iseg_quantize_rows": ([_P, _I32, _I64, _I64, _I64, _P, _I32, _I32, _P, _I64, _P, _P, _P], C.c_int),
+    "iseg_quantize_cols_ws": ([_I64, _I64], _SZ),
+    "iseg_quantize_cols": ([_P, _I32, _I64, _I64, _I64, _P, _I32, _I32, _P, _I64, _P, _P, _P, _SZ, _P, _P],
+                           C.c_int),
+    "iseg_transpose_i8": ([_P, _I64, _I64, _I64, _P, _I64, _P], C.c_int),
+    "iseg_matmul_i8_ws": ([_P], _SZ),
+    "iseg_matmul_i8": ([_P, _P, _P, _P, _P, _P, _P, _P, _SZ, _P], C.c_int),
+    "iseg_logprob_fwd_ws": ([_P], _SZ),
+    "iseg_logprob_fwd": ([_P, _P, _P, _P, _P, _P, _P, _P, _P, _SZ, _P, _P], C.c_int),
+    "iseg_logprob_bwd": ([_P, _P, _P, _P, _P, _P, _P, _P, _P, _P], C.c_int),
     "iseg_philox4x32_10": ([_P, _P, _P], None),
     "iseg_profile_arm": ([_I32, _P, _P], C.c_int),
     "iseg_conv_last_plan": ([], C.c_char_p),
@@ -452,6 +483,54 @@ def mse_onehot(y, y_exp, labels, bits=8, status=None):
     ws = workspace(y.device).get(lib().iseg_mse_onehot_ws(y.numel()))
     iseg_mse_onehot(y, y_exp, labels, bits, loss, err, e, ws, status)
     return loss, err, e
+
+
+def iseg_layernorm_fwd(x, gamma, beta, geom, y, mean, rstd, status=None):
+    rc = lib().iseg_layernorm_fwd(_ptr(x), _ptr(gamma), _ptr(beta), C.byref(geom), _ptr(y), _ptr(mean),
+                                  _ptr(rstd), _ptr(status), _stream())
+    _check(rc, "iseg_layernorm_fwd")
+
+
+def iseg_layernorm_bwd(dy, x, gamma, mean, rstd, geom, dx, dgamma, dbeta, ws):
+    rc = lib().iseg_layernorm_bwd(_ptr(dy), _ptr(x), _ptr(gamma), _ptr(mean), _ptr(rstd), C.byref(geom), _ptr(dx),
+                                  _ptr(dgamma), _ptr(dbeta), *_ws_tuple(ws), _stream())
+    _check(rc, "iseg_layernorm_bwd")
+
+
+def iseg_quantize_rows(x, x_dtype, M, Cc, x_ld, mul, bits, scale_mode, codes, codes_ld, scale, status=None):
+    rc = lib().iseg_quantize_rows(_ptr(x), x_dtype, M, Cc, x_ld, _ptr(mul), bits, scale_mode, _ptr(codes),
+                                  codes_ld, _ptr(scale), _ptr(status), _stream())
+    _check(rc, "iseg_quantize_rows")
+
+
+def iseg_quantize_cols(x, x_dtype, M, Cc, x_ld, mul, bits, scale_mode, codes, codes_ld, scale, sums, ws,
+                       status=None):
+    rc = lib().iseg_quantize_cols(_ptr(x), x_dtype, M, Cc, x_ld, _ptr(mul), bits, scale_mode, _ptr(codes),
+                                  codes_ld, _ptr(scale), _ptr(sums), *_ws_tuple(ws), _ptr(status), _stream())
+    _check(rc, "iseg_quantize_cols")
+
+
+def iseg_transpose_i8(inp, M, Cc, in_ld, out, out_ld):
+    rc = lib().iseg_transpose_i8(_ptr(inp), M, Cc, in_ld, _ptr(out), out_ld, _stream())
+    _check(rc, "iseg_transpose_i8")
+
+
+def iseg_matmul_i8(a, a_scale, b, b_scale, bias, geom, out, ws):
+    rc = lib().iseg_matmul_i8(_ptr(a), _ptr(a_scale), _ptr(b), _ptr(b_scale), _ptr(bias), C.byref(geom), _ptr(out),
+                              *_ws_tuple(ws), _stream())
+    _check(rc, "iseg_matmul_i8")
+
+
+def iseg_logprob_fwd(logits, tokens, geom, logprob, lse, entropy, top_ids, top_logprob, ws, status=None):
+    rc = lib().iseg_logprob_fwd(_ptr(logits), _ptr(tokens), C.byref(geom), _ptr(logprob), _ptr(lse), _ptr(entropy),
+                                _ptr(top_ids), _ptr(top_logprob), *_ws_tuple(ws), _ptr(status), _stream())
+    _check(rc, "iseg_logprob_fwd")
+
+
+def iseg_logprob_bwd(logits, tokens, lse, entropy, g_logprob, g_entropy, geom, dlogits, status=None):
+    rc = lib().iseg_logprob_bwd(_ptr(logits), _ptr(tokens), _ptr(lse), _ptr(entropy), _ptr(g_logprob),
+                                _ptr(g_entropy), C.byref(geom), _ptr(dlogits), _ptr(status), _stream())
+    _check(rc, "iseg_logprob_bwd")
 
 
 def iseg_philox4x32_10(ctr, key):
@@ -1153,3 +1232,331 @@ def update_table(entries, device):
         d.k_w = e.get("k_w", 0)
     raw = torch.frombuffer(bytearray(bytes(host)), dtype=torch.uint8)
     return raw.to(device), n
+
+
+# --------------------------------------------------------------------------
+# operators of language models: layer norm, quantizers per row and column,
+# int8 products with a scale for each row of either operand, log probabilities
+# --------------------------------------------------------------------------
+# Matrices are tensors whose last dimension is the row; leading dimensions are
+# folded.  Rows may be strided (a slice of a wider buffer); any other layout is
+# copied first.  Calls run on the tensors' own device and its current stream.
+_FLOATS = {torch.float32: ISEG_F32, torch.float16: ISEG_F16, torch.bfloat16: ISEG_BF16}
+
+
+def _on_device(f):
+    """Run f with its first tensor's device current (the library launches on
+    the current device)."""
+    @functools.wraps(f)
+    def call(x, *args, **kw):
+        if not x.is_cuda or x.device.index == _raw_device():
+            return f(x, *args, **kw)
+        with torch.cuda.device(x.device):
+            return f(x, *args, **kw)
+    return call
+
+
+def _float_code(t, what):
+    c = _FLOATS.get(t.dtype if isinstance(t, torch.Tensor) else t)
+    if c is None:
+        raise ValueError(f"{what}: float32, float16 or bfloat16 expected")
+    return c
+
+
+def _rows(t, what):
+    """(tensor, rows, columns, row stride) of a matrix with dense rows."""
+    if t.dim() < 1:
+        raise ValueError(f"{what}: at least one dimension expected")
+    Cc = t.shape[-1]
+    if t.dim() != 2:
+        p = t.data_ptr()
+        t = t.reshape(math.prod(t.shape[:-1]), Cc)
+        if _REC is not None and t.data_ptr() != p:
+            raise IsegError(f"{what}: a recorded call needs dense rows")
+    M = t.shape[0]
+    ld = t.stride(0) if M > 1 else max(Cc, 1)
+    if (Cc > 1 and t.stride(1) != 1) or ld < Cc:
+        if _REC is not None:
+            raise IsegError(f"{what}: a recorded call needs dense rows")
+        t = t.contiguous()
+        ld = max(Cc, 1)
+    return t, M, Cc, ld
+
+
+def _vec(t, n, dtype, device, what):
+    """A dense vector of n elements on `device`, or None."""
+    if t is None:
+        return None
+    if t.dtype != dtype or t.numel() != n or t.device != device:
+        raise ValueError(f"{what}: {n} elements of {dtype} on {device} expected")
+    if t.dim() == 1 and (n <= 1 or t.stride(0) == 1):
+        return t
+    if _REC is not None and not t.is_contiguous():
+        raise IsegError(f"{what}: a recorded call needs a dense vector")
+    return t.contiguous()
+
+
+def _gpu(*ts):
+    for t in ts:
+        if t is not None and not t.is_cuda:
+            raise ValueError("GPU tensors expected")
+        if t is not None and t.device != ts[0].device:
+            raise ValueError("tensors on one device expected")
+
+
+def _scratch(device, nbytes):
+    """Workspace of a call: the stream's, or, under graph capture, memory of
+    the graph's own (a graph outlives the stream's workspace, and two graphs
+    may replay at once)."""
+    if torch.cuda.is_current_stream_capturing():
+        return torch.empty(max(nbytes, 256), dtype=torch.uint8, device=device)
+    return workspace(device).get(nbytes)
+
+
+@functools.lru_cache(maxsize=256)
+def _layernorm_geom(M, Cc, x_ld, y_ld, dx_ld, x_dtype, p_dtype, eps):
+    return LayernormGeom(M, Cc, x_ld, y_ld, dx_ld, x_dtype, p_dtype, eps, 0)
+
+
+@functools.lru_cache(maxsize=256)
+def _matmul_geom(M, N, K, lda, ldb, ldc, out_dtype):
+    g = MatmulGeom(M, N, K, lda, ldb, ldc, out_dtype, 0)
+    return g, lib().iseg_matmul_i8_ws(C.byref(g))
+
+
+@functools.lru_cache(maxsize=256)
+def _logprob_geom(M, V, ld, out_ld, dtype, token_dtype, top_k):
+    g = LogprobGeom(M, V, ld, out_ld, dtype, token_dtype, top_k, 0)
+    return g, lib().iseg_logprob_fwd_ws(C.byref(g))
+
+
+@_on_device
+def layernorm_fwd(x, gamma=None, beta=None, eps=1e-5, status=None):
+    """Layer norm over the last dimension: (y, mean, rstd), the statistics
+    float32 with one element per row.  gamma and beta of one float type."""
+    xd = _float_code(x, "x")
+    xr, M, Cc, ld = _rows(x, "x")
+    if Cc < 1:
+        raise ValueError("x: empty rows")
+    if not (eps > 0 and math.isfinite(eps)):
+        raise ValueError("eps: positive and finite expected")
+    p = gamma if gamma is not None else beta
+    pd = _float_code(p, "gamma, beta") if p is not None else ISEG_F32
+    gamma = _vec(gamma, Cc, p.dtype if p is not None else None, x.device, "gamma")
+    beta = _vec(beta, Cc, p.dtype if p is not None else None, x.device, "beta")
+    _gpu(x, status)
+    y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    stats = torch.empty((2,) + x.shape[:-1], dtype=torch.float32, device=x.device)
+    mean, rstd = stats[0], stats[1]
+    iseg_layernorm_fwd(xr, gamma, beta, _layernorm_geom(M, Cc, ld, Cc, Cc, xd, pd, eps), y, mean, rstd, status)
+    return y, mean, rstd
+
+
+@_on_device
+def layernorm_bwd(dy, x, gamma, mean, rstd, want_params=True):
+    """(dx, dgamma, dbeta) of layernorm_fwd; dgamma and dbeta take gamma's type
+    (float32 without gamma) and are None without want_params."""
+    xd = _float_code(x, "x")
+    if dy.dtype != x.dtype or dy.shape != x.shape:
+        raise ValueError("dy: x's shape and type expected")
+    xr, M, Cc, ld = _rows(x, "x")
+    dr, _, _, dld = _rows(dy, "dy")
+    if Cc < 1:
+        raise ValueError("x: empty rows")
+    pdt = gamma.dtype if gamma is not None else torch.float32
+    pd = _float_code(pdt, "gamma")
+    gamma = _vec(gamma, Cc, pdt, x.device, "gamma")
+    mean = _vec(mean, M, torch.float32, x.device, "mean")
+    rstd = _vec(rstd, M, torch.float32, x.device, "rstd")
+    _gpu(x, dy)
+    dx = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    dgamma = torch.empty(Cc, dtype=pdt, device=x.device) if want_params else None
+    dbeta = torch.empty(Cc, dtype=pdt, device=x.device) if want_params else None
+    g = _layernorm_geom(M, Cc, ld, dld, Cc, xd, pd, 1.0)
+    iseg_layernorm_bwd(dr, xr, gamma, mean, rstd, g, dx, dgamma, dbeta,
+                       _scratch(x.device, lib().iseg_layernorm_bwd_ws(C.byref(g))))
+    return dx, dgamma, dbeta
+
+
+def _codes_matrix(rows, cols, device):
+    """int8 [rows, cols] in rows of a multiple of 16 bytes (the alignment that
+    the products' wide loads take)."""
+    return torch.empty((rows, (cols + 15) // 16 * 16), dtype=torch.int8, device=device)[:, :cols]
+
+
+def _quant_args(bits, scale_mode):
+    if not 2 <= bits <= 8:
+        raise ValueError("bits: 2 to 8 expected")
+    if scale_mode not in (ISEG_SCALE_MAX, ISEG_SCALE_POW2):
+        raise ValueError("scale_mode: ISEG_SCALE_MAX or ISEG_SCALE_POW2 expected")
+
+
+@_on_device
+def quantize_rows(x, bits=8, scale_mode=ISEG_SCALE_MAX, mul=None, status=None):
+    """Codes and a scale for each row of x [..., C] (times mul [C]): int8
+    [M, C] with M the folded rows, and float32 [M]."""
+    xd = _float_code(x, "x")
+    _quant_args(bits, scale_mode)
+    xr, M, Cc, ld = _rows(x, "x")
+    mul = _vec(mul, Cc, torch.float32, x.device, "mul")
+    _gpu(x, status)
+    codes = _codes_matrix(M, Cc, x.device)
+    scale = torch.empty(M, dtype=torch.float32, device=x.device)
+    iseg_quantize_rows(xr, xd, M, Cc, ld, mul, bits, scale_mode, codes, codes.stride(0), scale, status)
+    return codes, scale
+
+
+@_on_device
+def quantize_cols(x, bits=8, scale_mode=ISEG_SCALE_MAX, mul=None, want_sums=False, status=None):
+    """Codes and a scale for each column of x [..., C] (times mul [M], one for
+    each folded row): int8 [C, M], transposed, and float32 [C]; with want_sums
+    also the plain column sums of x, float32 [C] (None without)."""
+    xd = _float_code(x, "x")
+    _quant_args(bits, scale_mode)
+    xr, M, Cc, ld = _rows(x, "x")
+    mul = _vec(mul, M, torch.float32, x.device, "mul")
+    _gpu(x, status)
+    codes = _codes_matrix(Cc, M, x.device)
+    scale = torch.empty(Cc, dtype=torch.float32, device=x.device)
+    sums = torch.empty(Cc, dtype=torch.float32, device=x.device) if want_sums else None
+    iseg_quantize_cols(xr, xd, M, Cc, ld, mul, bits, scale_mode, codes, codes.stride(0), scale, sums,
+                       _scratch(x.device, lib().iseg_quantize_cols_ws(M, Cc)), status)
+    return codes, scale, sums
+
+
+def _code_rows(t, what):
+    if t.dtype != torch.int8 or t.dim() != 2:
+        raise ValueError(f"{what}: an int8 matrix expected")
+    return _rows(t, what)
+
+
+@_on_device
+def transpose_i8(codes):
+    """int8 [C, M] from int8 [M, C]."""
+    cr, M, Cc, ld = _code_rows(codes, "codes")
+    _gpu(codes)
+    out = _codes_matrix(Cc, M, codes.device)
+    iseg_transpose_i8(cr, M, Cc, ld, out, out.stride(0))
+    return out
+
+
+@_on_device
+def matmul_i8(a, b, a_scale=None, b_scale=None, bias=None, out_dtype=torch.float32):
+    """a_scale[m] b_scale[n] sum_k a[m, k] b[n, k] + bias[n] of int8 matrices
+    a [M, K] and b [N, K]: [M, N] of out_dtype."""
+    od = _float_code(out_dtype, "out_dtype")
+    ar, M, K, lda = _code_rows(a, "a")
+    br, N, Kb, ldb = _code_rows(b, "b")
+    if K != Kb:
+        raise ValueError("a and b: rows of one length expected")
+    if K > 131071:
+        raise ValueError("a and b: rows of at most 131071 codes expected")
+    a_scale = _vec(a_scale, M, torch.float32, a.device, "a_scale")
+    b_scale = _vec(b_scale, N, torch.float32, a.device, "b_scale")
+    bias = _vec(bias, N, torch.float32, a.device, "bias")
+    _gpu(a, b)
+    out = torch.empty((M, N), dtype=out_dtype, device=a.device)
+    g, wsb = _matmul_geom(M, N, K, lda, ldb, max(N, 1), od)
+    iseg_matmul_i8(ar, a_scale, br, b_scale, bias, g, out, _scratch(a.device, wsb))
+    return out
+
+
+@_on_device
+def linear_i8_fwd(x, w, w_scale=None, bias=None, bits=8, scale_mode=ISEG_SCALE_MAX, out_dtype=None, status=None):
+    """A linear layer in integers: x [..., K] quantized per row, then the
+    product with the weight codes w [N, K].  Returns (y [..., N] of out_dtype,
+    by default x's, the codes and scales of x, which the backward needs)."""
+    if x.dim() < 1 or w.dim() != 2 or x.shape[-1] != w.shape[1]:
+        raise ValueError("x and w: rows of one length expected")
+    codes, scale = quantize_rows(x, bits, scale_mode, None, status)
+    y = matmul_i8(codes, w, scale, w_scale, bias, x.dtype if out_dtype is None else out_dtype)
+    return y.view(x.shape[:-1] + (w.shape[0],)), codes, scale
+
+
+@_on_device
+def linear_i8_bwd(dy, a, a_scale, w, w_scale=None, w_t=None, bits=8, scale_mode=ISEG_SCALE_MAX, out_dtype=None,
+                  want_input=True, want_weight=True, want_bias=False, status=None):
+    """Backward of linear_i8_fwd with straight-through quantizers, its products
+    in integers too: (dx, dw, dbias), None where not wanted.
+      dx = Q_rows(dy w_scale) w, dw = Q_cols(dy a_scale)^T a, dbias = sum dy
+    a, a_scale: the forward's codes and scales; w_t: the transposed weight
+    codes (transpose_i8), which a program keeps between updates.  dx [M, K] and
+    dw [N, K] have out_dtype (by default dy's), dbias is float32."""
+    _float_code(dy, "dy")
+    if a.dim() != 2 or w.dim() != 2 or dy.dim() < 1 or a.shape[1] != w.shape[1] or dy.shape[-1] != w.shape[0]:
+        raise ValueError("dy [..., N], a [M, K] and w [N, K] expected")
+    dr, M, N, _ = _rows(dy, "dy")
+    if M != a.shape[0]:
+        raise ValueError("dy and a: as many rows expected")
+    if w_t is not None and tuple(w_t.shape) != (w.shape[1], w.shape[0]):
+        raise ValueError("w_t: the transposed w expected")
+    out_dtype = dy.dtype if out_dtype is None else out_dtype
+    dx = dw = dbias = None
+    if want_input:
+        q, s = quantize_rows(dr, bits, scale_mode, w_scale, status)
+        dx = matmul_i8(q, transpose_i8(w) if w_t is None else w_t, s, None, None, out_dtype)
+    if want_weight or want_bias:
+        q, s, dbias = quantize_cols(dr, bits, scale_mode, a_scale, want_bias, status)
+        if want_weight:
+            dw = matmul_i8(q, transpose_i8(a), s, None, None, out_dtype)
+    return dx, dw, dbias
+
+
+def _tokens(tokens, logits):
+    if tokens.dtype not in (torch.int32, torch.int64) or tokens.shape != logits.shape[:-1]:
+        raise ValueError("tokens: int32 or int64 of the logits' leading shape expected")
+    if tokens.device != logits.device:
+        raise ValueError("tokens: on the logits' device expected")
+    if not tokens.is_contiguous():
+        if _REC is not None:
+            raise IsegError("tokens: a recorded call needs a dense tensor")
+        tokens = tokens.contiguous()
+    return tokens, ISEG_I32 if tokens.dtype == torch.int32 else ISEG_I64
+
+
+@_on_device
+def logprob_fwd(logits, tokens, top_k=0, want_entropy=True, status=None):
+    """Log probabilities of the given tokens under logits [..., V]: (logprob,
+    lse, entropy, top_ids, top_logprob), float32 and int32, the last two
+    [..., top_k] (None if top_k = 0; entropy None without want_entropy)."""
+    dt = _float_code(logits, "logits")
+    lr, M, V, ld = _rows(logits, "logits")
+    tokens, td = _tokens(tokens, logits)
+    if V < 1:
+        raise ValueError("logits: empty rows")
+    if not 0 <= top_k <= min(64, V):
+        raise ValueError("top_k: 0 to 64, and at most the logits of a row expected")
+    _gpu(logits, tokens, status)
+    shape, dev = logits.shape[:-1], logits.device
+    g, wsb = _logprob_geom(M, V, ld, V, dt, td, top_k)
+    out = torch.empty((3 if want_entropy else 2,) + shape, dtype=torch.float32, device=dev)
+    logprob, lse, entropy = out[0], out[1], out[2] if want_entropy else None
+    ids = torch.empty(shape + (top_k,), dtype=torch.int32, device=dev) if top_k else None
+    tlp = torch.empty(shape + (top_k,), dtype=torch.float32, device=dev) if top_k else None
+    iseg_logprob_fwd(lr, tokens, g, logprob, lse, entropy, ids, tlp, _scratch(dev, wsb), status)
+    return logprob, lse, entropy, ids, tlp
+
+
+@_on_device
+def logprob_bwd(logits, tokens, lse, entropy, g_logprob=None, g_entropy=None, status=None):
+    """Gradient w.r.t. the logits of sum(g_logprob logprob) + sum(g_entropy
+    entropy), given logprob_fwd's lse and entropy; one of the gradients may be
+    None."""
+    dt = _float_code(logits, "logits")
+    lr, M, V, ld = _rows(logits, "logits")
+    tokens, td = _tokens(tokens, logits)
+    if V < 1:
+        raise ValueError("logits: empty rows")
+    if g_logprob is None and g_entropy is None:
+        raise ValueError("g_logprob or g_entropy expected")
+    if lse is None or (g_entropy is not None and entropy is None):
+        raise ValueError("the forward's lse and, with g_entropy, its entropy expected")
+    lse = _vec(lse, M, torch.float32, logits.device, "lse")
+    entropy = _vec(entropy, M, torch.float32, logits.device, "entropy")
+    g_logprob = _vec(g_logprob, M, torch.float32, logits.device, "g_logprob")
+    g_entropy = _vec(g_entropy, M, torch.float32, logits.device, "g_entropy")
+    _gpu(logits, tokens, status)
+    dx = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
+    g, _ = _logprob_geom(M, V, ld, V, dt, td, 0)
+    iseg_logprob_bwd(lr, tokens, lse, entropy, g_logprob, g_entropy, g, dx, status)
+    return dx

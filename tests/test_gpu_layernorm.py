@@ -1,0 +1,174 @@
+"""Layer norm forward and backward against the formulas in 64 bits: row
+lengths on both sides of every register width, strides, types, offsets, one
+row and many, and the refusals."""
+import numpy as np
+import pytest
+import torch
+
+from lm_util import DEV, DT, HALF, TINY, U, normal, strided, within
+
+pytestmark = pytest.mark.gpu
+
+# (rows, columns, type of x, type of gamma, row stride - columns)
+CASES = [
+    (1, 1, "fp32", "fp32", 0), (3, 2, "bf16", "bf16", 0), (5, 7, "fp16", "fp16", 1), (2, 64, "bf16", "fp32", 0),
+    (300, 100, "fp32", "fp32", 3), (1, 2048, "bf16", "bf16", 0), (33, 2049, "bf16", "fp32", 0), (17, 1537, "fp32", "bf16", 0),
+    (1025, 513, "fp16", "fp32", 7), (9, 4096, "bf16", "bf16", 8), (4, 4100, "fp32", "fp32", 0), (3, 8192, "bf16", "fp16", 0),
+    (5, 8200, "fp16", "fp16", 0), (2, 16384, "fp32", "fp32", 0), (2, 16389, "bf16", "bf16", 0), (3, 32779, "bf16", "bf16", 2),
+    (2, 16391, "fp32", "fp32", 0), (1, 70001, "fp16", "fp32", 0), (2100, 40, "bf16", "bf16", 0),
+]
+
+
+def _inputs(case, offset=0.5):
+    M, C, t, p, gap = case
+    x = (normal(M + C, M, C) * (0.5 + normal(C, M, 1).abs()) + offset).to(DT[t])
+    return x, (1 + 0.2 * normal(1, C)).to(DT[p]), (0.3 * normal(2, C)).to(DT[p]), normal(3 + C, M, C).to(DT[t])
+
+
+def _stats(x, eps):
+    d = x.double()
+    mean = d.mean(1)
+    var = ((d - mean[:, None]) ** 2).mean(1)
+    return mean, 1 / torch.sqrt(var + float(np.float32(eps)))
+
+
+# A thread adds at most 69 terms in sequence, then 6 + 16 more; statistics are
+# therefore within 100 half-steps of the mean magnitude of their terms.
+K = 100
+
+
+def _check_fwd(iseg, x, xg, gamma, beta, t, eps):
+    y, mean, rstd = iseg.layernorm_fwd(xg, None if gamma is None else gamma.to(DEV),
+                                       None if beta is None else beta.to(DEV), eps=eps)
+    m64, r64 = _stats(x, eps)
+    d = x.double() - m64[:, None]
+    spread = d.abs().mean(1)
+    within(mean, m64, U * m64.abs() + K * U * spread, "mean")
+    # the variance within K + 4, its root half of that, the root and quotient 2 more
+    within(rstd, r64, r64 * (K / 2 + 6) * U, "rstd")
+    g = gamma.double() if gamma is not None else torch.ones(x.shape[1], dtype=torch.float64)
+    b = beta.double() if beta is not None else torch.zeros(x.shape[1], dtype=torch.float64)
+    xh = d * r64[:, None]
+    want = xh * g + b
+    tol = g.abs() * U * ((K / 2 + 10) * xh.abs() + (K + 2) * (spread * r64)[:, None]) + 2 * U * want.abs()
+    within(y, want, tol * (1 + HALF[t]) + HALF[t] * want.abs() + TINY[t], "y")
+
+
+@pytest.mark.parametrize("case", CASES, ids=str)
+def test_forward(case):
+    from paper_2011_14504_amd import iseg
+    print(f"[layernorm fwd] {case}", flush=True)
+    x, gamma, beta, _ = _inputs(case)
+    xg = strided(x, case[1] + case[4], float("nan"))
+    _check_fwd(iseg, x, xg, gamma, beta, case[2], 1e-5)
+    _check_fwd(iseg, x, xg, gamma, None, case[2], 1e-6)
+    _check_fwd(iseg, x, xg, None, None, case[2], 0.25)
+
+
+def test_forward_rows_with_an_offset_far_above_their_spread():
+    from paper_2011_14504_amd import iseg
+    x = (normal(5, 6, 3000) * 0.01 + torch.tensor([0., 1., 30., -900., 4000., 1e4])[:, None]).float()
+    _check_fwd(iseg, x, x.to(DEV), None, None, "fp32", 1e-12)
+    c = torch.full((2, 129), 3.25)                       # no spread at all
+    y, mean, rstd = iseg.layernorm_fwd(c.to(DEV), eps=1e-5)
+    assert torch.equal(y.cpu(), torch.zeros(2, 129)) and torch.equal(mean.cpu(), torch.full((2,), 3.25))
+
+
+@pytest.mark.parametrize("case", CASES, ids=str)
+def test_backward(case):
+    from paper_2011_14504_amd import iseg
+    print(f"[layernorm bwd] {case}", flush=True)
+    M, C, t, p, gap = case
+    x, gamma, _, dy = _inputs(case)
+    m64, r64 = _stats(x, 1e-5)
+    mean, rstd = m64.float(), r64.float()
+    xg, dg = strided(x, C + gap, float("nan")), strided(dy, C + 2 * gap, float("nan"))
+    for gm in (gamma, None):
+        dx, dgam, dbet = iseg.layernorm_bwd(dg, xg, None if gm is None else gm.to(DEV), mean.to(DEV), rstd.to(DEV))
+        r = rstd.double()[:, None]
+        xh = (x.double() - mean.double()[:, None]) * r
+        g = dy.double() * (gm.double() if gm is not None else 1.0)
+        s1, s2 = g.mean(1, keepdim=True), (g * xh).mean(1, keepdim=True)
+        want = r * (g - s1 - xh * s2)
+        a1, a2 = g.abs().mean(1, keepdim=True), (g * xh).abs().mean(1, keepdim=True)
+        tol = r * U * (6 * g.abs() + (K + 6) * a1 + xh.abs() * (K + 10) * a2)
+        within(dx, want, tol + HALF[t] * (want.abs() + tol) + TINY[t], "dx")
+        # rows per block, then partials per wave: at most 5 + 128 + 10 additions in sequence
+        prod = dy.double() * xh
+        ht, tt = (HALF[p], TINY[p]) if gm is not None else (HALF["fp32"], TINY["fp32"])
+        for got, terms, what in ((dgam, prod, "dgamma"), (dbet, dy.double(), "dbeta")):
+            w, e = terms.sum(0), 150 * U * terms.abs().sum(0)
+            within(got, w, e + ht * (w.abs() + e) + tt, what)
+            assert got.dtype == (DT[p] if gm is not None else torch.float32)
+    again = iseg.layernorm_bwd(dg, xg, None, mean.to(DEV), rstd.to(DEV))
+    assert torch.equal(again[0], dx) and torch.equal(again[1], dgam) and torch.equal(again[2], dbet)
+
+
+def test_backward_against_differences():
+    """dx, dgamma, dbeta against central differences of the formula in 64 bits."""
+    from paper_2011_14504_amd import iseg
+    x, gamma, beta, w = normal(1, 3, 37).float(), normal(2, 37).float(), normal(3, 37).float(), normal(4, 3, 37).float()
+
+    def loss(x, gamma, beta):
+        m, r = _stats(x, 1e-5)
+        return float((((x - m[:, None]) * r[:, None] * gamma + beta) * w.double()).sum())
+
+    y, mean, rstd = iseg.layernorm_fwd(x.to(DEV), gamma.to(DEV), beta.to(DEV), eps=1e-5)
+    got = iseg.layernorm_bwd(w.to(DEV), x.to(DEV), gamma.to(DEV), mean, rstd)
+    args = [x.double(), gamma.double(), beta.double()]
+    for k, h in ((0, 1e-5), (1, 1e-4), (2, 1e-4)):
+        flat = args[k].reshape(-1)
+        for i in range(0, flat.numel(), 7):
+            keep = float(flat[i])
+            flat[i] = keep + h
+            up = loss(*args)
+            flat[i] = keep - h
+            dn = loss(*args)
+            flat[i] = keep
+            # the difference's own error is h^2 times a third derivative of order 10
+            assert abs((up - dn) / (2 * h) - float(got[k].reshape(-1)[i])) < 2e-5, (k, i)
+
+
+def test_rows_between_and_behind_stay_as_they_were():
+    from paper_2011_14504_amd import iseg
+    x = normal(9, 5, 100).to(torch.bfloat16).to(DEV)
+    y = torch.full((7, 111), 5.0, dtype=torch.bfloat16, device=DEV)
+    g = iseg.LayernormGeom(5, 100, 100, 111, 111, iseg.ISEG_BF16, iseg.ISEG_F32, 1e-5, 0)
+    iseg.iseg_layernorm_fwd(x, None, None, g, y, None, None)
+    ref = iseg.layernorm_fwd(x)[0]
+    assert torch.equal(y[:5, :100], ref)
+    assert bool((y[5:] == 5).all()) and bool((y[:, 100:] == 5).all())
+
+
+def test_empty_and_status():
+    from paper_2011_14504_amd import iseg
+    st = torch.zeros(1, dtype=torch.int32, device=DEV)
+    y, mean, rstd = iseg.layernorm_fwd(torch.empty(0, 8, device=DEV), status=st)
+    assert y.shape == (0, 8) and mean.shape == (0,)
+    dx, dg, db = iseg.layernorm_bwd(torch.empty(0, 8, device=DEV), torch.empty(0, 8, device=DEV),
+                                    torch.ones(8, device=DEV), mean, rstd)
+    assert dx.shape == (0, 8) and torch.equal(dg.cpu(), torch.zeros(8)) and torch.equal(db.cpu(), torch.zeros(8))
+    iseg.layernorm_fwd(normal(1, 4, 50).float().to(DEV), status=st)
+    assert iseg.iseg_status_read(st) == 0
+    for bad in (float("nan"), float("inf"), 3e38):
+        x = normal(2, 4, 50).float()
+        x[2, 49] = bad
+        ok = iseg.layernorm_fwd(x.to(DEV), status=st)[0]
+        assert iseg.iseg_status_read(st) == iseg.ISEG_DEV_NONFINITE
+        assert bool(torch.isfinite(ok[[0, 1, 3]]).all())
+        iseg.iseg_status_clear(st)
+
+
+def test_layouts_and_leading_dimensions():
+    from paper_2011_14504_amd import iseg
+    x = normal(3, 2, 3, 5, 24).float().to(DEV)
+    y, mean, rstd = iseg.layernorm_fwd(x)
+    assert y.shape == x.shape and mean.shape == (2, 3, 5)
+    flat = iseg.layernorm_fwd(x.reshape(30, 24))
+    assert torch.equal(y.reshape(30, 24), flat[0]) and torch.equal(rstd.reshape(30), flat[2])
+    t = iseg.layernorm_fwd(x.reshape(30, 24).t())                       # columns as rows: copied first
+    assert torch.equal(t[0], iseg.layernorm_fwd(x.reshape(30, 24).t().contiguous())[0])
+    e = iseg.layernorm_fwd(x[0, 0, :1].expand(6, 24))                   # one row broadcast over six
+    assert torch.equal(e[0][5], y[0, 0, 0])
+    one = iseg.layernorm_fwd(x[0, 0, 0])
+    assert torch.equal(one[0], y[0, 0, 0]) and one[1].shape == ()
