@@ -646,11 +646,14 @@ int iseg_transpose_i8(const int8_t* in, int64_t M, int64_t C, int64_t in_ld, int
  * float32, each may be NULL (1, 1, 0).  The sums are exact int32 (K <= 131071,
  * ISEG_ERR_UNSUPPORTED beyond), rounded to float32, multiplied by a_scale, by
  * b_scale, added to bias, and rounded to out_dtype (a float type).  K = 0
- * gives the bias. */
+ * gives the bias.  a and b start at multiples of 16 bytes unless `unaligned`
+ * is set (ISEG_ERR_ARG); with it, or with lda or ldb off a multiple of 16, the
+ * workspace holds aligned copies of both (not for M <= 32). */
 typedef struct iseg_matmul_geom {
     int64_t M, N, K;
     int64_t lda, ldb, ldc;
-    int32_t out_dtype, reserved;
+    int32_t out_dtype;
+    int32_t unaligned;           /* not 0: a or b may start off a multiple of 16 bytes */
 } iseg_matmul_geom;
 size_t iseg_matmul_i8_ws(const iseg_matmul_geom* g);
 int iseg_matmul_i8(const int8_t* a, const float* a_scale, const int8_t* b, const float* b_scale, const float* bias,

@@ -15,6 +15,14 @@ struct MmArgs {
     const float *sa, *sb, *bias;
     void* out;
     int64_t M, N, K, lda, ldb, ldc;
+    uint32_t tm, tn;             // tiles
+    int64_t ksplit;              // reduction of one split (a multiple of 128)
+    int64_t ldc_part;            // rows of the splits' sums (N rounded up to 4)
+};
+
+template <typename TO>
+struct alignas(4 * sizeof(TO)) OutVec {
+    TO v[4];
 };
 
 // 16 bytes of a row from column k on, zero from the row's end on
@@ -35,74 +43,492 @@ __device__ __forceinline__ v4i load16(const int8_t* row, int64_t k, int64_t K)
     return r;
 }
 
-__device__ __forceinline__ float mm_scale(const MmArgs& p, int sum, int64_t m, int64_t n)
+// the fragment of the last K % 16 columns: zero but for the first 16 bytes of
+// the reduction step (lp = 0)
+__device__ __forceinline__ v4i mm_tail(const int8_t* x, int64_t ld, int64_t row, int64_t rows, int64_t K, int lp)
 {
-    float v = (float)sum;
-    if (p.sa) v *= p.sa[m];
-    if (p.sb) v *= p.sb[n];
-    return p.bias ? v + p.bias[n] : v;
+    const v4i z = {0, 0, 0, 0};
+    return lp == 0 && row < rows ? load16(x + row * ld, K & ~(int64_t)15, K) : z;
 }
 
-__device__ __forceinline__ int mm_swz(int row, int part) { return row * 64 + ((part ^ ((row >> 1) & 3)) << 4); }
+// byte of a 16-byte piece in an LDS tile of 128-byte rows: the pieces of a row
+// are turned by half the row's number, which spreads the 16 rows of a fragment
+// read over the banks
+__device__ __forceinline__ int mm_swz(int row, int part) { return row * 128 + ((part ^ ((row >> 1) & 7)) << 4); }
 
-// 64 x 64 outputs per block, 64 of the reduction per step
-template <typename TO>
-__global__ __launch_bounds__(256) void k_matmul_i8(MmArgs p)
+// ---------------------------------------------------------------------------
+// tiles with direct-to-LDS loads
+// ---------------------------------------------------------------------------
+typedef __attribute__((address_space(3))) void lds_ptr_t;
+__device__ __attribute__((aligned(64))) int8_t g_mm_zero[64];
+
+__device__ __forceinline__ void mm_dma16(const void* g, int8_t* lds_wave_base)
 {
-    __shared__ __attribute__((aligned(16))) int8_t As[64 * 64], Bs[64 * 64];
-    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
-    const int64_t n0 = (int64_t)blockIdx.x * 64;
-    const int row = tid >> 2, part = tid & 3;
+    __builtin_amdgcn_global_load_lds(g, (lds_ptr_t*)lds_wave_base, 16, 0, 0);
+}
+
+// wait until at most VM loads of this wave are outstanding and its LDS reads are done
+template <int VM>
+__device__ __forceinline__ void mm_wait()
+{
+    static_assert(VM >= 0 && VM < 64, "vmcnt range");
+    __builtin_amdgcn_s_waitcnt((VM & 15) | ((VM >> 4) << 14) | (7 << 4));
+}
+
+// the tile (row, column) of a block: the blocks of one XCD (dealt round-robin
+// over 8) take a contiguous run of tiles, walked in bands of 8 rows, so the
+// tiles that run at one time on an XCD share rows of a and b in its L2
+__device__ __forceinline__ void mm_tile(uint32_t bid, uint32_t tm, uint32_t tn, uint32_t& im, uint32_t& in)
+{
+    const uint32_t T = tm * tn, q = T >> 3, r = T & 7, x = bid & 7, i = bid >> 3;
+    const uint32_t t = x * q + (x < r ? x : r) + i;
+    const uint32_t band = 8 * tn, b = t / band, first = b * 8, h = tm - first < 8 ? tm - first : 8;
+    const uint32_t u = t - b * band;
+    im = first + u % h;
+    in = u / h;
+}
+
+// BM x BN outputs per block of WM x WN waves, 128 of the reduction per stage
+// (whole cache lines of every row), ST stages of LDS.
+template <typename TO, int BM, int BN, int WM, int WN, int ST>
+__global__ __launch_bounds__(WM * WN * 64) void k_mm_tile(MmArgs p)
+{
+    constexpr int NW = WM * WN;
+    constexpr int TM = BM / WM / 16, TN = BN / WN / 16;
+    constexpr int NA = BM / 8 / NW, NB = BN / 8 / NW, LPW = NA + NB;
+    constexpr int SA = BM * 128, SB = BN * 128;
+    constexpr bool kSplit = sizeof(TO) == 4 && (TO)0.5f == (TO)0;      // int32 sums of a part of the reduction
+    static_assert(NW % 2 == 0, "a lane's piece is the same in all its loads");
+    extern __shared__ __attribute__((aligned(16))) int8_t smem[];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    uint32_t im, in;
+    mm_tile(blockIdx.x, p.tm, p.tn, im, in);
+    const int64_t m0 = (int64_t)im * BM, n0 = (int64_t)in * BN;
+    if constexpr (kSplit) {                   // this split's part of the reduction
+        const int64_t k0 = (int64_t)blockIdx.y * p.ksplit;
+        p.a += k0;
+        p.b += k0;
+        p.K = p.K - k0 < p.ksplit ? p.K - k0 : p.ksplit;
+        p.out = (int32_t*)p.out + (int64_t)blockIdx.y * p.M * p.ldc;
+    }
+    const int K16 = (int)p.K & ~15;
+    const int kfull = K16 / 128, nk = (K16 + 127) / 128;
+
+    // this lane's pieces: row 8 * instruction + lane / 8 of the tile in slot
+    // lane % 8; rows past the end repeat the last one (their outputs are dropped)
+    const int rin = lane >> 3, part = (lane & 7) ^ (4 * (wave & 1) + (rin >> 1));
+    const int8_t *ap[NA], *bp[NB];
+#pragma unroll
+    for (int j = 0; j < NA; j++) {
+        const int64_t r = m0 + 8 * (wave + NW * j) + rin;
+        ap[j] = p.a + (r < p.M ? r : p.M - 1) * p.lda + part * 16;
+    }
+#pragma unroll
+    for (int j = 0; j < NB; j++) {
+        const int64_t r = n0 + 8 * (wave + NW * j) + rin;
+        bp[j] = p.b + (r < p.N ? r : p.N - 1) * p.ldb + part * 16;
+    }
+    auto issue = [&](int kb) {
+        int8_t* st = smem + (kb % ST) * (SA + SB);
+#pragma unroll
+        for (int j = 0; j < NA; j++) mm_dma16(ap[j] + kb * 128, st + (wave + NW * j) * 1024);
+#pragma unroll
+        for (int j = 0; j < NB; j++) mm_dma16(bp[j] + kb * 128, st + SA + (wave + NW * j) * 1024);
+    };
+    auto issue_end = [&](int kb) {            // zeros past the last whole 16-byte piece
+        int8_t* st = smem + (kb % ST) * (SA + SB);
+        const bool live = kb * 128 + part * 16 < K16;
+#pragma unroll
+        for (int j = 0; j < NA; j++)
+            mm_dma16(live ? (const void*)(ap[j] + kb * 128) : (const void*)g_mm_zero, st + (wave + NW * j) * 1024);
+#pragma unroll
+        for (int j = 0; j < NB; j++)
+            mm_dma16(live ? (const void*)(bp[j] + kb * 128) : (const void*)g_mm_zero,
+                     st + SA + (wave + NW * j) * 1024);
+    };
+
+    const int wm = wave / WN, wn = wave % WN;
     const int lr = lane & 15, lp = lane >> 4;
-    const int wm = (w >> 1) * 32, wn = (w & 1) * 32;
-    const int64_t mt = ceil_div64(p.M, 64);
-    for (int64_t b = blockIdx.y; b < mt; b += gridDim.y) {
-        const int64_t m0 = b * 64;
-        const int8_t* ar = m0 + row < p.M ? p.a + (m0 + row) * p.lda : nullptr;
-        const int8_t* br = n0 + row < p.N ? p.b + (n0 + row) * p.ldb : nullptr;
-        v4i acc[2][2];
+    v4i acc[TM][TN];
 #pragma unroll
-        for (int i = 0; i < 2; i++)
+    for (int i = 0; i < TM; i++)
 #pragma unroll
-            for (int j = 0; j < 2; j++) acc[i][j] = (v4i){0, 0, 0, 0};
-        for (int64_t k0 = 0; k0 < p.K; k0 += 64) {
-            const v4i z = {0, 0, 0, 0};
-            const v4i va = ar ? load16(ar, k0 + part * 16, p.K) : z;
-            const v4i vb = br ? load16(br, k0 + part * 16, p.K) : z;
-            __syncthreads();
-            *(v4i*)&As[mm_swz(row, part)] = va;
-            *(v4i*)&Bs[mm_swz(row, part)] = vb;
-            __syncthreads();
-            v4i fa[2], fb[2];
+        for (int j = 0; j < TN; j++) acc[i][j] = (v4i){0, 0, 0, 0};
+    // fragments of half h (64 of the reduction) of a stage
+    auto frags = [&](int kb, int h, v4i* fa, v4i* fb) {
+        const int8_t* A = smem + (kb % ST) * (SA + SB);
+        const int8_t* B = A + SA;
 #pragma unroll
-            for (int i = 0; i < 2; i++) fa[i] = *(const v4i*)&As[mm_swz(wm + i * 16 + lr, lp)];
+        for (int j = 0; j < TN; j++) fb[j] = *(const v4i*)&B[mm_swz(wn * (TN * 16) + j * 16 + lr, h * 4 + lp)];
 #pragma unroll
-            for (int j = 0; j < 2; j++) fb[j] = *(const v4i*)&Bs[mm_swz(wn + j * 16 + lr, lp)];
+        for (int i = 0; i < TM; i++) fa[i] = *(const v4i*)&A[mm_swz(wm * (TM * 16) + i * 16 + lr, h * 4 + lp)];
+    };
+    // b's fragment first: a lane then holds four neighbouring columns of one row
+    auto mma = [&](const v4i* fa, const v4i* fb) {
 #pragma unroll
-            for (int i = 0; i < 2; i++)
+        for (int i = 0; i < TM; i++)
 #pragma unroll
-                for (int j = 0; j < 2; j++)
-                    acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(fa[i], fb[j], acc[i][j], 0, 0, 0);
+            for (int j = 0; j < TN; j++)
+                acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(fb[j], fa[i], acc[i][j], 0, 0, 0);
+    };
+    v4i fa[2][TM], fb[2][TN];
+    // one stage: while its first half is multiplied its second half is read;
+    // then stage kb + 1 becomes visible and stage kb's buffer free (its reads
+    // are done in every wave), and under the second half's products the next
+    // loads go out and the next fragments are read
+    auto stage = [&](int kb, auto&& issue_next) {
+        frags(kb, 1, fa[1], fb[1]);
+        mma(fa[0], fb[0]);
+        __builtin_amdgcn_sched_barrier(0);
+        mm_wait<(ST - 2) * LPW>();
+        __builtin_amdgcn_s_barrier();
+        issue_next(kb + ST);
+        frags(kb + 1, 0, fa[0], fb[0]);
+        mma(fa[1], fb[1]);
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    if (nk > 0) {
+#pragma unroll
+        for (int i = 0; i < ST; i++) issue_end(i);
+        mm_wait<(ST - 1) * LPW>();
+        __builtin_amdgcn_s_barrier();
+        frags(0, 0, fa[0], fb[0]);
+        int kb = 0;
+        for (; kb + ST < kfull; kb++) stage(kb, issue);
+        for (; kb < nk; kb++) stage(kb, issue_end);
+        mm_wait<0>();                         // the zeros still on their way to LDS
+    }
+    if (p.K & 15) {
+        // the last 1 to 15 of the reduction straight into the fragments
+        const int64_t ra = m0 + wm * (TM * 16) + lr, rb = n0 + wn * (TN * 16) + lr;
+#pragma unroll
+        for (int j = 0; j < TN; j++) fb[0][j] = mm_tail(p.b, p.ldb, rb + j * 16, p.N, p.K, lp);
+#pragma unroll
+        for (int i = 0; i < TM; i++) fa[0][i] = mm_tail(p.a, p.lda, ra + i * 16, p.M, p.K, lp);
+        mma(fa[0], fb[0]);
+    }
+    // Epilogue: 16 rows of the wave's outputs at a time through its own part of
+    // LDS, so that rows leave in whole cache lines (a lane's four columns alone
+    // are 32 bytes of a row per store instruction).
+    constexpr int ES = (int)sizeof(TO), ROW = TN * 16 * ES, PITCH = ROW + 16, CH = ROW / 16;
+    static_assert(16 * PITCH * NW <= ST * (SA + SB), "epilogue buffers");
+    __syncthreads();                          // every wave is done with the stages
+    int8_t* t = smem + wave * 16 * PITCH;     // a wave's LDS accesses keep their order
+    TO* out = (TO*)p.out;
+    const int64_t mw = m0 + wm * (TM * 16), nw = n0 + wn * (TN * 16);
+    float sb[TN][4], bias[TN][4];
+#pragma unroll
+    for (int j = 0; j < TN && !kSplit; j++) {
+        const int64_t n = nw + j * 16 + lp * 4;
+#pragma unroll
+        for (int r = 0; r < 4; r++) { sb[j][r] = 1.f; bias[j][r] = 0.f; }
+        if (n + 4 <= p.N) {
+            if (p.sb) __builtin_memcpy(sb[j], p.sb + n, 16);
+            if (p.bias) __builtin_memcpy(bias[j], p.bias + n, 16);
+        } else {
+#pragma unroll
+            for (int r = 0; r < 4; r++) {
+                if (p.sb && n + r < p.N) sb[j][r] = p.sb[n + r];
+                if (p.bias && n + r < p.N) bias[j][r] = p.bias[n + r];
+            }
+        }
+    }
+    float sa[TM];
+#pragma unroll
+    for (int i = 0; i < TM && !kSplit; i++) {
+        const int64_t m = mw + i * 16 + lr;
+        sa[i] = p.sa ? p.sa[m < p.M ? m : p.M - 1] : 1.f;
+    }
+#pragma unroll
+    for (int i = 0; i < TM; i++) {
+#pragma unroll
+        for (int j = 0; j < TN; j++) {
+            OutVec<TO> o;
+#pragma unroll
+            for (int r = 0; r < 4; r++) {
+                if constexpr (kSplit) o.v[r] = acc[i][j][r];
+                else o.v[r] = (TO)((float)acc[i][j][r] * sa[i] * sb[j][r] + bias[j][r]);
+            }
+            *(OutVec<TO>*)(t + lr * PITCH + (j * 16 + lp * 4) * ES) = o;
         }
 #pragma unroll
-        for (int i = 0; i < 2; i++)
+        for (int c = lane; c < 16 * CH; c += 64) {
+            const int r = c / CH, q = c % CH;
+            const v4i v = *(const v4i*)(t + r * PITCH + q * 16);
+            const int64_t m = mw + i * 16 + r, n = nw + q * (16 / ES);
+            if (m < p.M && n < p.N) {
+                TO* d = out + m * p.ldc + n;
+                if (n + 16 / ES <= p.N) {
+                    __builtin_memcpy(d, &v, 16);
+                } else {
+                    TO e[16 / ES];
+                    __builtin_memcpy(e, &v, 16);
 #pragma unroll
-            for (int j = 0; j < 2; j++)
-#pragma unroll
-                for (int r = 0; r < 4; r++) {
-                    const int64_t m = m0 + wm + i * 16 + lp * 4 + r, n = n0 + wn + j * 16 + lr;
-                    if (m < p.M && n < p.N) ((TO*)p.out)[m * p.ldc + n] = (TO)mm_scale(p, acc[i][j][r], m, n);
+                    for (int x = 0; x < 16 / ES; x++)
+                        if (n + x < p.N) d[x] = e[x];
                 }
+            }
+        }
     }
 }
 
-template <typename TO>
-int launch_mm(const MmArgs& p, hipStream_t s)
+// Rows of a and b copied into buffers of zero-padded rows of Kp bytes (a
+// multiple of 64): operands whose rows start off 16 bytes, where loads to LDS
+// would straddle.  One pass over them, against M N K / 64 products.
+__global__ __launch_bounds__(256) void k_mm_pack(MmArgs p, int8_t* __restrict__ a, int8_t* __restrict__ b, int64_t Kp)
 {
-    const int64_t mt = ceil_div64(p.M, 64);
-    hipLaunchKernelGGL(k_matmul_i8<TO>, dim3((unsigned)ceil_div64(p.N, 64), (unsigned)(mt < 4096 ? mt : 4096)),
-                       dim3(256), 0, s, p);
+    const int64_t pieces = Kp / 16, na = p.M * pieces, all = na + p.N * pieces;
+    for (int64_t i = blockIdx.x * (int64_t)256 + threadIdx.x; i < all; i += (int64_t)gridDim.x * 256) {
+        const bool first = i < na;
+        const int64_t e = first ? i : i - na, r = e / pieces, k = (e - r * pieces) * 16;
+        *(v4i*)((first ? a : b) + r * Kp + k) = load16(first ? p.a + r * p.lda : p.b + r * p.ldb, k, p.K);
+    }
+}
+
+// Outputs from the int32 sums of `splits` (<= 16) parts of the reduction, four
+// neighbours per thread; every part's load is in flight at once.
+template <typename TO>
+__global__ __launch_bounds__(256) void k_mm_join(MmArgs p, const int32_t* __restrict__ part, int splits)
+{
+    const int64_t per = (p.N + 3) / 4;
+    for (int64_t i = blockIdx.x * (int64_t)256 + threadIdx.x; i < p.M * per; i += (int64_t)gridDim.x * 256) {
+        const int64_t m = i / per, n = (i - m * per) * 4;
+        const int32_t* q = part + m * p.ldc_part + n;
+        v4i t[16];
+#pragma unroll
+        for (int k = 0; k < 16; k++) t[k] = *(const v4i*)(q + (k < splits ? k : 0) * p.M * p.ldc_part);
+        v4i s = t[0];
+#pragma unroll
+        for (int k = 1; k < 16; k++)
+            if (k < splits) s += t[k];
+        const float sa = p.sa ? p.sa[m] : 1.f;
+        OutVec<TO> o;
+#pragma unroll
+        for (int r = 0; r < 4; r++) {
+            float v = (float)s[r] * sa;
+            if (n + r < p.N) {
+                if (p.sb) v *= p.sb[n + r];
+                if (p.bias) v += p.bias[n + r];
+            }
+            o.v[r] = (TO)v;
+        }
+        TO* d = (TO*)p.out + m * p.ldc + n;
+        if (n + 4 <= p.N) {
+            __builtin_memcpy(d, &o, sizeof(o));
+        } else {
+#pragma unroll
+            for (int r = 0; r < 4; r++)
+                if (n + r < p.N) d[r] = o.v[r];
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------
+// few rows of a: the bytes of b
+// ---------------------------------------------------------------------------
+// A block takes J * 16 rows of b, its NW waves deal out their reduction in
+// pieces of 256; b comes straight into fragments (nothing of it is used
+// twice), a from the caches, and the waves' sums meet in LDS.
+template <typename TO, int MT, int J, int NW>
+__global__ __launch_bounds__(NW * 64) void k_mm_rows(MmArgs p)
+{
+    __shared__ __attribute__((aligned(16))) int red[NW][MT * J][256];
+    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+    const int lr = lane & 15, lp = lane >> 4;
+    const int64_t n0 = (int64_t)blockIdx.x * (J * 16);
+    const int8_t *ap[MT], *bp[J];
+#pragma unroll
+    for (int i = 0; i < MT; i++) {
+        const int64_t r = i * 16 + lr;
+        ap[i] = p.a + (r < p.M ? r : p.M - 1) * p.lda;
+    }
+#pragma unroll
+    for (int j = 0; j < J; j++) {
+        const int64_t r = n0 + j * 16 + lr;
+        bp[j] = p.b + (r < p.N ? r : p.N - 1) * p.ldb;
+    }
+    v4i acc[MT][J];
+#pragma unroll
+    for (int i = 0; i < MT; i++)
+#pragma unroll
+        for (int j = 0; j < J; j++) acc[i][j] = (v4i){0, 0, 0, 0};
+    const int K = (int)p.K;
+    for (int k0 = w * 256; k0 < K; k0 += NW * 256) {
+        v4i fa[4][MT], fb[4][J];
+        if (k0 + 256 <= K) {
+#pragma unroll
+            for (int u = 0; u < 4; u++)
+#pragma unroll
+                for (int j = 0; j < J; j++) __builtin_memcpy(&fb[u][j], bp[j] + k0 + u * 64 + lp * 16, 16);
+#pragma unroll
+            for (int u = 0; u < 4; u++)
+#pragma unroll
+                for (int i = 0; i < MT; i++) __builtin_memcpy(&fa[u][i], ap[i] + k0 + u * 64 + lp * 16, 16);
+        } else {
+#pragma unroll
+            for (int u = 0; u < 4; u++) {
+#pragma unroll
+                for (int j = 0; j < J; j++) fb[u][j] = load16(bp[j], k0 + u * 64 + lp * 16, K);
+#pragma unroll
+                for (int i = 0; i < MT; i++) fa[u][i] = load16(ap[i], k0 + u * 64 + lp * 16, K);
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < 4; u++)
+#pragma unroll
+            for (int i = 0; i < MT; i++)
+#pragma unroll
+                for (int j = 0; j < J; j++)
+                    acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(fb[u][j], fa[u][i], acc[i][j], 0, 0, 0);
+    }
+#pragma unroll
+    for (int i = 0; i < MT; i++)
+#pragma unroll
+        for (int j = 0; j < J; j++) *(v4i*)&red[w][i * J + j][lane * 4] = acc[i][j];
+    __syncthreads();
+    // output e of a 16 x 16 tile: row e / 16, column e % 16, held by lane
+    // (e % 16) / 4 * 16 + e / 16 in element e % 4
+    for (int e = tid; e < MT * J * 256; e += NW * 64) {
+        const int col = e % (J * 16), row = e / (J * 16);
+        const int64_t n = n0 + col;
+        if (row >= p.M || n >= p.N) continue;
+        const int t = (row >> 4) * J + (col >> 4), r = row & 15, c = col & 15;
+        const int at = ((c >> 2) * 16 + r) * 4 + (c & 3);
+        int sum = 0;
+#pragma unroll
+        for (int i = 0; i < NW; i++) sum += red[i][t][at];
+        float v = (float)sum;
+        if (p.sa) v *= p.sa[row];
+        if (p.sb) v *= p.sb[n];
+        if (p.bias) v += p.bias[n];
+        ((TO*)p.out)[row * p.ldc + n] = (TO)v;
+    }
+}
+
+template <typename TO, int BM, int BN, int WM, int WN, int ST>
+int launch_tile(MmArgs p, hipStream_t s, int splits = 1)
+{
+    constexpr size_t lds = (size_t)ST * (BM + BN) * 128;
+    if (lds > 65536 && !lds_limit((const void*)k_mm_tile<TO, BM, BN, WM, WN, ST>, lds)) return ISEG_ERR_DEVICE;
+    const int64_t tiles = ceil_div64(p.M, BM) * ceil_div64(p.N, BN);
+    if (tiles * (WM * WN * 64) >= (int64_t)1 << 32) return ISEG_ERR_UNSUPPORTED;      // a launch's threads
+    p.tm = (uint32_t)ceil_div64(p.M, BM);
+    p.tn = (uint32_t)ceil_div64(p.N, BN);
+    hipLaunchKernelGGL((k_mm_tile<TO, BM, BN, WM, WN, ST>), dim3(p.tm * p.tn, splits), dim3(WM * WN * 64), lds, s, p);
     return launch_ok();
+}
+
+template <typename TO, int MT, int J, int NW>
+int launch_rows(const MmArgs& p, hipStream_t s)
+{
+    const int64_t nb = ceil_div64(p.N, J * 16);
+    if (nb * (NW * 64) >= (int64_t)1 << 32) return ISEG_ERR_UNSUPPORTED;
+    hipLaunchKernelGGL((k_mm_rows<TO, MT, J, NW>), dim3((unsigned)nb), dim3(NW * 64), 0, s, p);
+    return launch_ok();
+}
+
+template <typename TO, int BM, int BN, int WM, int WN, int ST>
+int launch_split(const MmArgs& p, int splits, int32_t* ws, hipStream_t s)
+{
+    MmArgs q = p;
+    q.ksplit = ceil_div64(ceil_div64(p.K, 128), splits) * 128;
+    q.out = ws;
+    q.ldc = q.ldc_part = (p.N + 3) / 4 * 4;
+    const int n = (int)ceil_div64(p.K, q.ksplit);
+    const int rc = launch_tile<int32_t, BM, BN, WM, WN, ST>(q, s, n);
+    if (rc != ISEG_OK) return rc;
+    MmArgs r = p;
+    r.ldc_part = q.ldc_part;
+    hipLaunchKernelGGL(k_mm_join<TO>, dim3(grid_for(p.M * (q.ldc_part / 4), 256, 1 << 16)), dim3(256), 0, s, r,
+                       (const int32_t*)ws, n);
+    return launch_ok();
+}
+
+// How a product is run.  The tile kernels' times on MI355X, in us, for one
+// round of blocks over the 256 CUs (te + ts per 128 of the reduction), once
+// with one block per CU and once with as many as fit:
+//   256 x 256          9.5 + 1.6          (one fits)
+//   128 x 128, 2 waves 3.5 + 0.6 (four stages)   4.2 + 0.9 (two blocks of two stages)
+//   64 x 128           2.0 + 0.3          3.0 + 0.7
+//   64 x 64            0.6 + 0.27         1.5 + 0.55
+// The plan with the least estimate is taken; a reduction cut into parts costs
+// a second kernel (4.5 us).  Against the estimate, e.g. 2048 x 8192 x 2048:
+// 256 x 256 tiles 37.7 us, 128 x 128 39.5; 1024 x 2048 x 2048: 64 x 128 9.4,
+// 128 x 128 12.7; 64 x 2048 x 8192: 64 x 64 in 8 parts 12.3, in one 20.7.
+enum MmKind { MM_ROWS16, MM_ROWS32, MM_256, MM_128, MM_128_DEEP, MM_64x128, MM_64 };
+struct MmPlan {
+    MmKind kind;
+    int splits;
+    bool pack;
+};
+
+MmPlan mm_plan(const iseg_matmul_geom* g)
+{
+    // few rows: b's bytes are what counts (see k_mm_rows)
+    if (g->M <= 32) return {g->M <= 16 ? MM_ROWS16 : MM_ROWS32, 1, false};
+    struct Kind {
+        MmKind one, full;
+        int64_t bm, bn;
+        int fit;
+        double te1, ts1, te, ts;
+    };
+    static const Kind kinds[] = {
+        {MM_256, MM_256, 256, 256, 1, 9.5, 1.6, 9.5, 1.6},
+        {MM_128_DEEP, MM_128, 128, 128, 2, 3.5, 0.6, 4.2, 0.9},
+        {MM_64x128, MM_64x128, 64, 128, 2, 2.0, 0.3, 3.0, 0.7},
+        {MM_64, MM_64, 64, 64, 2, 0.6, 0.27, 1.5, 0.55},
+    };
+    const int64_t st = ceil_div64(g->K, 128);
+    MmPlan best = {MM_64, 1, false};
+    double least = 1e30;
+    for (const Kind& k : kinds) {
+        const int64_t tiles = ceil_div64(g->M, k.bm) * ceil_div64(g->N, k.bn);
+        const double t = tiles <= 256 ? k.te1 + k.ts1 * (double)st
+                                      : (double)ceil_div64(tiles, 256 * k.fit) * (k.te + k.ts * (double)st);
+        if (t < least) { least = t; best = {tiles <= 256 ? k.one : k.full, 1, false}; }
+        if (k.one == MM_64 && tiles <= 128) {
+            int64_t sp = 256 / tiles < 16 ? 256 / tiles : 16;
+            sp = sp < st / 4 ? sp : st / 4;              // parts of at least 512 of the reduction
+            const double u = sp > 1 ? k.te1 + k.ts1 * (double)ceil_div64(st, sp) + 4.5 : 1e30;
+            if (u < least) { least = u; best = {MM_64, (int)sp, false}; }
+        }
+    }
+    best.pack = g->unaligned || g->lda % 16 || g->ldb % 16;
+    return best;
+}
+
+int64_t mm_packed_row(int64_t K) { return (K + 63) / 64 * 64; }
+
+size_t mm_pack_bytes(const iseg_matmul_geom* g, const MmPlan& pl)
+{
+    return pl.pack ? align256((size_t)g->M * mm_packed_row(g->K)) + align256((size_t)g->N * mm_packed_row(g->K)) : 0;
+}
+
+template <typename TO>
+int launch_mm(MmArgs p, const iseg_matmul_geom* g, const MmPlan& pl, char* ws, hipStream_t s)
+{
+    // Rows of b per block and waves on them, 16-row products on 1 x 4096 x 4096
+    // / 8 x 12288 x 4096: 16 rows, 8 waves 6.5 / 17.0 us, 32 rows 7.0 / 14.1.
+    if (pl.kind == MM_ROWS16) return g->N <= 8192 ? launch_rows<TO, 1, 1, 8>(p, s) : launch_rows<TO, 1, 2, 8>(p, s);
+    if (pl.kind == MM_ROWS32) return g->N <= 4096 ? launch_rows<TO, 2, 1, 8>(p, s) : launch_rows<TO, 2, 2, 8>(p, s);
+    if (pl.pack && p.K > 0) {
+        const int64_t Kp = mm_packed_row(p.K);
+        int8_t* pa = (int8_t*)ws;
+        int8_t* pb = pa + align256((size_t)p.M * Kp);
+        hipLaunchKernelGGL(k_mm_pack, dim3(grid_for((p.M + p.N) * (Kp / 16), 256, 8192)), dim3(256), 0, s, p, pa, pb, Kp);
+        p.a = pa;
+        p.b = pb;
+        p.lda = p.ldb = p.K = Kp;
+    }
+    switch (pl.kind) {
+    case MM_256: return launch_tile<TO, 256, 256, 2, 4, 2>(p, s);
+    case MM_128: return launch_tile<TO, 128, 128, 2, 4, 2>(p, s);
+    case MM_128_DEEP: return launch_tile<TO, 128, 128, 2, 4, 4>(p, s);
+    case MM_64x128: return launch_tile<TO, 64, 128, 2, 4, 3>(p, s);
+    default:
+        if (pl.splits > 1) return launch_split<TO, 64, 64, 2, 4, 4>(p, pl.splits, (int32_t*)(ws + mm_pack_bytes(g, pl)), s);
+        return launch_tile<TO, 64, 64, 2, 4, 4>(p, s);
+    }
 }
 
 int mm_check(const iseg_matmul_geom* g)
@@ -120,7 +546,12 @@ int mm_check(const iseg_matmul_geom* g)
 
 extern "C" size_t iseg_matmul_i8_ws(const iseg_matmul_geom* g)
 {
-    return mm_check(g) == ISEG_OK ? 256 : 0;
+    if (mm_check(g) != ISEG_OK) return 0;
+    if (g->M == 0 || g->N == 0) return 256;
+    const MmPlan pl = mm_plan(g);
+    size_t b = mm_pack_bytes(g, pl);
+    if (pl.splits > 1) b += align256((size_t)pl.splits * g->M * ((g->N + 3) / 4 * 4) * 4);
+    return b > 256 ? b : 256;
 }
 
 extern "C" int iseg_matmul_i8(const int8_t* a, const float* a_scale, const int8_t* b, const float* b_scale,
@@ -131,10 +562,13 @@ extern "C" int iseg_matmul_i8(const int8_t* a, const float* a_scale, const int8_
     if (rc != ISEG_OK) return rc;
     if (g->M == 0 || g->N == 0) return ISEG_OK;
     if (!out || (g->K > 0 && (!a || !b))) return ISEG_ERR_ARG;
+    if (!g->unaligned && (((uintptr_t)a | (uintptr_t)b) & 15)) return ISEG_ERR_ARG;
     if (!ws || ws_bytes < iseg_matmul_i8_ws(g)) return ISEG_ERR_WORKSPACE;
     MmArgs p = {};
     p.a = a; p.b = b; p.sa = a_scale; p.sb = b_scale; p.bias = bias; p.out = out;
     p.M = g->M; p.N = g->N; p.K = g->K; p.lda = g->lda; p.ldb = g->ldb; p.ldc = g->ldc;
-    return g->out_dtype == ISEG_F32 ? launch_mm<float>(p, stream)
-                                    : g->out_dtype == ISEG_F16 ? launch_mm<f16_t>(p, stream) : launch_mm<bf16_t>(p, stream);
+    const MmPlan pl = mm_plan(g);
+    return g->out_dtype == ISEG_F32   ? launch_mm<float>(p, g, pl, (char*)ws, stream)
+           : g->out_dtype == ISEG_F16 ? launch_mm<f16_t>(p, g, pl, (char*)ws, stream)
+                                      : launch_mm<bf16_t>(p, g, pl, (char*)ws, stream);
 }

@@ -75,7 +75,7 @@ class LayernormGeom(C.Structure):
 
 class MatmulGeom(C.Structure):
     _fields_ = [(n, C.c_int64) for n in ("M", "N", "K", "lda", "ldb", "ldc")] + \
-               [("out_dtype", C.c_int32), ("reserved", C.c_int32)]
+               [("out_dtype", C.c_int32), ("unaligned", C.c_int32)]
 
 
 class LogprobGeom(C.Structure):
@@ -1319,8 +1319,8 @@ def _layernorm_geom(M, Cc, x_ld, y_ld, dx_ld, x_dtype, p_dtype, eps):
 
 
 @functools.lru_cache(maxsize=256)
-def _matmul_geom(M, N, K, lda, ldb, ldc, out_dtype):
-    g = MatmulGeom(M, N, K, lda, ldb, ldc, out_dtype, 0)
+def _matmul_geom(M, N, K, lda, ldb, ldc, out_dtype, unaligned):
+    g = MatmulGeom(M, N, K, lda, ldb, ldc, out_dtype, unaligned)
     return g, lib().iseg_matmul_i8_ws(C.byref(g))
 
 
@@ -1456,7 +1456,7 @@ def matmul_i8(a, b, a_scale=None, b_scale=None, bias=None, out_dtype=torch.float
     bias = _vec(bias, N, torch.float32, a.device, "bias")
     _gpu(a, b)
     out = torch.empty((M, N), dtype=out_dtype, device=a.device)
-    g, wsb = _matmul_geom(M, N, K, lda, ldb, max(N, 1), od)
+    g, wsb = _matmul_geom(M, N, K, lda, ldb, max(N, 1), od, int((ar.data_ptr() | br.data_ptr()) & 15 != 0))
     iseg_matmul_i8(ar, a_scale, br, b_scale, bias, g, out, _scratch(a.device, wsb))
     return out
 

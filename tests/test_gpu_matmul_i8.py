@@ -55,6 +55,31 @@ def test_product(case):
     assert got.dtype == DT[t] and got.shape == (M, N)
 
 
+# sizes that reach every way a product is run: few rows, each tile, a reduction
+# in parts; with whole and broken tiles and reductions, and rows off 16 bytes
+PATHS = [(15, 9000, 300), (16, 20, 8200), (20, 100, 500), (32, 5000, 272), (33, 20, 2050), (40, 40, 9000), (64, 2048, 4096), (512, 1024, 1536), (1024, 2048, 400),
+         (1000, 2050, 130), (1500, 2048, 1000), (2048, 2048, 128), (4000, 4100, 160), (4096, 8192, 256), (4100, 4100, 1), (260, 16000, 100)]
+
+
+@pytest.mark.parametrize("case", PATHS, ids=str)
+def test_every_path_of_a_product(case):
+    from paper_2011_14504_amd import iseg
+    M, N, K = case
+    print(f"[matmul_i8 paths] {case}", flush=True)
+    gen = torch.Generator(device=DEV)
+    gen.manual_seed(M + N + K)
+    a, b = (torch.randint(-128, 128, (r, K), dtype=torch.int8, device=DEV, generator=gen) for r in (M, N))
+    want = (a.double() @ b.double().t()).float()
+    pad = (K + 15) // 16 * 16
+    for la, lb, off in ((pad, pad, 0), (K, pad + 16, 0), (pad, pad + 32, 16), (pad + 1, K, 3), (pad, pad, 5)):
+        ba = torch.full((M * la + off,), 99, dtype=torch.int8, device=DEV)
+        bb = torch.full((N * lb + off,), -99, dtype=torch.int8, device=DEV)
+        va, vb = (t[off:].view(r, l)[:, :K] for t, r, l in ((ba, M, la), (bb, N, lb)))
+        va.copy_(a)
+        vb.copy_(b)
+        assert torch.equal(iseg.matmul_i8(va, vb), want), (la, lb, off)
+
+
 def test_product_extremes():
     """-128 codes at the longest reduction: the sums reach 2^31 - 2^14."""
     from paper_2011_14504_amd import iseg

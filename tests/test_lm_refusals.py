@@ -74,14 +74,18 @@ def test_quantizer_entries(iseg):
 def test_matmul_entry(iseg):
     L = iseg.lib()
 
-    def mm(M=4, N=4, K=16, lda=16, ldb=16, ldc=4, t=iseg.ISEG_F32, a=ONE, out=ONE, ws=ONE, n=BIG):
-        g = iseg.MatmulGeom(M, N, K, lda, ldb, ldc, t, 0)
+    def mm(M=4, N=4, K=16, lda=16, ldb=16, ldc=4, t=iseg.ISEG_F32, a=ONE, out=ONE, ws=ONE, n=BIG, un=0):
+        g = iseg.MatmulGeom(M, N, K, lda, ldb, ldc, t, un)
         return L.iseg_matmul_i8(a, None, ONE, None, None, C.byref(g), out, ws, n, None)
 
     assert mm(t=iseg.ISEG_I32) == iseg.ISEG_ERR_ARG
     for bad in (dict(M=-1), dict(N=-1), dict(K=-1), dict(lda=15), dict(ldb=15), dict(ldc=3), dict(M=1 << 31)):
         assert mm(**bad) == iseg.ISEG_ERR_SHAPE, bad
     assert mm(K=131072, lda=131072, ldb=131072) == iseg.ISEG_ERR_UNSUPPORTED
+    off = C.c_void_p(ONE.value + 8)
+    assert mm(a=off) == iseg.ISEG_ERR_ARG and mm(a=off, un=1, n=0) == iseg.ISEG_ERR_WORKSPACE
+    need = [L.iseg_matmul_i8_ws(C.byref(iseg.MatmulGeom(100, 200, 70, ld, 80, 200, iseg.ISEG_F32, un))) for ld, un in ((80, 0), (80, 1), (70, 0))]
+    assert need[0] == 256 and need[1] == need[2] >= 300 * 128
     assert mm(a=None) == iseg.ISEG_ERR_ARG and mm(out=None) == iseg.ISEG_ERR_ARG
     assert mm(ws=None) == iseg.ISEG_ERR_WORKSPACE and mm(n=1) == iseg.ISEG_ERR_WORKSPACE
     assert mm(M=0, a=None, out=None) == iseg.ISEG_OK and mm(N=0, ldc=0) == iseg.ISEG_OK
