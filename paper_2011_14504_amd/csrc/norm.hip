@@ -20,35 +20,52 @@ struct LnArgs {
 };
 
 // ---------------------------------------------------------------------------
-// forward: NW waves per row, VPT vectors of a row per thread
+// forward: NW waves per row (one, four or sixteen), VPT vectors of a row per
+// thread.  A block walks its rows with gamma and beta in registers and the
+// next row's x on its way.
 // ---------------------------------------------------------------------------
 template <typename T, typename P, int NW, int VPT>
-__global__ __launch_bounds__(NW * 64) void k_layernorm_fwd(LnArgs a)
+__global__ __launch_bounds__(NW < 4 ? 256 : NW * 64) void k_layernorm_fwd(LnArgs a)
 {
     constexpr int N = RowVec<T>::N;
-    constexpr int NT = NW * 64;
+    constexpr int NT = NW * 64, R = NW < 4 ? 4 / NW : 1;      // threads of a row, rows of a block
     __shared__ float red[4 * NW];
-    const int tid = threadIdx.x;
+    const int tid = threadIdx.x % NT;
     const int64_t C = a.C;
     const float inv_c = 1.f / (float)C;
-    const P* gamma = (const P*)a.gamma;
-    const P* beta = (const P*)a.beta;
-    for (int64_t m = blockIdx.x; m < a.M; m += gridDim.x) {
-        const T* x = (const T*)a.x + m * a.x_ld;
-        RowVec<T> xv[VPT];
+    RowSlot<N> sl[VPT];                                       // only the last one may be short
+    ParamVec<P, N> gm[VPT], bt[VPT];
+#pragma unroll
+    for (int j = 0; j < VPT; j++) {
+        const int64_t c = ((int64_t)j * NT + tid) * N;
+        sl[j] = j < VPT - 1 ? RowSlot<N>{c, 0} : row_slot<N>(c, C);
+        gm[j] = param_load<P, N>((const P*)a.gamma, sl[j], 1.f);
+        bt[j] = param_load<P, N>((const P*)a.beta, sl[j], 0.f);
+    }
+    RowVec<T> xv[VPT];
+    int64_t m = (int64_t)blockIdx.x * R + threadIdx.x / NT;
+    const int64_t step = (int64_t)gridDim.x * R;
+    if (m < a.M) {
+#pragma unroll
+        for (int j = 0; j < VPT; j++) xv[j] = slot_load<T, N>((const T*)a.x + m * a.x_ld, sl[j]);
+    }
+    for (; m < a.M; m += step) {
+        float v[VPT][N];
         float s = 0.f, z = 0.f;
 #pragma unroll
-        for (int j = 0; j < VPT; j++) {
-            const int64_t c = ((int64_t)j * NT + tid) * N;
-            if (c + N <= C) xv[j] = row_load(x + c);
-            else xv[j] = row_load_part(x + c, c < C ? (int)(C - c) : 0, (T)0.f);
+        for (int j = 0; j < VPT; j++)
+#pragma unroll
+            for (int i = 0; i < N; i++) v[j][i] = (float)xv[j].v[i];
+        if (m + step < a.M) {
+#pragma unroll
+            for (int j = 0; j < VPT; j++) xv[j] = slot_load<T, N>((const T*)a.x + (m + step) * a.x_ld, sl[j]);
         }
 #pragma unroll
         for (int j = 0; j < VPT; j++)
 #pragma unroll
-            for (int i = 0; i < N; i++) s += (float)xv[j].v[i];
+            for (int i = 0; i < N; i++) s += j < VPT - 1 || i >= sl[j].dup ? v[j][i] : 0.f;
         block_sum2_f32<NW>(s, z, red);
-        float mean = s * inv_c;
+        const float mean = s * inv_c;
         // squares around the mean, and the sum of the differences, whose mean
         // is what the first sum's rounding left out
         float d1 = 0.f, d2 = 0.f;
@@ -56,8 +73,8 @@ __global__ __launch_bounds__(NW * 64) void k_layernorm_fwd(LnArgs a)
         for (int j = 0; j < VPT; j++)
 #pragma unroll
             for (int i = 0; i < N; i++) {
-                const int64_t c = ((int64_t)j * NT + tid) * N + i;
-                const float d = c < C ? (float)xv[j].v[i] - mean : 0.f;
+                v[j][i] -= mean;
+                const float d = j < VPT - 1 || i >= sl[j].dup ? v[j][i] : 0.f;
                 d1 += d;
                 d2 = fmaf(d, d, d2);
             }
@@ -70,32 +87,24 @@ __global__ __launch_bounds__(NW * 64) void k_layernorm_fwd(LnArgs a)
             if (a.rstd) a.rstd[m] = rstd;
             if (!(fabsf(d2) <= 3.4028234e38f)) set_status(a.status, ISEG_DEV_NONFINITE);
         }
-        T* y = (T*)a.y + m * a.y_ld;
 #pragma unroll
         for (int j = 0; j < VPT; j++) {
-            const int64_t c = ((int64_t)j * NT + tid) * N;
-            if (c >= C) continue;
             RowVec<T> o;
 #pragma unroll
-            for (int i = 0; i < N; i++) {
-                const bool in = c + i < C;
-                const float g = gamma && in ? (float)gamma[c + i] : 1.f;
-                const float b = beta && in ? (float)beta[c + i] : 0.f;
-                o.v[i] = (T)fmaf(((float)xv[j].v[i] - mean - corr) * rstd, g, b);
-            }
-            if (c + N <= C) row_store(y + c, o);
-            else row_store_part(y + c, o, (int)(C - c));
+            for (int i = 0; i < N; i++)
+                o.v[i] = (T)fmaf((v[j][i] - corr) * rstd, (float)gm[j].v[i], (float)bt[j].v[i]);
+            if (j < VPT - 1 || sl[j].dup < N) row_store((T*)a.y + m * a.y_ld + sl[j].at, o);
         }
-        if (NW > 1) __syncthreads();          // red is written again by the next row
     }
 }
 
-// rows longer than the registers take: three passes over the row (the second
-// and third come from the caches)
-template <typename T, typename P>
-__global__ __launch_bounds__(1024) void k_layernorm_fwd_long(LnArgs a)
+// rows longer than the registers take, or shorter than a vector: three passes
+// over the row (the second and third come from the caches)
+template <typename T, typename P, int NW>
+__global__ __launch_bounds__(NW * 64) void k_layernorm_fwd_long(LnArgs a)
 {
-    __shared__ float red[64];
+    constexpr int NT = NW * 64;
+    __shared__ float red[4 * NW];
     const int tid = threadIdx.x;
     const int64_t C = a.C;
     const float inv_c = 1.f / (float)C;
@@ -104,16 +113,16 @@ __global__ __launch_bounds__(1024) void k_layernorm_fwd_long(LnArgs a)
     for (int64_t m = blockIdx.x; m < a.M; m += gridDim.x) {
         const T* x = (const T*)a.x + m * a.x_ld;
         float s = 0.f, z = 0.f;
-        for (int64_t c = tid; c < C; c += 1024) s += (float)x[c];
-        block_sum2_f32<16>(s, z, red);
+        for (int64_t c = tid; c < C; c += NT) s += (float)x[c];
+        block_sum2_f32<NW>(s, z, red);
         const float mean = s * inv_c;
         float d1 = 0.f, d2 = 0.f;
-        for (int64_t c = tid; c < C; c += 1024) {
+        for (int64_t c = tid; c < C; c += NT) {
             const float d = (float)x[c] - mean;
             d1 += d;
             d2 = fmaf(d, d, d2);
         }
-        block_sum2_f32<16>(d1, d2, red + 32);
+        block_sum2_f32<NW>(d1, d2, red + 2 * NW);
         const float corr = d1 * inv_c;
         const float var = fmaxf(d2 * inv_c - corr * corr, 0.f);
         const float rstd = 1.f / sqrtf(var + a.eps);
@@ -123,25 +132,48 @@ __global__ __launch_bounds__(1024) void k_layernorm_fwd_long(LnArgs a)
             if (!(fabsf(d2) <= 3.4028234e38f)) set_status(a.status, ISEG_DEV_NONFINITE);
         }
         T* y = (T*)a.y + m * a.y_ld;
-        for (int64_t c = tid; c < C; c += 1024) {
+        for (int64_t c = tid; c < C; c += NT) {
             const float g = gamma ? (float)gamma[c] : 1.f;
             const float b = beta ? (float)beta[c] : 0.f;
             y[c] = (T)fmaf(((float)x[c] - mean - corr) * rstd, g, b);
         }
-        __syncthreads();
     }
+}
+
+// Waves and vectors per row, by the row's vectors.  16384 x 4096 bf16 (512
+// vectors): four waves of two 48.9 us (5.5 TB/s), one wave of eight 57;
+// 32768 x 2048: four of one 50.6, one of four 51.5; 32768 x 1024: one of two
+// 28.9.  More blocks than the chip holds at once reload gamma and beta for
+// fewer rows each: 55 us with a block per row in the first case.
+template <typename T, typename P, int NW, int VPT>
+int fwd_grid(const LnArgs& a, unsigned cap, hipStream_t s)
+{
+    constexpr int R = NW < 4 ? 4 / NW : 1;
+    const int64_t nb = ceil_div64(a.M, R);
+    hipLaunchKernelGGL((k_layernorm_fwd<T, P, NW, VPT>), dim3((unsigned)(nb < cap ? nb : cap)),
+                       dim3(NW < 4 ? 256 : NW * 64), 0, s, a);
+    return launch_ok();
 }
 
 template <typename T, typename P>
 int launch_fwd(const LnArgs& a, hipStream_t s)
 {
     constexpr int N = RowVec<T>::N;
+    const int64_t v = ceil_div64(a.C, N);
     const unsigned grid = (unsigned)(a.M < kRowGridMax ? a.M : kRowGridMax);
-    if (a.C <= 256 * N) hipLaunchKernelGGL((k_layernorm_fwd<T, P, 4, 1>), dim3(grid), dim3(256), 0, s, a);
-    else if (a.C <= 512 * N) hipLaunchKernelGGL((k_layernorm_fwd<T, P, 4, 2>), dim3(grid), dim3(256), 0, s, a);
-    else if (a.C <= 1024 * N) hipLaunchKernelGGL((k_layernorm_fwd<T, P, 4, 4>), dim3(grid), dim3(256), 0, s, a);
-    else if (a.C <= 4096 * N) hipLaunchKernelGGL((k_layernorm_fwd<T, P, 16, 4>), dim3(grid), dim3(1024), 0, s, a);
-    else hipLaunchKernelGGL((k_layernorm_fwd_long<T, P>), dim3(grid), dim3(1024), 0, s, a);
+    if (a.C < N) {
+        hipLaunchKernelGGL((k_layernorm_fwd_long<T, P, 1>), dim3(grid), dim3(64), 0, s, a);
+        return launch_ok();
+    }
+    if (v <= 64) return fwd_grid<T, P, 1, 1>(a, 2048, s);
+    if (v <= 128) return fwd_grid<T, P, 1, 2>(a, 2048, s);
+    if (v <= 256) return fwd_grid<T, P, 4, 1>(a, 4096, s);
+    if (v <= 512) return fwd_grid<T, P, 4, 2>(a, 4096, s);
+    if (v <= 768) return fwd_grid<T, P, 4, 3>(a, 2048, s);
+    if (v <= 1024) return fwd_grid<T, P, 4, 4>(a, 2048, s);
+    if (v <= 1536) return fwd_grid<T, P, 8, 3>(a, 1024, s);
+    if (v <= 2048) return fwd_grid<T, P, 8, 4>(a, 1024, s);
+    hipLaunchKernelGGL((k_layernorm_fwd_long<T, P, 16>), dim3(grid), dim3(1024), 0, s, a);
     return launch_ok();
 }
 
@@ -149,8 +181,9 @@ int launch_fwd(const LnArgs& a, hipStream_t s)
 // backward
 // ---------------------------------------------------------------------------
 // One block walks rows b, b + grid, ... with its threads on fixed columns, so
-// the column sums of dy xhat and dy stay in registers; each block leaves one
-// row of partial sums that k_layernorm_param_sum adds in block order.
+// gamma and the column sums of dy xhat and dy stay in registers and the next
+// row's x and dy are on their way; each block leaves one row of partial sums
+// that k_layernorm_param_sum adds in block order.
 template <typename T, typename P, int NW, int VPT>
 __global__ __launch_bounds__(NW * 64) void k_layernorm_bwd(LnArgs a)
 {
@@ -160,75 +193,75 @@ __global__ __launch_bounds__(NW * 64) void k_layernorm_bwd(LnArgs a)
     const int tid = threadIdx.x;
     const int64_t C = a.C;
     const float inv_c = 1.f / (float)C;
-    const P* gamma = (const P*)a.gamma;
+    RowSlot<N> sl[VPT];                                       // only the last one may be short
+    ParamVec<P, N> gm[VPT];
     float dg[VPT][N], db[VPT][N];
 #pragma unroll
-    for (int j = 0; j < VPT; j++)
+    for (int j = 0; j < VPT; j++) {
+        const int64_t c = ((int64_t)j * NT + tid) * N;
+        sl[j] = j < VPT - 1 ? RowSlot<N>{c, 0} : row_slot<N>(c, C);
+        gm[j] = param_load<P, N>((const P*)a.gamma, sl[j], 1.f);
 #pragma unroll
         for (int i = 0; i < N; i++) dg[j][i] = db[j][i] = 0.f;
-    int flip = 0;
-    for (int64_t m = blockIdx.x; m < a.M; m += gridDim.x, flip ^= 1) {
-        const T* x = (const T*)a.x + m * a.x_ld;
-        const T* dy = (const T*)a.dy + m * a.y_ld;
-        const float mean = a.mean[m], rstd = a.rstd[m];
-        RowVec<T> xv[VPT], dv[VPT];
+    }
+    RowVec<T> xv[VPT], dv[VPT];
+    float mean_n = 0.f, rstd_n = 0.f;
+    auto fetch = [&](int64_t m) {
 #pragma unroll
         for (int j = 0; j < VPT; j++) {
-            const int64_t c = ((int64_t)j * NT + tid) * N;
-            if (c + N <= C) {
-                xv[j] = row_load(x + c);
-                dv[j] = row_load(dy + c);
-            } else {
-                const int n = c < C ? (int)(C - c) : 0;
-                xv[j] = row_load_part(x + c, n, (T)0.f);
-                dv[j] = row_load_part(dy + c, n, (T)0.f);
-            }
+            xv[j] = slot_load<T, N>((const T*)a.x + m * a.x_ld, sl[j]);
+            dv[j] = slot_load<T, N>((const T*)a.dy + m * a.y_ld, sl[j]);
         }
+        mean_n = a.mean[m];
+        rstd_n = a.rstd[m];
+    };
+    if (blockIdx.x < a.M) fetch(blockIdx.x);
+    int flip = 0;
+    for (int64_t m = blockIdx.x; m < a.M; m += gridDim.x, flip ^= 1) {
+        const float mean = mean_n, rstd = rstd_n;
+        float xh[VPT][N], g[VPT][N];
         float s1 = 0.f, s2 = 0.f;
 #pragma unroll
         for (int j = 0; j < VPT; j++)
 #pragma unroll
             for (int i = 0; i < N; i++) {
-                const int64_t c = ((int64_t)j * NT + tid) * N + i;
-                const float d = (float)dv[j].v[i];             // 0 past the row's end
-                const float xh = ((float)xv[j].v[i] - mean) * rstd;
-                const float g = gamma && c < C ? d * (float)gamma[c] : d;
-                s1 += g;
-                s2 = fmaf(g, xh, s2);
-                dg[j][i] = fmaf(d, xh, dg[j][i]);
-                db[j][i] += d;
+                const float d = (float)dv[j].v[i];
+                xh[j][i] = ((float)xv[j].v[i] - mean) * rstd;
+                g[j][i] = d * (float)gm[j].v[i];
+                const bool own = j < VPT - 1 || i >= sl[j].dup;
+                const float go = own ? g[j][i] : 0.f, dn = own ? d : 0.f;
+                s1 += go;
+                s2 = fmaf(go, xh[j][i], s2);
+                dg[j][i] = fmaf(dn, xh[j][i], dg[j][i]);
+                db[j][i] += dn;
             }
+        if (m + gridDim.x < a.M) fetch(m + gridDim.x);
         block_sum2_f32<NW>(s1, s2, red + flip * 2 * NW);
         s1 *= inv_c;
         s2 *= inv_c;
-        T* dx = (T*)a.dx + m * a.dx_ld;
 #pragma unroll
         for (int j = 0; j < VPT; j++) {
-            const int64_t c = ((int64_t)j * NT + tid) * N;
-            if (c >= C) continue;
             RowVec<T> o;
 #pragma unroll
-            for (int i = 0; i < N; i++) {
-                const float d = (float)dv[j].v[i];
-                const float xh = ((float)xv[j].v[i] - mean) * rstd;
-                const float g = gamma && c + i < C ? d * (float)gamma[c + i] : d;
-                o.v[i] = (T)((g - s1 - xh * s2) * rstd);
-            }
-            if (c + N <= C) row_store(dx + c, o);
-            else row_store_part(dx + c, o, (int)(C - c));
+            for (int i = 0; i < N; i++) o.v[i] = (T)((g[j][i] - s1 - xh[j][i] * s2) * rstd);
+            if (j < VPT - 1 || sl[j].dup < N) row_store((T*)a.dx + m * a.dx_ld + sl[j].at, o);
         }
     }
     float* part = a.part + (int64_t)blockIdx.x * 2 * C;
 #pragma unroll
-    for (int j = 0; j < VPT; j++)
+    for (int j = 0; j < VPT; j++) {
+        if (sl[j].dup == 0) {
+            __builtin_memcpy(part + sl[j].at, dg[j], sizeof(dg[j]));
+            __builtin_memcpy(part + C + sl[j].at, db[j], sizeof(db[j]));
+        } else {
 #pragma unroll
-        for (int i = 0; i < N; i++) {
-            const int64_t c = ((int64_t)j * NT + tid) * N + i;
-            if (c < C) {
-                part[c] = dg[j][i];
-                part[C + c] = db[j][i];
-            }
+            for (int i = 0; i < N; i++)
+                if (i >= sl[j].dup) {
+                    part[sl[j].at + i] = dg[j][i];
+                    part[C + sl[j].at + i] = db[j][i];
+                }
         }
+    }
 }
 
 // rows longer than the registers take: the two row sums first ...
@@ -278,41 +311,53 @@ __global__ __launch_bounds__(256) void k_layernorm_bwd_cols(LnArgs a, const floa
     part[a.C + c] = db;
 }
 
-// dgamma and dbeta: the np partial rows added in order, 64 columns per block
-// with the partials dealt to four waves
+// dgamma (blockIdx.y = 0) or dbeta (1): the np partial rows added in one
+// order, 64 columns per block, the rows dealt to its sixteen waves
 template <typename P>
-__global__ __launch_bounds__(256) void k_layernorm_param_sum(const float* __restrict__ part, int np, int64_t C,
-                                                             P* dgamma, P* dbeta)
+__global__ __launch_bounds__(1024) void k_layernorm_param_sum(const float* __restrict__ part, int np, int64_t C,
+                                                              P* dgamma, P* dbeta)
 {
-    __shared__ float red[4][2][64];
+    __shared__ float red[16][64];
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
     const int64_t c = (int64_t)blockIdx.x * 64 + lane;
-    float g = 0.f, b = 0.f;
-    if (c < C)
-        for (int p = w; p < np; p += 4) {
-            g += part[(int64_t)p * 2 * C + c];
-            b += part[(int64_t)p * 2 * C + C + c];
-        }
-    red[w][0][lane] = g;
-    red[w][1][lane] = b;
+    P* out = blockIdx.y ? dbeta : dgamma;
+    if (!out) return;
+    const float* col = part + blockIdx.y * C + (c < C ? c : C - 1);
+    float s = 0.f;
+    for (int p0 = w; p0 < np; p0 += 16 * 8) {
+        float t[8];
+#pragma unroll
+        for (int u = 0; u < 8; u++) t[u] = col[(int64_t)(p0 + 16 * u < np ? p0 + 16 * u : p0) * 2 * C];
+#pragma unroll
+        for (int u = 0; u < 8; u++) s += p0 + 16 * u < np ? t[u] : 0.f;
+    }
+    red[w][lane] = s;
     __syncthreads();
     if (w != 0 || c >= C) return;
-    g = red[0][0][lane] + red[1][0][lane] + red[2][0][lane] + red[3][0][lane];
-    b = red[0][1][lane] + red[1][1][lane] + red[2][1][lane] + red[3][1][lane];
-    if (dgamma) dgamma[c] = (P)g;
-    if (dbeta) dbeta[c] = (P)b;
+    s = 0.f;
+#pragma unroll
+    for (int i = 0; i < 16; i++) s += red[i][lane];
+    out[c] = (P)s;
 }
 
-int64_t ln_elem_size(int32_t t) { return t == ISEG_F32 ? 4 : 2; }
+// rows that the backward holds in registers: at most 1536 vectors
+int64_t ln_vectors(const iseg_layernorm_geom* g) { return ceil_div64(g->C, g->x_dtype == ISEG_F32 ? 4 : 8); }
 
-// rows that the backward holds in registers: 1024 threads with two vectors of
-// x and two of dy each
-bool ln_bwd_in_regs(const iseg_layernorm_geom* g) { return g->C <= 2048 * (16 / ln_elem_size(g->x_dtype)); }
+bool ln_bwd_in_regs(const iseg_layernorm_geom* g)
+{
+    return g->C >= (g->x_dtype == ISEG_F32 ? 4 : 8) && ln_vectors(g) <= 1536;
+}
 
-// blocks that walk the rows (one row of partial column sums each)
+// Blocks that walk the rows, each of which leaves 2 C floats of partial sums:
+// one per CU where a block's rows fill it, more where they are short.  bf16,
+// with the sum over the partials: 8192 x 4096 46.5 us with 256 blocks of 8
+// waves, 50.5 with 512; 1024 x 2048 (fp32) 12.5 and 15.7; 16384 x 2048 of 4
+// waves 61.6 / 47.0 / 49.0 with 256 / 512 / 768; 32768 x 512 of one wave 38.7
+// / 35.8 / 42.7 with 1024 / 1536 / 3072.
 int ln_bwd_blocks(const iseg_layernorm_geom* g)
 {
-    int64_t cap = ln_bwd_in_regs(g) ? 512 : 64;
+    const int64_t v = ln_vectors(g);
+    const int64_t cap = !ln_bwd_in_regs(g) ? 64 : v <= 64 ? 1536 : v <= 128 ? 1024 : v <= 256 ? 512 : 256;
     return (int)(g->M < cap ? g->M : cap);
 }
 
@@ -321,6 +366,7 @@ int launch_bwd(const LnArgs& a, const iseg_layernorm_geom* g, hipStream_t s)
 {
     constexpr int N = RowVec<T>::N;
     const int nb = ln_bwd_blocks(g);
+    const int64_t v = ceil_div64(a.C, N);
     if (nb > 0) {
         if (!ln_bwd_in_regs(g)) {
             float2* sums = (float2*)((char*)a.part + align256((size_t)nb * 2 * a.C * 4));
@@ -328,16 +374,22 @@ int launch_bwd(const LnArgs& a, const iseg_layernorm_geom* g, hipStream_t s)
             hipLaunchKernelGGL((k_layernorm_bwd_rows<T, P>), dim3(gr), dim3(1024), 0, s, a, sums);
             hipLaunchKernelGGL((k_layernorm_bwd_cols<T, P>), dim3((unsigned)ceil_div64(a.C, 256), nb), dim3(256), 0,
                                s, a, (const float2*)sums);
-        } else if (a.C <= 256 * N) {
+        } else if (v <= 64) {
+            hipLaunchKernelGGL((k_layernorm_bwd<T, P, 1, 1>), dim3(nb), dim3(64), 0, s, a);
+        } else if (v <= 128) {
+            hipLaunchKernelGGL((k_layernorm_bwd<T, P, 1, 2>), dim3(nb), dim3(64), 0, s, a);
+        } else if (v <= 256) {
             hipLaunchKernelGGL((k_layernorm_bwd<T, P, 4, 1>), dim3(nb), dim3(256), 0, s, a);
-        } else if (a.C <= 512 * N) {
-            hipLaunchKernelGGL((k_layernorm_bwd<T, P, 4, 2>), dim3(nb), dim3(256), 0, s, a);
+        } else if (v <= 512) {
+            hipLaunchKernelGGL((k_layernorm_bwd<T, P, 8, 1>), dim3(nb), dim3(512), 0, s, a);
+        } else if (v <= 1024) {
+            hipLaunchKernelGGL((k_layernorm_bwd<T, P, 8, 2>), dim3(nb), dim3(512), 0, s, a);
         } else {
-            hipLaunchKernelGGL((k_layernorm_bwd<T, P, 16, 2>), dim3(nb), dim3(1024), 0, s, a);
+            hipLaunchKernelGGL((k_layernorm_bwd<T, P, 8, 3>), dim3(nb), dim3(512), 0, s, a);
         }
     }
     if (a.dgamma || a.dbeta)
-        hipLaunchKernelGGL((k_layernorm_param_sum<P>), dim3((unsigned)ceil_div64(a.C, 64)), dim3(256), 0, s, a.part,
+        hipLaunchKernelGGL((k_layernorm_param_sum<P>), dim3((unsigned)ceil_div64(a.C, 64), 2), dim3(1024), 0, s, a.part,
                            nb, a.C, (P*)a.dgamma, (P*)a.dbeta);
     return launch_ok();
 }

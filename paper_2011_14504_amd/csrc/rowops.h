@@ -107,6 +107,55 @@ __device__ __forceinline__ void block_sum2_f32(float& a, float& b, float* red)
     for (int i = 0; i < NW; i++) { a += red[2 * i]; b += red[2 * i + 1]; }
 }
 
+// A row of C >= N elements dealt to NT threads in vectors of N.  The row's last
+// vector, when C is no multiple of N, starts N before the end instead: it
+// repeats `dup` elements of the vector before it, which sums leave out and
+// stores write a second time with the same bits.
+template <int N>
+struct RowSlot {
+    int64_t at;      // first element
+    int dup;         // repeated elements at its front; N if the thread has no vector here
+};
+
+template <int N>
+__device__ __forceinline__ RowSlot<N> row_slot(int64_t c, int64_t C)
+{
+    if (c >= C) return {0, N};
+    return c + N <= C ? RowSlot<N>{c, 0} : RowSlot<N>{C - N, (int)(c + N - C)};
+}
+
+template <typename T, int N>
+__device__ __forceinline__ RowVec<T> slot_load(const T* row, const RowSlot<N>& s)
+{
+    RowVec<T> r;
+    if (s.dup < N) {
+        r = row_load(row + s.at);
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; i++) r.v[i] = (T)0.f;
+    }
+    return r;
+}
+
+// N parameters of a column vector, `fill` without one
+template <typename P, int N>
+struct ParamVec {
+    P v[N];
+};
+
+template <typename P, int N>
+__device__ __forceinline__ ParamVec<P, N> param_load(const P* p, const RowSlot<N>& s, float fill)
+{
+    ParamVec<P, N> r;
+    if (p && s.dup < N) {
+        __builtin_memcpy(&r, p + s.at, sizeof(r));
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; i++) r.v[i] = (P)fill;
+    }
+    return r;
+}
+
 static inline bool is_float_dtype(int32_t t) { return t == ISEG_F32 || t == ISEG_F16 || t == ISEG_BF16; }
 
 // launches walk their rows in a loop, so the grid may be cut at any count
