@@ -1,11 +1,14 @@
 // rowquant.hip -- quantizers with a scale for each row or each column, and the
 // transposition of int8 codes: the operands of iseg_matmul_i8.
 //
-// Every decision is exact: v = x mul is held in double where mul is given
-// (24 x 24 bits), the largest magnitude is taken on the bit patterns (where a
-// NaN or an infinity is larger than every finite value, so it is seen), and a
-// code is settled by the sign of v - (n + 1/2) scale in double, whose product
-// is exact (9 x 24 bits).
+// Every decision is exact although the bulk of the work is float32.  With
+// h = fl(x mul) (x itself without mul), |h| grows with |x mul|, so the largest
+// exact magnitude is found among the elements with the largest |h|, and only
+// those are formed in double (24 x 24 bits).  Magnitudes are compared as bit
+// patterns, where a NaN or an infinity is larger than every finite value.  A
+// code is floor(h / s + 1/2); where h / s + 1/2 lies within 2^-14 of an integer
+// (its error, of three roundings of at most 128, is below 2^-15), the sign of
+// x mul - (n + 1/2) s in double settles it (the product is exact).
 #include "rowops.h"
 
 namespace {
@@ -44,27 +47,165 @@ __device__ __forceinline__ float scale_of(uint64_t big, int bits, int mode)
     return f < kScaleMin ? kScaleMin : (f <= 3.4028234e38f ? f : __builtin_nanf(""));
 }
 
-// clamp(floor(v / s + 1/2), +-lim): an estimate within one, then the two half-steps around it
-__device__ __forceinline__ int code_of(double v, float s, float inv, int lim)
+__device__ __forceinline__ uint64_t bits_of(double v) { return __builtin_bit_cast(uint64_t, v) & kAbs64; }
+__device__ __forceinline__ uint32_t bits_of(float v) { return __builtin_bit_cast(uint32_t, v) & 0x7fffffffu; }
+
+// How codes follow from a scale.  Scales above 2^100 (whose reciprocal may be
+// subnormal) and values whose float32 product overflows take the exact way.
+struct Coder {
+    double sd;
+    float inv;
+    int lim;
+    bool exact, ok;
+    __device__ __forceinline__ Coder(float s, int bits)
+        : sd(s), inv(1.f / s), lim((1 << (bits - 1)) - 1), exact(!(s <= 1.2676506e30f)), ok(s == s)
+    {
+    }
+};
+
+// clamp(floor(v / s + 1/2), +-lim) of the exact v: an estimate within one,
+// then the half-steps on either side of it
+__device__ __forceinline__ int code_exact(double v, const Coder& k)
 {
-    float q = fminf(fmaxf((float)v * inv, -128.f), 128.f);
-    int n = (int)floorf(q + 0.5f);
-    const double sd = (double)s;
-    if (v - ((double)n + 0.5) * sd >= 0.0) n++;
-    else if (v - ((double)n - 0.5) * sd < 0.0) n--;
-    return n > lim ? lim : (n < -lim ? -lim : n);
+    const double q = fmin(fmax(v * (1.0 / k.sd), -128.0), 128.0);
+    int n = (int)floor(q + 0.5);
+    if (v - ((double)n + 0.5) * k.sd >= 0.0) n++;
+    else if (v - ((double)n - 0.5) * k.sd < 0.0) n--;
+    return n > k.lim ? k.lim : (n < -k.lim ? -k.lim : n);
 }
 
-__device__ __forceinline__ uint64_t bits_of(double v) { return __builtin_bit_cast(uint64_t, v) & kAbs64; }
+// the same from h = fl(v); `far` becomes the largest distance of h / s + 1/2
+// from a half-integer seen so far (above 1/2 - 2^-14: near an integer)
+__device__ __forceinline__ int code_fast(float h, const Coder& k, float& far)
+{
+    const float q = fmaf(h, k.inv, 0.5f), f = floorf(q);
+    far = fmaxf(far, fabsf(q - f - 0.5f));
+    const float c = (float)k.lim;
+    return (int)fminf(fmaxf(f, -c), c);
+}
+constexpr float kNear = 0.5f - 6.1035156e-5f;
+
+// codes of N values x (times m, exactly) as N bytes
+template <int N, bool MUL>
+__device__ __forceinline__ void codes_of(const float* x, const float* m, const Coder& k, uint32_t* out)
+{
+    int n[N];
+    float far = 0.f;
+#pragma unroll
+    for (int i = 0; i < N; i++) n[i] = code_fast(MUL ? x[i] * m[i] : x[i], k, far);
+    if (k.exact || !(far < kNear)) {
+#pragma unroll
+        for (int i = 0; i < N; i++) n[i] = code_exact(MUL ? (double)x[i] * (double)m[i] : (double)x[i], k);
+    }
+#pragma unroll
+    for (int i = 0; i < N / 4; i++)
+        out[i] = !k.ok ? 0u
+                       : (uint32_t)(uint8_t)n[4 * i] | (uint32_t)(uint8_t)n[4 * i + 1] << 8 |
+                             (uint32_t)(uint8_t)n[4 * i + 2] << 16 | (uint32_t)n[4 * i + 3] << 24;
+}
 
 // ---------------------------------------------------------------------------
-// rows: one block per row, the row read twice (the second time from the caches)
+// rows
 // ---------------------------------------------------------------------------
+// largest bit pattern over the NW waves of a row (red: NW words that no
+// earlier call may still read)
+template <int NW>
+__device__ __forceinline__ uint32_t row_max_u32(uint32_t v, uint32_t* red)
+{
+    v = wave_max_u32(v);
+    if (NW == 1) return v;
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    if (lane == 0) red[w] = v;
+    __syncthreads();
+    v = 0;
+#pragma unroll
+    for (int i = 0; i < NW; i++) v = red[i] > v ? red[i] : v;
+    return v;
+}
+
+// NW waves per row (one, or the whole block), VPT vectors of it per thread, in
+// registers between the maximum and the codes.
+template <typename T, bool MUL, int NW, int VPT>
+__global__ __launch_bounds__(NW < 4 ? 256 : NW * 64) void k_quantize_rows(RqRowArgs a)
+{
+    constexpr int N = RowVec<T>::N;
+    constexpr int NT = NW * 64, R = NW < 4 ? 4 / NW : 1;
+    __shared__ uint32_t red[2][NW];
+    __shared__ unsigned long long top[2];
+    const int tid = threadIdx.x % NT;
+    RowSlot<N> sl[VPT];                                       // only the last one may be short
+    ParamVec<float, N> mv[VPT];
+#pragma unroll
+    for (int j = 0; j < VPT; j++) {
+        const int64_t c = ((int64_t)j * NT + tid) * N;
+        sl[j] = j < VPT - 1 ? RowSlot<N>{c, 0} : row_slot<N>(c, a.C);
+        if (MUL) mv[j] = param_load<float, N>(a.mul, sl[j], 0.f);
+    }
+    int flip = 0;
+    for (int64_t m = (int64_t)blockIdx.x * R + threadIdx.x / NT; m < a.M; m += (int64_t)gridDim.x * R, flip ^= 1) {
+        RowVec<T> xv[VPT];
+        uint32_t big = 0;
+#pragma unroll
+        for (int j = 0; j < VPT; j++) xv[j] = slot_load<T, N>((const T*)a.x + m * a.x_ld, sl[j]);
+#pragma unroll
+        for (int j = 0; j < VPT; j++)
+#pragma unroll
+            for (int i = 0; i < N; i++) {
+                const float x = (float)xv[j].v[i];
+                const uint32_t b = bits_of(MUL ? x * mv[j].v[i] : x);
+                big = b > big ? b : big;
+            }
+        big = row_max_u32<NW>(big, red[flip]);
+        uint64_t tb;
+        if constexpr (MUL) {
+            // the exact products of the elements that reach the float maximum
+            uint64_t e = 0;
+#pragma unroll
+            for (int j = 0; j < VPT; j++)
+#pragma unroll
+                for (int i = 0; i < N; i++) {
+                    const float x = (float)xv[j].v[i];
+                    if (bits_of(x * mv[j].v[i]) == big) {
+                        const uint64_t b = bits_of((double)x * (double)mv[j].v[i]);
+                        e = b > e ? b : e;
+                    }
+                }
+            if (NW == 1) {
+                tb = wave_max_u64(e);
+            } else {
+                if (threadIdx.x == 0) top[flip] = 0;
+                __syncthreads();
+                if (e) atomicMax(&top[flip], (unsigned long long)e);
+                __syncthreads();
+                tb = top[flip];
+            }
+        } else {
+            tb = bits_of((double)__builtin_bit_cast(float, big));
+        }
+        const float s = scale_of(tb, a.bits, a.mode);
+        const Coder k(s, a.bits);
+        if (tid == 0) {
+            a.scale[m] = s;
+            if (!k.ok) set_status(a.status, ISEG_DEV_NONFINITE);
+        }
+#pragma unroll
+        for (int j = 0; j < VPT; j++) {
+            float x[N];
+#pragma unroll
+            for (int i = 0; i < N; i++) x[i] = (float)xv[j].v[i];
+            uint32_t o[N / 4];
+            codes_of<N, MUL>(x, mv[j].v, k, o);
+            if (j < VPT - 1 || sl[j].dup < N) __builtin_memcpy(a.codes + m * a.codes_ld + sl[j].at, o, N);
+        }
+    }
+}
+
+// rows longer than the registers take, or shorter than a vector: read twice
+// (the second time from the caches), every product in double
 template <typename T>
-__global__ __launch_bounds__(256) void k_quantize_rows(RqRowArgs a)
+__global__ __launch_bounds__(256) void k_quantize_rows_long(RqRowArgs a)
 {
     const int tid = threadIdx.x;
-    const int lim = (1 << (a.bits - 1)) - 1;
     for (int64_t m = blockIdx.x; m < a.M; m += gridDim.x) {
         const T* x = (const T*)a.x + m * a.x_ld;
         int8_t* o = a.codes + m * a.codes_ld;
@@ -76,15 +217,14 @@ __global__ __launch_bounds__(256) void k_quantize_rows(RqRowArgs a)
         }
         big = block_max_u64(big);
         const float s = scale_of(big, a.bits, a.mode);
-        const bool ok = s == s;
+        const Coder k(s, a.bits);
         if (tid == 0) {
             a.scale[m] = s;
-            if (!ok) set_status(a.status, ISEG_DEV_NONFINITE);
+            if (!k.ok) set_status(a.status, ISEG_DEV_NONFINITE);
         }
-        const float inv = 1.f / s;
         for (int64_t c = tid; c < a.C; c += 256) {
             const double v = a.mul ? (double)(float)x[c] * (double)a.mul[c] : (double)(float)x[c];
-            o[c] = ok ? (int8_t)code_of(v, s, inv, lim) : 0;
+            o[c] = k.ok ? (int8_t)code_exact(v, k) : 0;
         }
     }
 }
@@ -92,32 +232,108 @@ __global__ __launch_bounds__(256) void k_quantize_rows(RqRowArgs a)
 // ---------------------------------------------------------------------------
 // columns
 // ---------------------------------------------------------------------------
-// Largest |v| and sum of x of 64 columns over a strip of rows.
-template <typename T>
+// Largest |v| (a double's bits) and sum of x of 64 columns over a strip of
+// rows.  A block's threads take vectors of N columns: 64 / N of them side by
+// side, the rows dealt to the others.
+template <typename T, bool MUL>
 __global__ __launch_bounds__(256) void k_cols_stats(RqRowArgs a, int64_t strip)
 {
+    constexpr int N = RowVec<T>::N, G = 64 / N, RS = 256 / G;       // vectors across, rows at once
     __shared__ uint64_t rm[4][64];
     __shared__ float rs[4][64];
-    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-    const int64_t c = (int64_t)blockIdx.x * 64 + lane;
+    const int tid = threadIdx.x, g = tid % G, r0 = tid / G, w = tid >> 6;
+    const int64_t c0 = (int64_t)blockIdx.x * 64;
+    const RowSlot<N> sl = row_slot<N>(c0 + g * N, a.C);
     const int64_t m0 = (int64_t)blockIdx.y * strip;
     const int64_t m1 = m0 + strip < a.M ? m0 + strip : a.M;
+    float sum[N];
+    uint64_t big[N];                          // exact magnitudes, formed where |fl(v)| reaches its largest so far
+#pragma unroll
+    for (int i = 0; i < N; i++) { sum[i] = 0.f; big[i] = 0; }
+    uint32_t bt[N];
+#pragma unroll
+    for (int i = 0; i < N; i++) bt[i] = 0;
+    for (int64_t m = m0 + r0; m < m1; m += RS * 4) {
+        RowVec<T> xv[4];
+        float mu[4];
+#pragma unroll
+        for (int u = 0; u < 4; u++) {         // past the strip's end: the first row again, counted as nothing
+            const int64_t mm = m + u * RS < m1 ? m + u * RS : m;
+            xv[u] = slot_load<T, N>((const T*)a.x + mm * a.x_ld, sl);
+            mu[u] = MUL ? a.mul[mm] : 1.f;
+        }
+#pragma unroll
+        for (int u = 0; u < 4; u++) {
+            const bool in = m + u * RS < m1;
+#pragma unroll
+            for (int i = 0; i < N; i++) {
+                const float x = (float)xv[u].v[i];
+                sum[i] += in ? x : 0.f;
+                const uint32_t b = bits_of(MUL ? x * mu[u] : x);
+                if (MUL) {
+                    if (b >= bt[i]) {
+                        const uint64_t e = bits_of((double)x * (double)mu[u]);
+                        bt[i] = b;
+                        big[i] = e > big[i] ? e : big[i];
+                    }
+                } else {
+                    bt[i] = b > bt[i] ? b : bt[i];
+                }
+            }
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < N; i++)
+        if (!MUL) big[i] = bits_of((double)__builtin_bit_cast(float, bt[i]));
+    // over the rows of a wave: the lanes with the same g are G apart
+#pragma unroll
+    for (int o = G; o < 64; o <<= 1)
+#pragma unroll
+        for (int i = 0; i < N; i++) {
+            const uint64_t t = __shfl_xor((unsigned long long)big[i], o, 64);
+            big[i] = t > big[i] ? t : big[i];
+            sum[i] += __shfl_xor(sum[i], o, 64);
+        }
+    if ((tid & 63) < G) {
+#pragma unroll
+        for (int i = 0; i < N; i++) {
+            rm[w][g * N + i] = big[i];
+            rs[w][g * N + i] = sum[i];
+        }
+    }
+    __syncthreads();
+    if (tid >= 64) return;
+    // element tid of the vectors: column at + tid % N of its vector, unless it
+    // repeats the vector before
+    const RowSlot<N> mine = row_slot<N>(c0 + tid / N * N, a.C);
+    if (tid % N < mine.dup) return;
+    const int64_t c = mine.at + tid % N;
+    uint64_t e = rm[0][tid];
+    float s = rs[0][tid];
+#pragma unroll
+    for (int i = 1; i < 4; i++) {
+        e = rm[i][tid] > e ? rm[i][tid] : e;
+        s += rs[i][tid];
+    }
+    a.pmax[(int64_t)blockIdx.y * a.C + c] = e;
+    a.psum[(int64_t)blockIdx.y * a.C + c] = s;
+}
+
+// the same for fewer columns than a vector: one thread per column and strip
+template <typename T>
+__global__ __launch_bounds__(64) void k_cols_stats_narrow(RqRowArgs a, int64_t strip)
+{
+    const int64_t m0 = (int64_t)blockIdx.y * strip;
+    const int64_t m1 = m0 + strip < a.M ? m0 + strip : a.M;
+    const int c = threadIdx.x;
+    if (c >= a.C) return;
     uint64_t big = 0;
     float sum = 0.f;
-    if (c < a.C)
-        for (int64_t m = m0 + w; m < m1; m += 4) {
-            const float x = (float)((const T*)a.x)[m * a.x_ld + c];
-            const uint64_t b = bits_of(a.mul ? (double)x * (double)a.mul[m] : (double)x);
-            big = b > big ? b : big;
-            sum += x;
-        }
-    rm[w][lane] = big;
-    rs[w][lane] = sum;
-    __syncthreads();
-    if (w != 0 || c >= a.C) return;
-    for (int i = 1; i < 4; i++) {
-        big = rm[i][lane] > big ? rm[i][lane] : big;
-        sum += rs[i][lane];
+    for (int64_t m = m0; m < m1; m++) {
+        const float x = (float)((const T*)a.x)[m * a.x_ld + c];
+        const uint64_t b = bits_of(a.mul ? (double)x * (double)a.mul[m] : (double)x);
+        big = b > big ? b : big;
+        sum += x;
     }
     a.pmax[(int64_t)blockIdx.y * a.C + c] = big;
     a.psum[(int64_t)blockIdx.y * a.C + c] = sum;
@@ -129,6 +345,7 @@ __global__ __launch_bounds__(256) void k_cols_scale(RqRowArgs a, int strips)
     if (c >= a.C) return;
     uint64_t big = 0;
     float sum = 0.f;
+#pragma unroll 8
     for (int i = 0; i < strips; i++) {
         const uint64_t b = a.pmax[(int64_t)i * a.C + c];
         big = b > big ? b : big;
@@ -140,89 +357,183 @@ __global__ __launch_bounds__(256) void k_cols_scale(RqRowArgs a, int strips)
     if (!(s == s)) set_status(a.status, ISEG_DEV_NONFINITE);
 }
 
-// codes of a 64 x 64 tile, turned in LDS (rows of 68 bytes: a column of the
-// tile then falls on 16 different banks)
-template <typename T>
+// Codes of 128 rows by 64 columns, turned in LDS: a thread codes four rows of a
+// column at a time into one word of the column's 128 bytes (33 words apart, so
+// a wave's columns fall on all the banks), and rows of codes leave 16 bytes
+// per lane, a whole line per column.
+template <typename T, bool MUL>
 __global__ __launch_bounds__(256) void k_cols_codes(RqRowArgs a)
 {
-    __shared__ int8_t t[64][68];
+    __shared__ uint32_t t[64][33];
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-    const int lim = (1 << (a.bits - 1)) - 1;
     const int64_t c = (int64_t)blockIdx.x * 64 + lane;
-    const float s = c < a.C ? a.scale[c] : 1.f;
-    const bool ok = s == s;
-    const float inv = 1.f / s;
-    const int64_t mt = ceil_div64(a.M, 64);
+    const int64_t cc = c < a.C ? c : a.C - 1;
+    const Coder k(a.scale[cc], a.bits);
+    const bool wide = (a.codes_ld & 15) == 0 && ((uintptr_t)a.codes & 15) == 0;
+    const int64_t mt = ceil_div64(a.M, 128);
     for (int64_t b = blockIdx.y; b < mt; b += gridDim.y) {
-        const int64_t m0 = b * 64;
-        for (int r = w; r < 64; r += 4) {
-            const int64_t m = m0 + r;
-            if (m < a.M && c < a.C) {
-                const float x = (float)((const T*)a.x)[m * a.x_ld + c];
-                const double v = a.mul ? (double)x * (double)a.mul[m] : (double)x;
-                t[lane][r] = ok ? (int8_t)code_of(v, s, inv, lim) : 0;
+        const int64_t m0 = b * 128;
+#pragma unroll 2
+        for (int q = w; q < 32; q += 4) {
+            float x[4], mu[4];
+#pragma unroll
+            for (int u = 0; u < 4; u++) {
+                const int64_t m = m0 + q * 4 + u < a.M ? m0 + q * 4 + u : a.M - 1;
+                x[u] = (float)((const T*)a.x)[m * a.x_ld + cc];
+                mu[u] = MUL ? a.mul[m] : 1.f;
             }
+            uint32_t o;
+            codes_of<4, MUL>(x, mu, k, &o);
+            t[lane][q] = o;
         }
         __syncthreads();
-        for (int r = w; r < 64; r += 4) {
-            const int64_t cc = (int64_t)blockIdx.x * 64 + r;
-            if (cc < a.C && m0 + lane < a.M) a.codes[cc * a.codes_ld + m0 + lane] = t[r][lane];
+        for (int i = threadIdx.x; i < 64 * 8; i += 256) {
+            const int col = i >> 3, p = i & 7;
+            const int64_t oc = (int64_t)blockIdx.x * 64 + col, m = m0 + p * 16;
+            if (oc < a.C && m < a.M) {
+                uint32_t v[4];
+#pragma unroll
+                for (int u = 0; u < 4; u++) v[u] = t[col][p * 4 + u];
+                int8_t* d = a.codes + oc * a.codes_ld + m;
+                if (wide && m + 16 <= a.M) {
+                    __builtin_memcpy(__builtin_assume_aligned(d, 16), v, 16);
+                } else {
+                    const int n = a.M - m < 16 ? (int)(a.M - m) : 16;
+                    for (int u = 0; u < n; u++) d[u] = (int8_t)(t[col][p * 4 + u / 4] >> (u % 4 * 8));
+                }
+            }
         }
         __syncthreads();
     }
 }
 
+// Transposition of 128 x 128 codes: four rows of four columns per thread are
+// turned by byte permutations into four words of four columns.
 __global__ __launch_bounds__(256) void k_transpose_i8(const int8_t* __restrict__ in, int64_t M, int64_t C,
                                                       int64_t in_ld, int8_t* __restrict__ out, int64_t out_ld)
 {
-    __shared__ int8_t t[64][68];
-    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-    const int64_t c0 = (int64_t)blockIdx.x * 64;
-    const int64_t mt = ceil_div64(M, 64);
+    __shared__ uint32_t t[128][33];           // [column][rows / 4]
+    const int64_t c0 = (int64_t)blockIdx.x * 128;
+    const bool rd = (in_ld & 3) == 0 && ((uintptr_t)in & 3) == 0;
+    const bool wide = (out_ld & 15) == 0 && ((uintptr_t)out & 15) == 0;
+    const int64_t mt = ceil_div64(M, 128);
     for (int64_t b = blockIdx.y; b < mt; b += gridDim.y) {
-        const int64_t m0 = b * 64;
-        for (int r = w; r < 64; r += 4)
-            if (m0 + r < M && c0 + lane < C) t[lane][r] = in[(m0 + r) * in_ld + c0 + lane];
+        const int64_t m0 = b * 128;
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+            const int e = threadIdx.x + i * 256, cq = e & 31, rq = e >> 5;     // columns / 4, rows / 4
+            const int64_t c = c0 + cq * 4;
+            uint32_t r[4];
+#pragma unroll
+            for (int u = 0; u < 4; u++) {
+                const int64_t m = m0 + rq * 4 + u < M ? m0 + rq * 4 + u : M - 1;
+                const int8_t* p = in + m * in_ld + c;
+                r[u] = 0;
+                if (rd && c + 4 <= C) {
+                    r[u] = *(const uint32_t*)p;
+                } else {
+                    for (int x = 0; x < 4; x++)
+                        if (c + x < C) r[u] |= (uint32_t)(uint8_t)p[x] << (8 * x);
+                }
+            }
+            // bytes (x, y) of the 4 x 4 block exchanged
+            const uint32_t a0 = __builtin_amdgcn_perm(r[1], r[0], 0x05010400), a1 = __builtin_amdgcn_perm(r[1], r[0], 0x07030602);
+            const uint32_t b0 = __builtin_amdgcn_perm(r[3], r[2], 0x05010400), b1 = __builtin_amdgcn_perm(r[3], r[2], 0x07030602);
+            t[cq * 4 + 0][rq] = (a0 & 0xffffu) | b0 << 16;
+            t[cq * 4 + 1][rq] = a0 >> 16 | (b0 & 0xffff0000u);
+            t[cq * 4 + 2][rq] = (a1 & 0xffffu) | b1 << 16;
+            t[cq * 4 + 3][rq] = a1 >> 16 | (b1 & 0xffff0000u);
+        }
         __syncthreads();
-        for (int r = w; r < 64; r += 4)
-            if (c0 + r < C && m0 + lane < M) out[(c0 + r) * out_ld + m0 + lane] = t[r][lane];
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+            const int e = threadIdx.x + i * 256, col = e >> 3, p = e & 7;
+            const int64_t oc = c0 + col, m = m0 + p * 16;
+            if (oc < C && m < M) {
+                int8_t* d = out + oc * out_ld + m;
+                if (wide && m + 16 <= M) {
+                    uint32_t v[4];
+#pragma unroll
+                    for (int u = 0; u < 4; u++) v[u] = t[col][p * 4 + u];
+                    __builtin_memcpy(__builtin_assume_aligned(d, 16), v, 16);
+                } else {
+                    const int n = M - m < 16 ? (int)(M - m) : 16;
+                    for (int u = 0; u < n; u++) d[u] = (int8_t)(t[col][p * 4 + u / 4] >> (u % 4 * 8));
+                }
+            }
+        }
         __syncthreads();
     }
 }
 
 constexpr int64_t kMaxCols = (int64_t)1 << 31;
 
-// strips of rows whose partials a column's scale is taken from
+// strips of rows whose partials a column's scale is taken from: blocks for the
+// chip, at least 128 rows each
 int64_t cols_strips(int64_t M, int64_t C)
 {
     const int64_t tiles = ceil_div64(C, 64);
-    int64_t n = ceil_div64(2048, tiles > 0 ? tiles : 1);
-    const int64_t most = ceil_div64(M, 64);
+    int64_t n = ceil_div64(1024, tiles > 0 ? tiles : 1);
+    const int64_t most = ceil_div64(M, 128);
     n = n < most ? n : most;
     return n > 0 ? (n < 256 ? n : 256) : 1;
+}
+
+template <typename T, bool MUL, int NW, int VPT>
+int rows_grid(const RqRowArgs& a, hipStream_t s)
+{
+    constexpr int R = NW < 4 ? 4 / NW : 1;
+    const int64_t nb = ceil_div64(a.M, R);
+    hipLaunchKernelGGL((k_quantize_rows<T, MUL, NW, VPT>), dim3((unsigned)(nb < 4096 ? nb : 4096)),
+                       dim3(NW < 4 ? 256 : NW * 64), 0, s, a);
+    return launch_ok();
+}
+
+template <typename T, bool MUL>
+int launch_rows_mul(const RqRowArgs& a, hipStream_t s)
+{
+    constexpr int N = RowVec<T>::N;
+    const int64_t v = ceil_div64(a.C, N);
+    if (a.C >= N) {
+        if (v <= 64) return rows_grid<T, MUL, 1, 1>(a, s);
+        if (v <= 256) return rows_grid<T, MUL, 4, 1>(a, s);
+        if (v <= 512) return rows_grid<T, MUL, 4, 2>(a, s);
+        if (v <= 1024) return rows_grid<T, MUL, 8, 2>(a, s);
+        if (v <= 2048) return rows_grid<T, MUL, 16, 2>(a, s);
+    }
+    const unsigned grid = (unsigned)(a.M < kRowGridMax ? a.M : kRowGridMax);
+    hipLaunchKernelGGL(k_quantize_rows_long<T>, dim3(grid), dim3(256), 0, s, a);
+    return launch_ok();
 }
 
 template <typename T>
 int launch_rows(const RqRowArgs& a, hipStream_t s)
 {
-    const unsigned grid = (unsigned)(a.M < kRowGridMax ? a.M : kRowGridMax);
-    hipLaunchKernelGGL(k_quantize_rows<T>, dim3(grid), dim3(256), 0, s, a);
+    return a.mul ? launch_rows_mul<T, true>(a, s) : launch_rows_mul<T, false>(a, s);
+}
+
+template <typename T, bool MUL>
+int launch_cols_mul(const RqRowArgs& a, hipStream_t s)
+{
+    const unsigned ct = (unsigned)ceil_div64(a.C, 64);
+    const int64_t strips = cols_strips(a.M, a.C);
+    const int64_t strip = ceil_div64(a.M, strips);
+    if (a.C >= RowVec<T>::N)
+        hipLaunchKernelGGL((k_cols_stats<T, MUL>), dim3(ct, (unsigned)strips), dim3(256), 0, s, a, strip);
+    else
+        hipLaunchKernelGGL(k_cols_stats_narrow<T>, dim3(1, (unsigned)strips), dim3(64), 0, s, a, strip);
+    hipLaunchKernelGGL(k_cols_scale, dim3((unsigned)ceil_div64(a.C, 256)), dim3(256), 0, s, a, (int)strips);
+    if (a.M > 0) {
+        const int64_t mt = ceil_div64(a.M, 128);
+        hipLaunchKernelGGL((k_cols_codes<T, MUL>), dim3(ct, (unsigned)(mt < 1024 ? mt : 1024)), dim3(256), 0, s, a);
+    }
     return launch_ok();
 }
 
 template <typename T>
 int launch_cols(const RqRowArgs& a, hipStream_t s)
 {
-    const unsigned ct = (unsigned)ceil_div64(a.C, 64);
-    const int64_t strips = cols_strips(a.M, a.C);
-    const int64_t strip = ceil_div64(a.M, strips);
-    hipLaunchKernelGGL(k_cols_stats<T>, dim3(ct, (unsigned)strips), dim3(256), 0, s, a, strip);
-    hipLaunchKernelGGL(k_cols_scale, dim3((unsigned)ceil_div64(a.C, 256)), dim3(256), 0, s, a, (int)strips);
-    if (a.M > 0) {
-        const int64_t mt = ceil_div64(a.M, 64);
-        hipLaunchKernelGGL(k_cols_codes<T>, dim3(ct, (unsigned)(mt < 1024 ? mt : 1024)), dim3(256), 0, s, a);
-    }
-    return launch_ok();
+    return a.mul ? launch_cols_mul<T, true>(a, s) : launch_cols_mul<T, false>(a, s);
 }
 
 int rq_check(int32_t x_dtype, int32_t bits, int32_t mode)
@@ -283,8 +594,8 @@ extern "C" int iseg_transpose_i8(const int8_t* in, int64_t M, int64_t C, int64_t
     if (M < 0 || C < 0 || C >= kMaxCols || in_ld < C || out_ld < M) return ISEG_ERR_SHAPE;
     if (M == 0 || C == 0) return ISEG_OK;
     if (!in || !out) return ISEG_ERR_ARG;
-    const int64_t mt = ceil_div64(M, 64);
-    hipLaunchKernelGGL(k_transpose_i8, dim3((unsigned)ceil_div64(C, 64), (unsigned)(mt < 1024 ? mt : 1024)),
+    const int64_t mt = ceil_div64(M, 128);
+    hipLaunchKernelGGL(k_transpose_i8, dim3((unsigned)ceil_div64(C, 128), (unsigned)(mt < 1024 ? mt : 1024)),
                        dim3(256), 0, stream, in, M, C, in_ld, out, out_ld);
     return launch_ok();
 }

@@ -181,6 +181,22 @@ def test_quantize_decides_half_steps_exactly():
             assert torch.equal(sc.cpu(), ws) and torch.equal(q.cpu(), wq), big
 
 
+def test_quantize_products_near_half_steps():
+    """x mul on half-steps where the float32 product is not: the exact product decides."""
+    from paper_2011_14504_amd import iseg
+    gen = torch.Generator().manual_seed(3)
+    for C in (5, 200, 3000):
+        mul = (torch.rand(C, generator=gen) + 0.5).float()
+        n = torch.randint(-127, 127, (40, C), generator=gen).double() + 0.5
+        x = (n * 0.01 / mul.double()).float()
+        x[:, 0] = (1.27 / mul[0].double()).float() * (1 + 2.0 ** -23 * torch.arange(40))
+        wq, ws = quantized(x.double() * mul.double(), 8, False)
+        q, s = iseg.quantize_rows(x.to(DEV), mul=mul.to(DEV))
+        assert torch.equal(s.cpu(), ws) and torch.equal(q.cpu(), wq)
+        q, s, _ = iseg.quantize_cols(x.t().contiguous().to(DEV), mul=mul.to(DEV))
+        assert torch.equal(s.cpu(), ws) and torch.equal(q.cpu(), wq)
+
+
 def test_quantize_tiny_huge_and_non_finite():
     from paper_2011_14504_amd import iseg
     x = torch.zeros(6, 40)
@@ -220,6 +236,18 @@ def test_quantize_tiny_huge_and_non_finite():
     # and one that leaves it below
     q, s = iseg.quantize_rows(torch.full((1, 4), 1e-38, device=DEV), mul=torch.full((4,), 1e-30, device=DEV))
     assert float(s[0]) == 2.0 ** -126 and not bool(q.any())
+    q, s, _ = iseg.quantize_cols(torch.full((3, 9), 1e-38, device=DEV), mul=torch.full((3,), 1e-30, device=DEV))
+    assert bool((s == 2.0 ** -126).all()) and not bool(q.any())
+    # float32 products past the range whose scale is inside it
+    for C in (3, 40):
+        x = torch.full((3, C), 1e38, dtype=torch.float64)
+        x[1, 0], x[2] = 3e38, -2.9e38
+        mul = torch.linspace(60, 100, C, dtype=torch.float64).float()
+        wq, ws = quantized(x.float().double() * mul.double(), 8, False)
+        q, s = iseg.quantize_rows(x.float().to(DEV), mul=mul.to(DEV))
+        assert torch.equal(s.cpu(), ws) and torch.equal(q.cpu(), wq)
+        q, s, _ = iseg.quantize_cols(x.float().t().contiguous().to(DEV), mul=mul.to(DEV))
+        assert torch.equal(s.cpu(), ws) and torch.equal(q.cpu(), wq)
 
 
 def test_quantize_empty():
