@@ -149,6 +149,7 @@ template <typename T, typename P, int NW, int VPT>
 int fwd_grid(const LnArgs& a, unsigned cap, hipStream_t s)
 {
     constexpr int R = NW < 4 ? 4 / NW : 1;
+    if (!slots_fit<T, NW, VPT>(a.C)) return ISEG_ERR_UNSUPPORTED;
     const int64_t nb = ceil_div64(a.M, R);
     hipLaunchKernelGGL((k_layernorm_fwd<T, P, NW, VPT>), dim3((unsigned)(nb < cap ? nb : cap)),
                        dim3(NW < 4 ? 256 : NW * 64), 0, s, a);
@@ -361,6 +362,14 @@ int ln_bwd_blocks(const iseg_layernorm_geom* g)
     return (int)(g->M < cap ? g->M : cap);
 }
 
+template <typename T, typename P, int NW, int VPT>
+int bwd_grid(const LnArgs& a, int nb, hipStream_t s)
+{
+    if (!slots_fit<T, NW, VPT>(a.C)) return ISEG_ERR_UNSUPPORTED;
+    hipLaunchKernelGGL((k_layernorm_bwd<T, P, NW, VPT>), dim3(nb), dim3(NW * 64), 0, s, a);
+    return launch_ok();
+}
+
 template <typename T, typename P>
 int launch_bwd(const LnArgs& a, const iseg_layernorm_geom* g, hipStream_t s)
 {
@@ -368,25 +377,28 @@ int launch_bwd(const LnArgs& a, const iseg_layernorm_geom* g, hipStream_t s)
     const int nb = ln_bwd_blocks(g);
     const int64_t v = ceil_div64(a.C, N);
     if (nb > 0) {
+        int rc;
         if (!ln_bwd_in_regs(g)) {
             float2* sums = (float2*)((char*)a.part + align256((size_t)nb * 2 * a.C * 4));
             const unsigned gr = (unsigned)(a.M < kRowGridMax ? a.M : kRowGridMax);
             hipLaunchKernelGGL((k_layernorm_bwd_rows<T, P>), dim3(gr), dim3(1024), 0, s, a, sums);
             hipLaunchKernelGGL((k_layernorm_bwd_cols<T, P>), dim3((unsigned)ceil_div64(a.C, 256), nb), dim3(256), 0,
                                s, a, (const float2*)sums);
+            rc = launch_ok();
         } else if (v <= 64) {
-            hipLaunchKernelGGL((k_layernorm_bwd<T, P, 1, 1>), dim3(nb), dim3(64), 0, s, a);
+            rc = bwd_grid<T, P, 1, 1>(a, nb, s);
         } else if (v <= 128) {
-            hipLaunchKernelGGL((k_layernorm_bwd<T, P, 1, 2>), dim3(nb), dim3(64), 0, s, a);
+            rc = bwd_grid<T, P, 1, 2>(a, nb, s);
         } else if (v <= 256) {
-            hipLaunchKernelGGL((k_layernorm_bwd<T, P, 4, 1>), dim3(nb), dim3(256), 0, s, a);
+            rc = bwd_grid<T, P, 4, 1>(a, nb, s);
         } else if (v <= 512) {
-            hipLaunchKernelGGL((k_layernorm_bwd<T, P, 8, 1>), dim3(nb), dim3(512), 0, s, a);
+            rc = bwd_grid<T, P, 8, 1>(a, nb, s);
         } else if (v <= 1024) {
-            hipLaunchKernelGGL((k_layernorm_bwd<T, P, 8, 2>), dim3(nb), dim3(512), 0, s, a);
+            rc = bwd_grid<T, P, 8, 2>(a, nb, s);
         } else {
-            hipLaunchKernelGGL((k_layernorm_bwd<T, P, 8, 3>), dim3(nb), dim3(512), 0, s, a);
+            rc = bwd_grid<T, P, 8, 3>(a, nb, s);
         }
+        if (rc != ISEG_OK) return rc;
     }
     if (a.dgamma || a.dbeta)
         hipLaunchKernelGGL((k_layernorm_param_sum<P>), dim3((unsigned)ceil_div64(a.C, 64), 2), dim3(1024), 0, s, a.part,

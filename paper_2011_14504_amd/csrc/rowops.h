@@ -156,6 +156,15 @@ __device__ __forceinline__ ParamVec<P, N> param_load(const P* p, const RowSlot<N
     return r;
 }
 
+// whether VPT vectors per thread of NW waves hold a row of C elements with only
+// the last vector of a thread short (what the row kernels take for granted)
+template <typename T, int NW, int VPT>
+static inline bool slots_fit(int64_t C)
+{
+    const int64_t v = ceil_div64(C, RowVec<T>::N), nt = NW * 64;
+    return C >= RowVec<T>::N && v > nt * (VPT - 1) && v <= nt * VPT;
+}
+
 static inline bool is_float_dtype(int32_t t) { return t == ISEG_F32 || t == ISEG_F16 || t == ISEG_BF16; }
 
 // launches walk their rows in a loop, so the grid may be cut at any count

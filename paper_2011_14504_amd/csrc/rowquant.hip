@@ -1,14 +1,16 @@
 // rowquant.hip -- quantizers with a scale for each row or each column, and the
 // transposition of int8 codes: the operands of iseg_matmul_i8.
 //
-// Every decision is exact although the bulk of the work is float32.  With
-// h = fl(x mul) (x itself without mul), |h| grows with |x mul|, so the largest
-// exact magnitude is found among the elements with the largest |h|, and only
-// those are formed in double (24 x 24 bits).  Magnitudes are compared as bit
-// patterns, where a NaN or an infinity is larger than every finite value.  A
-// code is floor(h / s + 1/2); where h / s + 1/2 lies within 2^-14 of an integer
-// (its error, of three roundings of at most 128, is below 2^-15), the sign of
-// x mul - (n + 1/2) s in double settles it (the product is exact).
+// Every decision is exact although the work is float32.  With h = fl(x mul) (x
+// itself without mul) and l = x mul - h (exact by one fma), |h| grows with
+// |x mul|, so the largest exact magnitude is found among the elements with the
+// largest |h|, and only those are formed in double (24 x 24 bits).  Magnitudes
+// are compared as bit patterns, where a NaN or an infinity is larger than
+// every finite value.  A code is n = floor(h / s + 1/2); where h / s + 1/2
+// lies within 2^-14 of an integer (its error, of three roundings of at most
+// 128, is below 2^-15), the sign of h - (n -+ 1/2) s + l settles it: (n + 1/2)
+// s has 33 bits, its difference from h so near a half-step fits 24, and the
+// last sum's sign is right however it rounds.
 #include "rowops.h"
 
 namespace {
@@ -50,58 +52,82 @@ __device__ __forceinline__ float scale_of(uint64_t big, int bits, int mode)
 __device__ __forceinline__ uint64_t bits_of(double v) { return __builtin_bit_cast(uint64_t, v) & kAbs64; }
 __device__ __forceinline__ uint32_t bits_of(float v) { return __builtin_bit_cast(uint32_t, v) & 0x7fffffffu; }
 
-// How codes follow from a scale.  Scales above 2^100 (whose reciprocal may be
-// subnormal) and values whose float32 product overflows take the exact way.
+// How codes follow from a scale.  Outside [2^-60, 2^100], where a reciprocal,
+// a product or its remainder may be subnormal or overflow, every code is
+// formed in double.
 struct Coder {
-    double sd;
-    float inv;
-    int lim;
-    bool exact, ok;
-    __device__ __forceinline__ Coder(float s, int bits)
-        : sd(s), inv(1.f / s), lim((1 << (bits - 1)) - 1), exact(!(s <= 1.2676506e30f)), ok(s == s)
+    float s, inv;
+    bool ok, wide;
+    __device__ __forceinline__ Coder() {}
+    __device__ __forceinline__ explicit Coder(float s_)
+        : s(s_), inv(1.f / s_), ok(s_ == s_), wide(!(s_ >= 8.6736174e-19f && s_ <= 1.2676506e30f))
     {
     }
 };
 
 // clamp(floor(v / s + 1/2), +-lim) of the exact v: an estimate within one,
 // then the half-steps on either side of it
-__device__ __forceinline__ int code_exact(double v, const Coder& k)
+__device__ __forceinline__ int code_wide(double v, const Coder& k, int lim)
 {
-    const double q = fmin(fmax(v * (1.0 / k.sd), -128.0), 128.0);
+    const double sd = (double)k.s, q = fmin(fmax(v / sd, -128.0), 128.0);
     int n = (int)floor(q + 0.5);
-    if (v - ((double)n + 0.5) * k.sd >= 0.0) n++;
-    else if (v - ((double)n - 0.5) * k.sd < 0.0) n--;
-    return n > k.lim ? k.lim : (n < -k.lim ? -k.lim : n);
+    if (v - ((double)n + 0.5) * sd >= 0.0) n++;
+    else if (v - ((double)n - 0.5) * sd < 0.0) n--;
+    return n > lim ? lim : (n < -lim ? -lim : n);
 }
 
-// the same from h = fl(v); `far` becomes the largest distance of h / s + 1/2
-// from a half-integer seen so far (above 1/2 - 2^-14: near an integer)
-__device__ __forceinline__ int code_fast(float h, const Coder& k, float& far)
+// floor(h / s + 1/2) within one; `far` becomes the largest distance of h / s +
+// 1/2 from a half-integer seen so far (kNear and above: near an integer)
+__device__ __forceinline__ float code_fast(float h, const Coder& k, float& far)
 {
     const float q = fmaf(h, k.inv, 0.5f), f = floorf(q);
     far = fmaxf(far, fabsf(q - f - 0.5f));
-    const float c = (float)k.lim;
-    return (int)fminf(fmaxf(f, -c), c);
+    return f;
 }
 constexpr float kNear = 0.5f - 6.1035156e-5f;
 
-// codes of N values x (times m, exactly) as N bytes
-template <int N, bool MUL>
-__device__ __forceinline__ void codes_of(const float* x, const float* m, const Coder& k, uint32_t* out)
+__device__ __forceinline__ float code_near(float n, float h, float l, const Coder& k)
 {
+    if (fmaf(-(n + 0.5f), k.s, h) + l >= 0.f) return n + 1.f;
+    return fmaf(-(n - 0.5f), k.s, h) + l < 0.f ? n - 1.f : n;
+}
+
+__device__ __forceinline__ uint32_t pack4(const int* n)
+{
+    return (uint32_t)(uint8_t)n[0] | (uint32_t)(uint8_t)n[1] << 8 | (uint32_t)(uint8_t)n[2] << 16 | (uint32_t)n[3] << 24;
+}
+
+// codes of N values x (times m, exactly) as N bytes; coder(i) is element i's
+template <int N, bool MUL, typename F>
+__device__ __forceinline__ void codes_of(const float* x, const float* m, F coder, int lim, uint32_t* out)
+{
+    float f[N], far = 0.f;
+    bool wide = false;
+#pragma unroll
+    for (int i = 0; i < N; i++) {
+        f[i] = code_fast(MUL ? x[i] * m[i] : x[i], coder(i), far);
+        wide |= coder(i).wide;
+    }
+    if (!(far < kNear)) {
+#pragma unroll
+        for (int i = 0; i < N; i++) {
+            const float h = MUL ? x[i] * m[i] : x[i];
+            f[i] = code_near(f[i], h, MUL ? fmaf(x[i], m[i], -h) : 0.f, coder(i));
+        }
+    }
     int n[N];
-    float far = 0.f;
+    const float c = (float)lim;
 #pragma unroll
-    for (int i = 0; i < N; i++) n[i] = code_fast(MUL ? x[i] * m[i] : x[i], k, far);
-    if (k.exact || !(far < kNear)) {
+    for (int i = 0; i < N; i++) n[i] = (int)fminf(fmaxf(f[i], -c), c);
+    if (wide) {
 #pragma unroll
-        for (int i = 0; i < N; i++) n[i] = code_exact(MUL ? (double)x[i] * (double)m[i] : (double)x[i], k);
+        for (int i = 0; i < N; i++) {
+            const Coder& k = coder(i);
+            if (k.wide) n[i] = k.ok ? code_wide(MUL ? (double)x[i] * (double)m[i] : (double)x[i], k, lim) : 0;
+        }
     }
 #pragma unroll
-    for (int i = 0; i < N / 4; i++)
-        out[i] = !k.ok ? 0u
-                       : (uint32_t)(uint8_t)n[4 * i] | (uint32_t)(uint8_t)n[4 * i + 1] << 8 |
-                             (uint32_t)(uint8_t)n[4 * i + 2] << 16 | (uint32_t)n[4 * i + 3] << 24;
+    for (int i = 0; i < N / 4; i++) out[i] = pack4(n + 4 * i);
 }
 
 // ---------------------------------------------------------------------------
@@ -141,12 +167,22 @@ __global__ __launch_bounds__(NW < 4 ? 256 : NW * 64) void k_quantize_rows(RqRowA
         sl[j] = j < VPT - 1 ? RowSlot<N>{c, 0} : row_slot<N>(c, a.C);
         if (MUL) mv[j] = param_load<float, N>(a.mul, sl[j], 0.f);
     }
+    const int lim = (1 << (a.bits - 1)) - 1;
+    RowVec<T> nv[VPT];
+    int64_t m = (int64_t)blockIdx.x * R + threadIdx.x / NT;
+    const int64_t step = (int64_t)gridDim.x * R;
+    auto fetch = [&](int64_t r) {
+#pragma unroll
+        for (int j = 0; j < VPT; j++) nv[j] = slot_load<T, N>((const T*)a.x + r * a.x_ld, sl[j]);
+    };
+    if (m < a.M) fetch(m);
     int flip = 0;
-    for (int64_t m = (int64_t)blockIdx.x * R + threadIdx.x / NT; m < a.M; m += (int64_t)gridDim.x * R, flip ^= 1) {
+    for (; m < a.M; m += step, flip ^= 1) {
         RowVec<T> xv[VPT];
         uint32_t big = 0;
 #pragma unroll
-        for (int j = 0; j < VPT; j++) xv[j] = slot_load<T, N>((const T*)a.x + m * a.x_ld, sl[j]);
+        for (int j = 0; j < VPT; j++) xv[j] = nv[j];
+        if (m + step < a.M) fetch(m + step);
 #pragma unroll
         for (int j = 0; j < VPT; j++)
 #pragma unroll
@@ -183,7 +219,7 @@ __global__ __launch_bounds__(NW < 4 ? 256 : NW * 64) void k_quantize_rows(RqRowA
             tb = bits_of((double)__builtin_bit_cast(float, big));
         }
         const float s = scale_of(tb, a.bits, a.mode);
-        const Coder k(s, a.bits);
+        const Coder k(s);
         if (tid == 0) {
             a.scale[m] = s;
             if (!k.ok) set_status(a.status, ISEG_DEV_NONFINITE);
@@ -194,7 +230,7 @@ __global__ __launch_bounds__(NW < 4 ? 256 : NW * 64) void k_quantize_rows(RqRowA
 #pragma unroll
             for (int i = 0; i < N; i++) x[i] = (float)xv[j].v[i];
             uint32_t o[N / 4];
-            codes_of<N, MUL>(x, mv[j].v, k, o);
+            codes_of<N, MUL>(x, mv[j].v, [&](int) -> const Coder& { return k; }, lim, o);
             if (j < VPT - 1 || sl[j].dup < N) __builtin_memcpy(a.codes + m * a.codes_ld + sl[j].at, o, N);
         }
     }
@@ -205,7 +241,7 @@ __global__ __launch_bounds__(NW < 4 ? 256 : NW * 64) void k_quantize_rows(RqRowA
 template <typename T>
 __global__ __launch_bounds__(256) void k_quantize_rows_long(RqRowArgs a)
 {
-    const int tid = threadIdx.x;
+    const int tid = threadIdx.x, lim = (1 << (a.bits - 1)) - 1;
     for (int64_t m = blockIdx.x; m < a.M; m += gridDim.x) {
         const T* x = (const T*)a.x + m * a.x_ld;
         int8_t* o = a.codes + m * a.codes_ld;
@@ -217,14 +253,14 @@ __global__ __launch_bounds__(256) void k_quantize_rows_long(RqRowArgs a)
         }
         big = block_max_u64(big);
         const float s = scale_of(big, a.bits, a.mode);
-        const Coder k(s, a.bits);
+        const Coder k(s);
         if (tid == 0) {
             a.scale[m] = s;
             if (!k.ok) set_status(a.status, ISEG_DEV_NONFINITE);
         }
         for (int64_t c = tid; c < a.C; c += 256) {
             const double v = a.mul ? (double)(float)x[c] * (double)a.mul[c] : (double)(float)x[c];
-            o[c] = k.ok ? (int8_t)code_exact(v, k) : 0;
+            o[c] = k.ok ? (int8_t)code_wide(v, k, lim) : 0;
         }
     }
 }
@@ -339,71 +375,152 @@ __global__ __launch_bounds__(64) void k_cols_stats_narrow(RqRowArgs a, int64_t s
     a.psum[(int64_t)blockIdx.y * a.C + c] = sum;
 }
 
-__global__ __launch_bounds__(256) void k_cols_scale(RqRowArgs a, int strips)
+// scale and sum of a column from the strips' partials
+__device__ __forceinline__ float col_scale(const RqRowArgs& a, int64_t c, int strips, float* sum)
 {
-    const int64_t c = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (c >= a.C) return;
     uint64_t big = 0;
-    float sum = 0.f;
-#pragma unroll 8
-    for (int i = 0; i < strips; i++) {
-        const uint64_t b = a.pmax[(int64_t)i * a.C + c];
-        big = b > big ? b : big;
-        sum += a.psum[(int64_t)i * a.C + c];
+    float s = 0.f;
+    for (int i0 = 0; i0 < strips; i0 += 8) {
+        uint64_t b[8];
+        float t[8];
+#pragma unroll
+        for (int u = 0; u < 8; u++) {         // past the end: the first of the eight again, counted as nothing
+            const int64_t at = (int64_t)(i0 + u < strips ? i0 + u : i0) * a.C + c;
+            b[u] = a.pmax[at];
+            t[u] = a.psum[at];
+        }
+#pragma unroll
+        for (int u = 0; u < 8; u++) {
+            big = b[u] > big ? b[u] : big;
+            s += i0 + u < strips ? t[u] : 0.f;
+        }
     }
-    const float s = scale_of(big, a.bits, a.mode);
-    a.scale[c] = s;
-    if (a.sums) a.sums[c] = sum;
-    if (!(s == s)) set_status(a.status, ISEG_DEV_NONFINITE);
+    *sum = s;
+    return scale_of(big, a.bits, a.mode);
 }
 
-// Codes of 128 rows by 64 columns, turned in LDS: a thread codes four rows of a
-// column at a time into one word of the column's 128 bytes (33 words apart, so
-// a wave's columns fall on all the banks), and rows of codes leave 16 bytes
-// per lane, a whole line per column.
-template <typename T, bool MUL>
-__global__ __launch_bounds__(256) void k_cols_codes(RqRowArgs a)
+// four words of four bytes each, turned: word x of the result holds byte x of
+// every r[u]
+__device__ __forceinline__ void turn4(const uint32_t* r, uint32_t* o)
 {
+    const uint32_t a0 = __builtin_amdgcn_perm(r[1], r[0], 0x05010400), a1 = __builtin_amdgcn_perm(r[1], r[0], 0x07030602);
+    const uint32_t b0 = __builtin_amdgcn_perm(r[3], r[2], 0x05010400), b1 = __builtin_amdgcn_perm(r[3], r[2], 0x07030602);
+    o[0] = (a0 & 0xffffu) | b0 << 16;
+    o[1] = a0 >> 16 | (b0 & 0xffff0000u);
+    o[2] = (a1 & 0xffffu) | b1 << 16;
+    o[3] = a1 >> 16 | (b1 & 0xffff0000u);
+}
+
+// 16 codes of a column from words t[0 .. 3] to d; n (1 .. 16) of them exist
+__device__ __forceinline__ void put16(const uint32_t* t, int8_t* d, int64_t n, bool wide)
+{
+    uint32_t v[4];
+#pragma unroll
+    for (int u = 0; u < 4; u++) v[u] = t[u];
+    if (wide && n >= 16) {
+        __builtin_memcpy(__builtin_assume_aligned(d, 16), v, 16);
+    } else {
+        const int e = n < 16 ? (int)n : 16;
+        for (int u = 0; u < e; u++) d[u] = (int8_t)(t[u / 4] >> (u % 4 * 8));
+    }
+}
+
+// Codes of 128 rows by 64 columns per step, turned by byte permutations and
+// LDS: a thread codes one vector of N columns in each of four rows and leaves a
+// word of four rows for each column (33 words apart, so a wave's columns fall
+// on all the banks); rows of codes leave 16 bytes per lane, a whole line per
+// column.  The block takes the scales from the strips' partials itself.
+template <typename T, bool MUL>
+__global__ __launch_bounds__(256) void k_cols_codes(RqRowArgs a, int strips)
+{
+    constexpr int N = RowVec<T>::N, G = 64 / N, RS = 256 / G;       // vectors across, row quads at once
     __shared__ uint32_t t[64][33];
-    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-    const int64_t c = (int64_t)blockIdx.x * 64 + lane;
-    const int64_t cc = c < a.C ? c : a.C - 1;
-    const Coder k(a.scale[cc], a.bits);
+    __shared__ float sc[64];
+    const int tid = threadIdx.x, g = tid % G, rq0 = tid / G;
+    const int64_t c0 = (int64_t)blockIdx.x * 64;
+    const int lim = (1 << (a.bits - 1)) - 1;
+    if (tid < 64) {
+        const int64_t c = c0 + tid;
+        float s = 1.f, sum = 0.f;
+        if (c < a.C) {
+            s = col_scale(a, c, strips, &sum);
+            if (blockIdx.y == 0) {
+                a.scale[c] = s;
+                if (a.sums) a.sums[c] = sum;
+                if (!(s == s)) set_status(a.status, ISEG_DEV_NONFINITE);
+            }
+        }
+        sc[tid] = s;
+    }
+    __syncthreads();
+    const RowSlot<N> sl = row_slot<N>(c0 + g * N, a.C);
+    Coder k[N];
+#pragma unroll
+    for (int i = 0; i < N; i++) k[i] = Coder(i >= sl.dup ? sc[sl.at - c0 + i] : 1.f);      // a repeated column's codes are dropped
     const bool wide = (a.codes_ld & 15) == 0 && ((uintptr_t)a.codes & 15) == 0;
     const int64_t mt = ceil_div64(a.M, 128);
     for (int64_t b = blockIdx.y; b < mt; b += gridDim.y) {
         const int64_t m0 = b * 128;
-#pragma unroll 2
-        for (int q = w; q < 32; q += 4) {
-            float x[4], mu[4];
+#pragma unroll
+        for (int rq = rq0; rq < 32; rq += RS) {
+            RowVec<T> xv[4];
+            float mu[4];
 #pragma unroll
             for (int u = 0; u < 4; u++) {
-                const int64_t m = m0 + q * 4 + u < a.M ? m0 + q * 4 + u : a.M - 1;
-                x[u] = (float)((const T*)a.x)[m * a.x_ld + cc];
+                const int64_t m = m0 + rq * 4 + u < a.M ? m0 + rq * 4 + u : a.M - 1;
+                xv[u] = slot_load<T, N>((const T*)a.x + m * a.x_ld, sl);
                 mu[u] = MUL ? a.mul[m] : 1.f;
             }
-            uint32_t o;
-            codes_of<4, MUL>(x, mu, k, &o);
-            t[lane][q] = o;
-        }
-        __syncthreads();
-        for (int i = threadIdx.x; i < 64 * 8; i += 256) {
-            const int col = i >> 3, p = i & 7;
-            const int64_t oc = (int64_t)blockIdx.x * 64 + col, m = m0 + p * 16;
-            if (oc < a.C && m < a.M) {
-                uint32_t v[4];
+            uint32_t w[4][N / 4];
 #pragma unroll
-                for (int u = 0; u < 4; u++) v[u] = t[col][p * 4 + u];
-                int8_t* d = a.codes + oc * a.codes_ld + m;
-                if (wide && m + 16 <= a.M) {
-                    __builtin_memcpy(__builtin_assume_aligned(d, 16), v, 16);
-                } else {
-                    const int n = a.M - m < 16 ? (int)(a.M - m) : 16;
-                    for (int u = 0; u < n; u++) d[u] = (int8_t)(t[col][p * 4 + u / 4] >> (u % 4 * 8));
+            for (int u = 0; u < 4; u++) {
+                float x[N], mm[N];
+#pragma unroll
+                for (int i = 0; i < N; i++) {
+                    x[i] = (float)xv[u].v[i];
+                    mm[i] = mu[u];
                 }
+                codes_of<N, MUL>(x, mm, [&](int i) -> const Coder& { return k[i]; }, lim, w[u]);
+            }
+#pragma unroll
+            for (int q = 0; q < N / 4; q++) {
+                const uint32_t r[4] = {w[0][q], w[1][q], w[2][q], w[3][q]};
+                uint32_t o[4];
+                turn4(r, o);
+#pragma unroll
+                for (int i = 0; i < 4; i++)
+                    if (q * 4 + i >= sl.dup) t[sl.at - c0 + q * 4 + i][rq] = o[i];
             }
         }
         __syncthreads();
+#pragma unroll
+        for (int i = tid; i < 64 * 8; i += 256) {
+            const int col = i >> 3, p = i & 7;
+            const int64_t oc = c0 + col, m = m0 + p * 16;
+            if (oc < a.C && m < a.M) put16(&t[col][p * 4], a.codes + oc * a.codes_ld + m, a.M - m, wide);
+        }
+        __syncthreads();
+    }
+}
+
+// the same for fewer columns than a vector, a code at a time
+template <typename T>
+__global__ __launch_bounds__(256) void k_cols_codes_narrow(RqRowArgs a, int strips)
+{
+    const int64_t c = blockIdx.x;
+    const int lim = (1 << (a.bits - 1)) - 1;
+    float sum;
+    const float s = col_scale(a, c, strips, &sum);
+    const Coder k(s);
+    if (blockIdx.y == 0 && threadIdx.x == 0) {
+        a.scale[c] = s;
+        if (a.sums) a.sums[c] = sum;
+        if (!k.ok) set_status(a.status, ISEG_DEV_NONFINITE);
+    }
+    for (int64_t m = (int64_t)blockIdx.y * 256 + threadIdx.x; m < a.M; m += (int64_t)gridDim.y * 256) {
+        const float x = (float)((const T*)a.x)[m * a.x_ld + c];
+        const double v = a.mul ? (double)x * (double)a.mul[m] : (double)x;
+        a.codes[c * a.codes_ld + m] = k.ok ? (int8_t)code_wide(v, k, lim) : 0;
     }
 }
 
@@ -436,31 +553,17 @@ __global__ __launch_bounds__(256) void k_transpose_i8(const int8_t* __restrict__
                         if (c + x < C) r[u] |= (uint32_t)(uint8_t)p[x] << (8 * x);
                 }
             }
-            // bytes (x, y) of the 4 x 4 block exchanged
-            const uint32_t a0 = __builtin_amdgcn_perm(r[1], r[0], 0x05010400), a1 = __builtin_amdgcn_perm(r[1], r[0], 0x07030602);
-            const uint32_t b0 = __builtin_amdgcn_perm(r[3], r[2], 0x05010400), b1 = __builtin_amdgcn_perm(r[3], r[2], 0x07030602);
-            t[cq * 4 + 0][rq] = (a0 & 0xffffu) | b0 << 16;
-            t[cq * 4 + 1][rq] = a0 >> 16 | (b0 & 0xffff0000u);
-            t[cq * 4 + 2][rq] = (a1 & 0xffffu) | b1 << 16;
-            t[cq * 4 + 3][rq] = a1 >> 16 | (b1 & 0xffff0000u);
+            uint32_t o[4];
+            turn4(r, o);
+#pragma unroll
+            for (int x = 0; x < 4; x++) t[cq * 4 + x][rq] = o[x];
         }
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < 4; i++) {
             const int e = threadIdx.x + i * 256, col = e >> 3, p = e & 7;
             const int64_t oc = c0 + col, m = m0 + p * 16;
-            if (oc < C && m < M) {
-                int8_t* d = out + oc * out_ld + m;
-                if (wide && m + 16 <= M) {
-                    uint32_t v[4];
-#pragma unroll
-                    for (int u = 0; u < 4; u++) v[u] = t[col][p * 4 + u];
-                    __builtin_memcpy(__builtin_assume_aligned(d, 16), v, 16);
-                } else {
-                    const int n = M - m < 16 ? (int)(M - m) : 16;
-                    for (int u = 0; u < n; u++) d[u] = (int8_t)(t[col][p * 4 + u / 4] >> (u % 4 * 8));
-                }
-            }
+            if (oc < C && m < M) put16(&t[col][p * 4], out + oc * out_ld + m, M - m, wide);
         }
         __syncthreads();
     }
@@ -483,6 +586,7 @@ template <typename T, bool MUL, int NW, int VPT>
 int rows_grid(const RqRowArgs& a, hipStream_t s)
 {
     constexpr int R = NW < 4 ? 4 / NW : 1;
+    if (!slots_fit<T, NW, VPT>(a.C)) return ISEG_ERR_UNSUPPORTED;
     const int64_t nb = ceil_div64(a.M, R);
     hipLaunchKernelGGL((k_quantize_rows<T, MUL, NW, VPT>), dim3((unsigned)(nb < 4096 ? nb : 4096)),
                        dim3(NW < 4 ? 256 : NW * 64), 0, s, a);
@@ -496,10 +600,12 @@ int launch_rows_mul(const RqRowArgs& a, hipStream_t s)
     const int64_t v = ceil_div64(a.C, N);
     if (a.C >= N) {
         if (v <= 64) return rows_grid<T, MUL, 1, 1>(a, s);
+        if (v <= 128) return rows_grid<T, MUL, 1, 2>(a, s);
         if (v <= 256) return rows_grid<T, MUL, 4, 1>(a, s);
         if (v <= 512) return rows_grid<T, MUL, 4, 2>(a, s);
         if (v <= 1024) return rows_grid<T, MUL, 8, 2>(a, s);
-        if (v <= 2048) return rows_grid<T, MUL, 16, 2>(a, s);
+        if (v <= 1536) return rows_grid<T, MUL, 8, 3>(a, s);
+        if (v <= 2048) return rows_grid<T, MUL, 8, 4>(a, s);
     }
     const unsigned grid = (unsigned)(a.M < kRowGridMax ? a.M : kRowGridMax);
     hipLaunchKernelGGL(k_quantize_rows_long<T>, dim3(grid), dim3(256), 0, s, a);
@@ -518,15 +624,17 @@ int launch_cols_mul(const RqRowArgs& a, hipStream_t s)
     const unsigned ct = (unsigned)ceil_div64(a.C, 64);
     const int64_t strips = cols_strips(a.M, a.C);
     const int64_t strip = ceil_div64(a.M, strips);
-    if (a.C >= RowVec<T>::N)
-        hipLaunchKernelGGL((k_cols_stats<T, MUL>), dim3(ct, (unsigned)strips), dim3(256), 0, s, a, strip);
-    else
+    if (a.C < RowVec<T>::N) {
         hipLaunchKernelGGL(k_cols_stats_narrow<T>, dim3(1, (unsigned)strips), dim3(64), 0, s, a, strip);
-    hipLaunchKernelGGL(k_cols_scale, dim3((unsigned)ceil_div64(a.C, 256)), dim3(256), 0, s, a, (int)strips);
-    if (a.M > 0) {
-        const int64_t mt = ceil_div64(a.M, 128);
-        hipLaunchKernelGGL((k_cols_codes<T, MUL>), dim3(ct, (unsigned)(mt < 1024 ? mt : 1024)), dim3(256), 0, s, a);
+        hipLaunchKernelGGL(k_cols_codes_narrow<T>, dim3((unsigned)a.C, grid_for(a.M, 256, 256)), dim3(256), 0, s, a,
+                           (int)strips);
+        return launch_ok();
     }
+    hipLaunchKernelGGL((k_cols_stats<T, MUL>), dim3(ct, (unsigned)strips), dim3(256), 0, s, a, strip);
+    // blocks for the chip, each with the scales' work once
+    const int64_t mt = ceil_div64(a.M, 128), most = ceil_div64(1024, ct);
+    const int64_t gy = mt < most ? mt : most;
+    hipLaunchKernelGGL((k_cols_codes<T, MUL>), dim3(ct, (unsigned)(gy > 1 ? gy : 1)), dim3(256), 0, s, a, (int)strips);
     return launch_ok();
 }
 

@@ -16,6 +16,9 @@ CASES = [
     (1025, 513, "fp16", "fp32", 7), (9, 4096, "bf16", "bf16", 8), (4, 4100, "fp32", "fp32", 0), (3, 8192, "bf16", "fp16", 0),
     (5, 8200, "fp16", "fp16", 0), (2, 16384, "fp32", "fp32", 0), (2, 16389, "bf16", "bf16", 0), (3, 32779, "bf16", "bf16", 2),
     (2, 16391, "fp32", "fp32", 0), (1, 70001, "fp16", "fp32", 0), (2100, 40, "bf16", "bf16", 0),
+    # every count of waves and vectors of a row, just above and at its limits
+    (70, 8, "bf16", "bf16", 0), (9, 513, "bf16", "fp32", 1), (9, 1025, "bf16", "bf16", 0), (3, 6145, "bf16", "bf16", 0), (3, 6144, "bf16", "bf16", 0),
+    (3, 8193, "bf16", "bf16", 0), (2, 12289, "bf16", "fp32", 0), (2, 12288, "bf16", "bf16", 0), (600, 2052, "fp32", "fp32", 0), (3, 6150, "fp32", "bf16", 0), (3, 4099, "fp32", "fp16", 0),
 ]
 
 

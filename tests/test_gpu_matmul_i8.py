@@ -115,6 +115,7 @@ QUANT = [
     (1, 1, "fp32", 0, 8, False, False), (3, 17, "bf16", 0, 8, False, True), (5, 64, "fp16", 3, 8, True, False), (64, 63, "fp32", 1, 8, False, True),
     (65, 130, "bf16", 0, 4, True, True), (1, 4096, "bf16", 0, 8, False, False), (300, 1000, "fp32", 0, 8, False, False),
     (130, 2052, "bf16", 4, 8, False, True), (9, 8193, "fp16", 0, 8, False, False), (7, 16384, "bf16", 0, 8, True, False),
+    (6, 2100, "fp32", 0, 8, False, True), (4, 4104, "fp32", 0, 8, False, False), (5, 6148, "fp32", 2, 8, False, True), (4, 12300, "bf16", 0, 8, False, True),
     (1000, 72, "fp32", 0, 8, True, True), (4100, 33, "bf16", 0, 8, False, True), (3, 20000, "fp32", 0, 2, False, False), (2, 40003, "bf16", 0, 8, False, True),
 ]
 
