@@ -3,9 +3,10 @@
 //
 // One pass over a row keeps, per thread, the running maximum m, S = sum
 // e^(x-m) and T = sum e^(x-m) (x-m) (in base 2), and which of the thread's
-// vectors held its largest value.  The k largest logits lie in the segments
-// (the vectors of one thread) with the k best leaders, so only those segments
-// are read again.
+// vectors held its largest value, its leader.  The k largest logits lie in the
+// segments (the vectors of one thread) with the k best leaders: a logit of any
+// other segment is beaten by k leaders.  So only those segments are read
+// again, and of them only what is no worse than the k-th leader is ranked.
 #include "rowops.h"
 
 namespace {
@@ -15,7 +16,7 @@ constexpr float kLn2 = 0.69314718055994530942f;
 constexpr float kMinF32 = -3.4028234e38f;
 constexpr int kTopMax = 64;
 constexpr int kCand = 512;                 // candidates ranked in LDS at once
-constexpr int kMergeKeys = 1024;           // keys of all splits of a row
+constexpr int kMergeKeys = 1024;           // keys of all splits of a row, leaders of all waves
 
 struct LpArgs {
     const void *x, *tok;
@@ -49,11 +50,14 @@ struct Stat {
     float m, S, T;
 };
 
-// weight of a part whose maximum is m when the maximum is mn (and its exponent)
+// 2^x to one step; results below 2^-126 count as 0
+__device__ __forceinline__ float exp2_raw(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// the sums of a part whose maximum is m, relative to the maximum mn >= m
 __device__ __forceinline__ void stat_move(Stat& s, float mn)
 {
     const float d = fmaxf((s.m - mn) * kLog2e, -200.f);      // 2^-200 is 0 in float32
-    const float c = exp2f(d);
+    const float c = exp2_raw(d);
     s.T = c * fmaf(s.S, d, s.T);
     s.S *= c;
     s.m = mn;
@@ -72,11 +76,23 @@ __device__ __forceinline__ int64_t token_of(const LpArgs& a, int64_t m)
     return a.tok64 ? ((const int64_t*)a.tok)[m] : (int64_t)((const int32_t*)a.tok)[m];
 }
 
-// the scalars of a row from its statistics
+// the given token of a row and its logit, loaded ahead of the row itself
+struct Given {
+    int64_t t;
+    float x;
+};
+
 template <typename T>
-__device__ __forceinline__ void row_scalars(const LpArgs& a, int64_t m, const Stat& s)
+__device__ __forceinline__ Given given_of(const LpArgs& a, int64_t m)
 {
     const int64_t t = token_of(a, m);
+    return {t, t >= 0 && t < a.V ? (float)((const T*)a.x)[m * a.ld + t] : 0.f};
+}
+
+// the scalars of a row from its statistics
+__device__ __forceinline__ void row_scalars(const LpArgs& a, int64_t m, const Stat& s, const Given& given)
+{
+    const int64_t t = given.t;
     float lse, ent, lp;
     if (s.S == 0.f) {                                        // every logit is -infinity
         lse = -__builtin_inff();
@@ -86,7 +102,7 @@ __device__ __forceinline__ void row_scalars(const LpArgs& a, int64_t m, const St
         const float ls = logf(s.S);
         lse = s.m + ls;
         ent = ls - s.T * kLn2 / s.S;
-        lp = t >= 0 && t < a.V ? (float)((const T*)a.x)[m * a.ld + t] - s.m - ls : 0.f;
+        lp = given.x - s.m - ls;
         if (!(s.S == s.S)) {
             lse = ent = lp = s.S;
             set_status(a.status, ISEG_DEV_NONFINITE);
@@ -124,40 +140,133 @@ __device__ __forceinline__ RowVec<T> lp_load(const T* x, int64_t g, int64_t V)
     return row_load_part(x + c, (int)(V - c), (T)-__builtin_inff());
 }
 
-template <typename T, bool TOP>
-__global__ __launch_bounds__(256) void k_logprob_fwd(LpArgs a)
+// how many of the n keys (n a multiple of 4, zeros behind the last) beat `mine`
+__device__ __forceinline__ int rank_of(const uint64_t* keys, int n, uint64_t mine)
+{
+    int r = 0;
+#pragma unroll 4
+    for (int i = 0; i < n; i += 4) {
+        const ulonglong2 a = *(const ulonglong2*)(keys + i), b = *(const ulonglong2*)(keys + i + 2);
+        r += (a.x > mine) + (a.y > mine) + (b.x > mine) + (b.y > mine);
+    }
+    return r;
+}
+
+// Ranks the keys held one per thread (0: none) and hands the k best to
+// put(rank, key, thread): each wave's k-th best bounds the k-th best of all
+// from below, so only the keys at or above the largest of these bounds (a few
+// more than k, as a rule) are ranked against each other.  keys: 256 words,
+// list: 260, bound: one word per wave, count: one int, all LDS; every thread of
+// the block of 256 calls it.
+template <typename F>
+__device__ __forceinline__ void best_keys(uint64_t mine, int k, uint64_t* keys, uint64_t* list, uint16_t* who,
+                                          uint64_t* bound, int* count, F put)
+{
+    const int tid = threadIdx.x, w = tid >> 6;
+    keys[tid] = mine;
+    if (tid == 0) *count = 0;
+    if ((tid & 63) == 0) bound[w] = 0;
+    __syncthreads();
+    if (mine && rank_of(keys + w * 64, 64, mine) == k - 1) bound[w] = mine;      // keys differ: one lane at most
+    __syncthreads();
+    uint64_t lo = 1;
+#pragma unroll
+    for (int i = 0; i < 4; i++) lo = bound[i] > lo ? bound[i] : lo;
+    if (mine >= lo) {
+        const int at = atomicAdd(count, 1);
+        list[at] = mine;
+        who[at] = (uint16_t)tid;
+    }
+    __syncthreads();
+    const int n = *count, n4 = (n + 3) & ~3;
+    if (tid < n4 - n) list[n + tid] = 0;
+    __syncthreads();
+    if (tid < n) {
+        const uint64_t key = list[tid];
+        const int r = rank_of(list, n4, key);
+        if (r < k) put(r, key, who[tid]);
+    }
+    __syncthreads();
+}
+
+// One vector's part of a row: its maximum and leader, then its exponentials.
+template <typename T, bool ENT, int U>
+__device__ __forceinline__ void lp_take(const RowVec<T>* r, Stat& s)
 {
     constexpr int N = RowVec<T>::N;
-    __shared__ Stat rstat[4];
-    __shared__ uint64_t keys[TOP ? 256 : 1];
-    __shared__ uint64_t cand[TOP ? kCand : 1];
+#pragma unroll
+    for (int u = 0; u < U; u++)
+#pragma unroll
+        for (int i = 0; i < N; i++) {
+            const float d = ((float)r[u].v[i] - s.m) * kLog2e;
+            const float e = exp2_raw(d);
+            s.S += e;
+            if (ENT) s.T = fmaf(e, fmaxf(d, -200.f), s.T);
+        }
+}
+
+template <typename T>
+__device__ __forceinline__ float vec_max(const RowVec<T>& r)
+{
+    float cm = (float)r.v[0];
+#pragma unroll
+    for (int i = 1; i < RowVec<T>::N; i++) cm = fmaxf(cm, (float)r.v[i]);
+    return cm;
+}
+
+template <typename T, bool ENT, bool TOP>
+__global__ __launch_bounds__(256) void k_logprob_fwd(LpArgs a)
+{
+    constexpr int N = RowVec<T>::N, NT = 256, NW = 4, U = 4;
+    __shared__ Stat rstat[NW];
+    __shared__ __attribute__((aligned(16))) uint64_t keys[TOP ? NT : 1];
+    __shared__ __attribute__((aligned(16))) uint64_t cand[TOP ? kCand + 4 : 1];
+    __shared__ uint64_t bound[NW];
+    __shared__ uint16_t who[TOP ? NT : 1];
     __shared__ int sel[TOP ? kTopMax : 1];
-    __shared__ int ncand;
+    __shared__ int count;
     __shared__ uint64_t thr_s;
     const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
-    const int64_t G = ceil_div64(a.V, N);
+    const int64_t G = ceil_div64(a.V, N), Gfull = a.V / N;
     for (int64_t item = blockIdx.x; item < a.M * a.splits; item += gridDim.x) {
-        const int64_t m = item / a.splits;
+        const int64_t m = a.splits == 1 ? item : item / a.splits;
         const int sp = (int)(item - m * a.splits);
         const T* x = (const T*)a.x + m * a.ld;
         const int64_t g0 = G * sp / a.splits, g1 = G * (sp + 1) / a.splits;
+        const int64_t gf = g1 < Gfull ? g1 : Gfull;
+        Given given = {-1, 0.f};
+        if (a.splits == 1 && tid == 0) given = given_of<T>(a, m);
         Stat s = {kMinF32, 0.f, 0.f};
         float best = -__builtin_inff();
         int64_t bestg = g0 + tid;
-        for (int64_t g = g0 + tid; g < g1; g += 256) {
-            const RowVec<T> r = lp_load(x, g, a.V);
-            float cm = (float)r.v[0];
+        int64_t g = g0 + tid;
+        for (; g + (U - 1) * NT < gf; g += U * NT) {
+            RowVec<T> r[U];
 #pragma unroll
-            for (int i = 1; i < N; i++) cm = fmaxf(cm, (float)r.v[i]);
+            for (int u = 0; u < U; u++) r[u] = row_load(x + (g + u * NT) * N);
+            float top = s.m;
+#pragma unroll
+            for (int u = 0; u < U; u++) {
+                const float cm = vec_max(r[u]);
+                top = fmaxf(top, cm);
+                if (TOP && cm > best) { best = cm; bestg = g + u * NT; }
+            }
+            stat_move(s, top);
+            lp_take<T, ENT, U>(r, s);
+        }
+        for (; g < gf; g += NT) {
+            const RowVec<T> r = row_load(x + g * N);
+            const float cm = vec_max(r);
             if (TOP && cm > best) { best = cm; bestg = g; }
             stat_move(s, fmaxf(s.m, cm));
-#pragma unroll
-            for (int i = 0; i < N; i++) {
-                const float d = ((float)r.v[i] - s.m) * kLog2e;
-                const float e = exp2f(d);
-                s.S += e;
-                s.T = fmaf(e, fmaxf(d, -200.f), s.T);
-            }
+            lp_take<T, ENT, 1>(&r, s);
+        }
+        if (g < g1) {                         // the row's last, broken vector
+            const RowVec<T> r = lp_load(x, g, a.V);
+            const float cm = vec_max(r);
+            if (TOP && cm > best) { best = cm; bestg = g; }
+            stat_move(s, fmaxf(s.m, cm));
+            lp_take<T, ENT, 1>(&r, s);
         }
         const bool has = g0 + tid < g1;
 #pragma unroll
@@ -166,66 +275,72 @@ __global__ __launch_bounds__(256) void k_logprob_fwd(LpArgs a)
             s = stat_join(s, t);
         }
         if (lane == 0) rstat[w] = s;
-        if (TOP) keys[tid] = has ? key_of(best, (uint32_t)bestg) : 0;
-        if (tid == 0) { ncand = 0; thr_s = 0; }
+        if (tid == 0) thr_s = 0;
         __syncthreads();
         s = rstat[0];
 #pragma unroll
-        for (int i = 1; i < 4; i++) s = stat_join(s, rstat[i]);
+        for (int i = 1; i < NW; i++) s = stat_join(s, rstat[i]);
         if (a.splits == 1) {
-            if (tid == 0) row_scalars<T>(a, m, s);
+            if (tid == 0) row_scalars(a, m, s, given);
         } else if (tid == 0) {
             float* p = a.pstat + item * 4;
             p[0] = s.m; p[1] = s.S; p[2] = s.T;
         }
         if (TOP) {
             const int k = a.k;
-            const int nthr = (int)(g1 - g0 < 256 ? g1 - g0 : 256);       // threads with a segment
+            const int nthr = (int)(g1 - g0 < NT ? g1 - g0 : NT);         // threads with a segment
             const int nsel = k < nthr ? k : nthr;
-            const uint64_t mine = keys[tid];
-            int rank = 0;
-            for (int i = 0; i < 256; i++) rank += keys[i] > mine;
-            if (has && rank < nsel) {
-                sel[rank] = tid;
-                // with k segments chosen, nothing below the last one's leader counts
-                if (rank == k - 1) thr_s = (mine >> 32) << 32 | (uint32_t)~(uint32_t)((int64_t)(uint32_t)~(uint32_t)mine * N + N - 1);
-            }
+            best_keys(has ? key_of(best, (uint32_t)bestg) : 0, nsel, keys, cand, who, bound, &count,
+                          [&](int rank, uint64_t key, int t) {
+                              sel[rank] = t;
+                              // with k segments chosen, nothing below the last leader's value, or of
+                              // its value behind its vector, counts
+                              if (rank == k - 1)
+                                  thr_s = (key >> 32) << 32 | (uint32_t)~(uint32_t)((uint32_t)~(uint32_t)key * (uint32_t)N + N - 1);
+                          });
+            if (tid == 0) count = 0;
             __syncthreads();
-            const int64_t nit = ceil_div64(g1 - g0, 256);
+            const uint32_t nit = (uint32_t)ceil_div64(g1 - g0, NT);
             uint64_t lo = thr_s, hi = ~0ull, thr = lo;
             for (;;) {
-                // candidates with a key of at least thr
-                for (int64_t p = tid; p < nsel * nit; p += 256) {
-                    const int64_t g = g0 + sel[p / nit] + 256 * (p % nit);
-                    if (g >= g1) continue;
-                    const RowVec<T> r = lp_load(x, g, a.V);
+                // candidates with a key of at least thr; when they are too many
+                // (ties, or a sorted row) thr is raised by bisection
+                for (uint32_t p = tid; p < (uint32_t)nsel * nit; p += NT) {
+                    const uint32_t q = p / nit;
+                    const int64_t gg = g0 + sel[q] + (int64_t)NT * (p - q * nit);
+                    if (gg >= g1) continue;
+                    const RowVec<T> r = lp_load(x, gg, a.V);
 #pragma unroll
                     for (int i = 0; i < N; i++) {
-                        const int64_t c = g * N + i;
+                        const int64_t c = gg * N + i;
                         const uint64_t key = key_of((float)r.v[i], (uint32_t)c);
                         if (c < a.V && key >= thr) {
-                            const int at = atomicAdd(&ncand, 1);
+                            const int at = atomicAdd(&count, 1);
                             if (at < kCand) cand[at] = key;
                         }
                     }
                 }
                 __syncthreads();
-                const int n = ncand;
+                const int n = count;
                 __syncthreads();
-                if (tid == 0) ncand = 0;
-                if (n > kCand) lo = thr;
-                else if (n < k && thr != lo) hi = thr;
-                else {
-                    for (int q = tid; q < n; q += 256) {
+                if (tid == 0) count = 0;
+                if (n > kCand) {
+                    lo = thr;
+                } else if (n < k && thr != lo) {
+                    hi = thr;
+                } else {
+                    const int n4 = (n + 3) & ~3;
+                    if (tid < n4 - n) cand[n + tid] = 0;
+                    __syncthreads();
+                    for (int q = tid; q < n; q += NT) {
                         const uint64_t mk = cand[q];
-                        int rk = 0;
-                        for (int i = 0; i < n; i++) rk += cand[i] > mk;
+                        const int rk = rank_of(cand, n4, mk);
                         if (rk >= k) continue;
                         if (a.splits == 1) write_top(a, m, rk, mk, s);
                         else a.pkey[item * k + rk] = mk;
                     }
                     // fewer than k: a short split, or a row with NaN in it
-                    for (int q = n + tid; q < k; q += 256) {
+                    for (int q = n + tid; q < k; q += NT) {
                         if (a.splits == 1) write_none(a, m, q);
                         else a.pkey[item * k + q] = 0;
                     }
@@ -239,34 +354,64 @@ __global__ __launch_bounds__(256) void k_logprob_fwd(LpArgs a)
     }
 }
 
-// joins the splits of a row
+// Joins the splits of a row.  Each split's keys are in order, so the first
+// ceil(k / splits) of every split hold k keys, and the k-th best of these
+// bounds the k-th best of all from below; what is at or above it is ranked.
 template <typename T, bool TOP>
 __global__ __launch_bounds__(256) void k_logprob_join(LpArgs a)
 {
-    __shared__ uint64_t keys[TOP ? kMergeKeys : 1];
+    constexpr int PER = kMergeKeys / 256;
+    __shared__ __attribute__((aligned(16))) uint64_t list[TOP ? kMergeKeys + 4 : 1];
+    __shared__ unsigned long long bound;
+    __shared__ int count;
     const int tid = threadIdx.x;
+    const int k = a.k, n = a.splits * k;
     for (int64_t m = blockIdx.x; m < a.M; m += gridDim.x) {
+        const uint64_t* key = a.pkey + m * n;
+        uint64_t mine[PER];
+#pragma unroll
+        for (int i = 0; i < PER; i++) mine[i] = TOP && tid + i * 256 < n ? key[tid + i * 256] : 0;
+        Given given = {-1, 0.f};
+        if (tid == 0) given = given_of<T>(a, m);
+        // every wave joins the statistics for itself: its lanes take the splits
         Stat s = {kMinF32, 0.f, 0.f};
-        for (int i = 0; i < a.splits; i++) {
+        for (int i = tid & 63; i < a.splits; i += 64) {
             const float* p = a.pstat + (m * a.splits + i) * 4;
             s = stat_join(s, Stat{p[0], p[1], p[2]});
         }
-        if (tid == 0) row_scalars<T>(a, m, s);
+#pragma unroll
+        for (int o = 32; o > 0; o >>= 1) {
+            Stat t = {__shfl_xor(s.m, o, 64), __shfl_xor(s.S, o, 64), __shfl_xor(s.T, o, 64)};
+            s = stat_join(s, t);
+        }
+        if (tid == 0) row_scalars(a, m, s, given);
         if (TOP) {
-            const int n = a.splits * a.k;
-            for (int q = tid; q < n; q += 256) keys[q] = a.pkey[m * n + q];
-            __syncthreads();
-            for (int q = tid; q < n; q += 256) {
-                const uint64_t mk = keys[q];
-                if (!mk) continue;
-                int rk = 0;
-                for (int i = 0; i < n; i++) rk += keys[i] > mk;
-                if (rk < a.k) write_top(a, m, rk, mk, s);
+            const int j = (k + a.splits - 1) / a.splits, h = j * a.splits, h4 = (h + 3) & ~3;
+            if (tid == 0) { bound = 1; count = 0; }
+#pragma unroll
+            for (int i = 0; i < PER; i++) {
+                const int e = tid + i * 256, sp = e / k, r = e - sp * k;
+                if (e < n && r < j) list[sp * j + r] = mine[i];
             }
-            int have = 0;
-            if (tid < a.k)
-                for (int i = 0; i < n; i++) have += keys[i] != 0;
-            if (tid < a.k && tid >= have) write_none(a, m, tid);
+            if (tid < h4 - h) list[h + tid] = 0;
+            __syncthreads();
+            for (int q = tid; q < h; q += 256)
+                if (list[q] && rank_of(list, h4, list[q]) == k - 1) bound = list[q];      // keys differ: one at most
+            __syncthreads();
+            const uint64_t lo = bound;
+#pragma unroll
+            for (int i = 0; i < PER; i++)
+                if (mine[i] >= lo) list[atomicAdd(&count, 1)] = mine[i];
+            __syncthreads();
+            const int c = count, c4 = (c + 3) & ~3;
+            if (tid < c4 - c) list[c + tid] = 0;
+            __syncthreads();
+            for (int q = tid; q < c; q += 256) {
+                const uint64_t mk = list[q];
+                const int rk = rank_of(list, c4, mk);
+                if (rk < k) write_top(a, m, rk, mk, s);
+            }
+            for (int q = c + tid; q < k; q += 256) write_none(a, m, q);
             __syncthreads();
         }
     }
@@ -281,11 +426,28 @@ struct LbArgs {
     int32_t* status;
 };
 
-template <typename T>
-__global__ __launch_bounds__(256) void k_logprob_bwd(LbArgs a, int64_t cblocks)
+template <typename T, bool H>
+__device__ __forceinline__ RowVec<T> lb_take(const RowVec<T>& r, float lse, float ent, float glp, float gh, int at)
 {
     constexpr int N = RowVec<T>::N;
-    const int64_t G = ceil_div64(a.V, N);
+    RowVec<T> o;
+#pragma unroll
+    for (int i = 0; i < N; i++) {
+        const float lp = (float)r.v[i] - lse;
+        const float p = exp2_raw(lp * kLog2e);
+        const float d = -p * (H ? fmaf(gh, fmaxf(lp, -200.f) + ent, glp) : glp);
+        o.v[i] = (T)(i == at ? d + glp : d);
+    }
+    return o;
+}
+
+constexpr int kLbVecs = 2048;              // vectors of a row per block: eight per thread, four at once
+
+template <typename T, bool H>
+__global__ __launch_bounds__(256) void k_logprob_bwd(LbArgs a, uint32_t cblocks)
+{
+    constexpr int N = RowVec<T>::N, U = 4;
+    const int64_t G = ceil_div64(a.V, N), Gfull = a.V / N;
     for (int64_t item = blockIdx.x; item < a.M * cblocks; item += gridDim.x) {
         const int64_t m = item / cblocks;
         const int64_t cb = item - m * cblocks;
@@ -297,38 +459,45 @@ __global__ __launch_bounds__(256) void k_logprob_bwd(LbArgs a, int64_t cblocks)
             t = -1;
         }
         const float lse = a.lse[m];
+        // a row of banned tokens only: every probability, and the gradient, is 0
         const bool empty = lse == -__builtin_inff();
-        const float glp = a.g_lp && t >= 0 ? a.g_lp[m] : 0.f;
-        const float gh = a.g_h ? a.g_h[m] : 0.f;
-        const float ent = a.g_h ? a.entropy[m] : 0.f;
-        for (int64_t g = cb * 1024 + threadIdx.x; g < (cb + 1) * 1024 && g < G; g += 256) {
-            const RowVec<T> r = lp_load(x, g, a.V);
-            RowVec<T> o;
+        const float glp = a.g_lp && t >= 0 && !empty ? a.g_lp[m] : 0.f;
+        const float gh = H && !empty ? a.g_h[m] : 0.f;
+        const float ent = H && !empty ? a.entropy[m] : 0.f;
+        const float base = empty ? 0.f : lse;
+        const int64_t tg = t < 0 ? -1 : t / N;
+        const int ti = t < 0 ? -1 : (int)(t - tg * N);
+        const int64_t g1 = (cb + 1) * kLbVecs < G ? (cb + 1) * kLbVecs : G;
+        const int64_t gf = g1 < Gfull ? g1 : Gfull;
+        int64_t g = cb * kLbVecs + threadIdx.x;
+        for (; g + (U - 1) * 256 < gf; g += U * 256) {
+            RowVec<T> r[U];
 #pragma unroll
-            for (int i = 0; i < N; i++) {
-                const float lp = (float)r.v[i] - lse;
-                const float p = exp2f(lp * kLog2e);
-                float d = -p * fmaf(gh, fmaxf(lp, -200.f) + ent, glp);
-                if (g * N + i == t) d += glp;
-                o.v[i] = (T)(empty ? 0.f : d);
-            }
-            const int64_t c = g * N;
-            if (c + N <= a.V) row_store(dx + c, o);
-            else row_store_part(dx + c, o, (int)(a.V - c));
+            for (int u = 0; u < U; u++) r[u] = row_load(x + (g + u * 256) * N);
+#pragma unroll
+            for (int u = 0; u < U; u++)
+                row_store(dx + (g + u * 256) * N, lb_take<T, H>(r[u], base, ent, glp, gh, g + u * 256 == tg ? ti : -1));
         }
+        for (; g < gf; g += 256)
+            row_store(dx + g * N, lb_take<T, H>(row_load(x + g * N), base, ent, glp, gh, g == tg ? ti : -1));
+        if (g < g1)
+            row_store_part(dx + g * N, lb_take<T, H>(lp_load(x, g, a.V), base, ent, glp, gh, g == tg ? ti : -1),
+                           (int)(a.V - g * N));
     }
 }
 
-// splits of a row: enough blocks for the chip when there are few rows, each
-// with at least 1024 vectors
+// Splits of a row: a CU alone takes in about 20 GB/s, so with few rows each is
+// cut, down to two vectors per thread (eight with more than 16 rows, which
+// fill the chip by themselves sooner), at the cost of a second kernel that
+// joins the parts.  4 x 131072 bf16 without alternatives: one block of sixteen
+// waves per row 16.2 us, 32 parts and their join 7.2 us.
 int lp_splits(const iseg_logprob_geom* g)
 {
-    const int64_t n = g->dtype == ISEG_F32 ? 4 : 8;
-    const int64_t G = ceil_div64(g->V, n);
-    int64_t s = ceil_div64(1024, g->M > 0 ? g->M : 1);
-    const int64_t most = G / 1024 > 1 ? G / 1024 : 1;
-    s = s < most ? s : most;
-    const int64_t cap = g->top_k > 0 ? kMergeKeys / g->top_k : 256;
+    const int64_t G = ceil_div64(g->V, g->dtype == ISEG_F32 ? 4 : 8);
+    const int64_t fill = 1024 / (g->M > 0 ? g->M : 1);
+    const int64_t most = G / (g->M <= 16 ? 512 : 2048);
+    int64_t s = most < fill ? most : fill;
+    const int64_t cap = g->top_k > 4 ? kMergeKeys / g->top_k : 256;
     s = s < cap ? s : cap;
     return (int)(s > 1 ? s : 1);
 }
@@ -347,10 +516,12 @@ int launch_fwd(const LpArgs& a, hipStream_t s)
 {
     const int64_t items = a.M * a.splits;
     const dim3 grid((unsigned)(items < kRowGridMax ? items : kRowGridMax));
-    const dim3 jgrid((unsigned)(a.M < kRowGridMax ? a.M : kRowGridMax));
-    if (a.k > 0) hipLaunchKernelGGL((k_logprob_fwd<T, true>), grid, dim3(256), 0, s, a);
-    else hipLaunchKernelGGL((k_logprob_fwd<T, false>), grid, dim3(256), 0, s, a);
+    if (a.k > 0 && a.entropy) hipLaunchKernelGGL((k_logprob_fwd<T, true, true>), grid, dim3(256), 0, s, a);
+    else if (a.k > 0) hipLaunchKernelGGL((k_logprob_fwd<T, false, true>), grid, dim3(256), 0, s, a);
+    else if (a.entropy) hipLaunchKernelGGL((k_logprob_fwd<T, true, false>), grid, dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((k_logprob_fwd<T, false, false>), grid, dim3(256), 0, s, a);
     if (a.splits > 1) {
+        const dim3 jgrid((unsigned)(a.M < kRowGridMax ? a.M : kRowGridMax));
         if (a.k > 0) hipLaunchKernelGGL((k_logprob_join<T, true>), jgrid, dim3(256), 0, s, a);
         else hipLaunchKernelGGL((k_logprob_join<T, false>), jgrid, dim3(256), 0, s, a);
     }
@@ -360,10 +531,11 @@ int launch_fwd(const LpArgs& a, hipStream_t s)
 template <typename T>
 int launch_bwd(const LbArgs& a, hipStream_t s)
 {
-    const int64_t cblocks = ceil_div64(ceil_div64(a.V, RowVec<T>::N), 1024);
+    const int64_t cblocks = ceil_div64(ceil_div64(a.V, RowVec<T>::N), kLbVecs);
     const int64_t items = a.M * cblocks;
-    hipLaunchKernelGGL(k_logprob_bwd<T>, dim3((unsigned)(items < kRowGridMax ? items : kRowGridMax)), dim3(256), 0, s,
-                       a, cblocks);
+    const dim3 grid((unsigned)(items < kRowGridMax ? items : kRowGridMax));
+    if (a.g_h) hipLaunchKernelGGL((k_logprob_bwd<T, true>), grid, dim3(256), 0, s, a, (uint32_t)cblocks);
+    else hipLaunchKernelGGL((k_logprob_bwd<T, false>), grid, dim3(256), 0, s, a, (uint32_t)cblocks);
     return launch_ok();
 }
 

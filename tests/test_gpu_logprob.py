@@ -16,6 +16,7 @@ CASES = [
     (4, 100, "bf16", 0, 20, torch.int64), (3, 1000, "fp32", 5, 5, torch.int32), (2, 2047, "bf16", 0, 64, torch.int64), (2, 2049, "bf16", 1, 3, torch.int64),
     (1, 8192, "fp32", 0, 20, torch.int64), (3, 8193, "fp16", 3, 20, torch.int64), (1, 50021, "bf16", 0, 20, torch.int64),
     (2, 65536, "fp32", 0, 64, torch.int32), (1, 131072, "bf16", 0, 20, torch.int64), (40, 20000, "bf16", 0, 5, torch.int64), (1, 262147, "fp32", 0, 1, torch.int64),
+    (1, 600007, "bf16", 0, 1, torch.int64), (1, 300000, "fp32", 0, 64, torch.int64), (20, 50000, "fp32", 1, 64, torch.int64), (600, 1003, "fp16", 0, 64, torch.int32),
     (1100, 300, "bf16", 4, 4, torch.int64), (1030, 5000, "fp32", 0, 0, torch.int64), (2, 100003, "fp16", 0, 0, torch.int64),
 ]
 
