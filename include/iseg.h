@@ -659,6 +659,25 @@ size_t iseg_matmul_i8_ws(const iseg_matmul_geom* g);
 int iseg_matmul_i8(const int8_t* a, const float* a_scale, const int8_t* b, const float* b_scale, const float* bias,
                    const iseg_matmul_geom* g, void* out, void* ws, size_t ws_bytes, hipStream_t stream);
 
+/* iseg_linear_i8_fwd -- a linear layer in integers: iseg_quantize_rows of x
+ * [M, K] into codes and scale, then iseg_matmul_i8 of the codes with the
+ * weight codes w [N, K]: y = scale[m] w_scale[n] sum_k codes[m, k] w[n, k] +
+ * bias[n], every value as the two calls give it.  One token of at most 8192
+ * elements takes one kernel.  codes (rows codes_ld apart, codes_ld a multiple of 16, and
+ * codes 16-byte aligned) and scale [M] are outputs, which the backward needs. */
+typedef struct iseg_linear_geom {
+    int64_t M, N, K;
+    int64_t x_ld, w_ld, codes_ld, y_ld;
+    int32_t x_dtype, y_dtype;
+    int32_t bits, scale_mode;
+    int32_t unaligned;           /* not 0: w may start off a multiple of 16 bytes */
+    int32_t reserved;            /* 0 */
+} iseg_linear_geom;
+size_t iseg_linear_i8_fwd_ws(const iseg_linear_geom* g);
+int iseg_linear_i8_fwd(const void* x, const int8_t* w, const float* w_scale, const float* bias,
+                       const iseg_linear_geom* g, int8_t* codes, float* scale, void* y, void* ws, size_t ws_bytes,
+                       int32_t* dev_status, hipStream_t stream);
+
 /* iseg_logprob_fwd -- for every row x of logits [M, V]:
  *   lse = log sum_v e^x_v; logprob = x_t - lse of the given token t;
  *   entropy = -sum_v p_v log p_v, p_v = e^(x_v - lse);

@@ -4,7 +4,7 @@
 // Both operands have the reduction along the row, so a 16-byte piece of a row
 // is one lane's operand of v_mfma_i32_16x16x64_i8.  The int32 sums are exact,
 // so any split of the reduction gives the same bits.
-#include "rowops.h"
+#include "coder.h"
 
 namespace {
 
@@ -405,6 +405,129 @@ __global__ __launch_bounds__(NW * 64) void k_mm_rows(MmArgs p)
     }
 }
 
+// ---------------------------------------------------------------------------
+// one token of a whole linear layer
+// ---------------------------------------------------------------------------
+struct LinArgs {
+    MmArgs p;                    // a: unused
+    const void* x;
+    int8_t* codes;
+    float* scale;
+    int32_t bits, mode;
+    int32_t* status;
+};
+
+constexpr int kTokenMax = 8192;            // longest token that a block quantizes for itself
+
+// k_mm_rows for one token, whose blocks quantize it for themselves: the first
+// weights are on their way while a block takes the maximum and leaves the
+// codes in LDS.  x is read by every block, from the caches; of the codes each
+// block writes out its own share.
+template <typename TX, typename TO, int J>
+__global__ __launch_bounds__(512) void k_linear_token(LinArgs a)
+{
+    constexpr int NW = 8, N = RowVec<TX>::N, VPT = kTokenMax / N / 512;
+    __shared__ __attribute__((aligned(16))) int red[NW][J][16];
+    __shared__ uint32_t top[NW];
+    __shared__ __attribute__((aligned(16))) int8_t cd[kTokenMax];
+    const MmArgs& p = a.p;
+    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+    const int lr = lane & 15, lp = lane >> 4;
+    const int K = (int)p.K, Kp = (K + 255) & ~255;
+    const int64_t n0 = (int64_t)blockIdx.x * (J * 16);
+    const TX* x = (const TX*)a.x;
+    RowSlot<N> sl[VPT];
+    RowVec<TX> xv[VPT];
+#pragma unroll
+    for (int j = 0; j < VPT; j++) {
+        sl[j] = row_slot<N>(((int64_t)j * 512 + tid) * N, K);
+        xv[j] = slot_load<TX, N>(x, sl[j]);
+    }
+    const int8_t* bp[J];
+#pragma unroll
+    for (int j = 0; j < J; j++) {
+        const int64_t r = n0 + j * 16 + lr;
+        bp[j] = p.b + (r < p.N ? r : p.N - 1) * p.ldb;
+    }
+    v4i fb[4][J];
+    auto weights = [&](int k0) {
+#pragma unroll
+        for (int u = 0; u < 4; u++)
+#pragma unroll
+            for (int j = 0; j < J; j++) {
+                const int k = k0 + u * 64 + lp * 16;
+                if (k0 + 256 <= K) __builtin_memcpy(&fb[u][j], bp[j] + k, 16);
+                else fb[u][j] = load16(bp[j], k, K);
+            }
+    };
+    if (w * 256 < K) weights(w * 256);
+    uint32_t big = 0;
+#pragma unroll
+    for (int j = 0; j < VPT; j++)
+#pragma unroll
+        for (int i = 0; i < N; i++) {
+            const uint32_t b = bits_of((float)xv[j].v[i]);
+            big = b > big ? b : big;
+        }
+    big = wave_max_u32(big);
+    if (lane == 0) top[w] = big;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < NW; i++) big = top[i] > big ? top[i] : big;
+    const float s = scale_of(bits_of((double)__builtin_bit_cast(float, big)), a.bits, a.mode);
+    const Coder k(s);
+    const int lim = (1 << (a.bits - 1)) - 1;
+    if (blockIdx.x == 0 && tid == 0) {
+        *a.scale = s;
+        if (!k.ok) set_status(a.status, ISEG_DEV_NONFINITE);
+    }
+#pragma unroll
+    for (int j = 0; j < VPT; j++)
+        if (sl[j].dup < N) {
+            float f[N];
+#pragma unroll
+            for (int i = 0; i < N; i++) f[i] = (float)xv[j].v[i];
+            uint32_t o[N / 4];
+            codes_of<N, false>(f, f, [&](int) -> const Coder& { return k; }, lim, o);
+            __builtin_memcpy(cd + sl[j].at, o, N);
+        }
+    if (tid < Kp - K) cd[K + tid] = 0;
+    __syncthreads();
+    // this block's share of the codes
+    for (int64_t q = ((int64_t)blockIdx.x * 512 + tid) * 16; q < K; q += (int64_t)gridDim.x * 512 * 16) {
+        if (q + 16 <= K) *(v4i*)(a.codes + q) = *(const v4i*)(cd + q);
+        else
+            for (int64_t e = q; e < K; e++) a.codes[e] = cd[e];
+    }
+    v4i acc[J];
+#pragma unroll
+    for (int j = 0; j < J; j++) acc[j] = (v4i){0, 0, 0, 0};
+    for (int k0 = w * 256; k0 < K; k0 += NW * 256) {
+        if (k0 != w * 256) weights(k0);
+#pragma unroll
+        for (int u = 0; u < 4; u++) {
+            const v4i fa = *(const v4i*)(cd + k0 + u * 64 + lp * 16);      // the token in all 16 rows
+#pragma unroll
+            for (int j = 0; j < J; j++)
+                acc[j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(fb[u][j], fa, acc[j], 0, 0, 0);
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < J; j++)
+        if (lr == 0) *(v4i*)&red[w][j][lp * 4] = acc[j];
+    __syncthreads();
+    if (tid < J * 16 && n0 + tid < p.N) {
+        const int64_t n = n0 + tid;
+        int sum = 0;
+#pragma unroll
+        for (int i = 0; i < NW; i++) sum += red[i][tid >> 4][tid & 15];
+        float v = (float)sum * s;
+        if (p.sb) v *= p.sb[n];
+        if (p.bias) v += p.bias[n];
+        ((TO*)p.out)[n] = (TO)v;
+    }
+}
+
 template <typename TO, int BM, int BN, int WM, int WN, int ST>
 int launch_tile(MmArgs p, hipStream_t s, int splits = 1)
 {
@@ -571,4 +694,90 @@ extern "C" int iseg_matmul_i8(const int8_t* a, const float* a_scale, const int8_
     return g->out_dtype == ISEG_F32   ? launch_mm<float>(p, g, pl, (char*)ws, stream)
            : g->out_dtype == ISEG_F16 ? launch_mm<f16_t>(p, g, pl, (char*)ws, stream)
                                       : launch_mm<bf16_t>(p, g, pl, (char*)ws, stream);
+}
+
+// ---------------------------------------------------------------------------
+// linear layer
+// ---------------------------------------------------------------------------
+namespace {
+
+int lin_check(const iseg_linear_geom* g)
+{
+    if (!g || !is_float_dtype(g->x_dtype) || !is_float_dtype(g->y_dtype) || g->bits < 2 || g->bits > 8 ||
+        (g->scale_mode != ISEG_SCALE_MAX && g->scale_mode != ISEG_SCALE_POW2))
+        return ISEG_ERR_ARG;
+    const int64_t big = (int64_t)1 << 31;
+    if (g->M < 0 || g->N < 0 || g->K < 0 || g->M >= big || g->N >= big || g->x_ld < g->K || g->w_ld < g->K ||
+        g->codes_ld < g->K || g->codes_ld % 16 || g->y_ld < g->N)
+        return ISEG_ERR_SHAPE;
+    if (g->K > 131071) return ISEG_ERR_UNSUPPORTED;
+    return ISEG_OK;
+}
+
+iseg_matmul_geom lin_product(const iseg_linear_geom* g)
+{
+    return {g->M, g->N, g->K, g->codes_ld, g->w_ld, g->y_ld, g->y_dtype, g->unaligned};
+}
+
+// One kernel for one token: 1 x 4096 x 4096 8.9 us against 9.4 for the two,
+// 1 x 2048 x 2048 4.9 against 6.3, and one launch less.  (With more tokens
+// every block's own quantization costs more than the launch: two tokens of
+// 4096 10.5 us against 9.3.)
+bool lin_fused(const iseg_linear_geom* g)
+{
+    return g->M == 1 && g->N > 0 && g->K >= 8 && g->K <= kTokenMax;
+}
+
+template <typename TX, typename TO>
+int launch_linear(const LinArgs& a, hipStream_t s)
+{
+    const bool two = a.p.N > 8192;         // rows of b per block as for k_mm_rows
+    const int64_t nb = ceil_div64(a.p.N, two ? 32 : 16);
+    if (nb * 512 >= (int64_t)1 << 32) return ISEG_ERR_UNSUPPORTED;
+    if (two) hipLaunchKernelGGL((k_linear_token<TX, TO, 2>), dim3((unsigned)nb), dim3(512), 0, s, a);
+    else hipLaunchKernelGGL((k_linear_token<TX, TO, 1>), dim3((unsigned)nb), dim3(512), 0, s, a);
+    return launch_ok();
+}
+
+template <typename TX>
+int launch_linear_out(const LinArgs& a, int32_t t, hipStream_t s)
+{
+    return t == ISEG_F32 ? launch_linear<TX, float>(a, s)
+                         : t == ISEG_F16 ? launch_linear<TX, f16_t>(a, s) : launch_linear<TX, bf16_t>(a, s);
+}
+
+}  // namespace
+
+extern "C" size_t iseg_linear_i8_fwd_ws(const iseg_linear_geom* g)
+{
+    if (lin_check(g) != ISEG_OK) return 0;
+    const iseg_matmul_geom p = lin_product(g);
+    return lin_fused(g) ? 256 : iseg_matmul_i8_ws(&p);
+}
+
+extern "C" int iseg_linear_i8_fwd(const void* x, const int8_t* w, const float* w_scale, const float* bias,
+                                  const iseg_linear_geom* g, int8_t* codes, float* scale, void* y, void* ws,
+                                  size_t ws_bytes, int32_t* dev_status, hipStream_t stream)
+{
+    int rc = lin_check(g);
+    if (rc != ISEG_OK) return rc;
+    if (g->M == 0) return ISEG_OK;
+    if (!scale || (g->K > 0 && (!x || !codes)) || (g->N > 0 && (!y || (g->K > 0 && !w)))) return ISEG_ERR_ARG;
+    if (((uintptr_t)codes & 15) || (!g->unaligned && ((uintptr_t)w & 15))) return ISEG_ERR_ARG;
+    if (!ws || ws_bytes < iseg_linear_i8_fwd_ws(g)) return ISEG_ERR_WORKSPACE;
+    if (lin_fused(g)) {
+        LinArgs a = {};
+        a.p.b = w; a.p.sb = w_scale; a.p.bias = bias; a.p.out = y;
+        a.p.M = g->M; a.p.N = g->N; a.p.K = g->K; a.p.ldb = g->w_ld; a.p.ldc = g->y_ld;
+        a.x = x; a.codes = codes; a.scale = scale;
+        a.bits = g->bits; a.mode = g->scale_mode; a.status = dev_status;
+        return g->x_dtype == ISEG_F32   ? launch_linear_out<float>(a, g->y_dtype, stream)
+               : g->x_dtype == ISEG_F16 ? launch_linear_out<f16_t>(a, g->y_dtype, stream)
+                                        : launch_linear_out<bf16_t>(a, g->y_dtype, stream);
+    }
+    rc = iseg_quantize_rows(x, g->x_dtype, g->M, g->K, g->x_ld, nullptr, g->bits, g->scale_mode, codes, g->codes_ld,
+                            scale, dev_status, stream);
+    if (rc != ISEG_OK) return rc;
+    const iseg_matmul_geom p = lin_product(g);
+    return iseg_matmul_i8(codes, scale, w, w_scale, bias, &p, y, ws, ws_bytes, stream);
 }

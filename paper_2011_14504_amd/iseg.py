@@ -78,6 +78,11 @@ class MatmulGeom(C.Structure):
                [("out_dtype", C.c_int32), ("unaligned", C.c_int32)]
 
 
+class LinearGeom(C.Structure):
+    _fields_ = [(n, C.c_int64) for n in ("M", "N", "K", "x_ld", "w_ld", "codes_ld", "y_ld")] + \
+               [(n, C.c_int32) for n in ("x_dtype", "y_dtype", "bits", "scale_mode", "unaligned", "reserved")]
+
+
 class LogprobGeom(C.Structure):
     _fields_ = [(n, C.c_int64) for n in ("M", "V", "ld", "out_ld")] + \
                [(n, C.c_int32) for n in ("dtype", "token_dtype", "top_k", "reserved")]
@@ -155,6 +160,8 @@ _SIGS = {
     "iseg_transpose_i8": ([_P, _I64, _I64, _I64, _P, _I64, _P], C.c_int),
     "iseg_matmul_i8_ws": ([_P], _SZ),
     "iseg_matmul_i8": ([_P, _P, _P, _P, _P, _P, _P, _P, _SZ, _P], C.c_int),
+    "iseg_linear_i8_fwd_ws": ([_P], _SZ),
+    "iseg_linear_i8_fwd": ([_P, _P, _P, _P, _P, _P, _P, _P, _P, _SZ, _P, _P], C.c_int),
     "iseg_logprob_fwd_ws": ([_P], _SZ),
     "iseg_logprob_fwd": ([_P, _P, _P, _P, _P, _P, _P, _P, _P, _SZ, _P, _P], C.c_int),
     "iseg_logprob_bwd": ([_P, _P, _P, _P, _P, _P, _P, _P, _P, _P], C.c_int),
@@ -519,6 +526,12 @@ def iseg_matmul_i8(a, a_scale, b, b_scale, bias, geom, out, ws):
     rc = lib().iseg_matmul_i8(_ptr(a), _ptr(a_scale), _ptr(b), _ptr(b_scale), _ptr(bias), C.byref(geom), _ptr(out),
                               *_ws_tuple(ws), _stream())
     _check(rc, "iseg_matmul_i8")
+
+
+def iseg_linear_i8_fwd(x, w, w_scale, bias, geom, codes, scale, y, ws, status=None):
+    rc = lib().iseg_linear_i8_fwd(_ptr(x), _ptr(w), _ptr(w_scale), _ptr(bias), C.byref(geom), _ptr(codes),
+                                  _ptr(scale), _ptr(y), *_ws_tuple(ws), _ptr(status), _stream())
+    _check(rc, "iseg_linear_i8_fwd")
 
 
 def iseg_logprob_fwd(logits, tokens, geom, logprob, lse, entropy, top_ids, top_logprob, ws, status=None):
@@ -1265,10 +1278,14 @@ def _float_code(t, what):
 
 def _rows(t, what):
     """(tensor, rows, columns, row stride) of a matrix with dense rows."""
-    if t.dim() < 1:
+    n = t.dim()
+    if n == 2 and t.is_contiguous():
+        M, Cc = t.shape
+        return t, M, Cc, Cc or 1
+    if n < 1:
         raise ValueError(f"{what}: at least one dimension expected")
     Cc = t.shape[-1]
-    if t.dim() != 2:
+    if n != 2:
         p = t.data_ptr()
         t = t.reshape(math.prod(t.shape[:-1]), Cc)
         if _REC is not None and t.data_ptr() != p:
@@ -1304,11 +1321,16 @@ def _gpu(*ts):
             raise ValueError("tensors on one device expected")
 
 
+def _like(t):
+    """An uninitialized dense tensor of t's shape and type."""
+    return torch.empty_like(t) if t.is_contiguous() else torch.empty(t.shape, dtype=t.dtype, device=t.device)
+
+
 def _scratch(device, nbytes):
     """Workspace of a call: the stream's, or, under graph capture, memory of
     the graph's own (a graph outlives the stream's workspace, and two graphs
     may replay at once)."""
-    if torch.cuda.is_current_stream_capturing():
+    if nbytes > 256 and torch.cuda.is_current_stream_capturing():      # 256: the least size, of calls that use none
         return torch.empty(max(nbytes, 256), dtype=torch.uint8, device=device)
     return workspace(device).get(nbytes)
 
@@ -1322,6 +1344,13 @@ def _layernorm_geom(M, Cc, x_ld, y_ld, dx_ld, x_dtype, p_dtype, eps):
 def _matmul_geom(M, N, K, lda, ldb, ldc, out_dtype, unaligned):
     g = MatmulGeom(M, N, K, lda, ldb, ldc, out_dtype, unaligned)
     return g, lib().iseg_matmul_i8_ws(C.byref(g))
+
+
+@functools.lru_cache(maxsize=256)
+def _linear_geom(M, N, K, x_ld, w_ld, codes_ld, y_ld, x_dtype, y_dtype, bits, scale_mode, unaligned):
+    g = LinearGeom(M, N, K, x_ld, w_ld, max((codes_ld + 15) // 16 * 16, 16), y_ld, x_dtype, y_dtype, bits,
+                   scale_mode, unaligned, 0)
+    return g, lib().iseg_linear_i8_fwd_ws(C.byref(g))
 
 
 @functools.lru_cache(maxsize=256)
@@ -1345,9 +1374,9 @@ def layernorm_fwd(x, gamma=None, beta=None, eps=1e-5, status=None):
     gamma = _vec(gamma, Cc, p.dtype if p is not None else None, x.device, "gamma")
     beta = _vec(beta, Cc, p.dtype if p is not None else None, x.device, "beta")
     _gpu(x, status)
-    y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-    stats = torch.empty((2,) + x.shape[:-1], dtype=torch.float32, device=x.device)
-    mean, rstd = stats[0], stats[1]
+    y = _like(x)
+    mean = torch.empty(M if x.dim() == 2 else x.shape[:-1], dtype=torch.float32, device=x.device)
+    rstd = torch.empty_like(mean)
     iseg_layernorm_fwd(xr, gamma, beta, _layernorm_geom(M, Cc, ld, Cc, Cc, xd, pd, eps), y, mean, rstd, status)
     return y, mean, rstd
 
@@ -1369,9 +1398,9 @@ def layernorm_bwd(dy, x, gamma, mean, rstd, want_params=True):
     mean = _vec(mean, M, torch.float32, x.device, "mean")
     rstd = _vec(rstd, M, torch.float32, x.device, "rstd")
     _gpu(x, dy)
-    dx = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    dx = _like(x)
     dgamma = torch.empty(Cc, dtype=pdt, device=x.device) if want_params else None
-    dbeta = torch.empty(Cc, dtype=pdt, device=x.device) if want_params else None
+    dbeta = torch.empty_like(dgamma) if want_params else None
     g = _layernorm_geom(M, Cc, ld, dld, Cc, xd, pd, 1.0)
     iseg_layernorm_bwd(dr, xr, gamma, mean, rstd, g, dx, dgamma, dbeta,
                        _scratch(x.device, lib().iseg_layernorm_bwd_ws(C.byref(g))))
@@ -1381,6 +1410,8 @@ def layernorm_bwd(dy, x, gamma, mean, rstd, want_params=True):
 def _codes_matrix(rows, cols, device):
     """int8 [rows, cols] in rows of a multiple of 16 bytes (the alignment that
     the products' wide loads take)."""
+    if cols % 16 == 0:
+        return torch.empty((rows, cols), dtype=torch.int8, device=device)
     return torch.empty((rows, (cols + 15) // 16 * 16), dtype=torch.int8, device=device)[:, :cols]
 
 
@@ -1468,9 +1499,24 @@ def linear_i8_fwd(x, w, w_scale=None, bias=None, bits=8, scale_mode=ISEG_SCALE_M
     by default x's, the codes and scales of x, which the backward needs)."""
     if x.dim() < 1 or w.dim() != 2 or x.shape[-1] != w.shape[1]:
         raise ValueError("x and w: rows of one length expected")
-    codes, scale = quantize_rows(x, bits, scale_mode, None, status)
-    y = matmul_i8(codes, w, scale, w_scale, bias, x.dtype if out_dtype is None else out_dtype)
-    return y.view(x.shape[:-1] + (w.shape[0],)), codes, scale
+    out_dtype = x.dtype if out_dtype is None else out_dtype
+    xd, od = _float_code(x, "x"), _float_code(out_dtype, "out_dtype")
+    _quant_args(bits, scale_mode)
+    xr, M, K, x_ld = _rows(x, "x")
+    wr, N, _, w_ld = _code_rows(w, "w")
+    if K > 131071:
+        raise ValueError("x and w: rows of at most 131071 elements expected")
+    dev = x.device
+    w_scale = _vec(w_scale, N, torch.float32, dev, "w_scale")
+    bias = _vec(bias, N, torch.float32, dev, "bias")
+    _gpu(x, w, status)
+    codes = _codes_matrix(M, K, dev)
+    scale = torch.empty(M, dtype=torch.float32, device=dev)
+    y = torch.empty((M, N) if x.dim() == 2 else x.shape[:-1] + (N,), dtype=out_dtype, device=dev)
+    g, wsb = _linear_geom(M, N, K, x_ld, w_ld, codes.stride(0) if K else 16, max(N, 1), xd, od, bits, scale_mode,
+                          int(wr.data_ptr() & 15 != 0))
+    iseg_linear_i8_fwd(xr, wr, w_scale, bias, g, codes, scale, y, _scratch(dev, wsb), status)
+    return y, codes, scale
 
 
 @_on_device
@@ -1529,10 +1575,11 @@ def logprob_fwd(logits, tokens, top_k=0, want_entropy=True, status=None):
     _gpu(logits, tokens, status)
     shape, dev = logits.shape[:-1], logits.device
     g, wsb = _logprob_geom(M, V, ld, V, dt, td, top_k)
-    out = torch.empty((3 if want_entropy else 2,) + shape, dtype=torch.float32, device=dev)
-    logprob, lse, entropy = out[0], out[1], out[2] if want_entropy else None
+    logprob = torch.empty(M if logits.dim() == 2 else shape, dtype=torch.float32, device=dev)
+    lse = torch.empty_like(logprob)
+    entropy = torch.empty_like(logprob) if want_entropy else None
     ids = torch.empty(shape + (top_k,), dtype=torch.int32, device=dev) if top_k else None
-    tlp = torch.empty(shape + (top_k,), dtype=torch.float32, device=dev) if top_k else None
+    tlp = torch.empty_like(ids, dtype=torch.float32) if top_k else None
     iseg_logprob_fwd(lr, tokens, g, logprob, lse, entropy, ids, tlp, _scratch(dev, wsb), status)
     return logprob, lse, entropy, ids, tlp
 
@@ -1556,7 +1603,7 @@ def logprob_bwd(logits, tokens, lse, entropy, g_logprob=None, g_entropy=None, st
     g_logprob = _vec(g_logprob, M, torch.float32, logits.device, "g_logprob")
     g_entropy = _vec(g_entropy, M, torch.float32, logits.device, "g_entropy")
     _gpu(logits, tokens, status)
-    dx = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
+    dx = _like(logits)
     g, _ = _logprob_geom(M, V, ld, V, dt, td, 0)
     iseg_logprob_bwd(lr, tokens, lse, entropy, g_logprob, g_entropy, g, dx, status)
     return dx

@@ -251,6 +251,34 @@ def test_quantize_tiny_huge_and_non_finite():
         assert torch.equal(s.cpu(), ws) and torch.equal(q.cpu(), wq)
 
 
+def test_linear_modes_strides_and_status():
+    from paper_2011_14504_amd import iseg
+    st = torch.zeros(1, dtype=torch.int32, device=DEV)
+    for M, K in ((2, 777), (40, 777)):
+        x, w = normal(1, M, K).float(), codes(2, 50, K).clamp_min(-127)
+        xg, wg = strided(x, K + 5, float("nan")), strided(w, K + 7, 99)
+        for bits, pow2 in ((8, True), (4, False), (2, False)):
+            y, q, s = iseg.linear_i8_fwd(xg, wg, None, None, bits, iseg.ISEG_SCALE_POW2 if pow2 else iseg.ISEG_SCALE_MAX, status=st)
+            wq, ws = quantized(x.double(), bits, pow2)
+            assert torch.equal(q.cpu(), wq) and torch.equal(s.cpu(), ws)
+            p = _sums(wq, w) * ws.double()[:, None]
+            within(y, p, 3 * U * p.abs(), "y")
+        assert iseg.iseg_status_read(st) == 0
+        x[1, 3] = float("nan")
+        y, q, s = iseg.linear_i8_fwd(x.to(DEV), wg, status=st)
+        assert iseg.iseg_status_read(st) == iseg.ISEG_DEV_NONFINITE
+        iseg.iseg_status_clear(st)
+        assert torch.isnan(y[1]).all() and bool(torch.isfinite(y[0]).all()) and not bool(q[1].any())
+        y3, q3, _ = iseg.linear_i8_fwd(x.to(DEV).view(1, M, K), wg)
+        assert y3.shape == (1, M, 50) and q3.shape == (M, K) and torch.equal(q3, q)
+    y, q, s = iseg.linear_i8_fwd(torch.empty(0, 16, device=DEV), wg[:, :16])
+    assert y.shape == (0, 50) and s.shape == (0,)
+    y, q, s = iseg.linear_i8_fwd(torch.ones(3, 16, device=DEV), torch.empty(0, 16, dtype=torch.int8, device=DEV))
+    assert y.shape == (3, 0) and bool((q == 127).all())
+    y, q, s = iseg.linear_i8_fwd(torch.empty(3, 0, device=DEV), torch.empty(5, 0, dtype=torch.int8, device=DEV), None, torch.arange(5., device=DEV))
+    assert torch.equal(y.cpu(), torch.arange(5.).expand(3, 5)) and bool((s == 1).all())
+
+
 def test_quantize_empty():
     from paper_2011_14504_amd import iseg
     q, s = iseg.quantize_rows(torch.empty(0, 8, device=DEV))
@@ -281,7 +309,9 @@ def test_transpose(shape):
 
 
 # (M, N, K, type)
-LINEAR = [(1, 40, 30, "fp32"), (5, 64, 128, "bf16"), (70, 100, 99, "fp16"), (128, 256, 192, "bf16"), (257, 129, 512, "fp32")]
+LINEAR = [(1, 40, 30, "fp32"), (1, 4096, 4096, "bf16"), (1, 9000, 1024, "fp16"), (2, 100, 4100, "bf16"), (3, 33, 5000, "fp32"), (4, 100, 4096, "bf16"), (16, 64, 1000, "fp16"),
+          (16, 8200, 512, "fp32"), (17, 64, 256, "bf16"), (1, 20, 3, "fp32"), (2, 20, 7, "bf16"), (1, 64, 16384, "bf16"), (1, 50, 16390, "fp32"),
+          (1, 100, 8, "bf16"), (1, 8193, 8192, "bf16"), (1, 17, 8191, "fp32"), (1, 9, 2049, "fp16"), (5, 64, 128, "bf16"), (70, 100, 99, "fp16"), (128, 256, 192, "bf16"), (257, 129, 512, "fp32")]
 
 
 @pytest.mark.parametrize("case", LINEAR, ids=str)
@@ -306,5 +336,8 @@ def test_linear_forward_and_backward(case):
         p = (q.double() @ wqa.double()) * s.double()[:, None]
         within(dw, p, 3 * U * p.abs() + HALF[t] * p.abs() * (1 + 4 * U) + TINY[t], "dw")
         within(db, dy.double().sum(0), (M + 4) * U * dy.double().abs().sum(0), "dbias")
+    # the same bits as its two parts, whichever way it is run
+    q2, s2 = iseg.quantize_rows(x.to(DEV))
+    assert torch.equal(iseg.matmul_i8(q2, w.to(DEV), s2, ws.to(DEV), bias.to(DEV), DT[t]), y)
     only = iseg.linear_i8_bwd(dy.to(DEV), qa, sa, w.to(DEV), ws.to(DEV), want_input=False)
     assert only[0] is None and only[2] is None and torch.equal(only[1], dw)

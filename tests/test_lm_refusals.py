@@ -91,6 +91,25 @@ def test_matmul_entry(iseg):
     assert mm(M=0, a=None, out=None) == iseg.ISEG_OK and mm(N=0, ldc=0) == iseg.ISEG_OK
 
 
+def test_linear_entry(iseg):
+    L = iseg.lib()
+
+    def lin(M=4, N=4, K=16, x_ld=16, w_ld=16, c_ld=16, y_ld=4, xd=iseg.ISEG_BF16, yd=iseg.ISEG_F32, bits=8, mode=0, un=0, x=ONE, w=ONE,
+            codes=ONE, scale=ONE, y=ONE, ws=ONE, n=BIG):
+        g = iseg.LinearGeom(M, N, K, x_ld, w_ld, c_ld, y_ld, xd, yd, bits, mode, un, 0)
+        return L.iseg_linear_i8_fwd(x, w, None, None, C.byref(g), codes, scale, y, ws, n, None, None)
+
+    off = C.c_void_p(ONE.value + 4)
+    for bad in (dict(xd=iseg.ISEG_I8), dict(yd=iseg.ISEG_I32), dict(bits=1), dict(bits=9), dict(mode=3), dict(x=None), dict(w=None), dict(codes=None),
+                dict(scale=None), dict(y=None), dict(w=off), dict(codes=off)):
+        assert lin(**bad) == iseg.ISEG_ERR_ARG, bad
+    for bad in (dict(M=-1), dict(N=-1), dict(K=-1), dict(x_ld=15), dict(w_ld=15), dict(c_ld=15), dict(c_ld=24), dict(y_ld=3), dict(N=1 << 31, y_ld=1 << 31)):
+        assert lin(**bad) == iseg.ISEG_ERR_SHAPE, bad
+    assert lin(K=131072, x_ld=131072, w_ld=131072, c_ld=131072) == iseg.ISEG_ERR_UNSUPPORTED
+    assert lin(ws=None) == iseg.ISEG_ERR_WORKSPACE and lin(n=1) == iseg.ISEG_ERR_WORKSPACE
+    assert lin(M=0, x=None, codes=None, scale=None, y=None) == iseg.ISEG_OK
+
+
 def test_logprob_entries(iseg):
     L = iseg.lib()
 
@@ -135,7 +154,8 @@ def test_helpers(iseg):
         lambda: iseg.matmul_i8(i8, x), lambda: iseg.matmul_i8(i8, i8[:, :31]), lambda: iseg.matmul_i8(i8, i8, v[:3]),
         lambda: iseg.matmul_i8(i8, i8, v, v.double()), lambda: iseg.matmul_i8(i8, i8, out_dtype=torch.int32),
         lambda: iseg.matmul_i8(i8, i8), lambda: iseg.matmul_i8(torch.zeros(1, 131072, dtype=torch.int8), torch.zeros(1, 131072, dtype=torch.int8)),
-        lambda: iseg.linear_i8_fwd(x, i8[:, :31]), lambda: iseg.linear_i8_fwd(x, i8),
+        lambda: iseg.linear_i8_fwd(x, i8[:, :31]), lambda: iseg.linear_i8_fwd(x, i8, v[:3]), lambda: iseg.linear_i8_fwd(x, i8, v, v.half()),
+        lambda: iseg.linear_i8_fwd(x, x), lambda: iseg.linear_i8_fwd(x, i8, bits=1), lambda: iseg.linear_i8_fwd(x, i8, out_dtype=torch.int8), lambda: iseg.linear_i8_fwd(x, i8),
         lambda: iseg.linear_i8_bwd(x, i8, v, i8), lambda: iseg.linear_i8_bwd(x[:, :4], i8, v, i8, w_t=i8),
         lambda: iseg.linear_i8_bwd(x[:3, :4], i8, v, i8),
         lambda: iseg.logprob_fwd(x, tok[:3]), lambda: iseg.logprob_fwd(x, tok.float()), lambda: iseg.logprob_fwd(x, tok, top_k=33),
@@ -153,6 +173,6 @@ def test_helpers(iseg):
 def test_tape_knows_the_operators(iseg):
     L = iseg.lib()
     for n in ("iseg_layernorm_fwd", "iseg_layernorm_bwd", "iseg_quantize_rows", "iseg_quantize_cols", "iseg_transpose_i8",
-              "iseg_matmul_i8", "iseg_logprob_fwd", "iseg_logprob_bwd"):
+              "iseg_matmul_i8", "iseg_linear_i8_fwd", "iseg_logprob_fwd", "iseg_logprob_bwd"):
         e = L.iseg_tape_entry(n.encode())
         assert e >= 0 and L.iseg_tape_entry_nargs(e) == len(iseg._SIGS[n][0])
