@@ -644,9 +644,10 @@ int iseg_transpose_i8(const int8_t* in, int64_t M, int64_t C, int64_t in_ld, int
  * bias[n].  a [M, K] and b [N, K] int8 codes, both with the reduction along
  * the row (b as a 1x1 conv's weights); a_scale [M], b_scale [N], bias [N]
  * float32, each may be NULL (1, 1, 0).  The sums are exact int32 (K <= 131071,
- * ISEG_ERR_UNSUPPORTED beyond), rounded to float32, multiplied by a_scale, by
- * b_scale, added to bias, and rounded to out_dtype (a float type).  K = 0
- * gives the bias.  a and b start at multiples of 16 bytes unless `unaligned`
+ * ISEG_ERR_UNSUPPORTED beyond), rounded to float32 and multiplied by a_scale;
+ * that times b_scale plus bias is rounded once, and then to out_dtype (a float
+ * type).  A row's outputs do not depend on the other rows.  K = 0 gives the
+ * bias.  a and b start at multiples of 16 bytes unless `unaligned`
  * is set (ISEG_ERR_ARG); with it, or with lda or ldb off a multiple of 16, the
  * workspace holds aligned copies of both (not for M <= 32). */
 typedef struct iseg_matmul_geom {

@@ -43,6 +43,13 @@ __device__ __forceinline__ v4i load16(const int8_t* row, int64_t k, int64_t K)
     return r;
 }
 
+// An output from its sum: two roundings after the sum's own, the same in every
+// kernel, so a row has the same bits alone and in a batch.
+__device__ __forceinline__ float mm_out(int sum, float sa, float sb, float bias)
+{
+    return fmaf((float)sum * sa, sb, bias);
+}
+
 // the fragment of the last K % 16 columns: zero but for the first 16 bytes of
 // the reduction step (lp = 0)
 __device__ __forceinline__ v4i mm_tail(const int8_t* x, int64_t ld, int64_t row, int64_t rows, int64_t K, int lp)
@@ -247,7 +254,7 @@ __global__ __launch_bounds__(WM * WN * 64) void k_mm_tile(MmArgs p)
 #pragma unroll
             for (int r = 0; r < 4; r++) {
                 if constexpr (kSplit) o.v[r] = acc[i][j][r];
-                else o.v[r] = (TO)((float)acc[i][j][r] * sa[i] * sb[j][r] + bias[j][r]);
+                else o.v[r] = (TO)mm_out(acc[i][j][r], sa[i], sb[j][r], bias[j][r]);
             }
             *(OutVec<TO>*)(t + lr * PITCH + (j * 16 + lp * 4) * ES) = o;
         }
@@ -305,12 +312,8 @@ __global__ __launch_bounds__(256) void k_mm_join(MmArgs p, const int32_t* __rest
         OutVec<TO> o;
 #pragma unroll
         for (int r = 0; r < 4; r++) {
-            float v = (float)s[r] * sa;
-            if (n + r < p.N) {
-                if (p.sb) v *= p.sb[n + r];
-                if (p.bias) v += p.bias[n + r];
-            }
-            o.v[r] = (TO)v;
+            const bool in = n + r < p.N;
+            o.v[r] = (TO)mm_out(s[r], sa, p.sb && in ? p.sb[n + r] : 1.f, p.bias && in ? p.bias[n + r] : 0.f);
         }
         TO* d = (TO*)p.out + m * p.ldc + n;
         if (n + 4 <= p.N) {
@@ -397,11 +400,8 @@ __global__ __launch_bounds__(NW * 64) void k_mm_rows(MmArgs p)
         int sum = 0;
 #pragma unroll
         for (int i = 0; i < NW; i++) sum += red[i][t][at];
-        float v = (float)sum;
-        if (p.sa) v *= p.sa[row];
-        if (p.sb) v *= p.sb[n];
-        if (p.bias) v += p.bias[n];
-        ((TO*)p.out)[row * p.ldc + n] = (TO)v;
+        ((TO*)p.out)[row * p.ldc + n] =
+            (TO)mm_out(sum, p.sa ? p.sa[row] : 1.f, p.sb ? p.sb[n] : 1.f, p.bias ? p.bias[n] : 0.f);
     }
 }
 
@@ -521,10 +521,7 @@ __global__ __launch_bounds__(512) void k_linear_token(LinArgs a)
         int sum = 0;
 #pragma unroll
         for (int i = 0; i < NW; i++) sum += red[i][tid >> 4][tid & 15];
-        float v = (float)sum * s;
-        if (p.sb) v *= p.sb[n];
-        if (p.bias) v += p.bias[n];
-        ((TO*)p.out)[n] = (TO)v;
+        ((TO*)p.out)[n] = (TO)mm_out(sum, s, p.sb ? p.sb[n] : 1.f, p.bias ? p.bias[n] : 0.f);
     }
 }
 
