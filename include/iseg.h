@@ -679,6 +679,31 @@ int iseg_linear_i8_fwd(const void* x, const int8_t* w, const float* w_scale, con
                        const iseg_linear_geom* g, int8_t* codes, float* scale, void* y, void* ws, size_t ws_bytes,
                        int32_t* dev_status, hipStream_t stream);
 
+/* iseg_linear_i8_bwd -- backward of iseg_linear_i8_fwd with straight-through
+ * quantizers, its products in integers too:
+ *   dx = Q_rows(dy w_scale) w        (iseg_quantize_rows of dy with mul = w_scale)
+ *   dw = Q_cols(dy a_scale)^T a      (iseg_quantize_cols of dy with mul = a_scale)
+ *   dbias = sum of dy over the rows
+ * dy [M, N] of dy_dtype; a [M, K] and a_scale [M], the forward's codes and
+ * scales; w [N, K], w_scale [N] (NULL: 1); w_t [K, N]: w transposed
+ * (iseg_transpose_i8), which a program keeps between updates; wt_ld = 0 without
+ * it, and w is transposed in the workspace.  dx [M, K] and dw [N, K] of
+ * out_dtype, dbias [N] float32: each may be NULL (not wanted; what only it
+ * needs may then be NULL too).  Reductions, N for dx and M for dw, of at most
+ * 131071 (ISEG_ERR_UNSUPPORTED beyond). */
+typedef struct iseg_linear_bwd_geom {
+    int64_t M, N, K;
+    int64_t dy_ld, a_ld, w_ld, wt_ld, dx_ld, dw_ld;
+    int32_t dy_dtype, out_dtype;
+    int32_t bits, scale_mode;
+    int32_t unaligned;           /* not 0: w_t may start off a multiple of 16 bytes */
+    int32_t reserved;            /* 0 */
+} iseg_linear_bwd_geom;
+size_t iseg_linear_i8_bwd_ws(const iseg_linear_bwd_geom* g);
+int iseg_linear_i8_bwd(const void* dy, const int8_t* a, const float* a_scale, const int8_t* w, const float* w_scale,
+                       const int8_t* w_t, const iseg_linear_bwd_geom* g, void* dx, void* dw, float* dbias,
+                       void* ws, size_t ws_bytes, int32_t* dev_status, hipStream_t stream);
+
 /* iseg_logprob_fwd -- for every row x of logits [M, V]:
  *   lse = log sum_v e^x_v; logprob = x_t - lse of the given token t;
  *   entropy = -sum_v p_v log p_v, p_v = e^(x_v - lse);

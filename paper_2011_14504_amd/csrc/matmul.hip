@@ -43,6 +43,22 @@ __device__ __forceinline__ v4i load16(const int8_t* row, int64_t k, int64_t K)
     return r;
 }
 
+// 16 bytes from p + k of a row that starts off a multiple of four: five whole
+// words, shifted (loads at odd bytes run at a quarter of the rate of aligned
+// ones).  Touches up to three bytes before p + k and after its 16.
+__device__ __forceinline__ v4i load16_odd(const int8_t* p, int64_t k)
+{
+    const uint32_t sh = (uint32_t)((uintptr_t)p & 3);
+    const uint32_t* q = (const uint32_t*)(p - sh + k);
+    uint32_t d[5];
+    __builtin_memcpy(d, __builtin_assume_aligned(q, 4), 16);
+    d[4] = q[4];
+    v4i r;
+#pragma unroll
+    for (int i = 0; i < 4; i++) r[i] = (int)__builtin_amdgcn_alignbyte(d[i + 1], d[i], sh);
+    return r;
+}
+
 // An output from its sum: two roundings after the sum's own, the same in every
 // kernel, so a row has the same bits alone and in a batch.
 __device__ __forceinline__ float mm_out(int sum, float sa, float sb, float bias)
@@ -288,7 +304,8 @@ __global__ __launch_bounds__(256) void k_mm_pack(MmArgs p, int8_t* __restrict__ 
     for (int64_t i = blockIdx.x * (int64_t)256 + threadIdx.x; i < all; i += (int64_t)gridDim.x * 256) {
         const bool first = i < na;
         const int64_t e = first ? i : i - na, r = e / pieces, k = (e - r * pieces) * 16;
-        *(v4i*)((first ? a : b) + r * Kp + k) = load16(first ? p.a + r * p.lda : p.b + r * p.ldb, k, p.K);
+        const int8_t* row = first ? p.a + r * p.lda : p.b + r * p.ldb;
+        *(v4i*)((first ? a : b) + r * Kp + k) = k > 0 && k + 20 <= p.K ? load16_odd(row, k) : load16(row, k, p.K);
     }
 }
 
@@ -332,7 +349,8 @@ __global__ __launch_bounds__(256) void k_mm_join(MmArgs p, const int32_t* __rest
 // A block takes J * 16 rows of b, its NW waves deal out their reduction in
 // pieces of 256; b comes straight into fragments (nothing of it is used
 // twice), a from the caches, and the waves' sums meet in LDS.
-template <typename TO, int MT, int J, int NW>
+// ODD: rows of a or b may start off a multiple of four bytes.
+template <typename TO, int MT, int J, int NW, bool ODD>
 __global__ __launch_bounds__(NW * 64) void k_mm_rows(MmArgs p)
 {
     __shared__ __attribute__((aligned(16))) int red[NW][MT * J][256];
@@ -358,7 +376,16 @@ __global__ __launch_bounds__(NW * 64) void k_mm_rows(MmArgs p)
     const int K = (int)p.K;
     for (int k0 = w * 256; k0 < K; k0 += NW * 256) {
         v4i fa[4][MT], fb[4][J];
-        if (k0 + 256 <= K) {
+        if (ODD && k0 > 0 && k0 + 260 <= K) {
+#pragma unroll
+            for (int u = 0; u < 4; u++)
+#pragma unroll
+                for (int j = 0; j < J; j++) fb[u][j] = load16_odd(bp[j], k0 + u * 64 + lp * 16);
+#pragma unroll
+            for (int u = 0; u < 4; u++)
+#pragma unroll
+                for (int i = 0; i < MT; i++) fa[u][i] = load16_odd(ap[i], k0 + u * 64 + lp * 16);
+        } else if (k0 + 256 <= K) {
 #pragma unroll
             for (int u = 0; u < 4; u++)
 #pragma unroll
@@ -469,7 +496,7 @@ __global__ __launch_bounds__(512) void k_linear_token(LinArgs a)
             const uint32_t b = bits_of((float)xv[j].v[i]);
             big = b > big ? b : big;
         }
-    big = wave_max_u32(big);
+    big = wave_top_u32(big);
     if (lane == 0) top[w] = big;
     __syncthreads();
 #pragma unroll
@@ -543,7 +570,10 @@ int launch_rows(const MmArgs& p, hipStream_t s)
 {
     const int64_t nb = ceil_div64(p.N, J * 16);
     if (nb * (NW * 64) >= (int64_t)1 << 32) return ISEG_ERR_UNSUPPORTED;
-    hipLaunchKernelGGL((k_mm_rows<TO, MT, J, NW>), dim3((unsigned)nb), dim3(NW * 64), 0, s, p);
+    if (((uintptr_t)p.a | (uintptr_t)p.b | (uintptr_t)p.lda | (uintptr_t)p.ldb) & 3)
+        hipLaunchKernelGGL((k_mm_rows<TO, MT, J, NW, true>), dim3((unsigned)nb), dim3(NW * 64), 0, s, p);
+    else
+        hipLaunchKernelGGL((k_mm_rows<TO, MT, J, NW, false>), dim3((unsigned)nb), dim3(NW * 64), 0, s, p);
     return launch_ok();
 }
 
@@ -777,4 +807,114 @@ extern "C" int iseg_linear_i8_fwd(const void* x, const int8_t* w, const float* w
     if (rc != ISEG_OK) return rc;
     const iseg_matmul_geom p = lin_product(g);
     return iseg_matmul_i8(codes, scale, w, w_scale, bias, &p, y, ws, ws_bytes, stream);
+}
+
+// ---------------------------------------------------------------------------
+// backward of the linear layer
+// ---------------------------------------------------------------------------
+namespace {
+
+int64_t up16(int64_t n) { return (n + 15) / 16 * 16; }
+
+int lbw_check(const iseg_linear_bwd_geom* g)
+{
+    if (!g || !is_float_dtype(g->dy_dtype) || !is_float_dtype(g->out_dtype) || g->bits < 2 || g->bits > 8 ||
+        (g->scale_mode != ISEG_SCALE_MAX && g->scale_mode != ISEG_SCALE_POW2))
+        return ISEG_ERR_ARG;
+    const int64_t big = (int64_t)1 << 31;
+    if (g->M < 0 || g->N < 0 || g->K < 0 || g->M >= big || g->N >= big || g->K >= big || g->dy_ld < g->N ||
+        g->a_ld < g->K || g->w_ld < g->K || (g->wt_ld && g->wt_ld < g->N) || g->dx_ld < g->K || g->dw_ld < g->K)
+        return ISEG_ERR_SHAPE;
+    return ISEG_OK;
+}
+
+// products of the two gradients: dx = Q_rows(dy) [M, N] x w^T, dw = Q_cols(dy) [N, M] x a^T
+iseg_matmul_geom lbw_dx(const iseg_linear_bwd_geom* g)
+{
+    return {g->M, g->K, g->N, up16(g->N), g->wt_ld ? g->wt_ld : up16(g->N), g->dx_ld, g->out_dtype, g->unaligned};
+}
+
+iseg_matmul_geom lbw_dw(const iseg_linear_bwd_geom* g)
+{
+    return {g->N, g->K, g->M, up16(g->M), up16(g->M), g->dw_ld, g->out_dtype, 0};
+}
+
+// The workspace, the same for both gradients, which run one after the other:
+// codes, scales, the transposed second operand, the quantizer's own, the product's own.
+struct LbwWs {
+    size_t codes, scale, turned, quant, product, total;
+};
+
+LbwWs lbw_ws(const iseg_linear_bwd_geom* g, bool dw)
+{
+    const iseg_matmul_geom p = dw ? lbw_dw(g) : lbw_dx(g);
+    LbwWs w = {};
+    w.codes = 0;
+    w.scale = align256((size_t)p.M * p.lda);
+    w.turned = w.scale + align256((size_t)p.M * 4);
+    w.quant = w.turned + (dw || !g->wt_ld ? align256((size_t)p.N * p.ldb) : 0);
+    w.product = w.quant + (dw ? align256(iseg_quantize_cols_ws(g->M, g->N)) : 0);
+    w.total = w.product + iseg_matmul_i8_ws(&p);
+    return w;
+}
+
+}  // namespace
+
+extern "C" size_t iseg_linear_i8_bwd_ws(const iseg_linear_bwd_geom* g)
+{
+    if (lbw_check(g) != ISEG_OK) return 0;
+    const size_t a = lbw_ws(g, false).total, b = lbw_ws(g, true).total;
+    return a > b ? a : b;
+}
+
+extern "C" int iseg_linear_i8_bwd(const void* dy, const int8_t* a, const float* a_scale, const int8_t* w,
+                                  const float* w_scale, const int8_t* w_t, const iseg_linear_bwd_geom* g, void* dx,
+                                  void* dw, float* dbias, void* ws, size_t ws_bytes, int32_t* dev_status,
+                                  hipStream_t stream)
+{
+    int rc = lbw_check(g);
+    if (rc != ISEG_OK) return rc;
+    // what is asked for, of what is not empty
+    const bool want_x = dx && g->M > 0 && g->K > 0, want_w = dw && g->N > 0 && g->K > 0, want_b = dbias && g->N > 0;
+    if ((want_x && g->N > 131071) || (want_w && g->M > 131071)) return ISEG_ERR_UNSUPPORTED;
+    if (g->M > 0 && g->N > 0 && (want_x || want_w || want_b) && !dy) return ISEG_ERR_ARG;
+    if (want_x && g->N > 0 && !(g->wt_ld ? w_t : w)) return ISEG_ERR_ARG;
+    if (want_x && g->wt_ld && !g->unaligned && ((uintptr_t)w_t & 15)) return ISEG_ERR_ARG;
+    if (want_w && g->M > 0 && !a) return ISEG_ERR_ARG;
+    if (!ws || ws_bytes < iseg_linear_i8_bwd_ws(g)) return ISEG_ERR_WORKSPACE;
+    char* base = (char*)ws;
+    if (want_x) {
+        const iseg_matmul_geom p = lbw_dx(g);
+        const LbwWs o = lbw_ws(g, false);
+        int8_t* codes = (int8_t*)(base + o.codes);
+        float* scale = (float*)(base + o.scale);
+        const int8_t* wt = w_t;
+        if (!g->wt_ld) {
+            rc = iseg_transpose_i8(w, g->N, g->K, g->w_ld, (int8_t*)(base + o.turned), p.ldb, stream);
+            if (rc != ISEG_OK) return rc;
+            wt = (const int8_t*)(base + o.turned);
+        }
+        rc = iseg_quantize_rows(dy, g->dy_dtype, g->M, g->N, g->dy_ld, w_scale, g->bits, g->scale_mode, codes, p.lda,
+                                scale, dev_status, stream);
+        if (rc != ISEG_OK) return rc;
+        rc = iseg_matmul_i8(codes, scale, wt, nullptr, nullptr, &p, dx, base + o.product, ws_bytes - o.product, stream);
+        if (rc != ISEG_OK) return rc;
+    }
+    if (want_w || want_b) {
+        const iseg_matmul_geom p = lbw_dw(g);
+        const LbwWs o = lbw_ws(g, true);
+        int8_t* codes = (int8_t*)(base + o.codes);
+        float* scale = (float*)(base + o.scale);
+        rc = iseg_quantize_cols(dy, g->dy_dtype, g->M, g->N, g->dy_ld, a_scale, g->bits, g->scale_mode, codes, p.lda,
+                                scale, dbias, base + o.quant, o.product - o.quant, dev_status, stream);
+        if (rc != ISEG_OK) return rc;
+        if (want_w) {
+            int8_t* at = (int8_t*)(base + o.turned);
+            rc = iseg_transpose_i8(a, g->M, g->K, g->a_ld, at, p.ldb, stream);
+            if (rc != ISEG_OK) return rc;
+            rc = iseg_matmul_i8(codes, scale, at, nullptr, nullptr, &p, dw, base + o.product, ws_bytes - o.product,
+                                stream);
+        }
+    }
+    return rc;
 }

@@ -78,15 +78,23 @@ __device__ __forceinline__ float wave_sum_f32(float v)
     return lane63_f32(v);
 }
 
-__device__ __forceinline__ float wave_max_f32(float v)
+// largest of 64 lanes' unsigned values, the same in every lane
+template <int CTRL>
+__device__ __forceinline__ uint32_t dpp_max_step(uint32_t v)
 {
-    v = fmaxf(v, dpp_f32<0x111>(v, v));
-    v = fmaxf(v, dpp_f32<0x112>(v, v));
-    v = fmaxf(v, dpp_f32<0x114>(v, v));
-    v = fmaxf(v, dpp_f32<0x118>(v, v));
-    v = fmaxf(v, dpp_f32<0x142>(v, v));
-    v = fmaxf(v, dpp_f32<0x143>(v, v));
-    return lane63_f32(v);
+    const uint32_t t = (uint32_t)__builtin_amdgcn_update_dpp((int)v, (int)v, CTRL, 0xf, 0xf, false);
+    return t > v ? t : v;
+}
+
+__device__ __forceinline__ uint32_t wave_top_u32(uint32_t v)
+{
+    v = dpp_max_step<0x111>(v);
+    v = dpp_max_step<0x112>(v);
+    v = dpp_max_step<0x114>(v);
+    v = dpp_max_step<0x118>(v);
+    v = dpp_max_step<0x142>(v);
+    v = dpp_max_step<0x143>(v);
+    return (uint32_t)__builtin_amdgcn_readlane((int)v, 63);
 }
 
 // sums of two values over the NW waves of a block, the same in every thread.

@@ -26,7 +26,7 @@ struct RqRowArgs {
 template <int NW>
 __device__ __forceinline__ uint32_t row_max_u32(uint32_t v, uint32_t* red)
 {
-    v = wave_max_u32(v);
+    v = wave_top_u32(v);
     if (NW == 1) return v;
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
     if (lane == 0) red[w] = v;
@@ -419,7 +419,6 @@ __global__ __launch_bounds__(256) void k_transpose_i8(const int8_t* __restrict__
 {
     __shared__ uint32_t t[128][33];           // [column][rows / 4]
     const int64_t c0 = (int64_t)blockIdx.x * 128;
-    const bool rd = (in_ld & 3) == 0 && ((uintptr_t)in & 3) == 0;
     const bool wide = (out_ld & 15) == 0 && ((uintptr_t)out & 15) == 0;
     const int64_t mt = ceil_div64(M, 128);
     for (int64_t b = blockIdx.y; b < mt; b += gridDim.y) {
@@ -434,8 +433,8 @@ __global__ __launch_bounds__(256) void k_transpose_i8(const int8_t* __restrict__
                 const int64_t m = m0 + rq * 4 + u < M ? m0 + rq * 4 + u : M - 1;
                 const int8_t* p = in + m * in_ld + c;
                 r[u] = 0;
-                if (rd && c + 4 <= C) {
-                    r[u] = *(const uint32_t*)p;
+                if (c + 4 <= C) {
+                    __builtin_memcpy(&r[u], p, 4);
                 } else {
                     for (int x = 0; x < 4; x++)
                         if (c + x < C) r[u] |= (uint32_t)(uint8_t)p[x] << (8 * x);

@@ -91,6 +91,7 @@ const Entry kEntries[] = {
     ISEG_TAPE_ENTRY(iseg_transpose_i8)
     ISEG_TAPE_ENTRY(iseg_matmul_i8)
     ISEG_TAPE_ENTRY(iseg_linear_i8_fwd)
+    ISEG_TAPE_ENTRY(iseg_linear_i8_bwd)
     ISEG_TAPE_ENTRY(iseg_logprob_fwd)
     ISEG_TAPE_ENTRY(iseg_logprob_bwd)
     ISEG_TAPE_ENTRY(iseg_profile_arm)

@@ -83,6 +83,11 @@ class LinearGeom(C.Structure):
                [(n, C.c_int32) for n in ("x_dtype", "y_dtype", "bits", "scale_mode", "unaligned", "reserved")]
 
 
+class LinearBwdGeom(C.Structure):
+    _fields_ = [(n, C.c_int64) for n in ("M", "N", "K", "dy_ld", "a_ld", "w_ld", "wt_ld", "dx_ld", "dw_ld")] + \
+               [(n, C.c_int32) for n in ("dy_dtype", "out_dtype", "bits", "scale_mode", "unaligned", "reserved")]
+
+
 class LogprobGeom(C.Structure):
     _fields_ = [(n, C.c_int64) for n in ("M", "V", "ld", "out_ld")] + \
                [(n, C.c_int32) for n in ("dtype", "token_dtype", "top_k", "reserved")]
@@ -162,6 +167,8 @@ _SIGS = {
     "iseg_matmul_i8": ([_P, _P, _P, _P, _P, _P, _P, _P, _SZ, _P], C.c_int),
     "iseg_linear_i8_fwd_ws": ([_P], _SZ),
     "iseg_linear_i8_fwd": ([_P, _P, _P, _P, _P, _P, _P, _P, _P, _SZ, _P, _P], C.c_int),
+    "iseg_linear_i8_bwd_ws": ([_P], _SZ),
+    "iseg_linear_i8_bwd": ([_P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _SZ, _P, _P], C.c_int),
     "iseg_logprob_fwd_ws": ([_P], _SZ),
     "iseg_logprob_fwd": ([_P, _P, _P, _P, _P, _P, _P, _P, _P, _SZ, _P, _P], C.c_int),
     "iseg_logprob_bwd": ([_P, _P, _P, _P, _P, _P, _P, _P, _P, _P], C.c_int),
@@ -532,6 +539,12 @@ def iseg_linear_i8_fwd(x, w, w_scale, bias, geom, codes, scale, y, ws, status=No
     rc = lib().iseg_linear_i8_fwd(_ptr(x), _ptr(w), _ptr(w_scale), _ptr(bias), C.byref(geom), _ptr(codes),
                                   _ptr(scale), _ptr(y), *_ws_tuple(ws), _ptr(status), _stream())
     _check(rc, "iseg_linear_i8_fwd")
+
+
+def iseg_linear_i8_bwd(dy, a, a_scale, w, w_scale, w_t, geom, dx, dw, dbias, ws, status=None):
+    rc = lib().iseg_linear_i8_bwd(_ptr(dy), _ptr(a), _ptr(a_scale), _ptr(w), _ptr(w_scale), _ptr(w_t), C.byref(geom),
+                                  _ptr(dx), _ptr(dw), _ptr(dbias), *_ws_tuple(ws), _ptr(status), _stream())
+    _check(rc, "iseg_linear_i8_bwd")
 
 
 def iseg_logprob_fwd(logits, tokens, geom, logprob, lse, entropy, top_ids, top_logprob, ws, status=None):
@@ -1354,6 +1367,13 @@ def _linear_geom(M, N, K, x_ld, w_ld, codes_ld, y_ld, x_dtype, y_dtype, bits, sc
 
 
 @functools.lru_cache(maxsize=256)
+def _linear_bwd_geom(M, N, K, dy_ld, a_ld, w_ld, wt_ld, out_ld, dy_dtype, out_dtype, bits, scale_mode, unaligned):
+    g = LinearBwdGeom(M, N, K, dy_ld, a_ld, w_ld, wt_ld, out_ld, out_ld, dy_dtype, out_dtype, bits, scale_mode,
+                      unaligned, 0)
+    return g, lib().iseg_linear_i8_bwd_ws(C.byref(g))
+
+
+@functools.lru_cache(maxsize=256)
 def _logprob_geom(M, V, ld, out_ld, dtype, token_dtype, top_k):
     g = LogprobGeom(M, V, ld, out_ld, dtype, token_dtype, top_k, 0)
     return g, lib().iseg_logprob_fwd_ws(C.byref(g))
@@ -1528,23 +1548,31 @@ def linear_i8_bwd(dy, a, a_scale, w, w_scale=None, w_t=None, bits=8, scale_mode=
     a, a_scale: the forward's codes and scales; w_t: the transposed weight
     codes (transpose_i8), which a program keeps between updates.  dx [M, K] and
     dw [N, K] have out_dtype (by default dy's), dbias is float32."""
-    _float_code(dy, "dy")
-    if a.dim() != 2 or w.dim() != 2 or dy.dim() < 1 or a.shape[1] != w.shape[1] or dy.shape[-1] != w.shape[0]:
-        raise ValueError("dy [..., N], a [M, K] and w [N, K] expected")
-    dr, M, N, _ = _rows(dy, "dy")
-    if M != a.shape[0]:
-        raise ValueError("dy and a: as many rows expected")
-    if w_t is not None and tuple(w_t.shape) != (w.shape[1], w.shape[0]):
-        raise ValueError("w_t: the transposed w expected")
     out_dtype = dy.dtype if out_dtype is None else out_dtype
-    dx = dw = dbias = None
-    if want_input:
-        q, s = quantize_rows(dr, bits, scale_mode, w_scale, status)
-        dx = matmul_i8(q, transpose_i8(w) if w_t is None else w_t, s, None, None, out_dtype)
-    if want_weight or want_bias:
-        q, s, dbias = quantize_cols(dr, bits, scale_mode, a_scale, want_bias, status)
-        if want_weight:
-            dw = matmul_i8(q, transpose_i8(a), s, None, None, out_dtype)
+    dd, od = _float_code(dy, "dy"), _float_code(out_dtype, "out_dtype")
+    _quant_args(bits, scale_mode)
+    dr, M, N, dy_ld = _rows(dy, "dy")
+    ar, Ma, K, a_ld = _code_rows(a, "a")
+    wr, Nw, Kw, w_ld = _code_rows(w, "w")
+    if Ma != M or Nw != N or Kw != K:
+        raise ValueError("dy [..., N], a [M, K] and w [N, K] expected")
+    if (want_input and N > 131071) or (want_weight and M > 131071):
+        raise ValueError("dy: reductions of at most 131071 expected")
+    tr, wt_ld = None, 0
+    if w_t is not None:
+        tr, Kt, Nt, wt_ld = _code_rows(w_t, "w_t")
+        if Kt != K or Nt != N:
+            raise ValueError("w_t: the transposed w expected")
+    dev = dy.device
+    a_scale = _vec(a_scale, M, torch.float32, dev, "a_scale")
+    w_scale = _vec(w_scale, N, torch.float32, dev, "w_scale")
+    _gpu(dy, a, w, w_t, status)
+    dx = torch.empty((M, K), dtype=out_dtype, device=dev) if want_input else None
+    dw = torch.empty((N, K), dtype=out_dtype, device=dev) if want_weight else None
+    dbias = torch.empty(N, dtype=torch.float32, device=dev) if want_bias else None
+    g, wsb = _linear_bwd_geom(M, N, K, dy_ld, a_ld, w_ld, wt_ld, max(K, 1), dd, od, bits, scale_mode,
+                              0 if tr is None else int(tr.data_ptr() & 15 != 0))
+    iseg_linear_i8_bwd(dr, ar, a_scale, wr, w_scale, tr, g, dx, dw, dbias, _scratch(dev, wsb), status)
     return dx, dw, dbias
 
 

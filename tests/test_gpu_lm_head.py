@@ -190,7 +190,7 @@ def test_tape_replays_a_step():
     tape = iseg.Tape(0)
     with tape:
         out = _step(iseg, p, x, tok, g, h)
-    assert tape.size() == 10                    # three forward; one, five and one backward
+    assert tape.size() == 6                     # three forward, three backward
     for seed in (50, 60):
         x.copy_(normal(seed, M, D))
         tok.copy_((normal(seed + 1, M).abs() * 1e6).long() % V)

@@ -57,7 +57,7 @@ def test_product(case):
 
 # sizes that reach every way a product is run: few rows, each tile, a reduction
 # in parts; with whole and broken tiles and reductions, and rows off 16 bytes
-PATHS = [(15, 9000, 300), (16, 20, 8200), (20, 100, 500), (32, 5000, 272), (33, 20, 2050), (40, 40, 9000), (64, 2048, 4096), (512, 1024, 1536), (1024, 2048, 400),
+PATHS = [(11, 416, 14279), (1, 33, 1025), (32, 700, 2307), (15, 9000, 300), (16, 20, 8200), (20, 100, 500), (32, 5000, 272), (33, 20, 2050), (40, 40, 9000), (64, 2048, 4096), (512, 1024, 1536), (1024, 2048, 400),
          (1000, 2050, 130), (1500, 2048, 1000), (2048, 2048, 128), (4000, 4100, 160), (4096, 8192, 256), (4100, 4100, 1), (260, 16000, 100)]
 
 
@@ -251,6 +251,18 @@ def test_quantize_tiny_huge_and_non_finite():
         assert torch.equal(s.cpu(), ws) and torch.equal(q.cpu(), wq)
 
 
+def test_linear_backward_empty():
+    from paper_2011_14504_amd import iseg
+    w, one = codes(1, 5, 16).to(DEV), torch.ones(5, device=DEV)
+    dx, dw, db = iseg.linear_i8_bwd(torch.empty(0, 5, device=DEV), torch.empty(0, 16, dtype=torch.int8, device=DEV), one[:0], w, one, want_bias=True)
+    assert dx.shape == (0, 16) and torch.equal(dw.cpu(), torch.zeros(5, 16)) and torch.equal(db.cpu(), torch.zeros(5))
+    dx, dw, db = iseg.linear_i8_bwd(torch.empty(3, 0, device=DEV), torch.ones(3, 16, dtype=torch.int8, device=DEV), one[:3], w[:0], one[:0], want_bias=True)
+    assert torch.equal(dx.cpu(), torch.zeros(3, 16)) and dw.shape == (0, 16) and db.shape == (0,)
+    dx, dw, db = iseg.linear_i8_bwd(torch.ones(3, 5, device=DEV), torch.empty(3, 0, dtype=torch.int8, device=DEV), one[:3], torch.empty(5, 0, dtype=torch.int8, device=DEV), one,
+                                    want_bias=True)
+    assert dx.shape == (3, 0) and dw.shape == (5, 0) and torch.equal(db.cpu(), torch.full((5,), 3.0))
+
+
 def test_linear_modes_strides_and_status():
     from paper_2011_14504_amd import iseg
     st = torch.zeros(1, dtype=torch.int32, device=DEV)
@@ -339,5 +351,14 @@ def test_linear_forward_and_backward(case):
     # the same bits as its two parts, whichever way it is run
     q2, s2 = iseg.quantize_rows(x.to(DEV))
     assert torch.equal(iseg.matmul_i8(q2, w.to(DEV), s2, ws.to(DEV), bias.to(DEV), DT[t]), y)
+    wide = torch.zeros(K, N + 5, dtype=torch.int8, device=DEV)
+    wide[:, 5:] = wt
+    again = iseg.linear_i8_bwd(dy.to(DEV), strided(wqa, K + 3, 9), sa, strided(w, K + 1, 9), ws.to(DEV), w_t=wide[:, 5:], want_bias=True)
+    for g, e in zip(again, (dx, dw, db)):
+        assert torch.equal(g, e)
+    q3, s3, db3 = iseg.quantize_cols(dy.to(DEV), mul=sa, want_sums=True)
+    assert torch.equal(db3, db)
+    no = iseg.linear_i8_bwd(dy.to(DEV), qa, sa, w.to(DEV), ws.to(DEV), want_weight=False, want_bias=True)
+    assert no[1] is None and torch.equal(no[0], dx) and torch.equal(no[2], db)
     only = iseg.linear_i8_bwd(dy.to(DEV), qa, sa, w.to(DEV), ws.to(DEV), want_input=False)
     assert only[0] is None and only[2] is None and torch.equal(only[1], dw)

@@ -110,6 +110,28 @@ def test_linear_entry(iseg):
     assert lin(M=0, x=None, codes=None, scale=None, y=None) == iseg.ISEG_OK
 
 
+def test_linear_backward_entry(iseg):
+    L = iseg.lib()
+
+    def bwd(M=4, N=32, K=16, dy_ld=32, a_ld=16, w_ld=16, wt_ld=0, dx_ld=16, dw_ld=16, dd=iseg.ISEG_BF16, od=iseg.ISEG_F32, bits=8, mode=0, un=0,
+            dy=ONE, a=ONE, w=ONE, w_t=None, dx=ONE, dw=ONE, db=ONE, ws=ONE, n=BIG):
+        g = iseg.LinearBwdGeom(M, N, K, dy_ld, a_ld, w_ld, wt_ld, dx_ld, dw_ld, dd, od, bits, mode, un, 0)
+        return L.iseg_linear_i8_bwd(dy, a, None, w, None, w_t, C.byref(g), dx, dw, db, ws, n, None, None)
+
+    off = C.c_void_p(ONE.value + 4)
+    for bad in (dict(dd=iseg.ISEG_I8), dict(od=iseg.ISEG_I32), dict(bits=1), dict(bits=9), dict(mode=3), dict(dy=None), dict(w=None), dict(a=None),
+                dict(wt_ld=32, w_t=None), dict(wt_ld=32, w_t=off)):
+        assert bwd(**bad) == iseg.ISEG_ERR_ARG, bad
+    for bad in (dict(M=-1), dict(N=-1), dict(K=-1), dict(dy_ld=31), dict(a_ld=15), dict(w_ld=15), dict(wt_ld=31, w_t=ONE), dict(dx_ld=15), dict(dw_ld=15),
+                dict(K=1 << 31, a_ld=1 << 31, w_ld=1 << 31, dx_ld=1 << 31, dw_ld=1 << 31)):
+        assert bwd(**bad) == iseg.ISEG_ERR_SHAPE, bad
+    assert bwd(N=131072, dy_ld=131072, dw=None, db=None) == iseg.ISEG_ERR_UNSUPPORTED
+    assert bwd(M=131072, dx=None) == iseg.ISEG_ERR_UNSUPPORTED
+    assert bwd(ws=None) == iseg.ISEG_ERR_WORKSPACE and bwd(n=1) == iseg.ISEG_ERR_WORKSPACE
+    assert bwd(dx=None, dw=None, db=None, dy=None, a=None, w=None) == iseg.ISEG_OK
+    assert bwd(M=0, N=0, dy=None, a=None, w=None) == iseg.ISEG_OK
+
+
 def test_logprob_entries(iseg):
     L = iseg.lib()
 
@@ -173,6 +195,6 @@ def test_helpers(iseg):
 def test_tape_knows_the_operators(iseg):
     L = iseg.lib()
     for n in ("iseg_layernorm_fwd", "iseg_layernorm_bwd", "iseg_quantize_rows", "iseg_quantize_cols", "iseg_transpose_i8",
-              "iseg_matmul_i8", "iseg_linear_i8_fwd", "iseg_logprob_fwd", "iseg_logprob_bwd"):
+              "iseg_matmul_i8", "iseg_linear_i8_fwd", "iseg_linear_i8_bwd", "iseg_logprob_fwd", "iseg_logprob_bwd"):
         e = L.iseg_tape_entry(n.encode())
         assert e >= 0 and L.iseg_tape_entry_nargs(e) == len(iseg._SIGS[n][0])
