@@ -575,7 +575,8 @@ int iseg_mse_onehot(const int8_t* y, const int32_t* y_exp, const uint8_t* labels
  * and scales are float32 or wider whatever the tensors' type, and a result is
  * rounded to its type once.  Bytes between a row's end and the next row are
  * neither read into a result nor written.  An empty matrix (M = 0) is valid
- * and its pointers may be NULL. */
+ * and its pointers may be NULL.  A workspace query of 256 bytes means that the
+ * call touches none of it. */
 
 /* iseg_layernorm_fwd -- layer normalization of every row of x [M, C]:
  *   mean = sum x / C, var = sum (x - mean)^2 / C, rstd = 1 / sqrt(var + eps),
@@ -590,13 +591,13 @@ int iseg_mse_onehot(const int8_t* y, const int32_t* y_exp, const uint8_t* labels
  *   dgamma = sum over rows of dy xhat, dbeta = sum over rows of dy.
  * dy (rows y_ld apart) and dx have x_dtype; dgamma and dbeta [C] p_dtype, each
  * may be NULL.  Sums have one fixed order: the same call gives the same bits.
- * With M = 0, dgamma and dbeta are zeros. */
+ * With M = 0, dgamma and dbeta are zeros.  C <= 2^27. */
 typedef struct iseg_layernorm_geom {
     int64_t M, C;
     int64_t x_ld, y_ld, dx_ld;   /* y_ld: rows of y, or of dy in the backward; dx_ld: backward only */
     int32_t x_dtype, p_dtype;
     float eps;                   /* forward only */
-    int32_t reserved;            /* 0 */
+    int32_t reserved;            /* 0 (ISEG_ERR_ARG otherwise, here and below) */
 } iseg_layernorm_geom;
 int iseg_layernorm_fwd(const void* x, const void* gamma, const void* beta, const iseg_layernorm_geom* g,
                        void* y, float* mean, float* rstd, int32_t* dev_status, hipStream_t stream);
@@ -623,7 +624,7 @@ enum iseg_scale_mode { ISEG_SCALE_MAX = 0, ISEG_SCALE_POW2 = 1 };
  * iseg_quantize_cols -- a scale for each column (channel) of x [M, C], the
  * codes stored transposed: v = x[m, c] mul[m] (mul [M]), codes[c, m] with rows
  * codes_ld >= M apart, scale [C].  sums (may be NULL): [C] float32, the plain
- * column sums of x (without mul), in one fixed order.
+ * column sums of x (without mul), in one fixed order.  C <= 2^28.
  *
  * Both are the quantizer of an operand of iseg_matmul_i8: rows for y = x w^T
  * and for the input's gradient, columns for the weight's gradient. */
@@ -636,7 +637,7 @@ int iseg_quantize_cols(const void* x, int32_t x_dtype, int64_t M, int64_t C, int
                        float* sums, void* ws, size_t ws_bytes, int32_t* dev_status, hipStream_t stream);
 
 /* iseg_transpose_i8 -- out[c, m] = in[m, c] of int8 codes [M, C]: the second
- * operand of the gradients' products.  in_ld >= C, out_ld >= M. */
+ * operand of the gradients' products.  in_ld >= C, out_ld >= M, C <= 2^28. */
 int iseg_transpose_i8(const int8_t* in, int64_t M, int64_t C, int64_t in_ld, int8_t* out, int64_t out_ld,
                       hipStream_t stream);
 
@@ -649,7 +650,7 @@ int iseg_transpose_i8(const int8_t* in, int64_t M, int64_t C, int64_t in_ld, int
  * type).  A row's outputs do not depend on the other rows.  K = 0 gives the
  * bias.  a and b start at multiples of 16 bytes unless `unaligned`
  * is set (ISEG_ERR_ARG); with it, or with lda or ldb off a multiple of 16, the
- * workspace holds aligned copies of both (not for M <= 32). */
+ * workspace has room for aligned copies (not for M <= 32). */
 typedef struct iseg_matmul_geom {
     int64_t M, N, K;
     int64_t lda, ldb, ldc;
@@ -729,7 +730,8 @@ int iseg_linear_i8_bwd(const void* dy, const int8_t* a, const float* a_scale, co
 typedef struct iseg_logprob_geom {
     int64_t M, V;
     int64_t ld, out_ld;          /* out_ld: backward only */
-    int32_t dtype, token_dtype, top_k, reserved;
+    int32_t dtype, token_dtype, top_k;
+    int32_t reserved;            /* 0 */
 } iseg_logprob_geom;
 size_t iseg_logprob_fwd_ws(const iseg_logprob_geom* g);
 int iseg_logprob_fwd(const void* logits, const void* tokens, const iseg_logprob_geom* g, float* logprob, float* lse,

@@ -504,7 +504,7 @@ int lp_splits(const iseg_logprob_geom* g)
 
 int lp_check(const iseg_logprob_geom* g)
 {
-    if (!g || !is_float_dtype(g->dtype)) return ISEG_ERR_ARG;
+    if (!g || !is_float_dtype(g->dtype) || g->reserved) return ISEG_ERR_ARG;
     if (g->token_dtype != ISEG_I32 && g->token_dtype != ISEG_I64) return ISEG_ERR_ARG;
     if (g->M < 0 || g->V < 1 || g->V >= (int64_t)1 << 31 || g->ld < g->V) return ISEG_ERR_SHAPE;
     if (g->top_k < 0 || g->top_k > kTopMax || g->top_k > g->V) return ISEG_ERR_ARG;
@@ -545,8 +545,8 @@ extern "C" size_t iseg_logprob_fwd_ws(const iseg_logprob_geom* g)
 {
     if (lp_check(g) != ISEG_OK) return 0;
     const size_t sp = (size_t)lp_splits(g);
-    if (sp == 1 || g->M == 0) return 256;
-    return align256((size_t)g->M * sp * 16) + align256((size_t)g->M * sp * (size_t)g->top_k * 8);
+    if (sp == 1 || g->M == 0) return kNoWs;
+    return ws_used(align256((size_t)g->M * sp * 16) + align256((size_t)g->M * sp * (size_t)g->top_k * 8));
 }
 
 extern "C" int iseg_logprob_fwd(const void* logits, const void* tokens, const iseg_logprob_geom* g, float* logprob,

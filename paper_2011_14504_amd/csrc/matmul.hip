@@ -44,8 +44,8 @@ __device__ __forceinline__ v4i load16(const int8_t* row, int64_t k, int64_t K)
 }
 
 // 16 bytes from p + k of a row that starts off a multiple of four: five whole
-// words, shifted (loads at odd bytes run at a quarter of the rate of aligned
-// ones).  Touches up to three bytes before p + k and after its 16.
+// words, shifted (11 x 4160 x 14279: 62 us with loads at odd bytes, 36 so).
+// Touches up to three bytes before p + k and after its 16.
 __device__ __forceinline__ v4i load16_odd(const int8_t* p, int64_t k)
 {
     const uint32_t sh = (uint32_t)((uintptr_t)p & 3);
@@ -295,17 +295,18 @@ __global__ __launch_bounds__(WM * WN * 64) void k_mm_tile(MmArgs p)
     }
 }
 
-// Rows of a and b copied into buffers of zero-padded rows of Kp bytes (a
-// multiple of 64): operands whose rows start off 16 bytes, where loads to LDS
-// would straddle.  One pass over them, against M N K / 64 products.
-__global__ __launch_bounds__(256) void k_mm_pack(MmArgs p, int8_t* __restrict__ a, int8_t* __restrict__ b, int64_t Kp)
+// Rows of a, of b or of both copied into buffers of zero-padded rows of Kp
+// bytes (a multiple of 64): operands whose rows start off 16 bytes, where loads
+// to LDS would straddle.  One pass over them, against M N K / 64 products.
+// pa, pb: NULL for an operand that stays.
+__global__ __launch_bounds__(256) void k_mm_pack(MmArgs p, int8_t* __restrict__ pa, int8_t* __restrict__ pb, int64_t Kp)
 {
-    const int64_t pieces = Kp / 16, na = p.M * pieces, all = na + p.N * pieces;
+    const int64_t pieces = Kp / 16, na = pa ? p.M * pieces : 0, all = na + (pb ? p.N * pieces : 0);
     for (int64_t i = blockIdx.x * (int64_t)256 + threadIdx.x; i < all; i += (int64_t)gridDim.x * 256) {
         const bool first = i < na;
         const int64_t e = first ? i : i - na, r = e / pieces, k = (e - r * pieces) * 16;
         const int8_t* row = first ? p.a + r * p.lda : p.b + r * p.ldb;
-        *(v4i*)((first ? a : b) + r * Kp + k) = k > 0 && k + 20 <= p.K ? load16_odd(row, k) : load16(row, k, p.K);
+        *(v4i*)((first ? pa : pb) + r * Kp + k) = k > 0 && k + 20 <= p.K ? load16_odd(row, k) : load16(row, k, p.K);
     }
 }
 
@@ -594,28 +595,31 @@ int launch_split(const MmArgs& p, int splits, int32_t* ws, hipStream_t s)
     return launch_ok();
 }
 
-// How a product is run.  The tile kernels' times on MI355X, in us, for one
-// round of blocks over the 256 CUs (te + ts per 128 of the reduction), once
-// with one block per CU and once with as many as fit:
-//   256 x 256          9.5 + 1.6          (one fits)
-//   128 x 128, 2 waves 3.5 + 0.6 (four stages)   4.2 + 0.9 (two blocks of two stages)
-//   64 x 128           2.0 + 0.3          3.0 + 0.7
-//   64 x 64            0.6 + 0.27         1.5 + 0.55
+// How a product is run.  The tile kernels' times on MI355X, in us without the
+// launch, for one round of blocks over the 256 CUs (te + ts per 128 of the
+// reduction), once with one block per CU and once with as many as fit:
+//   256 x 256           9.7 + 1.55        (one fits)
+//   192 x 192           6.0 + 1.13        (one fits)
+//   128 x 192           4.5 + 0.8         5.5 + 1.27
+//   128 x 128           3.5 + 0.6 (four stages)   4.2 + 0.9 (two blocks of two stages)
+//   64 x 128            2.0 + 0.3         3.0 + 0.7
+//   64 x 64             0.6 + 0.27        1.5 + 0.55
 // The plan with the least estimate is taken; a reduction cut into parts costs
-// a second kernel (4.5 us).  Against the estimate, e.g. 2048 x 8192 x 2048:
-// 256 x 256 tiles 37.7 us, 128 x 128 39.5; 1024 x 2048 x 2048: 64 x 128 9.4,
-// 128 x 128 12.7; 64 x 2048 x 8192: 64 x 64 in 8 parts 12.3, in one 20.7.
-enum MmKind { MM_ROWS16, MM_ROWS32, MM_256, MM_128, MM_128_DEEP, MM_64x128, MM_64 };
+// a second kernel (4.5 us).  Measured beside it: 2048 x 8192 x 2048, 256 tiles
+// of 256 x 256 39.0 us, 128 x 128 44.8; 4544 x 1824 x 7488, 240 tiles of 192 x
+// 192 76, 144 of 256 x 256 102; 1024 x 2048 x 2048, 64 x 128 9.4, 128 x 128
+// 12.7; 64 x 2048 x 8192, 64 x 64 in 8 parts 12.3, in one 20.7.
+enum MmKind { MM_ROWS16, MM_ROWS32, MM_256, MM_192, MM_128x192, MM_128, MM_128_DEEP, MM_64x128, MM_64 };
 struct MmPlan {
     MmKind kind;
     int splits;
-    bool pack;
+    bool pack_a, pack_b;         // may have to be packed
 };
 
 MmPlan mm_plan(const iseg_matmul_geom* g)
 {
     // few rows: b's bytes are what counts (see k_mm_rows)
-    if (g->M <= 32) return {g->M <= 16 ? MM_ROWS16 : MM_ROWS32, 1, false};
+    if (g->M <= 32) return {g->M <= 16 ? MM_ROWS16 : MM_ROWS32, 1, false, false};
     struct Kind {
         MmKind one, full;
         int64_t bm, bn;
@@ -623,27 +627,30 @@ MmPlan mm_plan(const iseg_matmul_geom* g)
         double te1, ts1, te, ts;
     };
     static const Kind kinds[] = {
-        {MM_256, MM_256, 256, 256, 1, 9.5, 1.6, 9.5, 1.6},
+        {MM_256, MM_256, 256, 256, 1, 9.7, 1.55, 9.7, 1.55},
+        {MM_192, MM_192, 192, 192, 1, 6.0, 1.13, 6.0, 1.13},
+        {MM_128x192, MM_128x192, 128, 192, 2, 4.5, 0.8, 5.5, 1.27},
         {MM_128_DEEP, MM_128, 128, 128, 2, 3.5, 0.6, 4.2, 0.9},
         {MM_64x128, MM_64x128, 64, 128, 2, 2.0, 0.3, 3.0, 0.7},
         {MM_64, MM_64, 64, 64, 2, 0.6, 0.27, 1.5, 0.55},
     };
     const int64_t st = ceil_div64(g->K, 128);
-    MmPlan best = {MM_64, 1, false};
+    MmPlan best = {MM_64, 1, false, false};
     double least = 1e30;
     for (const Kind& k : kinds) {
         const int64_t tiles = ceil_div64(g->M, k.bm) * ceil_div64(g->N, k.bn);
         const double t = tiles <= 256 ? k.te1 + k.ts1 * (double)st
                                       : (double)ceil_div64(tiles, 256 * k.fit) * (k.te + k.ts * (double)st);
-        if (t < least) { least = t; best = {tiles <= 256 ? k.one : k.full, 1, false}; }
+        if (t < least) { least = t; best = {tiles <= 256 ? k.one : k.full, 1, false, false}; }
         if (k.one == MM_64 && tiles <= 128) {
             int64_t sp = 256 / tiles < 16 ? 256 / tiles : 16;
             sp = sp < st / 4 ? sp : st / 4;              // parts of at least 512 of the reduction
             const double u = sp > 1 ? k.te1 + k.ts1 * (double)ceil_div64(st, sp) + 4.5 : 1e30;
-            if (u < least) { least = u; best = {MM_64, (int)sp, false}; }
+            if (u < least) { least = u; best = {MM_64, (int)sp, false, false}; }
         }
     }
-    best.pack = g->unaligned || g->lda % 16 || g->ldb % 16;
+    best.pack_a = g->unaligned || g->lda % 16;
+    best.pack_b = g->unaligned || g->ldb % 16;
     return best;
 }
 
@@ -651,7 +658,8 @@ int64_t mm_packed_row(int64_t K) { return (K + 63) / 64 * 64; }
 
 size_t mm_pack_bytes(const iseg_matmul_geom* g, const MmPlan& pl)
 {
-    return pl.pack ? align256((size_t)g->M * mm_packed_row(g->K)) + align256((size_t)g->N * mm_packed_row(g->K)) : 0;
+    const size_t Kp = (size_t)mm_packed_row(g->K);
+    return (pl.pack_a ? align256((size_t)g->M * Kp) : 0) + (pl.pack_b ? align256((size_t)g->N * Kp) : 0);
 }
 
 template <typename TO>
@@ -661,17 +669,23 @@ int launch_mm(MmArgs p, const iseg_matmul_geom* g, const MmPlan& pl, char* ws, h
     // / 8 x 12288 x 4096: 16 rows, 8 waves 6.5 / 17.0 us, 32 rows 7.0 / 14.1.
     if (pl.kind == MM_ROWS16) return g->N <= 8192 ? launch_rows<TO, 1, 1, 8>(p, s) : launch_rows<TO, 1, 2, 8>(p, s);
     if (pl.kind == MM_ROWS32) return g->N <= 4096 ? launch_rows<TO, 2, 1, 8>(p, s) : launch_rows<TO, 2, 2, 8>(p, s);
-    if (pl.pack && p.K > 0) {
+    if (p.K > 0) {
         const int64_t Kp = mm_packed_row(p.K);
-        int8_t* pa = (int8_t*)ws;
-        int8_t* pb = pa + align256((size_t)p.M * Kp);
-        hipLaunchKernelGGL(k_mm_pack, dim3(grid_for((p.M + p.N) * (Kp / 16), 256, 8192)), dim3(256), 0, s, p, pa, pb, Kp);
-        p.a = pa;
-        p.b = pb;
-        p.lda = p.ldb = p.K = Kp;
+        int8_t* pa = pl.pack_a && ((p.lda | (int64_t)(uintptr_t)p.a) & 15) ? (int8_t*)ws : nullptr;
+        int8_t* pb = pl.pack_b && ((p.ldb | (int64_t)(uintptr_t)p.b) & 15)
+                         ? (int8_t*)ws + (pl.pack_a ? align256((size_t)p.M * Kp) : 0) : nullptr;
+        if (pa || pb) {
+            const int64_t rows = (pa ? p.M : 0) + (pb ? p.N : 0);
+            hipLaunchKernelGGL(k_mm_pack, dim3(grid_for(rows * (Kp / 16), 256, 8192)), dim3(256), 0, s, p, pa, pb, Kp);
+            if (pa) { p.a = pa; p.lda = Kp; }
+            if (pb) { p.b = pb; p.ldb = Kp; }
+            if (pa && pb) p.K = Kp;           // both padded with zeros: no broken last piece
+        }
     }
     switch (pl.kind) {
     case MM_256: return launch_tile<TO, 256, 256, 2, 4, 2>(p, s);
+    case MM_192: return launch_tile<TO, 192, 192, 2, 4, 3>(p, s);
+    case MM_128x192: return launch_tile<TO, 128, 192, 2, 4, 2>(p, s);
     case MM_128: return launch_tile<TO, 128, 128, 2, 4, 2>(p, s);
     case MM_128_DEEP: return launch_tile<TO, 128, 128, 2, 4, 4>(p, s);
     case MM_64x128: return launch_tile<TO, 64, 128, 2, 4, 3>(p, s);
@@ -697,11 +711,11 @@ int mm_check(const iseg_matmul_geom* g)
 extern "C" size_t iseg_matmul_i8_ws(const iseg_matmul_geom* g)
 {
     if (mm_check(g) != ISEG_OK) return 0;
-    if (g->M == 0 || g->N == 0) return 256;
+    if (g->M == 0 || g->N == 0) return kNoWs;
     const MmPlan pl = mm_plan(g);
     size_t b = mm_pack_bytes(g, pl);
     if (pl.splits > 1) b += align256((size_t)pl.splits * g->M * ((g->N + 3) / 4 * 4) * 4);
-    return b > 256 ? b : 256;
+    return b ? ws_used(b) : kNoWs;
 }
 
 extern "C" int iseg_matmul_i8(const int8_t* a, const float* a_scale, const int8_t* b, const float* b_scale,
@@ -731,7 +745,7 @@ namespace {
 int lin_check(const iseg_linear_geom* g)
 {
     if (!g || !is_float_dtype(g->x_dtype) || !is_float_dtype(g->y_dtype) || g->bits < 2 || g->bits > 8 ||
-        (g->scale_mode != ISEG_SCALE_MAX && g->scale_mode != ISEG_SCALE_POW2))
+        (g->scale_mode != ISEG_SCALE_MAX && g->scale_mode != ISEG_SCALE_POW2) || g->reserved)
         return ISEG_ERR_ARG;
     const int64_t big = (int64_t)1 << 31;
     if (g->M < 0 || g->N < 0 || g->K < 0 || g->M >= big || g->N >= big || g->x_ld < g->K || g->w_ld < g->K ||
@@ -779,7 +793,7 @@ extern "C" size_t iseg_linear_i8_fwd_ws(const iseg_linear_geom* g)
 {
     if (lin_check(g) != ISEG_OK) return 0;
     const iseg_matmul_geom p = lin_product(g);
-    return lin_fused(g) ? 256 : iseg_matmul_i8_ws(&p);
+    return lin_fused(g) ? kNoWs : iseg_matmul_i8_ws(&p);
 }
 
 extern "C" int iseg_linear_i8_fwd(const void* x, const int8_t* w, const float* w_scale, const float* bias,
@@ -819,7 +833,7 @@ int64_t up16(int64_t n) { return (n + 15) / 16 * 16; }
 int lbw_check(const iseg_linear_bwd_geom* g)
 {
     if (!g || !is_float_dtype(g->dy_dtype) || !is_float_dtype(g->out_dtype) || g->bits < 2 || g->bits > 8 ||
-        (g->scale_mode != ISEG_SCALE_MAX && g->scale_mode != ISEG_SCALE_POW2))
+        (g->scale_mode != ISEG_SCALE_MAX && g->scale_mode != ISEG_SCALE_POW2) || g->reserved)
         return ISEG_ERR_ARG;
     const int64_t big = (int64_t)1 << 31;
     if (g->M < 0 || g->N < 0 || g->K < 0 || g->M >= big || g->N >= big || g->K >= big || g->dy_ld < g->N ||
@@ -864,7 +878,7 @@ extern "C" size_t iseg_linear_i8_bwd_ws(const iseg_linear_bwd_geom* g)
 {
     if (lbw_check(g) != ISEG_OK) return 0;
     const size_t a = lbw_ws(g, false).total, b = lbw_ws(g, true).total;
-    return a > b ? a : b;
+    return ws_used(a > b ? a : b);
 }
 
 extern "C" int iseg_linear_i8_bwd(const void* dy, const int8_t* a, const float* a_scale, const int8_t* w,

@@ -248,6 +248,17 @@ __global__ __launch_bounds__(NW * 64) void k_layernorm_bwd(LnArgs a)
             if (j < VPT - 1 || sl[j].dup < N) row_store((T*)a.dx + m * a.dx_ld + sl[j].at, o);
         }
     }
+    if (gridDim.x == 1) {                                     // a few rows: the block's sums are the sums
+#pragma unroll
+        for (int j = 0; j < VPT; j++)
+#pragma unroll
+            for (int i = 0; i < N; i++)
+                if (i >= sl[j].dup) {
+                    if (a.dgamma) ((P*)a.dgamma)[sl[j].at + i] = (P)dg[j][i];
+                    if (a.dbeta) ((P*)a.dbeta)[sl[j].at + i] = (P)db[j][i];
+                }
+        return;
+    }
     float* part = a.part + (int64_t)blockIdx.x * 2 * C;
 #pragma unroll
     for (int j = 0; j < VPT; j++) {
@@ -358,6 +369,7 @@ bool ln_bwd_in_regs(const iseg_layernorm_geom* g)
 int ln_bwd_blocks(const iseg_layernorm_geom* g)
 {
     const int64_t v = ln_vectors(g);
+    if (ln_bwd_in_regs(g) && g->M <= 8) return g->M > 0;      // one block and no second kernel
     const int64_t cap = !ln_bwd_in_regs(g) ? 64 : v <= 64 ? 1536 : v <= 128 ? 1024 : v <= 256 ? 512 : 256;
     return (int)(g->M < cap ? g->M : cap);
 }
@@ -400,7 +412,7 @@ int launch_bwd(const LnArgs& a, const iseg_layernorm_geom* g, hipStream_t s)
         }
         if (rc != ISEG_OK) return rc;
     }
-    if (a.dgamma || a.dbeta)
+    if ((a.dgamma || a.dbeta) && !(nb == 1 && ln_bwd_in_regs(g)))
         hipLaunchKernelGGL((k_layernorm_param_sum<P>), dim3((unsigned)ceil_div64(a.C, 64), 2), dim3(1024), 0, s, a.part,
                            nb, a.C, (P*)a.dgamma, (P*)a.dbeta);
     return launch_ok();
@@ -410,7 +422,8 @@ int ln_check(const iseg_layernorm_geom* g)
 {
     if (!g || !is_float_dtype(g->x_dtype) || !is_float_dtype(g->p_dtype)) return ISEG_ERR_ARG;
     if (g->M < 0 || g->C < 1 || g->C >= (int64_t)1 << 31 || g->x_ld < g->C || g->y_ld < g->C) return ISEG_ERR_SHAPE;
-    return ISEG_OK;
+    if (g->reserved) return ISEG_ERR_ARG;
+    return g->C <= (int64_t)1 << 27 ? ISEG_OK : ISEG_ERR_UNSUPPORTED;      // a launch's threads
 }
 
 }  // namespace
@@ -448,7 +461,8 @@ extern "C" size_t iseg_layernorm_bwd_ws(const iseg_layernorm_geom* g)
     const size_t nb = (size_t)ln_bwd_blocks(g);
     size_t b = align256(nb * 2 * (size_t)g->C * 4);
     if (!ln_bwd_in_regs(g)) b += align256((size_t)g->M * 8);
-    return b > 256 ? b : 256;
+    else if (nb <= 1) return kNoWs;
+    return ws_used(b);
 }
 
 extern "C" int iseg_layernorm_bwd(const void* dy, const void* x, const void* gamma, const float* mean,

@@ -173,6 +173,11 @@ static inline bool slots_fit(int64_t C)
     return C >= RowVec<T>::N && v > nt * (VPT - 1) && v <= nt * VPT;
 }
 
+// Workspace sizes: kNoWs of a call that touches none of it (one such buffer may
+// then serve every stream), more than that of any other.
+constexpr size_t kNoWs = 256;
+static inline size_t ws_used(size_t bytes) { return bytes > 2 * kNoWs ? align256(bytes) : 2 * kNoWs; }
+
 static inline bool is_float_dtype(int32_t t) { return t == ISEG_F32 || t == ISEG_F16 || t == ISEG_BF16; }
 
 // launches walk their rows in a loop, so the grid may be cut at any count

@@ -456,7 +456,7 @@ __global__ __launch_bounds__(256) void k_transpose_i8(const int8_t* __restrict__
     }
 }
 
-constexpr int64_t kMaxCols = (int64_t)1 << 31;
+constexpr int64_t kMaxCols = (int64_t)1 << 31, kMaxTurned = (int64_t)1 << 28;      // a launch's threads
 
 // strips of rows whose partials a column's scale is taken from: blocks for the
 // chip, at least 128 rows each
@@ -558,9 +558,8 @@ extern "C" int iseg_quantize_rows(const void* x, int32_t x_dtype, int64_t M, int
 
 extern "C" size_t iseg_quantize_cols_ws(int64_t M, int64_t C)
 {
-    if (M < 0 || C < 0 || C >= kMaxCols) return 0;
-    const size_t b = (size_t)cols_strips(M, C) * (size_t)C * 12;
-    return b > 256 ? align256(b) : 256;
+    if (M < 0 || C < 0 || C > kMaxTurned) return 0;
+    return ws_used((size_t)cols_strips(M, C) * (size_t)C * 12);
 }
 
 extern "C" int iseg_quantize_cols(const void* x, int32_t x_dtype, int64_t M, int64_t C, int64_t x_ld,
@@ -571,6 +570,7 @@ extern "C" int iseg_quantize_cols(const void* x, int32_t x_dtype, int64_t M, int
     const int rc = rq_check(x_dtype, bits, scale_mode);
     if (rc != ISEG_OK) return rc;
     if (M < 0 || C < 0 || C >= kMaxCols || x_ld < C || codes_ld < M) return ISEG_ERR_SHAPE;
+    if (C > kMaxTurned) return ISEG_ERR_UNSUPPORTED;
     if (C == 0) return ISEG_OK;
     if (!scale || (M > 0 && (!x || !codes))) return ISEG_ERR_ARG;
     if (!ws || ws_bytes < iseg_quantize_cols_ws(M, C)) return ISEG_ERR_WORKSPACE;
@@ -587,6 +587,7 @@ extern "C" int iseg_transpose_i8(const int8_t* in, int64_t M, int64_t C, int64_t
                                  hipStream_t stream)
 {
     if (M < 0 || C < 0 || C >= kMaxCols || in_ld < C || out_ld < M) return ISEG_ERR_SHAPE;
+    if (C > kMaxTurned) return ISEG_ERR_UNSUPPORTED;
     if (M == 0 || C == 0) return ISEG_OK;
     if (!in || !out) return ISEG_ERR_ARG;
     const int64_t mt = ceil_div64(M, 128);

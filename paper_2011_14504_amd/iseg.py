@@ -1275,9 +1275,10 @@ def _on_device(f):
     the current device)."""
     @functools.wraps(f)
     def call(x, *args, **kw):
-        if not x.is_cuda or x.device.index == _raw_device():
+        i = x.get_device()
+        if i < 0 or i == _raw_device():
             return f(x, *args, **kw)
-        with torch.cuda.device(x.device):
+        with torch.cuda.device(i):
             return f(x, *args, **kw)
     return call
 
@@ -1313,25 +1314,26 @@ def _rows(t, what):
     return t, M, Cc, ld
 
 
-def _vec(t, n, dtype, device, what):
-    """A dense vector of n elements on `device`, or None."""
+def _vec(t, n, dtype, x, what):
+    """A dense vector of n elements beside x, or None."""
     if t is None:
         return None
-    if t.dtype != dtype or t.numel() != n or t.device != device:
-        raise ValueError(f"{what}: {n} elements of {dtype} on {device} expected")
-    if t.dim() == 1 and (n <= 1 or t.stride(0) == 1):
+    if t.dtype is not dtype or t.numel() != n or t.get_device() != x.get_device():
+        raise ValueError(f"{what}: {n} elements of {dtype} on {x.device} expected")
+    if t.is_contiguous():
         return t
-    if _REC is not None and not t.is_contiguous():
+    if _REC is not None:
         raise IsegError(f"{what}: a recorded call needs a dense vector")
     return t.contiguous()
 
 
-def _gpu(*ts):
+def _gpu(x, *ts):
+    i = x.get_device()
+    if i < 0:
+        raise ValueError("GPU tensors expected")
     for t in ts:
-        if t is not None and not t.is_cuda:
-            raise ValueError("GPU tensors expected")
-        if t is not None and t.device != ts[0].device:
-            raise ValueError("tensors on one device expected")
+        if t is not None and t.get_device() != i:
+            raise ValueError("GPU tensors on one device expected")
 
 
 def _like(t):
@@ -1339,13 +1341,22 @@ def _like(t):
     return torch.empty_like(t) if t.is_contiguous() else torch.empty(t.shape, dtype=t.dtype, device=t.device)
 
 
-def _scratch(device, nbytes):
-    """Workspace of a call: the stream's, or, under graph capture, memory of
-    the graph's own (a graph outlives the stream's workspace, and two graphs
-    may replay at once)."""
-    if nbytes > 256 and torch.cuda.is_current_stream_capturing():      # 256: the least size, of calls that use none
-        return torch.empty(max(nbytes, 256), dtype=torch.uint8, device=device)
-    return workspace(device).get(nbytes)
+_NO_WS = {}
+
+
+def _scratch(x, nbytes):
+    """Workspace of a call on x's device: the stream's, or, under graph
+    capture, memory of the graph's own (a graph outlives the stream's workspace,
+    and two graphs may replay at once)."""
+    if nbytes == 256:                # a call that touches none of it: one for all
+        i = x.get_device()
+        ws = _NO_WS.get(i)
+        if ws is None:
+            ws = _NO_WS[i] = torch.empty(256, dtype=torch.uint8, device=x.device)
+        return ws
+    if torch.cuda.is_current_stream_capturing():
+        return torch.empty(nbytes, dtype=torch.uint8, device=x.device)
+    return workspace(x.device).get(nbytes)
 
 
 @functools.lru_cache(maxsize=256)
@@ -1391,8 +1402,8 @@ def layernorm_fwd(x, gamma=None, beta=None, eps=1e-5, status=None):
         raise ValueError("eps: positive and finite expected")
     p = gamma if gamma is not None else beta
     pd = _float_code(p, "gamma, beta") if p is not None else ISEG_F32
-    gamma = _vec(gamma, Cc, p.dtype if p is not None else None, x.device, "gamma")
-    beta = _vec(beta, Cc, p.dtype if p is not None else None, x.device, "beta")
+    gamma = _vec(gamma, Cc, p.dtype if p is not None else None, x, "gamma")
+    beta = _vec(beta, Cc, p.dtype if p is not None else None, x, "beta")
     _gpu(x, status)
     y = _like(x)
     mean = torch.empty(M if x.dim() == 2 else x.shape[:-1], dtype=torch.float32, device=x.device)
@@ -1414,16 +1425,16 @@ def layernorm_bwd(dy, x, gamma, mean, rstd, want_params=True):
         raise ValueError("x: empty rows")
     pdt = gamma.dtype if gamma is not None else torch.float32
     pd = _float_code(pdt, "gamma")
-    gamma = _vec(gamma, Cc, pdt, x.device, "gamma")
-    mean = _vec(mean, M, torch.float32, x.device, "mean")
-    rstd = _vec(rstd, M, torch.float32, x.device, "rstd")
+    gamma = _vec(gamma, Cc, pdt, x, "gamma")
+    mean = _vec(mean, M, torch.float32, x, "mean")
+    rstd = _vec(rstd, M, torch.float32, x, "rstd")
     _gpu(x, dy)
     dx = _like(x)
     dgamma = torch.empty(Cc, dtype=pdt, device=x.device) if want_params else None
     dbeta = torch.empty_like(dgamma) if want_params else None
     g = _layernorm_geom(M, Cc, ld, dld, Cc, xd, pd, 1.0)
     iseg_layernorm_bwd(dr, xr, gamma, mean, rstd, g, dx, dgamma, dbeta,
-                       _scratch(x.device, lib().iseg_layernorm_bwd_ws(C.byref(g))))
+                       _scratch(x, lib().iseg_layernorm_bwd_ws(C.byref(g))))
     return dx, dgamma, dbeta
 
 
@@ -1431,7 +1442,7 @@ def _codes_matrix(rows, cols, device):
     """int8 [rows, cols] in rows of a multiple of 16 bytes (the alignment that
     the products' wide loads take)."""
     if cols % 16 == 0:
-        return torch.empty((rows, cols), dtype=torch.int8, device=device)
+        return torch.empty(rows, cols, dtype=torch.int8, device=device)
     return torch.empty((rows, (cols + 15) // 16 * 16), dtype=torch.int8, device=device)[:, :cols]
 
 
@@ -1449,7 +1460,7 @@ def quantize_rows(x, bits=8, scale_mode=ISEG_SCALE_MAX, mul=None, status=None):
     xd = _float_code(x, "x")
     _quant_args(bits, scale_mode)
     xr, M, Cc, ld = _rows(x, "x")
-    mul = _vec(mul, Cc, torch.float32, x.device, "mul")
+    mul = _vec(mul, Cc, torch.float32, x, "mul")
     _gpu(x, status)
     codes = _codes_matrix(M, Cc, x.device)
     scale = torch.empty(M, dtype=torch.float32, device=x.device)
@@ -1465,13 +1476,13 @@ def quantize_cols(x, bits=8, scale_mode=ISEG_SCALE_MAX, mul=None, want_sums=Fals
     xd = _float_code(x, "x")
     _quant_args(bits, scale_mode)
     xr, M, Cc, ld = _rows(x, "x")
-    mul = _vec(mul, M, torch.float32, x.device, "mul")
+    mul = _vec(mul, M, torch.float32, x, "mul")
     _gpu(x, status)
     codes = _codes_matrix(Cc, M, x.device)
     scale = torch.empty(Cc, dtype=torch.float32, device=x.device)
     sums = torch.empty(Cc, dtype=torch.float32, device=x.device) if want_sums else None
     iseg_quantize_cols(xr, xd, M, Cc, ld, mul, bits, scale_mode, codes, codes.stride(0), scale, sums,
-                       _scratch(x.device, lib().iseg_quantize_cols_ws(M, Cc)), status)
+                       _scratch(x, lib().iseg_quantize_cols_ws(M, Cc)), status)
     return codes, scale, sums
 
 
@@ -1502,13 +1513,13 @@ def matmul_i8(a, b, a_scale=None, b_scale=None, bias=None, out_dtype=torch.float
         raise ValueError("a and b: rows of one length expected")
     if K > 131071:
         raise ValueError("a and b: rows of at most 131071 codes expected")
-    a_scale = _vec(a_scale, M, torch.float32, a.device, "a_scale")
-    b_scale = _vec(b_scale, N, torch.float32, a.device, "b_scale")
-    bias = _vec(bias, N, torch.float32, a.device, "bias")
+    a_scale = _vec(a_scale, M, torch.float32, a, "a_scale")
+    b_scale = _vec(b_scale, N, torch.float32, a, "b_scale")
+    bias = _vec(bias, N, torch.float32, a, "bias")
     _gpu(a, b)
-    out = torch.empty((M, N), dtype=out_dtype, device=a.device)
+    out = torch.empty(M, N, dtype=out_dtype, device=a.device)
     g, wsb = _matmul_geom(M, N, K, lda, ldb, max(N, 1), od, int((ar.data_ptr() | br.data_ptr()) & 15 != 0))
-    iseg_matmul_i8(ar, a_scale, br, b_scale, bias, g, out, _scratch(a.device, wsb))
+    iseg_matmul_i8(ar, a_scale, br, b_scale, bias, g, out, _scratch(a, wsb))
     return out
 
 
@@ -1527,15 +1538,15 @@ def linear_i8_fwd(x, w, w_scale=None, bias=None, bits=8, scale_mode=ISEG_SCALE_M
     if K > 131071:
         raise ValueError("x and w: rows of at most 131071 elements expected")
     dev = x.device
-    w_scale = _vec(w_scale, N, torch.float32, dev, "w_scale")
-    bias = _vec(bias, N, torch.float32, dev, "bias")
+    w_scale = _vec(w_scale, N, torch.float32, x, "w_scale")
+    bias = _vec(bias, N, torch.float32, x, "bias")
     _gpu(x, w, status)
     codes = _codes_matrix(M, K, dev)
     scale = torch.empty(M, dtype=torch.float32, device=dev)
-    y = torch.empty((M, N) if x.dim() == 2 else x.shape[:-1] + (N,), dtype=out_dtype, device=dev)
+    y = torch.empty(*x.shape[:-1], N, dtype=out_dtype, device=dev)
     g, wsb = _linear_geom(M, N, K, x_ld, w_ld, codes.stride(0) if K else 16, max(N, 1), xd, od, bits, scale_mode,
                           int(wr.data_ptr() & 15 != 0))
-    iseg_linear_i8_fwd(xr, wr, w_scale, bias, g, codes, scale, y, _scratch(dev, wsb), status)
+    iseg_linear_i8_fwd(xr, wr, w_scale, bias, g, codes, scale, y, _scratch(x, wsb), status)
     return y, codes, scale
 
 
@@ -1564,15 +1575,15 @@ def linear_i8_bwd(dy, a, a_scale, w, w_scale=None, w_t=None, bits=8, scale_mode=
         if Kt != K or Nt != N:
             raise ValueError("w_t: the transposed w expected")
     dev = dy.device
-    a_scale = _vec(a_scale, M, torch.float32, dev, "a_scale")
-    w_scale = _vec(w_scale, N, torch.float32, dev, "w_scale")
+    a_scale = _vec(a_scale, M, torch.float32, dy, "a_scale")
+    w_scale = _vec(w_scale, N, torch.float32, dy, "w_scale")
     _gpu(dy, a, w, w_t, status)
-    dx = torch.empty((M, K), dtype=out_dtype, device=dev) if want_input else None
-    dw = torch.empty((N, K), dtype=out_dtype, device=dev) if want_weight else None
+    dx = torch.empty(M, K, dtype=out_dtype, device=dev) if want_input else None
+    dw = torch.empty(N, K, dtype=out_dtype, device=dev) if want_weight else None
     dbias = torch.empty(N, dtype=torch.float32, device=dev) if want_bias else None
     g, wsb = _linear_bwd_geom(M, N, K, dy_ld, a_ld, w_ld, wt_ld, max(K, 1), dd, od, bits, scale_mode,
                               0 if tr is None else int(tr.data_ptr() & 15 != 0))
-    iseg_linear_i8_bwd(dr, ar, a_scale, wr, w_scale, tr, g, dx, dw, dbias, _scratch(dev, wsb), status)
+    iseg_linear_i8_bwd(dr, ar, a_scale, wr, w_scale, tr, g, dx, dw, dbias, _scratch(dy, wsb), status)
     return dx, dw, dbias
 
 
@@ -1606,9 +1617,9 @@ def logprob_fwd(logits, tokens, top_k=0, want_entropy=True, status=None):
     logprob = torch.empty(M if logits.dim() == 2 else shape, dtype=torch.float32, device=dev)
     lse = torch.empty_like(logprob)
     entropy = torch.empty_like(logprob) if want_entropy else None
-    ids = torch.empty(shape + (top_k,), dtype=torch.int32, device=dev) if top_k else None
+    ids = torch.empty(*shape, top_k, dtype=torch.int32, device=dev) if top_k else None
     tlp = torch.empty_like(ids, dtype=torch.float32) if top_k else None
-    iseg_logprob_fwd(lr, tokens, g, logprob, lse, entropy, ids, tlp, _scratch(dev, wsb), status)
+    iseg_logprob_fwd(lr, tokens, g, logprob, lse, entropy, ids, tlp, _scratch(logits, wsb), status)
     return logprob, lse, entropy, ids, tlp
 
 
@@ -1626,10 +1637,10 @@ def logprob_bwd(logits, tokens, lse, entropy, g_logprob=None, g_entropy=None, st
         raise ValueError("g_logprob or g_entropy expected")
     if lse is None or (g_entropy is not None and entropy is None):
         raise ValueError("the forward's lse and, with g_entropy, its entropy expected")
-    lse = _vec(lse, M, torch.float32, logits.device, "lse")
-    entropy = _vec(entropy, M, torch.float32, logits.device, "entropy")
-    g_logprob = _vec(g_logprob, M, torch.float32, logits.device, "g_logprob")
-    g_entropy = _vec(g_entropy, M, torch.float32, logits.device, "g_entropy")
+    lse = _vec(lse, M, torch.float32, logits, "lse")
+    entropy = _vec(entropy, M, torch.float32, logits, "entropy")
+    g_logprob = _vec(g_logprob, M, torch.float32, logits, "g_logprob")
+    g_entropy = _vec(g_entropy, M, torch.float32, logits, "g_entropy")
     _gpu(logits, tokens, status)
     dx = _like(logits)
     g, _ = _logprob_geom(M, V, ld, V, dt, td, 0)

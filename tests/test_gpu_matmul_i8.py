@@ -58,7 +58,7 @@ def test_product(case):
 # sizes that reach every way a product is run: few rows, each tile, a reduction
 # in parts; with whole and broken tiles and reductions, and rows off 16 bytes
 PATHS = [(11, 416, 14279), (1, 33, 1025), (32, 700, 2307), (15, 9000, 300), (16, 20, 8200), (20, 100, 500), (32, 5000, 272), (33, 20, 2050), (40, 40, 9000), (64, 2048, 4096), (512, 1024, 1536), (1024, 2048, 400),
-         (1000, 2050, 130), (1500, 2048, 1000), (2048, 2048, 128), (4000, 4100, 160), (4096, 8192, 256), (4100, 4100, 1), (260, 16000, 100)]
+         (1000, 2050, 130), (1500, 2048, 1000), (2048, 2048, 128), (4000, 4100, 160), (4096, 8192, 256), (4100, 4100, 1), (260, 16000, 100), (2300, 3700, 1100), (3712, 2200, 300), (3200, 3200, 2000), (1900, 6100, 400)]
 
 
 @pytest.mark.parametrize("case", PATHS, ids=str)
