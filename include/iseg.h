@@ -650,7 +650,9 @@ int iseg_transpose_i8(const int8_t* in, int64_t M, int64_t C, int64_t in_ld, int
  * type).  A row's outputs do not depend on the other rows.  K = 0 gives the
  * bias.  a and b start at multiples of 16 bytes unless `unaligned`
  * is set (ISEG_ERR_ARG); with it, or with lda or ldb off a multiple of 16, the
- * workspace has room for aligned copies (not for M <= 32). */
+ * workspace has room for aligned copies (not for M <= 32).  More than 2^23 - 1
+ * tiles of 256 x 256 outputs, or with M <= 32 of 32 columns, are
+ * ISEG_ERR_UNSUPPORTED. */
 typedef struct iseg_matmul_geom {
     int64_t M, N, K;
     int64_t lda, ldb, ldc;

@@ -553,13 +553,15 @@ __global__ __launch_bounds__(512) void k_linear_token(LinArgs a)
     }
 }
 
+constexpr int kMmThreads = 512;            // of every product kernel's block
+constexpr int64_t kMmBlocks = ((int64_t)1 << 32) / kMmThreads - 1;      // a launch's threads fit 32 bits
+
 template <typename TO, int BM, int BN, int WM, int WN, int ST>
 int launch_tile(MmArgs p, hipStream_t s, int splits = 1)
 {
     constexpr size_t lds = (size_t)ST * (BM + BN) * 128;
+    static_assert(WM * WN * 64 == kMmThreads, "what mm_plan counts with");
     if (lds > 65536 && !lds_limit((const void*)k_mm_tile<TO, BM, BN, WM, WN, ST>, lds)) return ISEG_ERR_DEVICE;
-    const int64_t tiles = ceil_div64(p.M, BM) * ceil_div64(p.N, BN);
-    if (tiles * (WM * WN * 64) >= (int64_t)1 << 32) return ISEG_ERR_UNSUPPORTED;      // a launch's threads
     p.tm = (uint32_t)ceil_div64(p.M, BM);
     p.tn = (uint32_t)ceil_div64(p.N, BN);
     hipLaunchKernelGGL((k_mm_tile<TO, BM, BN, WM, WN, ST>), dim3(p.tm * p.tn, splits), dim3(WM * WN * 64), lds, s, p);
@@ -569,8 +571,8 @@ int launch_tile(MmArgs p, hipStream_t s, int splits = 1)
 template <typename TO, int MT, int J, int NW>
 int launch_rows(const MmArgs& p, hipStream_t s)
 {
+    static_assert(NW * 64 == kMmThreads, "what mm_check counts with");
     const int64_t nb = ceil_div64(p.N, J * 16);
-    if (nb * (NW * 64) >= (int64_t)1 << 32) return ISEG_ERR_UNSUPPORTED;
     if (((uintptr_t)p.a | (uintptr_t)p.b | (uintptr_t)p.lda | (uintptr_t)p.ldb) & 3)
         hipLaunchKernelGGL((k_mm_rows<TO, MT, J, NW, true>), dim3((unsigned)nb), dim3(NW * 64), 0, s, p);
     else
@@ -639,6 +641,7 @@ MmPlan mm_plan(const iseg_matmul_geom* g)
     double least = 1e30;
     for (const Kind& k : kinds) {
         const int64_t tiles = ceil_div64(g->M, k.bm) * ceil_div64(g->N, k.bn);
+        if (tiles > kMmBlocks) continue;
         const double t = tiles <= 256 ? k.te1 + k.ts1 * (double)st
                                       : (double)ceil_div64(tiles, 256 * k.fit) * (k.te + k.ts * (double)st);
         if (t < least) { least = t; best = {tiles <= 256 ? k.one : k.full, 1, false, false}; }
@@ -703,7 +706,10 @@ int mm_check(const iseg_matmul_geom* g)
         g->ldc < g->N)
         return ISEG_ERR_SHAPE;
     if (g->K > 131071) return ISEG_ERR_UNSUPPORTED;
-    return ISEG_OK;
+    // one launch: 32 rows of b per block, or the largest tiles
+    const int64_t blocks = g->M <= 32 ? (g->M > 0 ? ceil_div64(g->N, 32) : 0)
+                                      : ceil_div64(g->M, 256) * ceil_div64(g->N, 256);
+    return blocks <= kMmBlocks ? ISEG_OK : ISEG_ERR_UNSUPPORTED;
 }
 
 }  // namespace
@@ -742,22 +748,19 @@ extern "C" int iseg_matmul_i8(const int8_t* a, const float* a_scale, const int8_
 // ---------------------------------------------------------------------------
 namespace {
 
+iseg_matmul_geom lin_product(const iseg_linear_geom* g)
+{
+    return {g->M, g->N, g->K, g->codes_ld, g->w_ld, g->y_ld, g->y_dtype, g->unaligned};
+}
+
 int lin_check(const iseg_linear_geom* g)
 {
     if (!g || !is_float_dtype(g->x_dtype) || !is_float_dtype(g->y_dtype) || g->bits < 2 || g->bits > 8 ||
         (g->scale_mode != ISEG_SCALE_MAX && g->scale_mode != ISEG_SCALE_POW2) || g->reserved)
         return ISEG_ERR_ARG;
-    const int64_t big = (int64_t)1 << 31;
-    if (g->M < 0 || g->N < 0 || g->K < 0 || g->M >= big || g->N >= big || g->x_ld < g->K || g->w_ld < g->K ||
-        g->codes_ld < g->K || g->codes_ld % 16 || g->y_ld < g->N)
-        return ISEG_ERR_SHAPE;
-    if (g->K > 131071) return ISEG_ERR_UNSUPPORTED;
-    return ISEG_OK;
-}
-
-iseg_matmul_geom lin_product(const iseg_linear_geom* g)
-{
-    return {g->M, g->N, g->K, g->codes_ld, g->w_ld, g->y_ld, g->y_dtype, g->unaligned};
+    if (g->x_ld < g->K || g->codes_ld % 16) return ISEG_ERR_SHAPE;
+    const iseg_matmul_geom p = lin_product(g);
+    return mm_check(&p);
 }
 
 // One kernel for one token: 1 x 4096 x 4096 8.9 us against 9.4 for the two,
@@ -774,7 +777,6 @@ int launch_linear(const LinArgs& a, hipStream_t s)
 {
     const bool two = a.p.N > 8192;         // rows of b per block as for k_mm_rows
     const int64_t nb = ceil_div64(a.p.N, two ? 32 : 16);
-    if (nb * 512 >= (int64_t)1 << 32) return ISEG_ERR_UNSUPPORTED;
     if (two) hipLaunchKernelGGL((k_linear_token<TX, TO, 2>), dim3((unsigned)nb), dim3(512), 0, s, a);
     else hipLaunchKernelGGL((k_linear_token<TX, TO, 1>), dim3((unsigned)nb), dim3(512), 0, s, a);
     return launch_ok();
@@ -890,7 +892,8 @@ extern "C" int iseg_linear_i8_bwd(const void* dy, const int8_t* a, const float* 
     if (rc != ISEG_OK) return rc;
     // what is asked for, of what is not empty
     const bool want_x = dx && g->M > 0 && g->K > 0, want_w = dw && g->N > 0 && g->K > 0, want_b = dbias && g->N > 0;
-    if ((want_x && g->N > 131071) || (want_w && g->M > 131071)) return ISEG_ERR_UNSUPPORTED;
+    const iseg_matmul_geom px = lbw_dx(g), pw = lbw_dw(g);
+    if ((want_x && (rc = mm_check(&px)) != ISEG_OK) || (want_w && (rc = mm_check(&pw)) != ISEG_OK)) return rc;
     if (g->M > 0 && g->N > 0 && (want_x || want_w || want_b) && !dy) return ISEG_ERR_ARG;
     if (want_x && g->N > 0 && !(g->wt_ld ? w_t : w)) return ISEG_ERR_ARG;
     if (want_x && g->wt_ld && !g->unaligned && ((uintptr_t)w_t & 15)) return ISEG_ERR_ARG;
@@ -898,7 +901,7 @@ extern "C" int iseg_linear_i8_bwd(const void* dy, const int8_t* a, const float* 
     if (!ws || ws_bytes < iseg_linear_i8_bwd_ws(g)) return ISEG_ERR_WORKSPACE;
     char* base = (char*)ws;
     if (want_x) {
-        const iseg_matmul_geom p = lbw_dx(g);
+        const iseg_matmul_geom& p = px;
         const LbwWs o = lbw_ws(g, false);
         int8_t* codes = (int8_t*)(base + o.codes);
         float* scale = (float*)(base + o.scale);
@@ -915,7 +918,7 @@ extern "C" int iseg_linear_i8_bwd(const void* dy, const int8_t* a, const float* 
         if (rc != ISEG_OK) return rc;
     }
     if (want_w || want_b) {
-        const iseg_matmul_geom p = lbw_dw(g);
+        const iseg_matmul_geom& p = pw;
         const LbwWs o = lbw_ws(g, true);
         int8_t* codes = (int8_t*)(base + o.codes);
         float* scale = (float*)(base + o.scale);

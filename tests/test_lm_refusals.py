@@ -89,6 +89,9 @@ def test_matmul_entry(iseg):
     for bad in (dict(M=-1), dict(N=-1), dict(K=-1), dict(lda=15), dict(ldb=15), dict(ldc=3), dict(M=1 << 31)):
         assert mm(**bad) == iseg.ISEG_ERR_SHAPE, bad
     assert mm(K=131072, lda=131072, ldb=131072) == iseg.ISEG_ERR_UNSUPPORTED
+    n, m = 1 << 28, (1 << 31) - 1                            # more blocks than a launch holds
+    assert mm(N=n, ldc=n) == iseg.ISEG_ERR_UNSUPPORTED and mm(M=m, N=1) == iseg.ISEG_ERR_UNSUPPORTED
+    assert mm(M=0, N=n, ldc=n, a=None, out=None) == iseg.ISEG_OK
     off = C.c_void_p(ONE.value + 8)
     assert mm(a=off) == iseg.ISEG_ERR_ARG and mm(a=off, un=1, n=0) == iseg.ISEG_ERR_WORKSPACE
     need = [L.iseg_matmul_i8_ws(C.byref(iseg.MatmulGeom(100, 200, 70, ld, 80, 200, iseg.ISEG_F32, un))) for ld, un in ((80, 0), (80, 1), (70, 0))]
@@ -113,6 +116,8 @@ def test_linear_entry(iseg):
     for bad in (dict(M=-1), dict(N=-1), dict(K=-1), dict(x_ld=15), dict(w_ld=15), dict(c_ld=15), dict(c_ld=24), dict(y_ld=3), dict(N=1 << 31, y_ld=1 << 31)):
         assert lin(**bad) == iseg.ISEG_ERR_SHAPE, bad
     assert lin(K=131072, x_ld=131072, w_ld=131072, c_ld=131072) == iseg.ISEG_ERR_UNSUPPORTED
+    n = 1 << 28
+    assert lin(N=n, y_ld=n) == iseg.ISEG_ERR_UNSUPPORTED and lin(M=1, N=n, y_ld=n) == iseg.ISEG_ERR_UNSUPPORTED
     assert lin(ws=None) == iseg.ISEG_ERR_WORKSPACE and lin(n=1) == iseg.ISEG_ERR_WORKSPACE
     assert lin(M=0, x=None, codes=None, scale=None, y=None) == iseg.ISEG_OK
 
