@@ -98,43 +98,108 @@ __global__ __launch_bounds__(NW < 4 ? 256 : NW * 64) void k_layernorm_fwd(LnArgs
     }
 }
 
-// rows longer than the registers take, or shorter than a vector: three passes
-// over the row (the second and third come from the caches)
-template <typename T, typename P, int NW>
-__global__ __launch_bounds__(NW * 64) void k_layernorm_fwd_long(LnArgs a)
+// rows longer than the registers take: three passes over the row, the second
+// and third from the caches
+template <typename T, typename P>
+__global__ __launch_bounds__(1024) void k_layernorm_fwd_long(LnArgs a)
 {
-    constexpr int NT = NW * 64;
+    constexpr int N = RowVec<T>::N, NW = 16, U = 2;
     __shared__ float red[4 * NW];
-    const int tid = threadIdx.x;
     const int64_t C = a.C;
     const float inv_c = 1.f / (float)C;
-    const P* gamma = (const P*)a.gamma;
-    const P* beta = (const P*)a.beta;
     for (int64_t m = blockIdx.x; m < a.M; m += gridDim.x) {
         const T* x = (const T*)a.x + m * a.x_ld;
         float s = 0.f, z = 0.f;
-        for (int64_t c = tid; c < C; c += NT) s += (float)x[c];
+        for (int64_t c = threadIdx.x * N; c < C; c += U * 1024 * N) {
+            RowVec<T> v[U];
+            RowSlot<N> sl[U];
+#pragma unroll
+            for (int u = 0; u < U; u++) {
+                sl[u] = row_slot<N>(c + u * 1024 * N, C);
+                v[u] = slot_load<T, N>(x, sl[u]);
+            }
+#pragma unroll
+            for (int u = 0; u < U; u++)
+#pragma unroll
+                for (int i = 0; i < N; i++) s += i >= sl[u].dup ? (float)v[u].v[i] : 0.f;
+        }
         block_sum2_f32<NW>(s, z, red);
         const float mean = s * inv_c;
         float d1 = 0.f, d2 = 0.f;
-        for (int64_t c = tid; c < C; c += NT) {
-            const float d = (float)x[c] - mean;
-            d1 += d;
-            d2 = fmaf(d, d, d2);
+        for (int64_t c = threadIdx.x * N; c < C; c += U * 1024 * N) {
+            RowVec<T> v[U];
+            RowSlot<N> sl[U];
+#pragma unroll
+            for (int u = 0; u < U; u++) {
+                sl[u] = row_slot<N>(c + u * 1024 * N, C);
+                v[u] = slot_load<T, N>(x, sl[u]);
+            }
+#pragma unroll
+            for (int u = 0; u < U; u++)
+#pragma unroll
+                for (int i = 0; i < N; i++) {
+                    const float d = i >= sl[u].dup ? (float)v[u].v[i] - mean : 0.f;
+                    d1 += d;
+                    d2 = fmaf(d, d, d2);
+                }
         }
         block_sum2_f32<NW>(d1, d2, red + 2 * NW);
         const float corr = d1 * inv_c;
         const float var = fmaxf(d2 * inv_c - corr * corr, 0.f);
         const float rstd = 1.f / sqrtf(var + a.eps);
-        if (tid == 0) {
+        if (threadIdx.x == 0) {
             if (a.mean) a.mean[m] = mean + corr;
             if (a.rstd) a.rstd[m] = rstd;
             if (!(fabsf(d2) <= 3.4028234e38f)) set_status(a.status, ISEG_DEV_NONFINITE);
         }
+        // y may be x: the last vector shares elements with another thread's, so
+        // every thread stores its own only
         T* y = (T*)a.y + m * a.y_ld;
-        for (int64_t c = tid; c < C; c += NT) {
-            const float g = gamma ? (float)gamma[c] : 1.f;
-            const float b = beta ? (float)beta[c] : 0.f;
+        for (int64_t c = threadIdx.x * N; c < C; c += 1024 * N) {
+            const RowSlot<N> sl = row_slot<N>(c, C);
+            const RowVec<T> v = row_load(x + sl.at);
+            const ParamVec<P, N> gm = param_load<P, N>((const P*)a.gamma, sl, 1.f), bt = param_load<P, N>((const P*)a.beta, sl, 0.f);
+            RowVec<T> o;
+#pragma unroll
+            for (int i = 0; i < N; i++)
+                o.v[i] = (T)fmaf(((float)v.v[i] - mean - corr) * rstd, (float)gm.v[i], (float)bt.v[i]);
+            if (sl.dup == 0) {
+                row_store(y + sl.at, o);
+            } else {
+#pragma unroll
+                for (int i = 0; i < N; i++)
+                    if (i >= sl.dup) y[sl.at + i] = o.v[i];
+            }
+        }
+    }
+}
+
+// rows shorter than a vector, one per thread
+template <typename T, typename P>
+__global__ __launch_bounds__(256) void k_layernorm_fwd_narrow(LnArgs a)
+{
+    const int C = (int)a.C;
+    const float inv_c = 1.f / (float)C;
+    for (int64_t m = blockIdx.x * (int64_t)256 + threadIdx.x; m < a.M; m += (int64_t)gridDim.x * 256) {
+        const T* x = (const T*)a.x + m * a.x_ld;
+        float s = 0.f, d1 = 0.f, d2 = 0.f;
+        for (int c = 0; c < C; c++) s += (float)x[c];
+        const float mean = s * inv_c;
+        for (int c = 0; c < C; c++) {
+            const float d = (float)x[c] - mean;
+            d1 += d;
+            d2 = fmaf(d, d, d2);
+        }
+        const float corr = d1 * inv_c;
+        const float var = fmaxf(d2 * inv_c - corr * corr, 0.f);
+        const float rstd = 1.f / sqrtf(var + a.eps);
+        if (a.mean) a.mean[m] = mean + corr;
+        if (a.rstd) a.rstd[m] = rstd;
+        if (!(fabsf(d2) <= 3.4028234e38f)) set_status(a.status, ISEG_DEV_NONFINITE);
+        T* y = (T*)a.y + m * a.y_ld;
+        for (int c = 0; c < C; c++) {
+            const float g = a.gamma ? (float)((const P*)a.gamma)[c] : 1.f;
+            const float b = a.beta ? (float)((const P*)a.beta)[c] : 0.f;
             y[c] = (T)fmaf(((float)x[c] - mean - corr) * rstd, g, b);
         }
     }
@@ -163,7 +228,7 @@ int launch_fwd(const LnArgs& a, hipStream_t s)
     const int64_t v = ceil_div64(a.C, N);
     const unsigned grid = (unsigned)(a.M < kRowGridMax ? a.M : kRowGridMax);
     if (a.C < N) {
-        hipLaunchKernelGGL((k_layernorm_fwd_long<T, P, 1>), dim3(grid), dim3(64), 0, s, a);
+        hipLaunchKernelGGL((k_layernorm_fwd_narrow<T, P>), dim3(grid_for(a.M, 256, 4096)), dim3(256), 0, s, a);
         return launch_ok();
     }
     if (v <= 64) return fwd_grid<T, P, 1, 1>(a, 2048, s);
@@ -174,7 +239,11 @@ int launch_fwd(const LnArgs& a, hipStream_t s)
     if (v <= 1024) return fwd_grid<T, P, 4, 4>(a, 2048, s);
     if (v <= 1536) return fwd_grid<T, P, 8, 3>(a, 1024, s);
     if (v <= 2048) return fwd_grid<T, P, 8, 4>(a, 1024, s);
-    hipLaunchKernelGGL((k_layernorm_fwd_long<T, P, 16>), dim3(grid), dim3(1024), 0, s, a);
+    if constexpr (N == 4 || sizeof(P) == 2) {                 // the others' registers spill
+        if (v <= 3072) return fwd_grid<T, P, 16, 3>(a, 512, s);
+        if (v <= 4096) return fwd_grid<T, P, 16, 4>(a, 512, s);
+    }
+    hipLaunchKernelGGL((k_layernorm_fwd_long<T, P>), dim3(grid), dim3(1024), 0, s, a);
     return launch_ok();
 }
 
@@ -280,47 +349,121 @@ __global__ __launch_bounds__(NW * 64) void k_layernorm_bwd(LnArgs a)
 template <typename T, typename P>
 __global__ __launch_bounds__(1024) void k_layernorm_bwd_rows(LnArgs a, float2* __restrict__ sums)
 {
+    constexpr int N = RowVec<T>::N;
     __shared__ float red[32];
-    const int tid = threadIdx.x;
-    const P* gamma = (const P*)a.gamma;
     for (int64_t m = blockIdx.x; m < a.M; m += gridDim.x) {
         const T* x = (const T*)a.x + m * a.x_ld;
         const T* dy = (const T*)a.dy + m * a.y_ld;
         const float mean = a.mean[m], rstd = a.rstd[m];
         float s1 = 0.f, s2 = 0.f;
-        for (int64_t c = tid; c < a.C; c += 1024) {
-            const float d = (float)dy[c];
-            const float g = gamma ? d * (float)gamma[c] : d;
-            s1 += g;
-            s2 = fmaf(g, ((float)x[c] - mean) * rstd, s2);
+        for (int64_t c = threadIdx.x * N; c < a.C; c += 1024 * N) {
+            const RowSlot<N> sl = row_slot<N>(c, a.C);
+            const RowVec<T> xv = row_load(x + sl.at), dv = row_load(dy + sl.at);
+            const ParamVec<P, N> gm = param_load<P, N>((const P*)a.gamma, sl, 1.f);
+#pragma unroll
+            for (int i = 0; i < N; i++) {
+                const float g = i >= sl.dup ? (float)dv.v[i] * (float)gm.v[i] : 0.f;
+                s1 += g;
+                s2 = fmaf(g, ((float)xv.v[i] - mean) * rstd, s2);
+            }
         }
         block_sum2_f32<16>(s1, s2, red);
-        if (tid == 0) sums[m] = make_float2(s1 / (float)a.C, s2 / (float)a.C);
+        if (threadIdx.x == 0) sums[m] = make_float2(s1 / (float)a.C, s2 / (float)a.C);
         __syncthreads();
     }
 }
 
-// ... then dx and the column sums over tiles of 256 columns
+// ... then dx and the column sums: a wave takes 64 vectors of columns, its rows
+// one after the other
 template <typename T, typename P>
-__global__ __launch_bounds__(256) void k_layernorm_bwd_cols(LnArgs a, const float2* __restrict__ sums)
+__global__ __launch_bounds__(64) void k_layernorm_bwd_cols(LnArgs a, const float2* __restrict__ sums)
 {
-    const int64_t c = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (c >= a.C) return;
-    const P* gamma = (const P*)a.gamma;
-    const float gm = gamma ? (float)gamma[c] : 1.f;
-    float dg = 0.f, db = 0.f;
+    constexpr int N = RowVec<T>::N;
+    const RowSlot<N> sl = row_slot<N>(((int64_t)blockIdx.x * 64 + threadIdx.x) * N, a.C);
+    if (sl.dup == N) return;
+    const ParamVec<P, N> gm = param_load<P, N>((const P*)a.gamma, sl, 1.f);
+    float dg[N], db[N];
+#pragma unroll
+    for (int i = 0; i < N; i++) dg[i] = db[i] = 0.f;
+    RowVec<T> xn = row_load((const T*)a.x + blockIdx.y * a.x_ld + sl.at), dn = row_load((const T*)a.dy + blockIdx.y * a.y_ld + sl.at);
     for (int64_t m = blockIdx.y; m < a.M; m += gridDim.y) {
+        const RowVec<T> xv = xn, dv = dn;
+        if (m + gridDim.y < a.M) {
+            xn = row_load((const T*)a.x + (m + gridDim.y) * a.x_ld + sl.at);
+            dn = row_load((const T*)a.dy + (m + gridDim.y) * a.y_ld + sl.at);
+        }
         const float mean = a.mean[m], rstd = a.rstd[m];
         const float2 s = sums[m];
-        const float d = (float)((const T*)a.dy)[m * a.y_ld + c];
-        const float xh = ((float)((const T*)a.x)[m * a.x_ld + c] - mean) * rstd;
-        dg = fmaf(d, xh, dg);
-        db += d;
-        ((T*)a.dx)[m * a.dx_ld + c] = (T)((d * gm - s.x - xh * s.y) * rstd);
+        RowVec<T> o;
+#pragma unroll
+        for (int i = 0; i < N; i++) {
+            const float d = (float)dv.v[i], xh = ((float)xv.v[i] - mean) * rstd;
+            dg[i] = fmaf(d, xh, dg[i]);
+            db[i] += d;
+            o.v[i] = (T)((d * (float)gm.v[i] - s.x - xh * s.y) * rstd);
+        }
+        T* dx = (T*)a.dx + m * a.dx_ld + sl.at;
+        // dx may be dy or x: of a vector that shares elements with another
+        // thread's, each stores its own only
+        if (sl.dup == 0) {
+            row_store(dx, o);
+        } else {
+#pragma unroll
+            for (int i = 0; i < N; i++)
+                if (i >= sl.dup) dx[i] = o.v[i];
+        }
     }
-    float* part = a.part + (int64_t)blockIdx.y * 2 * a.C;
-    part[c] = dg;
-    part[a.C + c] = db;
+    float* part = a.part + (int64_t)blockIdx.y * 2 * a.C + sl.at;
+#pragma unroll
+    for (int i = 0; i < N; i++)
+        if (i >= sl.dup) {
+            part[i] = dg[i];
+            part[a.C + i] = db[i];
+        }
+}
+
+// rows shorter than a vector, one per thread
+template <typename T, typename P>
+__global__ __launch_bounds__(256) void k_layernorm_bwd_narrow(LnArgs a)
+{
+    constexpr int N = RowVec<T>::N;
+    __shared__ float red[2][8];
+    const int C = (int)a.C;
+    const float inv_c = 1.f / (float)C;
+    float gm[N], dg[N], db[N];
+#pragma unroll
+    for (int i = 0; i < N; i++) {
+        gm[i] = a.gamma && i < C ? (float)((const P*)a.gamma)[i] : 1.f;
+        dg[i] = db[i] = 0.f;
+    }
+    for (int64_t m = blockIdx.x * (int64_t)256 + threadIdx.x; m < a.M; m += (int64_t)gridDim.x * 256) {
+        const float mean = a.mean[m], rstd = a.rstd[m];
+        float g[N], xh[N], s1 = 0.f, s2 = 0.f;
+#pragma unroll
+        for (int i = 0; i < N; i++) {
+            const float d = i < C ? (float)((const T*)a.dy)[m * a.y_ld + i] : 0.f;
+            xh[i] = i < C ? ((float)((const T*)a.x)[m * a.x_ld + i] - mean) * rstd : 0.f;
+            g[i] = d * gm[i];
+            s1 += g[i];
+            s2 = fmaf(g[i], xh[i], s2);
+            dg[i] = fmaf(d, xh[i], dg[i]);
+            db[i] += d;
+        }
+        s1 *= inv_c;
+        s2 *= inv_c;
+#pragma unroll
+        for (int i = 0; i < N; i++)
+            if (i < C) ((T*)a.dx)[m * a.dx_ld + i] = (T)((g[i] - s1 - xh[i] * s2) * rstd);
+    }
+    float* part = a.part + (int64_t)blockIdx.x * 2 * C;
+#pragma unroll
+    for (int i = 0; i < N; i++) {
+        block_sum2_f32<4>(dg[i], db[i], red[i & 1]);
+        if (i < C && threadIdx.x == 0) {
+            part[i] = dg[i];
+            part[C + i] = db[i];
+        }
+    }
 }
 
 // dgamma (blockIdx.y = 0) or dbeta (1): the np partial rows added in one
@@ -352,12 +495,13 @@ __global__ __launch_bounds__(1024) void k_layernorm_param_sum(const float* __res
     out[c] = (P)s;
 }
 
-// rows that the backward holds in registers: at most 1536 vectors
+// rows that the backward holds in registers: 3072 vectors of float32 (at 16
+// waves), 2048 of a shorter type, whose vectors take twice the registers
 int64_t ln_vectors(const iseg_layernorm_geom* g) { return ceil_div64(g->C, g->x_dtype == ISEG_F32 ? 4 : 8); }
 
 bool ln_bwd_in_regs(const iseg_layernorm_geom* g)
 {
-    return g->C >= (g->x_dtype == ISEG_F32 ? 4 : 8) && ln_vectors(g) <= 1536;
+    return g->x_dtype == ISEG_F32 ? g->C >= 4 && ln_vectors(g) <= 3072 : g->C >= 8 && ln_vectors(g) <= 2048;
 }
 
 // Blocks that walk the rows, each of which leaves 2 C floats of partial sums:
@@ -369,7 +513,8 @@ bool ln_bwd_in_regs(const iseg_layernorm_geom* g)
 int ln_bwd_blocks(const iseg_layernorm_geom* g)
 {
     const int64_t v = ln_vectors(g);
-    if (ln_bwd_in_regs(g) && g->M <= 8) return g->M > 0;      // one block and no second kernel
+    // few and short: one block (25 GB/s), and no second kernel (5 us)
+    if (ln_bwd_in_regs(g) && g->M <= 8 && g->M * v <= 4096) return g->M > 0;
     const int64_t cap = !ln_bwd_in_regs(g) ? 64 : v <= 64 ? 1536 : v <= 128 ? 1024 : v <= 256 ? 512 : 256;
     return (int)(g->M < cap ? g->M : cap);
 }
@@ -390,11 +535,14 @@ int launch_bwd(const LnArgs& a, const iseg_layernorm_geom* g, hipStream_t s)
     const int64_t v = ceil_div64(a.C, N);
     if (nb > 0) {
         int rc;
-        if (!ln_bwd_in_regs(g)) {
+        if (a.C < N) {
+            hipLaunchKernelGGL((k_layernorm_bwd_narrow<T, P>), dim3(nb), dim3(256), 0, s, a);
+            rc = launch_ok();
+        } else if (!ln_bwd_in_regs(g)) {
             float2* sums = (float2*)((char*)a.part + align256((size_t)nb * 2 * a.C * 4));
             const unsigned gr = (unsigned)(a.M < kRowGridMax ? a.M : kRowGridMax);
             hipLaunchKernelGGL((k_layernorm_bwd_rows<T, P>), dim3(gr), dim3(1024), 0, s, a, sums);
-            hipLaunchKernelGGL((k_layernorm_bwd_cols<T, P>), dim3((unsigned)ceil_div64(a.C, 256), nb), dim3(256), 0,
+            hipLaunchKernelGGL((k_layernorm_bwd_cols<T, P>), dim3((unsigned)ceil_div64(a.C, 64 * N), nb), dim3(64), 0,
                                s, a, (const float2*)sums);
             rc = launch_ok();
         } else if (v <= 64) {
@@ -407,8 +555,14 @@ int launch_bwd(const LnArgs& a, const iseg_layernorm_geom* g, hipStream_t s)
             rc = bwd_grid<T, P, 8, 1>(a, nb, s);
         } else if (v <= 1024) {
             rc = bwd_grid<T, P, 8, 2>(a, nb, s);
-        } else {
+        } else if (v <= 1536) {
             rc = bwd_grid<T, P, 8, 3>(a, nb, s);
+        } else if (v <= 2048) {
+            rc = bwd_grid<T, P, 8, 4>(a, nb, s);
+        } else if constexpr (N == 4) {
+            rc = bwd_grid<T, P, 16, 3>(a, nb, s);
+        } else {
+            rc = ISEG_ERR_UNSUPPORTED;                        // ln_bwd_in_regs has none
         }
         if (rc != ISEG_OK) return rc;
     }

@@ -79,21 +79,39 @@ __global__ __launch_bounds__(NW < 4 ? 256 : NW * 64) void k_quantize_rows(RqRowA
                 const uint32_t b = bits_of(MUL ? x * mv[j].v[i] : x);
                 big = b > big ? b : big;
             }
+        const uint32_t mine = big;
         big = row_max_u32<NW>(big, red[flip]);
         uint64_t tb;
         if constexpr (MUL) {
-            // the exact products of the elements that reach the float maximum
+            // The exact products of the elements that reach the float maximum, in
+            // the few threads that have one: big + l, l = |x mul| - big exact by
+            // one fma.  Where that may be subnormal, or big is infinite, they are
+            // read again and formed in double.
             uint64_t e = 0;
+            if (mine == big) {
+                const float fb = __builtin_bit_cast(float, big);
+                float l = -__builtin_inff();
+                uint32_t any = 0;
 #pragma unroll
-            for (int j = 0; j < VPT; j++)
+                for (int j = 0; j < VPT; j++)
 #pragma unroll
-                for (int i = 0; i < N; i++) {
-                    const float x = (float)xv[j].v[i];
-                    if (bits_of(x * mv[j].v[i]) == big) {
-                        const uint64_t b = bits_of((double)x * (double)mv[j].v[i]);
-                        e = b > e ? b : e;
+                    for (int i = 0; i < N; i++) {
+                        const float x = (float)xv[j].v[i];
+                        any |= bits_of(x);
+                        if (bits_of(x * mv[j].v[i]) == big) l = fmaxf(l, fmaf(fabsf(x), fabsf(mv[j].v[i]), -fb));
                     }
+                if (fb >= 8.6736174e-19f && fb <= 3.4028234e38f) {
+                    e = bits_of((double)fb + (double)l);
+                } else if (any | big) {
+                    const T* x = (const T*)a.x + m * a.x_ld;
+                    for (int j = 0; j < VPT; j++)
+                        for (int64_t c = ((int64_t)j * NT + tid) * N; c < ((int64_t)j * NT + tid + 1) * N && c < a.C; c++) {
+                            const float f = (float)x[c];
+                            const uint64_t b = bits_of((double)f * (double)a.mul[c]);
+                            if (bits_of(f * a.mul[c]) == big && b > e) e = b;
+                        }
                 }
+            }
             if (NW == 1) {
                 tb = wave_max_u64(e);
             } else {
@@ -124,31 +142,84 @@ __global__ __launch_bounds__(NW < 4 ? 256 : NW * 64) void k_quantize_rows(RqRowA
     }
 }
 
-// rows longer than the registers take, or shorter than a vector: read twice
-// (the second time from the caches), every product in double
-template <typename T>
-__global__ __launch_bounds__(256) void k_quantize_rows_long(RqRowArgs a)
+// rows longer than the registers take: read twice, the second time from the
+// caches
+template <typename T, bool MUL>
+__global__ __launch_bounds__(1024) void k_quantize_rows_long(RqRowArgs a)
 {
-    const int tid = threadIdx.x, lim = (1 << (a.bits - 1)) - 1;
+    constexpr int N = RowVec<T>::N, U = 2;
+    const int lim = (1 << (a.bits - 1)) - 1;
     for (int64_t m = blockIdx.x; m < a.M; m += gridDim.x) {
         const T* x = (const T*)a.x + m * a.x_ld;
-        int8_t* o = a.codes + m * a.codes_ld;
-        uint64_t big = 0;
-        for (int64_t c = tid; c < a.C; c += 256) {
-            const double v = a.mul ? (double)(float)x[c] * (double)a.mul[c] : (double)(float)x[c];
-            const uint64_t b = bits_of(v);
-            big = b > big ? b : big;
+        uint64_t e = 0;
+        uint32_t big = 0;
+        for (int64_t c = threadIdx.x * N; c < a.C; c += U * 1024 * N) {
+            RowVec<T> v[U];
+            ParamVec<float, N> mv[U];
+#pragma unroll
+            for (int u = 0; u < U; u++) {
+                const RowSlot<N> sl = row_slot<N>(c + u * 1024 * N, a.C);
+                v[u] = slot_load<T, N>(x, sl);                // zeros without a vector
+                if (MUL) mv[u] = param_load<float, N>(a.mul, sl, 0.f);
+            }
+#pragma unroll
+            for (int u = 0; u < U; u++)
+#pragma unroll
+                for (int i = 0; i < N; i++) {
+                    const float f = (float)v[u].v[i];
+                    const uint32_t b = bits_of(MUL ? f * mv[u].v[i] : f);
+                    if (MUL) {
+                        // the exact product, of what reaches the largest so far
+                        if (b >= big) {
+                            const uint64_t t = bits_of((double)f * (double)mv[u].v[i]);
+                            e = t > e ? t : e;
+                        }
+                    }
+                    big = b > big ? b : big;
+                }
         }
-        big = block_max_u64(big);
-        const float s = scale_of(big, a.bits, a.mode);
+        if (!MUL) e = bits_of((double)__builtin_bit_cast(float, big));
+        const float s = scale_of(block_max_u64(e), a.bits, a.mode);
         const Coder k(s);
-        if (tid == 0) {
+        if (threadIdx.x == 0) {
             a.scale[m] = s;
             if (!k.ok) set_status(a.status, ISEG_DEV_NONFINITE);
         }
-        for (int64_t c = tid; c < a.C; c += 256) {
+        int8_t* o = a.codes + m * a.codes_ld;
+        for (int64_t c = threadIdx.x * N; c < a.C; c += 1024 * N) {
+            const RowSlot<N> sl = row_slot<N>(c, a.C);
+            const RowVec<T> v = row_load(x + sl.at);
+            ParamVec<float, N> mv;
+            if (MUL) mv = param_load<float, N>(a.mul, sl, 0.f);
+            float f[N];
+#pragma unroll
+            for (int i = 0; i < N; i++) f[i] = (float)v.v[i];
+            uint32_t w[N / 4];
+            codes_of<N, MUL>(f, mv.v, [&](int) -> const Coder& { return k; }, lim, w);
+            __builtin_memcpy(o + sl.at, w, N);
+        }
+    }
+}
+
+// rows shorter than a vector, one per thread
+template <typename T>
+__global__ __launch_bounds__(256) void k_quantize_rows_narrow(RqRowArgs a)
+{
+    const int C = (int)a.C, lim = (1 << (a.bits - 1)) - 1;
+    for (int64_t m = blockIdx.x * (int64_t)256 + threadIdx.x; m < a.M; m += (int64_t)gridDim.x * 256) {
+        const T* x = (const T*)a.x + m * a.x_ld;
+        uint64_t big = 0;
+        for (int c = 0; c < C; c++) {
+            const uint64_t b = bits_of(a.mul ? (double)(float)x[c] * (double)a.mul[c] : (double)(float)x[c]);
+            big = b > big ? b : big;
+        }
+        const float s = scale_of(big, a.bits, a.mode);
+        const Coder k(s);
+        a.scale[m] = s;
+        if (!k.ok) set_status(a.status, ISEG_DEV_NONFINITE);
+        for (int c = 0; c < C; c++) {
             const double v = a.mul ? (double)(float)x[c] * (double)a.mul[c] : (double)(float)x[c];
-            o[c] = k.ok ? (int8_t)code_wide(v, k, lim) : 0;
+            a.codes[m * a.codes_ld + c] = k.ok ? (int8_t)code_wide(v, k, lim) : 0;
         }
     }
 }
@@ -491,11 +562,20 @@ int launch_rows_mul(const RqRowArgs& a, hipStream_t s)
         if (v <= 256) return rows_grid<T, MUL, 4, 1>(a, s);
         if (v <= 512) return rows_grid<T, MUL, 4, 2>(a, s);
         if (v <= 1024) return rows_grid<T, MUL, 8, 2>(a, s);
+        if constexpr (MUL) {
+            if (v <= 2048) return rows_grid<T, MUL, 16, 2>(a, s);      // with mul in registers too
+        }
         if (v <= 1536) return rows_grid<T, MUL, 8, 3>(a, s);
         if (v <= 2048) return rows_grid<T, MUL, 8, 4>(a, s);
+        if constexpr (N == 4 || !MUL) {                       // the others' registers spill
+            if (v <= 3072) return rows_grid<T, MUL, 16, 3>(a, s);
+            if (v <= 4096) return rows_grid<T, MUL, 16, 4>(a, s);
+        }
+        hipLaunchKernelGGL((k_quantize_rows_long<T, MUL>), dim3((unsigned)(a.M < kRowGridMax ? a.M : kRowGridMax)),
+                           dim3(1024), 0, s, a);
+        return launch_ok();
     }
-    const unsigned grid = (unsigned)(a.M < kRowGridMax ? a.M : kRowGridMax);
-    hipLaunchKernelGGL(k_quantize_rows_long<T>, dim3(grid), dim3(256), 0, s, a);
+    hipLaunchKernelGGL(k_quantize_rows_narrow<T>, dim3(grid_for(a.M, 256, 4096)), dim3(256), 0, s, a);
     return launch_ok();
 }
 

@@ -19,6 +19,8 @@ CASES = [
     # every count of waves and vectors of a row, just above and at its limits
     (70, 8, "bf16", "bf16", 0), (9, 513, "bf16", "fp32", 1), (9, 1025, "bf16", "bf16", 0), (3, 6145, "bf16", "bf16", 0), (3, 6144, "bf16", "bf16", 0),
     (3, 8193, "bf16", "bf16", 0), (2, 12289, "bf16", "fp32", 0), (2, 12288, "bf16", "bf16", 0), (600, 2052, "fp32", "fp32", 0), (3, 6150, "fp32", "bf16", 0), (3, 4099, "fp32", "fp16", 0),
+    (300, 8196, "fp32", "fp32", 0), (3, 12288, "fp32", "bf16", 4), (70, 12291, "fp32", "fp32", 1), (3, 16384, "fp32", "fp16", 0), (66, 14000, "bf16", "bf16", 0),
+    (3, 24577, "bf16", "bf16", 0), (130, 16400, "fp16", "fp32", 3), (3, 32768, "bf16", "fp16", 0), (1000, 3, "fp32", "bf16", 0), (70000, 5, "bf16", "fp32", 1), (8, 4096, "bf16", "bf16", 0),
 ]
 
 
@@ -35,7 +37,7 @@ def _stats(x, eps):
     return mean, 1 / torch.sqrt(var + float(np.float32(eps)))
 
 
-# A thread adds at most 69 terms in sequence, then 6 + 16 more; statistics are
+# A thread adds at most 72 terms in sequence, then 6 + 16 more; statistics are
 # therefore within 100 half-steps of the mean magnitude of their terms.
 K = 100
 

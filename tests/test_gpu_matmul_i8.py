@@ -117,6 +117,8 @@ QUANT = [
     (130, 2052, "bf16", 4, 8, False, True), (9, 8193, "fp16", 0, 8, False, False), (7, 16384, "bf16", 0, 8, True, False),
     (6, 2100, "fp32", 0, 8, False, True), (4, 4104, "fp32", 0, 8, False, False), (5, 6148, "fp32", 2, 8, False, True), (4, 12300, "bf16", 0, 8, False, True),
     (1000, 72, "fp32", 0, 8, True, True), (4100, 33, "bf16", 0, 8, False, True), (3, 20000, "fp32", 0, 2, False, False), (2, 40003, "bf16", 0, 8, False, True),
+    (300, 9001, "bf16", 1, 8, False, True), (70, 12000, "fp32", 0, 8, False, False), (3, 16383, "fp32", 0, 8, False, True), (3, 16389, "fp32", 0, 8, False, True),
+    (3, 24581, "bf16", 0, 8, False, False), (3, 32768, "fp16", 0, 8, True, False), (3, 40000, "bf16", 0, 8, False, False), (70000, 3, "fp32", 1, 8, False, True),
 ]
 
 
@@ -249,6 +251,31 @@ def test_quantize_tiny_huge_and_non_finite():
         assert torch.equal(s.cpu(), ws) and torch.equal(q.cpu(), wq)
         q, s, _ = iseg.quantize_cols(x.float().t().contiguous().to(DEV), mul=mul.to(DEV))
         assert torch.equal(s.cpu(), ws) and torch.equal(q.cpu(), wq)
+
+
+@pytest.mark.parametrize("C", [3, 200, 1500, 5000, 9000, 33000])
+def test_quantize_products_out_of_float_range(C):
+    """Rows whose largest product is subnormal, 0 or infinite in float32, zero
+    rows, and infinities that meet a zero."""
+    from paper_2011_14504_amd import iseg
+    st = torch.zeros(1, dtype=torch.int32, device=DEV)
+    x = normal(1, 5, C).float()
+    mul = (normal(2, C).abs() + 0.1).float()
+    x[0] *= 1e-42
+    x[1] = 0
+    x[2] *= 1e-22
+    x[3] = x[3].clamp(-3, 3) * 1e38
+    for scale in (1.0, 1e-24):
+        m = (mul * scale).float()
+        wq, ws = quantized(x.double() * m.double(), 8, False)
+        q, s = iseg.quantize_rows(x.to(DEV), mul=m.to(DEV), status=st)
+        assert torch.equal(s.cpu(), ws) and torch.equal(q.cpu(), wq)
+    assert iseg.iseg_status_read(st) == 0
+    m = mul.clone()
+    m[C // 2] = float("inf")
+    q, s = iseg.quantize_rows(x.to(DEV), mul=m.to(DEV), status=st)
+    assert iseg.iseg_status_read(st) == iseg.ISEG_DEV_NONFINITE
+    assert bool(torch.isnan(s).all()) and not bool(q.any())
 
 
 def test_linear_backward_empty():
