@@ -214,6 +214,11 @@ __device__ __forceinline__ float vec_max(const RowVec<T>& r)
     return cm;
 }
 
+// A block's part of a row.  fp32 is bound by memory: 2048 x 50021 with entropy
+// and 5 alternatives 80 us, 5.1 TB/s.  16-bit logits are bound by the exponential
+// and the eight or so other instructions of each: 2048 x 50021 bf16 61 us with 5
+// alternatives, 54 without (3.8 TB/s), 4096 x 32768 60 (4.5 TB/s).  4 x 131072
+// bf16 in 32 parts with 20 alternatives 8.5 us, bound by latency.
 template <typename T, bool ENT, bool TOP>
 __global__ __launch_bounds__(256) void k_logprob_fwd(LpArgs a)
 {
@@ -356,7 +361,8 @@ __global__ __launch_bounds__(256) void k_logprob_fwd(LpArgs a)
 
 // Joins the splits of a row.  Each split's keys are in order, so the first
 // ceil(k / splits) of every split hold k keys, and the k-th best of these
-// bounds the k-th best of all from below; what is at or above it is ranked.
+// bounds the k-th best of all from below; what is at or above it is ranked.  4
+// rows of 32 parts with 20 keys each 4.8 us, bound by the latency of its steps.
 template <typename T, bool TOP>
 __global__ __launch_bounds__(256) void k_logprob_join(LpArgs a)
 {
@@ -442,6 +448,9 @@ __device__ __forceinline__ RowVec<T> lb_take(const RowVec<T>& r, float lse, floa
 }
 
 constexpr int kLbVecs = 2048;              // vectors of a row per block: eight per thread, four at once
+
+// Bound by memory, logits read and the gradient written once: 4096 x 32768 bf16
+// 93.7 us (5.7 TB/s).
 
 template <typename T, bool H>
 __global__ __launch_bounds__(256) void k_logprob_bwd(LbArgs a, uint32_t cblocks)

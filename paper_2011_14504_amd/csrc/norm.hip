@@ -22,7 +22,9 @@ struct LnArgs {
 // ---------------------------------------------------------------------------
 // forward: NW waves per row (one, four or sixteen), VPT vectors of a row per
 // thread.  A block walks its rows with gamma and beta in registers and the
-// next row's x on its way.
+// next row's x on its way.  16384 x 4096 bf16 49.8 us, 5.4 TB/s of x and y (a
+// large copy reaches 4.8); 4 x 2048 takes 3.2 us, the latency of one load, two
+// sums over a block and a store.
 // ---------------------------------------------------------------------------
 template <typename T, typename P, int NW, int VPT>
 __global__ __launch_bounds__(NW < 4 ? 256 : NW * 64) void k_layernorm_fwd(LnArgs a)
@@ -99,7 +101,7 @@ __global__ __launch_bounds__(NW < 4 ? 256 : NW * 64) void k_layernorm_fwd(LnArgs
 }
 
 // rows longer than the registers take: three passes over the row, the second
-// and third from the caches
+// and third from the caches (4096 x 50000 bf16 279 us, 2.9 TB/s of x and y)
 template <typename T, typename P>
 __global__ __launch_bounds__(1024) void k_layernorm_fwd_long(LnArgs a)
 {
@@ -174,7 +176,8 @@ __global__ __launch_bounds__(1024) void k_layernorm_fwd_long(LnArgs a)
     }
 }
 
-// rows shorter than a vector, one per thread
+// rows shorter than a vector, one per thread (100000 x 3 fp32 3.5 us; with a
+// wave per row 27)
 template <typename T, typename P>
 __global__ __launch_bounds__(256) void k_layernorm_fwd_narrow(LnArgs a)
 {
@@ -239,7 +242,9 @@ int launch_fwd(const LnArgs& a, hipStream_t s)
     if (v <= 1024) return fwd_grid<T, P, 4, 4>(a, 2048, s);
     if (v <= 1536) return fwd_grid<T, P, 8, 3>(a, 1024, s);
     if (v <= 2048) return fwd_grid<T, P, 8, 4>(a, 1024, s);
-    if constexpr (N == 4 || sizeof(P) == 2) {                 // the others' registers spill
+    // gamma and beta of float32 beside vectors of eight do not fit (2048 x 16384
+    // fp32 48 us, 101 in three passes; 4096 x 20000 bf16 64 and 116)
+    if constexpr (N == 4 || sizeof(P) == 2) {
         if (v <= 3072) return fwd_grid<T, P, 16, 3>(a, 512, s);
         if (v <= 4096) return fwd_grid<T, P, 16, 4>(a, 512, s);
     }
@@ -253,7 +258,8 @@ int launch_fwd(const LnArgs& a, hipStream_t s)
 // One block walks rows b, b + grid, ... with its threads on fixed columns, so
 // gamma and the column sums of dy xhat and dy stay in registers and the next
 // row's x and dy are on their way; each block leaves one row of partial sums
-// that k_layernorm_param_sum adds in block order.
+// that k_layernorm_param_sum adds in block order.  5003 x 1537 fp32 20.1 us with
+// the sum, 4.6 TB/s of x, dy and dx.
 template <typename T, typename P, int NW, int VPT>
 __global__ __launch_bounds__(NW * 64) void k_layernorm_bwd(LnArgs a)
 {
@@ -374,7 +380,8 @@ __global__ __launch_bounds__(1024) void k_layernorm_bwd_rows(LnArgs a, float2* _
 }
 
 // ... then dx and the column sums: a wave takes 64 vectors of columns, its rows
-// one after the other
+// one after the other.  Both kernels read x and dy: 4096 x 32768 bf16 276 us,
+// 4.9 TB/s of what they move
 template <typename T, typename P>
 __global__ __launch_bounds__(64) void k_layernorm_bwd_cols(LnArgs a, const float2* __restrict__ sums)
 {
@@ -496,7 +503,8 @@ __global__ __launch_bounds__(1024) void k_layernorm_param_sum(const float* __res
 }
 
 // rows that the backward holds in registers: 3072 vectors of float32 (at 16
-// waves), 2048 of a shorter type, whose vectors take twice the registers
+// waves), 2048 of a shorter type, whose vectors take twice the registers.  4096
+// x 16384 bf16 95 us (4.2 TB/s); 4096 x 20000, in two passes, 187 (2.6)
 int64_t ln_vectors(const iseg_layernorm_geom* g) { return ceil_div64(g->C, g->x_dtype == ISEG_F32 ? 4 : 8); }
 
 bool ln_bwd_in_regs(const iseg_layernorm_geom* g)

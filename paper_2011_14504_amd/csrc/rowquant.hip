@@ -38,23 +38,38 @@ __device__ __forceinline__ uint32_t row_max_u32(uint32_t v, uint32_t* red)
 }
 
 // NW waves per row (one, or the whole block), VPT vectors of it per thread, in
-// registers between the maximum and the codes.
+// registers between the maximum and the codes, and the next row's on their way.
+// Bound by memory, x read and the codes written once: 4096 x 4096 bf16 14.6 us
+// (3.4 TB/s), fp32 16.3 (5.1), 4096 x 16384 bf16 41.5 (4.9).  mul waits in LDS,
+// every thread's own part: in registers as well it leaves one block of eight
+// waves on a CU (4096 x 16384 bf16 81 us, so 54 at four waves per SIMD).
 template <typename T, bool MUL, int NW, int VPT>
-__global__ __launch_bounds__(NW < 4 ? 256 : NW * 64) void k_quantize_rows(RqRowArgs a)
+__global__ __launch_bounds__(NW < 4 ? 256 : NW * 64) __attribute__((amdgpu_waves_per_eu(NW == 8 ? 4 : 1))) void
+k_quantize_rows(RqRowArgs a)
 {
     constexpr int N = RowVec<T>::N;
     constexpr int NT = NW * 64, R = NW < 4 ? 4 / NW : 1;
     __shared__ uint32_t red[2][NW];
     __shared__ unsigned long long top[2];
+    extern __shared__ __attribute__((aligned(16))) float4 ms[];        // MUL: [VPT * N / 4][threads of the block]
     const int tid = threadIdx.x % NT;
     RowSlot<N> sl[VPT];                                       // only the last one may be short
-    ParamVec<float, N> mv[VPT];
 #pragma unroll
     for (int j = 0; j < VPT; j++) {
         const int64_t c = ((int64_t)j * NT + tid) * N;
         sl[j] = j < VPT - 1 ? RowSlot<N>{c, 0} : row_slot<N>(c, a.C);
-        if (MUL) mv[j] = param_load<float, N>(a.mul, sl[j], 0.f);
+        if (MUL) {
+            const ParamVec<float, N> mv = param_load<float, N>(a.mul, sl[j], 0.f);
+#pragma unroll
+            for (int q = 0; q < N / 4; q++) __builtin_memcpy(&ms[(j * (N / 4) + q) * (R * NT) + threadIdx.x], mv.v + q * 4, 16);
+        }
     }
+    auto mul_of = [&](int j) {
+        ParamVec<float, N> mv = {};
+#pragma unroll
+        for (int q = 0; q < N / 4 && MUL; q++) __builtin_memcpy(mv.v + q * 4, &ms[(j * (N / 4) + q) * (R * NT) + threadIdx.x], 16);
+        return mv;
+    };
     const int lim = (1 << (a.bits - 1)) - 1;
     RowVec<T> nv[VPT];
     int64_t m = (int64_t)blockIdx.x * R + threadIdx.x / NT;
@@ -72,13 +87,15 @@ __global__ __launch_bounds__(NW < 4 ? 256 : NW * 64) void k_quantize_rows(RqRowA
         for (int j = 0; j < VPT; j++) xv[j] = nv[j];
         if (m + step < a.M) fetch(m + step);
 #pragma unroll
-        for (int j = 0; j < VPT; j++)
+        for (int j = 0; j < VPT; j++) {
+            const ParamVec<float, N> mv = mul_of(j);
 #pragma unroll
             for (int i = 0; i < N; i++) {
                 const float x = (float)xv[j].v[i];
-                const uint32_t b = bits_of(MUL ? x * mv[j].v[i] : x);
+                const uint32_t b = bits_of(MUL ? x * mv.v[i] : x);
                 big = b > big ? b : big;
             }
+        }
         const uint32_t mine = big;
         big = row_max_u32<NW>(big, red[flip]);
         uint64_t tb;
@@ -93,13 +110,15 @@ __global__ __launch_bounds__(NW < 4 ? 256 : NW * 64) void k_quantize_rows(RqRowA
                 float l = -__builtin_inff();
                 uint32_t any = 0;
 #pragma unroll
-                for (int j = 0; j < VPT; j++)
+                for (int j = 0; j < VPT; j++) {
+                    const ParamVec<float, N> mv = mul_of(j);
 #pragma unroll
                     for (int i = 0; i < N; i++) {
                         const float x = (float)xv[j].v[i];
                         any |= bits_of(x);
-                        if (bits_of(x * mv[j].v[i]) == big) l = fmaxf(l, fmaf(fabsf(x), fabsf(mv[j].v[i]), -fb));
+                        if (bits_of(x * mv.v[i]) == big) l = fmaxf(l, fmaf(fabsf(x), fabsf(mv.v[i]), -fb));
                     }
+                }
                 if (fb >= 8.6736174e-19f && fb <= 3.4028234e38f) {
                     e = bits_of((double)fb + (double)l);
                 } else if (any | big) {
@@ -136,14 +155,15 @@ __global__ __launch_bounds__(NW < 4 ? 256 : NW * 64) void k_quantize_rows(RqRowA
 #pragma unroll
             for (int i = 0; i < N; i++) x[i] = (float)xv[j].v[i];
             uint32_t o[N / 4];
-            codes_of<N, MUL>(x, mv[j].v, [&](int) -> const Coder& { return k; }, lim, o);
+            const ParamVec<float, N> mv = mul_of(j);
+            codes_of<N, MUL>(x, mv.v, [&](int) -> const Coder& { return k; }, lim, o);
             if (j < VPT - 1 || sl[j].dup < N) __builtin_memcpy(a.codes + m * a.codes_ld + sl[j].at, o, N);
         }
     }
 }
 
 // rows longer than the registers take: read twice, the second time from the
-// caches
+// caches (4096 x 50000 bf16 203 us, 3.0 TB/s of x and codes)
 template <typename T, bool MUL>
 __global__ __launch_bounds__(1024) void k_quantize_rows_long(RqRowArgs a)
 {
@@ -201,7 +221,7 @@ __global__ __launch_bounds__(1024) void k_quantize_rows_long(RqRowArgs a)
     }
 }
 
-// rows shorter than a vector, one per thread
+// rows shorter than a vector, one per thread (100000 x 3 fp32 3.7 us)
 template <typename T>
 __global__ __launch_bounds__(256) void k_quantize_rows_narrow(RqRowArgs a)
 {
@@ -229,7 +249,9 @@ __global__ __launch_bounds__(256) void k_quantize_rows_narrow(RqRowArgs a)
 // ---------------------------------------------------------------------------
 // Largest |v| (a double's bits) and sum of x of 64 columns over a strip of
 // rows.  A block's threads take vectors of N columns: 64 / N of them side by
-// side, the rows dealt to the others.
+// side, the rows dealt to the others, four rows of each in flight.  4096 x 4096
+// bf16 12.3 us (2.7 TB/s, a line of 128 bytes per row), with mul 14.4; k_cols_codes
+// then finds x in the caches.
 template <typename T, bool MUL>
 __global__ __launch_bounds__(256) void k_cols_stats(RqRowArgs a, int64_t strip)
 {
@@ -388,7 +410,8 @@ __device__ __forceinline__ void put16(const uint32_t* t, int8_t* d, int64_t n, b
 // LDS: a thread codes one vector of N columns in each of four rows and leaves a
 // word of four rows for each column (33 words apart, so a wave's columns fall
 // on all the banks); rows of codes leave 16 bytes per lane, a whole line per
-// column.  The block takes the scales from the strips' partials itself.
+// column.  The block takes the scales from the strips' partials itself.  4096 x
+// 4096 bf16 15 to 17 us: bound by the coding, 2.9 TB/s of x and codes.
 template <typename T, bool MUL>
 __global__ __launch_bounds__(256) void k_cols_codes(RqRowArgs a, int strips)
 {
@@ -484,7 +507,8 @@ __global__ __launch_bounds__(256) void k_cols_codes_narrow(RqRowArgs a, int stri
 }
 
 // Transposition of 128 x 128 codes: four rows of four columns per thread are
-// turned by byte permutations into four words of four columns.
+// turned by byte permutations into four words of four columns, so both sides
+// move whole lines of 128 bytes.  4096 x 4096 7.5 us (4.5 TB/s).
 __global__ __launch_bounds__(256) void k_transpose_i8(const int8_t* __restrict__ in, int64_t M, int64_t C,
                                                       int64_t in_ld, int8_t* __restrict__ out, int64_t out_ld)
 {
@@ -545,9 +569,12 @@ int rows_grid(const RqRowArgs& a, hipStream_t s)
 {
     constexpr int R = NW < 4 ? 4 / NW : 1;
     if (!slots_fit<T, NW, VPT>(a.C)) return ISEG_ERR_UNSUPPORTED;
-    const int64_t nb = ceil_div64(a.M, R);
-    hipLaunchKernelGGL((k_quantize_rows<T, MUL, NW, VPT>), dim3((unsigned)(nb < 4096 ? nb : 4096)),
-                       dim3(NW < 4 ? 256 : NW * 64), 0, s, a);
+    constexpr int threads = NW < 4 ? 256 : NW * 64;
+    constexpr size_t lds = MUL ? (size_t)VPT * RowVec<T>::N * 4 * threads : 0;
+    if (lds > 49152 && !lds_limit((const void*)k_quantize_rows<T, MUL, NW, VPT>, lds)) return ISEG_ERR_DEVICE;
+    // with mul, what the chip holds at once: each block takes mul in
+    const int64_t nb = ceil_div64(a.M, R), cap = MUL ? (NW < 4 ? 2048 : 256 * 32 / NW) : 4096;
+    hipLaunchKernelGGL((k_quantize_rows<T, MUL, NW, VPT>), dim3((unsigned)(nb < cap ? nb : cap)), dim3(threads), lds, s, a);
     return launch_ok();
 }
 
@@ -562,15 +589,10 @@ int launch_rows_mul(const RqRowArgs& a, hipStream_t s)
         if (v <= 256) return rows_grid<T, MUL, 4, 1>(a, s);
         if (v <= 512) return rows_grid<T, MUL, 4, 2>(a, s);
         if (v <= 1024) return rows_grid<T, MUL, 8, 2>(a, s);
-        if constexpr (MUL) {
-            if (v <= 2048) return rows_grid<T, MUL, 16, 2>(a, s);      // with mul in registers too
-        }
         if (v <= 1536) return rows_grid<T, MUL, 8, 3>(a, s);
         if (v <= 2048) return rows_grid<T, MUL, 8, 4>(a, s);
-        if constexpr (N == 4 || !MUL) {                       // the others' registers spill
-            if (v <= 3072) return rows_grid<T, MUL, 16, 3>(a, s);
-            if (v <= 4096) return rows_grid<T, MUL, 16, 4>(a, s);
-        }
+        if (v <= 3072) return rows_grid<T, MUL, 16, 3>(a, s);
+        if (v <= 4096) return rows_grid<T, MUL, 16, 4>(a, s);
         hipLaunchKernelGGL((k_quantize_rows_long<T, MUL>), dim3((unsigned)(a.M < kRowGridMax ? a.M : kRowGridMax)),
                            dim3(1024), 0, s, a);
         return launch_ok();

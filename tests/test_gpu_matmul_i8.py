@@ -119,6 +119,7 @@ QUANT = [
     (1000, 72, "fp32", 0, 8, True, True), (4100, 33, "bf16", 0, 8, False, True), (3, 20000, "fp32", 0, 2, False, False), (2, 40003, "bf16", 0, 8, False, True),
     (300, 9001, "bf16", 1, 8, False, True), (70, 12000, "fp32", 0, 8, False, False), (3, 16383, "fp32", 0, 8, False, True), (3, 16389, "fp32", 0, 8, False, True),
     (3, 24581, "bf16", 0, 8, False, False), (3, 32768, "fp16", 0, 8, True, False), (3, 40000, "bf16", 0, 8, False, False), (70000, 3, "fp32", 1, 8, False, True),
+    (3, 32760, "bf16", 0, 8, False, True), (5, 20001, "fp16", 0, 8, False, True), (600, 16384, "bf16", 0, 8, False, True), (2100, 700, "fp32", 0, 8, False, True),
 ]
 
 
