@@ -935,13 +935,13 @@ extern "C" int iseg_linear_i8_bwd(const void* dy, const int8_t* a, const float* 
         const LbwWs o = lbw_ws(g, true);
         int8_t* codes = (int8_t*)(base + o.codes);
         float* scale = (float*)(base + o.scale);
-        rc = iseg_quantize_cols(dy, g->dy_dtype, g->M, g->N, g->dy_ld, a_scale, g->bits, g->scale_mode, codes, p.lda,
-                                scale, dbias, base + o.quant, o.product - o.quant, dev_status, stream);
+        int8_t* at = (int8_t*)(base + o.turned);
+        const TurnJob job = {a, g->M, g->K, g->a_ld, at, p.ldb};
+        rc = quantize_cols_turn(dy, g->dy_dtype, g->M, g->N, g->dy_ld, a_scale, g->bits, g->scale_mode, codes, p.lda,
+                                scale, dbias, base + o.quant, o.product - o.quant, dev_status, want_w ? &job : nullptr,
+                                stream);
         if (rc != ISEG_OK) return rc;
         if (want_w) {
-            int8_t* at = (int8_t*)(base + o.turned);
-            rc = iseg_transpose_i8(a, g->M, g->K, g->a_ld, at, p.ldb, stream);
-            if (rc != ISEG_OK) return rc;
             rc = iseg_matmul_i8(codes, scale, at, nullptr, nullptr, &p, dw, base + o.product, ws_bytes - o.product,
                                 stream);
         }

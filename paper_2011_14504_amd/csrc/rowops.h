@@ -182,3 +182,16 @@ static inline bool is_float_dtype(int32_t t) { return t == ISEG_F32 || t == ISEG
 
 // launches walk their rows in a loop, so the grid may be cut at any count
 constexpr int64_t kRowGridMax = 1 << 20;
+
+// iseg_quantize_cols with, where `job` is given, the transposition of another
+// matrix of codes (iseg_transpose_i8, its arguments checked by the caller) in
+// the same launch.
+struct TurnJob {
+    const int8_t* in;
+    int64_t M, C, in_ld;
+    int8_t* out;
+    int64_t out_ld;
+};
+int quantize_cols_turn(const void* x, int32_t x_dtype, int64_t M, int64_t C, int64_t x_ld, const float* mul,
+                       int32_t bits, int32_t scale_mode, int8_t* codes, int64_t codes_ld, float* scale, float* sums,
+                       void* ws, size_t ws_bytes, int32_t* dev_status, const TurnJob* job, hipStream_t stream);

@@ -252,17 +252,16 @@ __global__ __launch_bounds__(256) void k_quantize_rows_narrow(RqRowArgs a)
 // side, the rows dealt to the others, four rows of each in flight.  4096 x 4096
 // bf16 12.3 us (2.7 TB/s, a line of 128 bytes per row), with mul 14.4; k_cols_codes
 // then finds x in the caches.
+// A thread of the first 64 that holds a column gets its number, maximum and sum.
 template <typename T, bool MUL>
-__global__ __launch_bounds__(256) void k_cols_stats(RqRowArgs a, int64_t strip)
+__device__ __forceinline__ bool cols_part(const RqRowArgs& a, int64_t c0, int64_t m0, int64_t m1, int64_t& col,
+                                          uint64_t& top, float& total)
 {
     constexpr int N = RowVec<T>::N, G = 64 / N, RS = 256 / G;       // vectors across, rows at once
     __shared__ uint64_t rm[4][64];
     __shared__ float rs[4][64];
     const int tid = threadIdx.x, g = tid % G, r0 = tid / G, w = tid >> 6;
-    const int64_t c0 = (int64_t)blockIdx.x * 64;
     const RowSlot<N> sl = row_slot<N>(c0 + g * N, a.C);
-    const int64_t m0 = (int64_t)blockIdx.y * strip;
-    const int64_t m1 = m0 + strip < a.M ? m0 + strip : a.M;
     float sum[N];
     uint64_t big[N];                          // exact magnitudes, formed where |fl(v)| reaches its largest so far
 #pragma unroll
@@ -319,19 +318,31 @@ __global__ __launch_bounds__(256) void k_cols_stats(RqRowArgs a, int64_t strip)
         }
     }
     __syncthreads();
-    if (tid >= 64) return;
+    if (tid >= 64) return false;
     // element tid of the vectors: column at + tid % N of its vector, unless it
     // repeats the vector before
     const RowSlot<N> mine = row_slot<N>(c0 + tid / N * N, a.C);
-    if (tid % N < mine.dup) return;
-    const int64_t c = mine.at + tid % N;
-    uint64_t e = rm[0][tid];
-    float s = rs[0][tid];
+    if (tid % N < mine.dup) return false;
+    col = mine.at + tid % N;
+    top = rm[0][tid];
+    total = rs[0][tid];
 #pragma unroll
     for (int i = 1; i < 4; i++) {
-        e = rm[i][tid] > e ? rm[i][tid] : e;
-        s += rs[i][tid];
+        top = rm[i][tid] > top ? rm[i][tid] : top;
+        total += rs[i][tid];
     }
+    return true;
+}
+
+template <typename T, bool MUL>
+__global__ __launch_bounds__(256) void k_cols_stats(RqRowArgs a, int64_t strip)
+{
+    const int64_t m0 = (int64_t)blockIdx.y * strip;
+    const int64_t m1 = m0 + strip < a.M ? m0 + strip : a.M;
+    int64_t c;
+    uint64_t e;
+    float s;
+    if (!cols_part<T, MUL>(a, (int64_t)blockIdx.x * 64, m0, m1, c, e, s)) return;
     a.pmax[(int64_t)blockIdx.y * a.C + c] = e;
     a.psum[(int64_t)blockIdx.y * a.C + c] = s;
 }
@@ -356,8 +367,8 @@ __global__ __launch_bounds__(64) void k_cols_stats_narrow(RqRowArgs a, int64_t s
     a.psum[(int64_t)blockIdx.y * a.C + c] = sum;
 }
 
-// scale and sum of a column from the strips' partials
-__device__ __forceinline__ float col_scale(const RqRowArgs& a, int64_t c, int strips, float* sum)
+// largest magnitude and sum of a column from the strips' partials
+__device__ __forceinline__ uint64_t col_join(const RqRowArgs& a, int64_t c, int strips, float* sum)
 {
     uint64_t big = 0;
     float s = 0.f;
@@ -377,7 +388,7 @@ __device__ __forceinline__ float col_scale(const RqRowArgs& a, int64_t c, int st
         }
     }
     *sum = s;
-    return scale_of(big, a.bits, a.mode);
+    return big;
 }
 
 // four words of four bytes each, turned: word x of the result holds byte x of
@@ -406,33 +417,102 @@ __device__ __forceinline__ void put16(const uint32_t* t, int8_t* d, int64_t n, b
     }
 }
 
+struct TurnArgs {
+    const int8_t* in;
+    int8_t* out;
+    int64_t M, C, in_ld, out_ld;
+    uint32_t tx, ty;             // blocks over the columns and over the rows
+};
+
+// Transposition of 128 x 128 codes: four rows of four columns per thread are
+// turned by byte permutations into four words of four columns, so both sides
+// move whole lines of 128 bytes.  4096 x 4096 7.5 us (4.5 TB/s).
+// t: [column][rows / 4]; block (bx, by).
+__device__ __forceinline__ void turn_codes(const TurnArgs& a, uint32_t (*t)[33], uint32_t bx, uint32_t by)
+{
+    const int64_t c0 = (int64_t)bx * 128;
+    const bool wide = (a.out_ld & 15) == 0 && ((uintptr_t)a.out & 15) == 0;
+    const int64_t mt = ceil_div64(a.M, 128);
+    for (int64_t b = by; b < mt; b += a.ty) {
+        const int64_t m0 = b * 128;
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+            const int e = threadIdx.x + i * 256, cq = e & 31, rq = e >> 5;     // columns / 4, rows / 4
+            const int64_t c = c0 + cq * 4;
+            uint32_t r[4];
+#pragma unroll
+            for (int u = 0; u < 4; u++) {
+                const int64_t m = m0 + rq * 4 + u < a.M ? m0 + rq * 4 + u : a.M - 1;
+                const int8_t* p = a.in + m * a.in_ld + c;
+                r[u] = 0;
+                if (c + 4 <= a.C) {
+                    __builtin_memcpy(&r[u], p, 4);
+                } else {
+                    for (int x = 0; x < 4; x++)
+                        if (c + x < a.C) r[u] |= (uint32_t)(uint8_t)p[x] << (8 * x);
+                }
+            }
+            uint32_t o[4];
+            turn4(r, o);
+#pragma unroll
+            for (int x = 0; x < 4; x++) t[cq * 4 + x][rq] = o[x];
+        }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+            const int e = threadIdx.x + i * 256, col = e >> 3, p = e & 7;
+            const int64_t oc = c0 + col, m = m0 + p * 16;
+            if (oc < a.C && m < a.M) put16(&t[col][p * 4], a.out + oc * a.out_ld + m, a.M - m, wide);
+        }
+        __syncthreads();
+    }
+}
+
+__global__ __launch_bounds__(256) void k_transpose_i8(TurnArgs a)
+{
+    __shared__ uint32_t t[128][33];
+    turn_codes(a, t, blockIdx.x, blockIdx.y);
+}
+
 // Codes of 128 rows by 64 columns per step, turned by byte permutations and
 // LDS: a thread codes one vector of N columns in each of four rows and leaves a
 // word of four rows for each column (33 words apart, so a wave's columns fall
 // on all the banks); rows of codes leave 16 bytes per lane, a whole line per
-// column.  The block takes the scales from the strips' partials itself.  4096 x
-// 4096 bf16 15 to 17 us: bound by the coding, 2.9 TB/s of x and codes.
+// column.  The block takes the scales from the strips' partials itself, or
+// (strips = 0: at most 128 rows) from the columns, which spares a launch: 64 x
+// 1024 bf16 8.1 us, 10.4 with k_cols_stats.  4096 x 4096 bf16 15 to 17 us: bound
+// by the coding, 2.9 TB/s of x and codes.  Blocks behind the cx * cy that code
+// transpose the product's other operand (turn.ty = 0: none); of the linear
+// layer's backward, 295 x 1024 x 2560 30.6 us, with a launch of its own 36.
 template <typename T, bool MUL>
-__global__ __launch_bounds__(256) void k_cols_codes(RqRowArgs a, int strips)
+__global__ __launch_bounds__(256) void k_cols_codes(RqRowArgs a, int strips, uint32_t cx, uint32_t cy, TurnArgs turn)
 {
     constexpr int N = RowVec<T>::N, G = 64 / N, RS = 256 / G;       // vectors across, row quads at once
-    __shared__ uint32_t t[64][33];
+    __shared__ uint32_t t[128][33];
     __shared__ float sc[64];
     const int tid = threadIdx.x, g = tid % G, rq0 = tid / G;
-    const int64_t c0 = (int64_t)blockIdx.x * 64;
+    if (blockIdx.x >= cx * cy) {
+        const uint32_t b = blockIdx.x - cx * cy;
+        turn_codes(turn, t, b % turn.tx, b / turn.tx);
+        return;
+    }
+    const uint32_t bx = blockIdx.x % cx, by = blockIdx.x / cx;
+    const int64_t c0 = (int64_t)bx * 64;
     const int lim = (1 << (a.bits - 1)) - 1;
-    if (tid < 64) {
-        const int64_t c = c0 + tid;
-        float s = 1.f, sum = 0.f;
-        if (c < a.C) {
-            s = col_scale(a, c, strips, &sum);
-            if (blockIdx.y == 0) {
-                a.scale[c] = s;
-                if (a.sums) a.sums[c] = sum;
-                if (!(s == s)) set_status(a.status, ISEG_DEV_NONFINITE);
-            }
+    int64_t c = c0 + tid;
+    uint64_t top = 0;
+    float sum = 0.f;
+    bool mine = tid < 64 && c < a.C;
+    if (strips == 0) mine = cols_part<T, MUL>(a, c0, 0, a.M, c, top, sum);
+    else if (mine) top = col_join(a, c, strips, &sum);
+    if (mine) {
+        const float s = scale_of(top, a.bits, a.mode);
+        sc[c - c0] = s;
+        if (by == 0) {
+            a.scale[c] = s;
+            if (a.sums) a.sums[c] = sum;
+            if (!(s == s)) set_status(a.status, ISEG_DEV_NONFINITE);
         }
-        sc[tid] = s;
     }
     __syncthreads();
     const RowSlot<N> sl = row_slot<N>(c0 + g * N, a.C);
@@ -441,7 +521,7 @@ __global__ __launch_bounds__(256) void k_cols_codes(RqRowArgs a, int strips)
     for (int i = 0; i < N; i++) k[i] = Coder(i >= sl.dup ? sc[sl.at - c0 + i] : 1.f);      // a repeated column's codes are dropped
     const bool wide = (a.codes_ld & 15) == 0 && ((uintptr_t)a.codes & 15) == 0;
     const int64_t mt = ceil_div64(a.M, 128);
-    for (int64_t b = blockIdx.y; b < mt; b += gridDim.y) {
+    for (int64_t b = by; b < mt; b += cy) {
         const int64_t m0 = b * 128;
 #pragma unroll
         for (int rq = rq0; rq < 32; rq += RS) {
@@ -492,7 +572,7 @@ __global__ __launch_bounds__(256) void k_cols_codes_narrow(RqRowArgs a, int stri
     const int64_t c = blockIdx.x;
     const int lim = (1 << (a.bits - 1)) - 1;
     float sum;
-    const float s = col_scale(a, c, strips, &sum);
+    const float s = scale_of(col_join(a, c, strips, &sum), a.bits, a.mode);
     const Coder k(s);
     if (blockIdx.y == 0 && threadIdx.x == 0) {
         a.scale[c] = s;
@@ -503,51 +583,6 @@ __global__ __launch_bounds__(256) void k_cols_codes_narrow(RqRowArgs a, int stri
         const float x = (float)((const T*)a.x)[m * a.x_ld + c];
         const double v = a.mul ? (double)x * (double)a.mul[m] : (double)x;
         a.codes[c * a.codes_ld + m] = k.ok ? (int8_t)code_wide(v, k, lim) : 0;
-    }
-}
-
-// Transposition of 128 x 128 codes: four rows of four columns per thread are
-// turned by byte permutations into four words of four columns, so both sides
-// move whole lines of 128 bytes.  4096 x 4096 7.5 us (4.5 TB/s).
-__global__ __launch_bounds__(256) void k_transpose_i8(const int8_t* __restrict__ in, int64_t M, int64_t C,
-                                                      int64_t in_ld, int8_t* __restrict__ out, int64_t out_ld)
-{
-    __shared__ uint32_t t[128][33];           // [column][rows / 4]
-    const int64_t c0 = (int64_t)blockIdx.x * 128;
-    const bool wide = (out_ld & 15) == 0 && ((uintptr_t)out & 15) == 0;
-    const int64_t mt = ceil_div64(M, 128);
-    for (int64_t b = blockIdx.y; b < mt; b += gridDim.y) {
-        const int64_t m0 = b * 128;
-#pragma unroll
-        for (int i = 0; i < 4; i++) {
-            const int e = threadIdx.x + i * 256, cq = e & 31, rq = e >> 5;     // columns / 4, rows / 4
-            const int64_t c = c0 + cq * 4;
-            uint32_t r[4];
-#pragma unroll
-            for (int u = 0; u < 4; u++) {
-                const int64_t m = m0 + rq * 4 + u < M ? m0 + rq * 4 + u : M - 1;
-                const int8_t* p = in + m * in_ld + c;
-                r[u] = 0;
-                if (c + 4 <= C) {
-                    __builtin_memcpy(&r[u], p, 4);
-                } else {
-                    for (int x = 0; x < 4; x++)
-                        if (c + x < C) r[u] |= (uint32_t)(uint8_t)p[x] << (8 * x);
-                }
-            }
-            uint32_t o[4];
-            turn4(r, o);
-#pragma unroll
-            for (int x = 0; x < 4; x++) t[cq * 4 + x][rq] = o[x];
-        }
-        __syncthreads();
-#pragma unroll
-        for (int i = 0; i < 4; i++) {
-            const int e = threadIdx.x + i * 256, col = e >> 3, p = e & 7;
-            const int64_t oc = c0 + col, m = m0 + p * 16;
-            if (oc < C && m < M) put16(&t[col][p * 4], out + oc * out_ld + m, M - m, wide);
-        }
-        __syncthreads();
     }
 }
 
@@ -607,8 +642,15 @@ int launch_rows(const RqRowArgs& a, hipStream_t s)
     return a.mul ? launch_rows_mul<T, true>(a, s) : launch_rows_mul<T, false>(a, s);
 }
 
+int launch_turn(const TurnArgs& turn, hipStream_t s)
+{
+    if (turn.ty == 0) return ISEG_OK;
+    hipLaunchKernelGGL(k_transpose_i8, dim3(turn.tx, turn.ty), dim3(256), 0, s, turn);
+    return launch_ok();
+}
+
 template <typename T, bool MUL>
-int launch_cols_mul(const RqRowArgs& a, hipStream_t s)
+int launch_cols_mul(const RqRowArgs& a, const TurnArgs& turn, hipStream_t s)
 {
     const unsigned ct = (unsigned)ceil_div64(a.C, 64);
     const int64_t strips = cols_strips(a.M, a.C);
@@ -617,20 +659,32 @@ int launch_cols_mul(const RqRowArgs& a, hipStream_t s)
         hipLaunchKernelGGL(k_cols_stats_narrow<T>, dim3(1, (unsigned)strips), dim3(64), 0, s, a, strip);
         hipLaunchKernelGGL(k_cols_codes_narrow<T>, dim3((unsigned)a.C, grid_for(a.M, 256, 256)), dim3(256), 0, s, a,
                            (int)strips);
-        return launch_ok();
+        return launch_turn(turn, s);
     }
-    hipLaunchKernelGGL((k_cols_stats<T, MUL>), dim3(ct, (unsigned)strips), dim3(256), 0, s, a, strip);
+    // one strip of a few rows: read again by the block that codes it
+    const bool one = strips == 1 && a.M <= 128;
+    if (!one) hipLaunchKernelGGL((k_cols_stats<T, MUL>), dim3(ct, (unsigned)strips), dim3(256), 0, s, a, strip);
     // blocks for the chip, each with the scales' work once
     const int64_t mt = ceil_div64(a.M, 128), most = ceil_div64(1024, ct);
     const int64_t gy = mt < most ? mt : most;
-    hipLaunchKernelGGL((k_cols_codes<T, MUL>), dim3(ct, (unsigned)(gy > 1 ? gy : 1)), dim3(256), 0, s, a, (int)strips);
-    return launch_ok();
+    const unsigned cy = (unsigned)(gy > 1 ? gy : 1);
+    const int64_t blocks = (int64_t)ct * cy, extra = (int64_t)turn.tx * turn.ty;
+    const bool both = blocks + extra < (int64_t)1 << 24;                // a launch's threads
+    hipLaunchKernelGGL((k_cols_codes<T, MUL>), dim3((unsigned)(both ? blocks + extra : blocks)), dim3(256), 0, s, a,
+                       one ? 0 : (int)strips, ct, cy, turn);
+    return both ? launch_ok() : launch_turn(turn, s);
 }
 
 template <typename T>
-int launch_cols(const RqRowArgs& a, hipStream_t s)
+int launch_cols(const RqRowArgs& a, const TurnArgs& turn, hipStream_t s)
 {
-    return a.mul ? launch_cols_mul<T, true>(a, s) : launch_cols_mul<T, false>(a, s);
+    return a.mul ? launch_cols_mul<T, true>(a, turn, s) : launch_cols_mul<T, false>(a, turn, s);
+}
+
+TurnArgs turn_args(const TurnJob& j)
+{
+    const int64_t mt = ceil_div64(j.M, 128);
+    return {j.in, j.out, j.M, j.C, j.in_ld, j.out_ld, (uint32_t)ceil_div64(j.C, 128), (uint32_t)(mt < 1024 ? mt : 1024)};
 }
 
 int rq_check(int32_t x_dtype, int32_t bits, int32_t mode)
@@ -664,16 +718,17 @@ extern "C" size_t iseg_quantize_cols_ws(int64_t M, int64_t C)
     return ws_used((size_t)cols_strips(M, C) * (size_t)C * 12);
 }
 
-extern "C" int iseg_quantize_cols(const void* x, int32_t x_dtype, int64_t M, int64_t C, int64_t x_ld,
-                                  const float* mul, int32_t bits, int32_t scale_mode, int8_t* codes,
-                                  int64_t codes_ld, float* scale, float* sums, void* ws, size_t ws_bytes,
-                                  int32_t* dev_status, hipStream_t stream)
+int quantize_cols_turn(const void* x, int32_t x_dtype, int64_t M, int64_t C, int64_t x_ld, const float* mul,
+                       int32_t bits, int32_t scale_mode, int8_t* codes, int64_t codes_ld, float* scale, float* sums,
+                       void* ws, size_t ws_bytes, int32_t* dev_status, const TurnJob* job, hipStream_t stream)
 {
     const int rc = rq_check(x_dtype, bits, scale_mode);
     if (rc != ISEG_OK) return rc;
     if (M < 0 || C < 0 || C >= kMaxCols || x_ld < C || codes_ld < M) return ISEG_ERR_SHAPE;
-    if (C > kMaxTurned) return ISEG_ERR_UNSUPPORTED;
-    if (C == 0) return ISEG_OK;
+    if (C > kMaxTurned || (job && job->C > kMaxTurned)) return ISEG_ERR_UNSUPPORTED;
+    TurnArgs turn = {};
+    if (job && job->M > 0 && job->C > 0) turn = turn_args(*job);
+    if (C == 0) return launch_turn(turn, stream);
     if (!scale || (M > 0 && (!x || !codes))) return ISEG_ERR_ARG;
     if (!ws || ws_bytes < iseg_quantize_cols_ws(M, C)) return ISEG_ERR_WORKSPACE;
     RqRowArgs a = {};
@@ -681,8 +736,18 @@ extern "C" int iseg_quantize_cols(const void* x, int32_t x_dtype, int64_t M, int
     a.pmax = (uint64_t*)ws;
     a.psum = (float*)(a.pmax + cols_strips(M, C) * C);
     a.M = M; a.C = C; a.x_ld = x_ld; a.codes_ld = codes_ld; a.bits = bits; a.mode = scale_mode; a.status = dev_status;
-    return x_dtype == ISEG_F32 ? launch_cols<float>(a, stream)
-                               : x_dtype == ISEG_F16 ? launch_cols<f16_t>(a, stream) : launch_cols<bf16_t>(a, stream);
+    return x_dtype == ISEG_F32   ? launch_cols<float>(a, turn, stream)
+           : x_dtype == ISEG_F16 ? launch_cols<f16_t>(a, turn, stream)
+                                 : launch_cols<bf16_t>(a, turn, stream);
+}
+
+extern "C" int iseg_quantize_cols(const void* x, int32_t x_dtype, int64_t M, int64_t C, int64_t x_ld,
+                                  const float* mul, int32_t bits, int32_t scale_mode, int8_t* codes,
+                                  int64_t codes_ld, float* scale, float* sums, void* ws, size_t ws_bytes,
+                                  int32_t* dev_status, hipStream_t stream)
+{
+    return quantize_cols_turn(x, x_dtype, M, C, x_ld, mul, bits, scale_mode, codes, codes_ld, scale, sums, ws, ws_bytes,
+                              dev_status, nullptr, stream);
 }
 
 extern "C" int iseg_transpose_i8(const int8_t* in, int64_t M, int64_t C, int64_t in_ld, int8_t* out, int64_t out_ld,
@@ -692,8 +757,5 @@ extern "C" int iseg_transpose_i8(const int8_t* in, int64_t M, int64_t C, int64_t
     if (C > kMaxTurned) return ISEG_ERR_UNSUPPORTED;
     if (M == 0 || C == 0) return ISEG_OK;
     if (!in || !out) return ISEG_ERR_ARG;
-    const int64_t mt = ceil_div64(M, 128);
-    hipLaunchKernelGGL(k_transpose_i8, dim3((unsigned)ceil_div64(C, 128), (unsigned)(mt < 1024 ? mt : 1024)),
-                       dim3(256), 0, stream, in, M, C, in_ld, out, out_ld);
-    return launch_ok();
+    return launch_turn(turn_args({in, M, C, in_ld, out, out_ld}), stream);
 }
