@@ -1365,6 +1365,17 @@ def _layernorm_geom(M, Cc, x_ld, y_ld, dx_ld, x_dtype, p_dtype, eps):
 
 
 @functools.lru_cache(maxsize=256)
+def _layernorm_bwd_geom(M, Cc, x_ld, y_ld, dx_ld, x_dtype, p_dtype):
+    g = LayernormGeom(M, Cc, x_ld, y_ld, dx_ld, x_dtype, p_dtype, 1.0, 0)
+    return g, lib().iseg_layernorm_bwd_ws(C.byref(g))
+
+
+@functools.lru_cache(maxsize=256)
+def _quantize_cols_ws(M, Cc):
+    return lib().iseg_quantize_cols_ws(M, Cc)
+
+
+@functools.lru_cache(maxsize=256)
 def _matmul_geom(M, N, K, lda, ldb, ldc, out_dtype, unaligned):
     g = MatmulGeom(M, N, K, lda, ldb, ldc, out_dtype, unaligned)
     return g, lib().iseg_matmul_i8_ws(C.byref(g))
@@ -1432,9 +1443,8 @@ def layernorm_bwd(dy, x, gamma, mean, rstd, want_params=True):
     dx = _like(x)
     dgamma = torch.empty(Cc, dtype=pdt, device=x.device) if want_params else None
     dbeta = torch.empty_like(dgamma) if want_params else None
-    g = _layernorm_geom(M, Cc, ld, dld, Cc, xd, pd, 1.0)
-    iseg_layernorm_bwd(dr, xr, gamma, mean, rstd, g, dx, dgamma, dbeta,
-                       _scratch(x, lib().iseg_layernorm_bwd_ws(C.byref(g))))
+    g, wsb = _layernorm_bwd_geom(M, Cc, ld, dld, Cc, xd, pd)
+    iseg_layernorm_bwd(dr, xr, gamma, mean, rstd, g, dx, dgamma, dbeta, _scratch(x, wsb))
     return dx, dgamma, dbeta
 
 
@@ -1482,7 +1492,7 @@ def quantize_cols(x, bits=8, scale_mode=ISEG_SCALE_MAX, mul=None, want_sums=Fals
     scale = torch.empty(Cc, dtype=torch.float32, device=x.device)
     sums = torch.empty(Cc, dtype=torch.float32, device=x.device) if want_sums else None
     iseg_quantize_cols(xr, xd, M, Cc, ld, mul, bits, scale_mode, codes, codes.stride(0), scale, sums,
-                       _scratch(x, lib().iseg_quantize_cols_ws(M, Cc)), status)
+                       _scratch(x, _quantize_cols_ws(M, Cc)), status)
     return codes, scale, sums
 
 
