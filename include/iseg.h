@@ -693,7 +693,8 @@ int iseg_linear_i8_fwd(const void* x, const int8_t* w, const float* w_scale, con
  * it, and w is transposed in the workspace.  dx [M, K] and dw [N, K] of
  * out_dtype, dbias [N] float32: each may be NULL (not wanted; what only it
  * needs may then be NULL too).  Reductions, N for dx and M for dw, of at most
- * 131071 (ISEG_ERR_UNSUPPORTED beyond). */
+ * 131071, and N for dw and dbias and K for what is transposed of at most 2^28
+ * (ISEG_ERR_UNSUPPORTED beyond, before any work). */
 typedef struct iseg_linear_bwd_geom {
     int64_t M, N, K;
     int64_t dy_ld, a_ld, w_ld, wt_ld, dx_ld, dw_ld;

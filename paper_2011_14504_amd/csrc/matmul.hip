@@ -907,6 +907,8 @@ extern "C" int iseg_linear_i8_bwd(const void* dy, const int8_t* a, const float* 
     const bool want_x = dx && g->M > 0 && g->K > 0, want_w = dw && g->N > 0 && g->K > 0, want_b = dbias && g->N > 0;
     const iseg_matmul_geom px = lbw_dx(g), pw = lbw_dw(g);
     if ((want_x && (rc = mm_check(&px)) != ISEG_OK) || (want_w && (rc = mm_check(&pw)) != ISEG_OK)) return rc;
+    if (((want_w || want_b) && g->N > kMaxTurned) || ((want_w || (want_x && !g->wt_ld)) && g->K > kMaxTurned))
+        return ISEG_ERR_UNSUPPORTED;
     if (g->M > 0 && g->N > 0 && (want_x || want_w || want_b) && !dy) return ISEG_ERR_ARG;
     if (want_x && g->N > 0 && !(g->wt_ld ? w_t : w)) return ISEG_ERR_ARG;
     if (want_x && g->wt_ld && !g->unaligned && ((uintptr_t)w_t & 15)) return ISEG_ERR_ARG;

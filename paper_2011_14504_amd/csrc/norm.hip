@@ -245,7 +245,7 @@ int launch_fwd(const LnArgs& a, hipStream_t s)
     // gamma and beta of float32 beside vectors of eight do not fit (2048 x 16384
     // fp32 48 us, 101 in three passes; 4096 x 20000 bf16 64 and 116)
     if constexpr (N == 4 || sizeof(P) == 2) {
-        if (v <= 3072) return fwd_grid<T, P, 16, 3>(a, 512, s);
+        if (v <= 3 * 1024) return fwd_grid<T, P, 16, 3>(a, 512, s);
         if (v <= 4096) return fwd_grid<T, P, 16, 4>(a, 512, s);
     }
     hipLaunchKernelGGL((k_layernorm_fwd_long<T, P>), dim3(grid), dim3(1024), 0, s, a);
@@ -502,14 +502,14 @@ __global__ __launch_bounds__(1024) void k_layernorm_param_sum(const float* __res
     out[c] = (P)s;
 }
 
-// rows that the backward holds in registers: 3072 vectors of float32 (at 16
-// waves), 2048 of a shorter type, whose vectors take twice the registers.  4096
+// rows that the backward holds in registers: three vectors of float32 for each
+// thread of 16 waves, 2048 of a shorter type, whose vectors take twice the registers.  4096
 // x 16384 bf16 95 us (4.2 TB/s); 4096 x 20000, in two passes, 187 (2.6)
 int64_t ln_vectors(const iseg_layernorm_geom* g) { return ceil_div64(g->C, g->x_dtype == ISEG_F32 ? 4 : 8); }
 
 bool ln_bwd_in_regs(const iseg_layernorm_geom* g)
 {
-    return g->x_dtype == ISEG_F32 ? g->C >= 4 && ln_vectors(g) <= 3072 : g->C >= 8 && ln_vectors(g) <= 2048;
+    return g->x_dtype == ISEG_F32 ? g->C >= 4 && ln_vectors(g) <= 3 * 1024 : g->C >= 8 && ln_vectors(g) <= 2048;
 }
 
 // Blocks that walk the rows, each of which leaves 2 C floats of partial sums:
@@ -517,7 +517,7 @@ bool ln_bwd_in_regs(const iseg_layernorm_geom* g)
 // with the sum over the partials: 8192 x 4096 46.5 us with 256 blocks of 8
 // waves, 50.5 with 512; 1024 x 2048 (fp32) 12.5 and 15.7; 16384 x 2048 of 4
 // waves 61.6 / 47.0 / 49.0 with 256 / 512 / 768; 32768 x 512 of one wave 38.7
-// / 35.8 / 42.7 with 1024 / 1536 / 3072.
+// / 35.8 / 42.7 with 1024 / 1536 / twice that.
 int ln_bwd_blocks(const iseg_layernorm_geom* g)
 {
     const int64_t v = ln_vectors(g);

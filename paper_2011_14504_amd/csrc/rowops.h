@@ -183,6 +183,9 @@ static inline bool is_float_dtype(int32_t t) { return t == ISEG_F32 || t == ISEG
 // launches walk their rows in a loop, so the grid may be cut at any count
 constexpr int64_t kRowGridMax = 1 << 20;
 
+// columns of a matrix that is quantized by column or transposed: a launch's threads
+constexpr int64_t kMaxTurned = (int64_t)1 << 28;
+
 // iseg_quantize_cols with, where `job` is given, the transposition of another
 // matrix of codes (iseg_transpose_i8, its arguments checked by the caller) in
 // the same launch.

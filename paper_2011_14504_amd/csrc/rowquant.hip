@@ -586,7 +586,7 @@ __global__ __launch_bounds__(256) void k_cols_codes_narrow(RqRowArgs a, int stri
     }
 }
 
-constexpr int64_t kMaxCols = (int64_t)1 << 31, kMaxTurned = (int64_t)1 << 28;      // a launch's threads
+constexpr int64_t kMaxCols = (int64_t)1 << 31;
 
 // strips of rows whose partials a column's scale is taken from: blocks for the
 // chip, at least 128 rows each
@@ -626,7 +626,7 @@ int launch_rows_mul(const RqRowArgs& a, hipStream_t s)
         if (v <= 1024) return rows_grid<T, MUL, 8, 2>(a, s);
         if (v <= 1536) return rows_grid<T, MUL, 8, 3>(a, s);
         if (v <= 2048) return rows_grid<T, MUL, 8, 4>(a, s);
-        if (v <= 3072) return rows_grid<T, MUL, 16, 3>(a, s);
+        if (v <= 3 * 1024) return rows_grid<T, MUL, 16, 3>(a, s);
         if (v <= 4096) return rows_grid<T, MUL, 16, 4>(a, s);
         hipLaunchKernelGGL((k_quantize_rows_long<T, MUL>), dim3((unsigned)(a.M < kRowGridMax ? a.M : kRowGridMax)),
                            dim3(1024), 0, s, a);

@@ -139,6 +139,10 @@ def test_linear_backward_entry(iseg):
         assert bwd(**bad) == iseg.ISEG_ERR_SHAPE, bad
     assert bwd(N=131072, dy_ld=131072, dw=None, db=None) == iseg.ISEG_ERR_UNSUPPORTED
     assert bwd(M=131072, dx=None) == iseg.ISEG_ERR_UNSUPPORTED
+    n = (1 << 28) + 1                                        # columns beyond one launch, found before any work
+    wide = dict(M=40, N=2, K=n, a_ld=n, w_ld=n, dx_ld=n, dw_ld=n)
+    assert bwd(**wide) == bwd(**wide, dx=None, db=None) == bwd(**wide, dw=None, db=None) == iseg.ISEG_ERR_UNSUPPORTED
+    assert bwd(N=n, dy_ld=n, dx=None, dw=None) == iseg.ISEG_ERR_UNSUPPORTED
     assert bwd(ws=None) == iseg.ISEG_ERR_WORKSPACE and bwd(n=1) == iseg.ISEG_ERR_WORKSPACE
     assert bwd(dx=None, dw=None, db=None, dy=None, a=None, w=None) == iseg.ISEG_OK
     assert bwd(M=0, N=0, dy=None, a=None, w=None) == iseg.ISEG_OK
