@@ -145,6 +145,39 @@ def test_rows_between_and_behind_stay_as_they_were():
     assert bool((y[5:] == 5).all()) and bool((y[:, 100:] == 5).all())
 
 
+@pytest.mark.parametrize("C", [3, 300, 9000, 40000])
+def test_every_row_width_leaves_gaps_and_flags(C):
+    """Rows of one thread, of a wave, of 16 waves and beyond the registers: what
+    lies between and behind them stays, bad rows are flagged and stay alone."""
+    from paper_2011_14504_amd import iseg
+    M, ld, st = 11, C + 13, torch.zeros(1, dtype=torch.int32, device=DEV)
+    x, dy = normal(C, M, C).float(), normal(C + 1, M, C).float()
+    gamma = normal(3, C).float().to(DEV)
+    g = iseg.LayernormGeom(M, C, ld, ld, ld, iseg.ISEG_F32, iseg.ISEG_F32, 1e-5, 0)
+    y, dx = torch.full((2, M + 2, ld), 5.0, device=DEV)
+    mean, rstd = torch.full((2, M + 3), 7.0, device=DEV)
+    dg, db = torch.full((2, C + 5), 9.0, device=DEV)
+    xg, dyg = strided(x, ld, float("nan")), strided(dy, ld, float("nan"))
+    iseg.iseg_layernorm_fwd(xg, gamma, None, g, y, mean, rstd, st)
+    ws = torch.empty(iseg.lib().iseg_layernorm_bwd_ws(iseg.C.byref(g)), dtype=torch.uint8, device=DEV)
+    iseg.iseg_layernorm_bwd(dyg, xg, gamma, mean, rstd, g, dx, dg, db, ws)
+    ref = iseg.layernorm_fwd(x.to(DEV), gamma, None)
+    back = iseg.layernorm_bwd(dy.to(DEV), x.to(DEV), gamma, ref[1], ref[2])
+    for got, want in ((y, ref[0]), (dx, back[0])):
+        assert torch.equal(got[:M, :C], want) and bool((got[M:] == 5).all()) and bool((got[:, C:] == 5).all())
+    for got, want, fill in ((mean, ref[1], 7), (rstd, ref[2], 7), (dg, back[1], 9), (db, back[2], 9)):
+        assert torch.equal(got[:len(want)], want) and bool((got[len(want):] == fill).all())
+    assert iseg.iseg_status_read(st) == 0
+    for bad in (float("nan"), -float("inf")):
+        z = x.clone()
+        z[4, C - 1] = bad
+        got = iseg.layernorm_fwd(z.to(DEV), gamma, None, status=st)[0]
+        assert iseg.iseg_status_read(st) == iseg.ISEG_DEV_NONFINITE
+        iseg.iseg_status_clear(st)
+        keep = [i for i in range(M) if i != 4]
+        assert torch.equal(got[keep], ref[0][keep])
+
+
 def test_empty_and_status():
     from paper_2011_14504_amd import iseg
     st = torch.zeros(1, dtype=torch.int32, device=DEV)

@@ -319,6 +319,31 @@ def test_linear_modes_strides_and_status():
     assert torch.equal(y.cpu(), torch.arange(5.).expand(3, 5)) and bool((s == 1).all())
 
 
+@pytest.mark.parametrize("C", [3, 300, 9000, 40000])
+def test_every_row_width_leaves_gaps_and_flags(C):
+    from paper_2011_14504_amd import iseg
+    M, ld, st = 11, C + 13, torch.zeros(1, dtype=torch.int32, device=DEV)
+    x = normal(C, M, C).float()
+    mul = (normal(2, C).abs() + 0.1).float()
+    xg = strided(x, ld, float("nan"))
+    for m in (None, mul):
+        wq, ws = quantized(x.double() * (1.0 if m is None else m.double()), 8, False)
+        q = torch.full((M + 2, ld), 55, dtype=torch.int8, device=DEV)
+        s = torch.full((M + 3,), 7.0, device=DEV)
+        md = None if m is None else m.to(DEV)
+        iseg.iseg_quantize_rows(xg, iseg.ISEG_F32, M, C, ld, md, 8, iseg.ISEG_SCALE_MAX, q, ld, s, st)
+        assert torch.equal(q[:M, :C].cpu(), wq) and bool((q[M:] == 55).all()) and bool((q[:, C:] == 55).all())
+        assert torch.equal(s[:M].cpu(), ws) and bool((s[M:] == 7).all()) and iseg.iseg_status_read(st) == 0
+        for bad in (float("nan"), -float("inf")):
+            z = x.clone()
+            z[4, C - 1] = bad
+            q, s = iseg.quantize_rows(z.to(DEV), mul=md, status=st)
+            assert iseg.iseg_status_read(st) == iseg.ISEG_DEV_NONFINITE
+            iseg.iseg_status_clear(st)
+            keep = [i for i in range(M) if i != 4]
+            assert torch.equal(q.cpu()[keep], wq[keep]) and bool(torch.isnan(s[4])) and not bool(q[4].any())
+
+
 def test_quantize_empty():
     from paper_2011_14504_amd import iseg
     q, s = iseg.quantize_rows(torch.empty(0, 8, device=DEV))
@@ -351,7 +376,8 @@ def test_transpose(shape):
 # (M, N, K, type)
 LINEAR = [(1, 40, 30, "fp32"), (1, 4096, 4096, "bf16"), (1, 9000, 1024, "fp16"), (2, 100, 4100, "bf16"), (3, 33, 5000, "fp32"), (4, 100, 4096, "bf16"), (16, 64, 1000, "fp16"),
           (16, 8200, 512, "fp32"), (17, 64, 256, "bf16"), (1, 20, 3, "fp32"), (2, 20, 7, "bf16"), (1, 64, 16384, "bf16"), (1, 50, 16390, "fp32"),
-          (1, 100, 8, "bf16"), (1, 8193, 8192, "bf16"), (1, 17, 8191, "fp32"), (1, 9, 2049, "fp16"), (5, 64, 128, "bf16"), (70, 100, 99, "fp16"), (128, 256, 192, "bf16"), (257, 129, 512, "fp32")]
+          (1, 100, 8, "bf16"), (1, 8193, 8192, "bf16"), (1, 17, 8191, "fp32"), (1, 9, 2049, "fp16"), (5, 64, 128, "bf16"), (70, 100, 99, "fp16"), (128, 256, 192, "bf16"), (257, 129, 512, "fp32"),
+          (50, 5, 100, "bf16"), (300, 3, 64, "fp32"), (129, 64, 300, "bf16"), (127, 65, 1000, "fp16"), (1100, 200, 130, "bf16")]
 
 
 @pytest.mark.parametrize("case", LINEAR, ids=str)
