@@ -71,6 +71,21 @@ __device__ __forceinline__ Stat stat_join(Stat a, Stat b)
     return Stat{mn, a.S + b.S, a.T + b.T};
 }
 
+// a wave's 64 parts joined, the same in every lane: one move to the largest
+// maximum, then two sums (8192 x 4096 bf16 28.1 us, 30.2 joined pair by pair)
+__device__ __forceinline__ Stat wave_stat(Stat s)
+{
+    float mn = s.m;
+    mn = fmaxf(mn, dpp_f32<0x111>(mn, mn));
+    mn = fmaxf(mn, dpp_f32<0x112>(mn, mn));
+    mn = fmaxf(mn, dpp_f32<0x114>(mn, mn));
+    mn = fmaxf(mn, dpp_f32<0x118>(mn, mn));
+    mn = fmaxf(mn, dpp_f32<0x142>(mn, mn));
+    mn = fmaxf(mn, dpp_f32<0x143>(mn, mn));
+    stat_move(s, lane63_f32(mn));
+    return Stat{s.m, wave_sum_f32(s.S), wave_sum_f32(s.T)};
+}
+
 __device__ __forceinline__ int64_t token_of(const LpArgs& a, int64_t m)
 {
     return a.tok64 ? ((const int64_t*)a.tok)[m] : (int64_t)((const int32_t*)a.tok)[m];
@@ -219,8 +234,11 @@ __device__ __forceinline__ float vec_max(const RowVec<T>& r)
 // and the eight or so other instructions of each: 2048 x 50021 bf16 61 us with 5
 // alternatives, 54 without (3.8 TB/s), 4096 x 32768 60 (4.5 TB/s).  4 x 131072
 // bf16 in 32 parts with 20 alternatives 8.5 us, bound by latency.
+// Six waves per SIMD where alternatives are ranked hide more of the ranking's
+// latency (1957 x 13910 fp16, 20 of them, 25.8 us; 28 with the four that the
+// registers of four open vectors leave); without them it gains nothing.
 template <typename T, bool ENT, bool TOP>
-__global__ __launch_bounds__(256) void k_logprob_fwd(LpArgs a)
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(TOP ? 6 : 1))) void k_logprob_fwd(LpArgs a)
 {
     constexpr int N = RowVec<T>::N, NT = 256, NW = 4, U = 4;
     __shared__ Stat rstat[NW];
@@ -274,17 +292,11 @@ __global__ __launch_bounds__(256) void k_logprob_fwd(LpArgs a)
             lp_take<T, ENT, 1>(&r, s);
         }
         const bool has = g0 + tid < g1;
-#pragma unroll
-        for (int o = 32; o > 0; o >>= 1) {
-            Stat t = {__shfl_xor(s.m, o, 64), __shfl_xor(s.S, o, 64), __shfl_xor(s.T, o, 64)};
-            s = stat_join(s, t);
-        }
+        s = wave_stat(s);
         if (lane == 0) rstat[w] = s;
         if (tid == 0) thr_s = 0;
         __syncthreads();
-        s = rstat[0];
-#pragma unroll
-        for (int i = 1; i < NW; i++) s = stat_join(s, rstat[i]);
+        s = stat_join(stat_join(rstat[0], rstat[1]), stat_join(rstat[2], rstat[3]));
         if (a.splits == 1) {
             if (tid == 0) row_scalars(a, m, s, given);
         } else if (tid == 0) {
@@ -385,11 +397,7 @@ __global__ __launch_bounds__(256) void k_logprob_join(LpArgs a)
             const float* p = a.pstat + (m * a.splits + i) * 4;
             s = stat_join(s, Stat{p[0], p[1], p[2]});
         }
-#pragma unroll
-        for (int o = 32; o > 0; o >>= 1) {
-            Stat t = {__shfl_xor(s.m, o, 64), __shfl_xor(s.S, o, 64), __shfl_xor(s.T, o, 64)};
-            s = stat_join(s, t);
-        }
+        s = wave_stat(s);
         if (tid == 0) row_scalars(a, m, s, given);
         if (TOP) {
             const int j = (k + a.splits - 1) / a.splits, h = j * a.splits, h4 = (h + 3) & ~3;
