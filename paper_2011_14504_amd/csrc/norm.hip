@@ -20,7 +20,7 @@ struct LnArgs {
 };
 
 // ---------------------------------------------------------------------------
-// forward: NW waves per row (one, four or sixteen), VPT vectors of a row per
+// forward: NW waves per row (one, or the whole block), VPT vectors of a row per
 // thread.  A block walks its rows with gamma and beta in registers and the
 // next row's x on its way.  16384 x 4096 bf16 49.8 us, 5.4 TB/s of x and y (a
 // large copy reaches 4.8); 4 x 2048 takes 3.2 us, the latency of one load, two
