@@ -152,10 +152,6 @@ def prepare(case, seed):
             st["x"] = (randn(M, K) * (0.5 + torch.rand(M, 1, device=DEV, generator=gen))).to(dt)
         if case["way"] == "bwd":
             st["dy"] = (randn(M, N) * 1e-3).to(dt)
-            if own:
-                # the transposed weights that a program keeps until the next update
-                from paper_2011_14504_amd import iseg
-                st["w_t"] = iseg.transpose_i8(st["w"])
     else:
         M, V = case["M"], case["V"]
         x = randn(M, V) * 2.5
@@ -203,7 +199,9 @@ def _run_own(case, st):
     if case["op"] == "linear":
         if case["way"] == "fwd":
             return iseg.linear_i8_fwd(st["x"], st["w"], st["w_scale"], st["bias"])[0]
-        return iseg.linear_i8_bwd(st["dy"], st["a"], st["a_scale"], st["w"], st["w_scale"], w_t=st["w_t"],
+        # a training step changes the weights after each backward, so their
+        # transposition is part of every call
+        return iseg.linear_i8_bwd(st["dy"], st["a"], st["a_scale"], st["w"], st["w_scale"],
                                   want_bias=case["bias"])[:3 if case["bias"] else 2]
     if case["way"] == "fwd":
         out = iseg.logprob_fwd(st["logits"], st["tokens"], top_k=case["k"])
