@@ -13,6 +13,7 @@ import ctypes as C
 import functools
 import math
 import os
+import threading
 
 import torch
 
@@ -702,8 +703,11 @@ def _maybe_arm(kid, key):
 # workspace and helpers (allocation with torch; compute in the entry points)
 # --------------------------------------------------------------------------
 class Workspace:
-    """A growable device scratch buffer shared by consecutive calls on one
-    stream (stream order keeps the uses apart); each stream has its own."""
+    """A growable device scratch buffer shared by one thread's consecutive calls
+    on one stream (stream order keeps the uses apart).  Each stream has its own,
+    and each host thread: a call enqueues several kernels that hand data on
+    through it, and the kernels of two threads' calls on one stream may
+    alternate."""
 
     def __init__(self, device="cuda"):
         self.device = device
@@ -723,20 +727,26 @@ class Workspace:
         return v
 
 
-_WS = {}
+class _ThreadWorkspaces(threading.local):
+    def __init__(self):
+        self.of = {}
+
+
+_WS = _ThreadWorkspaces()
 
 
 def workspace(device):
-    """The workspace of the current stream."""
+    """The calling thread's workspace of the current stream."""
     d = device if isinstance(device, torch.device) else torch.device(device)
     if d.type == "cuda":
         idx = d.index if d.index is not None else _raw_device()
         key = (idx, _stream_handle(idx))
     else:
         idx, key = None, (str(d), 0)
-    ws = _WS.get(key)
+    mine = _WS.of
+    ws = mine.get(key)
     if ws is None:
-        ws = _WS[key] = Workspace(torch.device("cuda", idx) if d.type == "cuda" else d)
+        ws = mine[key] = Workspace(torch.device("cuda", idx) if d.type == "cuda" else d)
     return ws
 
 
@@ -829,7 +839,10 @@ class Tape:
     the step runs inside `with tape:` (every call of a tape entry point made
     then is appended after it returns ISEG_OK), replayed from native code by
     run(step).  Keeps every buffer the recorded calls use allocated; the
-    caller keeps the streams alive and replays with the same stream setup.""" 
+    caller keeps the streams alive and replays with the same stream setup, in
+    the order of the recording thread's own calls on these streams, whose
+    workspaces the recorded calls share.  Calls of other threads are recorded
+    too: only one thread calls while a tape records.""" 
 
     def __init__(self, step):
         L = lib()
@@ -1345,8 +1358,8 @@ _NO_WS = {}
 
 
 def _scratch(x, nbytes):
-    """Workspace of a call on x's device: the stream's, or, under graph
-    capture, memory of the graph's own (a graph outlives the stream's workspace,
+    """Workspace of a call on x's device: the thread's on this stream, or, under
+    graph capture, memory of the graph's own (a graph outlives the stream's workspace,
     and two graphs may replay at once)."""
     if nbytes == 256:                # a call that touches none of it: one for all
         i = x.get_device()
