@@ -1286,13 +1286,16 @@ _FLOATS = {torch.float32: ISEG_F32, torch.float16: ISEG_F16, torch.bfloat16: ISE
 def _on_device(f):
     """Run f with its first tensor's device current (the library launches on
     the current device)."""
+    first = f.__code__.co_varnames[0]
+
     @functools.wraps(f)
-    def call(x, *args, **kw):
-        i = x.get_device()
+    def call(*args, **kw):
+        x = args[0] if args else kw.get(first)
+        i = x.get_device() if isinstance(x, torch.Tensor) else -1      # f itself refuses what is no tensor
         if i < 0 or i == _raw_device():
-            return f(x, *args, **kw)
+            return f(*args, **kw)
         with torch.cuda.device(i):
-            return f(x, *args, **kw)
+            return f(*args, **kw)
     return call
 
 
