@@ -581,8 +581,10 @@ int iseg_mse_onehot(const int8_t* y, const int32_t* y_exp, const uint8_t* labels
 /* iseg_layernorm_fwd -- layer normalization of every row of x [M, C]:
  *   mean = sum x / C, var = sum (x - mean)^2 / C, rstd = 1 / sqrt(var + eps),
  *   y = (x - mean) rstd gamma + beta.
- * x and y have x_dtype, gamma and beta [C] p_dtype (NULL: 1 and 0); mean and
- * rstd [M] float32 (may be NULL) are what the backward needs.  eps > 0 and
+ * x and y have x_dtype, gamma and beta [C] p_dtype (NULL: 1 and 0; with both
+ * NULL x_dtype is the p_dtype to give, since 16-bit rows of more than 16384
+ * columns take three passes beside float32 parameters and one beside 16-bit
+ * ones); mean and rstd [M] float32 (may be NULL) are what the backward needs.  eps > 0 and
  * finite.  A row with a non-finite value, or whose sum or sum of squares
  * leaves float32's range, sets ISEG_DEV_NONFINITE (that row's y unspecified).
  *

@@ -1428,7 +1428,9 @@ def layernorm_fwd(x, gamma=None, beta=None, eps=1e-5, status=None):
     if not (eps > 0 and math.isfinite(eps)):
         raise ValueError("eps: positive and finite expected")
     p = gamma if gamma is not None else beta
-    pd = _float_code(p, "gamma, beta") if p is not None else ISEG_F32
+    # without either, the kernels of x's own type: those of float32 parameters
+    # keep shorter rows of 16-bit types in registers
+    pd = _float_code(p, "gamma, beta") if p is not None else xd
     gamma = _vec(gamma, Cc, p.dtype if p is not None else None, x, "gamma")
     beta = _vec(beta, Cc, p.dtype if p is not None else None, x, "beta")
     _gpu(x, status)

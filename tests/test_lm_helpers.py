@@ -37,6 +37,32 @@ def test_arguments_by_name(n):
         f(**{k: v for k, v in list(kw.items())[1:]})
 
 
+@pytest.mark.parametrize("t", [torch.bfloat16, torch.float16, torch.float32])
+def test_layernorm_parameter_type(monkeypatch, t):
+    """The type that the kernels are chosen by: the parameters', and x's own
+    without any (float32 parameters beside 16-bit rows of more than 16384
+    columns take more passes over the row)."""
+    from paper_2011_14504_amd import iseg
+    seen = []
+    monkeypatch.setattr(iseg, "_gpu", lambda x, *ts: None)
+    monkeypatch.setattr(iseg, "iseg_layernorm_fwd", lambda x, g, b, geom, *rest: seen.append(geom.p_dtype))
+    x, one = torch.zeros(2, 20000, dtype=t), torch.ones(20000)
+    iseg.layernorm_fwd(x)
+    iseg.layernorm_fwd(x, one)
+    iseg.layernorm_fwd(x, None, one.half())
+    assert seen == [iseg._FLOATS[t], iseg.ISEG_F32, iseg.ISEG_F16]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("C", [100, 9000, 20000, 40000])
+def test_layernorm_without_parameters_is_that_of_ones_and_zeros(C):
+    from paper_2011_14504_amd import iseg
+    x = (normal(C, 5, C) + 0.5).to(torch.bfloat16).to(DEV)
+    one = torch.ones(C, dtype=torch.bfloat16, device=DEV)
+    for a, b in zip(iseg.layernorm_fwd(x), iseg.layernorm_fwd(x, one, 0 * one)):
+        assert torch.equal(a, b)
+
+
 @pytest.mark.gpu
 @pytest.mark.parametrize("n", range(10))
 def test_arguments_by_name_give_the_same(n):
