@@ -728,6 +728,10 @@ int iseg_linear_i8_bwd(const void* dy, const int8_t* a, const float* a_scale, co
  * iseg_logprob_bwd -- gradient of sum_m g_logprob[m] logprob[m] +
  * g_entropy[m] entropy[m], given the forward's lse and entropy:
  *   dlogits_v = g_logprob ([v = t] - p_v) - g_entropy p_v (log p_v + entropy).
+ * Float32 holds lse to 2^-25 of its size.  Where |lse| >= 256 and lse is the
+ * row's own, p_v is therefore formed from the logits once more (a second pass
+ * over such a row); an lse of anything else, a longer row of which these logits
+ * are a part, say, is taken as given.
  * g_logprob, g_entropy [M] float32, one of them may be NULL (0); entropy may
  * be NULL with g_entropy.  dlogits has the logits' type, rows out_ld apart.
  * A row of banned tokens only has gradient 0; a token >= V sets
