@@ -1343,11 +1343,13 @@ def _vec(t, n, dtype, x, what):
     return t.contiguous()
 
 
-def _gpu(x, *ts):
+def _gpu(x, *ts, status=None):
+    if status is not None and (status.dtype != torch.int32 or status.numel() < 1):
+        raise ValueError("status: an int32 word expected")       # kernels write to it
     i = x.get_device()
     if i < 0:
         raise ValueError("GPU tensors expected")
-    for t in ts:
+    for t in (*ts, status):
         if t is not None and t.get_device() != i:
             raise ValueError("GPU tensors on one device expected")
 
@@ -1433,7 +1435,7 @@ def layernorm_fwd(x, gamma=None, beta=None, eps=1e-5, status=None):
     pd = _float_code(p, "gamma, beta") if p is not None else xd
     gamma = _vec(gamma, Cc, p.dtype if p is not None else None, x, "gamma")
     beta = _vec(beta, Cc, p.dtype if p is not None else None, x, "beta")
-    _gpu(x, status)
+    _gpu(x, status=status)
     y = _like(x)
     mean = torch.empty(M if x.dim() == 2 else x.shape[:-1], dtype=torch.float32, device=x.device)
     rstd = torch.empty_like(mean)
@@ -1489,7 +1491,7 @@ def quantize_rows(x, bits=8, scale_mode=ISEG_SCALE_MAX, mul=None, status=None):
     _quant_args(bits, scale_mode)
     xr, M, Cc, ld = _rows(x, "x")
     mul = _vec(mul, Cc, torch.float32, x, "mul")
-    _gpu(x, status)
+    _gpu(x, status=status)
     codes = _codes_matrix(M, Cc, x.device)
     scale = torch.empty(M, dtype=torch.float32, device=x.device)
     iseg_quantize_rows(xr, xd, M, Cc, ld, mul, bits, scale_mode, codes, codes.stride(0), scale, status)
@@ -1505,7 +1507,7 @@ def quantize_cols(x, bits=8, scale_mode=ISEG_SCALE_MAX, mul=None, want_sums=Fals
     _quant_args(bits, scale_mode)
     xr, M, Cc, ld = _rows(x, "x")
     mul = _vec(mul, M, torch.float32, x, "mul")
-    _gpu(x, status)
+    _gpu(x, status=status)
     codes = _codes_matrix(Cc, M, x.device)
     scale = torch.empty(Cc, dtype=torch.float32, device=x.device)
     sums = torch.empty(Cc, dtype=torch.float32, device=x.device) if want_sums else None
@@ -1568,7 +1570,7 @@ def linear_i8_fwd(x, w, w_scale=None, bias=None, bits=8, scale_mode=ISEG_SCALE_M
     dev = x.device
     w_scale = _vec(w_scale, N, torch.float32, x, "w_scale")
     bias = _vec(bias, N, torch.float32, x, "bias")
-    _gpu(x, w, status)
+    _gpu(x, w, status=status)
     codes = _codes_matrix(M, K, dev)
     scale = torch.empty(M, dtype=torch.float32, device=dev)
     y = torch.empty(*x.shape[:-1], N, dtype=out_dtype, device=dev)
@@ -1605,7 +1607,7 @@ def linear_i8_bwd(dy, a, a_scale, w, w_scale=None, w_t=None, bits=8, scale_mode=
     dev = dy.device
     a_scale = _vec(a_scale, M, torch.float32, dy, "a_scale")
     w_scale = _vec(w_scale, N, torch.float32, dy, "w_scale")
-    _gpu(dy, a, w, w_t, status)
+    _gpu(dy, a, w, w_t, status=status)
     dx = torch.empty(M, K, dtype=out_dtype, device=dev) if want_input else None
     dw = torch.empty(N, K, dtype=out_dtype, device=dev) if want_weight else None
     dbias = torch.empty(N, dtype=torch.float32, device=dev) if want_bias else None
@@ -1639,7 +1641,7 @@ def logprob_fwd(logits, tokens, top_k=0, want_entropy=True, status=None):
         raise ValueError("logits: empty rows")
     if not 0 <= top_k <= min(64, V):
         raise ValueError("top_k: 0 to 64, and at most the logits of a row expected")
-    _gpu(logits, tokens, status)
+    _gpu(logits, tokens, status=status)
     shape, dev = logits.shape[:-1], logits.device
     g, wsb = _logprob_geom(M, V, ld, V, dt, td, top_k)
     logprob = torch.empty(M if logits.dim() == 2 else shape, dtype=torch.float32, device=dev)
@@ -1669,7 +1671,7 @@ def logprob_bwd(logits, tokens, lse, entropy, g_logprob=None, g_entropy=None, st
     entropy = _vec(entropy, M, torch.float32, logits, "entropy")
     g_logprob = _vec(g_logprob, M, torch.float32, logits, "g_logprob")
     g_entropy = _vec(g_entropy, M, torch.float32, logits, "g_entropy")
-    _gpu(logits, tokens, status)
+    _gpu(logits, tokens, status=status)
     dx = _like(logits)
     g, _ = _logprob_geom(M, V, ld, V, dt, td, 0)
     iseg_logprob_bwd(lr, tokens, lse, entropy, g_logprob, g_entropy, g, dx, status)

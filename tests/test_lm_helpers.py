@@ -44,7 +44,7 @@ def test_layernorm_parameter_type(monkeypatch, t):
     columns take more passes over the row)."""
     from paper_2011_14504_amd import iseg
     seen = []
-    monkeypatch.setattr(iseg, "_gpu", lambda x, *ts: None)
+    monkeypatch.setattr(iseg, "_gpu", lambda x, *ts, **kw: None)
     monkeypatch.setattr(iseg, "iseg_layernorm_fwd", lambda x, g, b, geom, *rest: seen.append(geom.p_dtype))
     x, one = torch.zeros(2, 20000, dtype=t), torch.ones(20000)
     iseg.layernorm_fwd(x)
@@ -156,7 +156,8 @@ REFUSALS = [
     ("logprob_bwd", dict(entropy=torch.zeros(6).double()), "entropy: 6 elements of torch.float32"),
     ("logprob_bwd", dict(g_logprob=torch.zeros(7)), "g_logprob: 6 elements"),
     ("logprob_bwd", dict(g_entropy=torch.zeros(6).half()), "g_entropy: 6 elements of torch.float32"),
-]
+] + [(name, dict(status=st), "status: an int32 word") for st in (torch.zeros(1), torch.zeros(4, dtype=torch.uint8), torch.zeros(0, dtype=torch.int32))
+     for name in ("layernorm_fwd", "quantize_rows", "quantize_cols", "linear_i8_fwd", "linear_i8_bwd", "logprob_fwd", "logprob_bwd")]
 
 
 @pytest.mark.parametrize("i", range(len(REFUSALS)), ids=lambda i: f"{REFUSALS[i][0]}-{i}")
