@@ -593,6 +593,8 @@ int iseg_mse_onehot(const int8_t* y, const int32_t* y_exp, const uint8_t* labels
  *   dgamma = sum over rows of dy xhat, dbeta = sum over rows of dy.
  * dy (rows y_ld apart) and dx have x_dtype; dgamma and dbeta [C] p_dtype, each
  * may be NULL.  Sums have one fixed order: the same call gives the same bits.
+ * mean and rstd are taken as given: a mean rounded to float32 shifts xhat by up
+ * to 2^-24 |mean| rstd, which a row far from zero beside its spread shows.
  * With M = 0, dgamma and dbeta are zeros.  C <= 2^27. */
 typedef struct iseg_layernorm_geom {
     int64_t M, C;
@@ -649,8 +651,8 @@ int iseg_transpose_i8(const int8_t* in, int64_t M, int64_t C, int64_t in_ld, int
  * float32, each may be NULL (1, 1, 0).  The sums are exact int32 (K <= 131071,
  * ISEG_ERR_UNSUPPORTED beyond), rounded to float32 and multiplied by a_scale;
  * that times b_scale plus bias is rounded once, and then to out_dtype (a float
- * type).  A row's outputs do not depend on the other rows.  K = 0 gives the
- * bias.  a and b start at multiples of 16 bytes unless `unaligned`
+ * type).  A row's outputs do not depend on the other rows.  K = 0 gives sums
+ * of 0.  a and b start at multiples of 16 bytes unless `unaligned`
  * is set (ISEG_ERR_ARG); with it, or with lda or ldb off a multiple of 16, the
  * workspace has room for aligned copies (not for M <= 32).  More than 2^23 - 1
  * tiles of 256 x 256 outputs, or with M <= 32 of 32 columns, are
@@ -722,8 +724,8 @@ int iseg_linear_i8_bwd(const void* dy, const int8_t* a, const float* a_scale, co
  * (NULL if top_k = 0; top_k <= 64 and <= V).  A logit of -infinity is a banned
  * token: probability 0, no part of the entropy; a row of nothing else has lse
  * and every logprob -infinity, entropy 0.  A NaN or +infinity sets
- * ISEG_DEV_NONFINITE, that row's results are NaN, its ids unspecified within
- * [0, V).  V in [1, 2^31).
+ * ISEG_DEV_NONFINITE, that row's results are NaN (but 0 for a token that is not
+ * given), its ids unspecified within [0, V).  V in [1, 2^31).
  *
  * iseg_logprob_bwd -- gradient of sum_m g_logprob[m] logprob[m] +
  * g_entropy[m] entropy[m], given the forward's lse and entropy:

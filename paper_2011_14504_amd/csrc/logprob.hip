@@ -204,7 +204,7 @@ __device__ __forceinline__ void best_keys(uint64_t mine, int k, uint64_t* keys, 
     __syncthreads();
 }
 
-// One vector's part of a row: its maximum and leader, then its exponentials.
+// the exponentials of U vectors, to whose largest logit s has been moved
 template <typename T, bool ENT, int U>
 __device__ __forceinline__ void lp_take(const RowVec<T>* r, Stat& s)
 {
@@ -230,9 +230,10 @@ __device__ __forceinline__ float vec_max(const RowVec<T>& r)
 }
 
 // A block's part of a row.  fp32 is bound by memory: 2048 x 50021 with entropy
-// and 5 alternatives 80 us, 5.1 TB/s.  16-bit logits are bound by the exponential
-// and the eight or so other instructions of each: 2048 x 50021 bf16 61 us with 5
-// alternatives, 54 without (3.8 TB/s), 4096 x 32768 60 (4.5 TB/s).  4 x 131072
+// and 5 alternatives 80 us, 5.1 TB/s.  16-bit logits are bound by the
+// issue of 12 vector instructions for each, one of them an exponential that takes
+// four slots (15 with alternatives; counted at 4096 x 32768): 2048 x 50021 bf16 61
+// us with 5 alternatives, 54 without (3.8 TB/s), 4096 x 32768 60 (4.5 TB/s).  4 x 131072
 // bf16 in 32 parts with 20 alternatives 8.5 us, bound by latency.
 // Six waves per SIMD where alternatives are ranked hide more of the ranking's
 // latency (1957 x 13910 fp16, 20 of them, 25.8 us; 28 with the four that the

@@ -114,7 +114,9 @@ __device__ __forceinline__ void mm_tile(uint32_t bid, uint32_t tm, uint32_t tn, 
 // BM x BN outputs per block of WM x WN waves, 128 of the reduction per stage
 // (whole cache lines of every row), ST stages of LDS.  Large products are bound
 // by the matrix cores at the clock that their power leaves: 8192 x 8192 x 8192
-// bf16 out 441 to 500 us (2.2 to 2.5 POP/s), 4096 x 4096 x 4096 61 (2.25),
+// bf16 out 405 to 445 us back to back, by box (2.5 to 2.7 POP/s; 488 to 517 under
+// the profiler, where the matrix cores are busy for 64 % of the cycles; zeros as
+// operands 349), 4096 x 4096 x 4096 61 (2.25),
 // 2048 x 8192 x 2048 36.8 (1.9, one round of 256 tiles, whose epilogues write
 // 33 MB at once); small ones by the latency of a stage: 1024 x 2048 x 2048 9.9.
 // Eight waves of 128 x 64 outputs, not four of 128 x 128, whose accumulators
@@ -360,7 +362,10 @@ __global__ __launch_bounds__(256) void k_mm_join(MmArgs p, const int32_t* __rest
 // A block takes J * 16 rows of b, its NW waves deal out their reduction in
 // pieces of 256; b comes straight into fragments (nothing of it is used
 // twice), a from the caches, and the waves' sums meet in LDS.  Bound by b's
-// bytes: 8 x 12288 x 4096 12.2 us (4.1 TB/s), 24 x 12288 x 4096 16.2.
+// bytes where N fills the CUs: 8 x 12288 x 4096 14.6 us from memory (3.4 TB/s),
+// 12.4 from the last-level cache; 24 x 12288 x 4096 19.0 and 16.5.  The reduction
+// is not split over blocks, so narrow outputs leave CUs idle: 8 x 1024 x 8192 8.2
+// us (bytes 1.7), 8 x 256 x 16384 13.2 (0.9).
 // ODD: rows of a or b may start off a multiple of four bytes.
 template <typename TO, int MT, int J, int NW, bool ODD>
 __global__ __launch_bounds__(NW * 64) void k_mm_rows(MmArgs p)
@@ -461,9 +466,10 @@ constexpr int kTokenMax = 8192;            // longest token that a block quantiz
 // k_mm_rows for one token, whose blocks quantize it for themselves: the first
 // weights are on their way while a block takes the maximum and leaves the
 // codes in LDS.  x is read by every block, from the caches; of the codes each
-// block writes out its own share.  1 x 4096 x 4096 8.9 us with weights from
-// memory (1.9 TB/s), 5.5 from the caches: load, maximum, codes, products and sum
-// follow one another.
+// block writes out its own share.  1 x 4096 x 4096 6.7 us with weights from
+// memory (2.5 TB/s), 5.3 from the caches: load, maximum, codes, products and sum
+// follow one another, and only each wave's first 256 of the reduction are
+// requested ahead of the maximum, the others piece by piece behind the codes.
 template <typename TX, typename TO, int J>
 __global__ __launch_bounds__(512) void k_linear_token(LinArgs a)
 {
@@ -776,10 +782,12 @@ int lin_check(const iseg_linear_geom* g)
     return mm_check(&p);
 }
 
-// One kernel for one token: 1 x 4096 x 4096 8.9 us against 9.4 for the two,
-// 1 x 2048 x 2048 4.9 against 6.3, and one launch less.  (With more tokens
-// every block's own quantization costs more than the launch: two tokens of
-// 4096 10.5 us against 9.3.)
+// One kernel for one token, at every size that a block can hold: N x K 1024 x
+// 1024 3.2 us against 5.4 for the two, 4096 x 4096 6.7 / 9.1 (from the caches 5.3 /
+// 7.4), 1024 x 8192 8.0 / 10.3, 4096 x 8192 10.3 / 12.0, 12288 x 4096 16.2 / 17.1,
+// 8192 x 8192 15.7 / 18.8.  What it saves is a launch, the more of the whole the
+// fewer the weights' bytes.  (With more tokens every block's own quantization
+// costs more than the launch: two tokens of 4096 10.5 us against 9.3.)
 bool lin_fused(const iseg_linear_geom* g)
 {
     return g->M == 1 && g->N > 0 && g->K >= 8 && g->K <= kTokenMax;

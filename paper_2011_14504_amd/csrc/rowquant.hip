@@ -39,8 +39,10 @@ __device__ __forceinline__ uint32_t row_max_u32(uint32_t v, uint32_t* red)
 
 // NW waves per row (one, or the whole block), VPT vectors of it per thread, in
 // registers between the maximum and the codes, and the next row's on their way.
-// Bound by memory, x read and the codes written once: 4096 x 4096 bf16 14.6 us
-// (3.4 TB/s), fp32 16.3 (5.1), 4096 x 16384 bf16 41.5 (4.9).  mul waits in LDS,
+// x is read and the codes written once: 4096 x 4096 bf16 14.6 us (3.4 TB/s), fp32
+// 16.3 (5.1), 4096 x 16384 bf16 41.5 (4.9).  fp32 is bound by memory, 16-bit types
+// as much by the issue of 24 vector instructions per element (40 of 43 us at
+// 16384 x 4096, by counters).  mul waits in LDS,
 // every thread's own part: in registers as well it leaves one block of eight
 // waves on a CU (4096 x 16384 bf16 81 us, so 54 at four waves per SIMD).
 template <typename T, bool MUL, int NW, int VPT>
@@ -480,8 +482,9 @@ __global__ __launch_bounds__(256) void k_transpose_i8(TurnArgs a)
 // on all the banks); rows of codes leave 16 bytes per lane, a whole line per
 // column.  The block takes the scales from the strips' partials itself, or
 // (strips = 0: at most 128 rows) from the columns, which spares a launch: 64 x
-// 1024 bf16 8.1 us, 10.4 with k_cols_stats.  4096 x 4096 bf16 15 to 17 us: bound
-// by the coding, 2.9 TB/s of x and codes.  Blocks behind the cx * cy that code
+// 1024 bf16 8.1 us, 10.4 with k_cols_stats.  4096 x 4096 bf16 15 to 18 us: bound
+// by the coding, 24 vector instructions per element (40 of 54 us at 16384 x 4096,
+// by counters), with waits for the scales and each step's loads.  Blocks behind the cx * cy that code
 // transpose the product's other operand (turn.ty = 0: none); of the linear
 // layer's backward, 295 x 1024 x 2560 30.6 us, with a launch of its own 36.
 template <typename T, bool MUL>
