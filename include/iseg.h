@@ -753,6 +753,187 @@ int iseg_logprob_bwd(const void* logits, const void* tokens, const float* lse, c
                      int32_t* dev_status, hipStream_t stream);
 
 /* ------------------------------------------------------------------------ */
+/* A serving step of a language model over a cache held in 4 bits            */
+/* ------------------------------------------------------------------------ */
+/* Tokens of a step.  The new tokens of B requests lie one request after the
+ * other; q_start [B + 1] int32 holds each request's first row and the end.
+ * Head tensors are [T, H, D] with dense heads: a token's stride (_ld) and a
+ * head's (_hs) in elements, any alignment, so that slices of one projection's
+ * rows serve.  Block tables are [B, max_pages] int32 with rows table_ld apart:
+ * entry i of a request is the page of its tokens i page .. (i + 1) page - 1.  A
+ * slot is page id * page + the token's place in the page. */
+
+/* iseg_page_map -- the step's pages, slots and positions, built on the device
+ * from the requests' lengths.  For request b with ctx[b] tokens before the step
+ * and count[b] new ones: kv_len[b] = ctx[b] + count[b]; it holds held[b] pages
+ * and takes as many more as kv_len[b] needs, in the order of the requests, from
+ * the end of free_pages (its first n_free[0] entries are free); they are written
+ * into table's next columns.  q_start is the exclusive sum of count; for new
+ * token i of request b, at row q_start[b] + i, positions = ctx[b] + i and slots
+ * its slot.  Rows from q_start[B] to T get position 0 and slot -1.  held_out and
+ * n_free_out [1] hold the state after the step and may be held and n_free
+ * themselves (all int32).
+ * ISEG_DEV_RANGE: a negative length (taken as 0), held outside [0, max_pages]
+ * (clamped), n_free outside [0, F] (clamped), more tokens than T (those beyond
+ * are left out), no free page or no column left (the tokens of such a page get
+ * slot -1, its table entry -1 where there is a column, and held_out counts the
+ * pages that were got), or a page id outside [0, n_pages) (slot -1).
+ * n_pages page < 2^31; B and T < 2^31. */
+typedef struct iseg_page_map_geom {
+    int64_t B, T;
+    int64_t max_pages, table_ld;
+    int64_t F;                   /* entries of free_pages */
+    int64_t n_pages;
+    int32_t page;                /* tokens of a page, >= 1 */
+    int32_t reserved;            /* 0 (ISEG_ERR_ARG otherwise, here and below) */
+} iseg_page_map_geom;
+size_t iseg_page_map_ws(const iseg_page_map_geom* g);
+int iseg_page_map(const int32_t* ctx, const int32_t* count, const int32_t* held, const int32_t* free_pages,
+                  const int32_t* n_free, const iseg_page_map_geom* g, int32_t* table, int32_t* q_start,
+                  int32_t* kv_len, int32_t* positions, int32_t* slots, int32_t* held_out, int32_t* n_free_out,
+                  void* ws, size_t ws_bytes, int32_t* dev_status, hipStream_t stream);
+
+/* iseg_qk_norm_rope_fwd -- every head's row x of q [T, Hq, D] and k [T, Hk, D]:
+ *   n = x gamma / sqrt(sum x^2 / D + eps)      (norm = 0: n = x),
+ * then its first rope_dim elements rotated: with angle_i = position inv_freq[i],
+ * i < rope_dim / 2, the pair (a, b) = (n_i, n_{i + rope_dim / 2}) (pairs = 0) or
+ * (n_{2 i}, n_{2 i + 1}) (pairs = 1) becomes
+ *   (a cos - b sin, a sin + b cos) mscale.
+ * positions [T] of pos_dtype (ISEG_I32 or ISEG_I64, |position| <= 2^31),
+ * inv_freq float32; the angle is formed and reduced in 64 bits.  gamma_q,
+ * gamma_k [D] of p_dtype, each NULL: 1.  eps >= 0, finite.  yq, yk have dtype
+ * and may be q and k themselves (same strides).  Hq or Hk may be 0, their
+ * pointers NULL.  A row with norm whose sum of squares is not finite sets
+ * ISEG_DEV_NONFINITE (its y unspecified).
+ *
+ * iseg_qk_norm_rope_bwd -- with g the rotation of dy back (times mscale),
+ * r = 1 / sqrt(sum x^2 / D + eps) and xhat = x r:
+ *   dx = r (g gamma - xhat sum(g gamma xhat) / D),   (norm = 0: dx = g)
+ *   dgamma = sum over tokens and heads of g xhat
+ * dgamma_q, dgamma_k [D] of p_dtype, each may be NULL (with norm = 0 they must
+ * be); zeros if there are no rows.  Sums have one fixed order.
+ * D <= 512 (ISEG_ERR_UNSUPPORTED beyond), 0 <= rope_dim <= D and even. */
+typedef struct iseg_qk_norm_rope_geom {
+    int64_t T, Hq, Hk, D;
+    int64_t q_ld, q_hs, k_ld, k_hs;
+    int64_t yq_ld, yq_hs, yk_ld, yk_hs;      /* outputs; in the backward dyq, dyk */
+    int64_t dq_ld, dq_hs, dk_ld, dk_hs;      /* backward only */
+    int32_t dtype, p_dtype, pos_dtype;
+    int32_t rope_dim, pairs, norm;
+    float eps, mscale;
+} iseg_qk_norm_rope_geom;
+int iseg_qk_norm_rope_fwd(const void* q, const void* k, const void* positions, const float* inv_freq,
+                          const void* gamma_q, const void* gamma_k, const iseg_qk_norm_rope_geom* g, void* yq,
+                          void* yk, int32_t* dev_status, hipStream_t stream);
+size_t iseg_qk_norm_rope_bwd_ws(const iseg_qk_norm_rope_geom* g);
+int iseg_qk_norm_rope_bwd(const void* dyq, const void* dyk, const void* q, const void* k, const void* positions,
+                          const float* inv_freq, const void* gamma_q, const void* gamma_k,
+                          const iseg_qk_norm_rope_geom* g, void* dq, void* dk, void* dgamma_q, void* dgamma_k,
+                          void* ws, size_t ws_bytes, hipStream_t stream);
+
+/* The cache.  Keys and values are codes of 4 bits, n in [-7, 7] stored as n + 8,
+ * with one float32 scale for each token and head; the value is n * scale.  W, the
+ * stored width, is D rounded up to 32 (above 128: to 64); columns beyond D hold
+ * the code 0.  page is a multiple of 16, at most 8192.
+ *   k [n_pages, H, page, W / 2] bytes: a token's row, eight codes a 32-bit word:
+ *     of codes 8 w + e, even e in bits 4 (e / 2), odd e in bits 16 + 4 (e / 2).
+ *   v [n_pages, H, page / 16, 8 W] bytes, tiles of 16 tokens: token 4 g + j and
+ *     columns 32 i + c (low four bits) and 32 i + 16 + c (high), c < 16, in byte
+ *     ((4 c + g) (W / 32) + i) 4 + j.
+ *   k_scale, v_scale [n_pages, H, page].
+ * A wave's matrix operands are whole 16-byte pieces of either. */
+
+/* iseg_kv4_write -- tokens' keys and values k, v [T, H, D] into their slots:
+ * scale = max|x| / 7 (ISEG_SCALE_MAX) or the power-of-two step of
+ * iseg_quantize_rows with 4 bits (ISEG_SCALE_POW2), at least 2^-60 (so a row of
+ * zeros has 2^-60); codes = clamp(floor(x / scale + 1/2), +-7), decided exactly.
+ * slots [T] of slot_dtype; a negative slot is skipped, one outside the cache is
+ * skipped and sets ISEG_DEV_RANGE; the slots of a call are distinct (which of
+ * two writers' bytes stay is unspecified).  A row with a non-finite value gets
+ * codes 0 and a NaN scale and sets ISEG_DEV_NONFINITE.
+ *
+ * iseg_kv4_read -- the values at slots, code * scale rounded to dtype; zeros for
+ * a negative slot, and for one outside the cache, which sets ISEG_DEV_RANGE.
+ * D <= 256 (ISEG_ERR_UNSUPPORTED beyond). */
+typedef struct iseg_kv4_geom {
+    int64_t T, H, D;
+    int64_t k_ld, k_hs, v_ld, v_hs;
+    int64_t n_pages;
+    int32_t page, dtype, slot_dtype;
+    int32_t scale_mode;          /* write only */
+} iseg_kv4_geom;
+int iseg_kv4_write(const void* k, const void* v, const void* slots, const iseg_kv4_geom* g, uint8_t* k_codes,
+                   float* k_scale, uint8_t* v_codes, float* v_scale, int32_t* dev_status, hipStream_t stream);
+int iseg_kv4_read(const uint8_t* k_codes, const float* k_scale, const uint8_t* v_codes, const float* v_scale,
+                  const void* slots, const iseg_kv4_geom* g, void* k, void* v, int32_t* dev_status,
+                  hipStream_t stream);
+
+/* iseg_kv4_attention -- attention of the step's tokens over the cache.  Query i
+ * of request b, of its n = q_start[b + 1] - q_start[b], stands at position
+ * kv_len[b] - n + i (its own key is in the cache) and sees keys j < kv_len[b]
+ * with, if causal, j <= its position, and, if window > 0, j > its position -
+ * window.  Query head h reads key head h / (Hq / H):
+ *   s_j = scale (q . k_j),  out = sum_j softmax(s)_j v_j,
+ *   lse = log sum_j e^{s_j}   (float32 [T, Hq] dense, may be NULL).
+ * A row that sees no key has out 0 and lse -infinity.  Rows before q_start[0]
+ * and from q_start[B] on are left as they were.  q and out of dtype; scores and
+ * sums are float32, formed of the integer codes and q in float16, exact to 2^-25
+ * of its row's largest element (float32 tensors: two terms).  A softmax weight
+ * times its key's scale of v is a float16, off by at most 2^-11 of itself
+ * (float32 tensors: two terms, 2^-21) and at least 2^-31 of the request's
+ * largest scale of v.
+ * max_q, max_kv: what the caller knows of the longest request's new tokens and
+ * of the longest kv_len (0: T and max_pages page).  A request beyond either, a
+ * q_start that falls or leaves [0, T], a negative kv_len or a page id outside
+ * [0, n_pages) (its keys count as unseen) sets ISEG_DEV_RANGE.
+ * D a multiple of 8, at most 256; Hq a multiple of H; scale > 0, finite;
+ * max_kv < 2^31 - 2^16. */
+typedef struct iseg_kv4_attention_geom {
+    int64_t T, B, Hq, H, D;
+    int64_t q_ld, q_hs, o_ld, o_hs;
+    int64_t n_pages, max_pages, table_ld;
+    int64_t max_q, max_kv;
+    int64_t window;
+    int32_t page, dtype, causal;
+    float scale;
+} iseg_kv4_attention_geom;
+size_t iseg_kv4_attention_ws(const iseg_kv4_attention_geom* g);
+int iseg_kv4_attention(const void* q, const uint8_t* k_codes, const float* k_scale, const uint8_t* v_codes,
+                       const float* v_scale, const int32_t* table, const int32_t* q_start, const int32_t* kv_len,
+                       const iseg_kv4_attention_geom* g, void* out, float* lse, void* ws, size_t ws_bytes,
+                       int32_t* dev_status, hipStream_t stream);
+
+/* iseg_verify_drafts -- drafted tokens against the target's probabilities, from
+ * given random numbers.  Request b has drafted n_draft[b] <= S tokens x_i =
+ * tokens[b, i] from the distributions q_i = draft[b, i, :]; the target gave p_i =
+ * target[b, i, :], i <= n_draft[b].  Draft i is accepted if all before it are and
+ *   u[b, i] q_i(x_i) < p_i(x_i);
+ * after `accepted` of them one more token is taken: from p_i where all were
+ * accepted, from the remainder max(p_i - q_i, 0) of the first one refused (from
+ * p_i where the remainder is 0 throughout): the smallest v whose cumulative sum
+ * exceeds u_sample[b] times the whole.  draft NULL: each x_i was certain (q_i is
+ * 1 at x_i).  The decisions are exact: products and sums in float64 of the given
+ * probabilities.  out [B, S + 1] int32: the accepted drafts, the token taken,
+ * then -1; accepted [B] int32.
+ * target [B, S + 1, V] rows t_ld and requests t_bs elements apart, draft
+ * [B, S, V] with d_ld, d_bs; both of dtype.  tokens, u [B, S] dense, tokens of
+ * token_dtype, u and u_sample [B] float32 in [0, 1).
+ * ISEG_DEV_RANGE: n_draft outside [0, S] (clamped), a drafted token outside
+ * [0, V) (refused; the remainder is max(p_i - q_i, 0) still), a row without any
+ * mass (its token is -1).  ISEG_DEV_NONFINITE: a used row with a NaN, an infinity
+ * or a negative value (the token is unspecified within [-1, V)).
+ * V in [1, 2^31). */
+typedef struct iseg_verify_geom {
+    int64_t B, S, V;
+    int64_t t_bs, t_ld, d_bs, d_ld;
+    int32_t dtype, token_dtype;
+} iseg_verify_geom;
+size_t iseg_verify_drafts_ws(const iseg_verify_geom* g);
+int iseg_verify_drafts(const void* target, const void* draft, const void* tokens, const int32_t* n_draft,
+                       const float* u, const float* u_sample, const iseg_verify_geom* g, int32_t* out,
+                       int32_t* accepted, void* ws, size_t ws_bytes, int32_t* dev_status, hipStream_t stream);
+
+/* ------------------------------------------------------------------------ */
 /* Host-side utilities                                                       */
 /* ------------------------------------------------------------------------ */
 

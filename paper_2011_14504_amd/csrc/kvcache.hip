@@ -1,0 +1,441 @@
+// kvcache.hip -- the paged 4-bit cache: writing and reading tokens (iseg_kv4_write,
+// iseg_kv4_read), and the step's pages, slots and positions (iseg_page_map).
+#include "coder.h"
+#include "kv4.h"
+
+namespace {
+
+// ---------------------------------------------------------------------------
+// tokens into the cache and back
+// ---------------------------------------------------------------------------
+struct KvArgs {
+    const void *k, *v, *slots;
+    void *ko, *vo;
+    uint8_t *kc, *vc;
+    float *ks, *vs;
+    int64_t rows;                    // T * H
+    int64_t k_ld, k_hs, v_ld, v_hs;
+    int64_t n_slots;
+    int32_t H, D, W, page, slot64, mode;
+    int32_t* status;
+};
+
+// where a token lies: rows of pages, heads and tokens, counted in tokens
+struct KvPlace {
+    int64_t row;                     // (page id * H + head) * page + place in the page
+    int64_t tile;                    // first byte of its tile of 16 tokens in v
+    int t;                           // token of the tile
+};
+
+__device__ __forceinline__ KvPlace kv_place(const KvArgs& a, int64_t slot, int h)
+{
+    const uint32_t s = (uint32_t)slot, pg = s / (uint32_t)a.page, in = s - pg * (uint32_t)a.page;
+    KvPlace p;
+    p.row = ((int64_t)pg * a.H + h) * a.page + in;
+    p.tile = (p.row - (in & 15)) * (a.W / 2);
+    p.t = (int)(in & 15);
+    return p;
+}
+
+__device__ __forceinline__ int64_t kv_slot(const KvArgs& a, int64_t t)
+{
+    return a.slot64 ? ((const int64_t*)a.slots)[t] : ((const int32_t*)a.slots)[t];
+}
+
+// eight elements of a row from d on, zeros beyond D
+template <typename T>
+__device__ __forceinline__ void kv_get8(const T* p, int d, int D, float* f)
+{
+    if (d + 8 <= D) {
+        struct { T v[8]; } r;
+        __builtin_memcpy(&r, p + d, sizeof(r));
+#pragma unroll
+        for (int i = 0; i < 8; i++) f[i] = (float)r.v[i];
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; i++) f[i] = d + i < D ? (float)p[d + i] : 0.f;
+    }
+}
+
+// LPR lanes a row, eight columns (a word of codes) a lane; blockIdx.y: keys or
+// values.  The largest magnitude over the row's lanes, the scale, the codes.  A
+// byte of v holds columns 16 apart, which lie two lanes apart: each pair of
+// lanes exchanges words and stores half of the eight bytes.
+template <typename T, int LPR>
+__global__ __launch_bounds__(256) void k_kv4_write(KvArgs a)
+{
+    const int w = threadIdx.x % LPR, words = a.W / 8;
+    const int64_t r = (int64_t)blockIdx.x * (256 / LPR) + threadIdx.x / LPR;
+    if (r >= a.rows) return;
+    const bool val = blockIdx.y != 0;
+    const int64_t t = r / a.H;
+    const int h = (int)(r - t * a.H);
+    const int64_t slot = kv_slot(a, t);
+    if (slot < 0 || slot >= a.n_slots) {
+        if (slot >= 0 && w == 0) set_status(a.status, ISEG_DEV_RANGE);
+        return;
+    }
+    const T* x = val ? (const T*)a.v + t * a.v_ld + h * a.v_hs : (const T*)a.k + t * a.k_ld + h * a.k_hs;
+    float f[8];
+    kv_get8(x, w * 8, a.D, f);
+    uint32_t big = 0;
+#pragma unroll
+    for (int i = 0; i < 8; i++) {
+        const uint32_t b = bits_of(f[i]);
+        big = b > big ? b : big;
+    }
+#pragma unroll
+    for (int o = LPR / 2; o > 0; o >>= 1) {
+        const uint32_t b = (uint32_t)__shfl_xor((int)big, o, 64);
+        big = b > big ? b : big;
+    }
+    float s = kKvScaleMin;
+    if (big) s = scale_of(bits_of((double)__builtin_bit_cast(float, big)), 4, a.mode);
+    if (s < kKvScaleMin) s = kKvScaleMin;                      // a NaN stays
+    const Coder cd(s);
+    uint32_t n[2];
+    codes_of<8, false>(f, nullptr, [&](int) -> const Coder& { return cd; }, 7, n);
+    if (!cd.ok) {
+        n[0] = n[1] = 0;
+        if (w == 0) set_status(a.status, ISEG_DEV_NONFINITE);
+    }
+    // bytes n in [-7, 7] to n + 8
+    n[0] = (n[0] & 0x0f0f0f0fu) ^ 0x08080808u;
+    n[1] = (n[1] & 0x0f0f0f0fu) ^ 0x08080808u;
+    const KvPlace p = kv_place(a, slot, h);
+    if (!val) {
+        // even codes in the low half, odd ones in the high half
+        uint32_t word = 0;
+#pragma unroll
+        for (int e = 0; e < 8; e++) word |= ((n[e >> 2] >> (8 * (e & 3))) & 15u) << ((e & 1) * 16 + (e >> 1) * 4);
+        if (w < words) *(uint32_t*)(a.kc + p.row * (a.W / 2) + w * 4) = word;
+        if (w == 0) a.ks[p.row] = s;
+    } else {
+        // the lane without bit 1 has the low halves' columns, its partner the high ones'
+        const bool hi = w & 2;
+        const uint32_t give = hi ? n[0] : n[1], mine = hi ? n[1] : n[0];
+        const uint32_t got = (uint32_t)__shfl_xor((int)give, 2, 64);
+        const uint32_t b = hi ? got | mine << 4 : mine | got << 4;
+        if (w < words) {
+            const int i = w >> 2, c0 = (w & 1) * 8 + (hi ? 4 : 0), g = p.t >> 2, j = p.t & 3, nc = a.W / 32;
+            uint8_t* q = a.vc + p.tile;
+#pragma unroll
+            for (int e = 0; e < 4; e++) q[((int64_t)((c0 + e) * 4 + g) * nc + i) * 4 + j] = (uint8_t)(b >> (8 * e));
+        }
+        if (w == 0) a.vs[p.row] = s;
+    }
+}
+
+template <typename T, int LPR>
+__global__ __launch_bounds__(256) void k_kv4_read(KvArgs a)
+{
+    const int w = threadIdx.x % LPR, words = a.W / 8;
+    const int64_t r = (int64_t)blockIdx.x * (256 / LPR) + threadIdx.x / LPR;
+    if (r >= a.rows || w >= words) return;
+    const bool val = blockIdx.y != 0;
+    const int64_t t = r / a.H;
+    const int h = (int)(r - t * a.H);
+    const int64_t slot = kv_slot(a, t);
+    int n[8];
+    float s = 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; e++) n[e] = 0;
+    if (slot >= 0 && slot < a.n_slots) {
+        const KvPlace p = kv_place(a, slot, h);
+        if (!val) {
+            s = a.ks[p.row];
+            const uint32_t word = *(const uint32_t*)(a.kc + p.row * (a.W / 2) + w * 4);
+#pragma unroll
+            for (int e = 0; e < 8; e++) n[e] = (int)((word >> ((e & 1) * 16 + (e >> 1) * 4)) & 15u) - 8;
+        } else {
+            s = a.vs[p.row];
+            const int i = w >> 2, c0 = (w & 1) * 8, up = (w & 2) ? 4 : 0, g = p.t >> 2, j = p.t & 3, nc = a.W / 32;
+            const uint8_t* q = a.vc + p.tile;
+#pragma unroll
+            for (int e = 0; e < 8; e++) n[e] = (int)((q[((int64_t)((c0 + e) * 4 + g) * nc + i) * 4 + j] >> up) & 15) - 8;
+        }
+    } else if (slot >= 0 && w == 0) {
+        set_status(a.status, ISEG_DEV_RANGE);
+    }
+    T* out = val ? (T*)a.vo + t * a.v_ld + h * a.v_hs : (T*)a.ko + t * a.k_ld + h * a.k_hs;
+    struct { T v[8]; } o;
+#pragma unroll
+    for (int e = 0; e < 8; e++) o.v[e] = (T)((float)n[e] * s);
+    const int d = w * 8;
+    if (d + 8 <= a.D) {
+        __builtin_memcpy(out + d, &o, sizeof(o));
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; e++)
+            if (d + e < a.D) out[d + e] = o.v[e];
+    }
+}
+
+int kv_check(const iseg_kv4_geom* g)
+{
+    if (!g || !is_float_dtype(g->dtype) || (g->slot_dtype != ISEG_I32 && g->slot_dtype != ISEG_I64)) return ISEG_ERR_ARG;
+    if (g->T < 0 || g->H < 0 || g->D < 1 || g->T >= (int64_t)1 << 31 || g->page < 16 || g->page % 16 || g->n_pages < 0)
+        return ISEG_ERR_SHAPE;
+    if (g->D > 256 || g->page > 8192 || g->H > 65536 || !kv4_pages_ok(g->n_pages, g->page)) return ISEG_ERR_UNSUPPORTED;
+    return ISEG_OK;
+}
+
+KvArgs kv_args(const iseg_kv4_geom* g, const void* slots, int32_t* status)
+{
+    KvArgs a = {};
+    a.slots = slots; a.rows = g->T * g->H;
+    a.k_ld = g->k_ld; a.k_hs = g->k_hs; a.v_ld = g->v_ld; a.v_hs = g->v_hs;
+    a.n_slots = g->n_pages * g->page; a.H = (int32_t)g->H; a.D = (int32_t)g->D; a.W = kv4_width(g->D); a.page = g->page;
+    a.slot64 = g->slot_dtype == ISEG_I64; a.mode = g->scale_mode; a.status = status;
+    return a;
+}
+
+#define KV_LAUNCH(kernel, LPR)                                                                              \
+    hipLaunchKernelGGL((kernel<T, LPR>), dim3((unsigned)ceil_div64(a.rows, 256 / LPR), 2), dim3(256), 0, s, a)
+
+template <typename T>
+int kv_write(const KvArgs& a, hipStream_t s)
+{
+    if (a.W <= 32) KV_LAUNCH(k_kv4_write, 4);
+    else if (a.W <= 64) KV_LAUNCH(k_kv4_write, 8);
+    else if (a.W <= 128) KV_LAUNCH(k_kv4_write, 16);
+    else KV_LAUNCH(k_kv4_write, 32);
+    return launch_ok();
+}
+
+template <typename T>
+int kv_read(const KvArgs& a, hipStream_t s)
+{
+    if (a.W <= 32) KV_LAUNCH(k_kv4_read, 4);
+    else if (a.W <= 64) KV_LAUNCH(k_kv4_read, 8);
+    else if (a.W <= 128) KV_LAUNCH(k_kv4_read, 16);
+    else KV_LAUNCH(k_kv4_read, 32);
+    return launch_ok();
+}
+
+// ---------------------------------------------------------------------------
+// pages, slots and positions of a step
+// ---------------------------------------------------------------------------
+struct PmArgs {
+    const int32_t *ctx, *count, *free_pages;
+    const int32_t *held, *n_free;
+    int32_t *table, *q_start, *kv_len, *pos, *slots, *held_out, *n_free_out;
+    int32_t *w_held, *w_first, *w_free;       // workspace: pages held before, first page taken, free pages before
+    int64_t T, max_pages, table_ld, F, n_pages;
+    int32_t B, page;
+    int32_t* status;
+};
+
+// inclusive sums of two values over the block's 1024 threads
+__device__ __forceinline__ void scan2_1024(int64_t& x, int64_t& y, int64_t (*red)[16])
+{
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        const int64_t u = __shfl_up(x, o, 64), v = __shfl_up(y, o, 64);
+        if (lane >= o) { x += u; y += v; }
+    }
+    __syncthreads();
+    if (lane == 63) { red[0][w] = x; red[1][w] = y; }
+    __syncthreads();
+    for (int i = 0; i < w; i++) { x += red[0][i]; y += red[1][i]; }
+}
+
+__device__ __forceinline__ int32_t sat31(int64_t v) { return (int32_t)(v < 0x7fffffff ? v : 0x7fffffff); }
+
+// one block: lengths, pages wanted, their sums
+__global__ __launch_bounds__(1024) void k_page_scan(PmArgs a)
+{
+    __shared__ int64_t red[2][16];
+    __shared__ int64_t base[2];
+    int bad = 0;
+    int64_t nf = *a.n_free;
+    if (nf < 0 || nf > a.F) { bad = 1; nf = nf < 0 ? 0 : a.F; }
+    if (threadIdx.x == 0) { base[0] = base[1] = 0; }
+    __syncthreads();
+    for (int32_t b0 = 0; b0 < a.B; b0 += 1024) {
+        const int32_t b = b0 + (int32_t)threadIdx.x;
+        int64_t n = 0, need = 0, first_t, first_p;
+        int32_t held = 0;
+        if (b < a.B) {
+            int64_t c = a.ctx[b];
+            n = a.count[b];
+            held = a.held[b];
+            if (c < 0 || n < 0 || held < 0 || held > a.max_pages) bad = 1;
+            c = c < 0 ? 0 : c;
+            n = n < 0 ? 0 : n;
+            held = held < 0 ? 0 : (held > a.max_pages ? (int32_t)a.max_pages : held);
+            const int64_t kv = c + n;
+            int64_t want = (kv + a.page - 1) / a.page;
+            if (want > a.max_pages) { bad = 1; want = a.max_pages; }
+            need = want > held ? want - held : 0;
+            if (kv > 0x7fffffff) bad = 1;
+            a.kv_len[b] = sat31(kv);
+        }
+        int64_t sn = n, sp = need;
+        scan2_1024(sn, sp, red);
+        first_t = base[0] + sn - n;
+        first_p = base[1] + sp - need;
+        if (b < a.B) {
+            a.q_start[b] = sat31(first_t);
+            a.w_held[b] = held;
+            a.w_first[b] = sat31(first_p);
+            const int64_t got = nf - first_p < 0 ? 0 : (nf - first_p < need ? nf - first_p : need);
+            if (got < need) bad = 1;
+            a.held_out[b] = held + (int32_t)got;
+        }
+        __syncthreads();
+        if (threadIdx.x == 1023) { base[0] += sn; base[1] += sp; }
+        __syncthreads();
+    }
+    if (threadIdx.x == 0) {
+        if (base[0] > a.T) bad = 1;
+        a.q_start[a.B] = sat31(base[0]);
+        *a.w_free = (int32_t)nf;
+        *a.n_free_out = (int32_t)(nf > base[1] ? nf - base[1] : 0);
+    }
+    if (bad) set_status(a.status, ISEG_DEV_RANGE);
+}
+
+// page of column `col` of request b: taken now, or in the table already; -1: none
+__device__ __forceinline__ int32_t page_of(const PmArgs& a, int32_t b, int64_t col, int& bad)
+{
+    if (col >= a.max_pages) { bad = 1; return -1; }
+    const int32_t held = a.w_held[b];
+    int32_t pg = -1;
+    if (col < held) {
+        pg = a.table[(int64_t)b * a.table_ld + col];
+    } else {
+        const int64_t k = (int64_t)*a.w_free - 1 - a.w_first[b] - (col - held);
+        if (k >= 0) pg = a.free_pages[k];
+        else bad = 1;
+    }
+    if (pg < 0 || pg >= a.n_pages) { bad = 1; pg = -1; }
+    return pg;
+}
+
+// request of a row of the step: the last b with q_start[b] <= row
+__device__ __forceinline__ int32_t request_of(const int32_t* start, int32_t B, int64_t row)
+{
+    int32_t lo = 0, hi = B;                       // start[lo] <= row < start[hi]
+    while (hi - lo > 1) {
+        const int32_t mid = lo + (hi - lo) / 2;
+        if (start[mid] <= row) lo = mid;
+        else hi = mid;
+    }
+    return lo;
+}
+
+// a thread per token; the first new token of a page writes its table entry.  A
+// request without new tokens takes no page (its pages hold its context), unless
+// it holds too few: a thread per request adds those.
+__global__ __launch_bounds__(256) void k_page_fill(PmArgs a)
+{
+    const int64_t total = a.q_start[a.B];
+    int bad = 0;
+    for (int64_t r = (int64_t)blockIdx.x * 256 + threadIdx.x; r < a.T; r += (int64_t)gridDim.x * 256) {
+        if (r >= total) {
+            a.pos[r] = 0;
+            a.slots[r] = -1;
+            continue;
+        }
+        const int32_t b = request_of(a.q_start, a.B, r);
+        const int64_t c = a.ctx[b] < 0 ? 0 : a.ctx[b], p = c + (r - a.q_start[b]);
+        const int64_t col = p / a.page;
+        const int32_t pg = page_of(a, b, col, bad), in = (int32_t)(p - col * a.page);
+        a.pos[r] = sat31(p);
+        a.slots[r] = pg < 0 ? -1 : pg * a.page + in;
+    }
+    for (int64_t b = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); b < a.B; b += (int64_t)gridDim.x * 4) {
+        const int64_t c = a.ctx[b] < 0 ? 0 : a.ctx[b], n = a.count[b] < 0 ? 0 : a.count[b];
+        int64_t want = (c + n + a.page - 1) / a.page;
+        if (want > a.max_pages) want = a.max_pages;
+        for (int64_t col = a.w_held[b] + (int64_t)(threadIdx.x & 63); col < want; col += 64)
+            a.table[b * a.table_ld + col] = page_of(a, (int32_t)b, col, bad);
+    }
+    if (bad) set_status(a.status, ISEG_DEV_RANGE);
+}
+
+int pm_check(const iseg_page_map_geom* g)
+{
+    if (!g || g->reserved) return ISEG_ERR_ARG;
+    if (g->B < 0 || g->T < 0 || g->B >= ((int64_t)1 << 31) - 1 || g->T >= (int64_t)1 << 31 || g->max_pages < 0 ||
+        g->table_ld < g->max_pages || g->F < 0 || g->n_pages < 0 || g->page < 1)
+        return ISEG_ERR_SHAPE;
+    if (!kv4_pages_ok(g->n_pages, g->page) || g->max_pages >= (int64_t)1 << 31 || g->F >= (int64_t)1 << 31)
+        return ISEG_ERR_UNSUPPORTED;
+    return ISEG_OK;
+}
+
+}  // namespace
+
+extern "C" int iseg_kv4_write(const void* k, const void* v, const void* slots, const iseg_kv4_geom* g,
+                              uint8_t* k_codes, float* k_scale, uint8_t* v_codes, float* v_scale,
+                              int32_t* dev_status, hipStream_t stream)
+{
+    const int rc = kv_check(g);
+    if (rc != ISEG_OK) return rc;
+    if (g->scale_mode != ISEG_SCALE_MAX && g->scale_mode != ISEG_SCALE_POW2) return ISEG_ERR_ARG;
+    if (g->k_ld < 0 || g->k_hs < 0 || g->v_ld < 0 || g->v_hs < 0) return ISEG_ERR_SHAPE;
+    if (g->T == 0 || g->H == 0) return ISEG_OK;
+    if (!k || !v || !slots || (g->n_pages > 0 && (!k_codes || !k_scale || !v_codes || !v_scale))) return ISEG_ERR_ARG;
+    if (((uintptr_t)k_codes | (uintptr_t)v_codes) & 15) return ISEG_ERR_ARG;
+    KvArgs a = kv_args(g, slots, dev_status);
+    if (ceil_div64(a.rows, 8) >= (int64_t)1 << 24) return ISEG_ERR_UNSUPPORTED;
+    a.k = k; a.v = v; a.kc = k_codes; a.ks = k_scale; a.vc = v_codes; a.vs = v_scale;
+    return g->dtype == ISEG_F32 ? kv_write<float>(a, stream)
+                                : g->dtype == ISEG_F16 ? kv_write<f16_t>(a, stream) : kv_write<bf16_t>(a, stream);
+}
+
+extern "C" int iseg_kv4_read(const uint8_t* k_codes, const float* k_scale, const uint8_t* v_codes,
+                             const float* v_scale, const void* slots, const iseg_kv4_geom* g, void* k, void* v,
+                             int32_t* dev_status, hipStream_t stream)
+{
+    const int rc = kv_check(g);
+    if (rc != ISEG_OK) return rc;
+    if (!rows_apart(g->T, g->H, g->D, g->k_ld, g->k_hs) || !rows_apart(g->T, g->H, g->D, g->v_ld, g->v_hs))
+        return ISEG_ERR_SHAPE;
+    if (g->T == 0 || g->H == 0) return ISEG_OK;
+    if (!k || !v || !slots || (g->n_pages > 0 && (!k_codes || !k_scale || !v_codes || !v_scale))) return ISEG_ERR_ARG;
+    if (((uintptr_t)k_codes | (uintptr_t)v_codes) & 15) return ISEG_ERR_ARG;
+    KvArgs a = kv_args(g, slots, dev_status);
+    if (ceil_div64(a.rows, 8) >= (int64_t)1 << 24) return ISEG_ERR_UNSUPPORTED;
+    a.ko = k; a.vo = v; a.kc = (uint8_t*)k_codes; a.ks = (float*)k_scale; a.vc = (uint8_t*)v_codes;
+    a.vs = (float*)v_scale;
+    return g->dtype == ISEG_F32 ? kv_read<float>(a, stream)
+                                : g->dtype == ISEG_F16 ? kv_read<f16_t>(a, stream) : kv_read<bf16_t>(a, stream);
+}
+
+extern "C" size_t iseg_page_map_ws(const iseg_page_map_geom* g)
+{
+    if (pm_check(g) != ISEG_OK) return 0;
+    return ws_used(align256((size_t)g->B * 4) * 2 + 256);
+}
+
+extern "C" int iseg_page_map(const int32_t* ctx, const int32_t* count, const int32_t* held, const int32_t* free_pages,
+                             const int32_t* n_free, const iseg_page_map_geom* g, int32_t* table, int32_t* q_start,
+                             int32_t* kv_len, int32_t* positions, int32_t* slots, int32_t* held_out,
+                             int32_t* n_free_out, void* ws, size_t ws_bytes, int32_t* dev_status, hipStream_t stream)
+{
+    const int rc = pm_check(g);
+    if (rc != ISEG_OK) return rc;
+    if (!n_free || !n_free_out || !q_start || (g->F > 0 && !free_pages) || (g->T > 0 && (!positions || !slots)))
+        return ISEG_ERR_ARG;
+    if (g->B > 0 && (!ctx || !count || !held || !kv_len || !held_out || (g->max_pages > 0 && !table))) return ISEG_ERR_ARG;
+    if (!ws || ws_bytes < iseg_page_map_ws(g)) return ISEG_ERR_WORKSPACE;
+    PmArgs a = {};
+    a.ctx = ctx; a.count = count; a.held = held; a.free_pages = free_pages; a.n_free = n_free;
+    a.table = table; a.q_start = q_start; a.kv_len = kv_len; a.pos = positions; a.slots = slots;
+    a.held_out = held_out; a.n_free_out = n_free_out;
+    a.w_held = (int32_t*)ws;
+    a.w_first = (int32_t*)((char*)ws + align256((size_t)g->B * 4));
+    a.w_free = (int32_t*)((char*)ws + 2 * align256((size_t)g->B * 4));
+    a.T = g->T; a.max_pages = g->max_pages; a.table_ld = g->table_ld; a.F = g->F; a.n_pages = g->n_pages;
+    a.B = (int32_t)g->B; a.page = g->page; a.status = dev_status;
+    hipLaunchKernelGGL(k_page_scan, dim3(1), dim3(1024), 0, stream, a);
+    if (g->T > 0 || g->B > 0) {
+        const int64_t items = ceil_div64(g->T, 256) > ceil_div64(g->B, 4) ? ceil_div64(g->T, 256) : ceil_div64(g->B, 4);
+        hipLaunchKernelGGL(k_page_fill, dim3((unsigned)(items < 2048 ? items : 2048)), dim3(256), 0, stream, a);
+    }
+    return launch_ok();
+}

@@ -180,6 +180,16 @@ static inline size_t ws_used(size_t bytes) { return bytes > 2 * kNoWs ? align256
 
 static inline bool is_float_dtype(int32_t t) { return t == ISEG_F32 || t == ISEG_F16 || t == ISEG_BF16; }
 
+// whether no two rows of an output [T, H, D] with strides ld and hs overlap
+static inline bool rows_apart(int64_t T, int64_t H, int64_t D, int64_t ld, int64_t hs)
+{
+    if (T < 1 || H < 1) return true;
+    if (ld < 0 || hs < 0 || ld > (int64_t)1 << 40 || hs > (int64_t)1 << 40) return false;
+    if (T > 1 && ld < D) return false;
+    if (H > 1 && hs < D) return false;
+    return T == 1 || H == 1 || ld >= (H - 1) * hs + D || hs >= (T - 1) * ld + D;
+}
+
 // launches walk their rows in a loop, so the grid may be cut at any count
 constexpr int64_t kRowGridMax = 1 << 20;
 

@@ -94,6 +94,13 @@ const Entry kEntries[] = {
     ISEG_TAPE_ENTRY(iseg_linear_i8_bwd)
     ISEG_TAPE_ENTRY(iseg_logprob_fwd)
     ISEG_TAPE_ENTRY(iseg_logprob_bwd)
+    ISEG_TAPE_ENTRY(iseg_page_map)
+    ISEG_TAPE_ENTRY(iseg_qk_norm_rope_fwd)
+    ISEG_TAPE_ENTRY(iseg_qk_norm_rope_bwd)
+    ISEG_TAPE_ENTRY(iseg_kv4_write)
+    ISEG_TAPE_ENTRY(iseg_kv4_read)
+    ISEG_TAPE_ENTRY(iseg_kv4_attention)
+    ISEG_TAPE_ENTRY(iseg_verify_drafts)
     ISEG_TAPE_ENTRY(iseg_profile_arm)
     ISEG_TAPE_ENTRY(iseg_status_clear)
     ISEG_TAPE_ENTRY(iseg_check_codes)

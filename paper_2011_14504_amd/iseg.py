@@ -14,6 +14,7 @@ import functools
 import math
 import os
 import threading
+from typing import NamedTuple
 
 import torch
 
@@ -92,6 +93,34 @@ class LinearBwdGeom(C.Structure):
 class LogprobGeom(C.Structure):
     _fields_ = [(n, C.c_int64) for n in ("M", "V", "ld", "out_ld")] + \
                [(n, C.c_int32) for n in ("dtype", "token_dtype", "top_k", "reserved")]
+
+
+class PageMapGeom(C.Structure):
+    _fields_ = [(n, C.c_int64) for n in ("B", "T", "max_pages", "table_ld", "F", "n_pages")] + \
+               [("page", C.c_int32), ("reserved", C.c_int32)]
+
+
+class QkNormRopeGeom(C.Structure):
+    _fields_ = [(n, C.c_int64) for n in ("T", "Hq", "Hk", "D", "q_ld", "q_hs", "k_ld", "k_hs", "yq_ld", "yq_hs",
+                                         "yk_ld", "yk_hs", "dq_ld", "dq_hs", "dk_ld", "dk_hs")] + \
+               [(n, C.c_int32) for n in ("dtype", "p_dtype", "pos_dtype", "rope_dim", "pairs", "norm")] + \
+               [("eps", C.c_float), ("mscale", C.c_float)]
+
+
+class Kv4Geom(C.Structure):
+    _fields_ = [(n, C.c_int64) for n in ("T", "H", "D", "k_ld", "k_hs", "v_ld", "v_hs", "n_pages")] + \
+               [(n, C.c_int32) for n in ("page", "dtype", "slot_dtype", "scale_mode")]
+
+
+class Kv4AttentionGeom(C.Structure):
+    _fields_ = [(n, C.c_int64) for n in ("T", "B", "Hq", "H", "D", "q_ld", "q_hs", "o_ld", "o_hs", "n_pages",
+                                         "max_pages", "table_ld", "max_q", "max_kv", "window")] + \
+               [("page", C.c_int32), ("dtype", C.c_int32), ("causal", C.c_int32), ("scale", C.c_float)]
+
+
+class VerifyGeom(C.Structure):
+    _fields_ = [(n, C.c_int64) for n in ("B", "S", "V", "t_bs", "t_ld", "d_bs", "d_ld")] + \
+               [("dtype", C.c_int32), ("token_dtype", C.c_int32)]
 
 
 _lib = None
@@ -173,6 +202,17 @@ _SIGS = {
     "iseg_logprob_fwd_ws": ([_P], _SZ),
     "iseg_logprob_fwd": ([_P, _P, _P, _P, _P, _P, _P, _P, _P, _SZ, _P, _P], C.c_int),
     "iseg_logprob_bwd": ([_P, _P, _P, _P, _P, _P, _P, _P, _P, _P], C.c_int),
+    "iseg_page_map_ws": ([_P], _SZ),
+    "iseg_page_map": ([_P] * 14 + [_SZ, _P, _P], C.c_int),
+    "iseg_qk_norm_rope_fwd": ([_P] * 11, C.c_int),
+    "iseg_qk_norm_rope_bwd_ws": ([_P], _SZ),
+    "iseg_qk_norm_rope_bwd": ([_P] * 14 + [_SZ, _P], C.c_int),
+    "iseg_kv4_write": ([_P] * 10, C.c_int),
+    "iseg_kv4_read": ([_P] * 10, C.c_int),
+    "iseg_kv4_attention_ws": ([_P], _SZ),
+    "iseg_kv4_attention": ([_P] * 12 + [_SZ, _P, _P], C.c_int),
+    "iseg_verify_drafts_ws": ([_P], _SZ),
+    "iseg_verify_drafts": ([_P] * 10 + [_SZ, _P, _P], C.c_int),
     "iseg_philox4x32_10": ([_P, _P, _P], None),
     "iseg_profile_arm": ([_I32, _P, _P], C.c_int),
     "iseg_conv_last_plan": ([], C.c_char_p),
@@ -558,6 +598,54 @@ def iseg_logprob_bwd(logits, tokens, lse, entropy, g_logprob, g_entropy, geom, d
     rc = lib().iseg_logprob_bwd(_ptr(logits), _ptr(tokens), _ptr(lse), _ptr(entropy), _ptr(g_logprob),
                                 _ptr(g_entropy), C.byref(geom), _ptr(dlogits), _ptr(status), _stream())
     _check(rc, "iseg_logprob_bwd")
+
+
+def iseg_page_map(ctx, count, held, free_pages, n_free, geom, table, q_start, kv_len, positions, slots, held_out,
+                  n_free_out, ws, status=None):
+    rc = lib().iseg_page_map(_ptr(ctx), _ptr(count), _ptr(held), _ptr(free_pages), _ptr(n_free), C.byref(geom),
+                             _ptr(table), _ptr(q_start), _ptr(kv_len), _ptr(positions), _ptr(slots), _ptr(held_out),
+                             _ptr(n_free_out), *_ws_tuple(ws), _ptr(status), _stream())
+    _check(rc, "iseg_page_map")
+
+
+def iseg_qk_norm_rope_fwd(q, k, positions, inv_freq, gamma_q, gamma_k, geom, yq, yk, status=None):
+    rc = lib().iseg_qk_norm_rope_fwd(_ptr(q), _ptr(k), _ptr(positions), _ptr(inv_freq), _ptr(gamma_q), _ptr(gamma_k),
+                                     C.byref(geom), _ptr(yq), _ptr(yk), _ptr(status), _stream())
+    _check(rc, "iseg_qk_norm_rope_fwd")
+
+
+def iseg_qk_norm_rope_bwd(dyq, dyk, q, k, positions, inv_freq, gamma_q, gamma_k, geom, dq, dk, dgamma_q, dgamma_k,
+                          ws):
+    rc = lib().iseg_qk_norm_rope_bwd(_ptr(dyq), _ptr(dyk), _ptr(q), _ptr(k), _ptr(positions), _ptr(inv_freq),
+                                     _ptr(gamma_q), _ptr(gamma_k), C.byref(geom), _ptr(dq), _ptr(dk), _ptr(dgamma_q),
+                                     _ptr(dgamma_k), *_ws_tuple(ws), _stream())
+    _check(rc, "iseg_qk_norm_rope_bwd")
+
+
+def iseg_kv4_write(k, v, slots, geom, k_codes, k_scale, v_codes, v_scale, status=None):
+    rc = lib().iseg_kv4_write(_ptr(k), _ptr(v), _ptr(slots), C.byref(geom), _ptr(k_codes), _ptr(k_scale),
+                              _ptr(v_codes), _ptr(v_scale), _ptr(status), _stream())
+    _check(rc, "iseg_kv4_write")
+
+
+def iseg_kv4_read(k_codes, k_scale, v_codes, v_scale, slots, geom, k, v, status=None):
+    rc = lib().iseg_kv4_read(_ptr(k_codes), _ptr(k_scale), _ptr(v_codes), _ptr(v_scale), _ptr(slots), C.byref(geom),
+                             _ptr(k), _ptr(v), _ptr(status), _stream())
+    _check(rc, "iseg_kv4_read")
+
+
+def iseg_kv4_attention(q, k_codes, k_scale, v_codes, v_scale, table, q_start, kv_len, geom, out, lse, ws,
+                       status=None):
+    rc = lib().iseg_kv4_attention(_ptr(q), _ptr(k_codes), _ptr(k_scale), _ptr(v_codes), _ptr(v_scale), _ptr(table),
+                                  _ptr(q_start), _ptr(kv_len), C.byref(geom), _ptr(out), _ptr(lse), *_ws_tuple(ws),
+                                  _ptr(status), _stream())
+    _check(rc, "iseg_kv4_attention")
+
+
+def iseg_verify_drafts(target, draft, tokens, n_draft, u, u_sample, geom, out, accepted, ws, status=None):
+    rc = lib().iseg_verify_drafts(_ptr(target), _ptr(draft), _ptr(tokens), _ptr(n_draft), _ptr(u), _ptr(u_sample),
+                                  C.byref(geom), _ptr(out), _ptr(accepted), *_ws_tuple(ws), _ptr(status), _stream())
+    _check(rc, "iseg_verify_drafts")
 
 
 def iseg_philox4x32_10(ctr, key):
@@ -1676,3 +1764,386 @@ def logprob_bwd(logits, tokens, lse, entropy, g_logprob=None, g_entropy=None, st
     g, _ = _logprob_geom(M, V, ld, V, dt, td, 0)
     iseg_logprob_bwd(lr, tokens, lse, entropy, g_logprob, g_entropy, g, dx, status)
     return dx
+
+
+# --------------------------------------------------------------------------
+# a serving step over a cache held in 4 bits
+# --------------------------------------------------------------------------
+# Head tensors are [T, H, D] with any strides between tokens and heads (slices
+# of one projection's rows serve as they are); only their last dimension has to
+# be dense, or they are copied first.
+def _heads(t, what, D=None):
+    """(tensor, token stride, head stride) of a [T, H, D] tensor with dense heads."""
+    if t.dim() != 3 or (D is not None and t.shape[2] != D):
+        raise ValueError(f"{what}: [tokens, heads, {'D' if D is None else D}] expected")
+    if t.shape[2] > 1 and t.stride(2) != 1:
+        if _REC is not None:
+            raise IsegError(f"{what}: a recorded call needs dense heads")
+        t = t.contiguous()
+    return t, t.stride(0), t.stride(1)
+
+
+def _ints(t, n, x, what, dtypes=(torch.int32,)):
+    """A dense vector of n whole numbers beside x."""
+    if not isinstance(t, torch.Tensor) or t.dtype not in dtypes or t.numel() != n or t.get_device() != x.get_device():
+        names = " or ".join(str(d)[6:] for d in dtypes)
+        raise ValueError(f"{what}: {n} elements of {names} on {x.device} expected")
+    if t.is_contiguous():
+        return t
+    if _REC is not None:
+        raise IsegError(f"{what}: a recorded call needs a dense vector")
+    return t.contiguous()
+
+
+_INTS = (torch.int32, torch.int64)
+
+
+@functools.lru_cache(maxsize=256)
+def _page_map_geom(B, T, max_pages, table_ld, F, n_pages, page):
+    g = PageMapGeom(B, T, max_pages, table_ld, F, n_pages, page, 0)
+    return g, lib().iseg_page_map_ws(C.byref(g))
+
+
+@_on_device
+def page_map(ctx, count, table, held, free_pages, n_free, page, n_pages, n_tokens, in_place=False, status=None):
+    """The step's pages, slots and positions from the requests' lengths (all
+    int32): (q_start [B + 1], kv_len [B], positions [n_tokens], slots
+    [n_tokens], held [B], n_free [1]).  ctx and count [B]: tokens before the
+    step and new ones; table [B, max_pages], which gets the pages taken from
+    the end of free_pages; held [B]: pages of each request so far.  n_tokens:
+    rows of the step, at least sum(count).  in_place: held and n_free are
+    updated and returned themselves, as a captured step wants it."""
+    if not isinstance(ctx, torch.Tensor) or ctx.dim() != 1:
+        raise ValueError("ctx: a vector of int32 expected")
+    B = ctx.numel()
+    if table.dim() != 2 or table.dtype != torch.int32 or table.shape[0] != B or (table.shape[1] > 1 and table.stride(1) != 1) or \
+            (B > 1 and table.stride(0) < table.shape[1]):
+        raise ValueError("table: int32 [requests, pages] with dense rows expected")
+    if page < 1 or n_pages < 0 or n_tokens < 0:
+        raise ValueError("page, n_pages, n_tokens: sizes expected")
+    if n_pages * page > 1 << 31:
+        raise ValueError("n_pages: slots of 32 bits expected")
+    _gpu(ctx, table, status=status)
+    if in_place and not (held.is_contiguous() and n_free.is_contiguous()):
+        raise ValueError("in_place: dense held and n_free expected")
+    ctx, count, held = _ints(ctx, B, ctx, "ctx"), _ints(count, B, ctx, "count"), _ints(held, B, ctx, "held")
+    F = free_pages.numel()
+    free_pages, n_free = _ints(free_pages, F, ctx, "free_pages"), _ints(n_free, 1, ctx, "n_free")
+    new = functools.partial(torch.empty, dtype=torch.int32, device=ctx.device)
+    q_start, kv_len, positions, slots = new(B + 1), new(B), new(n_tokens), new(n_tokens)
+    held_out, n_free_out = (held, n_free) if in_place else (new(B), new(1))
+    g, wsb = _page_map_geom(B, n_tokens, table.shape[1], table.stride(0) if B > 1 else max(table.shape[1], 1), F, n_pages, page)
+    iseg_page_map(ctx, count, held, free_pages, n_free, g, table, q_start, kv_len, positions, slots, held_out,
+                  n_free_out, _scratch(ctx, wsb), status)
+    return q_start, kv_len, positions, slots, held_out, n_free_out
+
+
+def rope_frequencies(rope_dim, base=10000.0, factor=1.0, stretch=None, device="cuda"):
+    """inv_freq [rope_dim / 2] float32 of qk_norm_rope_fwd: base^(-2 i / rope_dim).
+    For contexts `factor` times as long as those trained on, positions are
+    interpolated: every frequency over factor, or, with stretch = (length, slow,
+    fast), only those that turn less than `slow` times within the trained
+    length; those of more than `fast` turns stay, the ones between blend
+    linearly in their turns."""
+    if rope_dim < 2 or rope_dim % 2 or not base > 0 or not factor > 0:
+        raise ValueError("rope_dim: even and positive, base and factor: positive expected")
+    f = torch.pow(torch.tensor(float(base), dtype=torch.float64), -torch.arange(0, rope_dim, 2, dtype=torch.float64) / rope_dim)
+    keep = torch.zeros_like(f)
+    if stretch is not None:
+        length, slow, fast = stretch
+        if not (length > 0 and fast > slow >= 0):
+            raise ValueError("stretch: (trained length, slow, fast) turns with fast > slow expected")
+        keep = ((length * f / (2 * math.pi) - slow) / (fast - slow)).clamp(0, 1)
+    return (f * keep + f / factor * (1 - keep)).float().to(device)
+
+
+def _rope_args(q, k, positions, inv_freq, gamma_q, gamma_k, norm):
+    if q is None and k is None:
+        raise ValueError("q or k expected")
+    x = q if q is not None else k
+    if not isinstance(x, torch.Tensor) or x.dim() != 3:
+        raise ValueError("q: [tokens, heads, D] expected")
+    dt, T, D = _float_code(x, "q"), x.shape[0], x.shape[2]
+    if D < 1 or D > 512:
+        raise ValueError("q: heads of 1 to 512 elements expected")
+    if k is not None and (k.dim() != 3 or k.dtype != x.dtype or k.shape[0] != T or k.shape[2] != D):
+        raise ValueError("k: q's tokens, head size and type expected")
+    n = inv_freq.numel() if inv_freq is not None else 0
+    if 2 * n > D:
+        raise ValueError("inv_freq: at most half a head's elements expected")
+    inv_freq = _vec(inv_freq, n, torch.float32, x, "inv_freq")
+    if n:
+        positions = _ints(positions, T, x, "positions", _INTS)
+    p = gamma_q if gamma_q is not None else gamma_k
+    if p is not None and not norm:
+        raise ValueError("gamma: norm expected")
+    pd = _float_code(p, "gamma") if p is not None else dt
+    pt = p.dtype if p is not None else x.dtype
+    gamma_q, gamma_k = _vec(gamma_q, D, pt, x, "gamma_q"), _vec(gamma_k, D, pt, x, "gamma_k")
+    pos64 = ISEG_I64 if n and positions.dtype == torch.int64 else ISEG_I32
+    return x, T, D, dt, pd, pt, 2 * n, positions if n else None, pos64, inv_freq if n else None, gamma_q, gamma_k
+
+
+@functools.lru_cache(maxsize=256)
+def _rope_geom(*a):
+    g = QkNormRopeGeom(*a)
+    return g, lib().iseg_qk_norm_rope_bwd_ws(C.byref(g))
+
+
+def _dense_like(t):
+    return None if t is None else torch.empty(t.shape, dtype=t.dtype, device=t.device)
+
+
+def _hd(t):
+    return 0 if t is None else t.shape[1]
+
+
+@_on_device
+def qk_norm_rope_fwd(q, k, positions, inv_freq, gamma_q=None, gamma_k=None, eps=1e-6, pairs=False, norm=True,
+                     mscale=1.0, in_place=False, status=None):
+    """Norm of every head of q [T, Hq, D] and k [T, Hk, D] (x gamma / sqrt(mean
+    x^2 + eps); not without norm) and the rotation of its first 2 len(inv_freq)
+    elements by positions [T]: (yq, yk).  pairs: neighbours rotate together
+    instead of halves.  Either of q and k may be None, inv_freq None for the norm
+    alone; in_place writes to q and k themselves."""
+    x, T, D, dt, pd, _, R, positions, pos64, inv_freq, gamma_q, gamma_k = _rope_args(q, k, positions, inv_freq, gamma_q, gamma_k, norm)
+    if not (eps >= 0 and math.isfinite(eps) and math.isfinite(mscale)):
+        raise ValueError("eps, mscale: finite, eps not negative expected")
+    _gpu(x, k, status=status)
+    s = []
+    ins = []
+    for t, what in ((q, "q"), (k, "k")):
+        if t is None:
+            ins.append(None)
+            s += (0, 0)
+            continue
+        if in_place and D > 1 and t.stride(2) != 1:
+            raise ValueError(f"{what}: dense heads expected for in_place")
+        t, ld, hs = _heads(t, what)
+        ins.append(t)
+        s += (ld, hs)
+    yq, yk = ins if in_place else (_dense_like(q), _dense_like(k))
+    o = s if in_place else [_hd(q) * D, D, _hd(k) * D, D]
+    g, _ = _rope_geom(T, _hd(q), _hd(k), D, *s, *o, 0, 0, 0, 0, dt, pd, pos64, R, int(pairs), int(norm), eps, mscale)
+    iseg_qk_norm_rope_fwd(ins[0], ins[1], positions, inv_freq, gamma_q, gamma_k, g, yq, yk, status)
+    return yq, yk
+
+
+@_on_device
+def qk_norm_rope_bwd(dyq, dyk, q, k, positions, inv_freq, gamma_q=None, gamma_k=None, eps=1e-6, pairs=False,
+                     norm=True, mscale=1.0, want_params=True):
+    """(dq, dk, dgamma_q, dgamma_k) of qk_norm_rope_fwd, the last two of gamma's
+    type (q's without gamma), None without norm or want_params."""
+    x, T, D, dt, pd, pt, R, positions, pos64, inv_freq, gamma_q, gamma_k = _rope_args(q, k, positions, inv_freq, gamma_q, gamma_k, norm)
+    if not (eps >= 0 and math.isfinite(eps) and math.isfinite(mscale)):
+        raise ValueError("eps, mscale: finite, eps not negative expected")
+    s, ds, ins, grads = [], [], [], []
+    for t, d, what in ((q, dyq, "q"), (k, dyk, "k")):
+        if t is None:
+            ins.append(None)
+            grads.append(None)
+            s += (0, 0)
+            ds += (0, 0)
+            continue
+        if d is None or d.shape != t.shape or d.dtype != t.dtype:
+            raise ValueError(f"dy{what}: {what}'s shape and type expected")
+        t, ld, hs = _heads(t, what)
+        d, dld, dhs = _heads(d, "dy" + what)
+        ins.append(t)
+        grads.append(d)
+        s += (ld, hs)
+        ds += (dld, dhs)
+    _gpu(x, k, dyq, dyk)
+    dq, dk = _dense_like(q), _dense_like(k)
+    want = want_params and norm
+    dgq = torch.empty(D, dtype=pt, device=x.device) if want and q is not None else None
+    dgk = torch.empty(D, dtype=pt, device=x.device) if want and k is not None else None
+    g, wsb = _rope_geom(T, _hd(q), _hd(k), D, *s, *ds, _hd(q) * D, D, _hd(k) * D, D, dt, pd, pos64, R, int(pairs), int(norm), eps, mscale)
+    iseg_qk_norm_rope_bwd(grads[0], grads[1], ins[0], ins[1], positions, inv_freq, gamma_q, gamma_k, g, dq, dk, dgq, dgk,
+                          _scratch(x, wsb))
+    return dq, dk, dgq, dgk
+
+
+class Kv4Cache(NamedTuple):
+    """Keys and values of n_pages pages in 4 bits (the layout of iseg.h)."""
+    k: torch.Tensor                # [n_pages, H, page, W / 2] uint8
+    k_scale: torch.Tensor          # [n_pages, H, page] float32
+    v: torch.Tensor                # [n_pages, H, page / 16, 8 W] uint8
+    v_scale: torch.Tensor          # [n_pages, H, page] float32
+
+
+def _kv4_width(D):
+    return (D + 31) // 32 * 32 if D <= 128 else (D + 63) // 64 * 64
+
+
+def kv4_cache(n_pages, heads, dim, page=64, device="cuda"):
+    """A cache of zeros."""
+    if n_pages < 0 or heads < 1 or not 1 <= dim <= 256 or page < 16 or page % 16 or page > 8192:
+        raise ValueError("kv4_cache: heads >= 1, dim of 1 to 256, page a multiple of 16 up to 8192 expected")
+    if n_pages * page > 1 << 31:
+        raise ValueError("n_pages: slots of 32 bits expected")
+    W = _kv4_width(dim)
+    one = functools.partial(torch.ones, n_pages, heads, page, device=device)
+    return Kv4Cache(torch.full((n_pages, heads, page, W // 2), 136, dtype=torch.uint8, device=device), one(),
+                    torch.full((n_pages, heads, page // 16, 8 * W), 136, dtype=torch.uint8, device=device), one())
+
+
+def _kv4_check(cache, D, x):
+    """(tensors, n_pages, heads, page) of a cache for heads of D elements beside x."""
+    k, ks, v, vs = cache
+    if not 1 <= D <= 256:
+        raise ValueError("heads of 1 to 256 elements expected")
+    W = _kv4_width(D)
+    if k.dim() != 4 or k.shape[3] * 2 != W:
+        raise ValueError(f"cache: rows of {W // 2} bytes expected for heads of {D} elements")
+    P, H, page, _ = k.shape
+    if k.dtype != torch.uint8 or v.dtype != torch.uint8 or ks.dtype != torch.float32 or vs.dtype != torch.float32 or \
+            page < 16 or page % 16 or page > 8192 or tuple(v.shape) != (P, H, page // 16, 8 * W) or \
+            tuple(ks.shape) != (P, H, page) or tuple(vs.shape) != (P, H, page):
+        raise ValueError("cache: the four tensors of kv4_cache expected")
+    if not (k.is_contiguous() and v.is_contiguous() and ks.is_contiguous() and vs.is_contiguous()):
+        raise ValueError("cache: dense tensors expected")
+    if (k.data_ptr() | v.data_ptr() | ks.data_ptr() | vs.data_ptr()) & 15:
+        raise ValueError("cache: tensors at multiples of 16 bytes expected")
+    if P * page > 1 << 31:
+        raise ValueError("cache: slots of 32 bits expected")
+    _gpu(x, k, ks, v, vs)
+    return P, H, page
+
+
+@functools.lru_cache(maxsize=256)
+def _kv4_geom(*a):
+    return Kv4Geom(*a)
+
+
+@_on_device
+def kv4_write(k, v, slots, cache, scale_mode=ISEG_SCALE_MAX, status=None):
+    """Keys and values [T, H, D] of tokens into their slots [T] (int32 or int64;
+    negative ones are skipped) of a Kv4Cache."""
+    dt = _float_code(k, "k")
+    if v.shape != k.shape or v.dtype != k.dtype:
+        raise ValueError("v: k's shape and type expected")
+    if scale_mode not in (ISEG_SCALE_MAX, ISEG_SCALE_POW2):
+        raise ValueError("scale_mode: ISEG_SCALE_MAX or ISEG_SCALE_POW2 expected")
+    k, k_ld, k_hs = _heads(k, "k")
+    v, v_ld, v_hs = _heads(v, "v")
+    T, H, D = k.shape
+    slots = _ints(slots, T, k, "slots", _INTS)
+    _gpu(k, v, status=status)
+    P, Hc, page = _kv4_check(cache, D, k)
+    if H != Hc:
+        raise ValueError("k: the cache's heads expected")
+    g = _kv4_geom(T, H, D, k_ld, k_hs, v_ld, v_hs, P, page, dt, ISEG_I64 if slots.dtype == torch.int64 else ISEG_I32, scale_mode)
+    iseg_kv4_write(k, v, slots, g, *cache, status)
+
+
+@_on_device
+def kv4_read(slots, cache, dim=None, dtype=torch.float32, status=None):
+    """(k, v), each [T, H, dim] of dtype: the values at slots [T], zeros for
+    negative ones.  dim: elements of a head (the cache's stored width without)."""
+    if not isinstance(slots, torch.Tensor) or slots.dtype not in _INTS or slots.dim() != 1:
+        raise ValueError("slots: a vector of int32 or int64 expected")
+    dt = _float_code(dtype, "dtype")
+    D = cache[0].shape[-1] * 2 if dim is None else dim
+    P, H, page = _kv4_check(cache, D, slots)
+    T = slots.numel()
+    slots = _ints(slots, T, slots, "slots", _INTS)
+    _gpu(slots, status=status)
+    k = torch.empty(T, H, D, dtype=dtype, device=slots.device)
+    v = torch.empty_like(k)
+    g = _kv4_geom(T, H, D, H * D, D, H * D, D, P, page, dt, ISEG_I64 if slots.dtype == torch.int64 else ISEG_I32, 0)
+    iseg_kv4_read(*cache, slots, g, k, v, status)
+    return k, v
+
+
+@functools.lru_cache(maxsize=256)
+def _kv4_attention_geom(*a):
+    g = Kv4AttentionGeom(*a)
+    return g, lib().iseg_kv4_attention_ws(C.byref(g))
+
+
+@_on_device
+def kv4_attention(q, cache, table, q_start, kv_len, scale=None, causal=True, window=0, max_q=0, max_kv=0,
+                  want_lse=True, out=None, status=None):
+    """Attention of q [T, Hq, D], the new tokens of B requests one after the
+    other (q_start [B + 1]), over the kv_len [B] tokens that each has in a
+    Kv4Cache under table [B, pages]: (out like q, lse float32 [T, Hq], None
+    without want_lse).  A request's queries are its last tokens; causal: each sees
+    no key after its own, window > 0: only that many up to its own.  max_q, max_kv:
+    bounds of the requests' new and cached tokens, where the caller has them (0:
+    T and all of table).  scale: 1 / sqrt(D) without.  Rows of no request keep
+    what `out` holds; there lse is unspecified."""
+    dt = _float_code(q, "q")
+    q, q_ld, q_hs = _heads(q, "q")
+    T, Hq, D = q.shape
+    if D % 8 or D > 256 or D < 1:
+        raise ValueError("q: heads of a multiple of 8 up to 256 elements expected")
+    P, H, page = _kv4_check(cache, D, q)
+    if Hq < 1 or Hq % H:
+        raise ValueError("q: a multiple of the cache's heads expected")
+    if table.dim() != 2 or table.dtype != torch.int32 or (table.shape[1] > 1 and table.stride(1) != 1) or \
+            (table.shape[0] > 1 and table.stride(0) < table.shape[1]):
+        raise ValueError("table: int32 [requests, pages] with dense rows expected")
+    B = table.shape[0]
+    q_start, kv_len = _ints(q_start, B + 1, q, "q_start"), _ints(kv_len, B, q, "kv_len")
+    scale = 1 / math.sqrt(D) if scale is None else scale
+    if not (scale > 0 and math.isfinite(scale)):
+        raise ValueError("scale: positive and finite expected")
+    if window < 0 or max_q < 0 or max_kv < 0:
+        raise ValueError("window, max_q, max_kv: not negative expected")
+    _gpu(q, table, status=status)
+    if out is None:
+        out = torch.empty(T, Hq, D, dtype=q.dtype, device=q.device)
+    elif out.shape != q.shape or out.dtype != q.dtype or out.get_device() != q.get_device() or (D > 1 and out.stride(2) != 1):
+        raise ValueError("out: q's shape and type with dense heads expected")
+    lse = torch.empty(T, Hq, dtype=torch.float32, device=q.device) if want_lse else None
+    g, wsb = _kv4_attention_geom(T, B, Hq, H, D, q_ld, q_hs, out.stride(0), out.stride(1), P, table.shape[1],
+                                 table.stride(0) if B > 1 else max(table.shape[1], 1), max_q, max_kv, window, page, dt, int(causal), scale)
+    if wsb == 0:
+        raise ValueError("kv4_attention: sizes beyond one launch")
+    iseg_kv4_attention(q, *cache, table, q_start, kv_len, g, out, lse, _scratch(q, wsb), status)
+    return out, lse
+
+
+@functools.lru_cache(maxsize=256)
+def _verify_geom(*a):
+    g = VerifyGeom(*a)
+    return g, lib().iseg_verify_drafts_ws(C.byref(g))
+
+
+def _distributions(t, what):
+    if t.shape[2] > 1 and t.stride(2) != 1:
+        if _REC is not None:
+            raise IsegError(f"{what}: a recorded call needs dense rows")
+        t = t.contiguous()
+    return t, t.stride(0), t.stride(1)
+
+
+@_on_device
+def verify_drafts(target, draft, tokens, n_draft, u, u_sample, status=None):
+    """Drafted tokens [B, S] against the target's probabilities [B, S + 1, V] and
+    those they were drawn from, draft [B, S, V] (None: each was certain): (out
+    [B, S + 1] int32, the accepted tokens, one more, then -1; accepted [B]
+    int32).  n_draft [B] int32: drafts of each request; u [B, S] and u_sample
+    [B] float32: uniform random numbers of [0, 1)."""
+    dt = _float_code(target, "target")
+    if target.dim() != 3 or target.shape[1] < 1 or target.shape[2] < 1:
+        raise ValueError("target: [requests, drafts + 1, tokens] expected")
+    B, S, V = target.shape[0], target.shape[1] - 1, target.shape[2]
+    if draft is not None and (draft.dtype != target.dtype or tuple(draft.shape) != (B, S, V)):
+        raise ValueError("draft: target's type and one row less expected")
+    target, t_bs, t_ld = _distributions(target, "target")
+    d_bs = d_ld = 0
+    if draft is not None:
+        draft, d_bs, d_ld = _distributions(draft, "draft")
+    if tokens.shape != (B, S) or u.shape != (B, S):
+        raise ValueError("tokens, u: [requests, drafts] expected")
+    tokens = _ints(tokens, B * S, target, "tokens", _INTS)
+    n_draft = _ints(n_draft, B, target, "n_draft")
+    u, u_sample = _vec(u, B * S, torch.float32, target, "u"), _vec(u_sample, B, torch.float32, target, "u_sample")
+    _gpu(target, draft, status=status)
+    out = torch.empty(B, S + 1, dtype=torch.int32, device=target.device)
+    accepted = torch.empty(B, dtype=torch.int32, device=target.device)
+    g, wsb = _verify_geom(B, S, V, t_bs, t_ld, d_bs, d_ld, dt, ISEG_I64 if tokens.dtype == torch.int64 else ISEG_I32)
+    iseg_verify_drafts(target, draft, tokens, n_draft, u, u_sample, g, out, accepted, _scratch(target, wsb), status)
+    return out, accepted
