@@ -22,6 +22,7 @@ typedef float f4_t __attribute__((ext_vector_type(4)));
 
 constexpr float kNone = -3.0e38f;        // maximum of a row that has seen no key
 constexpr float kRoom = 8.f;             // scores may pass the running maximum by 2^8
+constexpr int kSplitsMax = 128;
 
 struct KaArgs {
     const void* q;
@@ -34,6 +35,7 @@ struct KaArgs {
     uint64_t p16_inv;                    // 2^36 / p16, rounded up
     int32_t B, Hq, H, G, D, W, p16;      // p16: tiles of 16 tokens of a page
     int32_t splits, tiles, dtype, causal;
+    int32_t join_rows;                   // rows of a tile that may be there
     int32_t rows_min, rows_max;          // rows of the requests that this launch takes: (min, max]
     float scale;                         // times log2 e
     int32_t* status;
@@ -142,12 +144,43 @@ __device__ __forceinline__ void ka_span(const KaArgs& a, const KaSeq& s, int64_t
     lo = lo < 0 ? 0 : lo;
 }
 
-template <int NC>
-struct KaKeys {                          // 32 keys of one head: a lane's words and scales
-    uint32_t k[2][NC], v[2][NC];
-    f4_t ks[2], vs[2];
-    bool ok[2];
-};
+// four elements of an output row from d on: o / l, zeros for a row without keys
+__device__ __forceinline__ void ka_store(const KaArgs& a, int64_t tok, int64_t head, int d, f4_t o, float l)
+{
+    const float inv = l > 0.f ? 1.f / l : (l == l ? 0.f : l);
+    const int64_t at = tok * a.o_ld + head * a.o_hs + d;
+    o *= inv;
+    if (a.dtype == ISEG_F32) {
+        __builtin_memcpy((float*)a.out + at, &o, 16);
+    } else if (a.dtype == ISEG_F16) {
+        _Float16 x[4] = {(_Float16)o[0], (_Float16)o[1], (_Float16)o[2], (_Float16)o[3]};
+        __builtin_memcpy((_Float16*)a.out + at, x, 8);
+    } else {
+        __bf16 x[4] = {(__bf16)o[0], (__bf16)o[1], (__bf16)o[2], (__bf16)o[3]};
+        __builtin_memcpy((__bf16*)a.out + at, x, 8);
+    }
+}
+
+__device__ __forceinline__ float ka_lse(float m, float l)
+{
+    return l > 0.f || l != l ? (m + __builtin_amdgcn_logf(l)) * 0.69314718f : -__builtin_inff();
+}
+
+// four elements of row `r` of a tile from d on: the whole, or a split's part
+template <int TR>
+__device__ __forceinline__ void ka_put(const KaArgs& a, const KaSeq& s, int tile, int h, int split, int64_t row0, int r, int d, f4_t o,
+                                       float m, float l)
+{
+    if (a.splits > 1) {
+        const int64_t at = (((int64_t)tile * a.H + h) * TR + r) * a.splits + split;
+        *(f4_t*)(a.po + at * a.W + d) = o;
+        if (d == 0) { a.pm[at * 2] = m; a.pm[at * 2 + 1] = l; }
+        return;
+    }
+    const int64_t tok = s.q0 + (row0 + r) / a.G, head = h * a.G + (row0 + r) % a.G;
+    if (d < a.D) ka_store(a, tok, head, d, o, l);
+    if (d == 0 && a.lse) a.lse[tok * a.Hq + head] = ka_lse(m, l);
+}
 
 template <int NC>
 __device__ __forceinline__ void words(const uint8_t* p, uint32_t* w)
@@ -155,180 +188,118 @@ __device__ __forceinline__ void words(const uint8_t* p, uint32_t* w)
     __builtin_memcpy(w, __builtin_assume_aligned(p, NC % 4 == 0 ? 16 : NC % 2 == 0 ? 8 : 4), NC * 4);
 }
 
-// NC: words of a row's quarter (W / 32).  R: tiles of 16 rows a wave holds.
-// SHARED: the four waves hold the same rows and deal the keys among themselves;
-// otherwise each has rows of its own and sees all keys.  WIDE: q and p as two
-// float16 terms (float32 tensors).
-template <int NC, int R, bool SHARED, bool WIDE>
-__global__ __launch_bounds__(256) void k_kv4_attention(KaArgs a)
-{
-    constexpr int W = NC * 32, TR = SHARED ? 16 * R : 64 * R, NS = WIDE ? 2 : 1;
-    __shared__ float so[SHARED ? 4 * 16 * (W + 4) : 1];
-    __shared__ float sm[4][16], sl[4][16];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int c = lane & 15, g4 = lane >> 4;
-    const int h = blockIdx.x % a.H, split = (blockIdx.x / a.H) % a.splits, tile = blockIdx.x / a.H / a.splits;
-    int bad = 0;
-    KaSeq s;
-    int64_t b, row0;
-    const bool have = ka_tile<TR, SHARED>(a, tile, s, b, row0, bad);
-    if (bad) set_status(a.status, ISEG_DEV_RANGE);
-    if (!have) return;
-    const int64_t rows = s.n * a.G;
-    if (!SHARED) row0 += wave * 16 * R;
-
-    // the wave's rows: keys they see, and their queries as B operands
-    int64_t lo[R], hi[R];
-    h8_t qf[NS][R][NC];
-    float cf[R];
-#pragma unroll
-    for (int t = 0; t < R; t++) {
-        const int64_t r = row0 + t * 16 + c;
-        const bool in = r < rows;
-        lo[t] = hi[t] = 0;
-        if (in) ka_span(a, s, r, lo[t], hi[t]);
-        const int64_t at = in ? (s.q0 + r / a.G) * a.q_ld + (h * a.G + r % a.G) * a.q_hs : 0;
-        float f[NC][8];
-        float big = 0.f;
-#pragma unroll
-        for (int w = 0; w < NC; w++) {
-            const int d = g4 * 8 * NC + w * 8;
-#pragma unroll
-            for (int i = 0; i < 8; i++) f[w][i] = 0.f;
-            if (in && d < a.D) {
-                if (WIDE) {
-                    float x[8];
-                    __builtin_memcpy(x, (const float*)a.q + at + d, 32);
-#pragma unroll
-                    for (int i = 0; i < 8; i++) f[w][i] = x[i];
-                } else if (a.dtype == ISEG_F16) {
-                    _Float16 x[8];
-                    __builtin_memcpy(x, (const _Float16*)a.q + at + d, 16);
-#pragma unroll
-                    for (int i = 0; i < 8; i++) f[w][i] = (float)x[i];
-                } else {
-                    __bf16 x[8];
-                    __builtin_memcpy(x, (const __bf16*)a.q + at + d, 16);
-#pragma unroll
-                    for (int i = 0; i < 8; i++) f[w][i] = (float)x[i];
-                }
-            }
-#pragma unroll
-            for (int i = 0; i < 8; i++) big = fmaxf(big, fabsf(f[w][i]));
-        }
-        // float16 reaches no further than 65504 and 2^-24: rows of the other
-        // types are brought below 1 by a power of two first
-        int e = 0;
-        if (WIDE || a.dtype != ISEG_F16) {
-            big = max4(big);
-            if (big > 0.f && big <= 3.4028234e38f) (void)frexpf(big, &e);
-            e = e < -100 ? -100 : e;
-        }
-        cf[t] = fmaxf(ldexpf(a.scale, e), 1.17549435e-38f);      // never 0: a masked score is -infinity times this
-#pragma unroll
-        for (int w = 0; w < NC; w++)
-#pragma unroll
-            for (int i = 0; i < 8; i++) {
-                const float x = ldexpf(f[w][i], -e);
-                qf[0][t][w][i] = (_Float16)x;
-                if constexpr (WIDE) qf[NS - 1][t][w][i] = (_Float16)(x - (float)(_Float16)x);
-            }
-    }
-
-    // keys of the block (SHARED) or the wave: whole steps, dealt to the splits
-    const int64_t r_end = row0 + 16 * R < rows ? row0 + 16 * R : rows;
-    int64_t lo_first = 0, hi_first = 0, lo_last = 0, hi_last = 0;
-    if (row0 < rows) {
-        ka_span(a, s, row0, lo_first, hi_first);
-        ka_span(a, s, r_end - 1, lo_last, hi_last);
-    }
-    constexpr int STEP = SHARED ? 128 : 32;
-    const int64_t k_lo = lo_first & ~(int64_t)31;
-    const int64_t steps = hi_last > k_lo ? (hi_last - k_lo + STEP - 1) / STEP : 0;
-    const int64_t per = (steps + a.splits - 1) / a.splits;
-    const int64_t it0 = split * per;
-    const int n_it = (int)(it0 + per < steps ? per : (steps > it0 ? steps - it0 : 0));
-    const int32_t key0 = (int32_t)(k_lo + it0 * STEP + (SHARED ? wave * 32 : 0));
-    const int32_t kv = (int32_t)s.kv;
-    const int32_t full_lo = (int32_t)lo_last, full_hi = (int32_t)hi_first;
-
-    // tiles of 16 tokens for 32 steps at a time, a lane each: -1 past the keys or
-    // with a page id out of range
-    const int32_t* row_table = a.table + b * a.table_ld;
-    int tidx = -1;
-    auto fetch_tiles = [&](int it) {
-        const int32_t t16 = (key0 >> 4) + (it + (lane >> 1)) * (STEP / 16) + (lane & 1);
-        const int32_t col = (int32_t)(((uint64_t)(uint32_t)t16 * a.p16_inv) >> 36);
-        tidx = -1;
-        if (t16 < (kv + 15) >> 4) {
-            const int32_t pg = row_table[col];
-            if (pg >= 0 && pg < a.n_pages) tidx = (pg * a.H + h) * a.p16 + (t16 - col * a.p16);
-            else set_status(a.status, ISEG_DEV_RANGE);
-        }
-    };
-    KaKeys<NC> nx;
-    auto fetch = [&](int it) {
-        if ((it & 31) == 0) fetch_tiles(it);
-#pragma unroll
-        for (int i = 0; i < 2; i++) {
-            const int ti = __builtin_amdgcn_readlane(tidx, (it & 31) * 2 + i);
-            nx.ok[i] = ti >= 0;
-            const int64_t at = ti >= 0 ? ti : 0;
-            words<NC>(a.kc + at * (256 * NC) + (c * 4 + g4) * (4 * NC), nx.k[i]);
-            words<NC>(a.vc + at * (256 * NC) + (c * 4 + g4) * (4 * NC), nx.v[i]);
-            nx.ks[i] = *(const f4_t*)(a.ks + at * 16 + g4 * 4);
-            nx.vs[i] = *(const f4_t*)(a.vs + at * 16 + g4 * 4);
-        }
-    };
-
+// What a wave keeps of its 16 R rows.  WIDE: q and p as two float16 terms
+// (float32 tensors).
+template <int NC, int R, bool WIDE>
+struct KaRows {
+    static constexpr int NS = WIDE ? 2 : 1;
+    h8_t q[NS][R][NC];                   // queries as B operands
+    float cf[R];                         // score per unit of S^T and scale of k
+    int32_t lo[R], hi[R];                // keys that a lane's rows see
+    int32_t full_lo, full_hi;            // keys that all rows see
+    int32_t any_lo, any_hi;              // keys that some row sees
     f4_t acc[R][2 * NC];
     float m[R], l[R];
-#pragma unroll
-    for (int t = 0; t < R; t++) {
-        m[t] = kNone;
-        l[t] = 0.f;
-#pragma unroll
-        for (int i = 0; i < 2 * NC; i++) acc[t][i] = f4_t{0.f, 0.f, 0.f, 0.f};
-    }
-    float v_inv = 1.f, v_top = 0.f;      // V's scales times v_inv are below 2^7; up to v_top nothing moves
+    float v_inv, v_top;                  // V's scales times v_inv are below 2^7; up to v_top nothing moves
 
-    if (n_it > 0) fetch(0);
-    for (int it = 0; it < n_it; it++) {
-        const KaKeys<NC> x = nx;
-        if (it + 1 < n_it) fetch(it + 1);
-        const int32_t kb = key0 + it * STEP;
-        if (SHARED && kb >= (int32_t)hi_last) break;
-
-        f4_t st[R][2];
+    __device__ __forceinline__ void load(const KaArgs& a, const KaSeq& s, int64_t row0, int64_t rows, int h)
+    {
+        const int lane = threadIdx.x & 63, c = lane & 15, g4 = lane >> 4;
 #pragma unroll
-        for (int i = 0; i < 2; i++) {
-#pragma unroll
-            for (int t = 0; t < R; t++) st[t][i] = f4_t{0.f, 0.f, 0.f, 0.f};
+        for (int t = 0; t < R; t++) {
+            const int64_t r = row0 + t * 16 + c;
+            const bool in = r < rows;
+            int64_t l0 = 0, h0 = 0;
+            if (in) ka_span(a, s, r, l0, h0);
+            lo[t] = (int32_t)l0;
+            hi[t] = (int32_t)h0;
+            const int64_t at = in ? (s.q0 + r / a.G) * a.q_ld + (h * a.G + r % a.G) * a.q_hs : 0;
+            float f[NC][8];
+            float big = 0.f;
 #pragma unroll
             for (int w = 0; w < NC; w++) {
-                const uint32_t lo8 = x.k[i][w], hi8 = lo8 >> 8;
-                const h8_t kf = join8(codes_lo(lo8), codes_hi(lo8), codes_lo(hi8), codes_hi(hi8));
+                const int d = g4 * 8 * NC + w * 8;
 #pragma unroll
-                for (int t = 0; t < R; t++)
+                for (int i = 0; i < 8; i++) f[w][i] = 0.f;
+                if (in && d < a.D) {
+                    if (WIDE) {
+                        float x[8];
+                        __builtin_memcpy(x, (const float*)a.q + at + d, 32);
 #pragma unroll
-                    for (int n = 0; n < NS; n++)
-                        st[t][i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf, qf[n][t][w], st[t][i], 0, 0, 0);
+                        for (int i = 0; i < 8; i++) f[w][i] = x[i];
+                    } else if (a.dtype == ISEG_F16) {
+                        _Float16 x[8];
+                        __builtin_memcpy(x, (const _Float16*)a.q + at + d, 16);
+#pragma unroll
+                        for (int i = 0; i < 8; i++) f[w][i] = (float)x[i];
+                    } else {
+                        __bf16 x[8];
+                        __builtin_memcpy(x, (const __bf16*)a.q + at + d, 16);
+#pragma unroll
+                        for (int i = 0; i < 8; i++) f[w][i] = (float)x[i];
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < 8; i++) big = fmaxf(big, fabsf(f[w][i]));
             }
-        }
-
-        // V's scales; those of no key count as 0
-        f4_t vs[2] = {x.vs[0], x.vs[1]};
-        const bool full = x.ok[0] && x.ok[1] && kb >= full_lo && kb + 32 <= full_hi;
-        if (!full) {
+            // float16 reaches no further than 65504 and 2^-24: rows of the other
+            // types are brought below 1 by a power of two first
+            int e = 0;
+            if (WIDE || a.dtype != ISEG_F16) {
+                big = max4(big);
+                if (big > 0.f && big <= 3.4028234e38f) (void)frexpf(big, &e);
+                e = e < -100 ? -100 : e;
+            }
+            cf[t] = fmaxf(ldexpf(a.scale, e), 1.17549435e-38f);      // never 0: a masked score is -infinity times this
 #pragma unroll
-            for (int i = 0; i < 2; i++)
+            for (int w = 0; w < NC; w++)
+#pragma unroll
+                for (int i = 0; i < 8; i++) {
+                    const float x = ldexpf(f[w][i], -e);
+                    q[0][t][w][i] = (_Float16)x;
+                    if constexpr (WIDE) q[NS - 1][t][w][i] = (_Float16)(x - (float)(_Float16)x);
+                }
+            m[t] = kNone;
+            l[t] = 0.f;
+#pragma unroll
+            for (int i = 0; i < 2 * NC; i++) acc[t][i] = f4_t{0.f, 0.f, 0.f, 0.f};
+        }
+        v_inv = 1.f;
+        v_top = 0.f;
+        full_lo = full_hi = any_lo = any_hi = 0;
+        if (row0 < rows) {
+            const int64_t last = (row0 + 16 * R < rows ? row0 + 16 * R : rows) - 1;
+            int64_t l0, h0;
+            ka_span(a, s, row0, l0, h0);
+            any_lo = (int32_t)l0;
+            full_hi = (int32_t)h0;
+            ka_span(a, s, last, l0, h0);
+            full_lo = (int32_t)l0;
+            any_hi = (int32_t)h0;
+        }
+    }
+
+    // The softmax step of NT tiles of 16 keys from key kb on: scores st, the
+    // tiles' scales, whether a tile is there (ok).  Leaves the weights as B
+    // operands of V^T P^T in the order of V's words (tokens 0 2 1 3).
+    template <int NT>
+    __device__ __forceinline__ void soften(f4_t (&st)[R][NT], const f4_t* ks, f4_t* vs, const bool* ok, int32_t kb,
+                                           int32_t kv, h8_t (&pf)[NS][R][NT / 2])
+    {
+        const int g4 = (threadIdx.x & 63) >> 4;
+        bool full = kb >= full_lo && kb + 16 * NT <= full_hi;
+#pragma unroll
+        for (int i = 0; i < NT; i++) full = full && ok[i];
+        if (!full) {                                             // V's scales of no key count as 0
+#pragma unroll
+            for (int i = 0; i < NT; i++)
 #pragma unroll
                 for (int r = 0; r < 4; r++)
-                    if (!(x.ok[i] && kb + 16 * i + 4 * g4 + r < kv)) vs[i][r] = 0.f;
+                    if (!(ok[i] && kb + 16 * i + 4 * g4 + r < kv)) vs[i][r] = 0.f;
         }
         float top = 0.f;
 #pragma unroll
-        for (int i = 0; i < 2; i++)
+        for (int i = 0; i < NT; i++)
 #pragma unroll
             for (int r = 0; r < 4; r++) top = fmaxf(top, vs[i][r]);
         if (__any(top > v_top)) {
@@ -345,7 +316,7 @@ __global__ __launch_bounds__(256) void k_kv4_attention(KaArgs a)
                 for (int i = 0; i < 2 * NC; i++) acc[t][i] *= f;
         }
 #pragma unroll
-        for (int i = 0; i < 2; i++) vs[i] *= v_inv;
+        for (int i = 0; i < NT; i++) vs[i] *= v_inv;
 
         float mx[R];
         bool move = false;
@@ -353,13 +324,13 @@ __global__ __launch_bounds__(256) void k_kv4_attention(KaArgs a)
         for (int t = 0; t < R; t++) {
             mx[t] = -__builtin_inff();
 #pragma unroll
-            for (int i = 0; i < 2; i++)
+            for (int i = 0; i < NT; i++)
 #pragma unroll
                 for (int r = 0; r < 4; r++) {
-                    float v = st[t][i][r] * x.ks[i][r];
+                    float v = st[t][i][r] * ks[i][r];
                     if (!full) {
                         const int32_t j = kb + 16 * i + 4 * g4 + r;
-                        if (!(x.ok[i] && j >= (int32_t)lo[t] && j < (int32_t)hi[t])) v = -__builtin_inff();
+                        if (!(ok[i] && j >= lo[t] && j < hi[t])) v = -__builtin_inff();
                     }
                     st[t][i][r] = v;
                     mx[t] = fmaxf(mx[t], v);
@@ -377,166 +348,398 @@ __global__ __launch_bounds__(256) void k_kv4_attention(KaArgs a)
                 for (int i = 0; i < 2 * NC; i++) acc[t][i] *= al;
             }
         }
-        h8_t pf[NS][R];
 #pragma unroll
-        for (int t = 0; t < R; t++) {
-            float p[2][4];
+        for (int t = 0; t < R; t++)
 #pragma unroll
-            for (int i = 0; i < 2; i++)
+            for (int i = 0; i < NT; i++) {
+                float p[4];
 #pragma unroll
                 for (int r = 0; r < 4; r++) {
                     const float v = __builtin_amdgcn_exp2f(fmaf(st[t][i][r], cf[t], -m[t]));
                     l[t] += v;
-                    p[i][r] = v * vs[i][r];
-                    if (!full && st[t][i][r] == -__builtin_inff()) p[i][r] = 0.f;      // a masked key's scale may be anything
+                    p[r] = v * vs[i][r];
+                    if (!full && st[t][i][r] == -__builtin_inff()) p[r] = 0.f;         // a masked key's scale may be anything
                 }
-            // V's words hold tokens 0 2 and 1 3 as pairs
-#pragma unroll
-            for (int i = 0; i < 2; i++) {
                 constexpr int order[4] = {0, 2, 1, 3};
 #pragma unroll
                 for (int r = 0; r < 4; r++) {
-                    const float v = p[i][order[r]];
-                    pf[0][t][4 * i + r] = (_Float16)v;
-                    if constexpr (WIDE) pf[NS - 1][t][4 * i + r] = (_Float16)(v - (float)(_Float16)v);
+                    const float v = p[order[r]];
+                    pf[0][t][i / 2][4 * (i & 1) + r] = (_Float16)v;
+                    if constexpr (WIDE) pf[NS - 1][t][i / 2][4 * (i & 1) + r] = (_Float16)(v - (float)(_Float16)v);
                 }
             }
+    }
+
+    template <int NT>
+    __device__ __forceinline__ void score(const h8_t kf, int w, int i, f4_t (&st)[R][NT])
+    {
+#pragma unroll
+        for (int t = 0; t < R; t++)
+#pragma unroll
+            for (int n = 0; n < NS; n++) st[t][i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf, q[n][t][w], st[t][i], 0, 0, 0);
+    }
+
+    // O^T += V^T P^T for columns 16 d .. of a pair of tiles
+    template <int NP>
+    __device__ __forceinline__ void add(const h8_t vf, int d, int pair, const h8_t (&pf)[NS][R][NP])
+    {
+#pragma unroll
+        for (int t = 0; t < R; t++)
+#pragma unroll
+            for (int n = 0; n < NS; n++)
+                acc[t][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf, pf[n][t][pair], acc[t][d], 0, 0, 0);
+    }
+};
+
+// Tiles of 16 tokens that a wave needs, PER a step, STRIDE apart from step to
+// step: looked up in the block table for many steps at a time, one lane each.
+template <int PER, int STRIDE>
+struct KaTiles {
+    static constexpr int N = 64 / PER;   // steps of a look-up
+    const int32_t* row;
+    int32_t first, end;                  // first tile, tiles of the request
+    int idx;
+    __device__ __forceinline__ void look(const KaArgs& a, int h, int it)
+    {
+        const int lane = threadIdx.x & 63;
+        const int32_t t16 = first + (it + lane / PER) * STRIDE + lane % PER;
+        idx = -1;                        // past the keys, or a page id out of range
+        if (t16 < end) {
+            const int32_t col = (int32_t)(((uint64_t)(uint32_t)t16 * a.p16_inv) >> 36);
+            const int32_t pg = row[col];
+            if (pg >= 0 && pg < a.n_pages) idx = (pg * a.H + h) * a.p16 + (t16 - col * a.p16);
+            else set_status(a.status, ISEG_DEV_RANGE);
         }
+    }
+    __device__ __forceinline__ int at(int it, int i) const { return __builtin_amdgcn_readlane(idx, (it % N) * PER + i); }
+};
+
+// ---------------------------------------------------------------------------
+// few rows: the four waves of a block hold the same rows and deal the keys among
+// themselves
+// ---------------------------------------------------------------------------
+template <int NC>
+struct KaKeys {                          // 32 keys of one head: a lane's words and scales
+    uint32_t k[2][NC], v[2][NC];
+    f4_t ks[2], vs[2];
+    bool ok[2];
+};
+
+// NC: words of a row's quarter (W / 32).  R: tiles of 16 rows.
+template <int NC, int R, bool WIDE>
+__global__ __launch_bounds__(256) void k_kv4_few(KaArgs a)
+{
+    constexpr int W = NC * 32, TR = 16 * R;
+    __shared__ float so[4 * 16 * (W + 4)];
+    __shared__ float sm[4][16], sl[4][16];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int c = lane & 15, g4 = lane >> 4;
+    const int h = blockIdx.x % a.H, split = (blockIdx.x / a.H) % a.splits, tile = blockIdx.x / a.H / a.splits;
+    int bad = 0;
+    KaSeq s;
+    int64_t b, row0;
+    const bool have = ka_tile<TR, true>(a, tile, s, b, row0, bad);
+    if (bad) set_status(a.status, ISEG_DEV_RANGE);
+    if (!have) return;
+    const int64_t rows = s.n * a.G;
+    KaRows<NC, R, WIDE> x;
+    x.load(a, s, 0, rows, h);
+
+    // whole steps of 128 keys, dealt to the splits
+    const int32_t k_lo = x.any_lo & ~31, kv = (int32_t)s.kv;
+    const int32_t steps = x.any_hi > k_lo ? (x.any_hi - k_lo + 127) / 128 : 0;
+    const int32_t per = (steps + a.splits - 1) / a.splits, it0 = split * per;
+    const int32_t n_it = it0 + per < steps ? per : (steps > it0 ? steps - it0 : 0);
+    const int32_t key0 = k_lo + it0 * 128 + wave * 32;
+
+    KaTiles<2, 8> tl = {a.table + b * a.table_ld, key0 >> 4, (kv + 15) >> 4, -1};
+    KaKeys<NC> nx;
+    auto fetch = [&](int it) {
+        if (it % tl.N == 0) tl.look(a, h, it);
+#pragma unroll
+        for (int i = 0; i < 2; i++) {
+            const int ti = tl.at(it, i);
+            nx.ok[i] = ti >= 0;
+            const int64_t at = ti >= 0 ? ti : 0;
+            words<NC>(a.kc + at * (256 * NC) + (c * 4 + g4) * (4 * NC), nx.k[i]);
+            words<NC>(a.vc + at * (256 * NC) + (c * 4 + g4) * (4 * NC), nx.v[i]);
+            nx.ks[i] = *(const f4_t*)(a.ks + at * 16 + g4 * 4);
+            nx.vs[i] = *(const f4_t*)(a.vs + at * 16 + g4 * 4);
+        }
+    };
+    if (n_it > 0) fetch(0);
+    for (int it = 0; it < n_it; it++) {
+        KaKeys<NC> y = nx;
+        if (it + 1 < n_it) fetch(it + 1);
+        const int32_t kb = key0 + it * 128;
+        if (kb >= x.any_hi) break;
+        f4_t st[R][2];
+#pragma unroll
+        for (int i = 0; i < 2; i++) {
+#pragma unroll
+            for (int t = 0; t < R; t++) st[t][i] = f4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int w = 0; w < NC; w++) {
+                const uint32_t u = y.k[i][w], v = u >> 8;
+                x.score(join8(codes_lo(u), codes_hi(u), codes_lo(v), codes_hi(v)), w, i, st);
+            }
+        }
+        h8_t pf[x.NS][R][1];
+        x.soften(st, y.ks, y.vs, y.ok, kb, kv, pf);
 #pragma unroll
         for (int w = 0; w < NC; w++) {
-            const uint32_t a0 = x.v[0][w], a1 = x.v[1][w], b0 = a0 >> 8, b1 = a1 >> 8;
-            const h8_t vl = join8(codes_lo(a0), codes_lo(b0), codes_lo(a1), codes_lo(b1));
-            const h8_t vh = join8(codes_hi(a0), codes_hi(b0), codes_hi(a1), codes_hi(b1));
-#pragma unroll
-            for (int t = 0; t < R; t++)
-#pragma unroll
-                for (int n = 0; n < NS; n++) {
-                    acc[t][2 * w] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vl, pf[n][t], acc[t][2 * w], 0, 0, 0);
-                    acc[t][2 * w + 1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vh, pf[n][t], acc[t][2 * w + 1], 0, 0, 0);
-                }
+            const uint32_t a0 = y.v[0][w], a1 = y.v[1][w], b0 = a0 >> 8, b1 = a1 >> 8;
+            x.add(join8(codes_lo(a0), codes_lo(b0), codes_lo(a1), codes_lo(b1)), 2 * w, 0, pf);
+            x.add(join8(codes_hi(a0), codes_hi(b0), codes_hi(a1), codes_hi(b1)), 2 * w + 1, 0, pf);
         }
     }
 
-    // rows out: the whole, or this split's part
-    const float v_out = 1.f / v_inv;
-    auto put = [&](int64_t r, int d, f4_t o, float mr, float lr) {     // four elements of row r from d on
-        if (a.splits > 1) {
-            const int64_t at = (((int64_t)tile * a.H + h) * TR + r) * a.splits + split;
-            *(f4_t*)(a.po + at * W + d) = o;
-            if (d == 0) { a.pm[at * 2] = mr; a.pm[at * 2 + 1] = lr; }
-            return;
-        }
-        const int64_t rr = SHARED ? r : row0 - wave * 16 * R + r;
-        const int64_t tok = s.q0 + rr / a.G, head = h * a.G + rr % a.G;
-        const float inv = lr > 0.f ? 1.f / lr : (lr == lr ? 0.f : lr);
-        if (d < a.D) {
-            if (WIDE) {
-                float x[4] = {o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv};
-                __builtin_memcpy((float*)a.out + tok * a.o_ld + head * a.o_hs + d, x, 16);
-            } else if (a.dtype == ISEG_F16) {
-                _Float16 x[4] = {(_Float16)(o[0] * inv), (_Float16)(o[1] * inv), (_Float16)(o[2] * inv), (_Float16)(o[3] * inv)};
-                __builtin_memcpy((_Float16*)a.out + tok * a.o_ld + head * a.o_hs + d, x, 8);
-            } else {
-                __bf16 x[4] = {(__bf16)(o[0] * inv), (__bf16)(o[1] * inv), (__bf16)(o[2] * inv), (__bf16)(o[3] * inv)};
-                __builtin_memcpy((__bf16*)a.out + tok * a.o_ld + head * a.o_hs + d, x, 8);
+    // the waves' rows joined, a tile of 16 at a time: the whole, or this split's part
+    const float v_out = 1.f / x.v_inv;
+#pragma unroll
+    for (int t = 0; t < R; t++) x.l[t] = sum4(x.l[t]);
+    for (int t = 0; t < R; t++) {
+        if (t * 16 >= rows) break;
+        __syncthreads();
+        float* mine = so + (wave * 16 + c) * (W + 4) + g4 * 4;
+#pragma unroll
+        for (int u = 0; u < R; u++)
+            if (u == t) {
+#pragma unroll
+                for (int i = 0; i < 2 * NC; i++) *(f4_t*)(mine + i * 16) = x.acc[u][i] * v_out;
+                if (g4 == 0) { sm[wave][c] = x.m[u]; sl[wave][c] = x.l[u]; }
             }
-        }
-        if (d == 0 && a.lse)
-            a.lse[tok * a.Hq + head] = lr > 0.f || lr != lr ? (mr + __builtin_amdgcn_logf(lr)) * 0.69314718f : -__builtin_inff();
-    };
+        __syncthreads();
+        for (int e = threadIdx.x; e < 16 * (W / 4); e += 256) {
+            const int r = e / (W / 4), d = (e - r * (W / 4)) * 4;
+            if (t * 16 + r >= rows) continue;
+            float mr = sm[0][r];
 #pragma unroll
-    for (int t = 0; t < R; t++) l[t] = sum4(l[t]);
-    if constexpr (!SHARED) {
+            for (int w = 1; w < 4; w++) mr = fmaxf(mr, sm[w][r]);
+            f4_t o = {0.f, 0.f, 0.f, 0.f};
+            float lr = 0.f;
 #pragma unroll
-        for (int t = 0; t < R; t++) {
-            if (row0 + t * 16 + c >= rows) continue;
-#pragma unroll
-            for (int i = 0; i < 2 * NC; i++)
-                put(wave * 16 * R + t * 16 + c, i * 16 + g4 * 4, acc[t][i] * v_out, m[t], l[t]);
-        }
-    } else {
-        for (int t = 0; t < R; t++) {
-            if (t * 16 >= rows) break;
-            __syncthreads();
-            float* mine = so + (wave * 16 + c) * (W + 4) + g4 * 4;
-#pragma unroll
-            for (int u = 0; u < R; u++)
-                if (u == t) {
-#pragma unroll
-                    for (int i = 0; i < 2 * NC; i++) *(f4_t*)(mine + i * 16) = acc[u][i] * v_out;
-                    if (g4 == 0) { sm[wave][c] = m[u]; sl[wave][c] = l[u]; }
-                }
-            __syncthreads();
-            for (int e = threadIdx.x; e < 16 * (W / 4); e += 256) {
-                const int r = e / (W / 4), d = (e - r * (W / 4)) * 4;
-                if (t * 16 + r >= rows) continue;
-                float mr = sm[0][r];
-#pragma unroll
-                for (int w = 1; w < 4; w++) mr = fmaxf(mr, sm[w][r]);
-                f4_t o = {0.f, 0.f, 0.f, 0.f};
-                float lr = 0.f;
-#pragma unroll
-                for (int w = 0; w < 4; w++) {
-                    const float f = __builtin_amdgcn_exp2f(sm[w][r] - mr);
-                    o += f * *(const f4_t*)(so + (w * 16 + r) * (W + 4) + d);
-                    lr += f * sl[w][r];
-                }
-                put(t * 16 + r, d, o, mr, lr);
+            for (int w = 0; w < 4; w++) {
+                const float f = __builtin_amdgcn_exp2f(sm[w][r] - mr);
+                o += f * *(const f4_t*)(so + (w * 16 + r) * (W + 4) + d);
+                lr += f * sl[w][r];
             }
+            ka_put<TR>(a, s, tile, h, split, 0, t * 16 + r, d, o, mr, lr);
         }
     }
 }
 
-// The splits' parts of a row, in their order: a block a row.
-template <int TR, bool SHARED>
-__global__ __launch_bounds__(64) void k_kv4_join(KaArgs a)
+// ---------------------------------------------------------------------------
+// many rows: eight waves with 16 R rows each; 64 keys at a time become float16
+// operands in LDS, once for all of them
+// ---------------------------------------------------------------------------
+constexpr int kWaves = 8;
+
+// a stage: operands of 64 keys, 1 KB each (64 lanes of 16 bytes), and their scales
+template <int NC>
+struct KaStage {
+    h8_t k[4][NC][64];                   // [tile][word]
+    h8_t v[2][2 * NC][64];               // [pair of tiles][16 columns]
+    float ks[64], vs[64];
+};
+
+template <int NC, int R, bool WIDE>
+__global__ __launch_bounds__(512) void k_kv4_many(KaArgs a)
 {
-    const int r = blockIdx.x % TR, h = (blockIdx.x / TR) % a.H, tile = blockIdx.x / TR / a.H;
+    constexpr int TR = 16 * R * kWaves;
+    extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
+    KaStage<NC>* stage = (KaStage<NC>*)smem;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int c = lane & 15, g4 = lane >> 4;
+    const int h = blockIdx.x % a.H, split = (blockIdx.x / a.H) % a.splits, tile = blockIdx.x / a.H / a.splits;
+    int bad = 0;
+    KaSeq s;
+    int64_t b, row0;
+    const bool have = ka_tile<TR, false>(a, tile, s, b, row0, bad);
+    if (bad) set_status(a.status, ISEG_DEV_RANGE);
+    if (!have) return;
+    const int64_t rows = s.n * a.G;
+    KaRows<NC, R, WIDE> x;
+    x.load(a, s, row0 + wave * 16 * R, rows, h);
+
+    // keys of the block's rows in steps of 64, dealt to the splits
+    int64_t l0, h0, l1, h1;
+    ka_span(a, s, row0, l0, h0);
+    ka_span(a, s, (row0 + TR < rows ? row0 + TR : rows) - 1, l1, h1);
+    const int32_t k_lo = (int32_t)l0 & ~63, k_hi = (int32_t)h1, kv = (int32_t)s.kv;
+    const int32_t steps = k_hi > k_lo ? (k_hi - k_lo + 63) / 64 : 0;
+    const int32_t per = (steps + a.splits - 1) / a.splits, it0 = split * per;
+    const int32_t n_it = it0 + per < steps ? per : (steps > it0 ? steps - it0 : 0);
+    const int32_t key0 = k_lo + it0 * 64;
+
+    // waves 0-3 bring a tile of keys each, waves 4-7 one nibble of a pair of tiles of values
+    KaTiles<4, 4> tl = {a.table + b * a.table_ld, key0 >> 4, (kv + 15) >> 4, -1};
+    const bool values = wave >= 4;
+    const int vp = (wave >> 1) & 1, vn = wave & 1;
+    uint32_t wa[NC], wb[NC];
+    float sc = 0.f;
+    auto fetch = [&](int it) {
+        if (it % tl.N == 0) tl.look(a, h, it);
+        const int own = tl.at(it, wave & 3);
+        const int64_t o = own >= 0 ? own : 0;
+        if (!values) {
+            words<NC>(a.kc + o * (256 * NC) + (c * 4 + g4) * (4 * NC), wa);
+            sc = a.ks[o * 16 + c];
+        } else {
+            const int u0 = tl.at(it, 2 * vp), u1 = tl.at(it, 2 * vp + 1);
+            const int64_t t0 = u0 >= 0 ? u0 : 0, t1 = u1 >= 0 ? u1 : 0;
+            words<NC>(a.vc + t0 * (256 * NC) + (c * 4 + g4) * (4 * NC), wa);
+            words<NC>(a.vc + t1 * (256 * NC) + (c * 4 + g4) * (4 * NC), wb);
+            sc = a.vs[o * 16 + c];
+        }
+    };
+    auto spread = [&](KaStage<NC>& d) {
+        if (!values) {
+#pragma unroll
+            for (int w = 0; w < NC; w++) {
+                const uint32_t u = wa[w], v = u >> 8;
+                d.k[wave][w][lane] = join8(codes_lo(u), codes_hi(u), codes_lo(v), codes_hi(v));
+            }
+            if (lane < 16) d.ks[wave * 16 + lane] = sc;
+        } else {
+#pragma unroll
+            for (int w = 0; w < NC; w++) {
+                const uint32_t a0 = wa[w] >> (4 * vn), a1 = wb[w] >> (4 * vn), b0 = a0 >> 8, b1 = a1 >> 8;
+                d.v[vp][2 * w + vn][lane] = join8(codes_lo(a0), codes_lo(b0), codes_lo(a1), codes_lo(b1));
+            }
+            if (lane < 16) d.vs[(wave - 4) * 16 + lane] = sc;
+        }
+    };
+    // the tiles that are there, as bits, looked at before the next look-up takes their place
+    auto there = [&](int it) {
+        int m = 0;
+#pragma unroll
+        for (int i = 0; i < 4; i++) m |= (tl.at(it, i) >= 0) << i;
+        return m;
+    };
+    int ok_now = 0, ok_next = 0;
+    if (n_it > 0) {
+        fetch(0);
+        ok_next = there(0);
+        spread(stage[0]);
+        if (n_it > 1) fetch(1);
+    }
+    for (int it = 0; it < n_it; it++) {
+        __syncthreads();
+        ok_now = ok_next;
+        if (it + 1 < n_it) {
+            ok_next = there(it + 1);
+            spread(stage[(it + 1) & 1]);
+            if (it + 2 < n_it) fetch(it + 2);
+        }
+        const int32_t kb = key0 + it * 64;
+        if (kb >= x.any_hi || kb + 64 <= x.any_lo) continue;
+        const KaStage<NC>& y = stage[it & 1];
+        f4_t st[R][4], ks[4], vs[4];
+        bool ok[4];
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+            ok[i] = ok_now >> i & 1;
+            ks[i] = *(const f4_t*)(y.ks + i * 16 + g4 * 4);
+            vs[i] = *(const f4_t*)(y.vs + i * 16 + g4 * 4);
+#pragma unroll
+            for (int t = 0; t < R; t++) st[t][i] = f4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int w = 0; w < NC; w++) x.score(y.k[i][w][lane], w, i, st);
+        }
+        h8_t pf[x.NS][R][2];
+        x.soften(st, ks, vs, ok, kb, kv, pf);
+#pragma unroll
+        for (int p = 0; p < 2; p++)
+#pragma unroll
+            for (int d = 0; d < 2 * NC; d++) x.add(y.v[p][d][lane], d, p, pf);
+    }
+    const float v_out = 1.f / x.v_inv;
+#pragma unroll
+    for (int t = 0; t < R; t++) {
+        const float l = sum4(x.l[t]);
+        const int r = wave * 16 * R + t * 16 + c;
+        if (row0 + r >= rows) continue;
+#pragma unroll
+        for (int i = 0; i < 2 * NC; i++) ka_put<TR>(a, s, tile, h, split, row0, r, i * 16 + g4 * 4, x.acc[t][i] * v_out, x.m[t], l);
+    }
+}
+
+// The splits' parts of a row: a block a row, whose groups of W / 4 threads take
+// every so many splits; the groups are added in their order.
+template <int TR, bool SHARED>
+__global__ __launch_bounds__(256) void k_kv4_join(KaArgs a)
+{
+    __shared__ float fs[kSplitsMax];
+    __shared__ f4_t red[256];
+    __shared__ float lsum;
+    const int r = blockIdx.x % a.join_rows, h = (blockIdx.x / a.join_rows) % a.H, tile = blockIdx.x / a.join_rows / a.H;
     int bad = 0;
     KaSeq s;
     int64_t b, row0;
     if (!ka_tile<TR, SHARED>(a, tile, s, b, row0, bad)) return;
     if (row0 + r >= s.n * a.G) return;
     const int64_t at = (((int64_t)tile * a.H + h) * TR + r) * a.splits;
-    float mr = kNone;
-    for (int i = threadIdx.x; i < a.splits; i += 64) mr = fmaxf(mr, a.pm[(at + i) * 2]);
+    const int lw = a.W / 4, groups = 256 / lw, grp = threadIdx.x / lw, d = (threadIdx.x - grp * lw) * 4;
+    if (threadIdx.x < 64) {
+        float m[kSplitsMax / 64], mr = kNone, lr = 0.f;
 #pragma unroll
-    for (int o = 32; o > 0; o >>= 1) mr = fmaxf(mr, __shfl_xor(mr, o, 64));
-    float lr = 0.f;
-    f4_t o = {0.f, 0.f, 0.f, 0.f};
-    const int d = threadIdx.x * 4;
-    for (int i = 0; i < a.splits; i++) {
-        const float f = __builtin_amdgcn_exp2f(a.pm[(at + i) * 2] - mr);
-        lr += f * a.pm[(at + i) * 2 + 1];
-        if (d < a.W) o += f * *(const f4_t*)(a.po + (at + i) * a.W + d);
-    }
-    const int64_t tok = s.q0 + (row0 + r) / a.G, head = h * a.G + (row0 + r) % a.G;
-    const float inv = lr > 0.f ? 1.f / lr : (lr == lr ? 0.f : lr);
-    if (d < a.D) {
+        for (int i = 0; i < kSplitsMax / 64; i++) {
+            const int k = i * 64 + threadIdx.x;
+            m[i] = k < a.splits ? a.pm[(at + k) * 2] : kNone;
+            mr = fmaxf(mr, m[i]);
+        }
 #pragma unroll
-        for (int i = 0; i < 4; i++) {
-            const int64_t p = tok * a.o_ld + head * a.o_hs + d + i;
-            if (a.dtype == ISEG_F32) ((float*)a.out)[p] = o[i] * inv;
-            else if (a.dtype == ISEG_F16) ((_Float16*)a.out)[p] = (_Float16)(o[i] * inv);
-            else ((__bf16*)a.out)[p] = (__bf16)(o[i] * inv);
+        for (int o = 32; o > 0; o >>= 1) mr = fmaxf(mr, __shfl_xor(mr, o, 64));
+#pragma unroll
+        for (int i = 0; i < kSplitsMax / 64; i++) {
+            const int k = i * 64 + threadIdx.x;
+            if (k < a.splits) {
+                const float f = __builtin_amdgcn_exp2f(m[i] - mr);
+                fs[k] = f;
+                lr += f * a.pm[(at + k) * 2 + 1];
+            }
+        }
+        lr = wave_sum_f32(lr);
+        if (threadIdx.x == 0) {
+            lsum = lr;
+            if (a.lse) {
+                const int64_t tok = s.q0 + (row0 + r) / a.G, head = h * a.G + (row0 + r) % a.G;
+                a.lse[tok * a.Hq + head] = ka_lse(mr, lr);
+            }
         }
     }
-    if (threadIdx.x == 0 && a.lse)
-        a.lse[tok * a.Hq + head] = lr > 0.f || lr != lr ? (mr + __builtin_amdgcn_logf(lr)) * 0.69314718f : -__builtin_inff();
+    __syncthreads();
+    f4_t o = {0.f, 0.f, 0.f, 0.f};
+    if (grp < groups) {
+#pragma unroll 4
+        for (int i = grp; i < a.splits; i += groups) o += fs[i] * *(const f4_t*)(a.po + (at + i) * a.W + d);
+    }
+    red[threadIdx.x] = o;
+    __syncthreads();
+    if (grp == 0 && d < a.D) {
+        for (int g = 1; g < groups; g++) o += red[g * lw + threadIdx.x];
+        const int64_t tok = s.q0 + (row0 + r) / a.G, head = h * a.G + (row0 + r) % a.G;
+        ka_store(a, tok, head, d, o, lsum);
+    }
 }
 
 // ---------------------------------------------------------------------------
 // host
 // ---------------------------------------------------------------------------
 // A call's launches: requests of up to 16 R rows by blocks whose waves share
-// them, the others in tiles of 64 or 128 rows.
+// them, the others in tiles of 128 R2 rows.
 struct KaPlan {
     int R;                       // tiles of 16 rows of the first kind; 0: none
-    int R2;                      // rows of the second kind's tiles / 64; 0: none
+    int R2;                      // tiles of 16 rows of a wave of the second kind; 0: none
     int64_t tiles2;
     int splits, splits2;
     size_t part, bytes;
 };
+
+// what a wave's registers hold
+constexpr int ka_few_most(int nc, bool wide) { return wide ? (nc <= 4 ? 2 : 1) : (nc <= 4 ? 4 : 2); }
+constexpr int ka_many(int nc, bool wide) { return wide || nc > 4 ? 1 : 2; }
 
 bool ka_wide(const iseg_kv4_attention_geom* g) { return g->dtype == ISEG_F32; }
 
@@ -553,7 +756,7 @@ KaPlan ka_plan(const iseg_kv4_attention_geom* g)
     KaPlan p = {};
     const int nc = kv4_width(g->D) / 32;
     const int64_t G = g->Hq / g->H, rows = ka_max_q(g) * G, pairs = g->B * g->H;
-    const int most = ka_wide(g) ? (nc <= 4 ? 2 : 1) : (nc <= 4 ? 4 : 2);     // registers
+    const int most = ka_few_most(nc, ka_wide(g));
     int64_t span = ka_max_kv(g);
     if (g->window > 0 && g->window + ka_max_q(g) < span) span = g->window + ka_max_q(g);
     if (rows <= 16 * most || g->B > 1) {
@@ -561,17 +764,17 @@ KaPlan ka_plan(const iseg_kv4_attention_geom* g)
         p.R = r <= 16 ? 1 : (r <= 32 ? 2 : 4);
         int64_t sp = ceil_div64(1024, pairs), longest = ceil_div64(span, 256);
         sp = sp < longest ? sp : longest;
-        p.splits = (int)(sp < 1 ? 1 : (sp > 128 ? 128 : sp));
+        p.splits = (int)(sp < 1 ? 1 : (sp > kSplitsMax ? kSplitsMax : sp));
     }
     if (rows > 16 * most) {
-        p.R2 = ka_wide(g) || nc > 4 ? 1 : 2;
-        p.tiles2 = ceil_div64(g->T * G, 64 * p.R2) + g->B;
-        int64_t sp = ceil_div64(512, p.tiles2 * g->H), longest = ceil_div64(span, 512);
+        p.R2 = ka_many(nc, ka_wide(g));
+        p.tiles2 = ceil_div64(g->T * G, 16 * kWaves * p.R2) + g->B;
+        int64_t sp = ceil_div64(256, p.tiles2 * g->H), longest = ceil_div64(span, 512);
         sp = sp < longest ? sp : longest;
         p.splits2 = (int)(sp < 1 ? 1 : (sp > 32 ? 32 : sp));
     }
     const int64_t n1 = p.R && p.splits > 1 ? pairs * 16 * p.R * p.splits : 0;
-    const int64_t n2 = p.R2 && p.splits2 > 1 ? p.tiles2 * g->H * 64 * p.R2 * p.splits2 : 0;
+    const int64_t n2 = p.R2 && p.splits2 > 1 ? p.tiles2 * g->H * 16 * kWaves * p.R2 * p.splits2 : 0;
     const int64_t n = n1 > n2 ? n1 : n2;
     p.part = align256((size_t)n * 8);
     p.bytes = n ? ws_used(p.part + (size_t)n * kv4_width(g->D) * 4) : kNoWs;
@@ -593,44 +796,50 @@ int ka_check(const iseg_kv4_attention_geom* g)
     if (g->T > 0 && g->B > 0) {
         const KaPlan p = ka_plan(g);
         const int64_t most = (int64_t)1 << 24;               // blocks of 256 threads of a launch
-        if (g->B * g->H * p.splits >= most || (p.splits > 1 && g->B * g->H * 16 * p.R >= 4 * most) ||
-            (p.R2 && (p.tiles2 * g->H * p.splits2 >= most || (p.splits2 > 1 && p.tiles2 * g->H * 64 * p.R2 >= 4 * most))))
+        if (g->B * g->H * p.splits >= most || (p.splits > 1 && g->B * g->H * 16 * p.R >= most) ||
+            (p.R2 && (p.tiles2 * g->H * p.splits2 >= most || (p.splits2 > 1 && p.tiles2 * g->H * 16 * kWaves * p.R2 >= most))))
             return ISEG_ERR_UNSUPPORTED;
     }
     return ISEG_OK;
 }
 
-template <int NC, int R, bool SHARED, bool WIDE>
-int ka_launch(const KaArgs& a, int64_t tiles, hipStream_t s)
+template <int NC, int R, bool WIDE>
+int ka_few(KaArgs& a, hipStream_t s)
 {
-    constexpr int TR = SHARED ? 16 * R : 64 * R;
-    hipLaunchKernelGGL((k_kv4_attention<NC, R, SHARED, WIDE>), dim3((unsigned)(tiles * a.H * a.splits)), dim3(256), 0, s, a);
+    hipLaunchKernelGGL((k_kv4_few<NC, R, WIDE>), dim3((unsigned)((int64_t)a.B * a.H * a.splits)), dim3(256), 0, s, a);
+    const int64_t rows = a.max_q * a.G;
+    a.join_rows = (int32_t)(rows < 16 * R ? rows : 16 * R);
     if (a.splits > 1)
-        hipLaunchKernelGGL((k_kv4_join<TR, SHARED>), dim3((unsigned)(tiles * a.H * TR)), dim3(64), 0, s, a);
+        hipLaunchKernelGGL((k_kv4_join<16 * R, true>), dim3((unsigned)((int64_t)a.B * a.H * a.join_rows)), dim3(256), 0, s, a);
     return launch_ok();
 }
 
 template <int NC, bool WIDE>
 int ka_run(KaArgs a, const KaPlan& p, hipStream_t s)
 {
-    constexpr int most = WIDE ? (NC <= 4 ? 2 : 1) : (NC <= 4 ? 4 : 2);
+    constexpr int most = ka_few_most(NC, WIDE), R2 = ka_many(NC, WIDE);
     int rc = ISEG_OK;
     if (p.R) {
         a.rows_min = 0;
         a.rows_max = 16 * p.R;
         a.splits = p.splits;
-        if (p.R == 1) rc = ka_launch<NC, 1, true, WIDE>(a, a.B, s);
+        if (p.R == 1) rc = ka_few<NC, 1, WIDE>(a, s);
         if constexpr (most >= 2)
-            if (p.R == 2) rc = ka_launch<NC, 2, true, WIDE>(a, a.B, s);
+            if (p.R == 2) rc = ka_few<NC, 2, WIDE>(a, s);
         if constexpr (most >= 4)
-            if (p.R == 4) rc = ka_launch<NC, 4, true, WIDE>(a, a.B, s);
+            if (p.R == 4) rc = ka_few<NC, 4, WIDE>(a, s);
     }
     if (rc == ISEG_OK && p.R2) {
-        constexpr int R2 = WIDE || NC > 4 ? 1 : 2;
+        constexpr size_t lds = 2 * sizeof(KaStage<NC>);
+        if (!lds_limit((const void*)&k_kv4_many<NC, R2, WIDE>, lds)) return ISEG_ERR_DEVICE;
         a.rows_min = p.R ? 16 * p.R : 0;
         a.rows_max = 0x7fffffff;
         a.splits = p.splits2;
-        rc = ka_launch<NC, R2, false, WIDE>(a, p.tiles2, s);
+        a.join_rows = 16 * kWaves * R2;
+        hipLaunchKernelGGL((k_kv4_many<NC, R2, WIDE>), dim3((unsigned)(p.tiles2 * a.H * a.splits)), dim3(512), lds, s, a);
+        if (a.splits > 1)
+            hipLaunchKernelGGL((k_kv4_join<16 * kWaves * R2, false>), dim3((unsigned)(p.tiles2 * a.H * a.join_rows)), dim3(256), 0, s, a);
+        rc = launch_ok();
     }
     return rc;
 }

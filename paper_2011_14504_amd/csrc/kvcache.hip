@@ -13,7 +13,7 @@ struct KvArgs {
     void *ko, *vo;
     uint8_t *kc, *vc;
     float *ks, *vs;
-    int64_t rows;                    // T * H
+    int64_t T, rows;                 // rows: heads of four tokens each
     int64_t k_ld, k_hs, v_ld, v_hs;
     int64_t n_slots;
     int32_t H, D, W, page, slot64, mode;
@@ -57,10 +57,19 @@ __device__ __forceinline__ void kv_get8(const T* p, int d, int D, float* f)
     }
 }
 
-// LPR lanes a row, eight columns (a word of codes) a lane; blockIdx.y: keys or
-// values.  The largest magnitude over the row's lanes, the scale, the codes.  A
-// byte of v holds columns 16 apart, which lie two lanes apart: each pair of
-// lanes exchanges words and stores half of the eight bytes.
+// whether four tokens lie side by side in one run of four of a tile
+__device__ __forceinline__ bool kv_beside(const int64_t* slot, const KvArgs& a)
+{
+    return slot[0] >= 0 && slot[0] + 3 < a.n_slots && (slot[0] & 3) == 0 && slot[1] == slot[0] + 1 && slot[2] == slot[0] + 2 &&
+           slot[3] == slot[0] + 3;
+}
+
+// LPR lanes a row, eight columns (a word of codes) a lane, four tokens of a head
+// at a time; blockIdx.y: keys or values.  The largest magnitude over the row's
+// lanes, the scale, the codes.  A byte of v holds columns 16 apart, which lie two
+// lanes apart: each pair of lanes exchanges words and has half of the eight
+// bytes.  Tokens side by side, as a prompt's are, store v in words of four
+// tokens, others in bytes.
 template <typename T, int LPR>
 __global__ __launch_bounds__(256) void k_kv4_write(KvArgs a)
 {
@@ -68,61 +77,88 @@ __global__ __launch_bounds__(256) void k_kv4_write(KvArgs a)
     const int64_t r = (int64_t)blockIdx.x * (256 / LPR) + threadIdx.x / LPR;
     if (r >= a.rows) return;
     const bool val = blockIdx.y != 0;
-    const int64_t t = r / a.H;
-    const int h = (int)(r - t * a.H);
-    const int64_t slot = kv_slot(a, t);
-    if (slot < 0 || slot >= a.n_slots) {
-        if (slot >= 0 && w == 0) set_status(a.status, ISEG_DEV_RANGE);
+    const int64_t t0 = r / a.H * 4;
+    const int h = (int)(r - t0 / 4 * a.H), nt = (int)(a.T - t0 < 4 ? a.T - t0 : 4);
+    const T* x0 = val ? (const T*)a.v + h * a.v_hs : (const T*)a.k + h * a.k_hs;
+    const int64_t ld = val ? a.v_ld : a.k_ld;
+    int64_t slot[4];
+    float f[4][8];
+#pragma unroll
+    for (int q = 0; q < 4; q++) {
+        slot[q] = q < nt ? kv_slot(a, t0 + q) : -1;
+        if (slot[q] >= a.n_slots) {
+            if (w == 0) set_status(a.status, ISEG_DEV_RANGE);
+            slot[q] = -1;
+        }
+    }
+#pragma unroll
+    for (int q = 0; q < 4; q++) kv_get8(x0 + (t0 + (q < nt ? q : 0)) * ld, w * 8, a.D, f[q]);
+    uint32_t bytes[4];                                         // v: of each token
+#pragma unroll
+    for (int q = 0; q < 4; q++) {
+        uint32_t big = 0;
+#pragma unroll
+        for (int i = 0; i < 8; i++) {
+            const uint32_t b = bits_of(f[q][i]);
+            big = b > big ? b : big;
+        }
+#pragma unroll
+        for (int o = LPR / 2; o > 0; o >>= 1) {
+            const uint32_t b = (uint32_t)__shfl_xor((int)big, o, 64);
+            big = b > big ? b : big;
+        }
+        float s = kKvScaleMin;
+        if (big) s = scale_of(bits_of((double)__builtin_bit_cast(float, big)), 4, a.mode);
+        if (s < kKvScaleMin) s = kKvScaleMin;                  // a NaN stays
+        const Coder cd(s);
+        uint32_t n[2];
+        codes_of<8, false>(f[q], nullptr, [&](int) -> const Coder& { return cd; }, 7, n);
+        if (!cd.ok) {
+            n[0] = n[1] = 0;
+            if (w == 0 && slot[q] >= 0) set_status(a.status, ISEG_DEV_NONFINITE);
+        }
+        // bytes n in [-7, 7] to n + 8
+        n[0] = (n[0] & 0x0f0f0f0fu) ^ 0x08080808u;
+        n[1] = (n[1] & 0x0f0f0f0fu) ^ 0x08080808u;
+        if (!val) {
+            if (slot[q] < 0) continue;
+            const KvPlace p = kv_place(a, slot[q], h);
+            // even codes in the low half, odd ones in the high half
+            uint32_t word = 0;
+#pragma unroll
+            for (int e = 0; e < 8; e++) word |= ((n[e >> 2] >> (8 * (e & 3))) & 15u) << ((e & 1) * 16 + (e >> 1) * 4);
+            if (w < words) *(uint32_t*)(a.kc + p.row * (a.W / 2) + w * 4) = word;
+            if (w == 0) a.ks[p.row] = s;
+        } else {
+            // the lane without bit 1 has the low halves' columns, its partner the high ones'
+            const bool hi = w & 2;
+            const uint32_t give = hi ? n[0] : n[1], mine = hi ? n[1] : n[0];
+            const uint32_t got = (uint32_t)__shfl_xor((int)give, 2, 64);
+            bytes[q] = hi ? got | mine << 4 : mine | got << 4;
+            if (w == 0 && slot[q] >= 0) a.vs[kv_place(a, slot[q], h).row] = s;
+        }
+    }
+    if (!val || w >= words) return;
+    const int i = w >> 2, c0 = (w & 1) * 8 + ((w & 2) ? 4 : 0), nc = a.W / 32;
+    if (kv_beside(slot, a)) {
+        const KvPlace p = kv_place(a, slot[0], h);
+        uint8_t* q = a.vc + p.tile + ((c0 * 4 + (p.t >> 2)) * nc + i) * 4;
+        // four tokens' bytes of four columns to four columns' bytes of four tokens
+        const uint32_t lo01 = __builtin_amdgcn_perm(bytes[1], bytes[0], 0x05010400), lo23 = __builtin_amdgcn_perm(bytes[3], bytes[2], 0x05010400);
+        const uint32_t hi01 = __builtin_amdgcn_perm(bytes[1], bytes[0], 0x07030602), hi23 = __builtin_amdgcn_perm(bytes[3], bytes[2], 0x07030602);
+        *(uint32_t*)(q) = __builtin_amdgcn_perm(lo23, lo01, 0x05040100);
+        *(uint32_t*)(q + 16 * nc) = __builtin_amdgcn_perm(lo23, lo01, 0x07060302);
+        *(uint32_t*)(q + 32 * nc) = __builtin_amdgcn_perm(hi23, hi01, 0x05040100);
+        *(uint32_t*)(q + 48 * nc) = __builtin_amdgcn_perm(hi23, hi01, 0x07060302);
         return;
     }
-    const T* x = val ? (const T*)a.v + t * a.v_ld + h * a.v_hs : (const T*)a.k + t * a.k_ld + h * a.k_hs;
-    float f[8];
-    kv_get8(x, w * 8, a.D, f);
-    uint32_t big = 0;
 #pragma unroll
-    for (int i = 0; i < 8; i++) {
-        const uint32_t b = bits_of(f[i]);
-        big = b > big ? b : big;
-    }
+    for (int t = 0; t < 4; t++) {
+        if (slot[t] < 0) continue;
+        const KvPlace p = kv_place(a, slot[t], h);
+        uint8_t* q = a.vc + p.tile + ((c0 * 4 + (p.t >> 2)) * nc + i) * 4 + (p.t & 3);
 #pragma unroll
-    for (int o = LPR / 2; o > 0; o >>= 1) {
-        const uint32_t b = (uint32_t)__shfl_xor((int)big, o, 64);
-        big = b > big ? b : big;
-    }
-    float s = kKvScaleMin;
-    if (big) s = scale_of(bits_of((double)__builtin_bit_cast(float, big)), 4, a.mode);
-    if (s < kKvScaleMin) s = kKvScaleMin;                      // a NaN stays
-    const Coder cd(s);
-    uint32_t n[2];
-    codes_of<8, false>(f, nullptr, [&](int) -> const Coder& { return cd; }, 7, n);
-    if (!cd.ok) {
-        n[0] = n[1] = 0;
-        if (w == 0) set_status(a.status, ISEG_DEV_NONFINITE);
-    }
-    // bytes n in [-7, 7] to n + 8
-    n[0] = (n[0] & 0x0f0f0f0fu) ^ 0x08080808u;
-    n[1] = (n[1] & 0x0f0f0f0fu) ^ 0x08080808u;
-    const KvPlace p = kv_place(a, slot, h);
-    if (!val) {
-        // even codes in the low half, odd ones in the high half
-        uint32_t word = 0;
-#pragma unroll
-        for (int e = 0; e < 8; e++) word |= ((n[e >> 2] >> (8 * (e & 3))) & 15u) << ((e & 1) * 16 + (e >> 1) * 4);
-        if (w < words) *(uint32_t*)(a.kc + p.row * (a.W / 2) + w * 4) = word;
-        if (w == 0) a.ks[p.row] = s;
-    } else {
-        // the lane without bit 1 has the low halves' columns, its partner the high ones'
-        const bool hi = w & 2;
-        const uint32_t give = hi ? n[0] : n[1], mine = hi ? n[1] : n[0];
-        const uint32_t got = (uint32_t)__shfl_xor((int)give, 2, 64);
-        const uint32_t b = hi ? got | mine << 4 : mine | got << 4;
-        if (w < words) {
-            const int i = w >> 2, c0 = (w & 1) * 8 + (hi ? 4 : 0), g = p.t >> 2, j = p.t & 3, nc = a.W / 32;
-            uint8_t* q = a.vc + p.tile;
-#pragma unroll
-            for (int e = 0; e < 4; e++) q[((int64_t)((c0 + e) * 4 + g) * nc + i) * 4 + j] = (uint8_t)(b >> (8 * e));
-        }
-        if (w == 0) a.vs[p.row] = s;
+        for (int e = 0; e < 4; e++) q[16 * e * nc] = (uint8_t)(bytes[t] >> (8 * e));
     }
 }
 
@@ -133,41 +169,73 @@ __global__ __launch_bounds__(256) void k_kv4_read(KvArgs a)
     const int64_t r = (int64_t)blockIdx.x * (256 / LPR) + threadIdx.x / LPR;
     if (r >= a.rows || w >= words) return;
     const bool val = blockIdx.y != 0;
-    const int64_t t = r / a.H;
-    const int h = (int)(r - t * a.H);
-    const int64_t slot = kv_slot(a, t);
-    int n[8];
-    float s = 0.f;
+    const int64_t t0 = r / a.H * 4;
+    const int h = (int)(r - t0 / 4 * a.H), nt = (int)(a.T - t0 < 4 ? a.T - t0 : 4);
+    int64_t slot[4];
+    float s[4];
+    int n[4][8];
 #pragma unroll
-    for (int e = 0; e < 8; e++) n[e] = 0;
-    if (slot >= 0 && slot < a.n_slots) {
-        const KvPlace p = kv_place(a, slot, h);
-        if (!val) {
-            s = a.ks[p.row];
+    for (int q = 0; q < 4; q++) {
+        slot[q] = q < nt ? kv_slot(a, t0 + q) : -1;
+        if (slot[q] >= a.n_slots) {
+            if (w == 0) set_status(a.status, ISEG_DEV_RANGE);
+            slot[q] = -1;
+        }
+        s[q] = 0.f;
+#pragma unroll
+        for (int e = 0; e < 8; e++) n[q][e] = 0;
+    }
+    const int i = w >> 2, c0 = (w & 1) * 8, up = (w & 2) ? 4 : 0, nc = a.W / 32;
+    if (!val) {
+#pragma unroll
+        for (int q = 0; q < 4; q++) {
+            if (slot[q] < 0) continue;
+            const KvPlace p = kv_place(a, slot[q], h);
+            s[q] = a.ks[p.row];
             const uint32_t word = *(const uint32_t*)(a.kc + p.row * (a.W / 2) + w * 4);
 #pragma unroll
-            for (int e = 0; e < 8; e++) n[e] = (int)((word >> ((e & 1) * 16 + (e >> 1) * 4)) & 15u) - 8;
-        } else {
-            s = a.vs[p.row];
-            const int i = w >> 2, c0 = (w & 1) * 8, up = (w & 2) ? 4 : 0, g = p.t >> 2, j = p.t & 3, nc = a.W / 32;
-            const uint8_t* q = a.vc + p.tile;
-#pragma unroll
-            for (int e = 0; e < 8; e++) n[e] = (int)((q[((int64_t)((c0 + e) * 4 + g) * nc + i) * 4 + j] >> up) & 15) - 8;
+            for (int e = 0; e < 8; e++) n[q][e] = (int)((word >> ((e & 1) * 16 + (e >> 1) * 4)) & 15u) - 8;
         }
-    } else if (slot >= 0 && w == 0) {
-        set_status(a.status, ISEG_DEV_RANGE);
-    }
-    T* out = val ? (T*)a.vo + t * a.v_ld + h * a.v_hs : (T*)a.ko + t * a.k_ld + h * a.k_hs;
-    struct { T v[8]; } o;
+    } else if (kv_beside(slot, a)) {
+        const KvPlace p = kv_place(a, slot[0], h);
+        const uint8_t* b = a.vc + p.tile + ((c0 * 4 + (p.t >> 2)) * nc + i) * 4;
+        uint32_t word[8];
 #pragma unroll
-    for (int e = 0; e < 8; e++) o.v[e] = (T)((float)n[e] * s);
-    const int d = w * 8;
-    if (d + 8 <= a.D) {
-        __builtin_memcpy(out + d, &o, sizeof(o));
+        for (int e = 0; e < 8; e++) word[e] = *(const uint32_t*)(b + 16 * e * nc);
+#pragma unroll
+        for (int q = 0; q < 4; q++) {
+            s[q] = a.vs[p.row + q];
+#pragma unroll
+            for (int e = 0; e < 8; e++) n[q][e] = (int)((word[e] >> (8 * q + up)) & 15u) - 8;
+        }
     } else {
 #pragma unroll
-        for (int e = 0; e < 8; e++)
-            if (d + e < a.D) out[d + e] = o.v[e];
+        for (int q = 0; q < 4; q++) {
+            if (slot[q] < 0) continue;
+            const KvPlace p = kv_place(a, slot[q], h);
+            s[q] = a.vs[p.row];
+            const uint8_t* b = a.vc + p.tile + ((c0 * 4 + (p.t >> 2)) * nc + i) * 4 + (p.t & 3);
+#pragma unroll
+            for (int e = 0; e < 8; e++) n[q][e] = (int)((b[16 * e * nc] >> up) & 15) - 8;
+        }
+    }
+    T* out = val ? (T*)a.vo + h * a.v_hs : (T*)a.ko + h * a.k_hs;
+    const int64_t ld = val ? a.v_ld : a.k_ld;
+    const int d = w * 8;
+#pragma unroll
+    for (int q = 0; q < 4; q++) {
+        if (q >= nt) break;
+        struct { T v[8]; } o;
+#pragma unroll
+        for (int e = 0; e < 8; e++) o.v[e] = (T)((float)n[q][e] * s[q]);
+        T* to = out + (t0 + q) * ld;
+        if (d + 8 <= a.D) {
+            __builtin_memcpy(to + d, &o, sizeof(o));
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; e++)
+                if (d + e < a.D) to[d + e] = o.v[e];
+        }
     }
 }
 
@@ -183,7 +251,7 @@ int kv_check(const iseg_kv4_geom* g)
 KvArgs kv_args(const iseg_kv4_geom* g, const void* slots, int32_t* status)
 {
     KvArgs a = {};
-    a.slots = slots; a.rows = g->T * g->H;
+    a.slots = slots; a.T = g->T; a.rows = ceil_div64(g->T, 4) * g->H;
     a.k_ld = g->k_ld; a.k_hs = g->k_hs; a.v_ld = g->v_ld; a.v_hs = g->v_hs;
     a.n_slots = g->n_pages * g->page; a.H = (int32_t)g->H; a.D = (int32_t)g->D; a.W = kv4_width(g->D); a.page = g->page;
     a.slot64 = g->slot_dtype == ISEG_I64; a.mode = g->scale_mode; a.status = status;

@@ -10,6 +10,7 @@
 namespace {
 
 constexpr int kTableMax = 2048;      // sines and cosines of a block (16 KB of LDS)
+constexpr int kBwdBlocks = 1024;     // of the backward, each with partial sums of gamma's gradient
 
 struct QrSide {                      // one of q and k
     const void *x, *dy, *gamma;
@@ -284,25 +285,28 @@ __global__ __launch_bounds__(256) void k_qk_norm_rope(QrArgs a)
     }
 }
 
-// gamma's gradient: the blocks' partial sums in their order, eight runs of them
-// side by side.  blockIdx.y: q or k.
+// gamma's gradient: the blocks' partial sums, 64 runs of them side by side, each
+// in its order and then the runs in theirs.  blockIdx.y: q or k.
 template <typename P>
-__global__ __launch_bounds__(256) void k_qk_dgamma(QrArgs a)
+__global__ __launch_bounds__(1024) void k_qk_dgamma(QrArgs a)
 {
-    __shared__ float red[8][32];
+    __shared__ float red[64][16];
     const QrSide& sd = a.side[blockIdx.y];
     if (!sd.dgamma) return;
-    const int c = threadIdx.x & 31, seg = threadIdx.x >> 5, d = blockIdx.x * 32 + c;
+    const int c = threadIdx.x & 15, seg = threadIdx.x >> 4, d = blockIdx.x * 16 + c;
+    const int per = (sd.blocks + 63) / 64, b0 = seg * per;
     float s = 0.f;
     if (d < a.D) {
-        const int per = (sd.blocks + 7) / 8, b1 = min(sd.blocks, (seg + 1) * per);
-        for (int b = seg * per; b < b1; b++) s += sd.part[(int64_t)b * a.D + d];
+        float v[kBwdBlocks / 64];
+#pragma unroll
+        for (int i = 0; i < kBwdBlocks / 64; i++) v[i] = i < per && b0 + i < sd.blocks ? sd.part[(int64_t)(b0 + i) * a.D + d] : 0.f;
+#pragma unroll
+        for (int i = 0; i < kBwdBlocks / 64; i++) s += v[i];
     }
     red[seg][c] = s;
     __syncthreads();
     if (seg == 0 && d < a.D) {
-#pragma unroll
-        for (int i = 1; i < 8; i++) s += red[i][c];
+        for (int i = 1; i < 64; i++) s += red[i][c];
         ((P*)sd.dgamma)[d] = (P)s;
     }
 }
@@ -319,8 +323,6 @@ int qr_check(const iseg_qk_norm_rope_geom* g)
     if ((g->Hq > 0 && (g->q_ld < 0 || g->q_hs < 0)) || (g->Hk > 0 && (g->k_ld < 0 || g->k_hs < 0))) return ISEG_ERR_SHAPE;
     return g->D <= 512 && g->Hq <= 65536 && g->Hk <= 65536 ? ISEG_OK : ISEG_ERR_UNSUPPORTED;
 }
-
-constexpr int kBwdBlocks = 1024;
 
 // tokens of a block's turn: about 128 rows, whose table fits, and blocks for
 // the whole card from few tokens
@@ -346,7 +348,7 @@ int qr_launch(const QrArgs& a, hipStream_t s)
     const int b = a.side[0].blocks > a.side[1].blocks ? a.side[0].blocks : a.side[1].blocks;
     if (b > 0) hipLaunchKernelGGL((k_qk_norm_rope<T, P, N, LPR, SPL, BWD>), dim3((unsigned)b, 2), dim3(256), 0, s, a);
     if (BWD && (a.side[0].dgamma || a.side[1].dgamma))
-        hipLaunchKernelGGL((k_qk_dgamma<P>), dim3((unsigned)ceil_div64(a.D, 32), 2), dim3(256), 0, s, a);
+        hipLaunchKernelGGL((k_qk_dgamma<P>), dim3((unsigned)ceil_div64(a.D, 16), 2), dim3(1024), 0, s, a);
     return launch_ok();
 }
 

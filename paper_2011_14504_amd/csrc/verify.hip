@@ -20,6 +20,7 @@ struct VfArgs {
     const float *u, *us;
     int32_t *out, *accepted;
     double* sums;                        // [B][parts][2]: of the remainder, of the target
+    int32_t* said;                       // [B]: twice the accepted drafts, and 1 if one was refused
     int64_t S, V, t_bs, t_ld, d_bs, d_ld, part;
     int32_t parts, tok64;
     int32_t* status;
@@ -128,6 +129,7 @@ __global__ __launch_bounds__(256) void k_verify_sums(VfArgs a)
     }
     if (odd) bad |= ISEG_DEV_NONFINITE;
     if (bad) set_status(a.status, bad);
+    if (part == 0 && threadIdx.x == 0) a.said[b] = (int32_t)(acc * 2 + refused);
     sr = wave_sum_f64(sr);
     sp = wave_sum_f64(sp);
     if ((threadIdx.x & 63) == 0) { red[0][threadIdx.x >> 6] = sr; red[1][threadIdx.x >> 6] = sp; }
@@ -138,111 +140,150 @@ __global__ __launch_bounds__(256) void k_verify_sums(VfArgs a)
     }
 }
 
-// sum of v over the threads before this one, of 256
-__device__ __forceinline__ double before_f64(double v, double* red)
+// sum of v over the lanes up to this one
+__device__ __forceinline__ double wave_scan_f64(double v)
 {
-    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-    double s = v;
+    const int lane = threadIdx.x & 63;
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) {
-        const double t = __shfl_up(s, o, 64);
-        if (lane >= o) s += t;
+        const double t = __shfl_up(v, o, 64);
+        if (lane >= o) v += t;
     }
-    __syncthreads();
-    if (lane == 63) red[w] = s;
-    __syncthreads();
-    const double t = __shfl_up(s, 1, 64);
-    s = lane ? t : 0.0;
-    for (int i = 0; i < w; i++) s += red[i];
-    return s;
+    return v;
 }
 
-// a block per request: the part, then the element.  Both walk runs of
-// consecutive values, one run a thread.
+// A block per request: the part, then the element.  Where u is below 1 the first
+// part whose running sum passes u times the whole has the token; should rounding
+// leave none, the last value with any mass is taken.
 template <typename T>
 __global__ __launch_bounds__(256) void k_verify_pick(VfArgs a)
 {
-    __shared__ double red[4];
-    __shared__ double first_sum;
+    constexpr int N = RowVec<T>::N, K = 32 / N;          // vectors of a thread in a turn of 8192 values
+    __shared__ double total[2], from[4], seg[4][K];
     __shared__ int first, last;
     const int64_t b = blockIdx.x;
-    int bad = 0;
-    bool refused;
-    const int64_t acc = vf_accepted<T>(a, b, refused, bad);
-    const VfRow<T> row = vf_row<T>(a, b, acc, refused);
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t said = a.said[b], acc = said >> 1;
+    const VfRow<T> row = vf_row<T>(a, b, acc, said & 1);
     const double* sums = a.sums + b * a.parts * 2;
-    const int run = (a.parts + 255) / 256;           // <= 4
-    double mine[4], all = 0.0;
-    // the remainder, or the target's row where nothing remains
-    int col = 0;
-    for (;; col++) {
+    int bad = 0;
+
+    // the parts: runs of four a thread
+    double mine[2][4], pre[2];
+#pragma unroll
+    for (int c = 0; c < 2; c++) {
         double s = 0.0;
 #pragma unroll
         for (int i = 0; i < 4; i++) {
-            const int k = (int)threadIdx.x * run + i;
-            mine[i] = i < run && k < a.parts ? sums[2 * k + col] : 0.0;
-            s += mine[i];
+            const int k = (int)threadIdx.x * 4 + i;
+            mine[c][i] = k < a.parts ? sums[2 * k + c] : 0.0;
+            s += mine[c][i];
         }
-        const double pre = before_f64(s, red);
-        if (threadIdx.x == 255) first_sum = pre + s;
-        if (threadIdx.x == 0) { first = 0x7fffffff; last = -1; }
-        __syncthreads();
-        all = first_sum;
-        if (all > 0.0 || col == 1) {
-            double t = (double)a.us[b] * all;
-            t = t > 0.0 ? t : 0.0;
-            double c = pre;
-            int hit = 0x7fffffff, pos = -1;
-            double at = 0.0;
-#pragma unroll
-            for (int i = 0; i < 4; i++) {
-                const int k = (int)threadIdx.x * run + i;
-                if (mine[i] > 0.0) {
-                    pos = k;
-                    if (hit == 0x7fffffff && c + mine[i] > t) { hit = k; at = c; }
-                }
-                c += mine[i];
-            }
-            if (hit != 0x7fffffff) atomicMin(&first, hit);
-            if (pos >= 0) atomicMax(&last, pos);
-            __syncthreads();
-            if (hit == first && hit != 0x7fffffff) first_sum = at;
-            break;
-        }
-        __syncthreads();
+        pre[c] = wave_scan_f64(s);
+        if (lane == 63) seg[wave][c] = pre[c];
+        pre[c] -= s;
     }
-    const bool any = all > 0.0;
-    double t = (double)a.us[b] * all;
-    t = t > 0.0 ? t : 0.0;
-    __syncthreads();
-    const bool found = first != 0x7fffffff;
-    const int64_t part = found ? first : last;
-    t = found ? t - first_sum : __builtin_inf();     // none: the last value with any mass
-    __syncthreads();
     if (threadIdx.x == 0) { first = 0x7fffffff; last = -1; }
-    int64_t token = -1;
-    if (any && part >= 0) {
-        const int64_t v0 = part * a.part, v1 = v0 + a.part < a.V ? v0 + a.part : a.V;
-        const int64_t per = (v1 - v0 + 255) / 256;
-        const int64_t s0 = v0 + (int64_t)threadIdx.x * per, s1 = s0 + per < v1 ? s0 + per : v1;
-        auto value = [&](int64_t v) {
-            const float pf = (float)row.p[v];
-            if (col) return (double)pf;
-            return left_of(pf, row.q ? (float)row.q[v] : (v == row.sure ? 1.f : 0.f));
-        };
-        double s = 0.0;
-        for (int64_t v = s0; v < s1; v++) s += value(v);
-        double c = before_f64(s, red);
+    __syncthreads();
+    if (threadIdx.x < 2) total[threadIdx.x] = seg[0][threadIdx.x] + seg[1][threadIdx.x] + seg[2][threadIdx.x] + seg[3][threadIdx.x];
+    __syncthreads();
+    const int col = total[0] > 0.0 ? 0 : 1;              // the target's row where nothing remains
+    double t = (double)a.us[b] * total[col];
+    t = t > 0.0 ? t : 0.0;
+    {
+        double c = col ? pre[1] : pre[0];
+        for (int i = 0; i < wave; i++) c += seg[i][col];
         int hit = 0x7fffffff, pos = -1;
-        for (int64_t v = s0; v < s1; v++) {
-            const double w = value(v);
-            c += w;
+        double at = 0.0;
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+            const double w = col ? mine[1][i] : mine[0][i];
+            const int k = (int)threadIdx.x * 4 + i;
             if (w > 0.0) {
-                pos = (int)(v - v0);
-                if (hit == 0x7fffffff && c > t) hit = pos;
+                pos = k;
+                if (hit == 0x7fffffff && c + w > t) { hit = k; at = c; }
             }
+            c += w;
         }
         if (hit != 0x7fffffff) atomicMin(&first, hit);
+        if (pos >= 0) atomicMax(&last, pos);
+        __syncthreads();
+        if (hit == first && hit != 0x7fffffff) from[0] = at;
+    }
+    __syncthreads();
+    const int64_t part = first != 0x7fffffff ? first : last;
+    t = first != 0x7fffffff ? t - from[0] : __builtin_inf();
+    const bool any = total[col] > 0.0 && part >= 0;
+    __syncthreads();
+    if (threadIdx.x == 0) { first = 0x7fffffff; last = -1; }
+
+    // the element: turns of 8192 values, a quarter a wave, in vectors; the sums of
+    // a wave's 64 N values first, then the lanes of the one that passes t
+    int64_t token = -1;
+    if (any) {
+        const int64_t v0 = part * a.part, v1 = v0 + a.part < a.V ? v0 + a.part : a.V;
+        double base = 0.0;
+        int pos = -1;                                    // this thread's last value with any mass
+        for (int64_t s0 = v0; s0 < v1; s0 += 8192) {
+            double w[K][N], s[K];
+#pragma unroll
+            for (int k = 0; k < K; k++) {
+                const int64_t v = s0 + ((int64_t)(wave * K + k) * 64 + lane) * N;
+                RowVec<T> p, q;
+                if (v + N <= v1) {
+                    p = row_load(row.p + v);
+                    if (row.q) q = row_load(row.q + v);
+                } else {
+                    const int n = v < v1 ? (int)(v1 - v) : 0;
+                    p = row_load_part(row.p + v, n, (T)0.f);
+                    if (row.q) q = row_load_part(row.q + v, n, (T)0.f);
+                }
+                s[k] = 0.0;
+#pragma unroll
+                for (int i = 0; i < N; i++) {
+                    const float pf = (float)p.v[i], qf = row.q ? (float)q.v[i] : (v + i == row.sure ? 1.f : 0.f);
+                    w[k][i] = col ? (double)pf : left_of(pf, qf);
+                    s[k] += w[k][i];
+                    if (w[k][i] > 0.0) pos = (int)(v + i - v0);
+                }
+            }
+#pragma unroll
+            for (int k = 0; k < K; k++) {
+                const double x = wave_sum_f64(s[k]);
+                if (lane == 0) seg[wave][k] = x;
+            }
+            __syncthreads();
+            double c = base;
+            for (int i = 0; i < 4; i++)
+#pragma unroll
+                for (int k = 0; k < K; k++) {
+                    const double x = seg[i][k];
+                    if (i == wave && c <= t && c + x > t) {          // at most one piece
+                        double e = c + wave_scan_f64(s[k]) - s[k];
+                        int hit = 0x7fffffff, end = -1;
+                        const int at = (int)(s0 - v0) + ((wave * K + k) * 64 + lane) * N;
+#pragma unroll
+                        for (int n = 0; n < N; n++) {
+                            e += w[k][n];
+                            if (w[k][n] > 0.0) {
+                                end = at + n;
+                                if (hit == 0x7fffffff && e > t) hit = at + n;
+                            }
+                        }
+                        // rounding may leave none: then its last value
+                        if (__any(hit != 0x7fffffff)) {
+                            if (hit != 0x7fffffff) atomicMin(&first, hit);
+                        } else {
+                            const uint32_t top = wave_top_u32((uint32_t)(end + 1));
+                            if (lane == 0 && top) atomicMin(&first, (int)top - 1);
+                        }
+                    }
+                    c += x;
+                }
+            base = c;
+            __syncthreads();
+            if (first != 0x7fffffff) break;
+        }
         if (pos >= 0) atomicMax(&last, pos);
         __syncthreads();
         const int at = first != 0x7fffffff ? first : last;
@@ -289,7 +330,7 @@ int vf_launch(const VfArgs& a, int64_t B, hipStream_t s)
 extern "C" size_t iseg_verify_drafts_ws(const iseg_verify_geom* g)
 {
     if (vf_check(g) != ISEG_OK) return 0;
-    return ws_used((size_t)g->B * (size_t)ceil_div64(g->V, vf_part(g)) * 16);
+    return ws_used(align256((size_t)g->B * (size_t)ceil_div64(g->V, vf_part(g)) * 16) + (size_t)g->B * 4);
 }
 
 extern "C" int iseg_verify_drafts(const void* target, const void* draft, const void* tokens, const int32_t* n_draft,
@@ -307,6 +348,7 @@ extern "C" int iseg_verify_drafts(const void* target, const void* draft, const v
     a.S = g->S; a.V = g->V; a.t_bs = g->t_bs; a.t_ld = g->t_ld; a.d_bs = g->d_bs; a.d_ld = g->d_ld;
     a.part = vf_part(g);
     a.parts = (int32_t)ceil_div64(g->V, a.part);
+    a.said = (int32_t*)((char*)ws + align256((size_t)g->B * a.parts * 16));
     a.tok64 = g->token_dtype == ISEG_I64; a.status = dev_status;
     return g->dtype == ISEG_F32   ? vf_launch<float>(a, g->B, stream)
            : g->dtype == ISEG_F16 ? vf_launch<f16_t>(a, g->B, stream)
