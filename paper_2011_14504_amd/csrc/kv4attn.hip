@@ -41,17 +41,26 @@ struct KaArgs {
     int32_t* status;
 };
 
+// (w & mask) | 1024.0 in both halves, in one instruction: from registers, since
+// it takes one literal and these are two
+__device__ __forceinline__ h2_t in_1024(uint32_t w, uint32_t mask)
+{
+    uint32_t k = 0x64006400u;
+    asm("" : "+s"(mask), "+v"(k));
+    return __builtin_bit_cast(h2_t, (w & mask) | k);
+}
+
 // eight float16 of a word of K: codes n + 8 in nibbles 0 4 1 5 (and 2 6 3 7 above)
 __device__ __forceinline__ h2_t codes_lo(uint32_t w)
 {
     const h2_t k = {(_Float16)1032.f, (_Float16)1032.f};
-    return __builtin_bit_cast(h2_t, (w & 0x000f000fu) | 0x64006400u) - k;
+    return in_1024(w, 0x000f000fu) - k;
 }
 
 __device__ __forceinline__ h2_t codes_hi(uint32_t w)
 {
     const h2_t s = {(_Float16)0.0625f, (_Float16)0.0625f}, k = {(_Float16)-72.f, (_Float16)-72.f};
-    return __builtin_elementwise_fma(__builtin_bit_cast(h2_t, (w & 0x00f000f0u) | 0x64006400u), s, k);
+    return __builtin_elementwise_fma(in_1024(w, 0x00f000f0u), s, k);
 }
 
 __device__ __forceinline__ h8_t join8(h2_t a, h2_t b, h2_t c, h2_t d)
@@ -144,11 +153,11 @@ __device__ __forceinline__ void ka_span(const KaArgs& a, const KaSeq& s, int64_t
     lo = lo < 0 ? 0 : lo;
 }
 
-// four elements of an output row from d on: o / l, zeros for a row without keys
-__device__ __forceinline__ void ka_store(const KaArgs& a, int64_t tok, int64_t head, int d, f4_t o, float l)
+// four elements of an output row that starts at element `at`, from d on: o times
+// the inverse of l
+__device__ __forceinline__ void ka_store(const KaArgs& a, int64_t at, int d, f4_t o, float inv)
 {
-    const float inv = l > 0.f ? 1.f / l : (l == l ? 0.f : l);
-    const int64_t at = tok * a.o_ld + head * a.o_hs + d;
+    at += d;
     o *= inv;
     if (a.dtype == ISEG_F32) {
         __builtin_memcpy((float*)a.out + at, &o, 16);
@@ -161,25 +170,43 @@ __device__ __forceinline__ void ka_store(const KaArgs& a, int64_t tok, int64_t h
     }
 }
 
+// 1 / l; 0 for a row without keys
+__device__ __forceinline__ float ka_inv(float l) { return l > 0.f ? 1.f / l : (l == l ? 0.f : l); }
+
 __device__ __forceinline__ float ka_lse(float m, float l)
 {
     return l > 0.f || l != l ? (m + __builtin_amdgcn_logf(l)) * 0.69314718f : -__builtin_inff();
 }
 
-// four elements of row `r` of a tile from d on: the whole, or a split's part
+// Where row r of a tile goes: its place among the parts, or its output row.
+struct KaOut {
+    int64_t at;                          // part, or first element of the output row
+    float inv;                           // outputs: 1 / l
+};
+
+// `one`: this thread writes the row's m and l, or its lse
 template <int TR>
-__device__ __forceinline__ void ka_put(const KaArgs& a, const KaSeq& s, int tile, int h, int split, int64_t row0, int r, int d, f4_t o,
-                                       float m, float l)
+__device__ __forceinline__ KaOut ka_row(const KaArgs& a, const KaSeq& s, int tile, int h, int split, int64_t row0, int r, float m, float l,
+                                        bool one)
 {
+    KaOut o;
     if (a.splits > 1) {
-        const int64_t at = (((int64_t)tile * a.H + h) * TR + r) * a.splits + split;
-        *(f4_t*)(a.po + at * a.W + d) = o;
-        if (d == 0) { a.pm[at * 2] = m; a.pm[at * 2 + 1] = l; }
-        return;
+        o.at = (((int64_t)tile * a.H + h) * TR + r) * a.splits + split;
+        o.inv = 0.f;
+        if (one) { a.pm[o.at * 2] = m; a.pm[o.at * 2 + 1] = l; }
+    } else {
+        const int64_t q = (row0 + r) / a.G, tok = s.q0 + q, head = h * a.G + (row0 + r - q * a.G);
+        o.at = tok * a.o_ld + head * a.o_hs;
+        o.inv = ka_inv(l);
+        if (one && a.lse) a.lse[tok * a.Hq + head] = ka_lse(m, l);
     }
-    const int64_t tok = s.q0 + (row0 + r) / a.G, head = h * a.G + (row0 + r) % a.G;
-    if (d < a.D) ka_store(a, tok, head, d, o, l);
-    if (d == 0 && a.lse) a.lse[tok * a.Hq + head] = ka_lse(m, l);
+    return o;
+}
+
+__device__ __forceinline__ void ka_put(const KaArgs& a, const KaOut& o, int d, f4_t v)
+{
+    if (a.splits > 1) *(f4_t*)(a.po + o.at * a.W + d) = v;
+    else if (d < a.D) ka_store(a, o.at, d, v, o.inv);
 }
 
 template <int NC>
@@ -214,51 +241,53 @@ struct KaRows {
             lo[t] = (int32_t)l0;
             hi[t] = (int32_t)h0;
             const int64_t at = in ? (s.q0 + r / a.G) * a.q_ld + (h * a.G + r % a.G) * a.q_hs : 0;
-            float f[NC][8];
-            float big = 0.f;
-#pragma unroll
-            for (int w = 0; w < NC; w++) {
+            auto get = [&](int w, float (&f)[8]) {
                 const int d = g4 * 8 * NC + w * 8;
 #pragma unroll
-                for (int i = 0; i < 8; i++) f[w][i] = 0.f;
-                if (in && d < a.D) {
-                    if (WIDE) {
-                        float x[8];
-                        __builtin_memcpy(x, (const float*)a.q + at + d, 32);
+                for (int i = 0; i < 8; i++) f[i] = 0.f;
+                if (!(in && d < a.D)) return;
+                if (WIDE) {
+                    __builtin_memcpy(f, (const float*)a.q + at + d, 32);
+                } else if (a.dtype == ISEG_F16) {
+                    _Float16 x[8];
+                    __builtin_memcpy(x, (const _Float16*)a.q + at + d, 16);
 #pragma unroll
-                        for (int i = 0; i < 8; i++) f[w][i] = x[i];
-                    } else if (a.dtype == ISEG_F16) {
-                        _Float16 x[8];
-                        __builtin_memcpy(x, (const _Float16*)a.q + at + d, 16);
+                    for (int i = 0; i < 8; i++) f[i] = (float)x[i];
+                } else {
+                    __bf16 x[8];
+                    __builtin_memcpy(x, (const __bf16*)a.q + at + d, 16);
 #pragma unroll
-                        for (int i = 0; i < 8; i++) f[w][i] = (float)x[i];
-                    } else {
-                        __bf16 x[8];
-                        __builtin_memcpy(x, (const __bf16*)a.q + at + d, 16);
-#pragma unroll
-                        for (int i = 0; i < 8; i++) f[w][i] = (float)x[i];
-                    }
+                    for (int i = 0; i < 8; i++) f[i] = (float)x[i];
                 }
-#pragma unroll
-                for (int i = 0; i < 8; i++) big = fmaxf(big, fabsf(f[w][i]));
-            }
+            };
             // float16 reaches no further than 65504 and 2^-24: rows of the other
             // types are brought below 1 by a power of two first
             int e = 0;
             if (WIDE || a.dtype != ISEG_F16) {
+                float big = 0.f;
+#pragma unroll
+                for (int w = 0; w < NC; w++) {
+                    float f[8];
+                    get(w, f);
+#pragma unroll
+                    for (int i = 0; i < 8; i++) big = fmaxf(big, fabsf(f[i]));
+                }
                 big = max4(big);
                 if (big > 0.f && big <= 3.4028234e38f) (void)frexpf(big, &e);
                 e = e < -100 ? -100 : e;
             }
             cf[t] = fmaxf(ldexpf(a.scale, e), 1.17549435e-38f);      // never 0: a masked score is -infinity times this
 #pragma unroll
-            for (int w = 0; w < NC; w++)
+            for (int w = 0; w < NC; w++) {
+                float f[8];
+                get(w, f);
 #pragma unroll
                 for (int i = 0; i < 8; i++) {
-                    const float x = ldexpf(f[w][i], -e);
+                    const float x = ldexpf(f[i], -e);
                     q[0][t][w][i] = (_Float16)x;
                     if constexpr (WIDE) q[NS - 1][t][w][i] = (_Float16)(x - (float)(_Float16)x);
                 }
+            }
             m[t] = kNone;
             l[t] = 0.f;
 #pragma unroll
@@ -283,19 +312,26 @@ struct KaRows {
     // tiles' scales, whether a tile is there (ok).  Leaves the weights as B
     // operands of V^T P^T in the order of V's words (tokens 0 2 1 3).
     template <int NT>
-    __device__ __forceinline__ void soften(f4_t (&st)[R][NT], const f4_t* ks, f4_t* vs, const bool* ok, int32_t kb,
+    __device__ __forceinline__ void soften(f4_t (&st)[R][NT], f4_t (&ks)[NT], f4_t (&vs)[NT], const bool (&ok)[NT], int32_t kb,
                                            int32_t kv, h8_t (&pf)[NS][R][NT / 2])
     {
         const int g4 = (threadIdx.x & 63) >> 4;
         bool full = kb >= full_lo && kb + 16 * NT <= full_hi;
 #pragma unroll
         for (int i = 0; i < NT; i++) full = full && ok[i];
-        if (!full) {                                             // V's scales of no key count as 0
+        if (!full) {
+            // a weight of 0 times any scale has to be 0: scales of v of no key count
+            // as 0, and those that are no number go to the scores that see them
 #pragma unroll
             for (int i = 0; i < NT; i++)
 #pragma unroll
-                for (int r = 0; r < 4; r++)
+                for (int r = 0; r < 4; r++) {
+                    if (!(vs[i][r] <= 3.4028234e38f)) {
+                        vs[i][r] = 0.f;
+                        ks[i][r] = __builtin_nanf("");
+                    }
                     if (!(ok[i] && kb + 16 * i + 4 * g4 + r < kv)) vs[i][r] = 0.f;
+                }
         }
         float top = 0.f;
 #pragma unroll
@@ -318,6 +354,21 @@ struct KaRows {
 #pragma unroll
         for (int i = 0; i < NT; i++) vs[i] *= v_inv;
 
+#pragma unroll
+        for (int t = 0; t < R; t++)
+#pragma unroll
+            for (int i = 0; i < NT; i++) st[t][i] *= ks[i];
+        if (!full) {
+#pragma unroll
+            for (int t = 0; t < R; t++)
+#pragma unroll
+                for (int i = 0; i < NT; i++)
+#pragma unroll
+                    for (int r = 0; r < 4; r++) {
+                        const int32_t j = kb + 16 * i + 4 * g4 + r;
+                        if (!(ok[i] && j >= lo[t] && j < hi[t])) st[t][i][r] = -__builtin_inff();
+                    }
+        }
         float mx[R];
         bool move = false;
 #pragma unroll
@@ -326,15 +377,7 @@ struct KaRows {
 #pragma unroll
             for (int i = 0; i < NT; i++)
 #pragma unroll
-                for (int r = 0; r < 4; r++) {
-                    float v = st[t][i][r] * ks[i][r];
-                    if (!full) {
-                        const int32_t j = kb + 16 * i + 4 * g4 + r;
-                        if (!(ok[i] && j >= lo[t] && j < hi[t])) v = -__builtin_inff();
-                    }
-                    st[t][i][r] = v;
-                    mx[t] = fmaxf(mx[t], v);
-                }
+                for (int r = 0; r < 4; r++) mx[t] = fmaxf(mx[t], st[t][i][r]);
             move = move || mx[t] * cf[t] > m[t] + kRoom;
         }
         if (__any(move)) {
@@ -358,12 +401,14 @@ struct KaRows {
                     const float v = __builtin_amdgcn_exp2f(fmaf(st[t][i][r], cf[t], -m[t]));
                     l[t] += v;
                     p[r] = v * vs[i][r];
-                    if (!full && st[t][i][r] == -__builtin_inff()) p[r] = 0.f;         // a masked key's scale may be anything
                 }
                 constexpr int order[4] = {0, 2, 1, 3};
 #pragma unroll
                 for (int r = 0; r < 4; r++) {
-                    const float v = p[order[r]];
+                    float v = p[order[r]];
+                    // the product is rounded once for both terms (contracted with one of
+                    // them it would not be the same number)
+                    if constexpr (WIDE) asm("" : "+v"(v));
                     pf[0][t][i / 2][4 * (i & 1) + r] = (_Float16)v;
                     if constexpr (WIDE) pf[NS - 1][t][i / 2][4 * (i & 1) + r] = (_Float16)(v - (float)(_Float16)v);
                 }
@@ -414,20 +459,20 @@ struct KaTiles {
     __device__ __forceinline__ int at(int it, int i) const { return __builtin_amdgcn_readlane(idx, (it % N) * PER + i); }
 };
 
+// waves per SIMD whose registers the rows leave room for
+constexpr int ka_few_waves(int nc, int r, bool wide)
+{
+    const int n = (wide ? 2 : 1) * r * nc;
+    return n <= 1 ? 4 : n <= 4 && r < 4 ? 3 : n <= 8 && nc < 8 ? 2 : 1;
+}
+
 // ---------------------------------------------------------------------------
 // few rows: the four waves of a block hold the same rows and deal the keys among
 // themselves
 // ---------------------------------------------------------------------------
-template <int NC>
-struct KaKeys {                          // 32 keys of one head: a lane's words and scales
-    uint32_t k[2][NC], v[2][NC];
-    f4_t ks[2], vs[2];
-    bool ok[2];
-};
-
 // NC: words of a row's quarter (W / 32).  R: tiles of 16 rows.
 template <int NC, int R, bool WIDE>
-__global__ __launch_bounds__(256) void k_kv4_few(KaArgs a)
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(ka_few_waves(NC, R, WIDE)))) void k_kv4_few(KaArgs a)
 {
     constexpr int W = NC * 32, TR = 16 * R;
     __shared__ float so[4 * 16 * (W + 4)];
@@ -452,27 +497,39 @@ __global__ __launch_bounds__(256) void k_kv4_few(KaArgs a)
     const int32_t n_it = it0 + per < steps ? per : (steps > it0 ? steps - it0 : 0);
     const int32_t key0 = k_lo + it0 * 128 + wave * 32;
 
+    // the words of 32 keys; the next step's keys are requested once the scores are
+    // there, its values once they are summed up
     KaTiles<2, 8> tl = {a.table + b * a.table_ld, key0 >> 4, (kv + 15) >> 4, -1};
-    KaKeys<NC> nx;
-    auto fetch = [&](int it) {
+    uint32_t kw[2][NC], vw[2][NC];
+    f4_t ks_next[2], vs_next[2];
+    auto fetch_k = [&](int it) {
         if (it % tl.N == 0) tl.look(a, h, it);
 #pragma unroll
         for (int i = 0; i < 2; i++) {
             const int ti = tl.at(it, i);
-            nx.ok[i] = ti >= 0;
             const int64_t at = ti >= 0 ? ti : 0;
-            words<NC>(a.kc + at * (256 * NC) + (c * 4 + g4) * (4 * NC), nx.k[i]);
-            words<NC>(a.vc + at * (256 * NC) + (c * 4 + g4) * (4 * NC), nx.v[i]);
-            nx.ks[i] = *(const f4_t*)(a.ks + at * 16 + g4 * 4);
-            nx.vs[i] = *(const f4_t*)(a.vs + at * 16 + g4 * 4);
+            words<NC>(a.kc + at * (256 * NC) + (c * 4 + g4) * (4 * NC), kw[i]);
+            ks_next[i] = *(const f4_t*)(a.ks + at * 16 + g4 * 4);
+            vs_next[i] = *(const f4_t*)(a.vs + at * 16 + g4 * 4);
         }
     };
-    if (n_it > 0) fetch(0);
+    auto fetch_v = [&](int it) {
+#pragma unroll
+        for (int i = 0; i < 2; i++) {
+            const int ti = tl.at(it, i);
+            const int64_t at = ti >= 0 ? ti : 0;
+            words<NC>(a.vc + at * (256 * NC) + (c * 4 + g4) * (4 * NC), vw[i]);
+        }
+    };
+    if (n_it > 0) {
+        fetch_k(0);
+        fetch_v(0);
+    }
     for (int it = 0; it < n_it; it++) {
-        KaKeys<NC> y = nx;
-        if (it + 1 < n_it) fetch(it + 1);
         const int32_t kb = key0 + it * 128;
         if (kb >= x.any_hi) break;
+        const bool ok[2] = {tl.at(it, 0) >= 0, tl.at(it, 1) >= 0};
+        const bool more = it + 1 < n_it;
         f4_t st[R][2];
 #pragma unroll
         for (int i = 0; i < 2; i++) {
@@ -480,18 +537,21 @@ __global__ __launch_bounds__(256) void k_kv4_few(KaArgs a)
             for (int t = 0; t < R; t++) st[t][i] = f4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int w = 0; w < NC; w++) {
-                const uint32_t u = y.k[i][w], v = u >> 8;
+                const uint32_t u = kw[i][w], v = u >> 8;
                 x.score(join8(codes_lo(u), codes_hi(u), codes_lo(v), codes_hi(v)), w, i, st);
             }
         }
+        f4_t ks[2] = {ks_next[0], ks_next[1]}, vs[2] = {vs_next[0], vs_next[1]};
+        if (more) fetch_k(it + 1);
         h8_t pf[x.NS][R][1];
-        x.soften(st, y.ks, y.vs, y.ok, kb, kv, pf);
+        x.soften(st, ks, vs, ok, kb, kv, pf);
 #pragma unroll
         for (int w = 0; w < NC; w++) {
-            const uint32_t a0 = y.v[0][w], a1 = y.v[1][w], b0 = a0 >> 8, b1 = a1 >> 8;
+            const uint32_t a0 = vw[0][w], a1 = vw[1][w], b0 = a0 >> 8, b1 = a1 >> 8;
             x.add(join8(codes_lo(a0), codes_lo(b0), codes_lo(a1), codes_lo(b1)), 2 * w, 0, pf);
             x.add(join8(codes_hi(a0), codes_hi(b0), codes_hi(a1), codes_hi(b1)), 2 * w + 1, 0, pf);
         }
+        if (more) fetch_v(it + 1);
     }
 
     // the waves' rows joined, a tile of 16 at a time: the whole, or this split's part
@@ -524,7 +584,7 @@ __global__ __launch_bounds__(256) void k_kv4_few(KaArgs a)
                 o += f * *(const f4_t*)(so + (w * 16 + r) * (W + 4) + d);
                 lr += f * sl[w][r];
             }
-            ka_put<TR>(a, s, tile, h, split, 0, t * 16 + r, d, o, mr, lr);
+            ka_put(a, ka_row<TR>(a, s, tile, h, split, 0, t * 16 + r, mr, lr, d == 0), d, o);
         }
     }
 }
@@ -660,8 +720,9 @@ __global__ __launch_bounds__(512) void k_kv4_many(KaArgs a)
         const float l = sum4(x.l[t]);
         const int r = wave * 16 * R + t * 16 + c;
         if (row0 + r >= rows) continue;
+        const KaOut o = ka_row<TR>(a, s, tile, h, split, row0, r, x.m[t], l, g4 == 0);
 #pragma unroll
-        for (int i = 0; i < 2 * NC; i++) ka_put<TR>(a, s, tile, h, split, row0, r, i * 16 + g4 * 4, x.acc[t][i] * v_out, x.m[t], l);
+        for (int i = 0; i < 2 * NC; i++) ka_put(a, o, i * 16 + g4 * 4, x.acc[t][i] * v_out);
     }
 }
 
@@ -720,7 +781,7 @@ __global__ __launch_bounds__(256) void k_kv4_join(KaArgs a)
     if (grp == 0 && d < a.D) {
         for (int g = 1; g < groups; g++) o += red[g * lw + threadIdx.x];
         const int64_t tok = s.q0 + (row0 + r) / a.G, head = h * a.G + (row0 + r) % a.G;
-        ka_store(a, tok, head, d, o, lsum);
+        ka_store(a, tok * a.o_ld + head * a.o_hs, d, o, ka_inv(lsum));
     }
 }
 
