@@ -131,11 +131,12 @@ __device__ __forceinline__ bool ka_tile(const KaArgs& a, int tile, KaSeq& s, int
         const uint64_t m = __ballot(base + sum > tile);
         if (m) {
             const int at = __builtin_ctzll(m);
-            const int64_t end = base + __shfl(sum, at, 64);
+            // uniform, and to be seen as such: branches on them are scalar
+            const int32_t back = __builtin_amdgcn_readfirstlane((int32_t)(base + __shfl(sum, at, 64) - 1 - tile));
             b = b0 + at;
             int ignored = 0;
             s = ka_seq(a, b, ignored);
-            row0 = (end - 1 - tile) * TR;
+            row0 = (int64_t)back * TR;
             return true;
         }
         base += __shfl(sum, 63, 64);
@@ -209,10 +210,40 @@ __device__ __forceinline__ void ka_put(const KaArgs& a, const KaOut& o, int d, f
     else if (d < a.D) ka_store(a, o.at, d, v, o.inv);
 }
 
-template <int NC>
-__device__ __forceinline__ void words(const uint8_t* p, uint32_t* w)
+// eight elements of q's row that starts at element `at`, from d on, or zeros
+template <bool WIDE>
+__device__ __forceinline__ void ka_get8(const KaArgs& a, int64_t at, int d, bool in, float (&f)[8])
 {
-    __builtin_memcpy(w, __builtin_assume_aligned(p, NC % 4 == 0 ? 16 : NC % 2 == 0 ? 8 : 4), NC * 4);
+#pragma unroll
+    for (int i = 0; i < 8; i++) f[i] = 0.f;
+    if (!in) return;
+    if (WIDE) {
+        __builtin_memcpy(f, (const float*)a.q + at + d, 32);
+    } else if (a.dtype == ISEG_F16) {
+        _Float16 x[8];
+        __builtin_memcpy(x, (const _Float16*)a.q + at + d, 16);
+#pragma unroll
+        for (int i = 0; i < 8; i++) f[i] = (float)x[i];
+    } else {
+        __bf16 x[8];
+        __builtin_memcpy(x, (const __bf16*)a.q + at + d, 16);
+#pragma unroll
+        for (int i = 0; i < 8; i++) f[i] = (float)x[i];
+    }
+}
+
+// a lane's words of a tile
+template <int NC>
+struct KaWords {
+    uint32_t w[NC];
+};
+
+template <int NC>
+__device__ __forceinline__ KaWords<NC> words(const uint8_t* p)
+{
+    KaWords<NC> r;
+    __builtin_memcpy(&r, __builtin_assume_aligned(p, NC % 4 == 0 ? 16 : NC % 2 == 0 ? 8 : 4), NC * 4);
+    return r;
 }
 
 // What a wave keeps of its 16 R rows.  WIDE: q and p as two float16 terms
@@ -243,22 +274,7 @@ struct KaRows {
             const int64_t at = in ? (s.q0 + r / a.G) * a.q_ld + (h * a.G + r % a.G) * a.q_hs : 0;
             auto get = [&](int w, float (&f)[8]) {
                 const int d = g4 * 8 * NC + w * 8;
-#pragma unroll
-                for (int i = 0; i < 8; i++) f[i] = 0.f;
-                if (!(in && d < a.D)) return;
-                if (WIDE) {
-                    __builtin_memcpy(f, (const float*)a.q + at + d, 32);
-                } else if (a.dtype == ISEG_F16) {
-                    _Float16 x[8];
-                    __builtin_memcpy(x, (const _Float16*)a.q + at + d, 16);
-#pragma unroll
-                    for (int i = 0; i < 8; i++) f[i] = (float)x[i];
-                } else {
-                    __bf16 x[8];
-                    __builtin_memcpy(x, (const __bf16*)a.q + at + d, 16);
-#pragma unroll
-                    for (int i = 0; i < 8; i++) f[i] = (float)x[i];
-                }
+                ka_get8<WIDE>(a, at, d, in && d < a.D, f);
             };
             // float16 reaches no further than 65504 and 2^-24: rows of the other
             // types are brought below 1 by a power of two first
@@ -320,6 +336,7 @@ struct KaRows {
 #pragma unroll
         for (int i = 0; i < NT; i++) full = full && ok[i];
         if (!full) {
+            asm volatile("");            // a branch: as selects these would be done for every step
             // a weight of 0 times any scale has to be 0: scales of v of no key count
             // as 0, and those that are no number go to the scores that see them
 #pragma unroll
@@ -359,6 +376,7 @@ struct KaRows {
 #pragma unroll
             for (int i = 0; i < NT; i++) st[t][i] *= ks[i];
         if (!full) {
+            asm volatile("");
 #pragma unroll
             for (int t = 0; t < R; t++)
 #pragma unroll
@@ -437,26 +455,41 @@ struct KaRows {
 };
 
 // Tiles of 16 tokens that a wave needs, PER a step, STRIDE apart from step to
-// step: looked up in the block table for many steps at a time, one lane each.
+// step: looked up in the block table for N steps at a time, one lane each, and the
+// page ids of the next N steps requested with them.
 template <int PER, int STRIDE>
 struct KaTiles {
     static constexpr int N = 64 / PER;   // steps of a look-up
     const int32_t* row;
     int32_t first, end;                  // first tile, tiles of the request
-    int idx;
-    __device__ __forceinline__ void look(const KaArgs& a, int h, int it)
+    int32_t page;                        // of the next look-up
+    int idx;                             // -1: past the keys, or a page id out of range
+    uint64_t there;                      // idx >= 0
+    __device__ __forceinline__ int32_t tile_of(int it) const
     {
         const int lane = threadIdx.x & 63;
-        const int32_t t16 = first + (it + lane / PER) * STRIDE + lane % PER;
-        idx = -1;                        // past the keys, or a page id out of range
-        if (t16 < end) {
-            const int32_t col = (int32_t)(((uint64_t)(uint32_t)t16 * a.p16_inv) >> 36);
-            const int32_t pg = row[col];
-            if (pg >= 0 && pg < a.n_pages) idx = (pg * a.H + h) * a.p16 + (t16 - col * a.p16);
-            else set_status(a.status, ISEG_DEV_RANGE);
-        }
+        return first + (it + lane / PER) * STRIDE + lane % PER;
+    }
+    __device__ __forceinline__ int32_t column(const KaArgs& a, int32_t t16) const
+    {
+        return (int32_t)(((uint64_t)(uint32_t)t16 * a.p16_inv) >> 36);
+    }
+    __device__ __forceinline__ void ask(const KaArgs& a, int it)
+    {
+        const int32_t t16 = tile_of(it);
+        page = row[t16 < end ? column(a, t16) : 0];
+    }
+    __device__ __forceinline__ void look(const KaArgs& a, int h, int it)
+    {
+        const int32_t t16 = tile_of(it), pg = page;
+        const bool in = t16 < end, ok = in && pg >= 0 && pg < a.n_pages;
+        if (in && !ok) set_status(a.status, ISEG_DEV_RANGE);
+        idx = ok ? (pg * a.H + h) * a.p16 + (t16 - column(a, t16) * a.p16) : -1;
+        there = __ballot(ok);
+        ask(a, it + N);
     }
     __device__ __forceinline__ int at(int it, int i) const { return __builtin_amdgcn_readlane(idx, (it % N) * PER + i); }
+    __device__ __forceinline__ uint32_t mask(int it) const { return (uint32_t)(there >> ((it % N) * PER)) & ((1u << PER) - 1); }
 };
 
 // waves per SIMD whose registers the rows leave room for
@@ -499,8 +532,9 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(ka_few_wave
 
     // the words of 32 keys; the next step's keys are requested once the scores are
     // there, its values once they are summed up
-    KaTiles<2, 8> tl = {a.table + b * a.table_ld, key0 >> 4, (kv + 15) >> 4, -1};
-    uint32_t kw[2][NC], vw[2][NC];
+    KaTiles<2, 8> tl = {a.table + b * a.table_ld, key0 >> 4, (kv + 15) >> 4, 0, -1, 0};
+    if (n_it > 0) tl.ask(a, 0);
+    KaWords<NC> kw[2], vw[2];
     f4_t ks_next[2], vs_next[2];
     auto fetch_k = [&](int it) {
         if (it % tl.N == 0) tl.look(a, h, it);
@@ -508,7 +542,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(ka_few_wave
         for (int i = 0; i < 2; i++) {
             const int ti = tl.at(it, i);
             const int64_t at = ti >= 0 ? ti : 0;
-            words<NC>(a.kc + at * (256 * NC) + (c * 4 + g4) * (4 * NC), kw[i]);
+            kw[i] = words<NC>(a.kc + at * (256 * NC) + (c * 4 + g4) * (4 * NC));
             ks_next[i] = *(const f4_t*)(a.ks + at * 16 + g4 * 4);
             vs_next[i] = *(const f4_t*)(a.vs + at * 16 + g4 * 4);
         }
@@ -518,7 +552,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(ka_few_wave
         for (int i = 0; i < 2; i++) {
             const int ti = tl.at(it, i);
             const int64_t at = ti >= 0 ? ti : 0;
-            words<NC>(a.vc + at * (256 * NC) + (c * 4 + g4) * (4 * NC), vw[i]);
+            vw[i] = words<NC>(a.vc + at * (256 * NC) + (c * 4 + g4) * (4 * NC));
         }
     };
     if (n_it > 0) {
@@ -528,7 +562,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(ka_few_wave
     for (int it = 0; it < n_it; it++) {
         const int32_t kb = key0 + it * 128;
         if (kb >= x.any_hi) break;
-        const bool ok[2] = {tl.at(it, 0) >= 0, tl.at(it, 1) >= 0};
+        const uint32_t oks = tl.mask(it);
+        const bool ok[2] = {(oks & 1) != 0, (oks & 2) != 0};
         const bool more = it + 1 < n_it;
         f4_t st[R][2];
 #pragma unroll
@@ -537,7 +572,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(ka_few_wave
             for (int t = 0; t < R; t++) st[t][i] = f4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int w = 0; w < NC; w++) {
-                const uint32_t u = kw[i][w], v = u >> 8;
+                const uint32_t u = kw[i].w[w], v = u >> 8;
                 x.score(join8(codes_lo(u), codes_hi(u), codes_lo(v), codes_hi(v)), w, i, st);
             }
         }
@@ -547,7 +582,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(ka_few_wave
         x.soften(st, ks, vs, ok, kb, kv, pf);
 #pragma unroll
         for (int w = 0; w < NC; w++) {
-            const uint32_t a0 = vw[0][w], a1 = vw[1][w], b0 = a0 >> 8, b1 = a1 >> 8;
+            const uint32_t a0 = vw[0].w[w], a1 = vw[1].w[w], b0 = a0 >> 8, b1 = a1 >> 8;
             x.add(join8(codes_lo(a0), codes_lo(b0), codes_lo(a1), codes_lo(b1)), 2 * w, 0, pf);
             x.add(join8(codes_hi(a0), codes_hi(b0), codes_hi(a1), codes_hi(b1)), 2 * w + 1, 0, pf);
         }
@@ -595,7 +630,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(ka_few_wave
 // ---------------------------------------------------------------------------
 constexpr int kWaves = 8;
 
-// a stage: operands of 64 keys, 1 KB each (64 lanes of 16 bytes), and their scales
+// a stage of 64 keys: operands of 1 KB each (64 lanes of 16 bytes), and scales
 template <int NC>
 struct KaStage {
     h8_t k[4][NC][64];                   // [tile][word]
@@ -604,11 +639,12 @@ struct KaStage {
 };
 
 template <int NC, int R, bool WIDE>
-__global__ __launch_bounds__(512) void k_kv4_many(KaArgs a)
+__global__ __launch_bounds__(64 * kWaves) void k_kv4_many(KaArgs a)
 {
-    constexpr int TR = 16 * R * kWaves;
+    constexpr int TR = 16 * R * kWaves, KT = 64;
+    typedef KaStage<NC> Stage;
     extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
-    KaStage<NC>* stage = (KaStage<NC>*)smem;
+    Stage* stage = (Stage*)smem;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int c = lane & 15, g4 = lane >> 4;
     const int h = blockIdx.x % a.H, split = (blockIdx.x / a.H) % a.splits, tile = blockIdx.x / a.H / a.splits;
@@ -619,68 +655,66 @@ __global__ __launch_bounds__(512) void k_kv4_many(KaArgs a)
     if (bad) set_status(a.status, ISEG_DEV_RANGE);
     if (!have) return;
     const int64_t rows = s.n * a.G;
-    KaRows<NC, R, WIDE> x;
-    x.load(a, s, row0 + wave * 16 * R, rows, h);
 
-    // keys of the block's rows in steps of 64, dealt to the splits
+    // keys of the block's rows in stages, dealt to the splits
     int64_t l0, h0, l1, h1;
     ka_span(a, s, row0, l0, h0);
     ka_span(a, s, (row0 + TR < rows ? row0 + TR : rows) - 1, l1, h1);
-    const int32_t k_lo = (int32_t)l0 & ~63, k_hi = (int32_t)h1, kv = (int32_t)s.kv;
-    const int32_t steps = k_hi > k_lo ? (k_hi - k_lo + 63) / 64 : 0;
+    const int32_t k_lo = (int32_t)l0 & ~(KT - 1), k_hi = (int32_t)h1, kv = (int32_t)s.kv;
+    const int32_t steps = k_hi > k_lo ? (k_hi - k_lo + KT - 1) / KT : 0;
     const int32_t per = (steps + a.splits - 1) / a.splits, it0 = split * per;
     const int32_t n_it = it0 + per < steps ? per : (steps > it0 ? steps - it0 : 0);
-    const int32_t key0 = k_lo + it0 * 64;
+    const int32_t key0 = k_lo + it0 * KT;
 
-    // waves 0-3 bring a tile of keys each, waves 4-7 one nibble of a pair of tiles of values
-    KaTiles<4, 4> tl = {a.table + b * a.table_ld, key0 >> 4, (kv + 15) >> 4, -1};
+    // one half of the waves bring a tile of keys each, the other one nibble of a
+    // pair of tiles of values and the scales of one tile
+    KaTiles<4, 4> tl = {a.table + b * a.table_ld, key0 >> 4, (kv + 15) >> 4, 0, -1, 0};
     const bool values = wave >= 4;
-    const int vp = (wave >> 1) & 1, vn = wave & 1;
-    uint32_t wa[NC], wb[NC];
+    const int own = wave & 3, vn = wave & 1;
+    KaWords<NC> wa, wb;
     float sc = 0.f;
     auto fetch = [&](int it) {
         if (it % tl.N == 0) tl.look(a, h, it);
-        const int own = tl.at(it, wave & 3);
-        const int64_t o = own >= 0 ? own : 0;
+        const int ti = tl.at(it, own);
+        const int64_t o = ti >= 0 ? ti : 0;
         if (!values) {
-            words<NC>(a.kc + o * (256 * NC) + (c * 4 + g4) * (4 * NC), wa);
+            wa = words<NC>(a.kc + o * (256 * NC) + (c * 4 + g4) * (4 * NC));
+            wb = wa;
             sc = a.ks[o * 16 + c];
         } else {
-            const int u0 = tl.at(it, 2 * vp), u1 = tl.at(it, 2 * vp + 1);
+            const int u0 = tl.at(it, own & ~1), u1 = tl.at(it, own | 1);
             const int64_t t0 = u0 >= 0 ? u0 : 0, t1 = u1 >= 0 ? u1 : 0;
-            words<NC>(a.vc + t0 * (256 * NC) + (c * 4 + g4) * (4 * NC), wa);
-            words<NC>(a.vc + t1 * (256 * NC) + (c * 4 + g4) * (4 * NC), wb);
+            wa = words<NC>(a.vc + t0 * (256 * NC) + (c * 4 + g4) * (4 * NC));
+            wb = words<NC>(a.vc + t1 * (256 * NC) + (c * 4 + g4) * (4 * NC));
             sc = a.vs[o * 16 + c];
         }
     };
-    auto spread = [&](KaStage<NC>& d) {
+    auto spread = [&](Stage& d) {
         if (!values) {
 #pragma unroll
             for (int w = 0; w < NC; w++) {
-                const uint32_t u = wa[w], v = u >> 8;
-                d.k[wave][w][lane] = join8(codes_lo(u), codes_hi(u), codes_lo(v), codes_hi(v));
+                const uint32_t u = wa.w[w], v = u >> 8;
+                d.k[own][w][lane] = join8(codes_lo(u), codes_hi(u), codes_lo(v), codes_hi(v));
             }
-            if (lane < 16) d.ks[wave * 16 + lane] = sc;
+            if (lane < 16) d.ks[own * 16 + lane] = sc;
         } else {
 #pragma unroll
             for (int w = 0; w < NC; w++) {
-                const uint32_t a0 = wa[w] >> (4 * vn), a1 = wb[w] >> (4 * vn), b0 = a0 >> 8, b1 = a1 >> 8;
-                d.v[vp][2 * w + vn][lane] = join8(codes_lo(a0), codes_lo(b0), codes_lo(a1), codes_lo(b1));
+                const uint32_t a0 = wa.w[w] >> (4 * vn), a1 = wb.w[w] >> (4 * vn), b0 = a0 >> 8, b1 = a1 >> 8;
+                d.v[own >> 1][2 * w + vn][lane] = join8(codes_lo(a0), codes_lo(b0), codes_lo(a1), codes_lo(b1));
             }
-            if (lane < 16) d.vs[(wave - 4) * 16 + lane] = sc;
+            if (lane < 16) d.vs[own * 16 + lane] = sc;
         }
     };
-    // the tiles that are there, as bits, looked at before the next look-up takes their place
-    auto there = [&](int it) {
-        int m = 0;
-#pragma unroll
-        for (int i = 0; i < 4; i++) m |= (tl.at(it, i) >= 0) << i;
-        return m;
-    };
-    int ok_now = 0, ok_next = 0;
     if (n_it > 0) {
-        fetch(0);
-        ok_next = there(0);
+        tl.ask(a, 0);
+        fetch(0);                        // under way while the queries come
+    }
+    KaRows<NC, R, WIDE> x;
+    x.load(a, s, row0 + wave * 16 * R, rows, h);
+    uint32_t ok_now = 0, ok_next = 0;    // tiles that are there, taken before the next look-up
+    if (n_it > 0) {
+        ok_next = tl.mask(0);
         spread(stage[0]);
         if (n_it > 1) fetch(1);
     }
@@ -688,13 +722,13 @@ __global__ __launch_bounds__(512) void k_kv4_many(KaArgs a)
         __syncthreads();
         ok_now = ok_next;
         if (it + 1 < n_it) {
-            ok_next = there(it + 1);
+            ok_next = tl.mask(it + 1);
             spread(stage[(it + 1) & 1]);
             if (it + 2 < n_it) fetch(it + 2);
         }
-        const int32_t kb = key0 + it * 64;
-        if (kb >= x.any_hi || kb + 64 <= x.any_lo) continue;
-        const KaStage<NC>& y = stage[it & 1];
+        const int32_t kb = key0 + it * KT;
+        if (kb >= x.any_hi || kb + KT <= x.any_lo) continue;
+        const Stage& y = stage[it & 1];
         f4_t st[R][4], ks[4], vs[4];
         bool ok[4];
 #pragma unroll
@@ -789,18 +823,18 @@ __global__ __launch_bounds__(256) void k_kv4_join(KaArgs a)
 // host
 // ---------------------------------------------------------------------------
 // A call's launches: requests of up to 16 R rows by blocks whose waves share
-// them, the others in tiles of 128 R2 rows.
+// them, the others in tiles of many_rows.
 struct KaPlan {
     int R;                       // tiles of 16 rows of the first kind; 0: none
-    int R2;                      // tiles of 16 rows of a wave of the second kind; 0: none
-    int64_t tiles2;
+    int64_t tiles2;              // of the second kind; 0: none
+    int many_rows;
     int splits, splits2;
     size_t part, bytes;
 };
 
 // what a wave's registers hold
-constexpr int ka_few_most(int nc, bool wide) { return wide ? (nc <= 4 ? 2 : 1) : (nc <= 4 ? 4 : 2); }
 constexpr int ka_many(int nc, bool wide) { return wide || nc > 4 ? 1 : 2; }
+constexpr int ka_few_most(int nc, bool wide) { return wide ? (nc <= 4 ? 2 : 1) : (nc <= 4 ? 4 : 2); }
 
 bool ka_wide(const iseg_kv4_attention_geom* g) { return g->dtype == ISEG_F32; }
 
@@ -828,14 +862,14 @@ KaPlan ka_plan(const iseg_kv4_attention_geom* g)
         p.splits = (int)(sp < 1 ? 1 : (sp > kSplitsMax ? kSplitsMax : sp));
     }
     if (rows > 16 * most) {
-        p.R2 = ka_many(nc, ka_wide(g));
-        p.tiles2 = ceil_div64(g->T * G, 16 * kWaves * p.R2) + g->B;
+        p.many_rows = 16 * kWaves * ka_many(nc, ka_wide(g));
+        p.tiles2 = ceil_div64(g->T * G, p.many_rows) + g->B;
         int64_t sp = ceil_div64(256, p.tiles2 * g->H), longest = ceil_div64(span, 512);
         sp = sp < longest ? sp : longest;
         p.splits2 = (int)(sp < 1 ? 1 : (sp > 32 ? 32 : sp));
     }
     const int64_t n1 = p.R && p.splits > 1 ? pairs * 16 * p.R * p.splits : 0;
-    const int64_t n2 = p.R2 && p.splits2 > 1 ? p.tiles2 * g->H * 16 * kWaves * p.R2 * p.splits2 : 0;
+    const int64_t n2 = p.splits2 > 1 ? p.tiles2 * g->H * p.many_rows * p.splits2 : 0;
     const int64_t n = n1 > n2 ? n1 : n2;
     p.part = align256((size_t)n * 8);
     p.bytes = n ? ws_used(p.part + (size_t)n * kv4_width(g->D) * 4) : kNoWs;
@@ -858,7 +892,7 @@ int ka_check(const iseg_kv4_attention_geom* g)
         const KaPlan p = ka_plan(g);
         const int64_t most = (int64_t)1 << 24;               // blocks of 256 threads of a launch
         if (g->B * g->H * p.splits >= most || (p.splits > 1 && g->B * g->H * 16 * p.R >= most) ||
-            (p.R2 && (p.tiles2 * g->H * p.splits2 >= most || (p.splits2 > 1 && p.tiles2 * g->H * 16 * kWaves * p.R2 >= most))))
+            p.tiles2 * g->H * p.splits2 >= most || (p.splits2 > 1 && p.tiles2 * g->H * p.many_rows >= most))
             return ISEG_ERR_UNSUPPORTED;
     }
     return ISEG_OK;
@@ -878,7 +912,7 @@ int ka_few(KaArgs& a, hipStream_t s)
 template <int NC, bool WIDE>
 int ka_run(KaArgs a, const KaPlan& p, hipStream_t s)
 {
-    constexpr int most = ka_few_most(NC, WIDE), R2 = ka_many(NC, WIDE);
+    constexpr int most = ka_few_most(NC, WIDE);
     int rc = ISEG_OK;
     if (p.R) {
         a.rows_min = 0;
@@ -890,16 +924,17 @@ int ka_run(KaArgs a, const KaPlan& p, hipStream_t s)
         if constexpr (most >= 4)
             if (p.R == 4) rc = ka_few<NC, 4, WIDE>(a, s);
     }
-    if (rc == ISEG_OK && p.R2) {
+    if (rc == ISEG_OK && p.tiles2 > 0) {
+        constexpr int R = ka_many(NC, WIDE);
         constexpr size_t lds = 2 * sizeof(KaStage<NC>);
-        if (!lds_limit((const void*)&k_kv4_many<NC, R2, WIDE>, lds)) return ISEG_ERR_DEVICE;
+        if (!lds_limit((const void*)&k_kv4_many<NC, R, WIDE>, lds)) return ISEG_ERR_DEVICE;
         a.rows_min = p.R ? 16 * p.R : 0;
         a.rows_max = 0x7fffffff;
         a.splits = p.splits2;
-        a.join_rows = 16 * kWaves * R2;
-        hipLaunchKernelGGL((k_kv4_many<NC, R2, WIDE>), dim3((unsigned)(p.tiles2 * a.H * a.splits)), dim3(512), lds, s, a);
+        a.join_rows = p.many_rows;
+        hipLaunchKernelGGL((k_kv4_many<NC, R, WIDE>), dim3((unsigned)(p.tiles2 * a.H * a.splits)), dim3(64 * kWaves), lds, s, a);
         if (a.splits > 1)
-            hipLaunchKernelGGL((k_kv4_join<16 * kWaves * R2, false>), dim3((unsigned)(p.tiles2 * a.H * a.join_rows)), dim3(256), 0, s, a);
+            hipLaunchKernelGGL((k_kv4_join<16 * kWaves * R, false>), dim3((unsigned)(p.tiles2 * a.H * a.join_rows)), dim3(256), 0, s, a);
         rc = launch_ok();
     }
     return rc;
