@@ -857,7 +857,12 @@ KaPlan ka_plan(const iseg_kv4_attention_geom* g)
     if (rows <= 16 * most || g->B > 1) {
         const int64_t r = rows <= 16 * most ? rows : 16 * most;
         p.R = r <= 16 ? 1 : (r <= 32 ? 2 : 4);
-        int64_t sp = ceil_div64(1024, pairs), longest = ceil_div64(span, 256);
+        // Few pairs of request and head: as many blocks as are resident, all of one
+        // length (1 request of 131072 keys, 8 heads: 32 us at 96 splits, 36 at 128).  Many:
+        // two rounds of blocks, which even out requests of different lengths (64 of
+        // 820 to 8192 keys: 81 us against 86 in one).
+        const int64_t resident = 256 * ka_few_waves(nc, p.R, ka_wide(g));
+        int64_t sp = 8 * pairs <= resident ? resident / pairs : ceil_div64(2 * resident, pairs), longest = ceil_div64(span, 256);
         sp = sp < longest ? sp : longest;
         p.splits = (int)(sp < 1 ? 1 : (sp > kSplitsMax ? kSplitsMax : sp));
     }

@@ -13,10 +13,10 @@ struct KvArgs {
     void *ko, *vo;
     uint8_t *kc, *vc;
     float *ks, *vs;
-    int64_t T, rows;                 // rows: heads of four tokens each
+    int64_t T, rows;                 // rows: heads of four tokens, or of one
     int64_t k_ld, k_hs, v_ld, v_hs;
     int64_t n_slots;
-    int32_t H, D, W, page, slot64, mode;
+    int32_t H, D, W, page, slot64, mode, four;
     int32_t* status;
 };
 
@@ -70,21 +70,21 @@ __device__ __forceinline__ bool kv_beside(const int64_t* slot, const KvArgs& a)
 // lanes apart: each pair of lanes exchanges words and has half of the eight
 // bytes.  Tokens side by side, as a prompt's are, store v in words of four
 // tokens, others in bytes.
-template <typename T, int LPR>
+template <typename T, int LPR, int Q>
 __global__ __launch_bounds__(256) void k_kv4_write(KvArgs a)
 {
     const int w = threadIdx.x % LPR, words = a.W / 8;
     const int64_t r = (int64_t)blockIdx.x * (256 / LPR) + threadIdx.x / LPR;
     if (r >= a.rows) return;
     const bool val = blockIdx.y != 0;
-    const int64_t t0 = r / a.H * 4;
-    const int h = (int)(r - t0 / 4 * a.H), nt = (int)(a.T - t0 < 4 ? a.T - t0 : 4);
+    const int64_t t0 = r / a.H * Q;
+    const int h = (int)(r - t0 / Q * a.H), nt = (int)(a.T - t0 < Q ? a.T - t0 : Q);
     const T* x0 = val ? (const T*)a.v + h * a.v_hs : (const T*)a.k + h * a.k_hs;
     const int64_t ld = val ? a.v_ld : a.k_ld;
-    int64_t slot[4];
-    float f[4][8];
+    int64_t slot[Q];
+    float f[Q][8];
 #pragma unroll
-    for (int q = 0; q < 4; q++) {
+    for (int q = 0; q < Q; q++) {
         slot[q] = q < nt ? kv_slot(a, t0 + q) : -1;
         if (slot[q] >= a.n_slots) {
             if (w == 0) set_status(a.status, ISEG_DEV_RANGE);
@@ -92,10 +92,10 @@ __global__ __launch_bounds__(256) void k_kv4_write(KvArgs a)
         }
     }
 #pragma unroll
-    for (int q = 0; q < 4; q++) kv_get8(x0 + (t0 + (q < nt ? q : 0)) * ld, w * 8, a.D, f[q]);
-    uint32_t bytes[4];                                         // v: of each token
+    for (int q = 0; q < Q; q++) kv_get8(x0 + (t0 + (q < nt ? q : 0)) * ld, w * 8, a.D, f[q]);
+    uint32_t bytes[Q];                                         // v: of each token
 #pragma unroll
-    for (int q = 0; q < 4; q++) {
+    for (int q = 0; q < Q; q++) {
         uint32_t big = 0;
 #pragma unroll
         for (int i = 0; i < 8; i++) {
@@ -140,7 +140,7 @@ __global__ __launch_bounds__(256) void k_kv4_write(KvArgs a)
     }
     if (!val || w >= words) return;
     const int i = w >> 2, c0 = (w & 1) * 8 + ((w & 2) ? 4 : 0), nc = a.W / 32;
-    if (kv_beside(slot, a)) {
+    if constexpr (Q == 4) if (kv_beside(slot, a)) {
         const KvPlace p = kv_place(a, slot[0], h);
         uint8_t* q = a.vc + p.tile + ((c0 * 4 + (p.t >> 2)) * nc + i) * 4;
         // four tokens' bytes of four columns to four columns' bytes of four tokens
@@ -153,7 +153,7 @@ __global__ __launch_bounds__(256) void k_kv4_write(KvArgs a)
         return;
     }
 #pragma unroll
-    for (int t = 0; t < 4; t++) {
+    for (int t = 0; t < Q; t++) {
         if (slot[t] < 0) continue;
         const KvPlace p = kv_place(a, slot[t], h);
         uint8_t* q = a.vc + p.tile + ((c0 * 4 + (p.t >> 2)) * nc + i) * 4 + (p.t & 3);
@@ -162,20 +162,20 @@ __global__ __launch_bounds__(256) void k_kv4_write(KvArgs a)
     }
 }
 
-template <typename T, int LPR>
+template <typename T, int LPR, int Q>
 __global__ __launch_bounds__(256) void k_kv4_read(KvArgs a)
 {
     const int w = threadIdx.x % LPR, words = a.W / 8;
     const int64_t r = (int64_t)blockIdx.x * (256 / LPR) + threadIdx.x / LPR;
     if (r >= a.rows || w >= words) return;
     const bool val = blockIdx.y != 0;
-    const int64_t t0 = r / a.H * 4;
-    const int h = (int)(r - t0 / 4 * a.H), nt = (int)(a.T - t0 < 4 ? a.T - t0 : 4);
-    int64_t slot[4];
-    float s[4];
-    int n[4][8];
+    const int64_t t0 = r / a.H * Q;
+    const int h = (int)(r - t0 / Q * a.H), nt = (int)(a.T - t0 < Q ? a.T - t0 : Q);
+    int64_t slot[Q];
+    float s[Q];
+    int n[Q][8];
 #pragma unroll
-    for (int q = 0; q < 4; q++) {
+    for (int q = 0; q < Q; q++) {
         slot[q] = q < nt ? kv_slot(a, t0 + q) : -1;
         if (slot[q] >= a.n_slots) {
             if (w == 0) set_status(a.status, ISEG_DEV_RANGE);
@@ -188,7 +188,7 @@ __global__ __launch_bounds__(256) void k_kv4_read(KvArgs a)
     const int i = w >> 2, c0 = (w & 1) * 8, up = (w & 2) ? 4 : 0, nc = a.W / 32;
     if (!val) {
 #pragma unroll
-        for (int q = 0; q < 4; q++) {
+        for (int q = 0; q < Q; q++) {
             if (slot[q] < 0) continue;
             const KvPlace p = kv_place(a, slot[q], h);
             s[q] = a.ks[p.row];
@@ -196,21 +196,21 @@ __global__ __launch_bounds__(256) void k_kv4_read(KvArgs a)
 #pragma unroll
             for (int e = 0; e < 8; e++) n[q][e] = (int)((word >> ((e & 1) * 16 + (e >> 1) * 4)) & 15u) - 8;
         }
-    } else if (kv_beside(slot, a)) {
+    } else if (Q == 4 && kv_beside(slot, a)) {
         const KvPlace p = kv_place(a, slot[0], h);
         const uint8_t* b = a.vc + p.tile + ((c0 * 4 + (p.t >> 2)) * nc + i) * 4;
         uint32_t word[8];
 #pragma unroll
         for (int e = 0; e < 8; e++) word[e] = *(const uint32_t*)(b + 16 * e * nc);
 #pragma unroll
-        for (int q = 0; q < 4; q++) {
+        for (int q = 0; q < Q; q++) {
             s[q] = a.vs[p.row + q];
 #pragma unroll
             for (int e = 0; e < 8; e++) n[q][e] = (int)((word[e] >> (8 * q + up)) & 15u) - 8;
         }
     } else {
 #pragma unroll
-        for (int q = 0; q < 4; q++) {
+        for (int q = 0; q < Q; q++) {
             if (slot[q] < 0) continue;
             const KvPlace p = kv_place(a, slot[q], h);
             s[q] = a.vs[p.row];
@@ -223,7 +223,7 @@ __global__ __launch_bounds__(256) void k_kv4_read(KvArgs a)
     const int64_t ld = val ? a.v_ld : a.k_ld;
     const int d = w * 8;
 #pragma unroll
-    for (int q = 0; q < 4; q++) {
+    for (int q = 0; q < Q; q++) {
         if (q >= nt) break;
         struct { T v[8]; } o;
 #pragma unroll
@@ -251,15 +251,23 @@ int kv_check(const iseg_kv4_geom* g)
 KvArgs kv_args(const iseg_kv4_geom* g, const void* slots, int32_t* status)
 {
     KvArgs a = {};
-    a.slots = slots; a.T = g->T; a.rows = ceil_div64(g->T, 4) * g->H;
+    a.slots = slots; a.T = g->T;
+    // one token a group of lanes until there are groups of four for the whole card:
+    // 64 tokens of 8 heads 4.0 us against 8.5, 30011 tokens 64 against 78
+    a.four = g->T * g->H >= 4096;
+    a.rows = ceil_div64(g->T, a.four ? 4 : 1) * g->H;
     a.k_ld = g->k_ld; a.k_hs = g->k_hs; a.v_ld = g->v_ld; a.v_hs = g->v_hs;
     a.n_slots = g->n_pages * g->page; a.H = (int32_t)g->H; a.D = (int32_t)g->D; a.W = kv4_width(g->D); a.page = g->page;
     a.slot64 = g->slot_dtype == ISEG_I64; a.mode = g->scale_mode; a.status = status;
     return a;
 }
 
-#define KV_LAUNCH(kernel, LPR)                                                                              \
-    hipLaunchKernelGGL((kernel<T, LPR>), dim3((unsigned)ceil_div64(a.rows, 256 / LPR), 2), dim3(256), 0, s, a)
+#define KV_LAUNCH(kernel, LPR)                                                                                   \
+    do {                                                                                                         \
+        const dim3 grid((unsigned)ceil_div64(a.rows, 256 / LPR), 2);                                             \
+        if (a.four) hipLaunchKernelGGL((kernel<T, LPR, 4>), grid, dim3(256), 0, s, a);                           \
+        else hipLaunchKernelGGL((kernel<T, LPR, 1>), grid, dim3(256), 0, s, a);                                  \
+    } while (0)
 
 template <typename T>
 int kv_write(const KvArgs& a, hipStream_t s)
