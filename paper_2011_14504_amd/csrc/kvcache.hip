@@ -57,6 +57,23 @@ __device__ __forceinline__ void kv_get8(const T* p, int d, int D, float* f)
     }
 }
 
+// Scale of a largest magnitude given as float32 bits: scale_of (coder.h) with 4
+// bits, in float32.  A float32 quotient rounded once is the float64 one rounded to
+// float32 (24 bits twice and two more fit in 53).  In float64 the write of 30011
+// tokens takes 2 us more.
+__device__ __forceinline__ float kv_scale(uint32_t big, int mode)
+{
+    if (big >= 0x7f800000u) return __builtin_nanf("");
+    const float t = __builtin_bit_cast(float, big);
+    float s = t / 7.f;
+    if (mode == ISEG_SCALE_POW2) {
+        int e;
+        (void)frexpf(t, &e);                           // t = f 2^e with f in [1/2, 1): 2^e is the power above t
+        s = big ? ldexpf(1.f, e - 3) : 0.f;
+    }
+    return s < kKvScaleMin ? kKvScaleMin : s;
+}
+
 // whether four tokens lie side by side in one run of four of a tile
 __device__ __forceinline__ bool kv_beside(const int64_t* slot, const KvArgs& a)
 {
@@ -77,8 +94,13 @@ __global__ __launch_bounds__(256) void k_kv4_write(KvArgs a)
     const int64_t r = (int64_t)blockIdx.x * (256 / LPR) + threadIdx.x / LPR;
     if (r >= a.rows) return;
     const bool val = blockIdx.y != 0;
-    const int64_t t0 = r / a.H * Q;
-    const int h = (int)(r - t0 / Q * a.H), nt = (int)(a.T - t0 < Q ? a.T - t0 : Q);
+    // four groups after one another have sixteen tokens of a head: a tile's lines are
+    // then written by one wave
+    const int64_t u = Q == 4 ? r >> 2 : r, ut = u / a.H;
+    const int h = (int)(u - ut * a.H);
+    const int64_t t0 = Q == 4 ? ut * 16 + (r & 3) * 4 : ut;
+    const int nt = (int)(a.T - t0 < Q ? a.T - t0 : Q);
+    if (nt <= 0) return;
     const T* x0 = val ? (const T*)a.v + h * a.v_hs : (const T*)a.k + h * a.k_hs;
     const int64_t ld = val ? a.v_ld : a.k_ld;
     int64_t slot[Q];
@@ -107,10 +129,8 @@ __global__ __launch_bounds__(256) void k_kv4_write(KvArgs a)
             const uint32_t b = (uint32_t)__shfl_xor((int)big, o, 64);
             big = b > big ? b : big;
         }
-        float s = kKvScaleMin;
-        if (big) s = scale_of(bits_of((double)__builtin_bit_cast(float, big)), 4, a.mode);
-        if (s < kKvScaleMin) s = kKvScaleMin;                  // a NaN stays
-        const Coder cd(s);
+        const Coder cd(kv_scale(big, a.mode));
+        const float s = cd.s;
         uint32_t n[2];
         codes_of<8, false>(f[q], nullptr, [&](int) -> const Coder& { return cd; }, 7, n);
         if (!cd.ok) {
@@ -169,8 +189,13 @@ __global__ __launch_bounds__(256) void k_kv4_read(KvArgs a)
     const int64_t r = (int64_t)blockIdx.x * (256 / LPR) + threadIdx.x / LPR;
     if (r >= a.rows || w >= words) return;
     const bool val = blockIdx.y != 0;
-    const int64_t t0 = r / a.H * Q;
-    const int h = (int)(r - t0 / Q * a.H), nt = (int)(a.T - t0 < Q ? a.T - t0 : Q);
+    // four groups after one another have sixteen tokens of a head: a tile's lines are
+    // then written by one wave
+    const int64_t u = Q == 4 ? r >> 2 : r, ut = u / a.H;
+    const int h = (int)(u - ut * a.H);
+    const int64_t t0 = Q == 4 ? ut * 16 + (r & 3) * 4 : ut;
+    const int nt = (int)(a.T - t0 < Q ? a.T - t0 : Q);
+    if (nt <= 0) return;
     int64_t slot[Q];
     float s[Q];
     int n[Q][8];
@@ -255,7 +280,7 @@ KvArgs kv_args(const iseg_kv4_geom* g, const void* slots, int32_t* status)
     // one token a group of lanes until there are groups of four for the whole card:
     // 64 tokens of 8 heads 4.0 us against 8.5, 30011 tokens 64 against 78
     a.four = g->T * g->H >= 4096;
-    a.rows = ceil_div64(g->T, a.four ? 4 : 1) * g->H;
+    a.rows = a.four ? ceil_div64(g->T, 16) * 4 * g->H : g->T * g->H;
     a.k_ld = g->k_ld; a.k_hs = g->k_hs; a.v_ld = g->v_ld; a.v_hs = g->v_hs;
     a.n_slots = g->n_pages * g->page; a.H = (int32_t)g->H; a.D = (int32_t)g->D; a.W = kv4_width(g->D); a.page = g->page;
     a.slot64 = g->slot_dtype == ISEG_I64; a.mode = g->scale_mode; a.status = status;
