@@ -344,8 +344,8 @@ __device__ __forceinline__ void scan2_1024(int64_t& x, int64_t& y, int64_t (*red
 
 __device__ __forceinline__ int32_t sat31(int64_t v) { return (int32_t)(v < 0x7fffffff ? v : 0x7fffffff); }
 
-// one block: lengths, pages wanted, their sums
-__global__ __launch_bounds__(1024) void k_page_scan(PmArgs a)
+// by one block: lengths, pages wanted, their sums
+__device__ __forceinline__ void page_scan(const PmArgs& a)
 {
     __shared__ int64_t red[2][16];
     __shared__ int64_t base[2];
@@ -427,14 +427,14 @@ __device__ __forceinline__ int32_t request_of(const int32_t* start, int32_t B, i
     return lo;
 }
 
-// a thread per token; the first new token of a page writes its table entry.  A
-// request without new tokens takes no page (its pages hold its context), unless
-// it holds too few: a thread per request adds those.
-__global__ __launch_bounds__(256) void k_page_fill(PmArgs a)
+// tokens and then requests, dealt to `blocks` blocks of NT threads: a thread per
+// token; a wave per request for the pages that it takes
+template <int NT>
+__device__ __forceinline__ void page_fill(const PmArgs& a, int64_t block, int64_t blocks)
 {
     const int64_t total = a.q_start[a.B];
     int bad = 0;
-    for (int64_t r = (int64_t)blockIdx.x * 256 + threadIdx.x; r < a.T; r += (int64_t)gridDim.x * 256) {
+    for (int64_t r = block * NT + threadIdx.x; r < a.T; r += blocks * NT) {
         if (r >= total) {
             a.pos[r] = 0;
             a.slots[r] = -1;
@@ -447,7 +447,7 @@ __global__ __launch_bounds__(256) void k_page_fill(PmArgs a)
         a.pos[r] = sat31(p);
         a.slots[r] = pg < 0 ? -1 : pg * a.page + in;
     }
-    for (int64_t b = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); b < a.B; b += (int64_t)gridDim.x * 4) {
+    for (int64_t b = block * (NT / 64) + (threadIdx.x >> 6); b < a.B; b += blocks * (NT / 64)) {
         const int64_t c = a.ctx[b] < 0 ? 0 : a.ctx[b], n = a.count[b] < 0 ? 0 : a.count[b];
         int64_t want = (c + n + a.page - 1) / a.page;
         if (want > a.max_pages) want = a.max_pages;
@@ -455,6 +455,19 @@ __global__ __launch_bounds__(256) void k_page_fill(PmArgs a)
             a.table[b * a.table_ld + col] = page_of(a, (int32_t)b, col, bad);
     }
     if (bad) set_status(a.status, ISEG_DEV_RANGE);
+}
+
+__global__ __launch_bounds__(1024) void k_page_scan(PmArgs a) { page_scan(a); }
+
+__global__ __launch_bounds__(256) void k_page_fill(PmArgs a) { page_fill<256>(a, blockIdx.x, gridDim.x); }
+
+// a decoding step: both in one block, whose own writes to q_start and the
+// workspace the barrier makes visible to it
+__global__ __launch_bounds__(1024) void k_page_map(PmArgs a)
+{
+    page_scan(a);
+    __syncthreads();
+    page_fill<1024>(a, 0, 1);
 }
 
 int pm_check(const iseg_page_map_geom* g)
@@ -533,8 +546,12 @@ extern "C" int iseg_page_map(const int32_t* ctx, const int32_t* count, const int
     a.w_free = (int32_t*)((char*)ws + 2 * align256((size_t)g->B * 4));
     a.T = g->T; a.max_pages = g->max_pages; a.table_ld = g->table_ld; a.F = g->F; a.n_pages = g->n_pages;
     a.B = (int32_t)g->B; a.page = g->page; a.status = dev_status;
-    hipLaunchKernelGGL(k_page_scan, dim3(1), dim3(1024), 0, stream, a);
-    if (g->T > 0 || g->B > 0) {
+    // up to 4096 tokens of 1024 requests the one block takes no longer than a second
+    // launch (256 requests of one token: 6 us, and 5 + 3 in two)
+    if (g->T <= 4096 && g->B <= 1024) {
+        hipLaunchKernelGGL(k_page_map, dim3(1), dim3(1024), 0, stream, a);
+    } else {
+        hipLaunchKernelGGL(k_page_scan, dim3(1), dim3(1024), 0, stream, a);
         const int64_t items = ceil_div64(g->T, 256) > ceil_div64(g->B, 4) ? ceil_div64(g->T, 256) : ceil_div64(g->B, 4);
         hipLaunchKernelGGL(k_page_fill, dim3((unsigned)(items < 2048 ? items : 2048)), dim3(256), 0, stream, a);
     }

@@ -1829,9 +1829,11 @@ def page_map(ctx, count, table, held, free_pages, n_free, page, n_pages, n_token
     ctx, count, held = _ints(ctx, B, ctx, "ctx"), _ints(count, B, ctx, "count"), _ints(held, B, ctx, "held")
     F = free_pages.numel()
     free_pages, n_free = _ints(free_pages, F, ctx, "free_pages"), _ints(n_free, 1, ctx, "n_free")
-    new = functools.partial(torch.empty, dtype=torch.int32, device=ctx.device)
-    q_start, kv_len, positions, slots = new(B + 1), new(B), new(n_tokens), new(n_tokens)
-    held_out, n_free_out = (held, n_free) if in_place else (new(B), new(1))
+    # one allocation: the host's time is what a decoding step's call takes
+    sizes = (B + 1, B, n_tokens, n_tokens) if in_place else (B + 1, B, n_tokens, n_tokens, B, 1)
+    outs = torch.empty(sum(sizes), dtype=torch.int32, device=ctx.device).split(sizes)
+    q_start, kv_len, positions, slots = outs[:4]
+    held_out, n_free_out = (held, n_free) if in_place else outs[4:]
     g, wsb = _page_map_geom(B, n_tokens, table.shape[1], table.stride(0) if B > 1 else max(table.shape[1], 1), F, n_pages, page)
     iseg_page_map(ctx, count, held, free_pages, n_free, g, table, q_start, kv_len, positions, slots, held_out,
                   n_free_out, _scratch(ctx, wsb), status)
@@ -1891,7 +1893,7 @@ def _rope_geom(*a):
 
 
 def _dense_like(t):
-    return None if t is None else torch.empty(t.shape, dtype=t.dtype, device=t.device)
+    return None if t is None else t.new_empty(t.shape)
 
 
 def _hd(t):
