@@ -42,18 +42,83 @@ __device__ __forceinline__ int64_t kv_slot(const KvArgs& a, int64_t t)
     return a.slot64 ? ((const int64_t*)a.slots)[t] : ((const int32_t*)a.slots)[t];
 }
 
-// eight elements of a row from d on, zeros beyond D
+// eight elements of a row, as words: halves apart, a wave would wait for them one by one
 template <typename T>
-__device__ __forceinline__ void kv_get8(const T* p, int d, int D, float* f)
+struct Kv8 {
+    uint32_t w[2 * sizeof(T)];
+    __device__ __forceinline__ void load(const T* p) { __builtin_memcpy(w, p, sizeof(w)); }
+    __device__ __forceinline__ void load(const T* p, int n)                  // n of them, then zeros
+    {
+#pragma unroll
+        for (int i = 0; i < 8; i++) {
+            uint32_t v = 0;
+            if (i < n) __builtin_memcpy(&v, p + i, sizeof(T));
+            if (sizeof(T) == 4) w[i % (2 * sizeof(T))] = v;
+            else if (i & 1) w[i / 2] |= v << 16;
+            else w[i / 2] = v;
+        }
+    }
+    __device__ __forceinline__ float at(int i) const
+    {
+        if constexpr (sizeof(T) == 4) return __builtin_bit_cast(float, w[i]);
+        else return (float)__builtin_bit_cast(T, (uint16_t)(w[i / 2] >> (i & 1) * 16));
+    }
+};
+
+// the largest magnitude of eight as its type's own bits: 16-bit types two at a time
+template <typename T>
+__device__ __forceinline__ uint32_t kv_big(const Kv8<T>& r)
 {
-    if (d + 8 <= D) {
-        struct { T v[8]; } r;
-        __builtin_memcpy(&r, p + d, sizeof(r));
+    if constexpr (sizeof(T) == 4) {
+        uint32_t big = 0;
 #pragma unroll
-        for (int i = 0; i < 8; i++) f[i] = (float)r.v[i];
+        for (int i = 0; i < 8; i++) {
+            const uint32_t b = r.w[i] & 0x7fffffffu;
+            big = b > big ? b : big;
+        }
+        return big;
     } else {
+        typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+        u16x2 m = 0;
 #pragma unroll
-        for (int i = 0; i < 8; i++) f[i] = d + i < D ? (float)p[d + i] : 0.f;
+        for (int i = 0; i < 4; i++) m = __builtin_elementwise_max(m, __builtin_bit_cast(u16x2, r.w[i] & 0x7fff7fffu));
+        return m.x > m.y ? m.x : m.y;
+    }
+}
+
+// a magnitude's bits as those of the float32 that it is
+template <typename T>
+__device__ __forceinline__ uint32_t kv_bits(uint32_t big)
+{
+    if constexpr (sizeof(T) == 4) return big;
+    else return bits_of((float)__builtin_bit_cast(T, (uint16_t)big));
+}
+
+// the maximum over LPR lanes, in all of them
+template <int LPR>
+__device__ __forceinline__ uint32_t kv_max(uint32_t v)
+{
+    v = dpp_max_step<0xb1>(v);                         // the other of two, of two pairs,
+    v = dpp_max_step<0x4e>(v);
+    if (LPR >= 8) v = dpp_max_step<0x141>(v);          // of eight turned round, of sixteen
+    if (LPR >= 16) v = dpp_max_step<0x140>(v);
+    if (LPR >= 32) {
+        const uint32_t t = (uint32_t)__shfl_xor((int)v, 16, 64);
+        v = t > v ? t : v;
+    }
+    return v;
+}
+
+// lane q's value in its four lanes
+template <int Q>
+__device__ __forceinline__ uint32_t kv_from(uint32_t v, int q)
+{
+    if (Q == 1) return v;
+    switch (q) {
+    case 0: return (uint32_t)__builtin_amdgcn_update_dpp((int)v, (int)v, 0x00, 0xf, 0xf, false);
+    case 1: return (uint32_t)__builtin_amdgcn_update_dpp((int)v, (int)v, 0x55, 0xf, 0xf, false);
+    case 2: return (uint32_t)__builtin_amdgcn_update_dpp((int)v, (int)v, 0xaa, 0xf, 0xf, false);
+    default: return (uint32_t)__builtin_amdgcn_update_dpp((int)v, (int)v, 0xff, 0xf, 0xf, false);
     }
 }
 
@@ -74,6 +139,149 @@ __device__ __forceinline__ float kv_scale(uint32_t big, int mode)
     return s < kKvScaleMin ? kKvScaleMin : s;
 }
 
+// The codes clamp(floor(v / s + 1/2), +-7) + 8 of eight elements in bits 19 to 22 of
+// x.  With v / s + 24.5 in [16, 32) the mantissa's first four bits are the code and
+// its other 19 the distance from the half-step below it.  The float32 sum is within
+// half a unit of 2^-19 of its terms' (the fma's one rounding) and 8 2^-24 of v / s
+// (1 / s rounded), together less than one: the floor can differ only where those 19
+// bits are zero, and there only from below, when v - (n - 1/2) s < 0.  That
+// remainder's sign is exact however its fma rounds.  s is in [2^-60, 2^126): its
+// reciprocal is normal, and v / s is at most 8, which only a power of two passes 7.5
+// with; the clamp leaves the outermost codes' middle.
+__device__ __forceinline__ void kv_codes(const float* f, float s, float inv, uint32_t* x)
+{
+    uint32_t near = ~0u;
+    float t[8];
+#pragma unroll
+    for (int e = 0; e < 8; e++) {
+        t[e] = __builtin_amdgcn_fmed3f(fmaf(f[e], inv, 24.5f), 17.5f, 31.5f);
+        x[e] = __builtin_bit_cast(uint32_t, t[e]);
+        const uint32_t frac = x[e] << 13;
+        near = frac < near ? frac : near;
+    }
+    if (near == 0) {
+#pragma unroll
+        for (int e = 0; e < 8; e++) x[e] -= (uint32_t)((x[e] << 13 == 0) & (fmaf(24.5f - t[e], s, f[e]) < 0.f)) << 19;
+    }
+}
+
+// byte 2 of four words
+__device__ __forceinline__ uint32_t kv_gather(uint32_t a, uint32_t b, uint32_t c, uint32_t d)
+{
+    return __builtin_amdgcn_perm(__builtin_amdgcn_perm(d, c, 0x0c0c0602), __builtin_amdgcn_perm(b, a, 0x0c0c0602), 0x05040100);
+}
+
+// codes in bits 3 to 6 of each byte to low and high halves
+__device__ __forceinline__ uint32_t kv_halves(uint32_t lo, uint32_t hi) { return (lo >> 3 & 0x0f0f0f0fu) | (hi << 1 & 0xf0f0f0f0u); }
+
+// LPR lanes a row, eight columns (a word of codes) a lane, four tokens of a head
+// at a time (Q = 4); blockIdx.y: keys or values.  What is the same for a row (its
+// place, its scale and that one's reciprocal) each of four lanes has for one of the
+// four tokens.  A byte of v holds columns 16 apart, which lie two lanes apart: each
+// pair of lanes exchanges words and has half of the eight bytes.  Tokens side by
+// side, as a prompt's are, store v in words of four tokens, others in bytes.
+template <typename T, int LPR, int Q>
+__global__ __launch_bounds__(256) void k_kv4_write(KvArgs a)
+{
+    const int w = threadIdx.x % LPR, words = a.W / 8;
+    const uint32_t r = blockIdx.x * (uint32_t)(256 / LPR) + threadIdx.x / LPR;
+    if (r >= a.rows) return;
+    const bool val = blockIdx.y != 0;
+    // four groups after one another have sixteen tokens of a head: a tile's lines are
+    // then written by one wave
+    const uint32_t u = Q == 4 ? r >> 2 : r, ut = u / (uint32_t)a.H;
+    const int h = (int)(u - ut * (uint32_t)a.H);
+    const int64_t t0 = Q == 4 ? (int64_t)ut * 16 + (r & 3) * 4 : ut;
+    const int nt = (int)(a.T - t0 < Q ? a.T - t0 : Q);
+    if (nt <= 0) return;
+    const T* x0 = val ? (const T*)a.v + h * a.v_hs : (const T*)a.k + h * a.k_hs;
+    const int64_t ld = val ? a.v_ld : a.k_ld;
+    Kv8<T> raw[Q];
+    const T* from = x0 + t0 * ld + w * 8;
+    const int n = a.D - w * 8;
+    if (n >= 8) {
+#pragma unroll
+        for (int q = 0; q < Q; q++, from += q < nt ? ld : 0) raw[q].load(from);
+    } else {
+#pragma unroll
+        for (int q = 0; q < Q; q++, from += q < nt ? ld : 0) raw[q].load(from, n);
+    }
+    const int m = Q == 4 ? w & 3 : 0;                          // the token that this lane sees to
+    int64_t at = m < nt ? kv_slot(a, t0 + m) : -1;
+    if (at >= a.n_slots) {
+        if (w < Q) set_status(a.status, ISEG_DEV_RANGE);
+        at = -1;
+    }
+    const int32_t slot = at < 0 ? -1 : (int32_t)at;
+    const KvPlace p = kv_place(a, slot < 0 ? 0 : slot, h);
+    const int nc = a.W / 32;
+    const int64_t off = val ? p.tile + (p.t >> 2) * nc * 4 + (p.t & 3) : p.row * (a.W / 2);      // in the codes
+    uint32_t big = 0;
+#pragma unroll
+    for (int q = 0; q < Q; q++) {
+        const uint32_t b = kv_max<LPR>(kv_big(raw[q]));
+        big = q == 0 || m == q ? b : big;
+    }
+    const float sm = kv_scale(kv_bits<T>(big), a.mode), im = 1.f / sm;
+    if (w < Q && slot >= 0) {
+        (val ? a.vs : a.ks)[p.row] = sm;
+        if (!(sm == sm)) set_status(a.status, ISEG_DEV_NONFINITE);
+    }
+    uint32_t x[Q][8];
+    int32_t slots[Q];
+    int64_t offs[Q];
+#pragma unroll
+    for (int q = 0; q < Q; q++) {
+        const float s = __builtin_bit_cast(float, kv_from<Q>(__builtin_bit_cast(uint32_t, sm), q));
+        const float inv = __builtin_bit_cast(float, kv_from<Q>(__builtin_bit_cast(uint32_t, im), q));
+        slots[q] = (int32_t)kv_from<Q>((uint32_t)slot, q);
+        offs[q] = (int64_t)((uint64_t)kv_from<Q>((uint32_t)(off >> 32), q) << 32 | kv_from<Q>((uint32_t)off, q));
+        float f[8];
+#pragma unroll
+        for (int e = 0; e < 8; e++) f[e] = raw[q].at(e);
+        kv_codes(f, s, inv, x[q]);
+        if (!(s == s)) {                                       // zeros
+#pragma unroll
+            for (int e = 0; e < 8; e++) x[q][e] = 8u << 19;
+        }
+    }
+    if (!val) {
+        // even codes in the low half, odd ones in the high half
+#pragma unroll
+        for (int q = 0; q < Q; q++) {
+            const uint32_t word = kv_halves(kv_gather(x[q][0], x[q][4], x[q][1], x[q][5]), kv_gather(x[q][2], x[q][6], x[q][3], x[q][7]));
+            if (slots[q] >= 0 && w < words) *(uint32_t*)(a.kc + offs[q] + w * 4) = word;
+        }
+        return;
+    }
+    // four tokens' codes of a column; the lane without bit 1 has the low halves'
+    // columns, its partner the high ones'
+    uint32_t word[4];
+    const bool hi = w & 2;
+#pragma unroll
+    for (int e = 0; e < 4; e++) {
+        const uint32_t y = Q == 4 ? kv_gather(x[0][e], x[Q / 4][e], x[Q / 2][e], x[Q - 1][e]) : x[0][e] >> 16;
+        const uint32_t z = Q == 4 ? kv_gather(x[0][4 + e], x[Q / 4][4 + e], x[Q / 2][4 + e], x[Q - 1][4 + e]) : x[0][4 + e] >> 16;
+        const uint32_t give = hi ? y : z, mine = hi ? z : y;
+        const uint32_t got = (uint32_t)__builtin_amdgcn_update_dpp((int)give, (int)give, 0x4e, 0xf, 0xf, false);
+        word[e] = kv_halves(hi ? got : mine, hi ? mine : got);
+    }
+    if (w >= words) return;
+    uint8_t* to = a.vc + ((w & 1) * 8 + ((w & 2) ? 4 : 0)) * 16 * nc + (w >> 2) * 4;
+    const int32_t first = slots[0];
+    if (Q == 4 && first >= 0 && (first & 3) == 0 && slots[Q / 4] == first + 1 && slots[Q / 2] == first + 2 && slots[Q - 1] == first + 3) {
+#pragma unroll
+        for (int e = 0; e < 4; e++) *(uint32_t*)(to + offs[0] + 16 * e * nc) = word[e];
+        return;
+    }
+#pragma unroll
+    for (int t = 0; t < Q; t++) {
+        if (slots[t] < 0) continue;
+#pragma unroll
+        for (int e = 0; e < 4; e++) to[offs[t] + 16 * e * nc] = (uint8_t)(word[e] >> (8 * t));
+    }
+}
+
 // whether four tokens lie side by side in one run of four of a tile
 __device__ __forceinline__ bool kv_beside(const int64_t* slot, const KvArgs& a)
 {
@@ -81,119 +289,17 @@ __device__ __forceinline__ bool kv_beside(const int64_t* slot, const KvArgs& a)
            slot[3] == slot[0] + 3;
 }
 
-// LPR lanes a row, eight columns (a word of codes) a lane, four tokens of a head
-// at a time; blockIdx.y: keys or values.  The largest magnitude over the row's
-// lanes, the scale, the codes.  A byte of v holds columns 16 apart, which lie two
-// lanes apart: each pair of lanes exchanges words and has half of the eight
-// bytes.  Tokens side by side, as a prompt's are, store v in words of four
-// tokens, others in bytes.
-template <typename T, int LPR, int Q>
-__global__ __launch_bounds__(256) void k_kv4_write(KvArgs a)
-{
-    const int w = threadIdx.x % LPR, words = a.W / 8;
-    const int64_t r = (int64_t)blockIdx.x * (256 / LPR) + threadIdx.x / LPR;
-    if (r >= a.rows) return;
-    const bool val = blockIdx.y != 0;
-    // four groups after one another have sixteen tokens of a head: a tile's lines are
-    // then written by one wave
-    const int64_t u = Q == 4 ? r >> 2 : r, ut = u / a.H;
-    const int h = (int)(u - ut * a.H);
-    const int64_t t0 = Q == 4 ? ut * 16 + (r & 3) * 4 : ut;
-    const int nt = (int)(a.T - t0 < Q ? a.T - t0 : Q);
-    if (nt <= 0) return;
-    const T* x0 = val ? (const T*)a.v + h * a.v_hs : (const T*)a.k + h * a.k_hs;
-    const int64_t ld = val ? a.v_ld : a.k_ld;
-    int64_t slot[Q];
-    float f[Q][8];
-#pragma unroll
-    for (int q = 0; q < Q; q++) {
-        slot[q] = q < nt ? kv_slot(a, t0 + q) : -1;
-        if (slot[q] >= a.n_slots) {
-            if (w == 0) set_status(a.status, ISEG_DEV_RANGE);
-            slot[q] = -1;
-        }
-    }
-#pragma unroll
-    for (int q = 0; q < Q; q++) kv_get8(x0 + (t0 + (q < nt ? q : 0)) * ld, w * 8, a.D, f[q]);
-    uint32_t bytes[Q];                                         // v: of each token
-#pragma unroll
-    for (int q = 0; q < Q; q++) {
-        uint32_t big = 0;
-#pragma unroll
-        for (int i = 0; i < 8; i++) {
-            const uint32_t b = bits_of(f[q][i]);
-            big = b > big ? b : big;
-        }
-#pragma unroll
-        for (int o = LPR / 2; o > 0; o >>= 1) {
-            const uint32_t b = (uint32_t)__shfl_xor((int)big, o, 64);
-            big = b > big ? b : big;
-        }
-        const Coder cd(kv_scale(big, a.mode));
-        const float s = cd.s;
-        uint32_t n[2];
-        codes_of<8, false>(f[q], nullptr, [&](int) -> const Coder& { return cd; }, 7, n);
-        if (!cd.ok) {
-            n[0] = n[1] = 0;
-            if (w == 0 && slot[q] >= 0) set_status(a.status, ISEG_DEV_NONFINITE);
-        }
-        // bytes n in [-7, 7] to n + 8
-        n[0] = (n[0] & 0x0f0f0f0fu) ^ 0x08080808u;
-        n[1] = (n[1] & 0x0f0f0f0fu) ^ 0x08080808u;
-        if (!val) {
-            if (slot[q] < 0) continue;
-            const KvPlace p = kv_place(a, slot[q], h);
-            // even codes in the low half, odd ones in the high half
-            uint32_t word = 0;
-#pragma unroll
-            for (int e = 0; e < 8; e++) word |= ((n[e >> 2] >> (8 * (e & 3))) & 15u) << ((e & 1) * 16 + (e >> 1) * 4);
-            if (w < words) *(uint32_t*)(a.kc + p.row * (a.W / 2) + w * 4) = word;
-            if (w == 0) a.ks[p.row] = s;
-        } else {
-            // the lane without bit 1 has the low halves' columns, its partner the high ones'
-            const bool hi = w & 2;
-            const uint32_t give = hi ? n[0] : n[1], mine = hi ? n[1] : n[0];
-            const uint32_t got = (uint32_t)__shfl_xor((int)give, 2, 64);
-            bytes[q] = hi ? got | mine << 4 : mine | got << 4;
-            if (w == 0 && slot[q] >= 0) a.vs[kv_place(a, slot[q], h).row] = s;
-        }
-    }
-    if (!val || w >= words) return;
-    const int i = w >> 2, c0 = (w & 1) * 8 + ((w & 2) ? 4 : 0), nc = a.W / 32;
-    if constexpr (Q == 4) if (kv_beside(slot, a)) {
-        const KvPlace p = kv_place(a, slot[0], h);
-        uint8_t* q = a.vc + p.tile + ((c0 * 4 + (p.t >> 2)) * nc + i) * 4;
-        // four tokens' bytes of four columns to four columns' bytes of four tokens
-        const uint32_t lo01 = __builtin_amdgcn_perm(bytes[1], bytes[0], 0x05010400), lo23 = __builtin_amdgcn_perm(bytes[3], bytes[2], 0x05010400);
-        const uint32_t hi01 = __builtin_amdgcn_perm(bytes[1], bytes[0], 0x07030602), hi23 = __builtin_amdgcn_perm(bytes[3], bytes[2], 0x07030602);
-        *(uint32_t*)(q) = __builtin_amdgcn_perm(lo23, lo01, 0x05040100);
-        *(uint32_t*)(q + 16 * nc) = __builtin_amdgcn_perm(lo23, lo01, 0x07060302);
-        *(uint32_t*)(q + 32 * nc) = __builtin_amdgcn_perm(hi23, hi01, 0x05040100);
-        *(uint32_t*)(q + 48 * nc) = __builtin_amdgcn_perm(hi23, hi01, 0x07060302);
-        return;
-    }
-#pragma unroll
-    for (int t = 0; t < Q; t++) {
-        if (slot[t] < 0) continue;
-        const KvPlace p = kv_place(a, slot[t], h);
-        uint8_t* q = a.vc + p.tile + ((c0 * 4 + (p.t >> 2)) * nc + i) * 4 + (p.t & 3);
-#pragma unroll
-        for (int e = 0; e < 4; e++) q[16 * e * nc] = (uint8_t)(bytes[t] >> (8 * e));
-    }
-}
-
 template <typename T, int LPR, int Q>
 __global__ __launch_bounds__(256) void k_kv4_read(KvArgs a)
 {
     const int w = threadIdx.x % LPR, words = a.W / 8;
-    const int64_t r = (int64_t)blockIdx.x * (256 / LPR) + threadIdx.x / LPR;
+    const uint32_t r = blockIdx.x * (uint32_t)(256 / LPR) + threadIdx.x / LPR;
     if (r >= a.rows || w >= words) return;
     const bool val = blockIdx.y != 0;
-    // four groups after one another have sixteen tokens of a head: a tile's lines are
-    // then written by one wave
-    const int64_t u = Q == 4 ? r >> 2 : r, ut = u / a.H;
-    const int h = (int)(u - ut * a.H);
-    const int64_t t0 = Q == 4 ? ut * 16 + (r & 3) * 4 : ut;
+    // sixteen tokens of a head by four groups after one another, as in the writing
+    const uint32_t u = Q == 4 ? r >> 2 : r, ut = u / (uint32_t)a.H;
+    const int h = (int)(u - ut * (uint32_t)a.H);
+    const int64_t t0 = Q == 4 ? (int64_t)ut * 16 + (r & 3) * 4 : ut;
     const int nt = (int)(a.T - t0 < Q ? a.T - t0 : Q);
     if (nt <= 0) return;
     int64_t slot[Q];

@@ -84,6 +84,35 @@ def test_codes_are_those_of_quantize_rows():
         assert torch.equal(k, want) and torch.equal(v, want)
 
 
+@pytest.mark.parametrize("t", ["fp32", "fp16", "bf16"])
+@pytest.mark.parametrize("pow2", [False, True])
+def test_codes_beside_the_half_steps(t, pow2):
+    """Elements on half-steps of their row's scale, as far as the type has them, and
+    its next numbers to either side; scales from the least to the largest."""
+    from paper_2011_14504_amd import iseg
+    r, rows, D = rng(5), 400, 128
+    info = torch.finfo(DT[t])
+    lo, hi = max(-50.0, np.log2(info.tiny) + 8), min(125.0, np.log2(info.max) - 1)
+    big = torch.from_numpy(np.exp2(r.uniform(lo, hi, rows))).to(DT[t])
+    big[:len(big) // 2] = (big[:len(big) // 2].double() / 7).to(DT[t]) * 7          # multiples of 7, where a tie is a number of the type
+    _, s = _quantized(big.double()[:, None], pow2)
+    half = (torch.arange(D) % 16 - 7.5)[None] * s.double()[:, None]
+    x = half.clamp(-info.max, info.max).to(DT[t])
+    x = torch.where(x.double().abs() > big.double()[:, None], big[:, None].expand(-1, D), x)
+    up, down = torch.nextafter(x, torch.full_like(x, info.max)), torch.nextafter(x, torch.full_like(x, -info.max))
+    pick = torch.from_numpy(r.integers(0, 3, (rows, D)))
+    x = torch.where(pick == 0, x, torch.where(pick == 1, up, down))
+    x = torch.where(x.double().abs() > big.double()[:, None], big[:, None].expand(-1, D), x)
+    x[:, 0] = big
+    c, sl = iseg.kv4_cache(rows // 16, 1, D, 16, DEV), torch.arange(rows, device=DEV)
+    n, s = _quantized(x.double(), pow2)
+    for at in (sl, torch.arange(rows - 1, -1, -1, device=DEV)):
+        iseg.kv4_write(x[:, None].to(DEV), x[:, None].to(DEV), at, c, iseg.ISEG_SCALE_POW2 if pow2 else iseg.ISEG_SCALE_MAX)
+        assert torch.equal(c.k_scale[:, 0].reshape(-1)[at].cpu(), s) and torch.equal(c.v_scale, c.k_scale)
+        for y in iseg.kv4_read(at, c, D):
+            assert torch.equal(y[:, 0].cpu(), n.float() * s[:, None])
+
+
 def test_extreme_rows():
     """Rows of zeros, of the smallest and largest numbers, of NaN and infinity."""
     from paper_2011_14504_amd import iseg
