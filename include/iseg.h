@@ -778,7 +778,8 @@ int iseg_logprob_bwd(const void* logits, const void* tokens, const float* lse, c
  * are left out), no free page or no column left (the tokens of such a page get
  * slot -1, its table entry -1 where there is a column, and held_out counts the
  * pages that were got), or a page id outside [0, n_pages) (slot -1).
- * n_pages page < 2^31; B and T < 2^31. */
+ * B and T < 2^31.  ISEG_ERR_UNSUPPORTED: n_pages page > 2^31, max_pages or F of
+ * 2^31 and more. */
 typedef struct iseg_page_map_geom {
     int64_t B, T;
     int64_t max_pages, table_ld;
@@ -812,7 +813,7 @@ int iseg_page_map(const int32_t* ctx, const int32_t* count, const int32_t* held,
  *   dgamma = sum over tokens and heads of g xhat
  * dgamma_q, dgamma_k [D] of p_dtype, each may be NULL (with norm = 0 they must
  * be); zeros if there are no rows.  Sums have one fixed order.
- * D <= 512 (ISEG_ERR_UNSUPPORTED beyond), 0 <= rope_dim <= D and even. */
+ * 0 <= rope_dim <= D and even.  ISEG_ERR_UNSUPPORTED: D > 512, Hq or Hk > 65536. */
 typedef struct iseg_qk_norm_rope_geom {
     int64_t T, Hq, Hk, D;
     int64_t q_ld, q_hs, k_ld, k_hs;
@@ -854,7 +855,8 @@ int iseg_qk_norm_rope_bwd(const void* dyq, const void* dyk, const void* q, const
  *
  * iseg_kv4_read -- the values at slots, code * scale rounded to dtype; zeros for
  * a negative slot, and for one outside the cache, which sets ISEG_DEV_RANGE.
- * D <= 256 (ISEG_ERR_UNSUPPORTED beyond). */
+ * ISEG_ERR_UNSUPPORTED: D > 256, page > 8192, n_pages page > 2^31, H > 65536,
+ * T H >= 2^27. */
 typedef struct iseg_kv4_geom {
     int64_t T, H, D;
     int64_t k_ld, k_hs, v_ld, v_hs;
@@ -885,9 +887,13 @@ int iseg_kv4_read(const uint8_t* k_codes, const float* k_scale, const uint8_t* v
  * max_q, max_kv: what the caller knows of the longest request's new tokens and
  * of the longest kv_len (0: T and max_pages page).  A request beyond either, a
  * q_start that falls or leaves [0, T], a negative kv_len or a page id outside
- * [0, n_pages) (its keys count as unseen) sets ISEG_DEV_RANGE.
- * D a multiple of 8, at most 256; Hq a multiple of H; scale > 0, finite;
- * max_kv < 2^31 - 2^16. */
+ * [0, n_pages) (its keys count as unseen) sets ISEG_DEV_RANGE.  Table entries whose
+ * tokens no query of the request sees, as those behind a window, may hold
+ * anything.
+ * D a multiple of 8, at most 256; Hq a multiple of H; scale > 0, finite.
+ * ISEG_ERR_UNSUPPORTED: Hq > 65536, max_pages >= 2^27, max_kv >= 2^31 - 2^16,
+ * window >= 2^40, n_pages H page / 16 >= 2^31, or a launch of 2^32 threads (H times
+ * B, or times T Hq / H over 128 to 256, beyond about 2^23). */
 typedef struct iseg_kv4_attention_geom {
     int64_t T, B, Hq, H, D;
     int64_t q_ld, q_hs, o_ld, o_hs;
@@ -922,7 +928,7 @@ int iseg_kv4_attention(const void* q, const uint8_t* k_codes, const float* k_sca
  * [0, V) (refused; the remainder is max(p_i - q_i, 0) still), a row without any
  * mass (its token is -1).  ISEG_DEV_NONFINITE: a used row with a NaN, an infinity
  * or a negative value (the token is unspecified within [-1, V)).
- * V in [1, 2^31). */
+ * V in [1, 2^31); ISEG_ERR_UNSUPPORTED: B > 2^16, S > 2^20. */
 typedef struct iseg_verify_geom {
     int64_t B, S, V;
     int64_t t_bs, t_ld, d_bs, d_ld;

@@ -461,7 +461,8 @@ template <int PER, int STRIDE>
 struct KaTiles {
     static constexpr int N = 64 / PER;   // steps of a look-up
     const int32_t* row;
-    int32_t first, end;                  // first tile, tiles of the request
+    int32_t first, from, end;            // first tile; those between [from, end) hold keys that a row sees, others are not
+                                         // asked for (pages behind a window may be gone)
     int32_t page;                        // of the next look-up
     int idx;                             // -1: past the keys, or a page id out of range
     uint64_t there;                      // idx >= 0
@@ -482,7 +483,7 @@ struct KaTiles {
     __device__ __forceinline__ void look(const KaArgs& a, int h, int it)
     {
         const int32_t t16 = tile_of(it), pg = page;
-        const bool in = t16 < end, ok = in && pg >= 0 && pg < a.n_pages;
+        const bool in = t16 >= from && t16 < end, ok = in && pg >= 0 && pg < a.n_pages;
         if (in && !ok) set_status(a.status, ISEG_DEV_RANGE);
         idx = ok ? (pg * a.H + h) * a.p16 + (t16 - column(a, t16) * a.p16) : -1;
         there = __ballot(ok);
@@ -532,7 +533,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(ka_few_wave
 
     // the words of 32 keys; the next step's keys are requested once the scores are
     // there, its values once they are summed up
-    KaTiles<2, 8> tl = {a.table + b * a.table_ld, key0 >> 4, (kv + 15) >> 4, 0, -1, 0};
+    KaTiles<2, 8> tl = {a.table + b * a.table_ld, key0 >> 4, x.any_lo >> 4, (kv + 15) >> 4, 0, -1, 0};
     if (n_it > 0) tl.ask(a, 0);
     KaWords<NC> kw[2], vw[2];
     f4_t ks_next[2], vs_next[2];
@@ -668,7 +669,7 @@ __global__ __launch_bounds__(64 * kWaves) void k_kv4_many(KaArgs a)
 
     // one half of the waves bring a tile of keys each, the other one nibble of a
     // pair of tiles of values and the scales of one tile
-    KaTiles<4, 4> tl = {a.table + b * a.table_ld, key0 >> 4, (kv + 15) >> 4, 0, -1, 0};
+    KaTiles<4, 4> tl = {a.table + b * a.table_ld, key0 >> 4, (int32_t)l0 >> 4, (kv + 15) >> 4, 0, -1, 0};
     const bool values = wave >= 4;
     const int own = wave & 3, vn = wave & 1;
     KaWords<NC> wa, wb;
@@ -895,9 +896,9 @@ int ka_check(const iseg_kv4_attention_geom* g)
         return ISEG_ERR_UNSUPPORTED;
     if (g->T > 0 && g->B > 0) {
         const KaPlan p = ka_plan(g);
-        const int64_t most = (int64_t)1 << 24;               // blocks of 256 threads of a launch
+        const int64_t most = (int64_t)1 << 24;               // blocks of 256 threads of a launch, half of 512
         if (g->B * g->H * p.splits >= most || (p.splits > 1 && g->B * g->H * 16 * p.R >= most) ||
-            p.tiles2 * g->H * p.splits2 >= most || (p.splits2 > 1 && p.tiles2 * g->H * p.many_rows >= most))
+            p.tiles2 * g->H * p.splits2 >= most / 2 || (p.splits2 > 1 && p.tiles2 * g->H * p.many_rows >= most))
             return ISEG_ERR_UNSUPPORTED;
     }
     return ISEG_OK;

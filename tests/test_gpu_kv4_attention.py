@@ -5,7 +5,7 @@ import numpy as np
 import pytest
 import torch
 
-from lm_util import DEV, DT, HALF, U, within
+from lm_util import DEV, DT, HALF, U, normal, within
 from serve_util import Cache, attention, rng, table_of, typed
 
 pytestmark = pytest.mark.gpu
@@ -215,3 +215,22 @@ def test_strides_of_queries_and_outputs():
         by_head = q.transpose(0, 1).contiguous().transpose(0, 1)         # heads before tokens
         got, _ = iseg.kv4_attention(by_head, cache.gpu(), table, *args)
         assert torch.equal(got, want)
+
+
+@pytest.mark.parametrize("gone", [-1, 1 << 30])
+@pytest.mark.parametrize("n,kv,window,page", [(1, 400, 40, 16), (1, 400, 65, 16), (1, 16, 1, 16), (5, 700, 100, 16), (100, 900, 90, 16), (100, 900, 90, 48), (40, 1500, 200, 32),
+                                              (1, 5000, 17, 16)])
+def test_pages_behind_the_window(n, kv, window, page, gone):
+    """Entries of pages whose tokens no query sees are not used."""
+    from paper_2011_14504_amd import iseg
+    held = -(-kv // page)
+    cache = Cache(3, held + 1, 2, 64, page)
+    full = table_of(4, [held], held + 1, held)
+    part = full.copy()
+    part[0, :max(0, kv - n + 1 - window) // page] = gone
+    q = normal(5, n, 8, 64).to(torch.bfloat16).to(DEV)
+    st = torch.zeros(1, dtype=torch.int32, device=DEV)
+    a, b = (iseg.kv4_attention(q, cache.gpu(), torch.from_numpy(t).to(DEV), torch.tensor([0, n], dtype=torch.int32, device=DEV),
+                               torch.tensor([kv], dtype=torch.int32, device=DEV), window=window, status=st) for t in (full, part))
+    assert iseg.iseg_status_read(st) == 0
+    assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
