@@ -504,6 +504,17 @@ constexpr int ka_few_waves(int nc, int r, bool wide)
 // few rows: the four waves of a block hold the same rows and deal the keys among
 // themselves
 // ---------------------------------------------------------------------------
+// Bound by the cache's bytes, each read once: with G = 4 a tile of 16 rows is a quarter
+// full and its products cost less than the bytes.  A wave has one step of 32 keys in
+// hand and the next one under way, and three waves a SIMD (168 registers; four waves
+// would spill: 220 us) keep about 13 MB on their way.  64 requests of 8192 keys, 8
+// heads of 128: 571 MB in 114 us, 5.0 TB/s, the copy's rate.  Shorter work has the
+// blocks' beginnings and ends on top (queries, table and first keys one after the
+// other, then the join): 64 of 820 to 8192 keys, 315 MB, 84 us, of which the loads
+// alone take 72; 1 of 131072, 143 MB, 32 us, the loads 28.  Parts dealt by length
+// (prefix sums of all requests in every block) took 85 and 33, and 120 where all have
+// one length.  float32 tensors: 133 us at 64 x 8192; heads of 256, 32 x 8192: 137.
+//
 // NC: words of a row's quarter (W / 32).  R: tiles of 16 rows.
 template <int NC, int R, bool WIDE>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(ka_few_waves(NC, R, WIDE)))) void k_kv4_few(KaArgs a)
@@ -629,6 +640,15 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(ka_few_wave
 // many rows: eight waves with 16 R rows each; 64 keys at a time become float16
 // operands in LDS, once for all of them
 // ---------------------------------------------------------------------------
+// Bound by the sum of matrix and vector instructions: a 16x16x32 product takes 16
+// cycles of the matrix cores and 8 of the wave's issue, so two waves a SIMD hardly
+// overlap them.  3 x 3001 queries behind as many keys, 32 heads over 8 of 128: 870 to
+// 920 us for 663 GFLOP that are needed (720 to 760 TFLOP/s; the library's largest
+// products reach 1377).  Without products and softmax it takes 502 (loads, codes to
+// LDS, barriers), without its stages 78.  1 x 4096: 210 us; in float32 (two terms of q
+// and p, twice the products) 390; heads of 256 225.
+// Tried and slower: sixteen waves of 16 rows (1158), twelve waves (spills), 32x32x16
+// products with V's scale per stage (897 to 945), stages of 128 keys (896).
 constexpr int kWaves = 8;
 
 // a stage of 64 keys: operands of 1 KB each (64 lanes of 16 bytes), and scales
@@ -762,7 +782,8 @@ __global__ __launch_bounds__(64 * kWaves) void k_kv4_many(KaArgs a)
 }
 
 // The splits' parts of a row: a block a row, whose groups of W / 4 threads take
-// every so many splits; the groups are added in their order.
+// every so many splits; the groups are added in their order.  4.6 us at 32 rows of 96
+// parts, 5.9 at 2048 of three: a launch and two trips to memory.
 template <int TR, bool SHARED>
 __global__ __launch_bounds__(256) void k_kv4_join(KaArgs a)
 {

@@ -124,8 +124,7 @@ __device__ __forceinline__ uint32_t kv_from(uint32_t v, int q)
 
 // Scale of a largest magnitude given as float32 bits: scale_of (coder.h) with 4
 // bits, in float32.  A float32 quotient rounded once is the float64 one rounded to
-// float32 (24 bits twice and two more fit in 53).  In float64 the write of 30011
-// tokens takes 2 us more.
+// float32 (24 bits twice and two more fit in 53).
 __device__ __forceinline__ float kv_scale(uint32_t big, int mode)
 {
     if (big >= 0x7f800000u) return __builtin_nanf("");
@@ -180,6 +179,11 @@ __device__ __forceinline__ uint32_t kv_halves(uint32_t lo, uint32_t hi) { return
 // four tokens.  A byte of v holds columns 16 apart, which lie two lanes apart: each
 // pair of lanes exchanges words and has half of the eight bytes.  Tokens side by
 // side, as a prompt's are, store v in words of four tokens, others in bytes.
+//
+// Bound by memory, with the vector instructions close behind (about 15 an element;
+// with the row quantizers' coder, a scale in every lane and loads that waited for one
+// another it was 58 us): 30011 tokens of 8 heads of 128 bf16, 156 MB, in 33 to 36 us,
+// 4.3 to 4.7 TB/s; float32, 278 MB, in 70.
 template <typename T, int LPR, int Q>
 __global__ __launch_bounds__(256) void k_kv4_write(KvArgs a)
 {
@@ -289,6 +293,8 @@ __device__ __forceinline__ bool kv_beside(const int64_t* slot, const KvArgs& a)
            slot[3] == slot[0] + 3;
 }
 
+// The same deal the other way: 30011 tokens of 8 heads of 128 to bf16, 156 MB, in 27
+// us (5.7 TB/s: the codes come from the last-level cache).
 template <typename T, int LPR, int Q>
 __global__ __launch_bounds__(256) void k_kv4_read(KvArgs a)
 {
@@ -383,9 +389,11 @@ KvArgs kv_args(const iseg_kv4_geom* g, const void* slots, int32_t* status)
 {
     KvArgs a = {};
     a.slots = slots; a.T = g->T;
-    // one token a group of lanes until there are groups of four for the whole card:
-    // 64 tokens of 8 heads 4.0 us against 8.5, 30011 tokens 64 against 78
-    a.four = g->T * g->H >= 4096;
+    // one token a group of lanes until there are groups of four for the whole card (8
+    // heads of 128 bf16, writing and reading: 64 tokens 3.9 + 3.2 us against 5.1 + 4.2, 512
+    // 4.8 + 3.6 against 5.2 + 4.6, 2048 8.4 + 6.3 against 5.9 + 5.4, 30011 69 + 45 against
+    // 33 + 27)
+    a.four = g->T * g->H >= 8192;
     a.rows = a.four ? ceil_div64(g->T, 16) * 4 * g->H : g->T * g->H;
     a.k_ld = g->k_ld; a.k_hs = g->k_hs; a.v_ld = g->v_ld; a.v_hs = g->v_hs;
     a.n_slots = g->n_pages * g->page; a.H = (int32_t)g->H; a.D = (int32_t)g->D; a.W = kv4_width(g->D); a.page = g->page;
@@ -430,6 +438,7 @@ struct PmArgs {
     int32_t *w_held, *w_first, *w_free;       // workspace: pages held before, first page taken, free pages before
     int64_t T, max_pages, table_ld, F, n_pages;
     int32_t B, page;
+    int32_t lanes;                   // 2^lanes threads write a request's new pages
     int32_t* status;
 };
 
@@ -450,8 +459,12 @@ __device__ __forceinline__ void scan2_1024(int64_t& x, int64_t& y, int64_t (*red
 
 __device__ __forceinline__ int32_t sat31(int64_t v) { return (int32_t)(v < 0x7fffffff ? v : 0x7fffffff); }
 
-// by one block: lengths, pages wanted, their sums
-__device__ __forceinline__ void page_scan(const PmArgs& a)
+// Pages of a step.  There is next to nothing to move (256 requests: 6 KB); what counts
+// is the chain lengths -> sums -> page taken -> slot, each link a trip to memory.
+//
+// by one block: lengths, pages wanted, their sums; `near` (LDS, or NULL) gets q_start
+// as well
+__device__ __forceinline__ void page_scan(const PmArgs& a, int32_t* near)
 {
     __shared__ int64_t red[2][16];
     __shared__ int64_t base[2];
@@ -485,6 +498,7 @@ __device__ __forceinline__ void page_scan(const PmArgs& a)
         first_p = base[1] + sp - need;
         if (b < a.B) {
             a.q_start[b] = sat31(first_t);
+            if (near) near[b] = sat31(first_t);
             a.w_held[b] = held;
             a.w_first[b] = sat31(first_p);
             const int64_t got = nf - first_p < 0 ? 0 : (nf - first_p < need ? nf - first_p : need);
@@ -498,10 +512,20 @@ __device__ __forceinline__ void page_scan(const PmArgs& a)
     if (threadIdx.x == 0) {
         if (base[0] > a.T) bad = 1;
         a.q_start[a.B] = sat31(base[0]);
+        if (near) near[a.B] = sat31(base[0]);
         *a.w_free = (int32_t)nf;
         *a.n_free_out = (int32_t)(nf > base[1] ? nf - base[1] : 0);
     }
     if (bad) set_status(a.status, ISEG_DEV_RANGE);
+}
+
+// entry k of the free list as a page; -1: none
+__device__ __forceinline__ int32_t page_taken(const PmArgs& a, int64_t k, int& bad)
+{
+    const int32_t pg = k >= 0 ? a.free_pages[k] : -1;
+    if (pg >= 0 && pg < a.n_pages) return pg;
+    bad = 1;
+    return -1;
 }
 
 // page of column `col` of request b: taken now, or in the table already; -1: none
@@ -513,9 +537,7 @@ __device__ __forceinline__ int32_t page_of(const PmArgs& a, int32_t b, int64_t c
     if (col < held) {
         pg = a.table[(int64_t)b * a.table_ld + col];
     } else {
-        const int64_t k = (int64_t)*a.w_free - 1 - a.w_first[b] - (col - held);
-        if (k >= 0) pg = a.free_pages[k];
-        else bad = 1;
+        return page_taken(a, (int64_t)*a.w_free - 1 - a.w_first[b] - (col - held), bad);
     }
     if (pg < 0 || pg >= a.n_pages) { bad = 1; pg = -1; }
     return pg;
@@ -534,11 +556,12 @@ __device__ __forceinline__ int32_t request_of(const int32_t* start, int32_t B, i
 }
 
 // tokens and then requests, dealt to `blocks` blocks of NT threads: a thread per
-// token; a wave per request for the pages that it takes
+// token, a few threads per request for the pages that it takes.  start: q_start, in LDS
+// where it fits, since the search for a token's request is a chain of reads
 template <int NT>
-__device__ __forceinline__ void page_fill(const PmArgs& a, int64_t block, int64_t blocks)
+__device__ __forceinline__ void page_fill(const PmArgs& a, const int32_t* start, int64_t block, int64_t blocks)
 {
-    const int64_t total = a.q_start[a.B];
+    const int64_t total = start[a.B];
     int bad = 0;
     for (int64_t r = block * NT + threadIdx.x; r < a.T; r += blocks * NT) {
         if (r >= total) {
@@ -546,34 +569,47 @@ __device__ __forceinline__ void page_fill(const PmArgs& a, int64_t block, int64_
             a.slots[r] = -1;
             continue;
         }
-        const int32_t b = request_of(a.q_start, a.B, r);
-        const int64_t c = a.ctx[b] < 0 ? 0 : a.ctx[b], p = c + (r - a.q_start[b]);
+        const int32_t b = request_of(start, a.B, r);
+        const int64_t c = a.ctx[b] < 0 ? 0 : a.ctx[b], p = c + (r - start[b]);
         const int64_t col = p / a.page;
         const int32_t pg = page_of(a, b, col, bad), in = (int32_t)(p - col * a.page);
         a.pos[r] = sat31(p);
         a.slots[r] = pg < 0 ? -1 : pg * a.page + in;
     }
-    for (int64_t b = block * (NT / 64) + (threadIdx.x >> 6); b < a.B; b += blocks * (NT / 64)) {
-        const int64_t c = a.ctx[b] < 0 ? 0 : a.ctx[b], n = a.count[b] < 0 ? 0 : a.count[b];
+    const int64_t free = *a.w_free;
+    for (int64_t r = block * NT + threadIdx.x; r < (int64_t)a.B << a.lanes; r += blocks * NT) {
+        const int64_t b = r >> a.lanes;
+        const int64_t c = a.ctx[b] < 0 ? 0 : a.ctx[b], n = a.count[b] < 0 ? 0 : a.count[b], held = a.w_held[b], first = a.w_first[b];
         int64_t want = (c + n + a.page - 1) / a.page;
         if (want > a.max_pages) want = a.max_pages;
-        for (int64_t col = a.w_held[b] + (int64_t)(threadIdx.x & 63); col < want; col += 64)
-            a.table[b * a.table_ld + col] = page_of(a, (int32_t)b, col, bad);
+        for (int64_t col = held + (r & ((1 << a.lanes) - 1)); col < want; col += (int64_t)1 << a.lanes)
+            a.table[b * a.table_ld + col] = page_taken(a, free - 1 - first - (col - held), bad);
     }
     if (bad) set_status(a.status, ISEG_DEV_RANGE);
 }
 
-__global__ __launch_bounds__(1024) void k_page_scan(PmArgs a) { page_scan(a); }
+constexpr int kStarts = 4096;              // requests whose first rows LDS holds
 
-__global__ __launch_bounds__(256) void k_page_fill(PmArgs a) { page_fill<256>(a, blockIdx.x, gridDim.x); }
+__global__ __launch_bounds__(1024) void k_page_scan(PmArgs a) { page_scan(a, nullptr); }
 
-// a decoding step: both in one block, whose own writes to q_start and the
-// workspace the barrier makes visible to it
+__global__ __launch_bounds__(256) void k_page_fill(PmArgs a)
+{
+    __shared__ int32_t near[kStarts + 1];
+    if (a.B <= kStarts) {
+        for (int32_t b = threadIdx.x; b <= a.B; b += 256) near[b] = a.q_start[b];
+        __syncthreads();
+    }
+    page_fill<256>(a, a.B <= kStarts ? near : a.q_start, blockIdx.x, gridDim.x);
+}
+
+// a decoding step: both in one block, whose own writes to the workspace the barrier
+// makes visible to it
 __global__ __launch_bounds__(1024) void k_page_map(PmArgs a)
 {
-    page_scan(a);
+    __shared__ int32_t near[1025];
+    page_scan(a, near);
     __syncthreads();
-    page_fill<1024>(a, 0, 1);
+    page_fill<1024>(a, near, 0, 1);
 }
 
 int pm_check(const iseg_page_map_geom* g)
@@ -652,13 +688,18 @@ extern "C" int iseg_page_map(const int32_t* ctx, const int32_t* count, const int
     a.w_free = (int32_t*)((char*)ws + 2 * align256((size_t)g->B * 4));
     a.T = g->T; a.max_pages = g->max_pages; a.table_ld = g->table_ld; a.F = g->F; a.n_pages = g->n_pages;
     a.B = (int32_t)g->B; a.page = g->page; a.status = dev_status;
-    // up to 4096 tokens of 1024 requests the one block takes no longer than a second
-    // launch (256 requests of one token: 6 us, and 5 + 3 in two)
+    // threads for about as many pages as a request takes on average, and the first few
+    const int64_t pages = g->B > 0 ? g->T / g->B / g->page : 0;
+    a.lanes = 2;
+    while (a.lanes < 6 && (1 << a.lanes) < pages) a.lanes++;
+    // up to 4096 tokens of 1024 requests by one block: a launch less for the host (about
+    // 4 us), and captured 256 requests of one token 5.7 us against 7.2, 1000 8.4 against
+    // 9.3, 900 of four 11.7 against 9.6
     if (g->T <= 4096 && g->B <= 1024) {
         hipLaunchKernelGGL(k_page_map, dim3(1), dim3(1024), 0, stream, a);
     } else {
         hipLaunchKernelGGL(k_page_scan, dim3(1), dim3(1024), 0, stream, a);
-        const int64_t items = ceil_div64(g->T, 256) > ceil_div64(g->B, 4) ? ceil_div64(g->T, 256) : ceil_div64(g->B, 4);
+        const int64_t fill = g->B << a.lanes, items = ceil_div64(g->T > fill ? g->T : fill, 256);
         hipLaunchKernelGGL(k_page_fill, dim3((unsigned)(items < 2048 ? items : 2048)), dim3(256), 0, stream, a);
     }
     return launch_ok();

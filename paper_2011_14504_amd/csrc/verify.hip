@@ -143,7 +143,9 @@ struct VfVec {
     }
 };
 
-// 64 x 131072 float32: 67 MB in 14.6 us, the copy's rate
+// Bound by memory, one row of p and one of q for each request: 64 x 131072 float32,
+// 67 MB, in 14.3 to 15.1 us, 4.5 to 4.7 TB/s.  One request: 4 us, the gathers and then
+// the row.
 template <typename T>
 __global__ __launch_bounds__(256) void k_verify_sums(VfArgs a)
 {
@@ -180,7 +182,8 @@ __global__ __launch_bounds__(256) void k_verify_sums(VfArgs a)
 
 // A block per request: the piece, then the element.  Where u is below 1 the first
 // piece whose running sum passes u times the whole has the token; should rounding
-// leave none, the last value with any mass is taken.
+// leave none, the last value with any mass is taken.  7.8 us at 64 requests, 5.9 at
+// one: a chain of five trips to memory and LDS.
 template <typename T>
 __global__ __launch_bounds__(256) void k_verify_pick(VfArgs a)
 {
