@@ -180,10 +180,11 @@ __device__ __forceinline__ uint32_t kv_halves(uint32_t lo, uint32_t hi) { return
 // pair of lanes exchanges words and has half of the eight bytes.  Tokens side by
 // side, as a prompt's are, store v in words of four tokens, others in bytes.
 //
-// Bound by memory, with the vector instructions close behind (about 15 an element;
-// with the row quantizers' coder, a scale in every lane and loads that waited for one
-// another it was 58 us): 30011 tokens of 8 heads of 128 bf16, 156 MB, in 33 to 36 us,
-// 4.3 to 4.7 TB/s; float32, 278 MB, in 70.
+// Bound by memory and, as closely, by the issue of 20 vector instructions an element
+// (five of them for ties, which a seventh of the rows of bf16 have; with the row
+// quantizers' coder, a scale in every lane and loads that waited for one another it was
+// 58 us): 30011 tokens of 8 heads of 128 bf16, 156 MB, in 33 to 37 us, 4.2 to 4.7 TB/s;
+// float32, 278 MB, in 70.
 template <typename T, int LPR, int Q>
 __global__ __launch_bounds__(256) void k_kv4_write(KvArgs a)
 {
