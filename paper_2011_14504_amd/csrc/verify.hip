@@ -4,7 +4,8 @@
 // Two kernels: in the first every wave decides how many drafts stand (2 S
 // gathers, all at once) and sums some pieces of the row that the next token comes
 // from; in the second a block per request finds the piece and then the element
-// where the running sum passes u times the whole.  Sums are float64: of float32
+// where the running sum passes u times the whole.  (Both in one block of 1024 threads
+// per request: 50021 tokens 20 us against 8.5 captured.)  Sums are float64: of float32
 // probabilities they are good to 2^-50, so that a random number of 24 bits meets a
 // border between tokens by accident about once in 2^26.
 #include "rowops.h"
