@@ -646,7 +646,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(ka_few_wave
 // 920 us for 663 GFLOP that are needed (720 to 760 TFLOP/s; the library's largest
 // products reach 1377).  Without products and softmax it takes 502 (loads, codes to
 // LDS, barriers), without its stages 78.  1 x 4096: 210 us; in float32 (two terms of q
-// and p, twice the products) 390; heads of 256 225.
+// and p, twice the products) 390; heads of 256 225.  R = 1 where a request has up to
+// 128 rows or a prompt is short (ka_cost).
 // Tried and slower: sixteen waves of 16 rows (1158), twelve waves (spills), 32x32x16
 // products with V's scale per stage (897 to 945), stages of 128 keys (896).
 constexpr int kWaves = 8;
@@ -781,10 +782,10 @@ __global__ __launch_bounds__(64 * kWaves) void k_kv4_many(KaArgs a)
     }
 }
 
-// The splits' parts of a row: a block a row, whose groups of W / 4 threads take
+// The splits' parts of the few rows: a block a row, whose groups of W / 4 threads take
 // every so many splits; the groups are added in their order.  4.6 us at 32 rows of 96
 // parts, 5.9 at 2048 of three: a launch and two trips to memory.
-template <int TR, bool SHARED>
+template <int TR>
 __global__ __launch_bounds__(256) void k_kv4_join(KaArgs a)
 {
     __shared__ float fs[kSplitsMax];
@@ -794,7 +795,7 @@ __global__ __launch_bounds__(256) void k_kv4_join(KaArgs a)
     int bad = 0;
     KaSeq s;
     int64_t b, row0;
-    if (!ka_tile<TR, SHARED>(a, tile, s, b, row0, bad)) return;
+    if (!ka_tile<TR, true>(a, tile, s, b, row0, bad)) return;
     if (row0 + r >= s.n * a.G) return;
     const int64_t at = (((int64_t)tile * a.H + h) * TR + r) * a.splits;
     const int lw = a.W / 4, groups = 256 / lw, grp = threadIdx.x / lw, d = (threadIdx.x - grp * lw) * 4;
@@ -841,6 +842,33 @@ __global__ __launch_bounds__(256) void k_kv4_join(KaArgs a)
     }
 }
 
+// The same for the rows of a tile of many: a group of W / 4 threads a row, the parts one
+// after the other (4000 rows of 8 heads in two parts: a block a row 63 us, so about 13).
+template <int TR>
+__global__ __launch_bounds__(256) void k_kv4_join_many(KaArgs a)
+{
+    const int lw = a.W / 4, rpb = 256 / lw, bpt = (TR + rpb - 1) / rpb, grp = threadIdx.x / lw, d = (threadIdx.x - grp * lw) * 4;
+    const int h = (blockIdx.x / bpt) % a.H, tile = blockIdx.x / bpt / a.H, r = blockIdx.x % bpt * rpb + grp;
+    int bad = 0;
+    KaSeq s;
+    int64_t b, row0;
+    if (!ka_tile<TR, false>(a, tile, s, b, row0, bad)) return;
+    if (grp >= rpb || r >= TR || row0 + r >= s.n * a.G) return;
+    const int64_t at = (((int64_t)tile * a.H + h) * TR + r) * a.splits;
+    float mr = kNone, lr = 0.f;
+    for (int i = 0; i < a.splits; i++) mr = fmaxf(mr, a.pm[(at + i) * 2]);
+    f4_t o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+    for (int i = 0; i < a.splits; i++) {
+        const float f = __builtin_amdgcn_exp2f(a.pm[(at + i) * 2] - mr);
+        lr += f * a.pm[(at + i) * 2 + 1];
+        o += f * *(const f4_t*)(a.po + (at + i) * a.W + d);
+    }
+    const int64_t q = (row0 + r) / a.G, tok = s.q0 + q, head = h * a.G + (row0 + r - q * a.G);
+    if (a.lse && d == 0) a.lse[tok * a.Hq + head] = ka_lse(mr, lr);
+    if (d < a.D) ka_store(a, tok * a.o_ld + head * a.o_hs, d, o, ka_inv(lr));
+}
+
 // ---------------------------------------------------------------------------
 // host
 // ---------------------------------------------------------------------------
@@ -849,7 +877,7 @@ __global__ __launch_bounds__(256) void k_kv4_join(KaArgs a)
 struct KaPlan {
     int R;                       // tiles of 16 rows of the first kind; 0: none
     int64_t tiles2;              // of the second kind; 0: none
-    int many_rows;
+    int R2, many_rows;
     int splits, splits2;
     size_t part, bytes;
 };
@@ -867,6 +895,21 @@ int64_t ka_max_kv(const iseg_kv4_attention_geom* g)
 }
 
 int64_t ka_max_q(const iseg_kv4_attention_geom* g) { return g->max_q > 0 && g->max_q < g->T ? g->max_q : g->T; }
+
+// Time of n tiles (with all heads) in sp splits, in stages of 64 keys for 256 rows (2.9
+// us): a block a CU at a time, each with three stages of beginning and end, the longest
+// first; with one tile of 16 rows a wave a stage takes 0.72 of that for 128 rows.  The
+// queries of a prompt see half of its own keys.  Splits write and read parts.  Without
+// it (256 rows always, splits for one round of blocks rounded up): 128 rows behind 131072
+// keys 261 us, 142 now; a prompt of 1000 100, 39 now; 100 tokens behind 99900 380, 281.
+double ka_cost(const iseg_kv4_attention_geom* g, int R, int64_t n, int sp, int64_t span)
+{
+    const double stages = span / 64 + 1, own = g->causal ? (double)(ka_max_q(g) < span ? ka_max_q(g) : span) / 128 : 0.0;
+    const double rounds = (double)ceil_div64(n * sp, 256), mean = rounds / sp * (stages - own);
+    const double time = (stages / sp > mean ? stages / sp : mean) + 3.0 * rounds;
+    const double parts = sp > 1 ? 2.0 + (double)(g->T * g->Hq * sp) * kv4_width(g->D) / 1.5e6 : 0.0;
+    return (R == 1 ? 0.72 : 1.0) * time + parts;
+}
 
 KaPlan ka_plan(const iseg_kv4_attention_geom* g)
 {
@@ -889,11 +932,23 @@ KaPlan ka_plan(const iseg_kv4_attention_geom* g)
         p.splits = (int)(sp < 1 ? 1 : (sp > kSplitsMax ? kSplitsMax : sp));
     }
     if (rows > 16 * most) {
-        p.many_rows = 16 * kWaves * ka_many(nc, ka_wide(g));
-        p.tiles2 = ceil_div64(g->T * G, p.many_rows) + g->B;
-        int64_t sp = ceil_div64(256, p.tiles2 * g->H), longest = ceil_div64(span, 512);
-        sp = sp < longest ? sp : longest;
-        p.splits2 = (int)(sp < 1 ? 1 : (sp > 32 ? 32 : sp));
+        // requests of more rows than the first kind's, each with a last tile that may not
+        // be full
+        const int64_t large = g->T * G / (p.R ? 16 * p.R + 1 : 1), ends = large < g->B ? large : g->B;
+        double best = 0.0;
+        for (int R = ka_many(nc, ka_wide(g)); R >= 1; R--) {
+            const int64_t TR = 16 * kWaves * R, all = (g->T * G - ends) / TR + ends, each = ends * ceil_div64(rows, TR);
+            const int64_t tiles = all < each ? all : each;
+            for (int sp = 1; sp <= 32 && (sp == 1 || sp * 512 <= span); sp++) {
+                const double c = ka_cost(g, R, tiles * g->H, sp, span);
+                if (p.tiles2 > 0 && c >= best) continue;
+                best = c;
+                p.R2 = R;
+                p.many_rows = (int)TR;
+                p.tiles2 = tiles;
+                p.splits2 = sp;
+            }
+        }
     }
     const int64_t n1 = p.R && p.splits > 1 ? pairs * 16 * p.R * p.splits : 0;
     const int64_t n2 = p.splits2 > 1 ? p.tiles2 * g->H * p.many_rows * p.splits2 : 0;
@@ -932,7 +987,19 @@ int ka_few(KaArgs& a, hipStream_t s)
     const int64_t rows = a.max_q * a.G;
     a.join_rows = (int32_t)(rows < 16 * R ? rows : 16 * R);
     if (a.splits > 1)
-        hipLaunchKernelGGL((k_kv4_join<16 * R, true>), dim3((unsigned)((int64_t)a.B * a.H * a.join_rows)), dim3(256), 0, s, a);
+        hipLaunchKernelGGL((k_kv4_join<16 * R>), dim3((unsigned)((int64_t)a.B * a.H * a.join_rows)), dim3(256), 0, s, a);
+    return launch_ok();
+}
+
+template <int NC, int R, bool WIDE>
+int ka_many_rows(const KaArgs& a, const KaPlan& p, hipStream_t s)
+{
+    constexpr size_t lds = 2 * sizeof(KaStage<NC>);
+    constexpr int TR = 16 * kWaves * R, rpb = 256 / (NC * 8);
+    if (!lds_limit((const void*)&k_kv4_many<NC, R, WIDE>, lds)) return ISEG_ERR_DEVICE;
+    hipLaunchKernelGGL((k_kv4_many<NC, R, WIDE>), dim3((unsigned)(p.tiles2 * a.H * a.splits)), dim3(64 * kWaves), lds, s, a);
+    if (a.splits > 1)
+        hipLaunchKernelGGL((k_kv4_join_many<TR>), dim3((unsigned)(p.tiles2 * a.H * ((TR + rpb - 1) / rpb))), dim3(256), 0, s, a);
     return launch_ok();
 }
 
@@ -952,17 +1019,11 @@ int ka_run(KaArgs a, const KaPlan& p, hipStream_t s)
             if (p.R == 4) rc = ka_few<NC, 4, WIDE>(a, s);
     }
     if (rc == ISEG_OK && p.tiles2 > 0) {
-        constexpr int R = ka_many(NC, WIDE);
-        constexpr size_t lds = 2 * sizeof(KaStage<NC>);
-        if (!lds_limit((const void*)&k_kv4_many<NC, R, WIDE>, lds)) return ISEG_ERR_DEVICE;
         a.rows_min = p.R ? 16 * p.R : 0;
         a.rows_max = 0x7fffffff;
         a.splits = p.splits2;
-        a.join_rows = p.many_rows;
-        hipLaunchKernelGGL((k_kv4_many<NC, R, WIDE>), dim3((unsigned)(p.tiles2 * a.H * a.splits)), dim3(64 * kWaves), lds, s, a);
-        if (a.splits > 1)
-            hipLaunchKernelGGL((k_kv4_join<16 * kWaves * R, false>), dim3((unsigned)(p.tiles2 * a.H * a.join_rows)), dim3(256), 0, s, a);
-        rc = launch_ok();
+        constexpr int R = ka_many(NC, WIDE);
+        rc = R == 1 || p.R2 == 1 ? ka_many_rows<NC, 1, WIDE>(a, p, s) : ka_many_rows<NC, R, WIDE>(a, p, s);
     }
     return rc;
 }
