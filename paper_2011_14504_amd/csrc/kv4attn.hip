@@ -211,15 +211,15 @@ __device__ __forceinline__ void ka_put(const KaArgs& a, const KaOut& o, int d, f
 }
 
 // eight elements of q's row that starts at element `at`, from d on, or zeros
-template <bool WIDE>
+template <int DT>
 __device__ __forceinline__ void ka_get8(const KaArgs& a, int64_t at, int d, bool in, float (&f)[8])
 {
 #pragma unroll
     for (int i = 0; i < 8; i++) f[i] = 0.f;
     if (!in) return;
-    if (WIDE) {
+    if constexpr (DT == ISEG_F32) {
         __builtin_memcpy(f, (const float*)a.q + at + d, 32);
-    } else if (a.dtype == ISEG_F16) {
+    } else if constexpr (DT == ISEG_F16) {
         _Float16 x[8];
         __builtin_memcpy(x, (const _Float16*)a.q + at + d, 16);
 #pragma unroll
@@ -246,12 +246,14 @@ __device__ __forceinline__ KaWords<NC> words(const uint8_t* p)
     return r;
 }
 
-// What a wave keeps of its 16 R rows.  WIDE: q and p as two float16 terms
-// (float32 tensors).
-template <int NC, int R, bool WIDE>
+// What a wave keeps of its 16 R rows.  DT: the tensors' type.  A float16 of q or p is
+// one rounding of 2^-11: q of float32 and p of float32 and float16 tensors are two such
+// terms.  (With one term of p, float16 outputs were 1.5 times as far from 64 bits as
+// their own rounding puts them; bfloat16's is eight times as large.)
+template <int NC, int R, int DT>
 struct KaRows {
-    static constexpr int NS = WIDE ? 2 : 1;
-    h8_t q[NS][R][NC];                   // queries as B operands
+    static constexpr int NQ = DT == ISEG_F32 ? 2 : 1, NS = DT == ISEG_BF16 ? 1 : 2;
+    h8_t q[NQ][R][NC];                   // queries as B operands
     float cf[R];                         // score per unit of S^T and scale of k
     int32_t lo[R], hi[R];                // keys that a lane's rows see
     int32_t full_lo, full_hi;            // keys that all rows see
@@ -274,12 +276,12 @@ struct KaRows {
             const int64_t at = in ? (s.q0 + r / a.G) * a.q_ld + (h * a.G + r % a.G) * a.q_hs : 0;
             auto get = [&](int w, float (&f)[8]) {
                 const int d = g4 * 8 * NC + w * 8;
-                ka_get8<WIDE>(a, at, d, in && d < a.D, f);
+                ka_get8<DT>(a, at, d, in && d < a.D, f);
             };
             // float16 reaches no further than 65504 and 2^-24: rows of the other
             // types are brought below 1 by a power of two first
             int e = 0;
-            if (WIDE || a.dtype != ISEG_F16) {
+            if (DT != ISEG_F16) {
                 float big = 0.f;
 #pragma unroll
                 for (int w = 0; w < NC; w++) {
@@ -301,7 +303,7 @@ struct KaRows {
                 for (int i = 0; i < 8; i++) {
                     const float x = ldexpf(f[i], -e);
                     q[0][t][w][i] = (_Float16)x;
-                    if constexpr (WIDE) q[NS - 1][t][w][i] = (_Float16)(x - (float)(_Float16)x);
+                    if constexpr (NQ > 1) q[NQ - 1][t][w][i] = (_Float16)(x - (float)(_Float16)x);
                 }
             }
             m[t] = kNone;
@@ -426,9 +428,9 @@ struct KaRows {
                     float v = p[order[r]];
                     // the product is rounded once for both terms (contracted with one of
                     // them it would not be the same number)
-                    if constexpr (WIDE) asm("" : "+v"(v));
+                    if constexpr (NS > 1) asm("" : "+v"(v));
                     pf[0][t][i / 2][4 * (i & 1) + r] = (_Float16)v;
-                    if constexpr (WIDE) pf[NS - 1][t][i / 2][4 * (i & 1) + r] = (_Float16)(v - (float)(_Float16)v);
+                    if constexpr (NS > 1) pf[NS - 1][t][i / 2][4 * (i & 1) + r] = (_Float16)(v - (float)(_Float16)v);
                 }
             }
     }
@@ -439,7 +441,7 @@ struct KaRows {
 #pragma unroll
         for (int t = 0; t < R; t++)
 #pragma unroll
-            for (int n = 0; n < NS; n++) st[t][i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf, q[n][t][w], st[t][i], 0, 0, 0);
+            for (int n = 0; n < NQ; n++) st[t][i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf, q[n][t][w], st[t][i], 0, 0, 0);
     }
 
     // O^T += V^T P^T for columns 16 d .. of a pair of tiles
@@ -494,9 +496,9 @@ struct KaTiles {
 };
 
 // waves per SIMD whose registers the rows leave room for
-constexpr int ka_few_waves(int nc, int r, bool wide)
+constexpr int ka_few_waves(int nc, int r, int dt)
 {
-    const int n = (wide ? 2 : 1) * r * nc;
+    const int n = (dt == ISEG_F32 ? 2 : 1) * r * nc;
     return n <= 1 ? 4 : n <= 4 && r < 4 ? 3 : n <= 8 && nc < 8 ? 2 : 1;
 }
 
@@ -516,8 +518,8 @@ constexpr int ka_few_waves(int nc, int r, bool wide)
 // one length.  float32 tensors: 133 us at 64 x 8192; heads of 256, 32 x 8192: 137.
 //
 // NC: words of a row's quarter (W / 32).  R: tiles of 16 rows.
-template <int NC, int R, bool WIDE>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(ka_few_waves(NC, R, WIDE)))) void k_kv4_few(KaArgs a)
+template <int NC, int R, int DT>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(ka_few_waves(NC, R, DT)))) void k_kv4_few(KaArgs a)
 {
     constexpr int W = NC * 32, TR = 16 * R;
     __shared__ float so[4 * 16 * (W + 4)];
@@ -532,7 +534,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(ka_few_wave
     if (bad) set_status(a.status, ISEG_DEV_RANGE);
     if (!have) return;
     const int64_t rows = s.n * a.G;
-    KaRows<NC, R, WIDE> x;
+    KaRows<NC, R, DT> x;
     x.load(a, s, 0, rows, h);
 
     // whole steps of 128 keys, dealt to the splits
@@ -660,7 +662,7 @@ struct KaStage {
     float ks[64], vs[64];
 };
 
-template <int NC, int R, bool WIDE>
+template <int NC, int R, int DT>
 __global__ __launch_bounds__(64 * kWaves) void k_kv4_many(KaArgs a)
 {
     constexpr int TR = 16 * R * kWaves, KT = 64;
@@ -732,7 +734,7 @@ __global__ __launch_bounds__(64 * kWaves) void k_kv4_many(KaArgs a)
         tl.ask(a, 0);
         fetch(0);                        // under way while the queries come
     }
-    KaRows<NC, R, WIDE> x;
+    KaRows<NC, R, DT> x;
     x.load(a, s, row0 + wave * 16 * R, rows, h);
     uint32_t ok_now = 0, ok_next = 0;    // tiles that are there, taken before the next look-up
     if (n_it > 0) {
@@ -883,10 +885,8 @@ struct KaPlan {
 };
 
 // what a wave's registers hold
-constexpr int ka_many(int nc, bool wide) { return wide || nc > 4 ? 1 : 2; }
-constexpr int ka_few_most(int nc, bool wide) { return wide ? (nc <= 4 ? 2 : 1) : (nc <= 4 ? 4 : 2); }
-
-bool ka_wide(const iseg_kv4_attention_geom* g) { return g->dtype == ISEG_F32; }
+constexpr int ka_many(int nc, int dt) { return dt == ISEG_F32 || nc > 4 ? 1 : 2; }
+constexpr int ka_few_most(int nc, int dt) { return dt == ISEG_F32 ? (nc <= 4 ? 2 : 1) : (nc <= 4 ? 4 : 2); }
 
 int64_t ka_max_kv(const iseg_kv4_attention_geom* g)
 {
@@ -916,7 +916,7 @@ KaPlan ka_plan(const iseg_kv4_attention_geom* g)
     KaPlan p = {};
     const int nc = kv4_width(g->D) / 32;
     const int64_t G = g->Hq / g->H, rows = ka_max_q(g) * G, pairs = g->B * g->H;
-    const int most = ka_few_most(nc, ka_wide(g));
+    const int most = ka_few_most(nc, g->dtype);
     int64_t span = ka_max_kv(g);
     if (g->window > 0 && g->window + ka_max_q(g) < span) span = g->window + ka_max_q(g);
     if (rows <= 16 * most || g->B > 1) {
@@ -926,7 +926,7 @@ KaPlan ka_plan(const iseg_kv4_attention_geom* g)
         // length (1 request of 131072 keys, 8 heads: 32 us at 96 splits, 36 at 128).  Many:
         // two rounds of blocks, which even out requests of different lengths (64 of
         // 820 to 8192 keys: 81 us against 86 in one).
-        const int64_t resident = 256 * ka_few_waves(nc, p.R, ka_wide(g));
+        const int64_t resident = 256 * ka_few_waves(nc, p.R, g->dtype);
         int64_t sp = 8 * pairs <= resident ? resident / pairs : ceil_div64(2 * resident, pairs), longest = ceil_div64(span, 256);
         sp = sp < longest ? sp : longest;
         p.splits = (int)(sp < 1 ? 1 : (sp > kSplitsMax ? kSplitsMax : sp));
@@ -936,7 +936,7 @@ KaPlan ka_plan(const iseg_kv4_attention_geom* g)
         // be full
         const int64_t large = g->T * G / (p.R ? 16 * p.R + 1 : 1), ends = large < g->B ? large : g->B;
         double best = 0.0;
-        for (int R = ka_many(nc, ka_wide(g)); R >= 1; R--) {
+        for (int R = ka_many(nc, g->dtype); R >= 1; R--) {
             const int64_t TR = 16 * kWaves * R, all = (g->T * G - ends) / TR + ends, each = ends * ceil_div64(rows, TR);
             const int64_t tiles = all < each ? all : each;
             for (int sp = 1; sp <= 32 && (sp == 1 || sp * 512 <= span); sp++) {
@@ -980,10 +980,10 @@ int ka_check(const iseg_kv4_attention_geom* g)
     return ISEG_OK;
 }
 
-template <int NC, int R, bool WIDE>
+template <int NC, int R, int DT>
 int ka_few(KaArgs& a, hipStream_t s)
 {
-    hipLaunchKernelGGL((k_kv4_few<NC, R, WIDE>), dim3((unsigned)((int64_t)a.B * a.H * a.splits)), dim3(256), 0, s, a);
+    hipLaunchKernelGGL((k_kv4_few<NC, R, DT>), dim3((unsigned)((int64_t)a.B * a.H * a.splits)), dim3(256), 0, s, a);
     const int64_t rows = a.max_q * a.G;
     a.join_rows = (int32_t)(rows < 16 * R ? rows : 16 * R);
     if (a.splits > 1)
@@ -991,53 +991,53 @@ int ka_few(KaArgs& a, hipStream_t s)
     return launch_ok();
 }
 
-template <int NC, int R, bool WIDE>
+template <int NC, int R, int DT>
 int ka_many_rows(const KaArgs& a, const KaPlan& p, hipStream_t s)
 {
     constexpr size_t lds = 2 * sizeof(KaStage<NC>);
     constexpr int TR = 16 * kWaves * R, rpb = 256 / (NC * 8);
-    if (!lds_limit((const void*)&k_kv4_many<NC, R, WIDE>, lds)) return ISEG_ERR_DEVICE;
-    hipLaunchKernelGGL((k_kv4_many<NC, R, WIDE>), dim3((unsigned)(p.tiles2 * a.H * a.splits)), dim3(64 * kWaves), lds, s, a);
+    if (!lds_limit((const void*)&k_kv4_many<NC, R, DT>, lds)) return ISEG_ERR_DEVICE;
+    hipLaunchKernelGGL((k_kv4_many<NC, R, DT>), dim3((unsigned)(p.tiles2 * a.H * a.splits)), dim3(64 * kWaves), lds, s, a);
     if (a.splits > 1)
         hipLaunchKernelGGL((k_kv4_join_many<TR>), dim3((unsigned)(p.tiles2 * a.H * ((TR + rpb - 1) / rpb))), dim3(256), 0, s, a);
     return launch_ok();
 }
 
-template <int NC, bool WIDE>
+template <int NC, int DT>
 int ka_run(KaArgs a, const KaPlan& p, hipStream_t s)
 {
-    constexpr int most = ka_few_most(NC, WIDE);
+    constexpr int most = ka_few_most(NC, DT);
     int rc = ISEG_OK;
     if (p.R) {
         a.rows_min = 0;
         a.rows_max = 16 * p.R;
         a.splits = p.splits;
-        if (p.R == 1) rc = ka_few<NC, 1, WIDE>(a, s);
+        if (p.R == 1) rc = ka_few<NC, 1, DT>(a, s);
         if constexpr (most >= 2)
-            if (p.R == 2) rc = ka_few<NC, 2, WIDE>(a, s);
+            if (p.R == 2) rc = ka_few<NC, 2, DT>(a, s);
         if constexpr (most >= 4)
-            if (p.R == 4) rc = ka_few<NC, 4, WIDE>(a, s);
+            if (p.R == 4) rc = ka_few<NC, 4, DT>(a, s);
     }
     if (rc == ISEG_OK && p.tiles2 > 0) {
         a.rows_min = p.R ? 16 * p.R : 0;
         a.rows_max = 0x7fffffff;
         a.splits = p.splits2;
-        constexpr int R = ka_many(NC, WIDE);
-        rc = R == 1 || p.R2 == 1 ? ka_many_rows<NC, 1, WIDE>(a, p, s) : ka_many_rows<NC, R, WIDE>(a, p, s);
+        constexpr int R = ka_many(NC, DT);
+        rc = R == 1 || p.R2 == 1 ? ka_many_rows<NC, 1, DT>(a, p, s) : ka_many_rows<NC, R, DT>(a, p, s);
     }
     return rc;
 }
 
-template <bool WIDE>
+template <int DT>
 int ka_widths(const KaArgs& a, const KaPlan& p, hipStream_t s)
 {
     switch (a.W / 32) {
-    case 1: return ka_run<1, WIDE>(a, p, s);
-    case 2: return ka_run<2, WIDE>(a, p, s);
-    case 3: return ka_run<3, WIDE>(a, p, s);
-    case 4: return ka_run<4, WIDE>(a, p, s);
-    case 6: return ka_run<6, WIDE>(a, p, s);
-    default: return ka_run<8, WIDE>(a, p, s);
+    case 1: return ka_run<1, DT>(a, p, s);
+    case 2: return ka_run<2, DT>(a, p, s);
+    case 3: return ka_run<3, DT>(a, p, s);
+    case 4: return ka_run<4, DT>(a, p, s);
+    case 6: return ka_run<6, DT>(a, p, s);
+    default: return ka_run<8, DT>(a, p, s);
     }
 }
 
@@ -1074,5 +1074,6 @@ extern "C" int iseg_kv4_attention(const void* q, const uint8_t* k_codes, const f
     a.D = (int32_t)g->D; a.W = kv4_width(g->D); a.p16 = g->page / 16;
     a.p16_inv = (((uint64_t)1 << 36) + a.p16 - 1) / a.p16;
     a.dtype = g->dtype; a.causal = g->causal; a.scale = g->scale * 1.44269504f; a.status = dev_status;
-    return ka_wide(g) ? ka_widths<true>(a, p, stream) : ka_widths<false>(a, p, stream);
+    return g->dtype == ISEG_F32 ? ka_widths<ISEG_F32>(a, p, stream)
+                                : g->dtype == ISEG_F16 ? ka_widths<ISEG_F16>(a, p, stream) : ka_widths<ISEG_BF16>(a, p, stream);
 }

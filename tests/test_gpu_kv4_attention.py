@@ -234,3 +234,21 @@ def test_pages_behind_the_window(n, kv, window, page, gone):
                                torch.tensor([kv], dtype=torch.int32, device=DEV), window=window, status=st) for t in (full, part))
     assert iseg.iseg_status_read(st) == 0
     assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+
+
+@pytest.mark.parametrize("n,kv,Hq,H,D", [(1, 300, 8, 2, 128), (1, 3000, 4, 1, 64), (9, 200, 8, 1, 96), (150, 420, 4, 2, 128), (300, 300, 2, 1, 256), (1, 2, 4, 4, 32)])
+@pytest.mark.parametrize("size", [0.3, 3.0])
+def test_float16_is_off_by_its_own_rounding(n, kv, Hq, H, D, size):
+    """float16 outputs: the weights' part of the bound is 2^-21 (two terms), not 2^-11."""
+    from paper_2011_14504_amd import iseg
+    held = -(-kv // 32)
+    cache = Cache(6, held, H, D, 32)
+    table = table_of(7, [held], held, held)
+    qg, qd = typed(size * rng(8).standard_normal((n, Hq, D)), "fp16")
+    scale = 1 / math.sqrt(D)
+    out, _ = iseg.kv4_attention(qg, cache.gpu(), torch.from_numpy(table).to(DEV), torch.tensor([0, n], dtype=torch.int32, device=DEV),
+                                torch.tensor([kv], dtype=torch.int32, device=DEV))
+    o, _, s, reach, far = attention(qd, cache, table, [0, n], [kv], H, scale, True, 0)
+    eps = 2 * (D + 16) * U * reach + 2.0 ** -25 * far + 4 * U
+    tol = (2 * eps[..., None] + 2.0 ** -21 + 40 * U) * s + (HALF["fp16"] + 4 * U) * np.abs(o) + kv * 7 * 2.0 ** -31 * float(cache.vs.max()) + 2.0 ** -24
+    within(out, torch.from_numpy(o), torch.from_numpy(tol), "out")
