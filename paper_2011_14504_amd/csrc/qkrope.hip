@@ -33,14 +33,16 @@ struct QrArgs {
 };
 
 // sine and cosine of pos * freq: the angle is formed in turns and reduced in 64
-// bits (at 2^31 radians the fraction of a turn is still good to 2^-24)
+// bits (at 2^31 radians the fraction of a turn is still good to 2^-24), and what its
+// float32 leaves off, up to 2^-25 half-turns, is turned by afterwards
 __device__ __forceinline__ float2 turn_of(int64_t pos, float freq, float mscale)
 {
     double t = (double)pos * (double)freq * 0.15915494309189533577;
-    t -= rint(t);
+    t = 2.0 * (t - rint(t));
+    const float hi = (float)t, lo = (float)(t - (double)hi) * 3.14159265f;
     float s, c;
-    sincospif((float)(2.0 * t), &s, &c);
-    return {c * mscale, s * mscale};
+    sincospif(hi, &s, &c);
+    return {fmaf(-s, lo, c) * mscale, fmaf(c, lo, s) * mscale};
 }
 
 template <typename T, int N>
@@ -306,30 +308,43 @@ __global__ __launch_bounds__(256) void k_qk_norm_rope(QrArgs a)
     }
 }
 
-// gamma's gradient: the blocks' partial sums, 64 runs of them side by side, each
-// in its order and then the runs in theirs (5.7 us; one thread a column 33).
+// gamma's gradient: the blocks' partial sums, 64 runs of them side by side, each by
+// halves and then the runs by eights in float64 (one after the other in float32 they
+// were the larger part of the gradient's error).  5.5 us; one thread a column 33.
 // blockIdx.y: q or k.
 template <typename P>
 __global__ __launch_bounds__(1024) void k_qk_dgamma(QrArgs a)
 {
-    __shared__ float red[64][16];
+    __shared__ double red[64][16];
     const QrSide& sd = a.side[blockIdx.y];
     if (!sd.dgamma) return;
     const int c = threadIdx.x & 15, seg = threadIdx.x >> 4, d = blockIdx.x * 16 + c;
     const int per = (sd.blocks + 63) / 64, b0 = seg * per;
-    float s = 0.f;
+    double s = 0.0;
     if (d < a.D) {
         float v[kBwdBlocks / 64];
 #pragma unroll
         for (int i = 0; i < kBwdBlocks / 64; i++) v[i] = i < per && b0 + i < sd.blocks ? sd.part[(int64_t)(b0 + i) * a.D + d] : 0.f;
 #pragma unroll
-        for (int i = 0; i < kBwdBlocks / 64; i++) s += v[i];
+        for (int n = kBwdBlocks / 128; n > 0; n /= 2)
+#pragma unroll
+            for (int i = 0; i < n; i++) v[i] += v[i + n];
+        s = v[0];
     }
     red[seg][c] = s;
     __syncthreads();
+    // eight runs by eight threads, then theirs
+    s = 0.0;
+    if (seg < 8)
+#pragma unroll
+        for (int i = 0; i < 8; i++) s += red[seg * 8 + i][c];
+    __syncthreads();
+    if (seg < 8) red[seg][c] = s;
+    __syncthreads();
     if (seg == 0 && d < a.D) {
-        for (int i = 1; i < 64; i++) s += red[i][c];
-        ((P*)sd.dgamma)[d] = (P)s;
+#pragma unroll
+        for (int i = 1; i < 8; i++) s += red[i][c];
+        ((P*)sd.dgamma)[d] = (P)(float)s;
     }
 }
 
