@@ -38,6 +38,7 @@ struct KaArgs {
     int32_t join_rows;                   // rows of a tile that may be there
     int32_t rows_min, rows_max;          // rows of the requests that this launch takes: (min, max]
     float scale;                         // times log2 e
+    double scale_left;                   // the same before it was rounded, over it
     int32_t* status;
 };
 
@@ -174,9 +175,12 @@ __device__ __forceinline__ void ka_store(const KaArgs& a, int64_t at, int d, f4_
 // 1 / l; 0 for a row without keys
 __device__ __forceinline__ float ka_inv(float l) { return l > 0.f ? 1.f / l : (l == l ? 0.f : l); }
 
-__device__ __forceinline__ float ka_lse(float m, float l)
+// log sum of a row, in float64 and with what the scale's rounding left off: it is the
+// whole score's
+__device__ __forceinline__ float ka_lse(const KaArgs& a, float m, float l)
 {
-    return l > 0.f || l != l ? (m + __builtin_amdgcn_logf(l)) * 0.69314718f : -__builtin_inff();
+    if (!(l > 0.f || l != l)) return -__builtin_inff();
+    return (float)(((double)m * a.scale_left + log2((double)l)) * 0.693147180559945309);
 }
 
 // Where row r of a tile goes: its place among the parts, or its output row.
@@ -199,7 +203,7 @@ __device__ __forceinline__ KaOut ka_row(const KaArgs& a, const KaSeq& s, int til
         const int64_t q = (row0 + r) / a.G, tok = s.q0 + q, head = h * a.G + (row0 + r - q * a.G);
         o.at = tok * a.o_ld + head * a.o_hs;
         o.inv = ka_inv(l);
-        if (one && a.lse) a.lse[tok * a.Hq + head] = ka_lse(m, l);
+        if (one && a.lse) a.lse[tok * a.Hq + head] = ka_lse(a, m, l);
     }
     return o;
 }
@@ -647,8 +651,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(ka_few_wave
 // overlap them.  3 x 3001 queries behind as many keys, 32 heads over 8 of 128: 870 to
 // 920 us for 663 GFLOP that are needed (720 to 760 TFLOP/s; the library's largest
 // products reach 1377).  Without products and softmax it takes 502 (loads, codes to
-// LDS, barriers), without its stages 78.  1 x 4096: 210 us; in float32 (two terms of q
-// and p, twice the products) 390; heads of 256 225.  R = 1 where a request has up to
+// LDS, barriers), without its stages 78.  1 x 4096: 204 to 214 us; in float16 (two
+// terms of p) 243, in float32 (of q as well) 390 to 400; heads of 256 225.  R = 1 where a request has up to
 // 128 rows or a prompt is short (ka_cost).
 // Tried and slower: sixteen waves of 16 rows (1158), twelve waves (spills), 32x32x16
 // products with V's scale per stage (897 to 945), stages of 128 keys (896).
@@ -825,7 +829,7 @@ __global__ __launch_bounds__(256) void k_kv4_join(KaArgs a)
             lsum = lr;
             if (a.lse) {
                 const int64_t tok = s.q0 + (row0 + r) / a.G, head = h * a.G + (row0 + r) % a.G;
-                a.lse[tok * a.Hq + head] = ka_lse(mr, lr);
+                a.lse[tok * a.Hq + head] = ka_lse(a, mr, lr);
             }
         }
     }
@@ -867,7 +871,7 @@ __global__ __launch_bounds__(256) void k_kv4_join_many(KaArgs a)
         o += f * *(const f4_t*)(a.po + (at + i) * a.W + d);
     }
     const int64_t q = (row0 + r) / a.G, tok = s.q0 + q, head = h * a.G + (row0 + r - q * a.G);
-    if (a.lse && d == 0) a.lse[tok * a.Hq + head] = ka_lse(mr, lr);
+    if (a.lse && d == 0) a.lse[tok * a.Hq + head] = ka_lse(a, mr, lr);
     if (d < a.D) ka_store(a, tok * a.o_ld + head * a.o_hs, d, o, ka_inv(lr));
 }
 
@@ -1073,7 +1077,10 @@ extern "C" int iseg_kv4_attention(const void* q, const uint8_t* k_codes, const f
     a.window = g->window; a.B = (int32_t)g->B; a.Hq = (int32_t)g->Hq; a.H = (int32_t)g->H; a.G = (int32_t)(g->Hq / g->H);
     a.D = (int32_t)g->D; a.W = kv4_width(g->D); a.p16 = g->page / 16;
     a.p16_inv = (((uint64_t)1 << 36) + a.p16 - 1) / a.p16;
-    a.dtype = g->dtype; a.causal = g->causal; a.scale = g->scale * 1.44269504f; a.status = dev_status;
+    a.dtype = g->dtype; a.causal = g->causal; a.status = dev_status;
+    const double scale = (double)g->scale * 1.442695040888963407;
+    a.scale = (float)scale;
+    a.scale_left = scale / (double)a.scale;
     return g->dtype == ISEG_F32 ? ka_widths<ISEG_F32>(a, p, stream)
                                 : g->dtype == ISEG_F16 ? ka_widths<ISEG_F16>(a, p, stream) : ka_widths<ISEG_BF16>(a, p, stream);
 }

@@ -252,3 +252,32 @@ def test_float16_is_off_by_its_own_rounding(n, kv, Hq, H, D, size):
     eps = 2 * (D + 16) * U * reach + 2.0 ** -25 * far + 4 * U
     tol = (2 * eps[..., None] + 2.0 ** -21 + 40 * U) * s + (HALF["fp16"] + 4 * U) * np.abs(o) + kv * 7 * 2.0 ** -31 * float(cache.vs.max()) + 2.0 ** -24
     within(out, torch.from_numpy(o), torch.from_numpy(tol), "out")
+
+
+@pytest.mark.parametrize("t", ["bf16", "fp16", "fp32"])
+@pytest.mark.parametrize("B,n,kv,Hq,H,D", [(1, 1500, 1500, 64, 8, 64), (8, 24, 3000, 64, 8, 64), (2, 700, 1900, 32, 8, 96), (1, 16, 9000, 64, 8, 32)])
+def test_enough_rows_for_the_whole_card(B, n, kv, Hq, H, D, t):
+    """Tiles of 256 rows, whole and in splits, and of 128 in splits; the formula by
+    matrices."""
+    from paper_2011_14504_amd import iseg
+    page, G = 64, Hq // H
+    held = -(-kv // page)
+    cache = Cache(11, B * held, H, D, page)
+    table = table_of(12, [held] * B, B * held, held)
+    qg, qd = typed(rng(13).standard_normal((B * n, Hq, D)), t)
+    start = np.arange(B + 1) * n
+    out, lse = iseg.kv4_attention(qg, cache.gpu(), torch.from_numpy(table).to(DEV), torch.from_numpy(start.astype(np.int32)).to(DEV),
+                                  torch.full((B,), kv, dtype=torch.int32, device=DEV), max_q=n, max_kv=kv)
+    scale, want = 1 / math.sqrt(D), [np.zeros((B * n, Hq, D)), np.zeros((B * n, Hq)), np.zeros((B * n, Hq, D)), np.zeros((B * n, Hq)), np.zeros((B * n, Hq))]
+    unseen = torch.arange(kv)[None] > torch.arange(kv - n, kv)[:, None]
+    for b in range(B):
+        rows = slice(b * n, (b + 1) * n)
+        for h in range(Hq):
+            K, V = (torch.from_numpy(x) for x in cache.rows(table[b], kv, h // G))
+            x = torch.from_numpy(qd[rows, h])
+            s = (scale * (x @ K.t())).masked_fill(unseen, -math.inf)
+            p = torch.softmax(s, -1)
+            want[0][rows, h], want[1][rows, h], want[2][rows, h] = p @ V, torch.logsumexp(s, -1), p @ V.abs()
+            want[3][rows, h] = scale * (x.abs() @ K.abs().t()).amax(-1)
+            want[4][rows, h] = scale * x.abs().amax(-1) * K.abs().sum(1).max()
+    _check(out, lse, want, t, D, kv, float(cache.vs.max()), str((B, n, kv)))
