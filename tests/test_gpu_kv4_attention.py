@@ -277,7 +277,7 @@ def test_enough_rows_for_the_whole_card(B, n, kv, Hq, H, D, t):
             x = torch.from_numpy(qd[rows, h])
             s = (scale * (x @ K.t())).masked_fill(unseen, -math.inf)
             p = torch.softmax(s, -1)
-            want[0][rows, h], want[1][rows, h], want[2][rows, h] = p @ V, torch.logsumexp(s, -1), p @ V.abs()
-            want[3][rows, h] = scale * (x.abs() @ K.abs().t()).amax(-1)
-            want[4][rows, h] = scale * x.abs().amax(-1) * K.abs().sum(1).max()
+            of = (p @ V, torch.logsumexp(s, -1), p @ V.abs(), scale * (x.abs() @ K.abs().t()).amax(-1), scale * x.abs().amax(-1) * K.abs().sum(1).max())
+            for w, y in zip(want, of):
+                w[rows, h] = y.numpy()
     _check(out, lse, want, t, D, kv, float(cache.vs.max()), str((B, n, kv)))
