@@ -251,12 +251,12 @@ __device__ __forceinline__ KaWords<NC> words(const uint8_t* p)
 }
 
 // What a wave keeps of its 16 R rows.  DT: the tensors' type.  A float16 of q or p is
-// one rounding of 2^-11: q of float32 and p of float32 and float16 tensors are two such
-// terms.  (With one term of p, float16 outputs were 1.5 times as far from 64 bits as
-// their own rounding puts them; bfloat16's is eight times as large.)
+// one rounding of 2^-11: p is two such terms, and q of float32 tensors.  (With one term
+// of p, float16 outputs were 1.5 times as far from 64 bits as their own rounding puts
+// them, and bfloat16 ones rounded to the other neighbour in one element of fifteen.)
 template <int NC, int R, int DT>
 struct KaRows {
-    static constexpr int NQ = DT == ISEG_F32 ? 2 : 1, NS = DT == ISEG_BF16 ? 1 : 2;
+    static constexpr int NQ = DT == ISEG_F32 ? 2 : 1, NS = 2;
     h8_t q[NQ][R][NC];                   // queries as B operands
     float cf[R];                         // score per unit of S^T and scale of k
     int32_t lo[R], hi[R];                // keys that a lane's rows see
@@ -432,9 +432,9 @@ struct KaRows {
                     float v = p[order[r]];
                     // the product is rounded once for both terms (contracted with one of
                     // them it would not be the same number)
-                    if constexpr (NS > 1) asm("" : "+v"(v));
+                    asm("" : "+v"(v));
                     pf[0][t][i / 2][4 * (i & 1) + r] = (_Float16)v;
-                    if constexpr (NS > 1) pf[NS - 1][t][i / 2][4 * (i & 1) + r] = (_Float16)(v - (float)(_Float16)v);
+                    pf[1][t][i / 2][4 * (i & 1) + r] = (_Float16)(v - (float)(_Float16)v);
                 }
             }
     }
