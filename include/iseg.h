@@ -882,7 +882,7 @@ int iseg_kv4_read(const uint8_t* k_codes, const float* k_scale, const uint8_t* v
  * sums are float32, formed of the integer codes and q in float16, exact to 2^-25
  * of its row's largest element (float32 tensors: two terms).  A softmax weight
  * times its key's scale of v is off by at most 2^-21 of itself (two float16 terms)
- * and at least 2^-31 of the request's largest scale of v.
+ * or 2^-34 of the largest such product of its row (scales of v from 2^-80 on).
  * max_q, max_kv: what the caller knows of the longest request's new tokens and
  * of the longest kv_len (0: T and max_pages page).  A request beyond either, a
  * q_start that falls or leaves [0, T], a negative kv_len or a page id outside

@@ -5,11 +5,12 @@
 // over 32 keys at a time:
 //   S^T = K Q^T   on 16x16x32 float16 MFMAs, the codes as A: their scales are a
 //                 factor per row of S^T;
-//   p = 2^(s - m) with the running maximum m of a row (moved only when a score
-//                 passes it by 8: float16 has the room), l += p;
+//   p = 2^(s - m) with m 8 above the running maximum of a row, moved only when a
+//                 score passes it; l += p;
 //   O^T += V^T P^T, P in the registers that S^T left it in.  V's scale goes into
-//                 p, in float16 relative to the largest scale seen (a power of
-//                 two, also moved only when it must be).
+//                 p, and a power of two of the row's own (`up`) brings the largest
+//                 product that the row has seen into float16's range, moved only
+//                 when it must be.
 // Codes become float16 by placing them in the mantissa of 1024 (9 instructions
 // for 8 codes); the layout of the cache makes a lane's operands whole words.
 #include "kv4.h"
@@ -20,8 +21,10 @@ typedef _Float16 h2_t __attribute__((ext_vector_type(2)));
 typedef _Float16 h8_t __attribute__((ext_vector_type(8)));
 typedef float f4_t __attribute__((ext_vector_type(4)));
 
-constexpr float kNone = -3.0e38f;        // maximum of a row that has seen no key
-constexpr float kRoom = 8.f;             // scores may pass the running maximum by 2^8
+constexpr float kNone = -3.0e38f;        // m of a row that has seen no key
+constexpr float kRoom = 8.f;             // m is above the running maximum by
+constexpr float kTop = 32768.f;          // weights times scale times up are at most this, float16's largest is 65504
+constexpr int kUpLog = 10, kUpMost = 100;    // up brings a new largest below 2^10, and is 2^100 at most
 constexpr int kSplitsMax = 128;
 
 struct KaArgs {
@@ -264,7 +267,7 @@ struct KaRows {
     int32_t any_lo, any_hi;              // keys that some row sees
     f4_t acc[R][2 * NC];
     float m[R], l[R];
-    float v_inv, v_top;                  // V's scales times v_inv are below 2^7; up to v_top nothing moves
+    float up[R];                         // acc is sums of codes times weight times V's scale times up
 
     __device__ __forceinline__ void load(const KaArgs& a, const KaSeq& s, int64_t row0, int64_t rows, int h)
     {
@@ -312,11 +315,10 @@ struct KaRows {
             }
             m[t] = kNone;
             l[t] = 0.f;
+            up[t] = ldexpf(1.f, kUpMost);
 #pragma unroll
             for (int i = 0; i < 2 * NC; i++) acc[t][i] = f4_t{0.f, 0.f, 0.f, 0.f};
         }
-        v_inv = 1.f;
-        v_top = 0.f;
         full_lo = full_hi = any_lo = any_hi = 0;
         if (row0 < rows) {
             const int64_t last = (row0 + 16 * R < rows ? row0 + 16 * R : rows) - 1;
@@ -356,27 +358,6 @@ struct KaRows {
                     if (!(ok[i] && kb + 16 * i + 4 * g4 + r < kv)) vs[i][r] = 0.f;
                 }
         }
-        float top = 0.f;
-#pragma unroll
-        for (int i = 0; i < NT; i++)
-#pragma unroll
-            for (int r = 0; r < 4; r++) top = fmaxf(top, vs[i][r]);
-        if (__any(top > v_top)) {
-            top = fmaxf(v_top, fminf(max4(top), 3.4028234e38f));
-            int e;
-            (void)frexpf(top, &e);                               // top in [2^(e-1), 2^e)
-            e = e < -100 ? -100 : e;
-            const float inv = ldexpf(1.f, 7 - e), f = inv / v_inv;
-            v_top = ldexpf(1.f, e);
-            v_inv = inv;
-#pragma unroll
-            for (int t = 0; t < R; t++)
-#pragma unroll
-                for (int i = 0; i < 2 * NC; i++) acc[t][i] *= f;
-        }
-#pragma unroll
-        for (int i = 0; i < NT; i++) vs[i] *= v_inv;
-
 #pragma unroll
         for (int t = 0; t < R; t++)
 #pragma unroll
@@ -402,34 +383,61 @@ struct KaRows {
             for (int i = 0; i < NT; i++)
 #pragma unroll
                 for (int r = 0; r < 4; r++) mx[t] = fmaxf(mx[t], st[t][i][r]);
-            move = move || mx[t] * cf[t] > m[t] + kRoom;
+            move = move || mx[t] * cf[t] > m[t];
         }
         if (__any(move)) {
 #pragma unroll
             for (int t = 0; t < R; t++) {
-                const float mn = fmaxf(m[t], max4(mx[t]) * cf[t]);
-                const float al = __builtin_amdgcn_exp2f(m[t] - mn);
+                // weights that were 2^d as large: up makes good for it as far as it may,
+                // so that they keep their bits if what passed them has a small value
+                const float mn = fmaxf(m[t], fmaf(max4(mx[t]), cf[t], kRoom)), d = mn - m[t];
+                int e;
+                (void)frexpf(up[t], &e);                         // up = 2^(e - 1)
+                const float g = ceilf(fminf(d, (float)(kUpMost + 1 - e))), al = __builtin_amdgcn_exp2f(g - d);
                 m[t] = mn;
-                l[t] *= al;
+                l[t] *= __builtin_amdgcn_exp2f(-d);
+                up[t] = ldexpf(up[t], (int)g);
 #pragma unroll
                 for (int i = 0; i < 2 * NC; i++) acc[t][i] *= al;
+            }
+        }
+        float top[R];
+        bool high = false;
+#pragma unroll
+        for (int t = 0; t < R; t++) {
+            top[t] = 0.f;
+#pragma unroll
+            for (int i = 0; i < NT; i++)
+#pragma unroll
+                for (int r = 0; r < 4; r++) {
+                    const float v = __builtin_amdgcn_exp2f(fmaf(st[t][i][r], cf[t], -m[t]));
+                    l[t] += v;
+                    st[t][i][r] = v * vs[i][r];
+                    top[t] = fmaxf(top[t], st[t][i][r]);
+                }
+            high = high || top[t] * up[t] > kTop;
+        }
+        if (__any(high)) {
+#pragma unroll
+            for (int t = 0; t < R; t++) {
+                const float big = fminf(max4(top[t]), 3.4028234e38f);
+                if (!(big * up[t] > kTop)) continue;
+                int e;
+                (void)frexpf(big, &e);                           // big in [2^(e-1), 2^e)
+                const float n = ldexpf(1.f, kUpLog - e), f = n / up[t];
+                up[t] = n;
+#pragma unroll
+                for (int i = 0; i < 2 * NC; i++) acc[t][i] *= f;
             }
         }
 #pragma unroll
         for (int t = 0; t < R; t++)
 #pragma unroll
             for (int i = 0; i < NT; i++) {
-                float p[4];
-#pragma unroll
-                for (int r = 0; r < 4; r++) {
-                    const float v = __builtin_amdgcn_exp2f(fmaf(st[t][i][r], cf[t], -m[t]));
-                    l[t] += v;
-                    p[r] = v * vs[i][r];
-                }
                 constexpr int order[4] = {0, 2, 1, 3};
 #pragma unroll
                 for (int r = 0; r < 4; r++) {
-                    float v = p[order[r]];
+                    float v = st[t][i][order[r]] * up[t];
                     // the product is rounded once for both terms (contracted with one of
                     // them it would not be the same number)
                     asm("" : "+v"(v));
@@ -608,7 +616,6 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(ka_few_wave
     }
 
     // the waves' rows joined, a tile of 16 at a time: the whole, or this split's part
-    const float v_out = 1.f / x.v_inv;
 #pragma unroll
     for (int t = 0; t < R; t++) x.l[t] = sum4(x.l[t]);
     for (int t = 0; t < R; t++) {
@@ -619,7 +626,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(ka_few_wave
         for (int u = 0; u < R; u++)
             if (u == t) {
 #pragma unroll
-                for (int i = 0; i < 2 * NC; i++) *(f4_t*)(mine + i * 16) = x.acc[u][i] * v_out;
+                for (int i = 0; i < 2 * NC; i++) *(f4_t*)(mine + i * 16) = x.acc[u][i] * (1.f / x.up[u]);
                 if (g4 == 0) { sm[wave][c] = x.m[u]; sl[wave][c] = x.l[u]; }
             }
         __syncthreads();
@@ -776,7 +783,6 @@ __global__ __launch_bounds__(64 * kWaves) void k_kv4_many(KaArgs a)
 #pragma unroll
             for (int d = 0; d < 2 * NC; d++) x.add(y.v[p][d][lane], d, p, pf);
     }
-    const float v_out = 1.f / x.v_inv;
 #pragma unroll
     for (int t = 0; t < R; t++) {
         const float l = sum4(x.l[t]);
@@ -784,7 +790,7 @@ __global__ __launch_bounds__(64 * kWaves) void k_kv4_many(KaArgs a)
         if (row0 + r >= rows) continue;
         const KaOut o = ka_row<TR>(a, s, tile, h, split, row0, r, x.m[t], l, g4 == 0);
 #pragma unroll
-        for (int i = 0; i < 2 * NC; i++) ka_put(a, o, i * 16 + g4 * 4, x.acc[t][i] * v_out);
+        for (int i = 0; i < 2 * NC; i++) ka_put(a, o, i * 16 + g4 * 4, x.acc[t][i] * (1.f / x.up[t]));
     }
 }
 
