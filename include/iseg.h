@@ -879,8 +879,9 @@ int iseg_kv4_read(const uint8_t* k_codes, const float* k_scale, const uint8_t* v
  *   lse = log sum_j e^{s_j}   (float32 [T, Hq] dense, may be NULL).
  * A row that sees no key has out 0 and lse -infinity.  Rows before q_start[0]
  * and from q_start[B] on are left as they were.  q and out of dtype; scores and
- * sums are float32, formed of the integer codes and q in float16, exact to 2^-25
- * of its row's largest element (float32 tensors: two terms).  A softmax weight
+ * sums are float32, formed of the integer codes and q in float16 with a power of two
+ * for each row: an element of q is exact, or off by 2^-39 of its row's largest, those
+ * of float32 tensors (two terms) also by 2^-23 of themselves.  A softmax weight
  * times its key's scale of v is off by at most 2^-21 of itself (two float16 terms)
  * or 2^-34 of the largest such product of its row (scales of v from 2^-80 on).
  * max_q, max_kv: what the caller knows of the longest request's new tokens and

@@ -25,6 +25,7 @@ constexpr float kNone = -3.0e38f;        // m of a row that has seen no key
 constexpr float kRoom = 8.f;             // m is above the running maximum by
 constexpr float kTop = 32768.f;          // weights times scale times up are at most this, float16's largest is 65504
 constexpr int kUpLog = 10, kUpMost = 100;    // up brings a new largest below 2^10, and is 2^100 at most
+constexpr int kQLog = 15;                // queries that are not float16 are brought below 2^15
 constexpr int kSplitsMax = 128;
 
 struct KaArgs {
@@ -260,6 +261,7 @@ __device__ __forceinline__ KaWords<NC> words(const uint8_t* p)
 template <int NC, int R, int DT>
 struct KaRows {
     static constexpr int NQ = DT == ISEG_F32 ? 2 : 1, NS = 2;
+    static constexpr float k_down = DT == ISEG_F16 ? 1.f : 1.f / (1 << kQLog);      // of k's scales, for the queries' 2^15
     h8_t q[NQ][R][NC];                   // queries as B operands
     float cf[R];                         // score per unit of S^T and scale of k
     int32_t lo[R], hi[R];                // keys that a lane's rows see
@@ -285,8 +287,9 @@ struct KaRows {
                 const int d = g4 * 8 * NC + w * 8;
                 ka_get8<DT>(a, at, d, in && d < a.D, f);
             };
-            // float16 reaches no further than 65504 and 2^-24: rows of the other
-            // types are brought below 1 by a power of two first
+            // float16 reaches no further than 65504 and 2^-24: rows of the other types
+            // are brought below 2^15 by a power of two first, so that elements down to
+            // 2^-31 of the largest keep bfloat16's bits (below 1, down to 2^-16)
             int e = 0;
             if (DT != ISEG_F16) {
                 float big = 0.f;
@@ -308,7 +311,7 @@ struct KaRows {
                 get(w, f);
 #pragma unroll
                 for (int i = 0; i < 8; i++) {
-                    const float x = ldexpf(f[i], -e);
+                    const float x = DT == ISEG_F16 ? f[i] : ldexpf(f[i], kQLog - e);
                     q[0][t][w][i] = (_Float16)x;
                     if constexpr (NQ > 1) q[NQ - 1][t][w][i] = (_Float16)(x - (float)(_Float16)x);
                 }
@@ -602,7 +605,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(ka_few_wave
                 x.score(join8(codes_lo(u), codes_hi(u), codes_lo(v), codes_hi(v)), w, i, st);
             }
         }
-        f4_t ks[2] = {ks_next[0], ks_next[1]}, vs[2] = {vs_next[0], vs_next[1]};
+        f4_t ks[2] = {ks_next[0] * x.k_down, ks_next[1] * x.k_down}, vs[2] = {vs_next[0], vs_next[1]};
         if (more) fetch_k(it + 1);
         h8_t pf[x.NS][R][1];
         x.soften(st, ks, vs, ok, kb, kv, pf);
@@ -731,7 +734,7 @@ __global__ __launch_bounds__(64 * kWaves) void k_kv4_many(KaArgs a)
                 const uint32_t u = wa.w[w], v = u >> 8;
                 d.k[own][w][lane] = join8(codes_lo(u), codes_hi(u), codes_lo(v), codes_hi(v));
             }
-            if (lane < 16) d.ks[own * 16 + lane] = sc;
+            if (lane < 16) d.ks[own * 16 + lane] = sc * KaRows<NC, R, DT>::k_down;
         } else {
 #pragma unroll
             for (int w = 0; w < NC; w++) {
