@@ -885,9 +885,11 @@ int iseg_kv4_read(const uint8_t* k_codes, const float* k_scale, const uint8_t* v
  * times its key's scale of v is off by at most 2^-21 of itself (two float16 terms)
  * or 2^-34 of the largest such product of its row (scales of v from 2^-80 on).
  * max_q, max_kv: what the caller knows of the longest request's new tokens and
- * of the longest kv_len (0: T and max_pages page).  A request beyond either, a
- * q_start that falls or leaves [0, T], a negative kv_len or a page id outside
- * [0, n_pages) (its keys count as unseen) sets ISEG_DEV_RANGE.  Table entries whose
+ * of the longest kv_len (0: T and max_pages page).  A request beyond max_q or whose
+ * q_start falls or leaves [0, T] is left out (its rows stay as they were; where
+ * q_start falls, those of requests that overlap may too), one beyond max_kv has
+ * max_kv keys, a negative kv_len counts as 0, and the keys of a page id outside
+ * [0, n_pages) count as unseen; each sets ISEG_DEV_RANGE.  Table entries whose
  * tokens no query of the request sees, as those behind a window, may hold
  * anything.
  * D a multiple of 8, at most 256; Hq a multiple of H; scale > 0, finite.

@@ -98,7 +98,7 @@ __device__ __forceinline__ KaSeq ka_seq(const KaArgs& a, int64_t b, int& bad)
     s.n = (int64_t)a.q_start[b + 1] - s.q0;
     s.kv = a.kv_len[b];
     if (s.q0 < 0 || s.n < 0 || s.q0 + s.n > a.T) { bad = 1; s.n = 0; }
-    if (s.n > a.max_q) bad = 1;
+    if (s.n > a.max_q) { bad = 1; s.n = 0; }                     // its tiles are not among the launch's
     if (s.kv < 0) { bad = 1; s.kv = 0; }
     if (s.kv > a.max_kv) { bad = 1; s.kv = a.max_kv; }
     return s;
