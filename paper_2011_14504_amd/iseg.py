@@ -1379,6 +1379,8 @@ def _on_device(f):
     @functools.wraps(f)
     def call(*args, **kw):
         x = args[0] if args else kw.get(first)
+        if x is None:                    # queries or keys alone: another argument's
+            x = next((t for t in (*args, *kw.values()) if isinstance(t, torch.Tensor) and t.get_device() >= 0), None)
         i = x.get_device() if isinstance(x, torch.Tensor) else -1      # f itself refuses what is no tensor
         if i < 0 or i == _raw_device():
             return f(*args, **kw)
