@@ -928,8 +928,9 @@ int iseg_kv4_attention(const void* q, const uint8_t* k_codes, const float* k_sca
  * token_dtype, u and u_sample [B] float32 in [0, 1).
  * ISEG_DEV_RANGE: n_draft outside [0, S] (clamped), a drafted token outside
  * [0, V) (refused; the remainder is max(p_i - q_i, 0) still), a row without any
- * mass (its token is -1).  ISEG_DEV_NONFINITE: a used row with a NaN, an infinity
- * or a negative value (the token is unspecified within [-1, V)).
+ * mass (its token is -1).  ISEG_DEV_NONFINITE: an accepted draft with a probability
+ * that is infinite or negative, or a row that a token is taken from with such a value
+ * or a NaN (the token is unspecified within [-1, V)).
  * V in [1, 2^31); ISEG_ERR_UNSUPPORTED: B > 2^16, S > 2^20. */
 typedef struct iseg_verify_geom {
     int64_t B, S, V;

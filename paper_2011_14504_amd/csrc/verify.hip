@@ -34,7 +34,10 @@ __device__ __forceinline__ int64_t vf_token(const VfArgs& a, int64_t b, int64_t 
     return a.tok64 ? ((const int64_t*)a.tokens)[at] : (int64_t)((const int32_t*)a.tokens)[at];
 }
 
-// drafts of request b that stand, decided by a wave; `refused`: one did not
+__device__ __forceinline__ bool odd_value(float v) { return !(v >= 0.f && v <= 3.4028234e38f); }
+
+// drafts of request b that stand, decided by a wave; `refused`: one did not.  Their
+// probabilities are looked at here, the refused one's with its row.
 template <typename T>
 __device__ __forceinline__ int64_t vf_accepted(const VfArgs& a, int64_t b, bool& refused, int& bad)
 {
@@ -44,17 +47,19 @@ __device__ __forceinline__ int64_t vf_accepted(const VfArgs& a, int64_t b, bool&
     refused = false;
     for (int64_t i0 = 0; i0 < n; i0 += 64) {
         const int64_t i = i0 + lane;
-        bool no = false;
+        bool no = false, odd = false;
         if (i < n) {
             const int64_t x = vf_token(a, b, i);
             no = true;
             if (x >= 0 && x < a.V) {
-                const double p = (double)(float)((const T*)a.target)[b * a.t_bs + i * a.t_ld + x];
-                const double q = a.draft ? (double)(float)((const T*)a.draft)[b * a.d_bs + i * a.d_ld + x] : 1.0;
-                no = !((double)a.u[b * a.S + i] * q < p);
+                const float p = (float)((const T*)a.target)[b * a.t_bs + i * a.t_ld + x];
+                const float q = a.draft ? (float)((const T*)a.draft)[b * a.d_bs + i * a.d_ld + x] : 1.f;
+                no = !((double)a.u[b * a.S + i] * (double)q < (double)p);
+                odd = odd_value(p) || odd_value(q);
             }
         }
         const uint64_t m = __ballot(no);
+        if (__ballot(odd) & ((m & -m) - 1)) bad |= ISEG_DEV_NONFINITE;     // below the first refused, or all
         if (m) {
             const int64_t i = i0 + __builtin_ctzll(m), x = vf_token(a, b, i);
             if (x < 0 || x >= a.V) bad |= ISEG_DEV_RANGE;
@@ -88,8 +93,6 @@ __device__ __forceinline__ double left_of(float p, float q)
     const double d = (double)p - (double)q;
     return d > 0.0 ? d : 0.0;
 }
-
-__device__ __forceinline__ bool odd_value(float v) { return !(v >= 0.f && v <= 3.4028234e38f); }
 
 // a double moved by DPP, 0 where the pattern reads past its row
 template <int CTRL, int ROWS>
