@@ -12,5 +12,5 @@ static inline int kv4_width(int64_t D) { return (int)(D <= 128 ? ceil_div64(D, 3
 // whether a cache's pages can be addressed by slots of 32 bits
 static inline bool kv4_pages_ok(int64_t n_pages, int64_t page)
 {
-    return n_pages >= 0 && page >= 1 && n_pages < ((int64_t)1 << 31) / page + (((int64_t)1 << 31) % page != 0);
+    return n_pages >= 0 && page >= 1 && n_pages <= ((int64_t)1 << 31) / page;
 }
