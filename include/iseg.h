@@ -842,7 +842,8 @@ int iseg_qk_norm_rope_bwd(const void* dyq, const void* dyk, const void* q, const
  *     columns 32 i + c (low four bits) and 32 i + 16 + c (high), c < 16, in byte
  *     ((4 c + g) (W / 32) + i) 4 + j.
  *   k_scale, v_scale [n_pages, H, page].
- * A wave's matrix operands are whole 16-byte pieces of either. */
+ * A wave's matrix operands are whole 16-byte pieces of either: k and v have to lie at
+ * multiples of 16 bytes, for attention k_scale and v_scale too (ISEG_ERR_ARG). */
 
 /* iseg_kv4_write -- tokens' keys and values k, v [T, H, D] into their slots:
  * scale = max|x| / 7 (ISEG_SCALE_MAX) or the power-of-two step of
@@ -856,7 +857,7 @@ int iseg_qk_norm_rope_bwd(const void* dyq, const void* dyk, const void* q, const
  * iseg_kv4_read -- the values at slots, code * scale rounded to dtype; zeros for
  * a negative slot, and for one outside the cache, which sets ISEG_DEV_RANGE.
  * ISEG_ERR_UNSUPPORTED: D > 256, page > 8192, n_pages page > 2^31, H > 65536,
- * T H >= 2^27. */
+ * ceil(T / 16) H >= 2^25 - 1 (T H of about 2^29). */
 typedef struct iseg_kv4_geom {
     int64_t T, H, D;
     int64_t k_ld, k_hs, v_ld, v_hs;
