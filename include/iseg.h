@@ -854,8 +854,9 @@ int iseg_qk_norm_rope_bwd(const void* dyq, const void* dyk, const void* q, const
  * two writers' bytes stay is unspecified).  A row with a non-finite value gets
  * codes 0 and a NaN scale and sets ISEG_DEV_NONFINITE.
  *
- * iseg_kv4_read -- the values at slots, code * scale rounded to dtype; zeros for
- * a negative slot, and for one outside the cache, which sets ISEG_DEV_RANGE.
+ * iseg_kv4_read -- the values at slots, code * scale in float32, then rounded to
+ * dtype; zeros for a negative slot, and for one outside the cache, which sets
+ * ISEG_DEV_RANGE.
  * ISEG_ERR_UNSUPPORTED: D > 256, page > 8192, n_pages page > 2^31, H > 65536,
  * ceil(T / 16) H >= 2^25 - 1 (T H of about 2^29). */
 typedef struct iseg_kv4_geom {

@@ -365,7 +365,11 @@ __global__ __launch_bounds__(256) void k_kv4_read(KvArgs a)
         if (q >= nt) break;
         struct { T v[8]; } o;
 #pragma unroll
-        for (int e = 0; e < 8; e++) o.v[e] = (T)((float)n[q][e] * s[q]);
+        for (int e = 0; e < 8; e++) {
+            float f = (float)n[q][e] * s[q];
+            asm("" : "+v"(f));                                 // float32 first, whatever type follows: not one step to float16
+            o.v[e] = (T)f;
+        }
         T* to = out + (t0 + q) * ld;
         if (d + 8 <= a.D) {
             __builtin_memcpy(to + d, &o, sizeof(o));
