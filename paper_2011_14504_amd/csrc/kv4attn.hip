@@ -5,8 +5,8 @@
 // over 32 keys at a time:
 //   S^T = K Q^T   on 16x16x32 float16 MFMAs, the codes as A: their scales are a
 //                 factor per row of S^T;
-//   p = 2^(s - m) with m 8 above the running maximum of a row, moved only when a
-//                 score passes it; l += p;
+//   p = 2^(s - m) with m a whole number 8 to 9 above the running maximum of a row,
+//                 moved only when a score passes it; l += p;
 //   O^T += V^T P^T, P in the registers that S^T left it in.  V's scale goes into
 //                 p, and a power of two of the row's own (`up`) brings the largest
 //                 product that the row has seen into float16's range, moved only
@@ -22,7 +22,7 @@ typedef _Float16 h8_t __attribute__((ext_vector_type(8)));
 typedef float f4_t __attribute__((ext_vector_type(4)));
 
 constexpr float kNone = -3.0e38f;        // m of a row that has seen no key
-constexpr float kRoom = 8.f;             // m is above the running maximum by
+constexpr float kRoom = 8.f;             // m is whole and above the running maximum by this to one more
 constexpr float kTop = 32768.f;          // weights times scale times up are at most this, float16's largest is 65504
 constexpr int kUpLog = 10, kUpMost = 100;    // up brings a new largest below 2^10, and is 2^100 at most
 constexpr int kQLog = 15;                // queries that are not float16 are brought below 2^15
@@ -391,17 +391,20 @@ struct KaRows {
         if (__any(move)) {
 #pragma unroll
             for (int t = 0; t < R; t++) {
-                // weights that were 2^d as large: up makes good for it as far as it may,
-                // so that they keep their bits if what passed them has a small value
-                const float mn = fmaxf(m[t], fmaf(max4(mx[t]), cf[t], kRoom)), d = mn - m[t];
+                // what came before gets smaller by 2^d, d whole: up makes good for it as
+                // far as it may, so that acc stays as it is and keeps its bits if what
+                // passed it has a small value
+                const float mn = fmaxf(m[t], ceilf(fmaf(max4(mx[t]), cf[t], kRoom))), d = mn - m[t];
                 int e;
                 (void)frexpf(up[t], &e);                         // up = 2^(e - 1)
-                const float g = ceilf(fminf(d, (float)(kUpMost + 1 - e))), al = __builtin_amdgcn_exp2f(g - d);
+                const float g = fminf(d, (float)(kUpMost + 1 - e)), al = __builtin_amdgcn_exp2f(g - d);
                 m[t] = mn;
                 l[t] *= __builtin_amdgcn_exp2f(-d);
                 up[t] = ldexpf(up[t], (int)g);
+                if (__any(al != 1.f)) {
 #pragma unroll
-                for (int i = 0; i < 2 * NC; i++) acc[t][i] *= al;
+                    for (int i = 0; i < 2 * NC; i++) acc[t][i] *= al;
+                }
             }
         }
         float top[R];
