@@ -804,8 +804,10 @@ int iseg_page_map(const int32_t* ctx, const int32_t* count, const int32_t* held,
  * inv_freq float32; the angle is formed and reduced in 64 bits.  gamma_q,
  * gamma_k [D] of p_dtype, each NULL: 1.  eps >= 0, finite.  yq, yk have dtype
  * and may be q and k themselves (same strides).  Hq or Hk may be 0, their
- * pointers NULL.  A row with norm whose sum of squares is not finite sets
- * ISEG_DEV_NONFINITE (its y unspecified).
+ * pointers NULL.  A row with norm whose sum of squares
+ * leaves float32's range, or whose sum x^2 / D + eps is below 2^-126 (as a row of
+ * zeros with eps = 0), sets ISEG_DEV_NONFINITE (its y unspecified, and its dx and
+ * what it adds to dgamma in the backward, which has no status).
  *
  * iseg_qk_norm_rope_bwd -- with g the rotation of dy back (times mscale),
  * r = 1 / sqrt(sum x^2 / D + eps) and xhat = x r:

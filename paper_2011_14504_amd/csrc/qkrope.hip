@@ -222,8 +222,9 @@ __global__ __launch_bounds__(256) void k_qk_norm_rope(QrArgs a)
 #pragma unroll
                         for (int i = 0; i < N; i++) ss += xa[j][i] * xa[j][i] + xb[j][i] * xb[j][i];
                     ss = row_sum<LPR>(ss);
-                    if (!(ss <= 3.4028234e38f) && lane == 0) set_status(a.status, ISEG_DEV_NONFINITE);
-                    const float rs = 1.f / sqrtf(ss / (float)a.D + a.eps);
+                    const float mean = ss / (float)a.D + a.eps;
+                    if (!(mean >= 1.17549435e-38f && ss <= 3.4028234e38f) && lane == 0) set_status(a.status, ISEG_DEV_NONFINITE);
+                    const float rs = 1.f / sqrtf(mean);
 #pragma unroll
                     for (int j = 0; j < SPL; j++)
 #pragma unroll
