@@ -19,6 +19,7 @@ namespace {
 
 typedef _Float16 h2_t __attribute__((ext_vector_type(2)));
 typedef _Float16 h8_t __attribute__((ext_vector_type(8)));
+typedef float f2_t __attribute__((ext_vector_type(2)));
 typedef float f4_t __attribute__((ext_vector_type(4)));
 
 constexpr float kNone = -3.0e38f;        // m of a row that has seen no key
@@ -66,6 +67,16 @@ __device__ __forceinline__ h2_t codes_hi(uint32_t w)
 {
     const h2_t s = {(_Float16)0.0625f, (_Float16)0.0625f}, k = {(_Float16)-72.f, (_Float16)-72.f};
     return __builtin_elementwise_fma(in_1024(w, 0x00f000f0u), s, k);
+}
+
+// what a float16 leaves of the float32 it was rounded from: v - h[HALF], in one step
+template <int HALF>
+__device__ __forceinline__ float rest_of(float v, h2_t h)
+{
+    float r;
+    if constexpr (HALF == 0) asm("v_fma_mix_f32 %0, %1, -1.0, %2 op_sel_hi:[1,0,0]" : "=v"(r) : "v"(h), "v"(v));
+    else asm("v_fma_mix_f32 %0, %1, -1.0, %2 op_sel:[1,0,0] op_sel_hi:[1,0,0]" : "=v"(r) : "v"(h), "v"(v));
+    return r;
 }
 
 __device__ __forceinline__ h8_t join8(h2_t a, h2_t b, h2_t c, h2_t d)
@@ -440,15 +451,19 @@ struct KaRows {
         for (int t = 0; t < R; t++)
 #pragma unroll
             for (int i = 0; i < NT; i++) {
-                constexpr int order[4] = {0, 2, 1, 3};
 #pragma unroll
-                for (int r = 0; r < 4; r++) {
-                    float v = st[t][i][order[r]] * up[t];
+                for (int r = 0; r < 2; r++) {
+                    f2_t v = {st[t][i][r] * up[t], st[t][i][r + 2] * up[t]};
                     // the product is rounded once for both terms (contracted with one of
                     // them it would not be the same number)
-                    asm("" : "+v"(v));
-                    pf[0][t][i / 2][4 * (i & 1) + r] = (_Float16)v;
-                    pf[1][t][i / 2][4 * (i & 1) + r] = (_Float16)(v - (float)(_Float16)v);
+                    asm("" : "+v"(v.x), "+v"(v.y));
+                    const h2_t a = __builtin_convertvector(v, h2_t);
+                    const h2_t b = __builtin_convertvector((f2_t{rest_of<0>(v.x, a), rest_of<1>(v.y, a)}), h2_t);
+#pragma unroll
+                    for (int j = 0; j < 2; j++) {
+                        pf[0][t][i / 2][4 * (i & 1) + 2 * r + j] = a[j];
+                        pf[1][t][i / 2][4 * (i & 1) + 2 * r + j] = b[j];
+                    }
                 }
             }
     }
