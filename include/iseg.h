@@ -924,8 +924,8 @@ int iseg_kv4_attention(const void* q, const uint8_t* k_codes, const float* k_sca
  * accepted, from the remainder max(p_i - q_i, 0) of the first one refused (from
  * p_i where the remainder is 0 throughout): the smallest v whose cumulative sum
  * exceeds u_sample[b] times the whole.  draft NULL: each x_i was certain (q_i is
- * 1 at x_i).  The decisions are exact: products and sums in float64 of the given
- * probabilities.  out [B, S + 1] int32: the accepted drafts, the token taken,
+ * 1 at x_i).  Acceptance is exact for the given probabilities; sums are float64 in one
+ * fixed order.  out [B, S + 1] int32: the accepted drafts, the token taken,
  * then -1; accepted [B] int32.
  * target [B, S + 1, V] rows t_ld and requests t_bs elements apart, draft
  * [B, S, V] with d_ld, d_bs; both of dtype.  tokens, u [B, S] dense, tokens of

@@ -541,14 +541,16 @@ constexpr int ka_few_waves(int nc, int r, int dt)
 // ---------------------------------------------------------------------------
 // Bound by the cache's bytes, each read once: with G = 4 a tile of 16 rows is a quarter
 // full and its products cost less than the bytes.  A wave has one step of 32 keys in
-// hand and the next one under way, and three waves a SIMD (168 registers; four waves
-// would spill: 220 us) keep about 13 MB on their way.  64 requests of 8192 keys, 8
-// heads of 128: 571 MB in 114 us, 5.0 TB/s, the copy's rate.  Shorter work has the
-// blocks' beginnings and ends on top (queries, table and first keys one after the
-// other, then the join): 64 of 820 to 8192 keys, 315 MB, 84 us, of which the loads
-// alone take 72; 1 of 131072, 143 MB, 32 us, the loads 28.  Parts dealt by length
-// (prefix sums of all requests in every block) took 85 and 33, and 120 where all have
-// one length.  float32 tensors: 133 us at 64 x 8192; heads of 256, 32 x 8192: 137.
+// hand and the next one under way, and three waves a SIMD (139 registers; held to four
+// waves a call of 64 x 8192 keys takes 154 us, 124 with three) keep about 13 MB on
+// their way.  64 requests of 8192 keys, 8 heads of 128: 571 MB in 115 us, 5.0 TB/s, the
+// copy's rate.  Shorter work has the blocks' beginnings and ends on top (queries, table
+// and first keys one after the other, then the join): 64 of 820 to 8192 keys, 315 MB, 87
+// us, of which the loads alone take 72; 1 of 131072, 143 MB, 33 us, the loads 28.  Parts
+// dealt by length (prefix sums of all requests in every block) were no faster, and
+// slower where all have one length.  float32 tensors: 124 us at 64 x 8192; heads of 256,
+// 32 x 8192: 140.  Two and four tiles of rows hold 212 registers and all of them: 16 x
+// 8192 with 32 rows 61 us, 64 rows behind 131072 keys 127.
 //
 // NC: words of a row's quarter (W / 32).  R: tiles of 16 rows.
 template <int NC, int R, int DT>
@@ -675,15 +677,20 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(ka_few_wave
 // operands in LDS, once for all of them
 // ---------------------------------------------------------------------------
 // Bound by the sum of matrix and vector instructions: a 16x16x32 product takes 16
-// cycles of the matrix cores and 8 of the wave's issue, so two waves a SIMD hardly
-// overlap them.  3 x 3001 queries behind as many keys, 32 heads over 8 of 128: 870 to
-// 920 us for 663 GFLOP that are needed (720 to 760 TFLOP/s; the library's largest
-// products reach 1377).  Without products and softmax it takes 502 (loads, codes to
-// LDS, barriers), without its stages 78.  1 x 4096: 204 to 214 us; in float16 (two
-// terms of p) 243, in float32 (of q as well) 390 to 400; heads of 256 225.  R = 1 where a request has up to
-// 128 rows or a prompt is short (ka_cost).
-// Tried and slower: sixteen waves of 16 rows (1158), twelve waves (spills), 32x32x16
-// products with V's scale per stage (897 to 945), stages of 128 keys (896).
+// cycles of the matrix cores and 8 of the wave's issue, and a wave does a stage's scores,
+// softmax and V's products one after the other, so two waves a SIMD hardly overlap them.
+// 3 x 3001 queries behind as many keys, 32 heads over 8 of 128: 1160 to 1200 us for 663
+// GFLOP that are needed (550 to 570 TFLOP/s; the library's largest products reach 1377;
+// the weights' second term is half as many products again).  Matrix instructions take 400
+// of it, the issue of vector instructions 560, the exponentials 100 more.  With one part
+// left out: the softmax 760, the products 870, loads and codes to LDS 890.  Loads and
+// codes to LDS alone take 600 to 660: a stage's loads are requested one stage ahead and
+// wait for memory, which the arithmetic covers.  1 x 4096: 253; in float16 254, in float32
+// (two terms of q as well) 351; heads of 256 250.  R = 1 where a request has up to 128
+// rows or a prompt is short (ka_cost).
+// Tried with one term of the weights, which took 870 to 920, and slower: sixteen waves of
+// 16 rows (1158), twelve waves (spills), 32x32x16 products with V's scale per stage (897 to
+// 945), stages of 128 keys (896).
 constexpr int kWaves = 8;
 
 // a stage of 64 keys: operands of 1 KB each (64 lanes of 16 bytes), and scales
@@ -927,12 +934,15 @@ int64_t ka_max_kv(const iseg_kv4_attention_geom* g)
 
 int64_t ka_max_q(const iseg_kv4_attention_geom* g) { return g->max_q > 0 && g->max_q < g->T ? g->max_q : g->T; }
 
-// Time of n tiles (with all heads) in sp splits, in stages of 64 keys for 256 rows (2.9
+// Time of n tiles (with all heads) in sp splits, in stages of 64 keys for 256 rows (3.8
 // us): a block a CU at a time, each with three stages of beginning and end, the longest
-// first; with one tile of 16 rows a wave a stage takes 0.72 of that for 128 rows.  The
-// queries of a prompt see half of its own keys.  Splits write and read parts.  Without
-// it (256 rows always, splits for one round of blocks rounded up): 128 rows behind 131072
-// keys 261 us, 142 now; a prompt of 1000 100, 39 now; 100 tokens behind 99900 380, 281.
+// first.  With one tile of 16 rows a wave a stage is taken as 0.72 of that for 128 rows; it
+// is 0.55 where blocks follow one another (3 x 3001 in tiles of 128 1290 us, of 256 1180),
+// but whole rounds of blocks count more of them than there are.  The queries of a prompt
+// see half of its own keys.  Splits write and read parts.  Without it (256 rows always,
+// splits for one round of blocks rounded up): 128 rows behind 131072 keys 199 us, 148 now;
+// a prompt of 512 38, 27 now, of 1000 59, 44 now; 100 tokens behind 99900 332 both, 16 x 300
+// 93 both (90 in tiles of 128).
 double ka_cost(const iseg_kv4_attention_geom* g, int R, int64_t n, int sp, int64_t span)
 {
     const double stages = span / 64 + 1, own = g->causal ? (double)(ka_max_q(g) < span ? ka_max_q(g) : span) / 128 : 0.0;
@@ -954,9 +964,10 @@ KaPlan ka_plan(const iseg_kv4_attention_geom* g)
         const int64_t r = rows <= 16 * most ? rows : 16 * most;
         p.R = r <= 16 ? 1 : (r <= 32 ? 2 : 4);
         // Few pairs of request and head: as many blocks as are resident, all of one
-        // length (1 request of 131072 keys, 8 heads: 32 us at 96 splits, 36 at 128).  Many:
-        // two rounds of blocks, which even out requests of different lengths (64 of
-        // 820 to 8192 keys: 81 us against 86 in one).
+        // length (1 request of 131072 keys, 8 heads: a call 38 us at 96 splits, 43 at 128).
+        // Many: two rounds of blocks, which even out requests of different lengths (64
+        // of 820 to 8192 keys: 95 us against 98 in one; 64 x 8192 124 both; heads of 256, 32 x
+        // 8192, 140 against 129).
         const int64_t resident = 256 * ka_few_waves(nc, p.R, g->dtype);
         int64_t sp = 8 * pairs <= resident ? resident / pairs : ceil_div64(2 * resident, pairs), longest = ceil_div64(span, 256);
         sp = sp < longest ? sp : longest;

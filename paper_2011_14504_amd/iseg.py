@@ -2075,7 +2075,7 @@ def kv4_attention(q, cache, table, q_start, kv_len, scale=None, causal=True, win
     without want_lse).  A request's queries are its last tokens; causal: each sees
     no key after its own, window > 0: only that many up to its own.  max_q, max_kv:
     bounds of the requests' new and cached tokens, where the caller has them (0:
-    T and all of table).  scale: 1 / sqrt(D) without.  Rows of no request keep
+    T and all of table); a request of more than max_q is left out.  scale: 1 / sqrt(D) without.  Rows of no request keep
     what `out` holds; there lse is unspecified."""
     dt = _float_code(q, "q")
     q, q_ld, q_hs = _heads(q, "q")
